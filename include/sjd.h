@@ -59,10 +59,15 @@ extern "C" {
 #define SJD_ERR_BOUNDS 10        /* the bounds-checked build (libsjd_checked.so)
                                     found an index outside its array; the
                                     access was clamped, results are not valid  */
+#define SJD_ERR_PAGE 11          /* a span of tokens outside its page table, or a
+                                    page outside the cache (sjd_kv_*)           */
 
 /* Logit element types. */
 #define SJD_F32 0
 #define SJD_BF16 1
+/* Further element types of a cache (sjd_kv_config.kv_dtype). */
+#define SJD_E4M3 2               /* 8-bit floating point, 4 exponent bits        */
+#define SJD_S8 3                 /* signed 8-bit integers, -127..127             */
 
 /* sjd_draft modes. */
 #define SJD_DRAFT_PD 0           /* proactive drafting + window refill of the
@@ -380,6 +385,171 @@ const char* sjd_last_error(const sjd_ctx* ctx);
 
 /* Free the host handle (the workspace stays the caller's). */
 void sjd_destroy(sjd_ctx* ctx);
+
+/* ---------------------------------------------------------------------------
+ * Operators of the forward that makes the logits: rotary positions with
+ * several axes, a paged cache of keys and values that is quantised as it is
+ * written, and attention of a chunk of new tokens over it. A forward of the
+ * Jacobi window (sjd_forward_fn) calls them once per layer: sjd_kv_write
+ * puts the window's keys and values at its positions, over those of the
+ * step before, and sjd_kv_attend reads the cache with the window's queries.
+ * The chunk may as well be a prompt, the window followed by the nodes of the
+ * full drafting tree, or one token. Nothing here waits for the host: the
+ * sequences' positions are device arrays, so that a step needs no
+ * synchronisation and a captured call can be replayed as they move on.
+ *
+ * They have a handle of their own, sjd_kv, bound to a CUDA stream like
+ * sjd_ctx; calls are asynchronous on that stream and share the handle's
+ * workspace. The cache itself, one sjd_kv_layer per layer of the model, is
+ * passed to each call.
+ *
+ * Layouts. Cache: k_dev and v_dev [n_pages][kv_heads][page_size][head_dim]
+ * in kv_dtype, 16-byte aligned; with an 8-bit kv_dtype also k_scale_dev and v_scale_dev,
+ * fp32 [n_pages][kv_heads][page_size], one scale for each vector of
+ * head_dim codes. Token p of sequence b is in slot p % page_size of page
+ * table[b][p / page_size]. Entries of the table that no token of a call
+ * falls on are not read. Queries, keys and values are strided views
+ * (sjd_view), so that they may lie in one packed projection.
+ *
+ * Spans. A call is about tokens start[b] .. start[b] + count[b] - 1 of every
+ * sequence b, count[b] <= n (count_dev NULL: n of them in all sequences). A
+ * span that does not fit its sequence's table (max_pages * page_size tokens)
+ * is taken as empty, a page outside [0, n_pages) as zeros (reads) or not at
+ * all (writes), and SJD_ERR_PAGE is latched for sjd_kv_sync. */
+
+typedef struct {
+  int32_t batch;                 /* sequences: an image's conditional and
+                                    unconditional branches are two            */
+  int32_t heads;                 /* query heads, a multiple of kv_heads        */
+  int32_t kv_heads;              /* key and value heads; query head h reads
+                                    head h / (heads / kv_heads); heads /
+                                    kv_heads at most 128                       */
+  int32_t head_dim;              /* a multiple of 8, 8..128                    */
+  int32_t page_size;             /* tokens of a page, any number from 1 on     */
+  int32_t n_pages;               /* pages of the cache                         */
+  int32_t max_pages;             /* entries of one sequence's page table       */
+  int32_t max_new;               /* most new tokens of a sequence in a call    */
+  int32_t kv_dtype;              /* SJD_BF16, SJD_E4M3 or SJD_S8               */
+} sjd_kv_config;
+
+typedef struct sjd_kv sjd_kv;
+
+typedef struct {
+  void* k_dev;
+  void* v_dev;
+  float* k_scale_dev;            /* NULL with SJD_BF16                         */
+  float* v_scale_dev;
+} sjd_kv_layer;
+
+/* Element (b, t, h, i) of a [B][n][H][D] tensor is at data_dev + b *
+ * batch_stride + t * token_stride + h * head_stride + i, in elements. Reads
+ * and writes are widest when the data and the strides are 16-byte aligned. */
+typedef struct {
+  void* data_dev;
+  int64_t batch_stride, token_stride, head_stride;
+} sjd_view;
+
+typedef struct {
+  const int32_t* table_dev;      /* [batch][max_pages]                         */
+  const int32_t* start_dev;      /* [batch]                                    */
+  const int32_t* count_dev;      /* [batch], or NULL                           */
+  int32_t n;                     /* tokens of the call's tensors, 1..max_new   */
+} sjd_kv_span;
+
+/* Rotary positions with several axes (a running position, an image's row
+ * and column, ...): pair i of a vector is turned by the angle
+ * positions[axis_dev[i]] * f_i. The frequencies are given as fractions of a
+ * turn, turns_dev[i] = f_i / (2 pi) * 2^64 mod 2^64 (sjd_rope_turns), so
+ * that the angle is reduced exactly, in integers, at any position. The first
+ * 2 * pairs elements of a vector are turned and the others kept; pair i is
+ * elements 2i and 2i + 1 (interleaved) or i and pairs + i. */
+typedef struct {
+  const uint64_t* turns_dev;     /* [pairs]                                    */
+  const int32_t* axis_dev;       /* [pairs], each in [0, axes)                 */
+  int32_t pairs;                 /* a multiple of 4, at most head_dim / 2      */
+  int32_t axes;                  /* 1..8                                       */
+  int32_t interleaved;
+} sjd_rope;
+
+/* turns_host[i] = freq_host[i] / (2 pi) * 2^64 mod 2^64, freq in radians per
+ * position (host arrays). Errors: SJD_ERR_ARG (a frequency is not finite,
+ * or is 2^53 or more). */
+int sjd_rope_turns(const double* freq_host, int32_t n, uint64_t* turns_host);
+
+/* y = R(positions) x, or with inverse != 0 its transpose, which is both the
+ * inverse and the gradient: dL/dx = R^T dL/dy. x and y: [batch][n][heads]
+ * [dim] of dtype SJD_F32 or SJD_BF16 (fp32 inside), dim a multiple of 8 up
+ * to 256; y may be x, element for element, or apart from it. positions_dev:
+ * int32 [batch][n][axes], any value. Errors: SJD_ERR_ARG, SJD_ERR_CUDA. */
+int sjd_rotate(const sjd_rope* rope, const sjd_view* x, const sjd_view* y, const int32_t* positions_dev,
+               int32_t batch, int32_t n, int32_t heads, int32_t dim, int32_t dtype, int32_t inverse,
+               void* cuda_stream);
+
+/* Bytes of device workspace a handle needs (0: invalid configuration). */
+size_t sjd_kv_workspace_size(const sjd_kv_config* cfg);
+
+/* Check cfg and bind a handle to the caller's workspace (256-byte aligned,
+ * kept while the handle lives, not shared between handles) and stream.
+ * Errors: SJD_ERR_ARG, SJD_ERR_CAPACITY (workspace too small), SJD_ERR_CUDA. */
+int sjd_kv_init(const sjd_kv_config* cfg, void* workspace_dev, size_t ws_bytes, void* cuda_stream, sjd_kv** out);
+
+/* Write the spans' keys and values into the cache: k and v [batch][n]
+ * [kv_heads][head_dim] of dtype SJD_F32 or SJD_BF16. With an 8-bit cache
+ * each vector x is held as codes c and a scale s = max|x| / M (M = 448 for
+ * SJD_E4M3, 127 for SJD_S8), c = x / s rounded to nearest even, both in fp32
+ * arithmetic; a vector with a NaN or an infinity gets scale NaN and codes 0
+ * (all of it reads as NaN), a vector of zeros scale 0. With SJD_BF16 values
+ * are rounded to nearest even.
+ * rope (NULL: none) turns the keys first, in fp32, and, where q is given,
+ * also the queries q [batch][n][heads][head_dim] into q_out (same dtype; the
+ * rows from count[b] on are not written). positions_dev as for sjd_rotate.
+ * Errors: SJD_ERR_ARG, SJD_ERR_CUDA; SJD_ERR_PAGE via sjd_kv_sync. */
+int sjd_kv_write(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span, int32_t dtype,
+                 const sjd_view* k, const sjd_view* v, const sjd_rope* rope, const int32_t* positions_dev,
+                 const sjd_view* q, const sjd_view* q_out);
+
+/* Read the spans back: k_out_dev and v_out_dev [batch][n][kv_heads][head_dim],
+ * contiguous, of dtype SJD_F32 or SJD_BF16, codes times scale; zeros from
+ * count[b] on. Here n may be up to max_pages * page_size. Errors as
+ * sjd_kv_write. */
+int sjd_kv_read(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span, int32_t dtype,
+                void* k_out_dev, void* v_out_dev);
+
+/* sjd_kv_attend masks: which keys the chunk's token t sees, besides all
+ * tokens before start[b]. */
+#define SJD_MASK_CAUSAL 0        /* its own and those before it                 */
+#define SJD_MASK_ALL 1           /* the whole chunk                             */
+#define SJD_MASK_GIVEN 2         /* chunk token i where mask[b][t][i] != 0      */
+
+/* Attention of the spans' tokens, whose keys and values are in the cache
+ * already, over tokens 0 .. start[b] + count[b] - 1:
+ *   o = sum_j p_j v_j,  p = softmax_j(scale * q . k_j) over the keys seen,
+ *   lse = ln sum_j exp(scale * q . k_j).
+ * q [batch][n][heads][head_dim] in bf16, 16-byte aligned rows; o_dev
+ * [batch][n][heads][head_dim] in bf16, contiguous; lse_dev fp32 [batch][n]
+ * [heads], or NULL. Products are summed in fp32; the weights p are rounded
+ * to bf16 before their product with the values (an 8-bit value's scale goes
+ * into its weight first), their sum is not. A row that sees no key, and rows
+ * from count[b] on, give o = 0 and lse = -inf; a key that a row does not see
+ * has no effect on it, whatever it holds. The result does not depend on
+ * the GPU's timing: the same inputs give the same bits.
+ * mask_dev (SJD_MASK_GIVEN): bytes, element (b, t, i) at mask_batch_stride *
+ * b + mask_row_stride * t + i. Errors as sjd_kv_write, and SJD_ERR_TIMEOUT
+ * via sjd_kv_sync should a wait inside the kernel have run out (the results
+ * are then not valid). */
+int sjd_kv_attend(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span, const sjd_view* q,
+                  int32_t mask_kind, const uint8_t* mask_dev, int64_t mask_batch_stride, int64_t mask_row_stride,
+                  float scale, void* o_dev, float* lse_dev);
+
+/* Synchronise the handle's stream, then return and clear the first
+ * device-side error (SJD_OK if none). */
+int sjd_kv_sync(sjd_kv* kv);
+
+/* Text of the last error on this handle (never NULL). */
+const char* sjd_kv_last_error(const sjd_kv* kv);
+
+/* Free the host handle (workspace and cache stay the caller's). */
+void sjd_kv_destroy(sjd_kv* kv);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,81 @@
+// Shared by the window forward's operators: what a call gives the kernels
+// (sjd_rope.cu, sjd_kv.cu, sjd_attend.cu) and their launch entry points.
+#pragma once
+
+#include <cstdint>
+
+#include <cuda_runtime.h>
+
+#include "sjd.h"
+
+namespace sjd_kv_ops {
+
+constexpr int kMaxAxes = 8;
+constexpr int kMaxDim = 128;      // head size of a cache
+constexpr int kMaxRotateDim = 256;
+
+// Error bits of the handle's status word: bit (code - 1).
+__host__ __device__ constexpr uint32_t status_bit(int code) { return 1u << (code - 1); }
+
+struct View {
+  void* p;
+  long long sb, st, sh;  // strides of sequence, token and head, in elements
+};
+
+// The cache and the spans of one call.
+struct Cache {
+  int B, Hq, Hkv, D, ps, n_pages, max_pages;
+  void* k;
+  void* v;
+  float* ks;
+  float* vs;
+  const int32_t* table;
+  const int32_t* start;
+  const int32_t* count;
+  int n;
+  uint32_t* status;
+};
+
+struct Rope {
+  const uint64_t* turns;
+  const int32_t* axis;
+  const int32_t* positions;
+  int pairs, axes, interleaved, inverse;
+};
+
+struct RotateParams {
+  Rope rope;
+  View x, y;
+  int B, n, H, D;
+};
+
+struct WriteParams {
+  Cache c;
+  View k, v, q, q_out;  // q.p NULL: no queries
+  Rope rope;            // turns NULL: no rotation
+};
+
+struct ReadParams {
+  Cache c;
+  void* k_out;
+  void* v_out;
+};
+
+struct AttendParams {
+  Cache c;
+  View q;
+  int mask_kind;
+  const uint8_t* mask;
+  long long mask_b, mask_r;
+  float scale;
+  void* o;
+  float* lse;
+};
+
+// kv_dtype of the cache: SJD_BF16, SJD_E4M3, SJD_S8; dtype of the caller's tensors: SJD_F32, SJD_BF16.
+cudaError_t launch_rotate(const RotateParams& p, int dtype, cudaStream_t s);
+cudaError_t launch_write(const WriteParams& p, int dtype, int kv_dtype, cudaStream_t s);
+cudaError_t launch_read(const ReadParams& p, int dtype, int kv_dtype, cudaStream_t s);
+cudaError_t launch_attend(const AttendParams& p, int kv_dtype, cudaStream_t s);
+
+}  // namespace sjd_kv_ops

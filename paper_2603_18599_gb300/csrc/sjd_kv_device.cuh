@@ -1,0 +1,173 @@
+// Device helpers of the window forward's operators: spans and pages, elements
+// of the tensors' and the cache's types, rotary angles.
+#pragma once
+
+#include <cstdint>
+
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+
+#include "sjd_kv.h"
+
+namespace sjd_kv_ops {
+
+// Sequence b's span of the call, {0, 0} where it does not fit its table.
+__device__ __forceinline__ int2 span_of(const Cache& c, int b) {
+  const int start = c.start[b], count = c.count ? c.count[b] : c.n;
+  const long long room = static_cast<long long>(c.max_pages) * c.ps;
+  if (start < 0 || count < 0 || count > c.n || start + static_cast<long long>(count) > room) {
+    atomicOr(c.status, status_bit(SJD_ERR_PAGE));
+    return make_int2(0, 0);
+  }
+  return make_int2(start, count);
+}
+
+// Slot of token pos of sequence b for head 0, counted in vectors: head h's is
+// h * ps further. -1 where the table's entry is no page of the cache.
+__device__ __forceinline__ long long slot_of(const Cache& c, int b, int pos) {
+  const unsigned entry = static_cast<unsigned>(pos) / static_cast<unsigned>(c.ps);
+  const int page = c.table[static_cast<long long>(b) * c.max_pages + entry];
+  if (page < 0 || page >= c.n_pages) {
+    atomicOr(c.status, status_bit(SJD_ERR_PAGE));
+    return -1;
+  }
+  return static_cast<long long>(page) * c.Hkv * c.ps + (pos - static_cast<int>(entry) * c.ps);
+}
+
+// Four neighbouring elements as fp32, in one access where the address allows
+// it (`wide`).
+__device__ __forceinline__ void load4(const float* p, bool wide, float (&x)[4]) {
+  if (wide) {
+    const float4 v = *reinterpret_cast<const float4*>(p);
+    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = p[i];
+  }
+}
+__device__ __forceinline__ float2 unpack_bf16(uint32_t w) {
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void load4(const __nv_bfloat16* p, bool wide, float (&x)[4]) {
+  if (wide) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    const float2 a = unpack_bf16(v.x), b = unpack_bf16(v.y);
+    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __bfloat162float(p[i]);
+  }
+}
+__device__ __forceinline__ void store4(float* p, bool wide, const float (&x)[4]) {
+  if (wide) {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = x[i];
+  }
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, bool wide, const float (&x)[4]) {
+  if (wide) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = __float2bfloat16_rn(x[i]);
+  }
+}
+
+// Cosine and sine of pair i at a position. The product of a position and a
+// fraction of a turn in units of 2^-64, modulo 2^64, is the angle's fraction
+// of a turn: exact to 2^-64 turns for each position, so that no position is
+// too large. Its top 32 bits, as a signed fraction f of half turns in [-1,
+// 1), go to sincospi: the rounding to fp32 keeps 24 bits of f.
+__device__ __forceinline__ float2 turn_of(const Rope& r, const int32_t* positions, int i) {
+  const unsigned long long t = static_cast<unsigned long long>(static_cast<long long>(positions[r.axis[i]])) * r.turns[i];
+  const float f = static_cast<float>(static_cast<int32_t>(t >> 32)) * 4.656612873077393e-10f;  // 2^-31
+  float sn, cs;
+  sincospif(f, &sn, &cs);
+  return make_float2(cs, r.inverse ? -sn : sn);
+}
+
+// Where the two quads of a vector's 8-element chunk lie, and the pair its
+// rotation starts at (-1: it is not turned).
+struct Chunk {
+  int e0, e1, pair;
+};
+__device__ __forceinline__ Chunk chunk_at(int c, int pairs, int interleaved) {
+  if (4 * c >= pairs) return {8 * c, 8 * c + 4, -1};
+  if (interleaved) return {8 * c, 8 * c + 4, 4 * c};
+  return {4 * c, pairs + 4 * c, 4 * c};
+}
+
+// Turns the four pairs of a chunk.
+__device__ __forceinline__ void turn_chunk(float (&a)[4], float (&b)[4], const float2 (&cs)[4], int interleaved) {
+  if (interleaved) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float u = a[2 * i], w = b[2 * i];
+      a[2 * i] = u * cs[i].x - a[2 * i + 1] * cs[i].y;
+      a[2 * i + 1] = u * cs[i].y + a[2 * i + 1] * cs[i].x;
+      b[2 * i] = w * cs[2 + i].x - b[2 * i + 1] * cs[2 + i].y;
+      b[2 * i + 1] = w * cs[2 + i].y + b[2 * i + 1] * cs[2 + i].x;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float u = a[i];
+      a[i] = u * cs[i].x - b[i] * cs[i].y;
+      b[i] = u * cs[i].y + b[i] * cs[i].x;
+    }
+  }
+}
+
+template <int KV>
+struct Codes;  // one element of a cache of type KV
+template <>
+struct Codes<SJD_BF16> {
+  using type = __nv_bfloat16;
+};
+template <>
+struct Codes<SJD_E4M3> {
+  using type = uint8_t;
+  static constexpr float kMost = 448.0f;
+};
+template <>
+struct Codes<SJD_S8> {
+  using type = int8_t;
+  static constexpr float kMost = 127.0f;
+};
+
+// Four codes of the quotients y, in one word.
+template <int KV>
+__device__ __forceinline__ uint32_t codes4(const float (&y)[4]) {
+  if constexpr (KV == SJD_E4M3) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(y[0], y[1]), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(y[2], y[3]), __NV_SATFINITE, __NV_E4M3);
+    return lo | hi << 16;
+  } else {
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w |= static_cast<uint32_t>(max(-127, min(127, __float2int_rn(y[i]))) & 0xff) << 8 * i;
+    return w;
+  }
+}
+
+// The values of four codes in a word, fp32.
+template <int KV>
+__device__ __forceinline__ void values4(uint32_t w, float (&x)[4]) {
+  if constexpr (KV == SJD_E4M3) {
+    const __half2_raw lo = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w), __NV_E4M3);
+    const __half2_raw hi = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w >> 16), __NV_E4M3);
+    const float2 a = __half22float2(__half2(lo)), b = __half22float2(__half2(hi));
+    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = static_cast<float>(static_cast<int8_t>(w >> 8 * i));
+  }
+}
+
+}  // namespace sjd_kv_ops

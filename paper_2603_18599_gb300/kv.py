@@ -1,0 +1,333 @@
+"""Python binding of the window forward's operators (the sjd_rope, sjd_rotate
+and sjd_kv entry points of include/sjd.h): rotary positions with several
+axes, a paged cache of keys and values that is quantised as it is written,
+and attention of a chunk of new tokens over it. Argument marshalling only.
+
+    rope = kv.Rope.sections((16, 24, 24))               # time, row, column
+    cache = kv.KV(batch=2, heads=32, kv_heads=8, head_dim=128, n_pages=256, page_size=64,
+                  max_pages=64, max_new=16, dtype=torch.float8_e4m3fn)
+    layer = cache.new_layer()
+    q = cache.write(layer, k, v, table, start, rope=rope, positions=positions, q=q)
+    o = cache.attend(layer, q, table, start)
+
+Calls run on the handle's stream. Where that is not the caller's current
+stream, a call first waits for the current one, and the current one for the
+call, so that tensors may be made and used on either.
+"""
+
+import ctypes
+import math
+from ctypes import POINTER, byref, c_double, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
+
+import torch
+
+from . import sjd
+from .sjd import SJD_OK, SJDError
+
+_DTYPES = {torch.float32: sjd.SJD_F32, torch.bfloat16: sjd.SJD_BF16}
+_KV_DTYPES = {torch.bfloat16: sjd.SJD_BF16, torch.float8_e4m3fn: sjd.SJD_E4M3, torch.int8: sjd.SJD_S8}
+MASK_CAUSAL, MASK_ALL, MASK_GIVEN = 0, 1, 2
+
+
+class _config(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("batch", "heads", "kv_heads", "head_dim", "page_size", "n_pages", "max_pages",
+                                       "max_new", "kv_dtype")]
+
+
+class _layer(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class _view(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("batch_stride", c_int64), ("token_stride", c_int64), ("head_stride", c_int64)]
+
+
+class _span(ctypes.Structure):
+    _fields_ = [("table", c_void_p), ("start", c_void_p), ("count", c_void_p), ("n", c_int32)]
+
+
+class _rope(ctypes.Structure):
+    _fields_ = [("turns", c_void_p), ("axis", c_void_p), ("pairs", c_int32), ("axes", c_int32), ("interleaved", c_int32)]
+
+
+_lib = None
+
+
+def load():
+    global _lib
+    if _lib is not None:
+        return _lib
+    L = sjd.load()
+    P, I = c_void_p, c_int32
+    for name, args, res in (
+            ("sjd_rope_turns", [POINTER(c_double), I, POINTER(c_uint64)], I),
+            ("sjd_rotate", [P, P, P, P, I, I, I, I, I, I, P], I),
+            ("sjd_kv_workspace_size", [P], c_size_t),
+            ("sjd_kv_init", [P, P, c_size_t, P, POINTER(P)], I),
+            ("sjd_kv_write", [P, P, P, I, P, P, P, P, P, P], I),
+            ("sjd_kv_read", [P, P, P, I, P, P], I),
+            ("sjd_kv_attend", [P, P, P, P, I, P, c_int64, c_int64, c_float, P, P], I),
+            ("sjd_kv_sync", [P], I),
+            ("sjd_kv_last_error", [P], ctypes.c_char_p),
+            ("sjd_kv_destroy", [P], None)):
+        f = getattr(L, name)
+        f.argtypes, f.restype = args, res
+    _lib = L
+    return L
+
+
+def _device(device):
+    device = torch.device(device)
+    if device.type == "cuda" and device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    return device
+
+
+def _view_of(x, name, shape, dtype, device):
+    if x.shape != shape or x.dtype != dtype or x.device != device or x.stride(3) != 1:
+        raise ValueError("%s must be a %s tensor of shape %s on %s, its last dimension dense" % (name, dtype, tuple(shape), device))
+    s = x.stride()
+    return _view(x.data_ptr(), s[0], s[1], s[2])
+
+
+def _array(x, name, shape, device, dtype=torch.int32):
+    if x.shape != shape or x.dtype != dtype or x.device != device or not x.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, tuple(shape), device))
+    return x.data_ptr()
+
+
+class Rope:
+    """Rotary positions with several axes: pair i turns by positions[axis[i]]
+    * freq[i] (radians). Pairs are elements (i, i + pairs), or (2i, 2i + 1)
+    where interleaved; the elements after the pairs are kept."""
+
+    def __init__(self, freq, axis, interleaved=False, device="cuda"):
+        freq, axis = [float(f) for f in freq], [int(a) for a in axis]
+        if len(freq) != len(axis) or not freq or len(freq) % 4:
+            raise ValueError("freq and axis need a multiple of 4 entries each")
+        if min(axis) < 0 or max(axis) > 7:
+            raise ValueError("axes are numbered 0 to 7")
+        self.pairs, self.axes, self.interleaved = len(freq), max(axis) + 1, bool(interleaved)
+        turns = (c_uint64 * self.pairs)()
+        if load().sjd_rope_turns((c_double * self.pairs)(*freq), self.pairs, turns) != SJD_OK:
+            raise SJDError(sjd.SJD_ERR_ARG, "frequencies must be finite")
+        self.device = _device(device)
+        self._turns = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64, device=self.device)
+        self._axis = torch.tensor(axis, dtype=torch.int32, device=self.device)
+        self._c = _rope(self._turns.data_ptr(), self._axis.data_ptr(), self.pairs, self.axes, int(self.interleaved))
+        self._at = ctypes.addressof(self._c)
+
+    @classmethod
+    def sections(cls, pairs, theta=10000.0, shared=False, interleaved=False, device="cuda"):
+        """pairs[a] pairs for axis a. Each axis has its own frequencies
+        theta^(-i / pairs[a]), or with `shared` its section of one spectrum
+        theta^(-i / sum(pairs))."""
+        axis = [a for a, m in enumerate(pairs) for _ in range(m)]
+        if shared:
+            freq = [theta ** (-i / len(axis)) for i in range(len(axis))]
+        else:
+            freq = [theta ** (-i / m) for m in pairs for i in range(m)]
+        return cls(freq, axis, interleaved, device)
+
+    def rotate(self, x, positions, inverse=False, out=None):
+        """x [B, n, H, D] (bf16 or f32) turned by positions [B, n, axes]
+        int32; with `inverse` by the transpose, which takes the gradient of
+        the result to that of x. `out` may be x."""
+        if x.dim() != 4 or x.dtype not in _DTYPES or x.device != self.device:
+            raise ValueError("x must be a [B, n, H, D] bf16 or f32 tensor on %s" % (self.device,))
+        B, n, H, D = x.shape
+        at = _array(positions, "positions", (B, n, self.axes), self.device)
+        with torch.cuda.device(self.device):
+            if out is None:
+                out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            if x.numel() == 0:
+                return out
+            rc = load().sjd_rotate(self._at, byref(_view_of(x, "x", x.shape, x.dtype, x.device)),
+                                   byref(_view_of(out, "out", x.shape, x.dtype, x.device)), at, B, n, H, D, _DTYPES[x.dtype],
+                                   int(bool(inverse)), torch.cuda.current_stream(self.device).cuda_stream)
+        if rc != SJD_OK:
+            raise SJDError(rc, "sjd_rotate failed (dim a multiple of 8 up to 256, 2 * pairs at most dim)")
+        return out
+
+
+class Layer:
+    """One layer's cache: k, v [n_pages, kv_heads, page_size, head_dim] and,
+    of an 8-bit cache, k_scale, v_scale [n_pages, kv_heads, page_size] f32."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._for = None
+
+
+class KV:
+    """One handle: the sizes of a cache, the workspace and the stream that
+    the calls of all layers share. dtype: torch.bfloat16, torch.float8_e4m3fn
+    or torch.int8."""
+
+    def __init__(self, batch, heads, kv_heads, head_dim, n_pages, page_size, max_pages, max_new, dtype=torch.bfloat16,
+                 device="cuda", stream=None):
+        self.L = load()
+        self.ctx = c_void_p()
+        if dtype not in _KV_DTYPES:
+            raise ValueError("a cache holds bfloat16, float8_e4m3fn or int8")
+        self.cfg = _config(batch, heads, kv_heads, head_dim, page_size, n_pages, max_pages, max_new, _KV_DTYPES[dtype])
+        self.dtype = dtype
+        size = int(self.L.sjd_kv_workspace_size(byref(self.cfg)))
+        if size == 0:
+            raise SJDError(sjd.SJD_ERR_ARG, "invalid configuration")
+        self.device = _device(device)
+        self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
+            self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
+            rc = self.L.sjd_kv_init(byref(self.cfg), self.workspace.data_ptr(), size, self.stream.cuda_stream, byref(self.ctx))
+        if rc != SJD_OK:
+            self.ctx = c_void_p()
+            raise SJDError(rc, "sjd_kv_init failed")
+        c = self.cfg
+        self._shapes = ((c.n_pages, c.kv_heads, c.page_size, c.head_dim), (c.n_pages, c.kv_heads, c.page_size),
+                        (c.batch, c.max_pages), (c.batch,))
+
+    # -- helpers ------------------------------------------------------------
+    def _check(self, rc):
+        if rc != SJD_OK:
+            raise SJDError(rc, self.L.sjd_kv_last_error(self.ctx).decode())
+
+    def _layer_of(self, layer):
+        if layer._for is not self:
+            pages, scales = self._shapes[:2]
+            at = [_array(layer.k, "k", pages, self.device, self.dtype), _array(layer.v, "v", pages, self.device, self.dtype)]
+            if self.dtype != torch.bfloat16:
+                for name in ("k_scale", "v_scale"):
+                    if getattr(layer, name) is None:
+                        raise ValueError("an 8-bit cache needs k_scale and v_scale")
+                    at.append(_array(getattr(layer, name), name, scales, self.device, torch.float32))
+            else:
+                at += [None, None]
+            layer._c = _layer(*at)
+            layer._at = ctypes.addressof(layer._c)
+            layer._for = self
+        return layer._at
+
+    def _span(self, table, start, count, n):
+        return _span(_array(table, "table", self._shapes[2], self.device), _array(start, "start", self._shapes[3], self.device),
+                     None if count is None else _array(count, "count", self._shapes[3], self.device), n)
+
+    def _run(self, call, *tensors):
+        """call() with the handle's device current, ordered with the current
+        stream where that is another one. `tensors`: what the call uses."""
+        here = torch.cuda.current_stream(self.device)
+        if here == self.stream and torch.cuda.current_device() == self.device.index:
+            return call()
+        with torch.cuda.device(self.device):
+            if here == self.stream:
+                return call()
+            self.stream.wait_stream(here)
+            out = call()
+            here.wait_stream(self.stream)
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+            return out
+
+    # -- entry points ---------------------------------------------------------
+    def new_layer(self):
+        """A layer's cache, all zeros."""
+        pages, scales = self._shapes[:2]
+
+        def zeros(shape, dtype):
+            return torch.zeros(shape, dtype=dtype, device=self.device)
+
+        def held():
+            return zeros(pages, torch.uint8 if self.dtype == torch.float8_e4m3fn else self.dtype).view(self.dtype)
+
+        if self.dtype == torch.bfloat16:
+            return Layer(held(), held())
+        return Layer(held(), held(), zeros(scales, torch.float32), zeros(scales, torch.float32))
+
+    def write(self, layer, k, v, table, start, count=None, rope=None, positions=None, q=None, q_out=None):
+        """sjd_kv_write: k, v [B, n, kv_heads, D] (bf16 or f32) become tokens
+        start[b] .. start[b] + count[b] - 1 (count None: n) of the sequences
+        whose pages are table [B, max_pages]. With rope and positions [B, n,
+        axes] the keys are turned first, and q [B, n, heads, D], if given, is
+        turned into the result."""
+        c = self.cfg
+        B, n, dt = c.batch, k.shape[1], k.dtype
+        if dt not in _DTYPES:
+            raise ValueError("k must be bf16 or f32")
+        shape = (B, n, c.kv_heads, c.head_dim)
+        kw, vw = _view_of(k, "k", shape, dt, self.device), _view_of(v, "v", shape, dt, self.device)
+        at, span = self._layer_of(layer), self._span(table, start, count, n)
+        rope_at = pos = qw = ow = None
+        if rope is not None:
+            rope_at, pos = rope._at, _array(positions, "positions", (B, n, rope.axes), self.device)
+        if q is not None:
+            shape = (B, n, c.heads, c.head_dim)
+            if q_out is None:
+                q_out = torch.empty(shape, dtype=dt, device=self.device)
+            qw, ow = byref(_view_of(q, "q", shape, dt, self.device)), byref(_view_of(q_out, "q_out", shape, dt, self.device))
+        self._check(self._run(lambda: self.L.sjd_kv_write(self.ctx, at, byref(span), _DTYPES[dt], byref(kw), byref(vw), rope_at,
+                                                          pos, qw, ow),
+                              layer.k, layer.v, layer.k_scale, layer.v_scale, k, v, table, start, count, positions, q, q_out))
+        return q_out
+
+    def read(self, layer, table, start, n, count=None, dtype=torch.bfloat16):
+        """sjd_kv_read: (k, v) [B, n, kv_heads, D] of the spans, zeros from
+        count[b] on."""
+        c = self.cfg
+        if dtype not in _DTYPES:
+            raise ValueError("dtype must be bf16 or f32")
+        at, span = self._layer_of(layer), self._span(table, start, count, n)
+        shape = (c.batch, n, c.kv_heads, c.head_dim)
+        k, v = (torch.empty(shape, dtype=dtype, device=self.device) for _ in range(2))
+        self._check(self._run(lambda: self.L.sjd_kv_read(self.ctx, at, byref(span), _DTYPES[dtype], k.data_ptr(), v.data_ptr()),
+                              layer.k, layer.v, layer.k_scale, layer.v_scale, table, start, count, k, v))
+        return k, v
+
+    def attend(self, layer, q, table, start, count=None, mask="causal", scale=None, lse=False, out=None):
+        """sjd_kv_attend: q [B, n, heads, D] bf16, the chunk's keys and
+        values in the cache already. mask: "causal", None (the whole chunk is
+        seen) or a bool or uint8 tensor [B or 1, n, n] of what each chunk
+        token sees of the chunk. Returns o [B, n, heads, D], or (o, lse
+        [B, n, heads] f32)."""
+        c = self.cfg
+        B, n = c.batch, q.shape[1]
+        qw = _view_of(q, "q", (B, n, c.heads, c.head_dim), torch.bfloat16, self.device)
+        at, span = self._layer_of(layer), self._span(table, start, count, n)
+        kind, mask_at, mb, mr, given = MASK_CAUSAL, None, 0, 0, None
+        if mask is None:
+            kind = MASK_ALL
+        elif isinstance(mask, torch.Tensor):
+            kind, given = MASK_GIVEN, mask
+            if mask.dtype not in (torch.bool, torch.uint8) or mask.device != self.device or mask.dim() != 3 or \
+                    mask.shape[0] not in (1, B) or mask.shape[1:] != (n, n) or (mask.stride(2) != 1 and n > 1):
+                raise ValueError("mask must be a bool or uint8 tensor [%d or 1, %d, %d] on %s, its rows dense" % (B, n, n, self.device))
+            mask_at, mb, mr = mask.data_ptr(), mask.stride(0) if mask.shape[0] == B else 0, mask.stride(1)
+        elif mask != "causal":
+            raise ValueError("mask must be \"causal\", None or a tensor")
+        if out is None:
+            out = torch.empty((B, n, c.heads, c.head_dim), dtype=torch.bfloat16, device=self.device)
+        o_at = _array(out, "out", (B, n, c.heads, c.head_dim), self.device, torch.bfloat16)
+        sums = torch.empty((B, n, c.heads), dtype=torch.float32, device=self.device) if lse else None
+        scale = 1.0 / math.sqrt(c.head_dim) if scale is None else float(scale)
+        self._check(self._run(lambda: self.L.sjd_kv_attend(self.ctx, at, byref(span), byref(qw), kind, mask_at, mb, mr, scale, o_at,
+                                                           None if sums is None else sums.data_ptr()),
+                              layer.k, layer.v, layer.k_scale, layer.v_scale, q, table, start, count, given, out, sums))
+        return (out, sums) if lse else out
+
+    def sync(self):
+        """Returns the device-side status code (0 = OK) and clears it."""
+        return int(self.L.sjd_kv_sync(self.ctx))
+
+    def last_error(self):
+        return self.L.sjd_kv_last_error(self.ctx).decode()
+
+    def close(self):
+        if self.ctx:
+            self.L.sjd_kv_destroy(self.ctx)
+            self.ctx = c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

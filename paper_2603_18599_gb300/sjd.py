@@ -30,9 +30,12 @@ SJD_ERR_CALLBACK = 7
 SJD_ERR_STATE = 8
 SJD_ERR_TIMEOUT = 9
 SJD_ERR_BOUNDS = 10
+SJD_ERR_PAGE = 11
 
 SJD_F32 = 0
 SJD_BF16 = 1
+SJD_E4M3 = 2
+SJD_S8 = 3
 
 SJD_DRAFT_PD = 0
 SJD_DRAFT_FROM_LOGITS = 1
@@ -43,6 +46,7 @@ ERROR_NAMES = {
     SJD_ERR_NONFINITE: "SJD_ERR_NONFINITE", SJD_ERR_STEP_LIMIT: "SJD_ERR_STEP_LIMIT",
     SJD_ERR_INVALID_DRAFT: "SJD_ERR_INVALID_DRAFT", SJD_ERR_CALLBACK: "SJD_ERR_CALLBACK",
     SJD_ERR_STATE: "SJD_ERR_STATE", SJD_ERR_TIMEOUT: "SJD_ERR_TIMEOUT", SJD_ERR_BOUNDS: "SJD_ERR_BOUNDS",
+    SJD_ERR_PAGE: "SJD_ERR_PAGE",
 }
 
 
