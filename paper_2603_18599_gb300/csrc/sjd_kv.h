@@ -2,6 +2,7 @@
 // (sjd_rope.cu, sjd_kv.cu, sjd_attend.cu) and their launch entry points.
 #pragma once
 
+#include <cstddef>
 #include <cstdint>
 
 #include <cuda_runtime.h>
@@ -13,6 +14,7 @@ namespace sjd_kv_ops {
 constexpr int kMaxAxes = 8;
 constexpr int kMaxDim = 128;      // head size of a cache
 constexpr int kMaxRotateDim = 256;
+constexpr int kMaxAttendBlocks = 160;  // blocks of the attention kernel, one per SM
 
 // Error bits of the handle's status word: bit (code - 1).
 __host__ __device__ constexpr uint32_t status_bit(int code) { return 1u << (code - 1); }
@@ -76,6 +78,8 @@ struct AttendParams {
 cudaError_t launch_rotate(const RotateParams& p, int dtype, cudaStream_t s);
 cudaError_t launch_write(const WriteParams& p, int dtype, int kv_dtype, cudaStream_t s);
 cudaError_t launch_read(const ReadParams& p, int dtype, int kv_dtype, cudaStream_t s);
-cudaError_t launch_attend(const AttendParams& p, int kv_dtype, cudaStream_t s);
+// scratch: attend_scratch_bytes(head_dim, max_new * heads / kv_heads), 256-byte aligned.
+cudaError_t launch_attend(const AttendParams& p, int kv_dtype, int sms, unsigned char* scratch, cudaStream_t s);
+size_t attend_scratch_bytes(int head_dim, long long rows);
 
 }  // namespace sjd_kv_ops

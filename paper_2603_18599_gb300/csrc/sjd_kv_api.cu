@@ -11,8 +11,9 @@ using namespace sjd_kv_ops;
 
 struct sjd_kv {
   sjd_kv_config cfg;
-  unsigned char* ws;
+  unsigned char* ws;  // the status word, then the attention's scratch from kAlign on
   cudaStream_t stream;
+  int sms;
   char last_error[256];
 };
 
@@ -102,7 +103,10 @@ int sjd_rotate(const sjd_rope* rope, const sjd_view* x, const sjd_view* y, const
   return launch_rotate(p, dtype, static_cast<cudaStream_t>(stream)) == cudaSuccess ? SJD_OK : SJD_ERR_CUDA;
 }
 
-size_t sjd_kv_workspace_size(const sjd_kv_config* cfg) { return valid(cfg) ? kAlign : 0; }
+size_t sjd_kv_workspace_size(const sjd_kv_config* cfg) {
+  if (!valid(cfg)) return 0;
+  return kAlign + attend_scratch_bytes(cfg->head_dim, static_cast<long long>(cfg->max_new) * (cfg->heads / cfg->kv_heads));
+}
 
 int sjd_kv_init(const sjd_kv_config* cfg, void* workspace, size_t ws_bytes, void* stream, sjd_kv** out) {
   if (!out) return SJD_ERR_ARG;
@@ -110,8 +114,11 @@ int sjd_kv_init(const sjd_kv_config* cfg, void* workspace, size_t ws_bytes, void
   if (!valid(cfg) || !workspace || !aligned(workspace, kAlign)) return SJD_ERR_ARG;
   if (ws_bytes < sjd_kv_workspace_size(cfg)) return SJD_ERR_CAPACITY;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  int device = 0, sms = 0;
+  if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
+    return SJD_ERR_CUDA;
   if (cudaMemsetAsync(workspace, 0, kAlign, s) != cudaSuccess) return SJD_ERR_CUDA;
-  sjd_kv* kv = new (std::nothrow) sjd_kv{*cfg, static_cast<unsigned char*>(workspace), s, ""};
+  sjd_kv* kv = new (std::nothrow) sjd_kv{*cfg, static_cast<unsigned char*>(workspace), s, sms, ""};
   if (!kv) return SJD_ERR_CAPACITY;
   *out = kv;
   return SJD_OK;
@@ -176,7 +183,7 @@ int sjd_kv_attend(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span
   p.scale = scale;
   p.o = o;
   p.lse = lse;
-  return launched(kv, launch_attend(p, kv->cfg.kv_dtype, kv->stream), "attend");
+  return launched(kv, launch_attend(p, kv->cfg.kv_dtype, kv->sms, kv->ws + kAlign, kv->stream), "attend");
 }
 
 int sjd_kv_sync(sjd_kv* kv) {
