@@ -17,12 +17,12 @@
 // item that a cut went through is left as unnormalised parts with their
 // maxima and sums, which a second kernel joins in the order of the parts.
 //
-// A block has four kinds of warps. 0-3 and 4-7 take the softmax, each group a
+// A block has three kinds of warps. 0-3 and 4-7 take the softmax, each group a
 // slot: with NM = 1 the even and the odd tiles of the same 128 rows (each with
 // an accumulator of its own, joined at the end), with NM = 2 the two halves
-// of 256 rows. 8-11 load keys, 12-15 the queries and values, one thread of
-// warp 16 issues the products: those of one slot run while the other's
-// softmax does.
+// of 256 rows. One thread of each group issues the slot's products, which run
+// while the other slot's softmax does. 8-11 load keys, 12-15 the queries and
+// values.
 
 #include <cfloat>
 
@@ -34,8 +34,7 @@ namespace sjd_kv_ops {
 namespace {
 
 constexpr int kTile = 128;              // rows of a product, and keys of a tile
-constexpr int kAttendThreads = 17 * 32;
-constexpr int kMmaWarp = 16;
+constexpr int kAttendThreads = 16 * 32;
 constexpr uint32_t kTmemColumns = 512;  // S of the two slots (P over them), then O of the two
 constexpr uint32_t kOColumn = 2 * kTile;
 constexpr long long kWaitClocks = 4000000000ll;  // about two seconds
@@ -44,28 +43,31 @@ constexpr float kRise = 8.0f;           // a row's reference maximum moves when 
 __host__ __device__ constexpr uint32_t tile_bytes(int dp) { return static_cast<uint32_t>(kTile) * dp * 2; }
 
 // Shared memory: queries, rings of key and value tiles (1024-byte aligned),
-// then the small things.
-template <int DP, int NM>
+// for an 8-bit cache rings of the codes as they come, then the small things.
+template <int KV, int DP, int NM>
 struct Plan {
+  static constexpr bool kCodes = KV != SJD_BF16;
   static constexpr uint32_t kQ = NM * tile_bytes(DP);
-  static constexpr int kK = DP == 128 ? 3 : 5;                       // key tiles
-  static constexpr int kV = DP == 128 ? (NM == 1 ? 3 : 2) : 5;       // value tiles
-  static constexpr uint32_t kAtK = kQ, kAtV = kAtK + kK * tile_bytes(DP), kAtMisc = kAtV + kV * tile_bytes(DP);
+  static constexpr int kK = kCodes ? (DP == 128 ? 2 : 3) : (DP == 128 ? 3 : 5);                       // key tiles
+  static constexpr int kV = kCodes ? (DP == 128 ? 2 : 3) : (DP == 128 ? (NM == 1 ? 3 : 2) : 5);       // value tiles
+  static constexpr int kRaw = !kCodes ? 0 : DP == 64 ? 4 : NM == 1 ? 2 : 1;  // of keys, and of values
+  static constexpr uint32_t kAtK = kQ, kAtV = kAtK + kK * tile_bytes(DP), kAtRawK = kAtV + kV * tile_bytes(DP),
+                            kAtRawV = kAtRawK + kRaw * kTile * DP, kAtMisc = kAtRawV + kRaw * kTile * DP;
 };
 
 struct Misc {
-  unsigned long long k_full[5], k_empty[5], v_full[5], v_empty[5], q_full, q_empty, s_full[2], p_full[2], o_full;
+  unsigned long long k_full[5], k_empty[5], v_full[5], v_empty[5], q_full, q_empty, s_full[2], o_full;
   uint32_t tmem;
   int abort;
   int bad_values[4];       // number of the piece (modulo 4) in which a value that some rows do not see is not finite
   int first[4];            // the block's first item: key head, sequence, row tile, key tile
   long long first_tile, tiles;  // the block's part of all key tiles
-  float row[2][2][kTile];  // per slot: factors of the tile's keys and values; at the end the rows' maxima and sums
+  alignas(16) float row[2][2][kTile];  // per slot: factors of the tile's keys and values; at the end the rows' maxima and sums
 };
 
-template <int DP, int NM>
+template <int KV, int DP, int NM>
 constexpr uint32_t shared_bytes() {
-  return Plan<DP, NM>::kAtMisc + static_cast<uint32_t>(sizeof(Misc));
+  return Plan<KV, DP, NM>::kAtMisc + static_cast<uint32_t>(sizeof(Misc));
 }
 
 // What a block leaves for the joining kernel: the item of which it has the
@@ -246,11 +248,9 @@ __device__ __forceinline__ uint4 eight_values(uint2 w) {
 
 // --- loading --------------------------------------------------------------------
 
-// Slot (in vectors) of key `key` of the item's key head, -1 for none.
-__device__ __forceinline__ long long vector_at(const Cache& c, const Item& it, int key) {
-  if (key >= it.keys) return -1;
-  const long long s = slot_of(c, it.b, key);
-  return s < 0 ? -1 : s + static_cast<long long>(it.kvh) * c.ps;
+// The page of key `key` of the item's sequence.
+__device__ __forceinline__ int key_page(const Cache& c, const Item& it, int key) {
+  return key < it.keys ? page_of(c, it.b, key) : kNoPage;
 }
 
 // Queries of the item: rows of 16-byte pieces, zeros beyond.
@@ -291,38 +291,49 @@ __device__ __forceinline__ bool take_out(uint32_t& w) {
 
 // The four warps of one operand, keys (IS_V false) or values, go through the
 // block's tiles. A thread has the piece tid % (DP / 8) of every 128 / (DP /
-// 8)-th row; a lane finds the slot of row (warp * 32 + lane) of the next tile
-// while this one's copies run, and the others ask it by shuffles.
+// 8)-th row; a lane finds the vector of row (warp * 32 + lane) and the others
+// ask it by shuffles. The page of the next tile's row is loaded while this
+// tile's copies are issued.
 template <int KV, int DP, int NM, bool IS_V>
 __device__ __forceinline__ void load_operand(const AttendParams& p, Misc* m, uint32_t smem) {
-  using P = Plan<DP, NM>;
+  using P = Plan<KV, DP, NM>;
   using Code = typename Codes<KV>::type;
   constexpr int kPieces = DP / 8, kStep = 32 / kPieces, kRounds = 32 / kStep;  // rows of a warp at a time; rounds
-  constexpr int kStages = IS_V ? P::kV : P::kK, kLag = kStages - 1;
-  const int tid = threadIdx.x & 127, warp = tid / 32, lane = tid & 31, piece = lane % kPieces;
+  constexpr int kStages = IS_V ? P::kV : P::kK;
+  const int tid = threadIdx.x & 127, warp = tid / 32, lane = tid & 31, piece = lane % kPieces, first = lane / kPieces;
   const uint32_t ring = smem + (IS_V ? P::kAtV : P::kAtK);
   unsigned long long* full = IS_V ? m->v_full : m->k_full;
   unsigned long long* empty = IS_V ? m->v_empty : m->k_empty;
   const Code* data = static_cast<const Code*>(IS_V ? p.c.v : p.c.k);
-  const bool in = 8 * piece < p.c.D;
+  const uint32_t in = 8 * piece < p.c.D ? 8 * sizeof(Code) : 0;  // bytes of the thread's pieces
+  auto queries = [&](int number) {
+    wait(m, &m->q_empty, (number & 1) ^ 1);
+  };
+  auto queries_there = [&]() {
+    fence_async_shared();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_addr(&m->q_full));
+  };
   Walk<NM> w;
   if (!w.begin(p, m)) return;
   int stage = 0;              // of the tile being loaded
   uint32_t round = 1;         // parity of the empty barriers' phase before it
+  int page = key_page(p.c, w.it, w.k0 * kTile + tid);
   if constexpr (KV == SJD_BF16) {
-    int owed = 0, owed_stage = 0;             // tiles whose arrival has not been told yet, and the first one's stage
-    unsigned owed_mixed = 0;                  // of them, bit i: the i-th is to be looked over (take_out)
+    constexpr int kLag = kStages - 1;
+    int owed = 0, owed_stage = 0;  // tiles whose arrival has not been told yet, and the first one's stage
+    unsigned owed_mixed = 0;       // of them, bit i: the i-th is to be looked over (take_out)
     int owed_piece = 0;
     auto tell = [&]() {
       if constexpr (IS_V) {
         if (owed_mixed & 1) {
           bool bad = false;
+#pragma unroll 1
           for (int i = 0; i < kRounds; ++i) {
-            const int row = warp * 32 + i * kStep + lane / kPieces;
-            uint4* at = reinterpret_cast<uint4*>(__cvta_shared_to_generic(ring + owed_stage * tile_bytes(DP) + piece_at(row, piece)));
-            uint4 v = *at;
+            const uint32_t at = ring + owed_stage * tile_bytes(DP) + piece_at(warp * 32 + i * kStep + first, piece);
+            uint4 v = shared_load16(at);
             const bool a = take_out(v.x), b = take_out(v.y), c = take_out(v.z), d = take_out(v.w);
-            if (a || b || c || d) *at = v, bad = true;
+            if (a || b || c || d) shared_store16(at, v), bad = true;
           }
           if (bad) m->bad_values[owed_piece & 3] = owed_piece + 1;
         }
@@ -338,30 +349,34 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc* m, uin
       copy_wait<0>();
       while (owed > 0) tell();
     };
-    do {
-      long long mine = vector_at(p.c, w.it, w.k0 * kTile + warp * 32 + lane);
+    bool more = true;
+    while (more) {
       if constexpr (IS_V) {
         drain();
-        wait(m, &m->q_empty, (w.piece & 1) ^ 1);
+        queries(w.piece);
         load_queries<DP, NM>(p, w.it, smem, tid);
-        fence_async_shared();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_addr(&m->q_full));
+        queries_there();
         owed_piece = w.piece;
       }
-      const int common = IS_V ? common_keys<NM>(p, w.it) : 0;
-      for (int k = w.k0; k < w.k1; ++k) {
+      const int common = IS_V ? common_keys<NM>(p, w.it) : 0, k1 = w.k1;
+      for (int k = w.k0; k < k1; ++k) {
+        const uint32_t mine = vector_in(p.c, page, k * kTile + tid, w.it.kvh);
+        if (k + 1 < k1) {
+          page = key_page(p.c, w.it, (k + 1) * kTile + tid);
+        } else {
+          more = w.next(p);
+          if (more) page = key_page(p.c, w.it, w.k0 * kTile + tid);
+        }
         wait(m, &empty[stage], round);
         const uint32_t to = ring + stage * tile_bytes(DP);
 #pragma unroll
         for (int i = 0; i < kRounds; ++i) {
-          const int row = i * kStep + lane / kPieces;
-          const long long at = __shfl_sync(0xffffffffu, mine, row);
-          const bool here = at >= 0 && in;
-          copy16(to + piece_at(warp * 32 + row, piece), here ? data + at * p.c.D + 8 * piece : data, here ? 16 : 0);
+          const uint32_t at = __shfl_sync(0xffffffffu, mine, i * kStep + first);
+          const bool here = at != kNoVector;
+          copy16(to + piece_at(warp * 32 + i * kStep + first, piece),
+                 here ? data + static_cast<size_t>(at) * p.c.D + 8 * piece : data, here ? in : 0);
         }
         copy_commit();
-        if (k + 1 < w.k1) mine = vector_at(p.c, w.it, (k + 1) * kTile + warp * 32 + lane);
         if constexpr (IS_V) {
           if ((k + 1) * kTile > common) owed_mixed |= 1u << owed;
         }
@@ -372,107 +387,77 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc* m, uin
           tell();
         }
       }
-    } while (w.next(p));
+    }
     drain();
   } else {
-    // 8 codes to a thread and row, two tiles in registers: one on its way while
-    // the other is turned into bf16
-    uint2 now[kRounds], then[kRounds];
-    auto fetch = [&](uint2 (&to)[kRounds], const Item& it, int k) {
-      const long long mine = vector_at(p.c, it, k * kTile + warp * 32 + lane);
-#pragma unroll
-      for (int i = 0; i < kRounds; ++i) {
-        const long long at = __shfl_sync(0xffffffffu, mine, i * kStep + lane / kPieces);
-        to[i] = at >= 0 && in ? *reinterpret_cast<const uint2*>(data + at * p.c.D + 8 * piece) : make_uint2(0, 0);
-      }
-    };
-    fetch(now, w.it, w.k0);
-    bool more = true;
-    while (more) {
-      if constexpr (IS_V) {
-        wait(m, &m->q_empty, (w.piece & 1) ^ 1);
-        load_queries<DP, NM>(p, w.it, smem, tid);
-        fence_async_shared();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_addr(&m->q_full));
-      }
-      const int k1 = w.k1;
-      for (int k = w.k0; k < k1; ++k) {
-        if (k + 1 < k1) {
-          fetch(then, w.it, k + 1);
-        } else {
-          more = w.next(p);
-          if (more) fetch(then, w.it, w.k0);
-        }
-        wait(m, &empty[stage], round);
-        const uint32_t to = ring + stage * tile_bytes(DP);
+    // The codes come into a ring of their own, up to kRaw tiles ahead; each
+    // thread turns the pieces that it has asked for into bf16.
+    const uint32_t raw = smem + (IS_V ? P::kAtRawV : P::kAtRawK) + (warp * 32 + first) * DP + 8 * piece;
+    Walk<NM> a = w;           // the tile to be asked for
+    int ka = a.k0, slot = 0;
+    bool ahead = true;
+    auto ask = [&](int to) {
+      if (ahead) {
+        const uint32_t mine = vector_in(p.c, page, ka * kTile + tid, a.it.kvh);
 #pragma unroll
         for (int i = 0; i < kRounds; ++i) {
-          const int row = warp * 32 + i * kStep + lane / kPieces;
-          *reinterpret_cast<uint4*>(__cvta_shared_to_generic(to + piece_at(row, piece))) = eight_values<KV>(now[i]);
-          now[i] = then[i];
+          const uint32_t at = __shfl_sync(0xffffffffu, mine, i * kStep + first);
+          const bool here = at != kNoVector;
+          copy8(raw + to * (kTile * DP) + i * kStep * DP, here ? data + static_cast<size_t>(at) * p.c.D + 8 * piece : data, here ? in : 0);
         }
+        if (++ka == a.k1) {
+          ahead = a.next(p);
+          ka = a.k0;
+        }
+        if (ahead) page = key_page(p.c, a.it, ka * kTile + tid);
+      }
+      copy_commit();
+    };
+#pragma unroll 1
+    for (int i = 0; i < P::kRaw; ++i) ask(i);
+    do {
+      if constexpr (IS_V) {
+        queries(w.piece);
+        load_queries<DP, NM>(p, w.it, smem, tid);
+        queries_there();
+      }
+      for (int k = w.k0; k < w.k1; ++k) {
+        wait(m, &empty[stage], round);
+        copy_wait<P::kRaw - 1>();
+        const uint32_t to = ring + stage * tile_bytes(DP);
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i)
+          shared_store16(to + piece_at(warp * 32 + i * kStep + first, piece),
+                         eight_values<KV>(shared_load8(raw + slot * (kTile * DP) + i * kStep * DP)));
         fence_async_shared();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_addr(&full[stage]));
         if (++stage == kStages) stage = 0, round ^= 1;
+        ask(slot);
+        if (++slot == P::kRaw) slot = 0;
       }
-    }
+    } while (w.next(p));
   }
 }
 
 // --- products -------------------------------------------------------------------
 
-template <int DP, int NM>
-__device__ __forceinline__ void issue_products(const AttendParams& p, Misc* m, uint32_t smem, uint32_t tmem) {
-  using P = Plan<DP, NM>;
-  constexpr uint32_t kQK = product_kind(kTile, kTile, false), kPV = product_kind(kTile, DP, true);
-  Walk<NM> w;
-  if (!w.begin(p, m)) return;
-  int ks = 0, vs = 0;
-  uint32_t kp = 0, vp = 0, pp[2] = {0, 0};
-  do {
-    const int units = NM * (w.k1 - w.k0);  // of a slot and a tile, the slots in turn
-    auto scores = [&](int u) {
-      const int slot = u & 1;
-      if (NM == 1 || slot == 0) wait(m, &m->k_full[ks], kp);
-      tc_fence_after();
-      const uint32_t q = smem + (NM == 2 ? slot * tile_bytes(DP) : 0), k = smem + P::kAtK + ks * tile_bytes(DP);
+// S of a slot = Q K^T.
+template <int DP>
+__device__ __forceinline__ void issue_scores(uint32_t s, uint32_t q, uint32_t k) {
+  constexpr uint32_t kKind = product_kind(kTile, kTile, false);
 #pragma unroll
-      for (int i = 0; i < DP / 16; ++i) {
-        const uint32_t at = (i / 4) * (kTile * 128) + (i % 4) * 32;
-        mma_ss(tmem + slot * kTile, operand_k(q + at), operand_k(k + at), kQK, i > 0);
-      }
-      mma_commit(smem_addr(&m->s_full[slot]));
-      if (NM == 1 || slot == 1) {
-        mma_commit(smem_addr(&m->k_empty[ks]));
-        if (++ks == P::kK) ks = 0, kp ^= 1;
-      }
-      if (u + 1 == units) mma_commit(smem_addr(&m->q_empty));
-    };
-    wait(m, &m->q_full, w.piece & 1);
-    scores(0);
-    if (units > 1) scores(1);
-    for (int u = 0; u < units; ++u) {
-      const int slot = u & 1;
-      if (NM == 1 || slot == 0) wait(m, &m->v_full[vs], vp);
-      wait(m, &m->p_full[slot], pp[slot]);
-      pp[slot] ^= 1;
-      tc_fence_after();
-      const uint32_t v = smem + P::kAtV + vs * tile_bytes(DP);
+  for (int i = 0; i < DP / 16; ++i) {
+    const uint32_t at = (i / 4) * (kTile * 128) + (i % 4) * 32;
+    mma_ss(s, operand_k(q + at), operand_k(k + at), kKind, i > 0);
+  }
+}
+// O of a slot = P V, or += with `add`; P lies over S, two weights to a column.
+template <int DP>
+__device__ __forceinline__ void issue_values(uint32_t o, uint32_t s, uint32_t v, bool add) {
+  constexpr uint32_t kKind = product_kind(kTile, DP, true);
 #pragma unroll
-      for (int i = 0; i < kTile / 16; ++i)
-        mma_ts(tmem + kOColumn + slot * DP, tmem + slot * kTile + i * 8, operand_n(v + i * 2048, kTile * 128), kPV, u >= 2 || i > 0);
-      if (NM == 1 || slot == 1) {
-        mma_commit(smem_addr(&m->v_empty[vs]));
-        if (++vs == P::kV) vs = 0, vp ^= 1;
-      }
-      if (u + 2 < units) scores(u + 2);
-    }
-    mma_commit(smem_addr(&m->o_full));
-  } while (w.next(p));
-  // (the last commits' arrivals are waited for below, so that no product is in flight when the block ends)
-  wait(m, &m->o_full, w.piece & 1);
+  for (int i = 0; i < kTile / 16; ++i) mma_ts(o, s + i * 8, operand_n(v + i * 2048, kTile * 128), kKind, add || i > 0);
 }
 
 // --- softmax --------------------------------------------------------------------
@@ -485,9 +470,9 @@ __device__ __noinline__ void add_bad_values(const AttendParams& p, const Item& i
     for (int key = max(k0 * kTile, it.start); key < end; ++key) {
       const bool seen = p.mask_kind == SJD_MASK_CAUSAL ? key <= it.start + t
                                                        : p.mask[p.mask_b * it.b + p.mask_r * t + (key - it.start)] != 0;
-      const long long at = seen ? vector_at(p.c, it, key) : -1;
-      if (at < 0) continue;
-      const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.c.v) + at * p.c.D;
+      const uint32_t at = seen ? vector_in(p.c, key_page(p.c, it, key), key, it.kvh) : kNoVector;
+      if (at == kNoVector) continue;
+      const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.c.v) + static_cast<size_t>(at) * p.c.D;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         if (column + i >= p.c.D) break;
@@ -498,11 +483,83 @@ __device__ __noinline__ void add_bad_values(const AttendParams& p, const Item& i
   }
 }
 
+// One pass over a row's scores: the weights against `base`, packed, their sum,
+// and the largest score (times c). seen: the row's keys, where MIXED.
+template <int KV, bool MIXED>
+__device__ __forceinline__ float weights(uint32_t s_at, const float* factors_k, const float* factors_v, float c, float base,
+                                         const uint32_t (&seen)[4], uint32_t (&out)[64], float& total) {
+  const Pair c2 = pair(c, c), less = pair(-base, -base);
+  Pair sum[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+  float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < kTile / 16; ++i) {
+    uint32_t s[16];
+    tmem_load16(s_at + 16 * i, s);
+    tmem_wait_load(s);
+    const uint32_t bits = MIXED ? seen[i / 2] >> (16 * (i & 1)) : 0;
+#pragma unroll
+    for (int j = 0; j < 16; j += 4) {
+      float4 fk, fv;
+      if constexpr (KV != SJD_BF16) {
+        fk = *reinterpret_cast<const float4*>(factors_k + 16 * i + j);
+        fv = *reinterpret_cast<const float4*>(factors_v + 16 * i + j);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        float x = __uint_as_float(s[j + e]), y = __uint_as_float(s[j + e + 1]);
+        Pair t = pair(x, y);
+        if constexpr (KV != SJD_BF16) {
+          t = mul2(t, e ? pair(fk.z, fk.w) : pair(fk.x, fk.y));
+          const float2 u = halves(t);
+          x = u.x, y = u.y;
+        }
+        const bool sx = !MIXED || (bits >> (j + e) & 1), sy = !MIXED || (bits >> (j + e + 1) & 1);
+        if (MIXED) x = sx ? x : -INFINITY, y = sy ? y : -INFINITY;
+        top[e / 2] = fmaxf(top[e / 2], fmaxf(x, y));
+        const float2 d = halves(KV == SJD_BF16 ? fma2(t, c2, less) : add2(t, less));
+        x = exp2_fast(sx ? d.x : -INFINITY), y = exp2_fast(sy ? d.y : -INFINITY);
+        t = pair(x, y);
+        sum[e / 2] = add2(sum[e / 2], t);
+        if constexpr (KV != SJD_BF16) {
+          const float2 f = e ? make_float2(fv.z, fv.w) : make_float2(fv.x, fv.y);
+          const float2 v = halves(mul2(t, pair(sx ? f.x : 0.0f, sy ? f.y : 0.0f)));
+          x = v.x, y = v.y;
+        }
+        out[(16 * i + j + e) / 2] = pack_bf16(x, y);
+      }
+    }
+  }
+  const float2 a = halves(add2(sum[0], sum[1]));
+  total = a.x + a.y;
+  const float t = fmaxf(top[0], top[1]);
+  return KV == SJD_BF16 && t != -INFINITY ? t * c : t;
+}
+
+// The largest score alone.
+template <int KV>
+__device__ __forceinline__ float largest(uint32_t s_at, const float* factors_k, float c, const uint32_t (&seen)[4]) {
+  float top = -INFINITY;
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    uint32_t s[32];
+    tmem_load32(s_at + 32 * i, s);
+    tmem_wait_load(s);
+    const uint32_t bits = i == 0 ? seen[0] : i == 1 ? seen[1] : i == 2 ? seen[2] : seen[3];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const float x = __uint_as_float(s[j]) * (KV == SJD_BF16 ? 1.0f : factors_k[32 * i + j]);
+      top = fmaxf(top, bits >> j & 1 ? x : -INFINITY);
+    }
+  }
+  return KV == SJD_BF16 && top != -INFINITY ? top * c : top;
+}
+
 template <int KV, int DP, int NM>
-__device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc* m, uint32_t tmem, float* parts, float2* part_rows, Shared* shared) {
+__device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc* m, uint32_t smem, uint32_t tmem, float* parts, float2* part_rows, Shared* shared) {
+  using P = Plan<KV, DP, NM>;
   const int slot = threadIdx.x / 128, row = threadIdx.x & 127, warp_row = row & ~31;
   const uint32_t lanes = static_cast<uint32_t>(warp_row) << 16;
-  const uint32_t s_at = tmem + lanes + slot * kTile;
+  const uint32_t s_at = tmem + lanes + slot * kTile, o_at = tmem + lanes + kOColumn;
   const int G = p.c.Hq / p.c.Hkv;
   const float c = fabsf(p.scale) * 1.4426950408889634f;  // log2 e: weights are powers of two
   Walk<NM> w;
@@ -520,23 +577,50 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc* m, uin
     const int limit = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_CAUSAL ? it.start + t + 1 : it.keys;
     const int whole = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_GIVEN ? it.start : limit;
     float ref = -INFINITY, sum = 0.0f;
-    float next_k = 0.0f, next_v = 0.0f;
-    auto factors = [&](int k) {
-      if constexpr (KV != SJD_BF16) {
-        const long long at = vector_at(p.c, it, k * kTile + row);
-        next_k = at >= 0 ? p.c.ks[at] * c : 0.0f;
-        next_v = at >= 0 ? p.c.vs[at] : 0.0f;
-      }
+    // this slot's products; unit u is the block's tile `tile0` + u * stride
+    const int tile0 = static_cast<int>(at_tile - m->first_tile) + k_first - w.k0;
+    auto scores = [&](int u) {
+      const int tile = tile0 + u * stride, stage = tile % P::kK;
+      wait(m, &m->k_full[stage], tile / P::kK & 1);
+      tc_fence_after();
+      issue_scores<DP>(tmem + slot * kTile, smem + (NM == 2 ? slot * tile_bytes(DP) : 0), smem + P::kAtK + stage * tile_bytes(DP));
+      mma_commit(smem_addr(&m->s_full[slot]));
+      mma_commit(smem_addr(&m->k_empty[stage]));
+      if (u + 1 == units) mma_commit(smem_addr(&m->q_empty));
     };
-    if (units > 0) factors(k_first);
+    if (row == 0) {
+      if (units > 0) {
+        wait(m, &m->q_full, w.piece & 1);
+        scores(0);
+      } else {
+        mbar_arrive(smem_addr(&m->q_empty));
+        mbar_arrive(smem_addr(&m->o_full));
+      }
+    }
+    __syncwarp();
+    // an 8-bit cache's factors of key `row` of the tiles: the next tile's are on their way while
+    // one is worked on, and the page of the one after that
+    float next_k = 0.0f, next_v = 0.0f;
+    int page = kNoPage;
+    auto factors = [&](int u) {
+      const int key = (k_first + u * stride) * kTile + row;
+      const uint32_t at = vector_in(p.c, page, key, it.kvh);
+      next_k = next_v = 0.0f;
+      if (at != kNoVector) next_k = p.c.ks[at], next_v = p.c.vs[at];
+      page = u + 1 < units ? key_page(p.c, it, key + stride * kTile) : kNoPage;
+    };
+    if (KV != SJD_BF16 && units > 0) {
+      page = key_page(p.c, it, k_first * kTile + row);
+      factors(0);
+    }
+#pragma unroll 1
     for (int u = 0; u < units; ++u) {
       const int key0 = (k_first + u * stride) * kTile;
       if constexpr (KV != SJD_BF16) {
-        named_barrier(2 + slot, 128);
-        m->row[slot][0][row] = next_k;
+        m->row[slot][0][row] = next_k * c;
         m->row[slot][1][row] = next_v;
         named_barrier(2 + slot, 128);
-        if (u + 1 < units) factors(k_first + (u + 1) * stride);
+        if (u + 1 < units) factors(u + 1);
       }
       wait(m, &m->s_full[slot], sp);
       sp ^= 1;
@@ -555,82 +639,65 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc* m, uin
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int a = max(key0 + 32 * i, it.start), e = min(key0 + 32 * i + 32, it.keys);
+#pragma unroll 1
               for (int key = a; key < e; ++key)
                 if (!mask[key]) seen[i] &= ~(1u << (key - key0 - 32 * i));
             }
           }
         }
         __syncwarp();
-        // the largest score
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t s[32];
-          tmem_load32(s_at + 32 * i, s);
-          tmem_wait_load(s);
-          float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          if (mixed) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const float x = __uint_as_float(s[j]) * (KV == SJD_BF16 ? 1.0f : m->row[slot][0][32 * i + j]);
-              a[j & 3] = fmaxf(a[j & 3], seen[i] >> j & 1 ? x : -INFINITY);
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              a[j & 3] = fmaxf(a[j & 3], __uint_as_float(s[j]) * (KV == SJD_BF16 ? 1.0f : m->row[slot][0][32 * i + j]));
-          }
-          top = fmaxf(top, fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])));
+        const float* fk = m->row[slot][0];
+        const float* fv = m->row[slot][1];
+        // The reference that the weights are taken against moves only where a
+        // weight could pass 2^8 (their relative precision is the same below
+        // that): mostly one pass over the scores does. A row's first needs
+        // the largest score before.
+        bool moved = false;
+        float f = 1.0f;
+        if (__any_sync(0xffffffffu, ref == -INFINITY)) {
+          const float top = largest<KV>(s_at, fk, c, seen);
+          if (ref == -INFINITY) ref = top;
         }
-        if (KV == SJD_BF16 && top != -INFINITY) top *= c;
-        // The reference moves only where a weight could pass 2^8: the weights'
-        // relative precision is the same below that, and O is left alone.
-        const bool move = top > ref + kRise || (ref == -INFINITY && top != -INFINITY);
-        if (__any_sync(0xffffffffu, move)) {
-          const float f = !move ? 1.0f : ref == -INFINITY ? 0.0f : exp2_fast(ref - top);
-          if (move) ref = top, sum *= f;
+        uint32_t out[64];
+        float total, top;
+#pragma unroll 1
+        for (;;) {
+          const float base = ref == -INFINITY ? 0.0f : ref;
+          top = mixed ? weights<KV, true>(s_at, fk, fv, c, base, seen, out, total) : weights<KV, false>(s_at, fk, fv, c, base, seen, out, total);
+          const bool move = top > ref + kRise;
+          if (!__any_sync(0xffffffffu, move)) break;
+          if (move) f = exp2_fast(ref - top), ref = top, sum *= f;
+          moved = true;
           __syncwarp();
-          if (u > 0) {
-            for (int i = 0; i < DP / 32; ++i) {
-              uint32_t o[32];
-              tmem_load32(tmem + lanes + kOColumn + slot * DP + 32 * i, o);
-              tmem_wait_load(o);
+        }
+        sum += total;
+        if (moved && u > 0) {
+          // (the weights wait in their registers: 32 columns of O at a time would not fit beside them)
+#pragma unroll 1
+          for (int i = 0; i < DP / 16; ++i) {
+            uint32_t o[16];
+            tmem_load16(o_at + slot * DP + 16 * i, o);
+            tmem_wait_load(o);
 #pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tmem_store32(tmem + lanes + kOColumn + slot * DP + 32 * i, o);
-            }
+            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+            tmem_store16(o_at + slot * DP + 16 * i, o);
           }
         }
-        const float base = ref == -INFINITY ? 0.0f : ref;
-        float a[4] = {};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t s[32], out[16];
-          tmem_load32(s_at + 32 * i, s);
-          tmem_wait_load(s);
-#pragma unroll
-          for (int j = 0; j < 32; j += 2) {
-            float x[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              x[e] = exp2_fast(fmaf(__uint_as_float(s[j + e]), KV == SJD_BF16 ? c : m->row[slot][0][32 * i + j + e], -base));
-              if (mixed && !(seen[i] >> (j + e) & 1)) x[e] = 0.0f;
-              a[(j + e) & 3] += x[e];
-              if (KV != SJD_BF16) {
-                const float f = m->row[slot][1][32 * i + j + e];
-                x[e] = mixed && !(seen[i] >> (j + e) & 1) ? 0.0f : x[e] * f;
-              }
-            }
-            out[j / 2] = pack_bf16(x[0], x[1]);
-          }
-          tmem_store16(s_at + 16 * i, out);
-        }
-        sum += (a[0] + a[1]) + (a[2] + a[3]);
+        tmem_store64(s_at, out);
         tmem_wait_store();
         tc_fence_before();
       }
+      named_barrier(4 + slot, 128);  // all weights are there, and the factors were used
+      if (row == 0) {
+        const int tile = tile0 + u * stride, stage = tile % P::kV;
+        wait(m, &m->v_full[stage], tile / P::kV & 1);
+        tc_fence_after();
+        issue_values<DP>(o_at + slot * DP, tmem + slot * kTile, smem + P::kAtV + stage * tile_bytes(DP), u > 0);
+        mma_commit(smem_addr(&m->v_empty[stage]));
+        if (u + 1 < units) scores(u + 1);
+        else mma_commit(smem_addr(&m->o_full));
+      }
       __syncwarp();
-      if ((threadIdx.x & 31) == 0) mbar_arrive(smem_addr(&m->p_full[slot]));
     }
     // the end of the piece: O of both slots is complete
     wait(m, &m->o_full, w.piece & 1);
@@ -638,7 +705,6 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc* m, uin
     float f[2] = {1.0f, 1.0f};
     bool take[2] = {NM == 1 || slot == 0, NM == 1 ? tiles > 1 : slot == 1};
     if constexpr (NM == 1) {
-      named_barrier(2 + slot, 128);  // (all of the group are done with the factors)
       m->row[slot][0][row] = ref;
       m->row[slot][1][row] = sum;
       named_barrier(1, 256);
@@ -670,7 +736,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc* m, uin
         for (int e = 0; e < 2; ++e) {
           if (!take[e]) continue;
           uint32_t x[32];
-          tmem_load32(tmem + lanes + kOColumn + e * DP + column, x);
+          tmem_load32(o_at + e * DP + column, x);
           tmem_wait_load(x);
 #pragma unroll
           for (int j = 0; j < 32; ++j) o[j] = NM == 1 ? fmaf(__uint_as_float(x[j]), f[e], o[j]) : __uint_as_float(x[j]);
@@ -719,19 +785,19 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc* m, uin
 template <int KV, int DP, int NM>
 __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendParams p, float* parts, float2* part_rows, Shared* shared) {
   extern __shared__ __align__(1024) unsigned char raw[];
-  using P = Plan<DP, NM>;
+  using P = Plan<KV, DP, NM>;
   Misc* m = reinterpret_cast<Misc*>(raw + P::kAtMisc);
   const uint32_t smem = smem_addr(raw);
   const int warp = threadIdx.x / 32;
   if (warp == 0) locate<NM>(p, m);
-  if (warp == kMmaWarp) tmem_alloc(smem_addr(&m->tmem), kTmemColumns);
-  if (threadIdx.x == 128) {
+  if (warp == 4) tmem_alloc(smem_addr(&m->tmem), kTmemColumns);
+  if (threadIdx.x == 256) {
     for (int i = 0; i < 5; ++i) {
-      mbar_init(smem_addr(&m->k_full[i]), 4), mbar_init(smem_addr(&m->k_empty[i]), 1);
-      mbar_init(smem_addr(&m->v_full[i]), 4), mbar_init(smem_addr(&m->v_empty[i]), 1);
+      mbar_init(smem_addr(&m->k_full[i]), 4), mbar_init(smem_addr(&m->k_empty[i]), NM);
+      mbar_init(smem_addr(&m->v_full[i]), 4), mbar_init(smem_addr(&m->v_empty[i]), NM);
     }
-    mbar_init(smem_addr(&m->q_full), 4), mbar_init(smem_addr(&m->q_empty), 1), mbar_init(smem_addr(&m->o_full), 1);
-    for (int i = 0; i < 2; ++i) mbar_init(smem_addr(&m->s_full[i]), 1), mbar_init(smem_addr(&m->p_full[i]), 4);
+    mbar_init(smem_addr(&m->q_full), 4), mbar_init(smem_addr(&m->q_empty), 2), mbar_init(smem_addr(&m->o_full), 2);
+    for (int i = 0; i < 2; ++i) mbar_init(smem_addr(&m->s_full[i]), 1);
     m->abort = 0;
     for (int i = 0; i < 4; ++i) m->bad_values[i] = 0;
     shared[blockIdx.x].parts = 0;
@@ -741,19 +807,12 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = m->tmem;
-  if (warp < 8) {
-    softmax_rows<KV, DP, NM>(p, m, tmem, parts, part_rows, shared);
-  } else if (warp < 12) {
-    load_operand<KV, DP, NM, false>(p, m, smem);
-  } else if (warp < 16) {
-    load_operand<KV, DP, NM, true>(p, m, smem);
-  } else {
-    if ((threadIdx.x & 31) == 0) issue_products<DP, NM>(p, m, smem, tmem);
-    __syncwarp();
-  }
+  if (warp < 8) softmax_rows<KV, DP, NM>(p, m, smem, tmem, parts, part_rows, shared);
+  else if (warp < 12) load_operand<KV, DP, NM, false>(p, m, smem);
+  else load_operand<KV, DP, NM, true>(p, m, smem);
   tc_fence_before();
   __syncthreads();
-  if (warp == kMmaWarp) {
+  if (warp == 4) {
     tc_fence_after();
     tmem_free(tmem, kTmemColumns);
   }
@@ -824,9 +883,9 @@ cudaError_t launch(const AttendParams& p, int sms, unsigned char* scratch, cudaS
   float2* part_rows = reinterpret_cast<float2*>(scratch + kMaxAttendBlocks * sizeof(Shared));
   float* parts = reinterpret_cast<float*>(part_rows + rows);
   auto* kernel = attend_kernel<KV, DP, NM>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_bytes<DP, NM>());
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_bytes<KV, DP, NM>());
   if (e != cudaSuccess) return e;
-  kernel<<<blocks, kAttendThreads, shared_bytes<DP, NM>(), s>>>(p, parts, part_rows, shared);
+  kernel<<<blocks, kAttendThreads, shared_bytes<KV, DP, NM>(), s>>>(p, parts, part_rows, shared);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   join_kernel<DP><<<dim3(blocks, 8), 32 * kJoinWarps, 0, s>>>(p, parts, part_rows, shared, kTile * NM);

@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kBlock) write_kernel(const WriteParams p) {
   const int b = static_cast<int>(token / c.n), t = static_cast<int>(token % c.n);
   const int2 span = span_of(c, b);
   if (t >= span.y) return;
-  const long long slot = slot_of(c, b, span.x + t);
+  const uint32_t slot = vector_in(c, page_of(c, b, span.x + t), span.x + t, 0);  // head 0's
   const int L = lanes_of(c.D / 8), lane = threadIdx.x & (L - 1), groups = kBlock / L;
   const bool turned = p.rope.turns != nullptr, in = 8 * lane < c.D;
   const int n_q = p.q.p ? c.Hq : 0, n_vec = n_q + 2 * c.Hkv;
@@ -107,10 +107,10 @@ __global__ void __launch_bounds__(kBlock) write_kernel(const WriteParams p) {
       if constexpr (KV == SJD_BF16) continue;
     }
     using Code = typename Codes<KV>::type;
-    const long long at = slot + static_cast<long long>(h) * c.ps;
+    const long long at = slot + static_cast<uint32_t>(h * c.ps);
     Code* out = static_cast<Code*>(is_k ? c.k : c.v) + at * c.D;
     if constexpr (KV == SJD_BF16) {
-      if (here && slot >= 0) {
+      if (here && slot != kNoVector) {
         store4(out + ch.e0, true, u);
         store4(out + ch.e1, true, w);
       }
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(kBlock) write_kernel(const WriteParams p) {
         u[i] = some ? __fdiv_rn(u[i], scale) : 0.0f;
         w[i] = some ? __fdiv_rn(w[i], scale) : 0.0f;
       }
-      if (here && !is_q && slot >= 0) {
+      if (here && !is_q && slot != kNoVector) {
         *reinterpret_cast<uint32_t*>(out + ch.e0) = codes4<KV>(u);
         *reinterpret_cast<uint32_t*>(out + ch.e1) = codes4<KV>(w);
         if (lane == 0) (is_k ? c.ks : c.vs)[at] = top <= FLT_MAX ? scale : NAN;
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kBlock) read_kernel(const ReadParams p) {
   const long long token = blockIdx.x;
   const int b = static_cast<int>(token / c.n), t = static_cast<int>(token % c.n);
   const int2 span = span_of(c, b);
-  const long long slot = t < span.y ? slot_of(c, b, span.x + t) : -1;
+  const uint32_t slot = t < span.y ? vector_in(c, page_of(c, b, span.x + t), span.x + t, 0) : kNoVector;
   const int L = lanes_of(c.D / 8), lane = threadIdx.x & (L - 1), groups = kBlock / L;
   if (8 * lane >= c.D) return;
   using Code = typename Codes<KV>::type;
@@ -153,8 +153,8 @@ __global__ void __launch_bounds__(kBlock) read_kernel(const ReadParams p) {
     const bool is_k = vec < c.Hkv;
     const int h = is_k ? vec : vec - c.Hkv;
     float u[4] = {}, w[4] = {};
-    if (slot >= 0) {
-      const long long at = slot + static_cast<long long>(h) * c.ps;
+    if (slot != kNoVector) {
+      const long long at = slot + static_cast<uint32_t>(h * c.ps);
       const Code* x = static_cast<const Code*>(is_k ? c.k : c.v) + at * c.D + 8 * lane;
       if constexpr (KV == SJD_BF16) {
         load4(x, true, u);

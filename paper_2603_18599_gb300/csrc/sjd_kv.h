@@ -36,6 +36,8 @@ struct Cache {
   const int32_t* count;
   int n;
   uint32_t* status;
+  uint32_t ps_mul;  // key / ps = key * ps_mul >> (31 + ps_shift), key < 2^31
+  int ps_shift;
 };
 
 struct Rope {

@@ -26,6 +26,8 @@ bool valid(const sjd_kv_config* c) {
          c->heads / c->kv_heads <= 128 && c->head_dim >= 8 && c->head_dim <= kMaxDim && c->head_dim % 8 == 0 &&
          c->page_size >= 1 && c->n_pages >= 1 && c->max_pages >= 1 && c->max_new >= 1 &&
          static_cast<long long>(c->max_pages) * c->page_size <= 0x7fffffffLL &&
+         // (vectors are counted in 32 bits)
+         static_cast<double>(c->n_pages) * c->kv_heads * c->page_size < 4294967295.0 &&
          static_cast<long long>(c->batch) * c->max_new <= 0x7fffffffLL / 256 &&
          (c->kv_dtype == SJD_BF16 || c->kv_dtype == SJD_E4M3 || c->kv_dtype == SJD_S8);
 }
@@ -69,9 +71,13 @@ const char* cache_of(sjd_kv* kv, const sjd_kv_layer* l, const sjd_kv_span* s, lo
     return "layer: an 8-bit cache needs scales";
   if (!s->table_dev || !s->start_dev) return "span: table or start is NULL";
   if (s->n < 1 || s->n > most) return "span: n out of range";
+  // log = ceil(log2 ps), mul = ceil(2^(31 + log) / ps): the quotient is exact below 2^31
+  int log = 0;
+  while ((1ll << log) < g.page_size) ++log;
+  const uint32_t mul = static_cast<uint32_t>(((1ull << (31 + log)) + g.page_size - 1) / g.page_size);
   *c = {g.batch, g.heads, g.kv_heads, g.head_dim, g.page_size, g.n_pages, g.max_pages, l->k_dev, l->v_dev,
         scaled ? l->k_scale_dev : nullptr, scaled ? l->v_scale_dev : nullptr, s->table_dev, s->start_dev, s->count_dev,
-        s->n, reinterpret_cast<uint32_t*>(kv->ws)};
+        s->n, reinterpret_cast<uint32_t*>(kv->ws), mul, log};
   return nullptr;
 }
 

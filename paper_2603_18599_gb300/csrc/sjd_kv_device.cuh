@@ -22,16 +22,24 @@ __device__ __forceinline__ int2 span_of(const Cache& c, int b) {
   return make_int2(start, count);
 }
 
-// Slot of token pos of sequence b for head 0, counted in vectors: head h's is
-// h * ps further. -1 where the table's entry is no page of the cache.
-__device__ __forceinline__ long long slot_of(const Cache& c, int b, int pos) {
-  const unsigned entry = static_cast<unsigned>(pos) / static_cast<unsigned>(c.ps);
-  const int page = c.table[static_cast<long long>(b) * c.max_pages + entry];
-  if (page < 0 || page >= c.n_pages) {
-    atomicOr(c.status, status_bit(SJD_ERR_PAGE));
-    return -1;
+// Vectors (of head_dim elements) of the cache are counted in 32 bits.
+constexpr uint32_t kNoVector = 0xffffffffu;
+constexpr int kNoPage = -0x7fffffff - 1;  // a token that is not there
+
+// The table's entry of token pos of sequence b, as it stands there.
+__device__ __forceinline__ int entry_of(const Cache& c, int pos) {
+  return static_cast<int>(static_cast<unsigned long long>(static_cast<uint32_t>(pos)) * c.ps_mul >> (31 + c.ps_shift));
+}
+__device__ __forceinline__ int page_of(const Cache& c, int b, int pos) {
+  return c.table[static_cast<long long>(b) * c.max_pages + entry_of(c, pos)];
+}
+// Token pos's vector of head h, or none where the page is no page of the cache.
+__device__ __forceinline__ uint32_t vector_in(const Cache& c, int page, int pos, int h) {
+  if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(c.n_pages)) {
+    if (page != kNoPage) atomicOr(c.status, status_bit(SJD_ERR_PAGE));
+    return kNoVector;
   }
-  return static_cast<long long>(page) * c.Hkv * c.ps + (pos - static_cast<int>(entry) * c.ps);
+  return (static_cast<uint32_t>(page) * c.Hkv + h) * c.ps + (pos - entry_of(c, pos) * c.ps);
 }
 
 // Four neighbouring elements as fp32, in one access where the address allows
