@@ -55,41 +55,16 @@ struct Plan {
                             kAtRawV = kAtRawK + kRaw * kTile * DP, kAtMisc = kAtRawV + kRaw * kTile * DP;
 };
 
-struct Misc {
-  unsigned long long k_full[5], k_empty[5], v_full[5], v_empty[5], q_full, q_empty, s_full[2], o_full;
-  uint32_t tmem;
-  int abort;
-  int bad_values[4];       // number of the piece (modulo 4) in which a value that some rows do not see is not finite
-  int first[4];            // the block's first item: key head, sequence, row tile, key tile
-  long long first_tile, tiles;  // the block's part of all key tiles
-  alignas(16) float row[2][2][kTile];  // per slot: factors of the tile's keys and values; at the end the rows' maxima and sums
+struct Start {
+  int kvh, b, mt, k;     // the block's first item: key head, sequence, row tile, key tile
+  long long tile, tiles;  // the block's part of all key tiles
 };
-
-template <int KV, int DP, int NM>
-constexpr uint32_t shared_bytes() {
-  return Plan<KV, DP, NM>::kAtMisc + static_cast<uint32_t>(sizeof(Misc));
-}
 
 // What a block leaves for the joining kernel: the item of which it has the
 // first part, if other blocks have the rest.
 struct Shared {
   int parts, kvh, b, mt;
 };
-
-__device__ __forceinline__ void wait(Misc* m, unsigned long long* bar, uint32_t parity) {
-  const uint32_t at = smem_addr(bar);
-  if (mbar_try(at, parity)) return;
-  const long long begun = clock64();
-  while (!mbar_try(at, parity)) {
-    // once a wait has run out, none waits any more: the block goes on to its
-    // end over results that do not count
-    if (*const_cast<volatile int*>(&m->abort)) return;
-    if (clock64() - begun > kWaitClocks) {
-      *const_cast<volatile int*>(&m->abort) = 1;
-      return;
-    }
-  }
-}
 
 // An item's position and its keys.
 struct Item {
@@ -133,16 +108,16 @@ struct Walk {
   int k0, k1;
   int piece;          // number of the piece
 
-  __device__ __forceinline__ bool begin(const AttendParams& p, const Misc* m) {
-    left = m->tiles;
+  __device__ __forceinline__ bool begin(const AttendParams& p, const Start& s) {
+    left = s.tiles;
+    piece = 0;
     if (left <= 0) return false;
-    it.kvh = m->first[0], it.b = m->first[1], it.mt = m->first[2];
+    it.kvh = s.kvh, it.b = s.b, it.mt = s.mt;
     const int2 span = span_of(p.c, it.b);
     it.start = span.x, it.count = span.y;
     fill<NM>(p, it);
-    k0 = m->first[3];
+    k0 = s.k;
     k1 = static_cast<int>(min(static_cast<long long>(it.tiles), k0 + left));
-    piece = 0;
     return true;
   }
   __device__ __forceinline__ bool next(const AttendParams& p) {
@@ -167,9 +142,42 @@ struct Walk {
   }
 };
 
+template <int NM>
+struct Misc {
+  unsigned long long k_full[5], k_empty[5], v_full[5], v_empty[5], q_full, q_empty, s_full[2], o_full;
+  uint32_t tmem;
+  int abort;
+  int bad_values[4];       // number of the piece (modulo 4) in which a value that some rows do not see is not finite
+  Start start;
+  Walk<NM> walk[2];        // the softmax groups' ways
+  alignas(16) float row[2][2][kTile];  // per slot: factors of the tile's keys and values; at the end the rows' maxima and sums
+};
+
+template <int KV, int DP, int NM>
+constexpr uint32_t shared_bytes() {
+  static_assert(Plan<KV, DP, NM>::kAtMisc + sizeof(Misc<NM>) <= 227 * 1024, "shared memory");
+  return Plan<KV, DP, NM>::kAtMisc + static_cast<uint32_t>(sizeof(Misc<NM>));
+}
+
+template <int NM>
+__device__ __forceinline__ void wait(Misc<NM>* m, unsigned long long* bar, uint32_t parity) {
+  const uint32_t at = smem_addr(bar);
+  if (mbar_try(at, parity)) return;
+  const long long begun = clock64();
+  while (!mbar_try(at, parity)) {
+    // once a wait has run out, none waits any more: the block goes on to its
+    // end over results that do not count
+    if (*const_cast<volatile int*>(&m->abort)) return;
+    if (clock64() - begun > kWaitClocks) {
+      *const_cast<volatile int*>(&m->abort) = 1;
+      return;
+    }
+  }
+}
+
 // Where the block's part begins (warp 0).
 template <int NM>
-__device__ void locate(const AttendParams& p, Misc* m) {
+__device__ void locate(const AttendParams& p, Start* s) {
   const int lane = threadIdx.x & 31;
   long long per_head = 0;
   for (int b0 = 0; b0 < p.c.B; b0 += 32) {
@@ -179,7 +187,7 @@ __device__ void locate(const AttendParams& p, Misc* m) {
   }
   const long long all = per_head * p.c.Hkv, per = (all + gridDim.x - 1) / gridDim.x, from = blockIdx.x * per;
   const long long mine = max(0ll, min(per, all - from));
-  if (lane == 0) m->first_tile = from, m->tiles = mine;
+  if (lane == 0) s->tile = from, s->tiles = mine;
   if (mine == 0) return;
   const int kvh = static_cast<int>(from / per_head);
   long long rest = from % per_head;
@@ -198,7 +206,7 @@ __device__ void locate(const AttendParams& p, Misc* m) {
         const int2 span = span_of(p.c, b0 + at);
         int mt = 0, t;
         while (rest >= (t = (keys_of<NM>(p, span.x, span.y, mt) + kTile - 1) / kTile)) rest -= t, ++mt;
-        m->first[0] = kvh, m->first[1] = b0 + at, m->first[2] = mt, m->first[3] = static_cast<int>(rest);
+        s->kvh = kvh, s->b = b0 + at, s->mt = mt, s->k = static_cast<int>(rest);
       }
       return;
     }
@@ -295,7 +303,7 @@ __device__ __forceinline__ bool take_out(uint32_t& w) {
 // ask it by shuffles. The page of the next tile's row is loaded while this
 // tile's copies are issued.
 template <int KV, int DP, int NM, bool IS_V>
-__device__ __forceinline__ void load_operand(const AttendParams& p, Misc* m, uint32_t smem) {
+__device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m, uint32_t smem) {
   using P = Plan<KV, DP, NM>;
   using Code = typename Codes<KV>::type;
   constexpr int kPieces = DP / 8, kStep = 32 / kPieces, kRounds = 32 / kStep;  // rows of a warp at a time; rounds
@@ -315,7 +323,7 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc* m, uin
     if (lane == 0) mbar_arrive(smem_addr(&m->q_full));
   };
   Walk<NM> w;
-  if (!w.begin(p, m)) return;
+  if (!w.begin(p, m->start)) return;
   int stage = 0;              // of the tile being loaded
   uint32_t round = 1;         // parity of the empty barriers' phase before it
   int page = key_page(p.c, w.it, w.k0 * kTile + tid);
@@ -483,102 +491,111 @@ __device__ __noinline__ void add_bad_values(const AttendParams& p, const Item& i
   }
 }
 
-// One pass over a row's scores: the weights against `base`, packed, their sum,
-// and the largest score (times c). seen: the row's keys, where MIXED.
+// The largest score (times c) of a row. seen: its keys, where MIXED.
 template <int KV, bool MIXED>
-__device__ __forceinline__ float weights(uint32_t s_at, const float* factors_k, const float* factors_v, float c, float base,
-                                         const uint32_t (&seen)[4], uint32_t (&out)[64], float& total) {
-  const Pair c2 = pair(c, c), less = pair(-base, -base);
-  Pair sum[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+__device__ __forceinline__ float largest(uint32_t s_at, const float* factors, float c, const uint32_t (&seen)[4]) {
   float top[2] = {-INFINITY, -INFINITY};
+  uint32_t s[2][32];
+  tmem_load32(s_at, s[0]);
 #pragma unroll
-  for (int i = 0; i < kTile / 16; ++i) {
-    uint32_t s[16];
-    tmem_load16(s_at + 16 * i, s);
-    tmem_wait_load(s);
-    const uint32_t bits = MIXED ? seen[i / 2] >> (16 * (i & 1)) : 0;
+  for (int i = 0; i < 4; ++i) {
+    tmem_wait_load(s[i & 1]);
+    if (i < 3) tmem_load32(s_at + 32 * (i + 1), s[(i + 1) & 1]);
 #pragma unroll
-    for (int j = 0; j < 16; j += 4) {
-      float4 fk, fv;
+    for (int j = 0; j < 32; j += 4) {
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(s[i & 1][j + e]);
       if constexpr (KV != SJD_BF16) {
-        fk = *reinterpret_cast<const float4*>(factors_k + 16 * i + j);
-        fv = *reinterpret_cast<const float4*>(factors_v + 16 * i + j);
+        const float4 f = *reinterpret_cast<const float4*>(factors + 32 * i + j);
+        const float2 u = halves(mul2(pair(x[0], x[1]), pair(f.x, f.y))), v = halves(mul2(pair(x[2], x[3]), pair(f.z, f.w)));
+        x[0] = u.x, x[1] = u.y, x[2] = v.x, x[3] = v.y;
       }
+      if constexpr (MIXED) {
 #pragma unroll
-      for (int e = 0; e < 4; e += 2) {
-        float x = __uint_as_float(s[j + e]), y = __uint_as_float(s[j + e + 1]);
-        Pair t = pair(x, y);
-        if constexpr (KV != SJD_BF16) {
-          t = mul2(t, e ? pair(fk.z, fk.w) : pair(fk.x, fk.y));
-          const float2 u = halves(t);
-          x = u.x, y = u.y;
-        }
-        const bool sx = !MIXED || (bits >> (j + e) & 1), sy = !MIXED || (bits >> (j + e + 1) & 1);
-        if (MIXED) x = sx ? x : -INFINITY, y = sy ? y : -INFINITY;
-        top[e / 2] = fmaxf(top[e / 2], fmaxf(x, y));
-        const float2 d = halves(KV == SJD_BF16 ? fma2(t, c2, less) : add2(t, less));
-        x = exp2_fast(sx ? d.x : -INFINITY), y = exp2_fast(sy ? d.y : -INFINITY);
-        t = pair(x, y);
-        sum[e / 2] = add2(sum[e / 2], t);
-        if constexpr (KV != SJD_BF16) {
-          const float2 f = e ? make_float2(fv.z, fv.w) : make_float2(fv.x, fv.y);
-          const float2 v = halves(mul2(t, pair(sx ? f.x : 0.0f, sy ? f.y : 0.0f)));
-          x = v.x, y = v.y;
-        }
-        out[(16 * i + j + e) / 2] = pack_bf16(x, y);
+        for (int e = 0; e < 4; ++e) x[e] = seen[i] >> (j + e) & 1 ? x[e] : -INFINITY;
       }
+      top[0] = max3(top[0], x[0], x[1]);
+      top[1] = max3(top[1], x[2], x[3]);
     }
   }
-  const float2 a = halves(add2(sum[0], sum[1]));
-  total = a.x + a.y;
   const float t = fmaxf(top[0], top[1]);
   return KV == SJD_BF16 && t != -INFINITY ? t * c : t;
 }
 
-// The largest score alone.
-template <int KV>
-__device__ __forceinline__ float largest(uint32_t s_at, const float* factors_k, float c, const uint32_t (&seen)[4]) {
-  float top = -INFINITY;
-#pragma unroll 1
-  for (int i = 0; i < 4; ++i) {
-    uint32_t s[32];
-    tmem_load32(s_at + 32 * i, s);
-    tmem_wait_load(s);
-    const uint32_t bits = i == 0 ? seen[0] : i == 1 ? seen[1] : i == 2 ? seen[2] : seen[3];
+// A row's weights against `base`, written over the scores as bf16 (32 scores
+// are in registers before the first 16 columns of weights are written, and
+// the weights stay behind the scores), and their sum.
+template <int KV, bool MIXED>
+__device__ __forceinline__ float weights(uint32_t s_at, const float* factors_k, const float* factors_v, float c, float base,
+                                         const uint32_t (&seen)[4]) {
+  const Pair c2 = pair(c, c), less = pair(-base, -base);
+  Pair sum[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+  uint32_t s[2][32];
+  tmem_load32(s_at, s[0]);
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      const float x = __uint_as_float(s[j]) * (KV == SJD_BF16 ? 1.0f : factors_k[32 * i + j]);
-      top = fmaxf(top, bits >> j & 1 ? x : -INFINITY);
+  for (int i = 0; i < 4; ++i) {
+    uint32_t out[16];
+    tmem_wait_load(s[i & 1]);
+    if (i < 3) tmem_load32(s_at + 32 * (i + 1), s[(i + 1) & 1]);
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+      float4 fk, fv;
+      if constexpr (KV != SJD_BF16) {
+        fk = *reinterpret_cast<const float4*>(factors_k + 32 * i + j);
+        fv = *reinterpret_cast<const float4*>(factors_v + 32 * i + j);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        const Pair t = pair(__uint_as_float(s[i & 1][j + e]), __uint_as_float(s[i & 1][j + e + 1]));
+        const bool sx = !MIXED || (seen[i] >> (j + e) & 1), sy = !MIXED || (seen[i] >> (j + e + 1) & 1);
+        const float2 d = halves(fma2(t, KV == SJD_BF16 ? c2 : e ? pair(fk.z, fk.w) : pair(fk.x, fk.y), less));
+        float x = exp2_fast(sx ? d.x : -INFINITY), y = exp2_fast(sy ? d.y : -INFINITY);
+        const Pair w = pair(x, y);
+        sum[e / 2] = add2(sum[e / 2], w);
+        if constexpr (KV != SJD_BF16) {
+          const float2 f = e ? make_float2(fv.z, fv.w) : make_float2(fv.x, fv.y);
+          const float2 v = halves(mul2(w, pair(sx ? f.x : 0.0f, sy ? f.y : 0.0f)));
+          x = v.x, y = v.y;
+        }
+        out[(j + e) / 2] = pack_bf16(x, y);
+      }
     }
+    tmem_store16(s_at + 16 * i, out);
   }
-  return KV == SJD_BF16 && top != -INFINITY ? top * c : top;
+  const float2 a = halves(add2(sum[0], sum[1]));
+  return a.x + a.y;
 }
 
 template <int KV, int DP, int NM>
-__device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc* m, uint32_t smem, uint32_t tmem, float* parts, float2* part_rows, Shared* shared) {
+__device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m, uint32_t smem, uint32_t tmem, float* parts, float2* part_rows, Shared* shared) {
   using P = Plan<KV, DP, NM>;
   const int slot = threadIdx.x / 128, row = threadIdx.x & 127, warp_row = row & ~31;
   const uint32_t lanes = static_cast<uint32_t>(warp_row) << 16;
   const uint32_t s_at = tmem + lanes + slot * kTile, o_at = tmem + lanes + kOColumn;
   const int G = p.c.Hq / p.c.Hkv;
   const float c = fabsf(p.scale) * 1.4426950408889634f;  // log2 e: weights are powers of two
-  Walk<NM> w;
-  if (!w.begin(p, m)) return;
-  long long at_tile = m->first_tile;  // number, among all, of the piece's first tile
+  // (the group's way is kept in shared memory: its registers are for the scores)
+  Walk<NM>& w = m->walk[slot];
+  const Item& it = w.it;
+  if (m->start.tiles <= 0) return;
+  if (row == 0) w.begin(p, m->start);
+  named_barrier(2 + slot, 128);
+  int tile_no = 0;  // the block's number of the piece's first tile
   uint32_t sp = 0;
-  do {
-    const Item& it = w.it;
-    const int r0 = it.mt * (kTile * NM) + (NM == 2 ? slot * kTile : 0), r = r0 + row;
-    const bool valid = r < it.rows, active = r0 + warp_row < it.rows;
-    const int t = r / G, g = r - t * G;
-    const int tiles = w.k1 - w.k0, units = NM == 2 ? tiles : (tiles + 1 - slot) / 2, stride = NM == 2 ? 1 : 2;
+  for (;;) {
+    const int r0 = it.mt * (kTile * NM) + (NM == 2 ? slot * kTile : 0);
+    const bool valid = r0 + row < it.rows, active = r0 + warp_row < it.rows;
+    const int t = (r0 + row) / G;
+    const int units = NM == 2 ? w.k1 - w.k0 : (w.k1 - w.k0 + 1 - slot) / 2;
+    constexpr int stride = NM == 2 ? 1 : 2;
     const int k_first = w.k0 + (NM == 2 ? 0 : slot);
     // keys below `whole` are seen, those from `limit` on are not (a given mask tells between)
     const int limit = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_CAUSAL ? it.start + t + 1 : it.keys;
     const int whole = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_GIVEN ? it.start : limit;
     float ref = -INFINITY, sum = 0.0f;
     // this slot's products; unit u is the block's tile `tile0` + u * stride
-    const int tile0 = static_cast<int>(at_tile - m->first_tile) + k_first - w.k0;
+    const int tile0 = tile_no + (NM == 2 ? 0 : slot);
     auto scores = [&](int u) {
       const int tile = tile0 + u * stride, stage = tile % P::kK;
       wait(m, &m->k_full[stage], tile / P::kK & 1);
@@ -649,41 +666,28 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc* m, uin
         const float* fk = m->row[slot][0];
         const float* fv = m->row[slot][1];
         // The reference that the weights are taken against moves only where a
-        // weight could pass 2^8 (their relative precision is the same below
-        // that): mostly one pass over the scores does. A row's first needs
-        // the largest score before.
-        bool moved = false;
-        float f = 1.0f;
-        if (__any_sync(0xffffffffu, ref == -INFINITY)) {
-          const float top = largest<KV>(s_at, fk, c, seen);
-          if (ref == -INFINITY) ref = top;
-        }
-        uint32_t out[64];
-        float total, top;
-#pragma unroll 1
-        for (;;) {
-          const float base = ref == -INFINITY ? 0.0f : ref;
-          top = mixed ? weights<KV, true>(s_at, fk, fv, c, base, seen, out, total) : weights<KV, false>(s_at, fk, fv, c, base, seen, out, total);
-          const bool move = top > ref + kRise;
-          if (!__any_sync(0xffffffffu, move)) break;
-          if (move) f = exp2_fast(ref - top), ref = top, sum *= f;
-          moved = true;
+        // weight could pass 2^8: their relative precision is the same below
+        // that, and O is left alone.
+        const float top = mixed ? largest<KV, true>(s_at, fk, c, seen) : largest<KV, false>(s_at, fk, c, seen);
+        const bool move = top > ref + kRise || (ref == -INFINITY && top != -INFINITY);
+        if (__any_sync(0xffffffffu, move)) {
+          const float f = !move ? 1.0f : ref == -INFINITY ? 0.0f : exp2_fast(ref - top);
+          if (move) ref = top, sum *= f;
           __syncwarp();
-        }
-        sum += total;
-        if (moved && u > 0) {
-          // (the weights wait in their registers: 32 columns of O at a time would not fit beside them)
+          if (u > 0) {
 #pragma unroll 1
-          for (int i = 0; i < DP / 16; ++i) {
-            uint32_t o[16];
-            tmem_load16(o_at + slot * DP + 16 * i, o);
-            tmem_wait_load(o);
+            for (int i = 0; i < DP / 32; ++i) {
+              uint32_t o[32];
+              tmem_load32(o_at + slot * DP + 32 * i, o);
+              tmem_wait_load(o);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-            tmem_store16(o_at + slot * DP + 16 * i, o);
+              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_store32(o_at + slot * DP + 32 * i, o);
+            }
           }
         }
-        tmem_store64(s_at, out);
+        const float base = ref == -INFINITY ? 0.0f : ref;
+        sum += mixed ? weights<KV, true>(s_at, fk, fv, c, base, seen) : weights<KV, false>(s_at, fk, fv, c, base, seen);
         tmem_wait_store();
         tc_fence_before();
       }
@@ -703,7 +707,8 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc* m, uin
     wait(m, &m->o_full, w.piece & 1);
     tc_fence_after();
     float f[2] = {1.0f, 1.0f};
-    bool take[2] = {NM == 1 || slot == 0, NM == 1 ? tiles > 1 : slot == 1};
+    const int tiles = w.k1 - w.k0;
+    const bool take[2] = {NM == 1 || slot == 0, NM == 1 ? tiles > 1 : slot == 1};
     if constexpr (NM == 1) {
       m->row[slot][0][row] = ref;
       m->row[slot][1][row] = sum;
@@ -723,6 +728,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc* m, uin
     const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     const long long part = 2ll * blockIdx.x + (w.k0 == 0 ? 1 : 0);
     const long long token = static_cast<long long>(it.b) * p.c.n + t;
+    const int g = r0 + row - t * G;
     const long long head = token * p.c.Hq + static_cast<long long>(it.kvh) * G + g;
     if (active) {
 #pragma unroll
@@ -771,25 +777,30 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc* m, uin
     }
     if (threadIdx.x == 0 && w.k0 == 0 && w.k1 < it.tiles) {
       // the rest of the item lies in the blocks after this one
-      const long long per = m->tiles, beyond = at_tile + it.tiles - 1;
-      shared[blockIdx.x] = {static_cast<int>(beyond / per - blockIdx.x + 1), it.kvh, it.b, it.mt};
+      const long long beyond = m->start.tile + tile_no + it.tiles - 1;
+      shared[blockIdx.x] = {static_cast<int>(beyond / m->start.tiles - blockIdx.x + 1), it.kvh, it.b, it.mt};
     }
-    if constexpr (NM == 1) {
+    tile_no += tiles;
+    if (NM == 1) {  // both groups have read both accumulators and the rows' sums
       tc_fence_before();
-      named_barrier(1, 256);  // both groups have read both accumulators and the rows' sums
+      named_barrier(1, 256);
+    } else {
+      named_barrier(2 + slot, 128);
     }
-    at_tile += w.k1 - w.k0;
-  } while (w.next(p));
+    if (tile_no == m->start.tiles) return;
+    if (row == 0) w.next(p);
+    named_barrier(2 + slot, 128);
+  }
 }
 
 template <int KV, int DP, int NM>
 __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendParams p, float* parts, float2* part_rows, Shared* shared) {
   extern __shared__ __align__(1024) unsigned char raw[];
   using P = Plan<KV, DP, NM>;
-  Misc* m = reinterpret_cast<Misc*>(raw + P::kAtMisc);
+  Misc<NM>* m = reinterpret_cast<Misc<NM>*>(raw + P::kAtMisc);
   const uint32_t smem = smem_addr(raw);
   const int warp = threadIdx.x / 32;
-  if (warp == 0) locate<NM>(p, m);
+  if (warp == 0) locate<NM>(p, &m->start);
   if (warp == 4) tmem_alloc(smem_addr(&m->tmem), kTmemColumns);
   if (threadIdx.x == 256) {
     for (int i = 0; i < 5; ++i) {
