@@ -405,8 +405,8 @@ void sjd_destroy(sjd_ctx* ctx);
  *
  * Layouts. Cache: k_dev and v_dev [n_pages][kv_heads][page_size][head_dim]
  * in kv_dtype, 16-byte aligned; with an 8-bit kv_dtype also k_scale_dev and v_scale_dev,
- * fp32 [n_pages][kv_heads][page_size], one scale for each vector of
- * head_dim codes. Token p of sequence b is in slot p % page_size of page
+ * fp32 [n_pages][kv_heads][page_size], one scale, not negative, for each
+ * vector of head_dim codes. Token p of sequence b is in slot p % page_size of page
  * table[b][p / page_size]. Entries of the table that no token of a call
  * falls on are not read. Queries, keys and values are strided views
  * (sjd_view), so that they may lie in one packed projection.

@@ -38,6 +38,7 @@ constexpr int kAttendThreads = 16 * 32;
 constexpr uint32_t kTmemColumns = 512;  // S of the two slots (P over them), then O of the two
 constexpr uint32_t kOColumn = 2 * kTile;
 constexpr long long kWaitClocks = 4000000000ll;  // about two seconds
+constexpr float kLeast = 1e-30f;
 constexpr float kRise = 8.0f;           // a row's reference maximum moves when it is behind by more than 2^8
 
 __host__ __device__ constexpr uint32_t tile_bytes(int dp) { return static_cast<uint32_t>(kTile) * dp * 2; }
@@ -57,6 +58,7 @@ struct Plan {
 
 struct Start {
   int kvh, b, mt, k;     // the block's first item: key head, sequence, row tile, key tile
+  int start, count;      // the sequence's span
   long long tile, tiles;  // the block's part of all key tiles
 };
 
@@ -78,15 +80,13 @@ struct Item {
 template <int NM>
 __device__ __forceinline__ int keys_of(const AttendParams& p, int start, int count, int mt) {
   if (p.mask_kind != SJD_MASK_CAUSAL) return start + count;
-  const int G = p.c.Hq / p.c.Hkv;
-  return start + (min((mt + 1) * (kTile * NM), count * G) - 1) / G + 1;
+  return start + by_group(p.c, min((mt + 1) * (kTile * NM), count * p.c.group) - 1) + 1;
 }
 
-// Key tiles of one key head of sequence b, all its items.
+// Key tiles of one key head of a sequence, all its items.
 template <int NM>
-__device__ int tiles_of(const AttendParams& p, int b) {
-  const int2 span = span_of(p.c, b);
-  const int items = (span.y * (p.c.Hq / p.c.Hkv) + kTile * NM - 1) / (kTile * NM);
+__device__ int tiles_of(const AttendParams& p, int2 span) {
+  const int items = (span.y * p.c.group + kTile * NM - 1) / (kTile * NM);
   int sum = 0;
   for (int mt = 0; mt < items; ++mt) sum += (keys_of<NM>(p, span.x, span.y, mt) + kTile - 1) / kTile;
   return sum;
@@ -94,7 +94,7 @@ __device__ int tiles_of(const AttendParams& p, int b) {
 
 template <int NM>
 __device__ __forceinline__ void fill(const AttendParams& p, Item& it) {
-  it.rows = it.count * (p.c.Hq / p.c.Hkv);
+  it.rows = it.count * p.c.group;
   it.keys = keys_of<NM>(p, it.start, it.count, it.mt);
   it.tiles = (it.keys + kTile - 1) / kTile;
 }
@@ -112,9 +112,7 @@ struct Walk {
     left = s.tiles;
     piece = 0;
     if (left <= 0) return false;
-    it.kvh = s.kvh, it.b = s.b, it.mt = s.mt;
-    const int2 span = span_of(p.c, it.b);
-    it.start = span.x, it.count = span.y;
+    it.kvh = s.kvh, it.b = s.b, it.mt = s.mt, it.start = s.start, it.count = s.count;
     fill<NM>(p, it);
     k0 = s.k;
     k1 = static_cast<int>(min(static_cast<long long>(it.tiles), k0 + left));
@@ -150,6 +148,7 @@ struct Misc {
   int bad_values[4];       // number of the piece (modulo 4) in which a value that some rows do not see is not finite
   Start start;
   Walk<NM> walk[2];        // the softmax groups' ways
+  uint32_t poison[2][4];   // per slot: keys of the tile whose factor is no number
   alignas(16) float row[2][2][kTile];  // per slot: factors of the tile's keys and values; at the end the rows' maxima and sums
 };
 
@@ -179,20 +178,20 @@ __device__ __forceinline__ void wait(Misc<NM>* m, unsigned long long* bar, uint3
 template <int NM>
 __device__ void locate(const AttendParams& p, Start* s) {
   const int lane = threadIdx.x & 31;
-  long long per_head = 0;
-  for (int b0 = 0; b0 < p.c.B; b0 += 32) {
-    long long x = b0 + lane < p.c.B ? tiles_of<NM>(p, b0 + lane) : 0;
-    for (int o = 16; o > 0; o /= 2) x += __shfl_xor_sync(0xffffffffu, x, o);
-    per_head += x;
-  }
+  const int2 none = make_int2(0, 0);
+  auto span_at = [&](int b) { return b < p.c.B ? span_of(p.c, b) : none; };
+  int2 span = span_at(lane);
+  long long x = tiles_of<NM>(p, span), per_head = x;
+  for (int b = 32 + lane; b - lane < p.c.B; b += 32) per_head += tiles_of<NM>(p, span_at(b));
+  for (int o = 16; o > 0; o /= 2) per_head += __shfl_xor_sync(0xffffffffu, per_head, o);
   const long long all = per_head * p.c.Hkv, per = (all + gridDim.x - 1) / gridDim.x, from = blockIdx.x * per;
   const long long mine = max(0ll, min(per, all - from));
   if (lane == 0) s->tile = from, s->tiles = mine;
   if (mine == 0) return;
   const int kvh = static_cast<int>(from / per_head);
-  long long rest = from % per_head;
+  long long rest = from - kvh * per_head;
   for (int b0 = 0; b0 < p.c.B; b0 += 32) {
-    const long long x = b0 + lane < p.c.B ? tiles_of<NM>(p, b0 + lane) : 0;
+    if (b0 > 0) span = span_at(b0 + lane), x = tiles_of<NM>(p, span);
     long long upto = x;
     for (int o = 1; o < 32; o *= 2) {
       const long long y = __shfl_up_sync(0xffffffffu, upto, o);
@@ -200,13 +199,11 @@ __device__ void locate(const AttendParams& p, Start* s) {
     }
     const unsigned past = __ballot_sync(0xffffffffu, upto > rest);
     if (past) {
-      const int at = __ffs(past) - 1;
-      rest -= __shfl_sync(0xffffffffu, upto - x, at);
-      if (lane == 0) {
-        const int2 span = span_of(p.c, b0 + at);
+      if (lane == __ffs(past) - 1) {
+        rest -= upto - x;
         int mt = 0, t;
         while (rest >= (t = (keys_of<NM>(p, span.x, span.y, mt) + kTile - 1) / kTile)) rest -= t, ++mt;
-        s->kvh = kvh, s->b = b0 + at, s->mt = mt, s->k = static_cast<int>(rest);
+        *s = {kvh, b0 + lane, mt, static_cast<int>(rest), span.x, span.y, from, mine};
       }
       return;
     }
@@ -219,7 +216,7 @@ template <int NM>
 __device__ __forceinline__ int common_keys(const AttendParams& p, const Item& it) {
   if (p.mask_kind == SJD_MASK_ALL) return it.keys;
   if (p.mask_kind == SJD_MASK_GIVEN) return it.start;
-  return it.start + it.mt * (kTile * NM) / (p.c.Hq / p.c.Hkv) + 1;
+  return it.start + by_group(p.c, it.mt * (kTile * NM)) + 1;
 }
 
 // Byte offset of a 16-byte piece (8 bf16 columns) of a row in a tile.
@@ -265,12 +262,12 @@ __device__ __forceinline__ int key_page(const Cache& c, const Item& it, int key)
 template <int DP, int NM>
 __device__ __forceinline__ void load_queries(const AttendParams& p, const Item& it, uint32_t smem, int tid) {
   constexpr int kPieces = DP / 8;
-  const int G = p.c.Hq / p.c.Hkv, pieces = p.c.D / 8;
+  const int G = p.c.group, pieces = p.c.D / 8;
   const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q.p) + it.b * p.q.sb + static_cast<long long>(it.kvh) * G * p.q.sh;
   const int piece = tid % kPieces;
 #pragma unroll 8
   for (int row = tid / kPieces; row < kTile * NM; row += 128 / kPieces) {
-    const int r = it.mt * (kTile * NM) + row, t = r / G, g = r - t * G;
+    const int r = it.mt * (kTile * NM) + row, t = by_group(p.c, r), g = r - t * G;
     const bool in = r < it.rows && piece < pieces;
     copy16(smem + (row / kTile) * tile_bytes(DP) + piece_at(row % kTile, piece),
            in ? q + t * p.q.st + g * p.q.sh + 8 * piece : static_cast<const __nv_bfloat16*>(p.q.p), in ? 16 : 0);
@@ -312,7 +309,9 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
   const uint32_t ring = smem + (IS_V ? P::kAtV : P::kAtK);
   unsigned long long* full = IS_V ? m->v_full : m->k_full;
   unsigned long long* empty = IS_V ? m->v_empty : m->k_empty;
-  const Code* data = static_cast<const Code*>(IS_V ? p.c.v : p.c.k);
+  const uint32_t vector_bytes = p.c.D * sizeof(Code);
+  // (a thread beyond the head's elements asks for nothing, at the vector's start)
+  const unsigned char* own = static_cast<const unsigned char*>(IS_V ? p.c.v : p.c.k) + (8 * piece < p.c.D ? 8 * piece * sizeof(Code) : 0);
   const uint32_t in = 8 * piece < p.c.D ? 8 * sizeof(Code) : 0;  // bytes of the thread's pieces
   auto queries = [&](int number) {
     wait(m, &m->q_empty, (number & 1) ^ 1);
@@ -377,13 +376,13 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
         }
         wait(m, &empty[stage], round);
         const uint32_t to = ring + stage * tile_bytes(DP);
+        uint32_t at[kRounds];
 #pragma unroll
-        for (int i = 0; i < kRounds; ++i) {
-          const uint32_t at = __shfl_sync(0xffffffffu, mine, i * kStep + first);
-          const bool here = at != kNoVector;
-          copy16(to + piece_at(warp * 32 + i * kStep + first, piece),
-                 here ? data + static_cast<size_t>(at) * p.c.D + 8 * piece : data, here ? in : 0);
-        }
+        for (int i = 0; i < kRounds; ++i) at[i] = __shfl_sync(0xffffffffu, mine, i * kStep + first);
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i)
+          copy16(to + piece_at(warp * 32 + i * kStep + first, piece), own + static_cast<size_t>(at[i] != kNoVector ? at[i] : 0) * vector_bytes,
+                 at[i] != kNoVector ? in : 0);
         copy_commit();
         if constexpr (IS_V) {
           if ((k + 1) * kTile > common) owed_mixed |= 1u << owed;
@@ -407,12 +406,13 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
     auto ask = [&](int to) {
       if (ahead) {
         const uint32_t mine = vector_in(p.c, page, ka * kTile + tid, a.it.kvh);
+        uint32_t at[kRounds];
 #pragma unroll
-        for (int i = 0; i < kRounds; ++i) {
-          const uint32_t at = __shfl_sync(0xffffffffu, mine, i * kStep + first);
-          const bool here = at != kNoVector;
-          copy8(raw + to * (kTile * DP) + i * kStep * DP, here ? data + static_cast<size_t>(at) * p.c.D + 8 * piece : data, here ? in : 0);
-        }
+        for (int i = 0; i < kRounds; ++i) at[i] = __shfl_sync(0xffffffffu, mine, i * kStep + first);
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i)
+          copy8(raw + to * (kTile * DP) + i * kStep * DP, own + static_cast<size_t>(at[i] != kNoVector ? at[i] : 0) * vector_bytes,
+                at[i] != kNoVector ? in : 0);
         if (++ka == a.k1) {
           ahead = a.next(p);
           ka = a.k0;
@@ -434,9 +434,14 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
         copy_wait<P::kRaw - 1>();
         const uint32_t to = ring + stage * tile_bytes(DP);
 #pragma unroll
-        for (int i = 0; i < kRounds; ++i)
-          shared_store16(to + piece_at(warp * 32 + i * kStep + first, piece),
-                         eight_values<KV>(shared_load8(raw + slot * (kTile * DP) + i * kStep * DP)));
+        for (int i0 = 0; i0 < kRounds; i0 += 8) {
+          uint2 codes[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) codes[i] = shared_load8(raw + slot * (kTile * DP) + (i0 + i) * kStep * DP);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            shared_store16(to + piece_at(warp * 32 + (i0 + i) * kStep + first, piece), eight_values<KV>(codes[i]));
+        }
         fence_async_shared();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_addr(&full[stage]));
@@ -470,31 +475,52 @@ __device__ __forceinline__ void issue_values(uint32_t o, uint32_t s, uint32_t v,
 
 // --- softmax --------------------------------------------------------------------
 
-// Values that were taken out of the tiles (take_out), for the rows that see them.
-template <int KV, int N>
+// Values that were taken out of the tiles (take_out) or whose factor was set
+// aside, for the rows that see them.
+template <int KV, int NM, int N>
 __device__ __noinline__ void add_bad_values(const AttendParams& p, const Item& it, int k0, int k1, int t, int column, float (&o)[N]) {
-  if constexpr (KV == SJD_BF16) {
-    const int end = min(it.keys, k1 * kTile);
-    for (int key = max(k0 * kTile, it.start); key < end; ++key) {
-      const bool seen = p.mask_kind == SJD_MASK_CAUSAL ? key <= it.start + t
-                                                       : p.mask[p.mask_b * it.b + p.mask_r * t + (key - it.start)] != 0;
-      const uint32_t at = seen ? vector_in(p.c, key_page(p.c, it, key), key, it.kvh) : kNoVector;
-      if (at == kNoVector) continue;
+  // (the tiles that were looked over: those with a key that some row does not see)
+  const int end = min(it.keys, k1 * kTile), begin = max(k0, common_keys<NM>(p, it) / kTile) * kTile;
+  for (int key = begin; key < end; ++key) {
+    const bool seen = key < it.start || p.mask_kind == SJD_MASK_ALL ||
+                      (p.mask_kind == SJD_MASK_CAUSAL ? key <= it.start + t : p.mask[p.mask_b * it.b + p.mask_r * t + (key - it.start)] != 0);
+    const uint32_t at = seen ? vector_in(p.c, key_page(p.c, it, key), key, it.kvh) : kNoVector;
+    if (at == kNoVector) continue;
+    if constexpr (KV == SJD_BF16) {
       const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.c.v) + static_cast<size_t>(at) * p.c.D;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        if (column + i >= p.c.D) break;
+      for (int i = 0; i < N && column + i < p.c.D; ++i) {
         const float x = __bfloat162float(v[column + i]);
         if (!(fabsf(x) <= FLT_MAX)) o[i] += x;
+      }
+    } else {
+      const float f = p.c.vs[at];
+      if (f != f) {
+        for (int i = 0; i < N; ++i) o[i] += f;
       }
     }
   }
 }
 
-// The largest score (times c) of a row. seen: its keys, where MIXED.
-template <int KV, bool MIXED>
-__device__ __forceinline__ float largest(uint32_t s_at, const float* factors, float c, const uint32_t (&seen)[4]) {
-  float top[2] = {-INFINITY, -INFINITY};
+// Scores of keys that the row does not see become -inf; of those that it
+// sees and whose factor is no number (poison), NaN.
+__device__ __forceinline__ void mask_scores(uint32_t s_at, const uint32_t* seen, const uint32_t* poison) {
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    uint32_t s[32];
+    tmem_load32(s_at + 32 * i, s);
+    tmem_wait_load(s);
+    const uint32_t bits = i == 0 ? seen[0] : i == 1 ? seen[1] : i == 2 ? seen[2] : seen[3], bad = bits & poison[i];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) s[j] = bits >> j & 1 ? (bad >> j & 1 ? 0x7fc00000u : s[j]) : 0xff800000u;
+    tmem_store32(s_at + 32 * i, s);
+  }
+  tmem_wait_store();
+}
+
+// The largest score (times c) of a row.
+template <int KV>
+__device__ __forceinline__ float largest(uint32_t s_at, const float* factors, float c) {
+  float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
   uint32_t s[2][32];
   tmem_load32(s_at, s[0]);
 #pragma unroll
@@ -511,24 +537,19 @@ __device__ __forceinline__ float largest(uint32_t s_at, const float* factors, fl
         const float2 u = halves(mul2(pair(x[0], x[1]), pair(f.x, f.y))), v = halves(mul2(pair(x[2], x[3]), pair(f.z, f.w)));
         x[0] = u.x, x[1] = u.y, x[2] = v.x, x[3] = v.y;
       }
-      if constexpr (MIXED) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = seen[i] >> (j + e) & 1 ? x[e] : -INFINITY;
-      }
-      top[0] = max3(top[0], x[0], x[1]);
-      top[1] = max3(top[1], x[2], x[3]);
+      top[j / 4 & 1] = max3(top[j / 4 & 1], x[0], x[1]);
+      top[2 + (j / 4 & 1)] = max3(top[2 + (j / 4 & 1)], x[2], x[3]);
     }
   }
-  const float t = fmaxf(top[0], top[1]);
-  return KV == SJD_BF16 && t != -INFINITY ? t * c : t;
+  const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+  return KV == SJD_BF16 ? t * c : t;
 }
 
 // A row's weights against `base`, written over the scores as bf16 (32 scores
 // are in registers before the first 16 columns of weights are written, and
 // the weights stay behind the scores), and their sum.
-template <int KV, bool MIXED>
-__device__ __forceinline__ float weights(uint32_t s_at, const float* factors_k, const float* factors_v, float c, float base,
-                                         const uint32_t (&seen)[4]) {
+template <int KV>
+__device__ __forceinline__ float weights(uint32_t s_at, const float* factors_k, const float* factors_v, float c, float base) {
   const Pair c2 = pair(c, c), less = pair(-base, -base);
   Pair sum[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
   uint32_t s[2][32];
@@ -548,17 +569,11 @@ __device__ __forceinline__ float weights(uint32_t s_at, const float* factors_k, 
 #pragma unroll
       for (int e = 0; e < 4; e += 2) {
         const Pair t = pair(__uint_as_float(s[i & 1][j + e]), __uint_as_float(s[i & 1][j + e + 1]));
-        const bool sx = !MIXED || (seen[i] >> (j + e) & 1), sy = !MIXED || (seen[i] >> (j + e + 1) & 1);
         const float2 d = halves(fma2(t, KV == SJD_BF16 ? c2 : e ? pair(fk.z, fk.w) : pair(fk.x, fk.y), less));
-        float x = exp2_fast(sx ? d.x : -INFINITY), y = exp2_fast(sy ? d.y : -INFINITY);
-        const Pair w = pair(x, y);
+        const Pair w = pair(exp2_fast(d.x), exp2_fast(d.y));
         sum[e / 2] = add2(sum[e / 2], w);
-        if constexpr (KV != SJD_BF16) {
-          const float2 f = e ? make_float2(fv.z, fv.w) : make_float2(fv.x, fv.y);
-          const float2 v = halves(mul2(w, pair(sx ? f.x : 0.0f, sy ? f.y : 0.0f)));
-          x = v.x, y = v.y;
-        }
-        out[(j + e) / 2] = pack_bf16(x, y);
+        const float2 v = halves(KV == SJD_BF16 ? w : mul2(w, e ? pair(fv.z, fv.w) : pair(fv.x, fv.y)));
+        out[(j + e) / 2] = pack_bf16(v.x, v.y);
       }
     }
     tmem_store16(s_at + 16 * i, out);
@@ -573,8 +588,9 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
   const int slot = threadIdx.x / 128, row = threadIdx.x & 127, warp_row = row & ~31;
   const uint32_t lanes = static_cast<uint32_t>(warp_row) << 16;
   const uint32_t s_at = tmem + lanes + slot * kTile, o_at = tmem + lanes + kOColumn;
-  const int G = p.c.Hq / p.c.Hkv;
-  const float c = fabsf(p.scale) * 1.4426950408889634f;  // log2 e: weights are powers of two
+  const int G = p.c.group;
+  // log2 e: weights are powers of two. (The factors are never 0: times a score of -inf they are -inf.)
+  const float c = fmaxf(fabsf(p.scale) * 1.4426950408889634f, kLeast);
   // (the group's way is kept in shared memory: its registers are for the scores)
   Walk<NM>& w = m->walk[slot];
   const Item& it = w.it;
@@ -586,13 +602,14 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
   for (;;) {
     const int r0 = it.mt * (kTile * NM) + (NM == 2 ? slot * kTile : 0);
     const bool valid = r0 + row < it.rows, active = r0 + warp_row < it.rows;
-    const int t = (r0 + row) / G;
+    const int t = by_group(p.c, r0 + row);
     const int units = NM == 2 ? w.k1 - w.k0 : (w.k1 - w.k0 + 1 - slot) / 2;
     constexpr int stride = NM == 2 ? 1 : 2;
     const int k_first = w.k0 + (NM == 2 ? 0 : slot);
     // keys below `whole` are seen, those from `limit` on are not (a given mask tells between)
     const int limit = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_CAUSAL ? it.start + t + 1 : it.keys;
     const int whole = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_GIVEN ? it.start : limit;
+    const int common = common_keys<NM>(p, it);
     float ref = -INFINITY, sum = 0.0f;
     // this slot's products; unit u is the block's tile `tile0` + u * stride
     const int tile0 = tile_no + (NM == 2 ? 0 : slot);
@@ -634,8 +651,15 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     for (int u = 0; u < units; ++u) {
       const int key0 = (k_first + u * stride) * kTile;
       if constexpr (KV != SJD_BF16) {
-        m->row[slot][0][row] = next_k * c;
-        m->row[slot][1][row] = next_v;
+        // a factor that is no number would reach rows that do not see its key: it is set aside
+        // in tiles where there can be such rows (the values' are given to the others at the end)
+        const bool apart = key0 + kTile > common;
+        const bool bad_k = apart && next_k != next_k, bad_v = apart && next_v != next_v;
+        m->row[slot][0][row] = bad_k ? kLeast : fmaxf(next_k * c, next_k == next_k ? kLeast : next_k);
+        m->row[slot][1][row] = bad_v ? 0.0f : next_v;
+        const unsigned poison = __ballot_sync(0xffffffffu, bad_k);
+        if ((threadIdx.x & 31) == 0) m->poison[slot][row / 32] = poison;
+        if (bad_v) m->bad_values[w.piece & 3] = w.piece + 1;
         named_barrier(2 + slot, 128);
         if (u + 1 < units) factors(u + 1);
       }
@@ -643,9 +667,10 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
       sp ^= 1;
       tc_fence_after();
       if (active) {
-        const bool mixed = !__all_sync(0xffffffffu, key0 + kTile <= whole);
-        uint32_t seen[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
+        const uint32_t* poison = m->poison[slot];
+        const bool mixed = !__all_sync(0xffffffffu, key0 + kTile <= whole) || (KV != SJD_BF16 && (poison[0] | poison[1] | poison[2] | poison[3]));
         if (mixed) {
+          uint32_t seen[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int n = limit - (key0 + 32 * i);
@@ -661,14 +686,15 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
                 if (!mask[key]) seen[i] &= ~(1u << (key - key0 - 32 * i));
             }
           }
+          __syncwarp();
+          mask_scores(s_at, seen, poison);
         }
-        __syncwarp();
         const float* fk = m->row[slot][0];
         const float* fv = m->row[slot][1];
         // The reference that the weights are taken against moves only where a
         // weight could pass 2^8: their relative precision is the same below
         // that, and O is left alone.
-        const float top = mixed ? largest<KV, true>(s_at, fk, c, seen) : largest<KV, false>(s_at, fk, c, seen);
+        const float top = largest<KV>(s_at, fk, c);
         const bool move = top > ref + kRise || (ref == -INFINITY && top != -INFINITY);
         if (__any_sync(0xffffffffu, move)) {
           const float f = !move ? 1.0f : ref == -INFINITY ? 0.0f : exp2_fast(ref - top);
@@ -687,7 +713,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
           }
         }
         const float base = ref == -INFINITY ? 0.0f : ref;
-        sum += mixed ? weights<KV, true>(s_at, fk, fv, c, base, seen) : weights<KV, false>(s_at, fk, fv, c, base, seen);
+        sum += weights<KV>(s_at, fk, fv, c, base);
         tmem_wait_store();
         tc_fence_before();
       }
@@ -721,7 +747,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
       sum = s0 * f[0] + s1 * f[1];
     }
     const bool wholly = w.k0 == 0 && w.k1 == it.tiles;
-    const bool bad = KV == SJD_BF16 && *const_cast<volatile int*>(&m->bad_values[w.piece & 3]) == w.piece + 1;
+    const bool bad = *const_cast<volatile int*>(&m->bad_values[w.piece & 3]) == w.piece + 1;
     // this thread's columns of its row
     constexpr int kColumns = NM == 1 ? DP / 2 : DP;
     const int column0 = NM == 1 ? slot * kColumns : 0;
@@ -747,10 +773,12 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
 #pragma unroll
           for (int j = 0; j < 32; ++j) o[j] = NM == 1 ? fmaf(__uint_as_float(x[j]), f[e], o[j]) : __uint_as_float(x[j]);
         }
-        if (KV == SJD_BF16 && bad && valid) {
+        if (bad && valid) {
           float with[32];
+#pragma unroll
           for (int j = 0; j < 32; ++j) with[j] = o[j];
-          add_bad_values<KV>(p, it, w.k0, w.k1, t, column, with);
+          add_bad_values<KV, NM>(p, it, w.k0, w.k1, t, column, with);
+#pragma unroll
           for (int j = 0; j < 32; ++j) o[j] = with[j];
         }
         if (valid && wholly) {
@@ -800,6 +828,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
   Misc<NM>* m = reinterpret_cast<Misc<NM>*>(raw + P::kAtMisc);
   const uint32_t smem = smem_addr(raw);
   const int warp = threadIdx.x / 32;
+  let_next_start();
+  wait_for_previous();
   if (warp == 0) locate<NM>(p, &m->start);
   if (warp == 4) tmem_alloc(smem_addr(&m->tmem), kTmemColumns);
   if (threadIdx.x == 256) {
@@ -810,7 +840,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
     mbar_init(smem_addr(&m->q_full), 4), mbar_init(smem_addr(&m->q_empty), 2), mbar_init(smem_addr(&m->o_full), 2);
     for (int i = 0; i < 2; ++i) mbar_init(smem_addr(&m->s_full[i]), 1);
     m->abort = 0;
-    for (int i = 0; i < 4; ++i) m->bad_values[i] = 0;
+    for (int i = 0; i < 4; ++i) m->bad_values[i] = m->poison[0][i] = m->poison[1][i] = 0;
     shared[blockIdx.x].parts = 0;
     fence_barrier_init();
   }
@@ -837,7 +867,9 @@ constexpr int kJoinWarps = 8;
 template <int DP>
 __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const AttendParams p, const float* parts, const float2* part_rows,
                                                                const Shared* shared, int rows_per_item) {
-  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, G = p.c.Hq / p.c.Hkv;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, G = p.c.group;
+  let_next_start();
+  wait_for_previous();
   const Shared s = shared[blockIdx.x];
   const int row0 = blockIdx.y * kJoinWarps + warp, step = gridDim.y * kJoinWarps;
   if (s.parts > 1) {
@@ -865,7 +897,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const AttendParam
         }
       }
       const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-      const int t = r / G, g = r - t * G;
+      const int t = by_group(p.c, r), g = r - t * G;
       const long long head = (static_cast<long long>(s.b) * p.c.n + t) * p.c.Hq + static_cast<long long>(s.kvh) * G + g;
       __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.o) + head * p.c.D + lane * (DP / 32);
       if (lane * (DP / 32) < p.c.D) {
@@ -893,14 +925,9 @@ cudaError_t launch(const AttendParams& p, int sms, unsigned char* scratch, cudaS
   Shared* shared = reinterpret_cast<Shared*>(scratch);
   float2* part_rows = reinterpret_cast<float2*>(scratch + kMaxAttendBlocks * sizeof(Shared));
   float* parts = reinterpret_cast<float*>(part_rows + rows);
-  auto* kernel = attend_kernel<KV, DP, NM>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_bytes<KV, DP, NM>());
+  const cudaError_t e = launch_early(attend_kernel<KV, DP, NM>, blocks, kAttendThreads, shared_bytes<KV, DP, NM>(), s, p, parts, part_rows, shared);
   if (e != cudaSuccess) return e;
-  kernel<<<blocks, kAttendThreads, shared_bytes<KV, DP, NM>(), s>>>(p, parts, part_rows, shared);
-  e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
-  join_kernel<DP><<<dim3(blocks, 8), 32 * kJoinWarps, 0, s>>>(p, parts, part_rows, shared, kTile * NM);
-  return cudaGetLastError();
+  return launch_early(join_kernel<DP>, dim3(blocks, 8), 32 * kJoinWarps, 0, s, p, parts, part_rows, shared, kTile * NM);
 }
 
 template <int KV>
@@ -911,6 +938,24 @@ cudaError_t launch_of(const AttendParams& p, int sms, unsigned char* scratch, cu
 }
 
 }  // namespace
+
+namespace {
+
+template <int KV, int DP>
+cudaError_t raise_limits() {
+  const cudaError_t e = cudaFuncSetAttribute(attend_kernel<KV, DP, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_bytes<KV, DP, 1>());
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(attend_kernel<KV, DP, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_bytes<KV, DP, 2>());
+}
+
+}  // namespace
+
+cudaError_t prepare_attend(int kv_dtype, int head_dim) {
+  const bool small = head_dim <= 64;
+  if (kv_dtype == SJD_BF16) return small ? raise_limits<SJD_BF16, 64>() : raise_limits<SJD_BF16, 128>();
+  if (kv_dtype == SJD_E4M3) return small ? raise_limits<SJD_E4M3, 64>() : raise_limits<SJD_E4M3, 128>();
+  return small ? raise_limits<SJD_S8, 64>() : raise_limits<SJD_S8, 128>();
+}
 
 size_t attend_scratch_bytes(int head_dim, long long rows) {
   const size_t per = (rows > kTile ? 2 : 1) * static_cast<size_t>(kTile), dp = head_dim <= 64 ? 64 : 128;

@@ -38,6 +38,8 @@ __device__ __forceinline__ void angles(const Rope& r, long long token, float2* c
 
 template <typename T>
 __global__ void __launch_bounds__(kBlock) rotate_kernel(const RotateParams p) {
+  let_next_start();
+  wait_for_previous();
   __shared__ float2 cs[kMaxRotateDim / 2];
   const long long token = blockIdx.x;
   const int b = static_cast<int>(token / p.n), t = static_cast<int>(token % p.n);
@@ -65,6 +67,8 @@ __global__ void __launch_bounds__(kBlock) rotate_kernel(const RotateParams p) {
 
 template <typename T, int KV>
 __global__ void __launch_bounds__(kBlock) write_kernel(const WriteParams p) {
+  let_next_start();
+  wait_for_previous();
   __shared__ float2 cs[kMaxDim / 2];
   const Cache& c = p.c;
   const long long token = blockIdx.x;
@@ -141,6 +145,8 @@ __global__ void __launch_bounds__(kBlock) write_kernel(const WriteParams p) {
 
 template <typename T, int KV>
 __global__ void __launch_bounds__(kBlock) read_kernel(const ReadParams p) {
+  let_next_start();
+  wait_for_previous();
   const Cache& c = p.c;
   const long long token = blockIdx.x;
   const int b = static_cast<int>(token / c.n), t = static_cast<int>(token % c.n);
@@ -177,28 +183,25 @@ __global__ void __launch_bounds__(kBlock) read_kernel(const ReadParams p) {
 template <typename T>
 cudaError_t write_of(const WriteParams& p, int kv_dtype, cudaStream_t s) {
   const unsigned blocks = static_cast<unsigned>(p.c.B) * p.c.n;
-  if (kv_dtype == SJD_BF16) write_kernel<T, SJD_BF16><<<blocks, kBlock, 0, s>>>(p);
-  else if (kv_dtype == SJD_E4M3) write_kernel<T, SJD_E4M3><<<blocks, kBlock, 0, s>>>(p);
-  else write_kernel<T, SJD_S8><<<blocks, kBlock, 0, s>>>(p);
-  return cudaGetLastError();
+  if (kv_dtype == SJD_BF16) return launch_early(write_kernel<T, SJD_BF16>, blocks, kBlock, 0, s, p);
+  if (kv_dtype == SJD_E4M3) return launch_early(write_kernel<T, SJD_E4M3>, blocks, kBlock, 0, s, p);
+  return launch_early(write_kernel<T, SJD_S8>, blocks, kBlock, 0, s, p);
 }
 
 template <typename T>
 cudaError_t read_of(const ReadParams& p, int kv_dtype, cudaStream_t s) {
   const unsigned blocks = static_cast<unsigned>(p.c.B) * p.c.n;
-  if (kv_dtype == SJD_BF16) read_kernel<T, SJD_BF16><<<blocks, kBlock, 0, s>>>(p);
-  else if (kv_dtype == SJD_E4M3) read_kernel<T, SJD_E4M3><<<blocks, kBlock, 0, s>>>(p);
-  else read_kernel<T, SJD_S8><<<blocks, kBlock, 0, s>>>(p);
-  return cudaGetLastError();
+  if (kv_dtype == SJD_BF16) return launch_early(read_kernel<T, SJD_BF16>, blocks, kBlock, 0, s, p);
+  if (kv_dtype == SJD_E4M3) return launch_early(read_kernel<T, SJD_E4M3>, blocks, kBlock, 0, s, p);
+  return launch_early(read_kernel<T, SJD_S8>, blocks, kBlock, 0, s, p);
 }
 
 }  // namespace
 
 cudaError_t launch_rotate(const RotateParams& p, int dtype, cudaStream_t s) {
   const unsigned blocks = static_cast<unsigned>(p.B) * p.n;
-  if (dtype == SJD_BF16) rotate_kernel<__nv_bfloat16><<<blocks, kBlock, 0, s>>>(p);
-  else rotate_kernel<float><<<blocks, kBlock, 0, s>>>(p);
-  return cudaGetLastError();
+  if (dtype == SJD_BF16) return launch_early(rotate_kernel<__nv_bfloat16>, blocks, kBlock, 0, s, p);
+  return launch_early(rotate_kernel<float>, blocks, kBlock, 0, s, p);
 }
 
 cudaError_t launch_write(const WriteParams& p, int dtype, int kv_dtype, cudaStream_t s) {

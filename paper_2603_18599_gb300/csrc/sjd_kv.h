@@ -36,8 +36,9 @@ struct Cache {
   const int32_t* count;
   int n;
   uint32_t* status;
-  uint32_t ps_mul;  // key / ps = key * ps_mul >> (31 + ps_shift), key < 2^31
-  int ps_shift;
+  int group;                     // query heads of a key head
+  uint32_t ps_mul, group_mul;    // x / ps = x * ps_mul >> (31 + ps_shift) below 2^31, and so for group
+  int ps_shift, group_shift;
 };
 
 struct Rope {
@@ -76,12 +77,31 @@ struct AttendParams {
   float* lse;
 };
 
+// Launches a kernel that may start while the one before it on the stream
+// drains (it calls wait_for_previous).
+template <typename... Args, typename... Given>
+cudaError_t launch_early(void (*kernel)(Args...), dim3 grid, int threads, size_t shared, cudaStream_t s, Given&&... given) {
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t at = {};
+  at.gridDim = grid;
+  at.blockDim = dim3(threads);
+  at.dynamicSmemBytes = shared;
+  at.stream = s;
+  at.attrs = &early;
+  at.numAttrs = 1;
+  return cudaLaunchKernelEx(&at, kernel, static_cast<Args>(given)...);
+}
+
 // kv_dtype of the cache: SJD_BF16, SJD_E4M3, SJD_S8; dtype of the caller's tensors: SJD_F32, SJD_BF16.
 cudaError_t launch_rotate(const RotateParams& p, int dtype, cudaStream_t s);
 cudaError_t launch_write(const WriteParams& p, int dtype, int kv_dtype, cudaStream_t s);
 cudaError_t launch_read(const ReadParams& p, int dtype, int kv_dtype, cudaStream_t s);
 // scratch: attend_scratch_bytes(head_dim, max_new * heads / kv_heads), 256-byte aligned.
 cudaError_t launch_attend(const AttendParams& p, int kv_dtype, int sms, unsigned char* scratch, cudaStream_t s);
+// Sets the kernels' limits on the current device, once for a handle.
+cudaError_t prepare_attend(int kv_dtype, int head_dim);
 size_t attend_scratch_bytes(int head_dim, long long rows);
 
 }  // namespace sjd_kv_ops

@@ -61,6 +61,18 @@ View view_of(const sjd_view* v) { return {v->data_dev, v->batch_stride, v->token
 
 size_t size_of(int dtype) { return dtype == SJD_BF16 ? 2 : 4; }
 
+// x / d = x * mul >> (31 + shift) for x < 2^31: shift = ceil(log2 d), mul =
+// ceil(2^(31 + shift) / d) is above the true factor by less than 2^-31 of it.
+struct Divisor {
+  uint32_t mul;
+  int shift;
+};
+Divisor divisor(int d) {
+  int shift = 0;
+  while ((1ll << shift) < d) ++shift;
+  return {static_cast<uint32_t>(((1ull << (31 + shift)) + d - 1) / d), shift};
+}
+
 // The cache and spans of a call; a text if an argument is wrong.
 const char* cache_of(sjd_kv* kv, const sjd_kv_layer* l, const sjd_kv_span* s, long long most, Cache* c) {
   const sjd_kv_config& g = kv->cfg;
@@ -71,13 +83,11 @@ const char* cache_of(sjd_kv* kv, const sjd_kv_layer* l, const sjd_kv_span* s, lo
     return "layer: an 8-bit cache needs scales";
   if (!s->table_dev || !s->start_dev) return "span: table or start is NULL";
   if (s->n < 1 || s->n > most) return "span: n out of range";
-  // log = ceil(log2 ps), mul = ceil(2^(31 + log) / ps): the quotient is exact below 2^31
-  int log = 0;
-  while ((1ll << log) < g.page_size) ++log;
-  const uint32_t mul = static_cast<uint32_t>(((1ull << (31 + log)) + g.page_size - 1) / g.page_size);
+  const int group = g.heads / g.kv_heads;
+  const Divisor page = divisor(g.page_size), heads = divisor(group);
   *c = {g.batch, g.heads, g.kv_heads, g.head_dim, g.page_size, g.n_pages, g.max_pages, l->k_dev, l->v_dev,
         scaled ? l->k_scale_dev : nullptr, scaled ? l->v_scale_dev : nullptr, s->table_dev, s->start_dev, s->count_dev,
-        s->n, reinterpret_cast<uint32_t*>(kv->ws), mul, log};
+        s->n, reinterpret_cast<uint32_t*>(kv->ws), group, page.mul, heads.mul, page.shift, heads.shift};
   return nullptr;
 }
 
@@ -123,6 +133,7 @@ int sjd_kv_init(const sjd_kv_config* cfg, void* workspace, size_t ws_bytes, void
   int device = 0, sms = 0;
   if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
     return SJD_ERR_CUDA;
+  if (prepare_attend(cfg->kv_dtype, cfg->head_dim) != cudaSuccess) return SJD_ERR_CUDA;
   if (cudaMemsetAsync(workspace, 0, kAlign, s) != cudaSuccess) return SJD_ERR_CUDA;
   sjd_kv* kv = new (std::nothrow) sjd_kv{*cfg, static_cast<unsigned char*>(workspace), s, sms, ""};
   if (!kv) return SJD_ERR_CAPACITY;

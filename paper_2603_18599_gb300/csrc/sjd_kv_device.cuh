@@ -11,6 +11,11 @@
 
 namespace sjd_kv_ops {
 
+// The kernels are launched while the one before them on the stream drains:
+// this waits until it is done. Nothing is read or written before.
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Sequence b's span of the call, {0, 0} where it does not fit its table.
 __device__ __forceinline__ int2 span_of(const Cache& c, int b) {
   const int start = c.start[b], count = c.count ? c.count[b] : c.n;
@@ -26,10 +31,13 @@ __device__ __forceinline__ int2 span_of(const Cache& c, int b) {
 constexpr uint32_t kNoVector = 0xffffffffu;
 constexpr int kNoPage = -0x7fffffff - 1;  // a token that is not there
 
-// The table's entry of token pos of sequence b, as it stands there.
-__device__ __forceinline__ int entry_of(const Cache& c, int pos) {
-  return static_cast<int>(static_cast<unsigned long long>(static_cast<uint32_t>(pos)) * c.ps_mul >> (31 + c.ps_shift));
+__device__ __forceinline__ int divide(int x, uint32_t mul, int shift) {
+  return static_cast<int>(static_cast<unsigned long long>(static_cast<uint32_t>(x)) * mul >> (31 + shift));
 }
+__device__ __forceinline__ int entry_of(const Cache& c, int pos) { return divide(pos, c.ps_mul, c.ps_shift); }
+__device__ __forceinline__ int by_group(const Cache& c, int x) { return divide(x, c.group_mul, c.group_shift); }
+
+// The table's entry of token pos of sequence b, as it stands there.
 __device__ __forceinline__ int page_of(const Cache& c, int b, int pos) {
   return c.table[static_cast<long long>(b) * c.max_pages + entry_of(c, pos)];
 }

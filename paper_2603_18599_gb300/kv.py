@@ -17,6 +17,7 @@ call, so that tensors may be made and used on either.
 
 import ctypes
 import math
+import struct
 from ctypes import POINTER, byref, c_double, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 
 import torch
@@ -34,20 +35,12 @@ class _config(ctypes.Structure):
                                        "max_new", "kv_dtype")]
 
 
-class _layer(ctypes.Structure):
-    _fields_ = [(n, c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
-
-
-class _view(ctypes.Structure):
-    _fields_ = [("data", c_void_p), ("batch_stride", c_int64), ("token_stride", c_int64), ("head_stride", c_int64)]
-
-
-class _span(ctypes.Structure):
-    _fields_ = [("table", c_void_p), ("start", c_void_p), ("count", c_void_p), ("n", c_int32)]
-
-
-class _rope(ctypes.Structure):
-    _fields_ = [("turns", c_void_p), ("axis", c_void_p), ("pairs", c_int32), ("axes", c_int32), ("interleaved", c_int32)]
+# The other structures of include/sjd.h, packed for each call (a window's
+# calls are short: what the host does for one counts)
+_LAYER = struct.Struct("4Q")        # sjd_kv_layer
+_VIEW = struct.Struct("Q3q")        # sjd_view
+_SPAN = struct.Struct("3Qi4x")      # sjd_kv_span
+_ROPE = struct.Struct("2Q3i4x")     # sjd_rope
 
 
 _lib = None
@@ -76,6 +69,11 @@ def load():
     return L
 
 
+# (as torch.cuda.current_stream and current_device, without making an object)
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
+
+
 def _device(device):
     device = torch.device(device)
     if device.type == "cuda" and device.index is None:
@@ -87,7 +85,7 @@ def _view_of(x, name, shape, dtype, device):
     if x.shape != shape or x.dtype != dtype or x.device != device or x.stride(3) != 1:
         raise ValueError("%s must be a %s tensor of shape %s on %s, its last dimension dense" % (name, dtype, tuple(shape), device))
     s = x.stride()
-    return _view(x.data_ptr(), s[0], s[1], s[2])
+    return _VIEW.pack(x.data_ptr(), s[0], s[1], s[2])
 
 
 def _array(x, name, shape, device, dtype=torch.int32):
@@ -114,8 +112,7 @@ class Rope:
         self.device = _device(device)
         self._turns = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64, device=self.device)
         self._axis = torch.tensor(axis, dtype=torch.int32, device=self.device)
-        self._c = _rope(self._turns.data_ptr(), self._axis.data_ptr(), self.pairs, self.axes, int(self.interleaved))
-        self._at = ctypes.addressof(self._c)
+        self._c = _ROPE.pack(self._turns.data_ptr(), self._axis.data_ptr(), self.pairs, self.axes, self.interleaved)
 
     @classmethod
     def sections(cls, pairs, theta=10000.0, shared=False, interleaved=False, device="cuda"):
@@ -137,14 +134,17 @@ class Rope:
             raise ValueError("x must be a [B, n, H, D] bf16 or f32 tensor on %s" % (self.device,))
         B, n, H, D = x.shape
         at = _array(positions, "positions", (B, n, self.axes), self.device)
-        with torch.cuda.device(self.device):
-            if out is None:
-                out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-            if x.numel() == 0:
-                return out
-            rc = load().sjd_rotate(self._at, byref(_view_of(x, "x", x.shape, x.dtype, x.device)),
-                                   byref(_view_of(out, "out", x.shape, x.dtype, x.device)), at, B, n, H, D, _DTYPES[x.dtype],
-                                   int(bool(inverse)), torch.cuda.current_stream(self.device).cuda_stream)
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if x.numel() == 0:
+            return out
+        args = (self._c, _view_of(x, "x", x.shape, x.dtype, x.device), _view_of(out, "out", x.shape, x.dtype, x.device), at,
+                B, n, H, D, _DTYPES[x.dtype], 1 if inverse else 0, _raw_stream(self.device.index))
+        if _current_device() == self.device.index:
+            rc = load().sjd_rotate(*args)
+        else:
+            with torch.cuda.device(self.device):
+                rc = load().sjd_rotate(*args)
         if rc != SJD_OK:
             raise SJDError(rc, "sjd_rotate failed (dim a multiple of 8 up to 256, 2 * pairs at most dim)")
         return out
@@ -154,9 +154,15 @@ class Layer:
     """One layer's cache: k, v [n_pages, kv_heads, page_size, head_dim] and,
     of an 8-bit cache, k_scale, v_scale [n_pages, kv_heads, page_size] f32."""
 
+    __slots__ = ("_t", "_for")
+
     def __init__(self, k, v, k_scale=None, v_scale=None):
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self._for = None
+        self._t, self._for = (k, v, k_scale, v_scale), None
+
+    k = property(lambda self: self._t[0])
+    v = property(lambda self: self._t[1])
+    k_scale = property(lambda self: self._t[2])
+    v_scale = property(lambda self: self._t[3])
 
 
 class KV:
@@ -177,6 +183,7 @@ class KV:
             raise SJDError(sjd.SJD_ERR_ARG, "invalid configuration")
         self.device = _device(device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self._raw = self.stream.cuda_stream
         with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
             self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
             rc = self.L.sjd_kv_init(byref(self.cfg), self.workspace.data_ptr(), size, self.stream.cuda_stream, byref(self.ctx))
@@ -186,48 +193,46 @@ class KV:
         c = self.cfg
         self._shapes = ((c.n_pages, c.kv_heads, c.page_size, c.head_dim), (c.n_pages, c.kv_heads, c.page_size),
                         (c.batch, c.max_pages), (c.batch,))
+        self._scale = 1.0 / math.sqrt(c.head_dim)
 
     # -- helpers ------------------------------------------------------------
-    def _check(self, rc):
-        if rc != SJD_OK:
-            raise SJDError(rc, self.L.sjd_kv_last_error(self.ctx).decode())
-
     def _layer_of(self, layer):
-        if layer._for is not self:
+        k, v, ks, vs = layer._t
+        if layer._for is not self:   # (a handle's sizes and a layer's tensors do not change)
             pages, scales = self._shapes[:2]
-            at = [_array(layer.k, "k", pages, self.device, self.dtype), _array(layer.v, "v", pages, self.device, self.dtype)]
+            _array(k, "k", pages, self.device, self.dtype)
+            _array(v, "v", pages, self.device, self.dtype)
             if self.dtype != torch.bfloat16:
-                for name in ("k_scale", "v_scale"):
-                    if getattr(layer, name) is None:
-                        raise ValueError("an 8-bit cache needs k_scale and v_scale")
-                    at.append(_array(getattr(layer, name), name, scales, self.device, torch.float32))
-            else:
-                at += [None, None]
-            layer._c = _layer(*at)
-            layer._at = ctypes.addressof(layer._c)
+                if ks is None or vs is None:
+                    raise ValueError("an 8-bit cache needs k_scale and v_scale")
+                _array(ks, "k_scale", scales, self.device, torch.float32)
+                _array(vs, "v_scale", scales, self.device, torch.float32)
             layer._for = self
-        return layer._at
+        if self.dtype == torch.bfloat16:
+            return _LAYER.pack(k.data_ptr(), v.data_ptr(), 0, 0)
+        return _LAYER.pack(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr())
 
     def _span(self, table, start, count, n):
-        return _span(_array(table, "table", self._shapes[2], self.device), _array(start, "start", self._shapes[3], self.device),
-                     None if count is None else _array(count, "count", self._shapes[3], self.device), n)
+        return _SPAN.pack(_array(table, "table", self._shapes[2], self.device), _array(start, "start", self._shapes[3], self.device),
+                          0 if count is None else _array(count, "count", self._shapes[3], self.device), n)
 
-    def _run(self, call, *tensors):
-        """call() with the handle's device current, ordered with the current
-        stream where that is another one. `tensors`: what the call uses."""
-        here = torch.cuda.current_stream(self.device)
-        if here == self.stream and torch.cuda.current_device() == self.device.index:
-            return call()
-        with torch.cuda.device(self.device):
-            if here == self.stream:
-                return call()
-            self.stream.wait_stream(here)
-            out = call()
-            here.wait_stream(self.stream)
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
-            return out
+    def _run(self, call, args, tensors):
+        """call(*args) with the handle's device current, ordered with the
+        current stream where that is another one. `tensors`: what it uses."""
+        index = self.device.index
+        if _raw_stream(index) == self._raw and _current_device() == index:
+            rc = call(*args)
+        else:
+            with torch.cuda.device(self.device):
+                here = torch.cuda.current_stream(self.device)
+                self.stream.wait_stream(here)
+                rc = call(*args)
+                here.wait_stream(self.stream)
+                for t in tensors:
+                    if t is not None:
+                        t.record_stream(self.stream)
+        if rc != SJD_OK:
+            raise SJDError(rc, self.L.sjd_kv_last_error(self.ctx).decode())
 
     # -- entry points ---------------------------------------------------------
     def new_layer(self):
@@ -257,17 +262,16 @@ class KV:
         shape = (B, n, c.kv_heads, c.head_dim)
         kw, vw = _view_of(k, "k", shape, dt, self.device), _view_of(v, "v", shape, dt, self.device)
         at, span = self._layer_of(layer), self._span(table, start, count, n)
-        rope_at = pos = qw = ow = None
+        rope_c = pos = qw = ow = turns = axis = None
         if rope is not None:
-            rope_at, pos = rope._at, _array(positions, "positions", (B, n, rope.axes), self.device)
+            rope_c, pos, turns, axis = rope._c, _array(positions, "positions", (B, n, rope.axes), self.device), rope._turns, rope._axis
         if q is not None:
             shape = (B, n, c.heads, c.head_dim)
             if q_out is None:
                 q_out = torch.empty(shape, dtype=dt, device=self.device)
-            qw, ow = byref(_view_of(q, "q", shape, dt, self.device)), byref(_view_of(q_out, "q_out", shape, dt, self.device))
-        self._check(self._run(lambda: self.L.sjd_kv_write(self.ctx, at, byref(span), _DTYPES[dt], byref(kw), byref(vw), rope_at,
-                                                          pos, qw, ow),
-                              layer.k, layer.v, layer.k_scale, layer.v_scale, k, v, table, start, count, positions, q, q_out))
+            qw, ow = _view_of(q, "q", shape, dt, self.device), _view_of(q_out, "q_out", shape, dt, self.device)
+        self._run(self.L.sjd_kv_write, (self.ctx, at, span, _DTYPES[dt], kw, vw, rope_c, pos, qw, ow),
+                  (*layer._t, k, v, table, start, count, positions, q, q_out, turns, axis))
         return q_out
 
     def read(self, layer, table, start, n, count=None, dtype=torch.bfloat16):
@@ -278,9 +282,10 @@ class KV:
             raise ValueError("dtype must be bf16 or f32")
         at, span = self._layer_of(layer), self._span(table, start, count, n)
         shape = (c.batch, n, c.kv_heads, c.head_dim)
-        k, v = (torch.empty(shape, dtype=dtype, device=self.device) for _ in range(2))
-        self._check(self._run(lambda: self.L.sjd_kv_read(self.ctx, at, byref(span), _DTYPES[dtype], k.data_ptr(), v.data_ptr()),
-                              layer.k, layer.v, layer.k_scale, layer.v_scale, table, start, count, k, v))
+        k = torch.empty(shape, dtype=dtype, device=self.device)
+        v = torch.empty(shape, dtype=dtype, device=self.device)
+        self._run(self.L.sjd_kv_read, (self.ctx, at, span, _DTYPES[dtype], k.data_ptr(), v.data_ptr()),
+                  (*layer._t, table, start, count, k, v))
         return k, v
 
     def attend(self, layer, q, table, start, count=None, mask="causal", scale=None, lse=False, out=None):
@@ -304,14 +309,16 @@ class KV:
             mask_at, mb, mr = mask.data_ptr(), mask.stride(0) if mask.shape[0] == B else 0, mask.stride(1)
         elif mask != "causal":
             raise ValueError("mask must be \"causal\", None or a tensor")
+        shape = (B, n, c.heads, c.head_dim)
         if out is None:
-            out = torch.empty((B, n, c.heads, c.head_dim), dtype=torch.bfloat16, device=self.device)
-        o_at = _array(out, "out", (B, n, c.heads, c.head_dim), self.device, torch.bfloat16)
+            out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+            o_at = out.data_ptr()
+        else:
+            o_at = _array(out, "out", shape, self.device, torch.bfloat16)
         sums = torch.empty((B, n, c.heads), dtype=torch.float32, device=self.device) if lse else None
-        scale = 1.0 / math.sqrt(c.head_dim) if scale is None else float(scale)
-        self._check(self._run(lambda: self.L.sjd_kv_attend(self.ctx, at, byref(span), byref(qw), kind, mask_at, mb, mr, scale, o_at,
-                                                           None if sums is None else sums.data_ptr()),
-                              layer.k, layer.v, layer.k_scale, layer.v_scale, q, table, start, count, given, out, sums))
+        scale = self._scale if scale is None else float(scale)
+        self._run(self.L.sjd_kv_attend, (self.ctx, at, span, qw, kind, mask_at, mb, mr, scale, o_at, sums.data_ptr() if lse else None),
+                  (*layer._t, q, table, start, count, given, out, sums))
         return (out, sums) if lse else out
 
     def sync(self):

@@ -447,6 +447,37 @@ def test_unseen_keys_have_no_effect_whatever_they_hold(dtype, kind, bad):
             assert hit.isnan().any(-1).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kind", ["causal", None, "given"])
+@pytest.mark.parametrize("heads,n", [(4, 9), (2, 200)])
+def test_context_keys_that_hold_nan(dtype, kind, heads, n):
+    """A NaN in a key or value of the context, in the tile where the chunk
+    begins and in one before it, reaches every row of its head; with mask
+    None one of the chunk does too."""
+    starts, D = [300], 64
+    h, layer, table, start, g = make(1, heads, 2, D, dtype, 16, starts, n)
+    filled(h, layer, table, starts, n, g)
+    q = normal(g, 1, n, heads, D).bfloat16()
+    mask = torch.eye(n, device=DEV).bool()[None] if kind == "given" else kind
+    one = torch.ones(1, dtype=torch.int32, device=DEV)
+    for where in [298, 20] + ([299 + n] if kind is None else []):
+        at = torch.tensor([where], dtype=torch.int32, device=DEV)
+        k, v = h.read(layer, table, at, 1, dtype=torch.float32)
+        for which in ("k", "v"):
+            x = (k if which == "k" else v).clone()
+            x[0, 0, 1, 7] = math.nan
+            h.write(layer, *((x, v) if which == "k" else (k, x)), table, at, one)
+            o = h.attend(layer, q, table, start, mask=mask)
+            assert o[:, :, :heads // 2].isfinite().all()
+            hit = o[:, :, heads // 2:]
+            if which == "v" and dtype == torch.bfloat16:
+                assert hit[..., 7].isnan().all() and hit[..., :7].isfinite().all() and hit[..., 8:].isfinite().all()
+            else:
+                assert hit.isnan().all()
+            h.write(layer, k, v, table, at, one)
+    assert h.attend(layer, q, table, start, mask=mask).isfinite().all()
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.int8])
 def test_offsets_past_32_bits(dtype):
     """A cache of more than 2^32 elements: its last pages, written, read and

@@ -26,10 +26,10 @@ def config(**over):
 def test_struct_sizes_match_the_header(lib):
     from paper_2603_18599_gb300 import kv
     assert ctypes.sizeof(kv._config) == 36
-    assert ctypes.sizeof(kv._view) == 32
-    assert ctypes.sizeof(kv._span) == 32
-    assert ctypes.sizeof(kv._rope) == 32
-    assert ctypes.sizeof(kv._layer) == 32
+    assert kv._VIEW.size == 32
+    assert kv._SPAN.size == 32
+    assert kv._ROPE.size == 32
+    assert kv._LAYER.size == 32
 
 
 def test_workspace_size_validates_configs(lib):
