@@ -17,12 +17,13 @@
 // item that a cut went through is left as unnormalised parts with their
 // maxima and sums, which a second kernel joins in the order of the parts.
 //
-// A block has three kinds of warps. 0-3 and 4-7 take the softmax, each group a
+// A block has four kinds of warps. 0-3 and 4-7 take the softmax, each group a
 // slot: with NM = 1 the even and the odd tiles of the same 128 rows (each with
 // an accumulator of its own, joined at the end), with NM = 2 the two halves
-// of 256 rows. One thread of each group issues the slot's products, which run
-// while the other slot's softmax does. 8-11 load keys, 12-15 the queries and
-// values.
+// of 256 rows. 8-11 load keys, 12-15 the queries and values, and warp 16
+// issues the products. A slot goes through a tile in two halves of
+// 64 keys with a place for scores each, so that one half's scores are made
+// while the other's softmax runs.
 
 #include <cfloat>
 
@@ -34,8 +35,10 @@ namespace sjd_kv_ops {
 namespace {
 
 constexpr int kTile = 128;              // rows of a product, and keys of a tile
-constexpr int kAttendThreads = 16 * 32;
-constexpr uint32_t kTmemColumns = 512;  // S of the two slots (P over them), then O of the two
+constexpr int kHalf = kTile / 2;        // keys of a unit
+constexpr int kAttendThreads = 17 * 32;
+constexpr int kMmaWarp = 16;
+constexpr uint32_t kTmemColumns = 512;  // S of the two slots, two halves each (P over them), then O of the two
 constexpr uint32_t kOColumn = 2 * kTile;
 constexpr long long kWaitClocks = 4000000000ll;  // about two seconds
 constexpr float kLeast = 1e-30f;
@@ -142,7 +145,8 @@ struct Walk {
 
 template <int NM>
 struct Misc {
-  unsigned long long k_full[5], k_empty[5], v_full[5], v_empty[5], q_full, q_empty, s_full[2], o_full;
+  unsigned long long k_full[5], k_empty[5], v_full[5], v_empty[5], q_full, q_empty, o_full,
+      s_full[2][2], p_full[2][2], o_done[2][2];  // by slot and half
   uint32_t tmem;
   int abort;
   int bad_values[4];       // number of the piece (modulo 4) in which a value that some rows do not see is not finite
@@ -397,22 +401,38 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
     }
     drain();
   } else {
-    // The codes come into a ring of their own, up to kRaw tiles ahead; each
-    // thread turns the pieces that it has asked for into bf16.
-    const uint32_t raw = smem + (IS_V ? P::kAtRawV : P::kAtRawK) + (warp * 32 + first) * DP + 8 * piece;
+    // The codes come into a ring of their own, up to kRaw tiles ahead, 16 to a
+    // copy where a vector's length is a multiple of that (past the L1 cache)
+    // and else 8; a warp turns its 32 rows into bf16, 8 codes to a thread.
+    constexpr int kWide = DP / 16, kWideStep = 32 / kWide;
+    const bool wide = p.c.D % 16 == 0;
+    const uint32_t raw = smem + (IS_V ? P::kAtRawV : P::kAtRawK) + warp * 32 * DP;
+    const uint32_t from = raw + first * DP + 8 * piece;
+    const unsigned char* data = static_cast<const unsigned char*>(IS_V ? p.c.v : p.c.k);
     Walk<NM> a = w;           // the tile to be asked for
     int ka = a.k0, slot = 0;
     bool ahead = true;
     auto ask = [&](int to) {
       if (ahead) {
         const uint32_t mine = vector_in(p.c, page, ka * kTile + tid, a.it.kvh);
-        uint32_t at[kRounds];
+        if (wide) {
+          const int part = 16 * (lane % kWide), row = lane / kWide, bytes = part < p.c.D ? 16 : 0;
+          uint32_t at[32 / kWideStep];
 #pragma unroll
-        for (int i = 0; i < kRounds; ++i) at[i] = __shfl_sync(0xffffffffu, mine, i * kStep + first);
+          for (int i = 0; i < 32 / kWideStep; ++i) at[i] = __shfl_sync(0xffffffffu, mine, i * kWideStep + row);
 #pragma unroll
-        for (int i = 0; i < kRounds; ++i)
-          copy8(raw + to * (kTile * DP) + i * kStep * DP, own + static_cast<size_t>(at[i] != kNoVector ? at[i] : 0) * vector_bytes,
-                at[i] != kNoVector ? in : 0);
+          for (int i = 0; i < 32 / kWideStep; ++i)
+            copy16(raw + to * (kTile * DP) + (i * kWideStep + row) * DP + part,
+                   data + static_cast<size_t>(at[i] != kNoVector ? at[i] : 0) * vector_bytes + (bytes ? part : 0), at[i] != kNoVector ? bytes : 0);
+        } else {
+          uint32_t at[kRounds];
+#pragma unroll
+          for (int i = 0; i < kRounds; ++i) at[i] = __shfl_sync(0xffffffffu, mine, i * kStep + first);
+#pragma unroll
+          for (int i = 0; i < kRounds; ++i)
+            copy8(from + to * (kTile * DP) + i * kStep * DP, own + static_cast<size_t>(at[i] != kNoVector ? at[i] : 0) * vector_bytes,
+                  at[i] != kNoVector ? in : 0);
+        }
         if (++ka == a.k1) {
           ahead = a.next(p);
           ka = a.k0;
@@ -432,12 +452,13 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
       for (int k = w.k0; k < w.k1; ++k) {
         wait(m, &empty[stage], round);
         copy_wait<P::kRaw - 1>();
+        __syncwarp();
         const uint32_t to = ring + stage * tile_bytes(DP);
 #pragma unroll
         for (int i0 = 0; i0 < kRounds; i0 += 8) {
           uint2 codes[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) codes[i] = shared_load8(raw + slot * (kTile * DP) + (i0 + i) * kStep * DP);
+          for (int i = 0; i < 8; ++i) codes[i] = shared_load8(from + slot * (kTile * DP) + (i0 + i) * kStep * DP);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             shared_store16(to + piece_at(warp * 32 + (i0 + i) * kStep + first, piece), eight_values<KV>(codes[i]));
@@ -455,22 +476,80 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
 
 // --- products -------------------------------------------------------------------
 
-// S of a slot = Q K^T.
-template <int DP>
-__device__ __forceinline__ void issue_scores(uint32_t s, uint32_t q, uint32_t k) {
-  constexpr uint32_t kKind = product_kind(kTile, kTile, false);
-#pragma unroll
-  for (int i = 0; i < DP / 16; ++i) {
-    const uint32_t at = (i / 4) * (kTile * 128) + (i % 4) * 32;
-    mma_ss(s, operand_k(q + at), operand_k(k + at), kKind, i > 0);
-  }
+// Units of 64 keys of a slot in a piece (the item's last tile may end in its first half).
+template <int NM>
+__device__ __forceinline__ int units_of(const Walk<NM>& w, int slot) {
+  const int tiles = w.k1 - w.k0, own = NM == 2 ? tiles : (tiles + 1 - slot) / 2;
+  const bool last = NM == 2 || ((tiles - 1) & 1) == slot;  // the piece's last tile is the slot's
+  return 2 * own - (last && w.it.keys - (w.k1 - 1) * kTile <= kHalf ? 1 : 0);
 }
-// O of a slot = P V, or += with `add`; P lies over S, two weights to a column.
-template <int DP>
-__device__ __forceinline__ void issue_values(uint32_t o, uint32_t s, uint32_t v, bool add) {
-  constexpr uint32_t kKind = product_kind(kTile, DP, true);
+
+// One warp issues the products of both slots, the slots in turn.
+template <int KV, int DP, int NM>
+__device__ __forceinline__ void issue_products(const AttendParams& p, Misc<NM>* m, uint32_t smem, uint32_t tmem) {
+  using P = Plan<KV, DP, NM>;
+  constexpr uint32_t kScores = product_kind(kTile, kHalf, false), kValues = product_kind(kTile, DP, true);
+  const bool lead = elect_lane();
+  Walk<NM> w;
+  if (!w.begin(p, m->start)) return;
+  int tile0 = 0;              // the block's number of the piece's first tile
+  uint32_t pp[2] = {0, 0};    // per slot, bit h: parity of p_full[slot][h]
+  do {
+    const int units[2] = {units_of(w, 0), units_of(w, 1)};
+    int left = units[0] + units[1];  // scores to be issued
+    auto tile_at = [&](int slot, int u) { return tile0 + (NM == 2 ? u / 2 : u / 2 * 2 + slot); };
+    // S of a slot and half = Q K^T
+    auto scores = [&](int slot, int u) {
+      const int tile = tile_at(slot, u), stage = tile % P::kK, h = u & 1;
+      if (h == 0 && (NM == 1 || slot == 0)) wait(m, &m->k_full[stage], tile / P::kK & 1);
+      tc_fence_after();
+      const uint32_t q = smem + (NM == 2 ? slot * tile_bytes(DP) : 0), k = smem + P::kAtK + stage * tile_bytes(DP) + h * (kHalf * 128);
+      --left;
+      if (lead) {
 #pragma unroll
-  for (int i = 0; i < kTile / 16; ++i) mma_ts(o, s + i * 8, operand_n(v + i * 2048, kTile * 128), kKind, add || i > 0);
+        for (int i = 0; i < DP / 16; ++i) {
+          const uint32_t at = (i / 4) * (kTile * 128) + (i % 4) * 32;
+          mma_ss(tmem + slot * kTile + h * kHalf, operand_k(q + at), operand_k(k + at), kScores, i > 0);
+        }
+        mma_commit(smem_addr(&m->s_full[slot][h]));
+        if ((h == 1 || u + 1 == units[slot]) && (NM == 1 || slot == 1)) mma_commit(smem_addr(&m->k_empty[stage]));
+        if (left == 0) mma_commit(smem_addr(&m->q_empty));
+      }
+      __syncwarp();
+    };
+    wait(m, &m->q_full, w.piece & 1);
+    for (int u = 0; u < 2; ++u)
+      for (int slot = 0; slot < 2; ++slot)
+        if (u < units[slot]) scores(slot, u);
+    for (int u = 0; u < units[0] || u < units[1]; ++u) {
+      const int h = u & 1;
+#pragma unroll
+      for (int slot = 0; slot < 2; ++slot) {
+        if (u >= units[slot]) continue;
+        const int tile = tile_at(slot, u), stage = tile % P::kV;
+        if (h == 0 && (NM == 1 || slot == 0)) wait(m, &m->v_full[stage], tile / P::kV & 1);
+        wait(m, &m->p_full[slot][h], pp[slot] >> h & 1);
+        pp[slot] ^= 1u << h;
+        tc_fence_after();
+        // O of a slot += P V; P lies over S, two weights to a column
+        const uint32_t v = smem + P::kAtV + stage * tile_bytes(DP) + h * (kHalf * 128);
+        if (lead) {
+#pragma unroll
+          for (int i = 0; i < kHalf / 16; ++i)
+            mma_ts(tmem + kOColumn + slot * DP, tmem + slot * kTile + h * kHalf + i * 8, operand_n(v + i * 2048, kTile * 128), kValues, u > 0 || i > 0);
+          mma_commit(smem_addr(&m->o_done[slot][h]));
+          if ((h == 1 || u + 1 == units[slot]) && (NM == 1 || slot == 1)) mma_commit(smem_addr(&m->v_empty[stage]));
+        }
+        __syncwarp();
+        if (u + 2 < units[slot]) scores(slot, u + 2);
+      }
+    }
+    if (lead) mma_commit(smem_addr(&m->o_full));
+    __syncwarp();
+    tile0 += w.k1 - w.k0;
+  } while (w.next(p));
+  // (nothing is in flight when the block ends)
+  wait(m, &m->o_full, w.piece & 1);
 }
 
 // --- softmax --------------------------------------------------------------------
@@ -503,13 +582,13 @@ __device__ __noinline__ void add_bad_values(const AttendParams& p, const Item& i
 
 // Scores of keys that the row does not see become -inf; of those that it
 // sees and whose factor is no number (poison), NaN.
-__device__ __forceinline__ void mask_scores(uint32_t s_at, const uint32_t* seen, const uint32_t* poison) {
+__device__ __forceinline__ void mask_scores(uint32_t s_at, const uint32_t (&seen)[2], const uint32_t* poison) {
 #pragma unroll 1
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 2; ++i) {
     uint32_t s[32];
     tmem_load32(s_at + 32 * i, s);
     tmem_wait_load(s);
-    const uint32_t bits = i == 0 ? seen[0] : i == 1 ? seen[1] : i == 2 ? seen[2] : seen[3], bad = bits & poison[i];
+    const uint32_t bits = i == 0 ? seen[0] : seen[1], bad = bits & poison[i];
 #pragma unroll
     for (int j = 0; j < 32; ++j) s[j] = bits >> j & 1 ? (bad >> j & 1 ? 0x7fc00000u : s[j]) : 0xff800000u;
     tmem_store32(s_at + 32 * i, s);
@@ -517,77 +596,51 @@ __device__ __forceinline__ void mask_scores(uint32_t s_at, const uint32_t* seen,
   tmem_wait_store();
 }
 
-// The largest score (times c) of a row.
-template <int KV>
-__device__ __forceinline__ float largest(uint32_t s_at, const float* factors, float c) {
-  float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-  uint32_t s[2][32];
-  tmem_load32(s_at, s[0]);
+// 32 scores times their keys' factors (an 8-bit cache).
+__device__ __forceinline__ void times_factors(uint32_t (&s)[32], const float* factors) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    tmem_wait_load(s[i & 1]);
-    if (i < 3) tmem_load32(s_at + 32 * (i + 1), s[(i + 1) & 1]);
-#pragma unroll
-    for (int j = 0; j < 32; j += 4) {
-      float x[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(s[i & 1][j + e]);
-      if constexpr (KV != SJD_BF16) {
-        const float4 f = *reinterpret_cast<const float4*>(factors + 32 * i + j);
-        const float2 u = halves(mul2(pair(x[0], x[1]), pair(f.x, f.y))), v = halves(mul2(pair(x[2], x[3]), pair(f.z, f.w)));
-        x[0] = u.x, x[1] = u.y, x[2] = v.x, x[3] = v.y;
-      }
-      top[j / 4 & 1] = max3(top[j / 4 & 1], x[0], x[1]);
-      top[2 + (j / 4 & 1)] = max3(top[2 + (j / 4 & 1)], x[2], x[3]);
-    }
+  for (int j = 0; j < 32; j += 4) {
+    const float4 f = *reinterpret_cast<const float4*>(factors + j);
+    const float2 u = halves(mul2(pair(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), pair(f.x, f.y)));
+    const float2 v = halves(mul2(pair(__uint_as_float(s[j + 2]), __uint_as_float(s[j + 3])), pair(f.z, f.w)));
+    s[j] = __float_as_uint(u.x), s[j + 1] = __float_as_uint(u.y), s[j + 2] = __float_as_uint(v.x), s[j + 3] = __float_as_uint(v.y);
   }
-  const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-  return KV == SJD_BF16 ? t * c : t;
 }
-
-// A row's weights against `base`, written over the scores as bf16 (32 scores
-// are in registers before the first 16 columns of weights are written, and
-// the weights stay behind the scores), and their sum.
-template <int KV>
-__device__ __forceinline__ float weights(uint32_t s_at, const float* factors_k, const float* factors_v, float c, float base) {
-  const Pair c2 = pair(c, c), less = pair(-base, -base);
-  Pair sum[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
-  uint32_t s[2][32];
-  tmem_load32(s_at, s[0]);
+__device__ __forceinline__ float largest_of(const uint32_t (&s)[32], float t) {
+  float top[4] = {t, t, t, t};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t out[16];
-    tmem_wait_load(s[i & 1]);
-    if (i < 3) tmem_load32(s_at + 32 * (i + 1), s[(i + 1) & 1]);
+  for (int j = 0; j < 32; j += 8) {
 #pragma unroll
-    for (int j = 0; j < 32; j += 4) {
-      float4 fk, fv;
-      if constexpr (KV != SJD_BF16) {
-        fk = *reinterpret_cast<const float4*>(factors_k + 32 * i + j);
-        fv = *reinterpret_cast<const float4*>(factors_v + 32 * i + j);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; e += 2) {
-        const Pair t = pair(__uint_as_float(s[i & 1][j + e]), __uint_as_float(s[i & 1][j + e + 1]));
-        const float2 d = halves(fma2(t, KV == SJD_BF16 ? c2 : e ? pair(fk.z, fk.w) : pair(fk.x, fk.y), less));
-        const Pair w = pair(exp2_fast(d.x), exp2_fast(d.y));
-        sum[e / 2] = add2(sum[e / 2], w);
-        const float2 v = halves(KV == SJD_BF16 ? w : mul2(w, e ? pair(fv.z, fv.w) : pair(fv.x, fv.y)));
-        out[(j + e) / 2] = pack_bf16(v.x, v.y);
-      }
-    }
-    tmem_store16(s_at + 16 * i, out);
+    for (int e = 0; e < 4; ++e) top[e] = max3(top[e], __uint_as_float(s[j + 2 * e]), __uint_as_float(s[j + 2 * e + 1]));
   }
-  const float2 a = halves(add2(sum[0], sum[1]));
-  return a.x + a.y;
+  return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+}
+// The weights of 32 scores against `base`, packed to bf16, in an 8-bit cache
+// times the values' factors; and their sum.
+template <int KV>
+__device__ __forceinline__ void weights_of(const uint32_t (&s)[32], const float* factors, float c, float base, uint32_t (&out)[16], Pair (&sum)[2]) {
+  const Pair c2 = pair(c, c), less = pair(-base, -base);
+#pragma unroll
+  for (int j = 0; j < 32; j += 4) {
+    float4 f;
+    if constexpr (KV != SJD_BF16) f = *reinterpret_cast<const float4*>(factors + j);
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {
+      const Pair t = pair(__uint_as_float(s[j + e]), __uint_as_float(s[j + e + 1]));
+      const float2 d = halves(KV == SJD_BF16 ? fma2(t, c2, less) : add2(t, less));
+      const Pair w = pair(exp2_fast(d.x), exp2_fast(d.y));
+      sum[e / 2] = add2(sum[e / 2], w);
+      const float2 v = halves(KV == SJD_BF16 ? w : mul2(w, e ? pair(f.z, f.w) : pair(f.x, f.y)));
+      out[(j + e) / 2] = pack_bf16(v.x, v.y);
+    }
+  }
 }
 
 template <int KV, int DP, int NM>
-__device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m, uint32_t smem, uint32_t tmem, float* parts, float2* part_rows, Shared* shared) {
-  using P = Plan<KV, DP, NM>;
+__device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m, uint32_t tmem, float* parts, float2* part_rows, Shared* shared) {
   const int slot = threadIdx.x / 128, row = threadIdx.x & 127, warp_row = row & ~31;
   const uint32_t lanes = static_cast<uint32_t>(warp_row) << 16;
-  const uint32_t s_at = tmem + lanes + slot * kTile, o_at = tmem + lanes + kOColumn;
+  const uint32_t o_at = tmem + lanes + kOColumn;
   const int G = p.c.group;
   // log2 e: weights are powers of two. (The factors are never 0: times a score of -inf they are -inf.)
   const float c = fmaxf(fabsf(p.scale) * 1.4426950408889634f, kLeast);
@@ -598,12 +651,12 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
   if (row == 0) w.begin(p, m->start);
   named_barrier(2 + slot, 128);
   int tile_no = 0;  // the block's number of the piece's first tile
-  uint32_t sp = 0;
+  uint32_t sp = 0;  // bit h: parity of s_full[slot][h]; it is also that of o_done before the half's next product
   for (;;) {
     const int r0 = it.mt * (kTile * NM) + (NM == 2 ? slot * kTile : 0);
     const bool valid = r0 + row < it.rows, active = r0 + warp_row < it.rows;
     const int t = by_group(p.c, r0 + row);
-    const int units = NM == 2 ? w.k1 - w.k0 : (w.k1 - w.k0 + 1 - slot) / 2;
+    const int units = units_of(w, slot);
     constexpr int stride = NM == 2 ? 1 : 2;
     const int k_first = w.k0 + (NM == 2 ? 0 : slot);
     // keys below `whole` are seen, those from `limit` on are not (a given mask tells between)
@@ -611,37 +664,16 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     const int whole = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_GIVEN ? it.start : limit;
     const int common = common_keys<NM>(p, it);
     float ref = -INFINITY, sum = 0.0f;
-    // this slot's products; unit u is the block's tile `tile0` + u * stride
-    const int tile0 = tile_no + (NM == 2 ? 0 : slot);
-    auto scores = [&](int u) {
-      const int tile = tile0 + u * stride, stage = tile % P::kK;
-      wait(m, &m->k_full[stage], tile / P::kK & 1);
-      tc_fence_after();
-      issue_scores<DP>(tmem + slot * kTile, smem + (NM == 2 ? slot * tile_bytes(DP) : 0), smem + P::kAtK + stage * tile_bytes(DP));
-      mma_commit(smem_addr(&m->s_full[slot]));
-      mma_commit(smem_addr(&m->k_empty[stage]));
-      if (u + 1 == units) mma_commit(smem_addr(&m->q_empty));
-    };
-    if (row == 0) {
-      if (units > 0) {
-        wait(m, &m->q_full, w.piece & 1);
-        scores(0);
-      } else {
-        mbar_arrive(smem_addr(&m->q_empty));
-        mbar_arrive(smem_addr(&m->o_full));
-      }
-    }
-    __syncwarp();
     // an 8-bit cache's factors of key `row` of the tiles: the next tile's are on their way while
     // one is worked on, and the page of the one after that
     float next_k = 0.0f, next_v = 0.0f;
     int page = kNoPage;
-    auto factors = [&](int u) {
-      const int key = (k_first + u * stride) * kTile + row;
+    auto factors = [&](int tile) {  // the slot's tile-th
+      const int key = (k_first + tile * stride) * kTile + row;
       const uint32_t at = vector_in(p.c, page, key, it.kvh);
       next_k = next_v = 0.0f;
       if (at != kNoVector) next_k = p.c.ks[at], next_v = p.c.vs[at];
-      page = u + 1 < units ? key_page(p.c, it, key + stride * kTile) : kNoPage;
+      page = 2 * tile + 2 < units ? key_page(p.c, it, key + stride * kTile) : kNoPage;
     };
     if (KV != SJD_BF16 && units > 0) {
       page = key_page(p.c, it, k_first * kTile + row);
@@ -649,37 +681,41 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     }
 #pragma unroll 1
     for (int u = 0; u < units; ++u) {
-      const int key0 = (k_first + u * stride) * kTile;
+      const int h = u & 1, tile_key = (k_first + u / 2 * stride) * kTile, key0 = tile_key + h * kHalf;
       if constexpr (KV != SJD_BF16) {
-        // a factor that is no number would reach rows that do not see its key: it is set aside
-        // in tiles where there can be such rows (the values' are given to the others at the end)
-        const bool apart = key0 + kTile > common;
-        const bool bad_k = apart && next_k != next_k, bad_v = apart && next_v != next_v;
-        m->row[slot][0][row] = bad_k ? kLeast : fmaxf(next_k * c, next_k == next_k ? kLeast : next_k);
-        m->row[slot][1][row] = bad_v ? 0.0f : next_v;
-        const unsigned poison = __ballot_sync(0xffffffffu, bad_k);
-        if ((threadIdx.x & 31) == 0) m->poison[slot][row / 32] = poison;
-        if (bad_v) m->bad_values[w.piece & 3] = w.piece + 1;
-        named_barrier(2 + slot, 128);
-        if (u + 1 < units) factors(u + 1);
+        if (h == 0) {
+          // a factor that is no number would reach rows that do not see its key: it is set aside
+          // in tiles where there can be such rows (the values' are given to the others at the end)
+          const bool apart = tile_key + kTile > common;
+          const bool bad_k = apart && next_k != next_k, bad_v = apart && next_v != next_v;
+          named_barrier(2 + slot, 128);  // all have used the factors of the tile before
+          m->row[slot][0][row] = bad_k ? kLeast : fmaxf(next_k * c, next_k == next_k ? kLeast : next_k);
+          m->row[slot][1][row] = bad_v ? 0.0f : next_v;
+          const unsigned poison = __ballot_sync(0xffffffffu, bad_k);
+          if ((threadIdx.x & 31) == 0) m->poison[slot][row / 32] = poison;
+          if (bad_v) m->bad_values[w.piece & 3] = w.piece + 1;
+          named_barrier(2 + slot, 128);
+          if (u + 2 < units) factors(u / 2 + 1);
+        }
       }
-      wait(m, &m->s_full[slot], sp);
-      sp ^= 1;
+      wait(m, &m->s_full[slot][h], sp >> h & 1);
+      sp ^= 1u << h;
       tc_fence_after();
       if (active) {
-        const uint32_t* poison = m->poison[slot];
-        const bool mixed = !__all_sync(0xffffffffu, key0 + kTile <= whole) || (KV != SJD_BF16 && (poison[0] | poison[1] | poison[2] | poison[3]));
+        const uint32_t s_at = tmem + lanes + slot * kTile + h * kHalf;
+        const uint32_t* poison = m->poison[slot] + 2 * h;
+        const bool mixed = !__all_sync(0xffffffffu, key0 + kHalf <= whole) || (KV != SJD_BF16 && (poison[0] | poison[1]));
         if (mixed) {
-          uint32_t seen[4];
+          uint32_t seen[2];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < 2; ++i) {
             const int n = limit - (key0 + 32 * i);
             seen[i] = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
           }
           if (p.mask_kind == SJD_MASK_GIVEN && valid) {
             const uint8_t* mask = p.mask + p.mask_b * it.b + p.mask_r * t - it.start;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 2; ++i) {
               const int a = max(key0 + 32 * i, it.start), e = min(key0 + 32 * i + 32, it.keys);
 #pragma unroll 1
               for (int key = a; key < e; ++key)
@@ -689,45 +725,68 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
           __syncwarp();
           mask_scores(s_at, seen, poison);
         }
-        const float* fk = m->row[slot][0];
-        const float* fv = m->row[slot][1];
+        // Two times 32 scores; those of an 8-bit cache are read and multiplied twice, since
+        // their factors' registers and 64 scores do not fit a thread.
+        const float* fk = m->row[slot][0] + h * kHalf;
+        const float* fv = m->row[slot][1] + h * kHalf;
+        uint32_t s0[32], s1[32];
+        tmem_load32(s_at, s0);
+        tmem_wait_load(s0);
+        if (KV == SJD_BF16) tmem_load32(s_at + 32, s1);
+        else times_factors(s0, fk);
+        float top = largest_of(s0, -INFINITY);
+        if (KV != SJD_BF16) tmem_load32(s_at + 32, s1);
+        tmem_wait_load(s1);
+        if (KV != SJD_BF16) times_factors(s1, fk + 32);
+        top = largest_of(s1, top);
+        if (KV == SJD_BF16) top *= c;
         // The reference that the weights are taken against moves only where a
         // weight could pass 2^8: their relative precision is the same below
         // that, and O is left alone.
-        const float top = largest<KV>(s_at, fk, c);
         const bool move = top > ref + kRise || (ref == -INFINITY && top != -INFINITY);
         if (__any_sync(0xffffffffu, move)) {
           const float f = !move ? 1.0f : ref == -INFINITY ? 0.0f : exp2_fast(ref - top);
           if (move) ref = top, sum *= f;
           __syncwarp();
           if (u > 0) {
+            // the product before this one is to be done (the one of this half, two units ago, is)
+            wait(m, &m->o_done[slot][h ^ 1], (sp >> (h ^ 1) & 1) ^ 1);
+            tc_fence_after();
 #pragma unroll 1
-            for (int i = 0; i < DP / 32; ++i) {
-              uint32_t o[32];
-              tmem_load32(o_at + slot * DP + 32 * i, o);
+            for (int i = 0; i < DP / 16; ++i) {
+              uint32_t o[16];
+              tmem_load16(o_at + slot * DP + 16 * i, o);
               tmem_wait_load(o);
 #pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tmem_store32(o_at + slot * DP + 32 * i, o);
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_store16(o_at + slot * DP + 16 * i, o);
             }
           }
         }
         const float base = ref == -INFINITY ? 0.0f : ref;
-        sum += weights<KV>(s_at, fk, fv, c, base);
+        Pair total[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+        uint32_t out[16];
+        if (KV != SJD_BF16) {
+          tmem_load32(s_at, s0);
+          tmem_wait_load(s0);
+          times_factors(s0, fk);
+        }
+        weights_of<KV>(s0, fv, c, base, out, total);
+        if (KV != SJD_BF16) tmem_load32(s_at + 32, s1);
+        tmem_store16(s_at, out);
+        if (KV != SJD_BF16) {
+          tmem_wait_load(s1);
+          times_factors(s1, fk + 32);
+        }
+        weights_of<KV>(s1, fv + 32, c, base, out, total);
+        tmem_store16(s_at + 16, out);
+        const float2 ends = halves(add2(total[0], total[1]));
+        sum += ends.x + ends.y;
         tmem_wait_store();
         tc_fence_before();
       }
-      named_barrier(4 + slot, 128);  // all weights are there, and the factors were used
-      if (row == 0) {
-        const int tile = tile0 + u * stride, stage = tile % P::kV;
-        wait(m, &m->v_full[stage], tile / P::kV & 1);
-        tc_fence_after();
-        issue_values<DP>(o_at + slot * DP, tmem + slot * kTile, smem + P::kAtV + stage * tile_bytes(DP), u > 0);
-        mma_commit(smem_addr(&m->v_empty[stage]));
-        if (u + 1 < units) scores(u + 1);
-        else mma_commit(smem_addr(&m->o_full));
-      }
       __syncwarp();
+      if ((threadIdx.x & 31) == 0) mbar_arrive(smem_addr(&m->p_full[slot][h]));
     }
     // the end of the piece: O of both slots is complete
     wait(m, &m->o_full, w.piece & 1);
@@ -736,6 +795,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     const int tiles = w.k1 - w.k0;
     const bool take[2] = {NM == 1 || slot == 0, NM == 1 ? tiles > 1 : slot == 1};
     if constexpr (NM == 1) {
+      named_barrier(2 + slot, 128);  // (the factors are done with)
       m->row[slot][0][row] = ref;
       m->row[slot][1][row] = sum;
       named_barrier(1, 256);
@@ -827,18 +887,21 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
   using P = Plan<KV, DP, NM>;
   Misc<NM>* m = reinterpret_cast<Misc<NM>*>(raw + P::kAtMisc);
   const uint32_t smem = smem_addr(raw);
-  const int warp = threadIdx.x / 32;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0);  // (the same for all lanes, to the compiler too)
   let_next_start();
   wait_for_previous();
   if (warp == 0) locate<NM>(p, &m->start);
-  if (warp == 4) tmem_alloc(smem_addr(&m->tmem), kTmemColumns);
+  if (warp == kMmaWarp) tmem_alloc(smem_addr(&m->tmem), kTmemColumns);
   if (threadIdx.x == 256) {
     for (int i = 0; i < 5; ++i) {
-      mbar_init(smem_addr(&m->k_full[i]), 4), mbar_init(smem_addr(&m->k_empty[i]), NM);
-      mbar_init(smem_addr(&m->v_full[i]), 4), mbar_init(smem_addr(&m->v_empty[i]), NM);
+      mbar_init(smem_addr(&m->k_full[i]), 4), mbar_init(smem_addr(&m->k_empty[i]), 1);
+      mbar_init(smem_addr(&m->v_full[i]), 4), mbar_init(smem_addr(&m->v_empty[i]), 1);
     }
-    mbar_init(smem_addr(&m->q_full), 4), mbar_init(smem_addr(&m->q_empty), 2), mbar_init(smem_addr(&m->o_full), 2);
-    for (int i = 0; i < 2; ++i) mbar_init(smem_addr(&m->s_full[i]), 1);
+    mbar_init(smem_addr(&m->q_full), 4), mbar_init(smem_addr(&m->q_empty), 1), mbar_init(smem_addr(&m->o_full), 1);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(smem_addr(&m->s_full[i / 2][i & 1]), 1), mbar_init(smem_addr(&m->p_full[i / 2][i & 1]), 4);
+      mbar_init(smem_addr(&m->o_done[i / 2][i & 1]), 1);
+    }
     m->abort = 0;
     for (int i = 0; i < 4; ++i) m->bad_values[i] = m->poison[0][i] = m->poison[1][i] = 0;
     shared[blockIdx.x].parts = 0;
@@ -848,12 +911,18 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = m->tmem;
-  if (warp < 8) softmax_rows<KV, DP, NM>(p, m, smem, tmem, parts, part_rows, shared);
-  else if (warp < 12) load_operand<KV, DP, NM, false>(p, m, smem);
-  else load_operand<KV, DP, NM, true>(p, m, smem);
+  if (warp < 8) {
+    softmax_rows<KV, DP, NM>(p, m, tmem, parts, part_rows, shared);
+  } else if (warp < 12) {
+    load_operand<KV, DP, NM, false>(p, m, smem);
+  } else if (warp < 16) {
+    load_operand<KV, DP, NM, true>(p, m, smem);
+  } else {
+    issue_products<KV, DP, NM>(p, m, smem, tmem);
+  }
   tc_fence_before();
   __syncthreads();
-  if (warp == 4) {
+  if (warp == kMmaWarp) {
     tc_fence_after();
     tmem_free(tmem, kTmemColumns);
   }
