@@ -21,9 +21,9 @@
 // slot: with NM = 1 the even and the odd tiles of the same 128 rows (each with
 // an accumulator of its own, joined at the end), with NM = 2 the two halves
 // of 256 rows. 8-11 load keys, 12-15 the queries and values, and warp 16
-// issues the products. A slot goes through a tile in two halves of
-// 64 keys with a place for scores each, so that one half's scores are made
-// while the other's softmax runs.
+// issues the products: those of one slot run while the other's softmax does.
+// A slot's weights are handed over in two halves of 64 keys, the second made
+// while the first is multiplied.
 
 #include <cfloat>
 
@@ -35,10 +35,10 @@ namespace sjd_kv_ops {
 namespace {
 
 constexpr int kTile = 128;              // rows of a product, and keys of a tile
-constexpr int kHalf = kTile / 2;        // keys of a unit
+constexpr int kHalf = kTile / 2;        // keys whose weights are handed over at a time
 constexpr int kAttendThreads = 17 * 32;
 constexpr int kMmaWarp = 16;
-constexpr uint32_t kTmemColumns = 512;  // S of the two slots, two halves each (P over them), then O of the two
+constexpr uint32_t kTmemColumns = 512;  // S of the two slots (P over them), then O of the two
 constexpr uint32_t kOColumn = 2 * kTile;
 constexpr long long kWaitClocks = 4000000000ll;  // about two seconds
 constexpr float kLeast = 1e-30f;
@@ -146,7 +146,7 @@ struct Walk {
 template <int NM>
 struct Misc {
   unsigned long long k_full[5], k_empty[5], v_full[5], v_empty[5], q_full, q_empty, o_full,
-      s_full[2][2], p_full[2][2], o_done[2][2];  // by slot and half
+      s_full[2], p_full[2][2];  // by slot (and half)
   uint32_t tmem;
   int abort;
   int bad_values[4];       // number of the piece (modulo 4) in which a value that some rows do not see is not finite
@@ -476,77 +476,63 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
 
 // --- products -------------------------------------------------------------------
 
-// Units of 64 keys of a slot in a piece (the item's last tile may end in its first half).
-template <int NM>
-__device__ __forceinline__ int units_of(const Walk<NM>& w, int slot) {
-  const int tiles = w.k1 - w.k0, own = NM == 2 ? tiles : (tiles + 1 - slot) / 2;
-  const bool last = NM == 2 || ((tiles - 1) & 1) == slot;  // the piece's last tile is the slot's
-  return 2 * own - (last && w.it.keys - (w.k1 - 1) * kTile <= kHalf ? 1 : 0);
-}
-
 // One warp issues the products of both slots, the slots in turn.
 template <int KV, int DP, int NM>
 __device__ __forceinline__ void issue_products(const AttendParams& p, Misc<NM>* m, uint32_t smem, uint32_t tmem) {
   using P = Plan<KV, DP, NM>;
-  constexpr uint32_t kScores = product_kind(kTile, kHalf, false), kValues = product_kind(kTile, DP, true);
+  constexpr uint32_t kScores = product_kind(kTile, kTile, false), kValues = product_kind(kTile, DP, true);
   const bool lead = elect_lane();
   Walk<NM> w;
   if (!w.begin(p, m->start)) return;
   int tile0 = 0;              // the block's number of the piece's first tile
-  uint32_t pp[2] = {0, 0};    // per slot, bit h: parity of p_full[slot][h]
+  uint32_t pp = 0;            // bit 2 * slot + h: parity of p_full[slot][h]
   do {
-    const int units[2] = {units_of(w, 0), units_of(w, 1)};
-    int left = units[0] + units[1];  // scores to be issued
-    auto tile_at = [&](int slot, int u) { return tile0 + (NM == 2 ? u / 2 : u / 2 * 2 + slot); };
-    // S of a slot and half = Q K^T
-    auto scores = [&](int slot, int u) {
-      const int tile = tile_at(slot, u), stage = tile % P::kK, h = u & 1;
-      if (h == 0 && (NM == 1 || slot == 0)) wait(m, &m->k_full[stage], tile / P::kK & 1);
+    const int tiles = w.k1 - w.k0, turns = NM * tiles;  // of a slot and a tile, the slots in turn
+    const bool half = w.it.keys - (w.k1 - 1) * kTile <= kHalf;  // of the piece's last tile
+    // S of a slot = Q K^T
+    auto scores = [&](int turn) {
+      const int slot = turn & 1, tile = tile0 + turn / NM, stage = tile % P::kK;
+      if (NM == 1 || slot == 0) wait(m, &m->k_full[stage], tile / P::kK & 1);
       tc_fence_after();
-      const uint32_t q = smem + (NM == 2 ? slot * tile_bytes(DP) : 0), k = smem + P::kAtK + stage * tile_bytes(DP) + h * (kHalf * 128);
-      --left;
+      const uint32_t q = smem + (NM == 2 ? slot * tile_bytes(DP) : 0), k = smem + P::kAtK + stage * tile_bytes(DP);
       if (lead) {
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
           const uint32_t at = (i / 4) * (kTile * 128) + (i % 4) * 32;
-          mma_ss(tmem + slot * kTile + h * kHalf, operand_k(q + at), operand_k(k + at), kScores, i > 0);
+          mma_ss(tmem + slot * kTile, operand_k(q + at), operand_k(k + at), kScores, i > 0);
         }
-        mma_commit(smem_addr(&m->s_full[slot][h]));
-        if ((h == 1 || u + 1 == units[slot]) && (NM == 1 || slot == 1)) mma_commit(smem_addr(&m->k_empty[stage]));
-        if (left == 0) mma_commit(smem_addr(&m->q_empty));
+        mma_commit(smem_addr(&m->s_full[slot]));
+        if (NM == 1 || slot == 1) mma_commit(smem_addr(&m->k_empty[stage]));
+        if (turn + 1 == turns) mma_commit(smem_addr(&m->q_empty));
       }
       __syncwarp();
     };
     wait(m, &m->q_full, w.piece & 1);
-    for (int u = 0; u < 2; ++u)
-      for (int slot = 0; slot < 2; ++slot)
-        if (u < units[slot]) scores(slot, u);
-    for (int u = 0; u < units[0] || u < units[1]; ++u) {
-      const int h = u & 1;
-#pragma unroll
-      for (int slot = 0; slot < 2; ++slot) {
-        if (u >= units[slot]) continue;
-        const int tile = tile_at(slot, u), stage = tile % P::kV;
-        if (h == 0 && (NM == 1 || slot == 0)) wait(m, &m->v_full[stage], tile / P::kV & 1);
-        wait(m, &m->p_full[slot][h], pp[slot] >> h & 1);
-        pp[slot] ^= 1u << h;
+    scores(0);
+    if (turns > 1) scores(1);
+    for (int turn = 0; turn < turns; ++turn) {
+      const int slot = turn & 1, tile = tile0 + turn / NM, stage = tile % P::kV;
+      const int halves = half && turn / NM + 1 == tiles ? 1 : 2;
+      if (NM == 1 || slot == 0) wait(m, &m->v_full[stage], tile / P::kV & 1);
+      for (int h = 0; h < halves; ++h) {
+        wait(m, &m->p_full[slot][h], pp >> (2 * slot + h) & 1);
+        pp ^= 1u << (2 * slot + h);
         tc_fence_after();
         // O of a slot += P V; P lies over S, two weights to a column
-        const uint32_t v = smem + P::kAtV + stage * tile_bytes(DP) + h * (kHalf * 128);
+        const uint32_t v = smem + P::kAtV + stage * tile_bytes(DP) + h * (kHalf * 128), from = tmem + slot * kTile + h * (kHalf / 2);
         if (lead) {
 #pragma unroll
           for (int i = 0; i < kHalf / 16; ++i)
-            mma_ts(tmem + kOColumn + slot * DP, tmem + slot * kTile + h * kHalf + i * 8, operand_n(v + i * 2048, kTile * 128), kValues, u > 0 || i > 0);
-          mma_commit(smem_addr(&m->o_done[slot][h]));
-          if ((h == 1 || u + 1 == units[slot]) && (NM == 1 || slot == 1)) mma_commit(smem_addr(&m->v_empty[stage]));
+            mma_ts(tmem + kOColumn + slot * DP, from + i * 8, operand_n(v + i * 2048, kTile * 128), kValues, turn >= 2 || h > 0 || i > 0);
+          if (h + 1 == halves && (NM == 1 || slot == 1)) mma_commit(smem_addr(&m->v_empty[stage]));
         }
         __syncwarp();
-        if (u + 2 < units[slot]) scores(slot, u + 2);
       }
+      if (turn + 2 < turns) scores(turn + 2);
     }
     if (lead) mma_commit(smem_addr(&m->o_full));
     __syncwarp();
-    tile0 += w.k1 - w.k0;
+    tile0 += tiles;
   } while (w.next(p));
   // (nothing is in flight when the block ends)
   wait(m, &m->o_full, w.piece & 1);
@@ -582,13 +568,13 @@ __device__ __noinline__ void add_bad_values(const AttendParams& p, const Item& i
 
 // Scores of keys that the row does not see become -inf; of those that it
 // sees and whose factor is no number (poison), NaN.
-__device__ __forceinline__ void mask_scores(uint32_t s_at, const uint32_t (&seen)[2], const uint32_t* poison) {
+__device__ __forceinline__ void mask_scores(uint32_t s_at, const uint32_t (&seen)[4], const uint32_t* poison) {
 #pragma unroll 1
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < 4; ++i) {
     uint32_t s[32];
     tmem_load32(s_at + 32 * i, s);
     tmem_wait_load(s);
-    const uint32_t bits = i == 0 ? seen[0] : seen[1], bad = bits & poison[i];
+    const uint32_t bits = i == 0 ? seen[0] : i == 1 ? seen[1] : i == 2 ? seen[2] : seen[3], bad = bits & poison[i];
 #pragma unroll
     for (int j = 0; j < 32; ++j) s[j] = bits >> j & 1 ? (bad >> j & 1 ? 0x7fc00000u : s[j]) : 0xff800000u;
     tmem_store32(s_at + 32 * i, s);
@@ -640,7 +626,7 @@ template <int KV, int DP, int NM>
 __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m, uint32_t tmem, float* parts, float2* part_rows, Shared* shared) {
   const int slot = threadIdx.x / 128, row = threadIdx.x & 127, warp_row = row & ~31;
   const uint32_t lanes = static_cast<uint32_t>(warp_row) << 16;
-  const uint32_t o_at = tmem + lanes + kOColumn;
+  const uint32_t s_at = tmem + lanes + slot * kTile, o_at = tmem + lanes + kOColumn;
   const int G = p.c.group;
   // log2 e: weights are powers of two. (The factors are never 0: times a score of -inf they are -inf.)
   const float c = fmaxf(fabsf(p.scale) * 1.4426950408889634f, kLeast);
@@ -651,12 +637,12 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
   if (row == 0) w.begin(p, m->start);
   named_barrier(2 + slot, 128);
   int tile_no = 0;  // the block's number of the piece's first tile
-  uint32_t sp = 0;  // bit h: parity of s_full[slot][h]; it is also that of o_done before the half's next product
+  uint32_t sp = 0;
   for (;;) {
     const int r0 = it.mt * (kTile * NM) + (NM == 2 ? slot * kTile : 0);
     const bool valid = r0 + row < it.rows, active = r0 + warp_row < it.rows;
     const int t = by_group(p.c, r0 + row);
-    const int units = units_of(w, slot);
+    const int units = NM == 2 ? w.k1 - w.k0 : (w.k1 - w.k0 + 1 - slot) / 2;  // tiles of the slot
     constexpr int stride = NM == 2 ? 1 : 2;
     const int k_first = w.k0 + (NM == 2 ? 0 : slot);
     // keys below `whole` are seen, those from `limit` on are not (a given mask tells between)
@@ -668,12 +654,12 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     // one is worked on, and the page of the one after that
     float next_k = 0.0f, next_v = 0.0f;
     int page = kNoPage;
-    auto factors = [&](int tile) {  // the slot's tile-th
-      const int key = (k_first + tile * stride) * kTile + row;
+    auto factors = [&](int u) {
+      const int key = (k_first + u * stride) * kTile + row;
       const uint32_t at = vector_in(p.c, page, key, it.kvh);
       next_k = next_v = 0.0f;
       if (at != kNoVector) next_k = p.c.ks[at], next_v = p.c.vs[at];
-      page = 2 * tile + 2 < units ? key_page(p.c, it, key + stride * kTile) : kNoPage;
+      page = u + 1 < units ? key_page(p.c, it, key + stride * kTile) : kNoPage;
     };
     if (KV != SJD_BF16 && units > 0) {
       page = key_page(p.c, it, k_first * kTile + row);
@@ -681,41 +667,39 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     }
 #pragma unroll 1
     for (int u = 0; u < units; ++u) {
-      const int h = u & 1, tile_key = (k_first + u / 2 * stride) * kTile, key0 = tile_key + h * kHalf;
+      const int key0 = (k_first + u * stride) * kTile;
+      const bool two = it.keys - key0 > kHalf;  // halves of the tile
       if constexpr (KV != SJD_BF16) {
-        if (h == 0) {
-          // a factor that is no number would reach rows that do not see its key: it is set aside
-          // in tiles where there can be such rows (the values' are given to the others at the end)
-          const bool apart = tile_key + kTile > common;
-          const bool bad_k = apart && next_k != next_k, bad_v = apart && next_v != next_v;
-          named_barrier(2 + slot, 128);  // all have used the factors of the tile before
-          m->row[slot][0][row] = bad_k ? kLeast : fmaxf(next_k * c, next_k == next_k ? kLeast : next_k);
-          m->row[slot][1][row] = bad_v ? 0.0f : next_v;
-          const unsigned poison = __ballot_sync(0xffffffffu, bad_k);
-          if ((threadIdx.x & 31) == 0) m->poison[slot][row / 32] = poison;
-          if (bad_v) m->bad_values[w.piece & 3] = w.piece + 1;
-          named_barrier(2 + slot, 128);
-          if (u + 2 < units) factors(u / 2 + 1);
-        }
+        // a factor that is no number would reach rows that do not see its key: it is set aside
+        // in tiles where there can be such rows (the values' are given to the others at the end)
+        const bool apart = key0 + kTile > common;
+        const bool bad_k = apart && next_k != next_k, bad_v = apart && next_v != next_v;
+        named_barrier(2 + slot, 128);  // all have used the factors of the tile before
+        m->row[slot][0][row] = bad_k ? kLeast : fmaxf(next_k * c, next_k == next_k ? kLeast : next_k);
+        m->row[slot][1][row] = bad_v ? 0.0f : next_v;
+        const unsigned poison = __ballot_sync(0xffffffffu, bad_k);
+        if ((threadIdx.x & 31) == 0) m->poison[slot][row / 32] = poison;
+        if (bad_v) m->bad_values[w.piece & 3] = w.piece + 1;
+        named_barrier(2 + slot, 128);
+        if (u + 1 < units) factors(u + 1);
       }
-      wait(m, &m->s_full[slot][h], sp >> h & 1);
-      sp ^= 1u << h;
+      wait(m, &m->s_full[slot], sp);
+      sp ^= 1;
       tc_fence_after();
       if (active) {
-        const uint32_t s_at = tmem + lanes + slot * kTile + h * kHalf;
-        const uint32_t* poison = m->poison[slot] + 2 * h;
-        const bool mixed = !__all_sync(0xffffffffu, key0 + kHalf <= whole) || (KV != SJD_BF16 && (poison[0] | poison[1]));
+        const uint32_t* poison = m->poison[slot];
+        const bool mixed = !__all_sync(0xffffffffu, key0 + kTile <= whole) || (KV != SJD_BF16 && (poison[0] | poison[1] | poison[2] | poison[3]));
         if (mixed) {
-          uint32_t seen[2];
+          uint32_t seen[4];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
+          for (int i = 0; i < 4; ++i) {
             const int n = limit - (key0 + 32 * i);
             seen[i] = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
           }
           if (p.mask_kind == SJD_MASK_GIVEN && valid) {
             const uint8_t* mask = p.mask + p.mask_b * it.b + p.mask_r * t - it.start;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < 4; ++i) {
               const int a = max(key0 + 32 * i, it.start), e = min(key0 + 32 * i + 32, it.keys);
 #pragma unroll 1
               for (int key = a; key < e; ++key)
@@ -725,20 +709,23 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
           __syncwarp();
           mask_scores(s_at, seen, poison);
         }
-        // Two times 32 scores; those of an 8-bit cache are read and multiplied twice, since
-        // their factors' registers and 64 scores do not fit a thread.
-        const float* fk = m->row[slot][0] + h * kHalf;
-        const float* fv = m->row[slot][1] + h * kHalf;
-        uint32_t s0[32], s1[32];
-        tmem_load32(s_at, s0);
-        tmem_wait_load(s0);
-        if (KV == SJD_BF16) tmem_load32(s_at + 32, s1);
-        else times_factors(s0, fk);
-        float top = largest_of(s0, -INFINITY);
-        if (KV != SJD_BF16) tmem_load32(s_at + 32, s1);
-        tmem_wait_load(s1);
-        if (KV != SJD_BF16) times_factors(s1, fk + 32);
-        top = largest_of(s1, top);
+        // The row's scores, 32 at a time (times their keys' factors in an 8-bit
+        // cache): first the largest, then the weights.
+        const float* fk = m->row[slot][0];
+        const float* fv = m->row[slot][1];
+        float top = -INFINITY;
+        uint32_t s[2][32];
+        tmem_load32(s_at, s[0]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i < 2 || two) {
+            tmem_wait_load(s[i & 1]);
+            if (i < 3) tmem_load32(s_at + 32 * (i + 1), s[(i + 1) & 1]);
+            if (KV != SJD_BF16) times_factors(s[i & 1], fk + 32 * i);
+            top = largest_of(s[i & 1], top);
+          }
+        }
+        if (!two) tmem_wait_load(s[0]);
         if (KV == SJD_BF16) top *= c;
         // The reference that the weights are taken against moves only where a
         // weight could pass 2^8: their relative precision is the same below
@@ -749,44 +736,44 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
           if (move) ref = top, sum *= f;
           __syncwarp();
           if (u > 0) {
-            // the product before this one is to be done (the one of this half, two units ago, is)
-            wait(m, &m->o_done[slot][h ^ 1], (sp >> (h ^ 1) & 1) ^ 1);
-            tc_fence_after();
 #pragma unroll 1
-            for (int i = 0; i < DP / 16; ++i) {
-              uint32_t o[16];
-              tmem_load16(o_at + slot * DP + 16 * i, o);
-              tmem_wait_load(o);
+            for (int i = 0; i < DP / 32; ++i) {
+              tmem_load32(o_at + slot * DP + 32 * i, s[0]);
+              tmem_wait_load(s[0]);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tmem_store16(o_at + slot * DP + 16 * i, o);
+              for (int j = 0; j < 32; ++j) s[0][j] = __float_as_uint(__uint_as_float(s[0][j]) * f);
+              tmem_store32(o_at + slot * DP + 32 * i, s[0]);
             }
           }
         }
         const float base = ref == -INFINITY ? 0.0f : ref;
         Pair total[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
-        uint32_t out[16];
-        if (KV != SJD_BF16) {
-          tmem_load32(s_at, s0);
-          tmem_wait_load(s0);
-          times_factors(s0, fk);
+        tmem_load32(s_at, s[0]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i < 2 || two) {
+            uint32_t out[16];
+            tmem_wait_load(s[i & 1]);
+            if (i < 3) tmem_load32(s_at + 32 * (i + 1), s[(i + 1) & 1]);
+            if (KV != SJD_BF16) times_factors(s[i & 1], fk + 32 * i);
+            weights_of<KV>(s[i & 1], fv + 32 * i, c, base, out, total);
+            tmem_store16(s_at + 16 * i, out);
+          }
+          if (i & 1) {
+            tmem_wait_store();
+            tc_fence_before();
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0 && (i == 1 || two)) mbar_arrive(smem_addr(&m->p_full[slot][i / 2]));
+          }
         }
-        weights_of<KV>(s0, fv, c, base, out, total);
-        if (KV != SJD_BF16) tmem_load32(s_at + 32, s1);
-        tmem_store16(s_at, out);
-        if (KV != SJD_BF16) {
-          tmem_wait_load(s1);
-          times_factors(s1, fk + 32);
-        }
-        weights_of<KV>(s1, fv + 32, c, base, out, total);
-        tmem_store16(s_at + 16, out);
+        if (!two) tmem_wait_load(s[0]);
         const float2 ends = halves(add2(total[0], total[1]));
         sum += ends.x + ends.y;
-        tmem_wait_store();
-        tc_fence_before();
+      } else if ((threadIdx.x & 31) == 0) {
+        mbar_arrive(smem_addr(&m->p_full[slot][0]));
+        if (two) mbar_arrive(smem_addr(&m->p_full[slot][1]));
       }
       __syncwarp();
-      if ((threadIdx.x & 31) == 0) mbar_arrive(smem_addr(&m->p_full[slot][h]));
     }
     // the end of the piece: O of both slots is complete
     wait(m, &m->o_full, w.piece & 1);
@@ -898,9 +885,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
       mbar_init(smem_addr(&m->v_full[i]), 4), mbar_init(smem_addr(&m->v_empty[i]), 1);
     }
     mbar_init(smem_addr(&m->q_full), 4), mbar_init(smem_addr(&m->q_empty), 1), mbar_init(smem_addr(&m->o_full), 1);
-    for (int i = 0; i < 4; ++i) {
-      mbar_init(smem_addr(&m->s_full[i / 2][i & 1]), 1), mbar_init(smem_addr(&m->p_full[i / 2][i & 1]), 4);
-      mbar_init(smem_addr(&m->o_done[i / 2][i & 1]), 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_addr(&m->s_full[i]), 1), mbar_init(smem_addr(&m->p_full[i][0]), 4), mbar_init(smem_addr(&m->p_full[i][1]), 4);
     }
     m->abort = 0;
     for (int i = 0; i < 4; ++i) m->bad_values[i] = m->poison[0][i] = m->poison[1][i] = 0;
