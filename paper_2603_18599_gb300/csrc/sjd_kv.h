@@ -77,6 +77,18 @@ struct AttendParams {
   float* lse;
 };
 
+// x / d = x * mul >> (31 + shift) for x < 2^31: shift = ceil(log2 d), mul =
+// ceil(2^(31 + shift) / d) is above the true factor by less than 2^-31 of it.
+struct Divisor {
+  uint32_t mul;
+  int shift;
+};
+inline Divisor divisor(int d) {
+  int shift = 0;
+  while ((1ll << shift) < d) ++shift;
+  return {static_cast<uint32_t>(((1ull << (31 + shift)) + d - 1) / d), shift};
+}
+
 // Launches a kernel that may start while the one before it on the stream
 // drains (it calls wait_for_previous).
 template <typename... Args, typename... Given>

@@ -61,18 +61,6 @@ View view_of(const sjd_view* v) { return {v->data_dev, v->batch_stride, v->token
 
 size_t size_of(int dtype) { return dtype == SJD_BF16 ? 2 : 4; }
 
-// x / d = x * mul >> (31 + shift) for x < 2^31: shift = ceil(log2 d), mul =
-// ceil(2^(31 + shift) / d) is above the true factor by less than 2^-31 of it.
-struct Divisor {
-  uint32_t mul;
-  int shift;
-};
-Divisor divisor(int d) {
-  int shift = 0;
-  while ((1ll << shift) < d) ++shift;
-  return {static_cast<uint32_t>(((1ull << (31 + shift)) + d - 1) / d), shift};
-}
-
 // The cache and spans of a call; a text if an argument is wrong.
 const char* cache_of(sjd_kv* kv, const sjd_kv_layer* l, const sjd_kv_span* s, long long most, Cache* c) {
   const sjd_kv_config& g = kv->cfg;

@@ -120,7 +120,7 @@ __device__ __forceinline__ Chunk chunk_at(int c, int pairs, int interleaved) {
 }
 
 // Turns the four pairs of a chunk.
-__device__ __forceinline__ void turn_chunk(float (&a)[4], float (&b)[4], const float2 (&cs)[4], int interleaved) {
+__device__ __forceinline__ void turn_chunk(float (&a)[4], float (&b)[4], const float2* cs, int interleaved) {
   if (interleaved) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -138,6 +138,36 @@ __device__ __forceinline__ void turn_chunk(float (&a)[4], float (&b)[4], const f
       b[i] = u * cs[i].y + b[i] * cs[i].x;
     }
   }
+}
+
+// Pairs of fp32.
+struct Pair {
+  unsigned long long v;
+};
+__device__ __forceinline__ Pair pair(float x, float y) {
+  Pair p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(x), "f"(y));
+  return p;
+}
+__device__ __forceinline__ float2 halves(Pair p) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p.v));
+  return f;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return d;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+  return d;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+  return d;
 }
 
 template <int KV>
@@ -165,10 +195,11 @@ __device__ __forceinline__ uint32_t codes4(const float (&y)[4]) {
     const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(y[2], y[3]), __NV_SATFINITE, __NV_E4M3);
     return lo | hi << 16;
   } else {
-    uint32_t w = 0;
+    // 1.5 * 2^23 + y, rounded to nearest even, ends in y's integer as a byte (|y| <= 127)
+    uint32_t b[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w |= static_cast<uint32_t>(max(-127, min(127, __float2int_rn(y[i]))) & 0xff) << 8 * i;
-    return w;
+    for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(y[i] + 12582912.0f);
+    return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
   }
 }
 
