@@ -42,6 +42,7 @@ constexpr uint32_t kTmemColumns = 512;  // S of the two slots (P over them), the
 constexpr uint32_t kOColumn = 2 * kTile;
 constexpr long long kWaitClocks = 4000000000ll;  // about two seconds
 constexpr float kLeast = 1e-30f;
+constexpr int kRoom = 6;
 constexpr float kRise = 8.0f;           // a row's reference maximum moves when it is behind by more than 2^8
 
 __host__ __device__ constexpr uint32_t tile_bytes(int dp) { return static_cast<uint32_t>(kTile) * dp * 2; }
@@ -153,6 +154,8 @@ struct Misc {
   Start start;
   Walk<NM> walk[2];        // the softmax groups' ways
   uint32_t poison[2][4];   // per slot: keys of the tile whose factor is no number
+  signed char exponents[2][NM * kTile];  // of the queries' rows (8-bit cache), by the piece's number modulo 2
+  uint32_t most[2][4];     // per slot and warp: the largest of the tile's value factors
   alignas(16) float row[2][2][kTile];  // per slot: factors of the tile's keys and values; at the end the rows' maxima and sums
 };
 
@@ -228,31 +231,24 @@ __device__ __forceinline__ uint32_t piece_at(int row, int piece) {
   return static_cast<uint32_t>((piece >> 3) * (kTile * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
 }
 
-// The bf16 values of 8 codes, exactly.
-template <int KV>
-__device__ __forceinline__ uint32_t two_values(uint32_t x) {
-  // x: one code in each half word, in its upper byte (e4m3) or its lower one (s8)
-  __nv_bfloat162 a, b;
-  if constexpr (KV == SJD_E4M3) {
-    // sign, exponent and fraction in bf16's places, the exponent 120 short
-    const uint32_t v = (x & 0x80008000u) | ((x >> 4) & 0x07f007f0u), up = 0x7b807b80u;  // 2^120
-    a = *reinterpret_cast<const __nv_bfloat162*>(&v);
-    b = *reinterpret_cast<const __nv_bfloat162*>(&up);
-    a = __hmul2(a, b);
-  } else {
-    // 128 + (low seven bits), less 128 or, of a negative one, 256
-    const uint32_t v = (x & 0x007f007fu) | 0x43004300u, w = (x & 0x00800080u) | 0x43004300u;
-    a = *reinterpret_cast<const __nv_bfloat162*>(&v);
-    b = *reinterpret_cast<const __nv_bfloat162*>(&w);
-    a = __hsub2(a, b);
-  }
-  return *reinterpret_cast<const uint32_t*>(&a);
-}
+// The fp16 values of 8 codes, exactly.
 template <int KV>
 __device__ __forceinline__ uint4 eight_values(uint2 w) {
-  constexpr uint32_t lo = KV == SJD_E4M3 ? 0x1404 : 0x4140, hi = KV == SJD_E4M3 ? 0x3424 : 0x4342;
-  return make_uint4(two_values<KV>(__byte_perm(w.x, 0, lo)), two_values<KV>(__byte_perm(w.x, 0, hi)),
-                    two_values<KV>(__byte_perm(w.y, 0, lo)), two_values<KV>(__byte_perm(w.y, 0, hi)));
+  uint32_t v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = i < 2 ? w.x : w.y;
+    if constexpr (KV == SJD_E4M3) {
+      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(i & 1 ? x >> 16 : x), __NV_E4M3);
+      v[i] = *reinterpret_cast<const uint32_t*>(&h);
+    } else {
+      // code + 128 in the last byte of 1024 + that, less 1152
+      const uint32_t u = __byte_perm(x ^ 0x80808080u, 0x64646464u, i & 1 ? 0x4342 : 0x4140), less = 0x64806480u;
+      const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&u), *reinterpret_cast<const __half2*>(&less));
+      v[i] = *reinterpret_cast<const uint32_t*>(&d);
+    }
+  }
+  return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // --- loading --------------------------------------------------------------------
@@ -284,6 +280,48 @@ __device__ __forceinline__ void load_queries(const AttendParams& p, const Item& 
       const uint4 v = *w;
       *w = make_uint4(v.x ^ 0x80008000u, v.y ^ 0x80008000u, v.z ^ 0x80008000u, v.w ^ 0x80008000u);
     }
+  }
+}
+
+// Queries for an 8-bit cache, whose codes are fp16 in the products: a row is
+// divided by the power of two of its largest magnitude (bf16's 8 bits then fit
+// fp16 but for elements below 2^-15 of it), which is kept for its scores.
+template <int DP, int NM>
+__device__ __forceinline__ void load_half_queries(const AttendParams& p, const Item& it, uint32_t smem, int tid, signed char* exponents) {
+  constexpr int kPieces = DP / 8;
+  const int G = p.c.group, pieces = p.c.D / 8;
+  const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q.p) + it.b * p.q.sb + static_cast<long long>(it.kvh) * G * p.q.sh;
+  const int piece = tid % kPieces;
+  const uint32_t flip = p.scale < 0.0f ? 0x80000000u : 0u;  // the kernel's factor is |scale|
+#pragma unroll 4
+  for (int row = tid / kPieces; row < kTile * NM; row += 128 / kPieces) {
+    const int r = it.mt * (kTile * NM) + row, t = by_group(p.c, r), g = r - t * G;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (r < it.rows && piece < pieces) v = *reinterpret_cast<const uint4*>(q + t * p.q.st + g * p.q.sh + 8 * piece);
+    uint32_t w[4] = {v.x, v.y, v.z, v.w}, most = 0;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = unpack_bf16(w[i]);
+      x[2 * i] = f.x, x[2 * i + 1] = f.y;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t bits = __float_as_uint(x[2 * i + e]) & 0x7fffffffu;
+        most = max(most, bits < 0x7f800000u ? bits : 0u);
+      }
+    }
+#pragma unroll
+    for (int o = kPieces / 2; o > 0; o /= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    // (-120 to 120: the factor and its inverse are normal numbers)
+    const int e = most == 0 ? 0 : max(-120, min(120, static_cast<int>(most >> 23) - 127));
+    const float f = __uint_as_float(static_cast<uint32_t>(127 - e) << 23 | flip);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __half2 h = __floats2half2_rn(x[2 * i] * f, x[2 * i + 1] * f);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    shared_store16(smem + (row / kTile) * tile_bytes(DP) + piece_at(row % kTile, piece), make_uint4(w[0], w[1], w[2], w[3]));
+    if (piece == 0) exponents[row] = static_cast<signed char>(e);
   }
 }
 
@@ -403,7 +441,9 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
   } else {
     // The codes come into a ring of their own, up to kRaw tiles ahead, 16 to a
     // copy where a vector's length is a multiple of that (past the L1 cache)
-    // and else 8; a warp turns its 32 rows into bf16, 8 codes to a thread.
+    // and else 8; a warp turns its 32 rows into fp16, 8 codes to a thread. (Into bf16
+    // it takes three times the instructions: 1280 of the 1395 cycles that HBM
+    // leaves a tile.)
     constexpr int kWide = DP / 16, kWideStep = 32 / kWide;
     const bool wide = p.c.D % 16 == 0;
     const uint32_t raw = smem + (IS_V ? P::kAtRawV : P::kAtRawK) + warp * 32 * DP;
@@ -446,7 +486,7 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
     do {
       if constexpr (IS_V) {
         queries(w.piece);
-        load_queries<DP, NM>(p, w.it, smem, tid);
+        load_half_queries<DP, NM>(p, w.it, smem, tid, m->exponents[w.piece & 1]);
         queries_there();
       }
       for (int k = w.k0; k < w.k1; ++k) {
@@ -480,7 +520,7 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
 template <int KV, int DP, int NM>
 __device__ __forceinline__ void issue_products(const AttendParams& p, Misc<NM>* m, uint32_t smem, uint32_t tmem) {
   using P = Plan<KV, DP, NM>;
-  constexpr uint32_t kScores = product_kind(kTile, kTile, false), kValues = product_kind(kTile, DP, true);
+  constexpr uint32_t kScores = product_kind(kTile, kTile, false, KV != SJD_BF16), kValues = product_kind(kTile, DP, true, KV != SJD_BF16);
   const bool lead = elect_lane();
   Walk<NM> w;
   if (!w.begin(p, m->start)) return;
@@ -601,8 +641,8 @@ __device__ __forceinline__ float largest_of(const uint32_t (&s)[32], float t) {
   }
   return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
 }
-// The weights of 32 scores against `base`, packed to bf16, in an 8-bit cache
-// times the values' factors; and their sum.
+// The weights of 32 scores, 2^(c s - base), packed to 16 bits, in an 8-bit
+// cache times the values' factors; and their sum.
 template <int KV>
 __device__ __forceinline__ void weights_of(const uint32_t (&s)[32], const float* factors, float c, float base, uint32_t (&out)[16], Pair (&sum)[2]) {
   const Pair c2 = pair(c, c), less = pair(-base, -base);
@@ -612,12 +652,17 @@ __device__ __forceinline__ void weights_of(const uint32_t (&s)[32], const float*
     if constexpr (KV != SJD_BF16) f = *reinterpret_cast<const float4*>(factors + j);
 #pragma unroll
     for (int e = 0; e < 4; e += 2) {
-      const Pair t = pair(__uint_as_float(s[j + e]), __uint_as_float(s[j + e + 1]));
-      const float2 d = halves(KV == SJD_BF16 ? fma2(t, c2, less) : add2(t, less));
+      const float2 d = halves(fma2(pair(__uint_as_float(s[j + e]), __uint_as_float(s[j + e + 1])), c2, less));
       const Pair w = pair(exp2_fast(d.x), exp2_fast(d.y));
       sum[e / 2] = add2(sum[e / 2], w);
-      const float2 v = halves(KV == SJD_BF16 ? w : mul2(w, e ? pair(f.z, f.w) : pair(f.x, f.y)));
-      out[(j + e) / 2] = pack_bf16(v.x, v.y);
+      if constexpr (KV == SJD_BF16) {
+        const float2 v = halves(w);
+        out[(j + e) / 2] = pack_bf16(v.x, v.y);
+      } else {
+        const float2 v = halves(mul2(w, e ? pair(f.z, f.w) : pair(f.x, f.y)));
+        const __half2 h = __floats2half2_rn(v.x, v.y);
+        out[(j + e) / 2] = *reinterpret_cast<const uint32_t*>(&h);
+      }
     }
   }
 }
@@ -650,6 +695,10 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     const int whole = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_GIVEN ? it.start : limit;
     const int common = common_keys<NM>(p, it);
     float ref = -INFINITY, sum = 0.0f;
+    // In an 8-bit cache the weights are fp16: 2^kRoom p (v / unit), the values' factors v in units
+    // of a power of two, the largest so far. With p up to 2^8 nothing overflows, and what is
+    // below 2^-30 of the largest is lost.
+    float c_row = c, unit = 0.0f;
     // an 8-bit cache's factors of key `row` of the tiles: the next tile's are on their way while
     // one is worked on, and the page of the one after that
     float next_k = 0.0f, next_v = 0.0f;
@@ -675,11 +724,14 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
         const bool apart = key0 + kTile > common;
         const bool bad_k = apart && next_k != next_k, bad_v = apart && next_v != next_v;
         named_barrier(2 + slot, 128);  // all have used the factors of the tile before
-        m->row[slot][0][row] = bad_k ? kLeast : fmaxf(next_k * c, next_k == next_k ? kLeast : next_k);
+        m->row[slot][0][row] = bad_k ? kLeast : fmaxf(next_k, next_k == next_k ? kLeast : next_k);
         m->row[slot][1][row] = bad_v ? 0.0f : next_v;
         const unsigned poison = __ballot_sync(0xffffffffu, bad_k);
         if ((threadIdx.x & 31) == 0) m->poison[slot][row / 32] = poison;
         if (bad_v) m->bad_values[w.piece & 3] = w.piece + 1;
+        const uint32_t bits = next_v < INFINITY ? __float_as_uint(next_v) : 0u;
+        const uint32_t most = __reduce_max_sync(0xffffffffu, bits);
+        if ((threadIdx.x & 31) == 0) m->most[slot][row / 32] = most;
         named_barrier(2 + slot, 128);
         if (u + 1 < units) factors(u + 1);
       }
@@ -713,7 +765,14 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
         // cache): first the largest, then the weights.
         const float* fk = m->row[slot][0];
         const float* fv = m->row[slot][1];
-        float top = -INFINITY;
+        float top = -INFINITY, grown = 1.0f;
+        if (KV != SJD_BF16) {
+          if (u == 0) c_row = fmaxf(c * __uint_as_float(static_cast<uint32_t>(127 + m->exponents[w.piece & 1][(NM == 2 ? slot * kTile : 0) + row]) << 23), 1e-37f);
+          const uint32_t most = max(max(m->most[slot][0], m->most[slot][1]), max(m->most[slot][2], m->most[slot][3]));
+          // (the power of two from there on, at least 2^-100 and at most 2^120)
+          const float now = __uint_as_float(max(27u << 23, min(247u << 23, (most + 0x7fffffu) & 0x7f800000u)));
+          if (now > unit) grown = unit > 0.0f ? unit / now : 1.0f, unit = now;
+        }
         uint32_t s[2][32];
         tmem_load32(s_at, s[0]);
 #pragma unroll
@@ -721,19 +780,24 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
           if (i < 2 || two) {
             tmem_wait_load(s[i & 1]);
             if (i < 3) tmem_load32(s_at + 32 * (i + 1), s[(i + 1) & 1]);
-            if (KV != SJD_BF16) times_factors(s[i & 1], fk + 32 * i);
+            if (KV != SJD_BF16) {
+              times_factors(s[i & 1], fk + 32 * i);
+              tmem_store32(s_at + 32 * i, s[i & 1]);
+            }
             top = largest_of(s[i & 1], top);
           }
         }
         if (!two) tmem_wait_load(s[0]);
-        if (KV == SJD_BF16) top *= c;
+        if (KV != SJD_BF16) tmem_wait_store();
+        top *= c_row;
         // The reference that the weights are taken against moves only where a
         // weight could pass 2^8: their relative precision is the same below
         // that, and O is left alone.
         const bool move = top > ref + kRise || (ref == -INFINITY && top != -INFINITY);
-        if (__any_sync(0xffffffffu, move)) {
-          const float f = !move ? 1.0f : ref == -INFINITY ? 0.0f : exp2_fast(ref - top);
+        if (__any_sync(0xffffffffu, move || grown != 1.0f)) {
+          float f = !move ? 1.0f : ref == -INFINITY ? 0.0f : exp2_fast(ref - top);
           if (move) ref = top, sum *= f;
+          f *= grown;
           __syncwarp();
           if (u > 0) {
 #pragma unroll 1
@@ -746,7 +810,9 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
             }
           }
         }
-        const float base = ref == -INFINITY ? 0.0f : ref;
+        // (the unit's exponent, less the room, goes into the powers of two)
+        const int shift = KV == SJD_BF16 ? 0 : static_cast<int>(__float_as_uint(unit) >> 23) - 127 - kRoom;
+        const float base = (ref == -INFINITY ? 0.0f : ref) + static_cast<float>(shift);
         Pair total[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
         tmem_load32(s_at, s[0]);
 #pragma unroll
@@ -755,8 +821,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
             uint32_t out[16];
             tmem_wait_load(s[i & 1]);
             if (i < 3) tmem_load32(s_at + 32 * (i + 1), s[(i + 1) & 1]);
-            if (KV != SJD_BF16) times_factors(s[i & 1], fk + 32 * i);
-            weights_of<KV>(s[i & 1], fv + 32 * i, c, base, out, total);
+            weights_of<KV>(s[i & 1], fv + 32 * i, c_row, base, out, total);
             tmem_store16(s_at + 16 * i, out);
           }
           if (i & 1) {
@@ -768,7 +833,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
         }
         if (!two) tmem_wait_load(s[0]);
         const float2 ends = halves(add2(total[0], total[1]));
-        sum += ends.x + ends.y;
+        sum += (ends.x + ends.y) * (KV == SJD_BF16 ? 1.0f : __uint_as_float(static_cast<uint32_t>(127 + shift) << 23));
       } else if ((threadIdx.x & 31) == 0) {
         mbar_arrive(smem_addr(&m->p_full[slot][0]));
         if (two) mbar_arrive(smem_addr(&m->p_full[slot][1]));
@@ -785,6 +850,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
       named_barrier(2 + slot, 128);  // (the factors are done with)
       m->row[slot][0][row] = ref;
       m->row[slot][1][row] = sum;
+      if (KV != SJD_BF16 && row == 0) m->most[slot][0] = __float_as_uint(unit);
       named_barrier(1, 256);
       const float r1 = tiles > 1 ? m->row[1][0][row] : -INFINITY, r0s = m->row[0][0][row];
       const float s1 = tiles > 1 ? m->row[1][1][row] : 0.0f, s0 = m->row[0][1][row];
@@ -792,6 +858,12 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
       f[0] = r0s == -INFINITY ? 0.0f : exp2_fast(r0s - ref);
       f[1] = r1 == -INFINITY ? 0.0f : exp2_fast(r1 - ref);
       sum = s0 * f[0] + s1 * f[1];
+      if (KV != SJD_BF16) {
+        f[0] *= __uint_as_float(m->most[0][0]) * (1.0f / (1 << kRoom));
+        if (tiles > 1) f[1] *= __uint_as_float(m->most[1][0]) * (1.0f / (1 << kRoom));
+      }
+    } else if (KV != SJD_BF16) {
+      f[0] = f[1] = unit * (1.0f / (1 << kRoom));
     }
     const bool wholly = w.k0 == 0 && w.k1 == it.tiles;
     const bool bad = *const_cast<volatile int*>(&m->bad_values[w.piece & 3]) == w.piece + 1;
@@ -818,7 +890,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
           tmem_load32(o_at + e * DP + column, x);
           tmem_wait_load(x);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) o[j] = NM == 1 ? fmaf(__uint_as_float(x[j]), f[e], o[j]) : __uint_as_float(x[j]);
+          for (int j = 0; j < 32; ++j) o[j] = NM == 1 || KV != SJD_BF16 ? fmaf(__uint_as_float(x[j]), f[e], o[j]) : __uint_as_float(x[j]);
         }
         if (bad && valid) {
           float with[32];

@@ -187,6 +187,7 @@ __global__ void __launch_bounds__(kBlock) write_kernel(const WriteParams p, cons
         }
       }
     }
+    if (n_q > 0 && __all_sync(0xffffffffu, is_q || item >= items)) continue;
     using Code = typename Codes<KV>::type;
     const uint32_t slot = slots[q.token];
     const bool store = item < items && !is_q && slot != kNoVector;

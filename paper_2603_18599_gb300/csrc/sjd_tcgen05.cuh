@@ -106,7 +106,7 @@ __device__ __forceinline__ void tmem_wait_load(uint32_t (&r)[32]) {
 __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // --- matrix products -------------------------------------------------------------
-// Operands in shared memory: tiles of 128-byte rows (64 bf16), 8 rows to a
+// Operands in shared memory: tiles of 128-byte rows (64 values of 16 bits), 8 rows to a
 // 1024-byte block whose 16-byte pieces are exchanged by the row's number
 // (the 128-byte swizzle).
 
@@ -119,9 +119,9 @@ __device__ __forceinline__ uint64_t operand_n(uint32_t smem, uint32_t next) {
   return static_cast<uint64_t>((smem & 0x3ffff) >> 4) | static_cast<uint64_t>(next >> 4) << 16 |
          static_cast<uint64_t>(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
-// bf16 x bf16 into fp32; A is K-major.
-__host__ __device__ constexpr uint32_t product_kind(int m, int n, bool b_n_major) {
-  return 1u << 4 | 1u << 7 | 1u << 10 | (b_n_major ? 1u << 16 : 0u) | static_cast<uint32_t>(n >> 3) << 17 | static_cast<uint32_t>(m >> 4) << 24;
+// bf16 x bf16 or fp16 x fp16 into fp32; A is K-major.
+__host__ __device__ constexpr uint32_t product_kind(int m, int n, bool b_n_major, bool half) {
+  return 1u << 4 | (half ? 0u : 1u << 7 | 1u << 10) | (b_n_major ? 1u << 16 : 0u) | static_cast<uint32_t>(n >> 3) << 17 | static_cast<uint32_t>(m >> 4) << 24;
 }
 // One lane of the warp. A warp issues its products with all lanes on the same
 // way and this one alone in the instruction: their descriptors then stay in
