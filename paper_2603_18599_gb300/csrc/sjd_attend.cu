@@ -20,10 +20,16 @@
 // A block has four kinds of warps. 0-3 and 4-7 take the softmax, each group a
 // slot: with NM = 1 the even and the odd tiles of the same 128 rows (each with
 // an accumulator of its own, joined at the end), with NM = 2 the two halves
-// of 256 rows. 8-11 load keys, 12-15 the queries and values, and warp 16
+// of 256 rows. 8-11 load keys, 12-15 the queries and values, and warp 19
 // issues the products: those of one slot run while the other's softmax does.
 // A slot's weights are handed over in two halves of 64 keys, the second made
 // while the first is multiplied.
+//
+// With at most 64 or 32 rows (a short window, one token) the rows lie in the
+// tile two or four times (SP), so that the warps of a slot all have work:
+// each copy takes the softmax over its own half or quarter of a tile's keys,
+// with a maximum and a sum of its own and weights of 0 for the other keys, and
+// the copies' accumulators are joined at the end like the slots'.
 
 #include <cfloat>
 
@@ -36,8 +42,8 @@ namespace {
 
 constexpr int kTile = 128;              // rows of a product, and keys of a tile
 constexpr int kHalf = kTile / 2;        // keys whose weights are handed over at a time
-constexpr int kAttendThreads = 17 * 32;
-constexpr int kMmaWarp = 16;
+constexpr int kAttendThreads = 20 * 32;
+constexpr int kMmaWarp = 19;            // (on another scheduler than the first rows' softmax)
 constexpr uint32_t kTmemColumns = 512;  // S of the two slots (P over them), then O of the two
 constexpr uint32_t kOColumn = 2 * kTile;
 constexpr long long kWaitClocks = 4000000000ll;  // about two seconds
@@ -259,7 +265,7 @@ __device__ __forceinline__ int key_page(const Cache& c, const Item& it, int key)
 }
 
 // Queries of the item: rows of 16-byte pieces, zeros beyond.
-template <int DP, int NM>
+template <int DP, int NM, int SP>
 __device__ __forceinline__ void load_queries(const AttendParams& p, const Item& it, uint32_t smem, int tid) {
   constexpr int kPieces = DP / 8;
   const int G = p.c.group, pieces = p.c.D / 8;
@@ -267,7 +273,7 @@ __device__ __forceinline__ void load_queries(const AttendParams& p, const Item& 
   const int piece = tid % kPieces;
 #pragma unroll 8
   for (int row = tid / kPieces; row < kTile * NM; row += 128 / kPieces) {
-    const int r = it.mt * (kTile * NM) + row, t = by_group(p.c, r), g = r - t * G;
+    const int r = it.mt * (kTile * NM) + row % (kTile * NM / SP), t = by_group(p.c, r), g = r - t * G;
     const bool in = r < it.rows && piece < pieces;
     copy16(smem + (row / kTile) * tile_bytes(DP) + piece_at(row % kTile, piece),
            in ? q + t * p.q.st + g * p.q.sh + 8 * piece : static_cast<const __nv_bfloat16*>(p.q.p), in ? 16 : 0);
@@ -286,7 +292,7 @@ __device__ __forceinline__ void load_queries(const AttendParams& p, const Item& 
 // Queries for an 8-bit cache, whose codes are fp16 in the products: a row is
 // divided by the power of two of its largest magnitude (bf16's 8 bits then fit
 // fp16 but for elements below 2^-15 of it), which is kept for its scores.
-template <int DP, int NM>
+template <int DP, int NM, int SP>
 __device__ __forceinline__ void load_half_queries(const AttendParams& p, const Item& it, uint32_t smem, int tid, signed char* exponents) {
   constexpr int kPieces = DP / 8;
   const int G = p.c.group, pieces = p.c.D / 8;
@@ -295,7 +301,7 @@ __device__ __forceinline__ void load_half_queries(const AttendParams& p, const I
   const uint32_t flip = p.scale < 0.0f ? 0x80000000u : 0u;  // the kernel's factor is |scale|
 #pragma unroll 4
   for (int row = tid / kPieces; row < kTile * NM; row += 128 / kPieces) {
-    const int r = it.mt * (kTile * NM) + row, t = by_group(p.c, r), g = r - t * G;
+    const int r = it.mt * (kTile * NM) + row % (kTile * NM / SP), t = by_group(p.c, r), g = r - t * G;
     uint4 v = make_uint4(0, 0, 0, 0);
     if (r < it.rows && piece < pieces) v = *reinterpret_cast<const uint4*>(q + t * p.q.st + g * p.q.sh + 8 * piece);
     uint32_t w[4] = {v.x, v.y, v.z, v.w}, most = 0;
@@ -341,7 +347,7 @@ __device__ __forceinline__ bool take_out(uint32_t& w) {
 // 8)-th row; a lane finds the vector of row (warp * 32 + lane) and the others
 // ask it by shuffles. The page of the next tile's row is loaded while this
 // tile's copies are issued.
-template <int KV, int DP, int NM, bool IS_V>
+template <int KV, int DP, int NM, int SP, bool IS_V>
 __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m, uint32_t smem) {
   using P = Plan<KV, DP, NM>;
   using Code = typename Codes<KV>::type;
@@ -403,7 +409,7 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
       if constexpr (IS_V) {
         drain();
         queries(w.piece);
-        load_queries<DP, NM>(p, w.it, smem, tid);
+        load_queries<DP, NM, SP>(p, w.it, smem, tid);
         queries_there();
         owed_piece = w.piece;
       }
@@ -486,7 +492,7 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
     do {
       if constexpr (IS_V) {
         queries(w.piece);
-        load_half_queries<DP, NM>(p, w.it, smem, tid, m->exponents[w.piece & 1]);
+        load_half_queries<DP, NM, SP>(p, w.it, smem, tid, m->exponents[w.piece & 1]);
         queries_there();
       }
       for (int k = w.k0; k < w.k1; ++k) {
@@ -940,7 +946,250 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
   }
 }
 
-template <int KV, int DP, int NM>
+// The softmax of at most 128 / SP rows, SP = 2 or 4 copies of them in the tile
+// (NM = 1). A warp has the 128 / SP keys of its copy.
+template <int KV, int DP, int SP>
+__device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m, unsigned char* queries, uint32_t tmem, float* parts, float2* part_rows,
+                                               Shared* shared) {
+  constexpr int kRows = kTile / SP, kKeys = kTile / SP, kChunks = kKeys / 32, kWarps = 4 / SP;  // of a copy
+  const int slot = threadIdx.x / 128, at = threadIdx.x & 127, lane = threadIdx.x & 31, copy = at / kRows, row = at % kRows;
+  const uint32_t lanes = static_cast<uint32_t>(at & ~31) << 16;
+  const uint32_t s_at = tmem + lanes + slot * kTile, o_at = tmem + lanes + kOColumn + slot * DP;
+  const int G = p.c.group;
+  const float c = fmaxf(fabsf(p.scale) * 1.4426950408889634f, kLeast);
+  auto copy_barrier = [&]() {  // the copy's warps
+    if constexpr (kWarps == 1) __syncwarp();
+    else named_barrier(4 + slot * SP + copy, 32 * kWarps);
+  };
+  Walk<1>& w = m->walk[slot];
+  const Item& it = w.it;
+  if (m->start.tiles <= 0) return;
+  if (at == 0) w.begin(p, m->start);
+  named_barrier(2 + slot, 128);
+  int tile_no = 0;
+  uint32_t sp = 0;
+  for (;;) {
+    const bool valid = row < it.rows, active = (at & ~31) % kRows < it.rows;
+    const int t = by_group(p.c, row);
+    const int units = (w.k1 - w.k0 + 1 - slot) / 2, k_first = w.k0 + slot;
+    const int limit = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_CAUSAL ? it.start + t + 1 : it.keys;
+    const int whole = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_GIVEN ? it.start : limit;
+    const int common = common_keys<1>(p, it);
+    float ref = -INFINITY, sum = 0.0f, c_row = c, unit = 0.0f;
+    // the factors of key `at` of a tile, as in softmax_rows
+    float next_k = 0.0f, next_v = 0.0f;
+    int page = kNoPage;
+    auto factors = [&](int u) {
+      const int key = (k_first + 2 * u) * kTile + at;
+      const uint32_t v = vector_in(p.c, page, key, it.kvh);
+      next_k = next_v = 0.0f;
+      if (v != kNoVector) next_k = p.c.ks[v], next_v = p.c.vs[v];
+      page = u + 1 < units ? key_page(p.c, it, key + 2 * kTile) : kNoPage;
+    };
+    if (KV != SJD_BF16 && units > 0) {
+      page = key_page(p.c, it, k_first * kTile + at);
+      factors(0);
+    }
+#pragma unroll 1
+    for (int u = 0; u < units; ++u) {
+      const int tile_key = (k_first + 2 * u) * kTile, key0 = tile_key + copy * kKeys;
+      const bool two = it.keys - tile_key > kHalf;
+      if constexpr (KV != SJD_BF16) {
+        const bool apart = tile_key + kTile > common;
+        const bool bad_k = apart && next_k != next_k, bad_v = apart && next_v != next_v;
+        copy_barrier();  // all have used the factors of the tile before
+        m->row[slot][0][at] = bad_k ? kLeast : fmaxf(next_k, next_k == next_k ? kLeast : next_k);
+        m->row[slot][1][at] = bad_v ? 0.0f : next_v;
+        const unsigned poison = __ballot_sync(0xffffffffu, bad_k);
+        if (bad_v) m->bad_values[w.piece & 3] = w.piece + 1;
+        const uint32_t most = __reduce_max_sync(0xffffffffu, next_v < INFINITY ? __float_as_uint(next_v) : 0u);
+        if (lane == 0) m->poison[slot][at / 32] = poison, m->most[slot][at / 32] = most;
+        copy_barrier();
+        if (u + 1 < units) factors(u + 1);
+      }
+      wait(m, &m->s_full[slot], sp);
+      sp ^= 1;
+      tc_fence_after();
+      if (active) {
+        const uint32_t* poison = m->poison[slot] + copy * kChunks;
+        uint32_t bad = 0;
+        if (KV != SJD_BF16) bad = SP == 4 ? poison[0] : poison[0] | poison[1];
+        const bool mixed = !__all_sync(0xffffffffu, key0 + kKeys <= whole) || bad;
+        float top = -INFINITY, grown = 1.0f;
+        if (KV != SJD_BF16) {
+          if (u == 0) c_row = fmaxf(c * __uint_as_float(static_cast<uint32_t>(127 + m->exponents[w.piece & 1][at]) << 23), 1e-37f);
+          const uint32_t* words = m->most[slot] + copy * kChunks;
+          const uint32_t most = SP == 4 ? words[0] : max(words[0], words[1]);
+          const float now = __uint_as_float(max(27u << 23, min(247u << 23, (most + 0x7fffffu) & 0x7f800000u)));
+          if (now > unit) grown = unit > 0.0f ? unit / now : 1.0f, unit = now;
+        }
+        const float* fk = m->row[slot][0] + copy * kKeys;
+        const float* fv = m->row[slot][1] + copy * kKeys;
+        // (64 scores do not stay in registers: they are read again for their weights)
+        uint32_t s[32];
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+          tmem_load32(s_at + copy * kKeys + 32 * i, s);
+          tmem_wait_load(s);
+          if (mixed) {
+            const int n = limit - (key0 + 32 * i);
+            uint32_t seen = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
+            if (p.mask_kind == SJD_MASK_GIVEN && valid) {
+              const uint8_t* mask = p.mask + p.mask_b * it.b + p.mask_r * t - it.start;
+              const int a = max(key0 + 32 * i, it.start), e = min(key0 + 32 * i + 32, it.keys);
+#pragma unroll 1
+              for (int key = a; key < e; ++key)
+                if (!mask[key]) seen &= ~(1u << (key - key0 - 32 * i));
+            }
+            const uint32_t none = KV != SJD_BF16 ? seen & poison[i] : 0u;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) s[j] = seen >> j & 1 ? (none >> j & 1 ? 0x7fc00000u : s[j]) : 0xff800000u;
+            __syncwarp();
+          }
+          if (KV != SJD_BF16) times_factors(s, fk + 32 * i);
+          if (kChunks > 1 && (KV != SJD_BF16 || mixed)) tmem_store32(s_at + copy * kKeys + 32 * i, s);
+          top = largest_of(s, top);
+        }
+        if (kChunks > 1) tmem_wait_store();
+        top *= c_row;
+        const bool move = top > ref + kRise || (ref == -INFINITY && top != -INFINITY);
+        if (__any_sync(0xffffffffu, move || grown != 1.0f)) {
+          float f = !move ? 1.0f : ref == -INFINITY ? 0.0f : exp2_fast(ref - top);
+          if (move) ref = top, sum *= f;
+          f *= grown;
+          __syncwarp();
+          if (u > 0) {
+#pragma unroll 1
+            for (int i = 0; i < DP / 16; ++i) {
+              uint32_t o[16];
+              tmem_load16(o_at + 16 * i, o);
+              tmem_wait_load(o);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_store16(o_at + 16 * i, o);
+            }
+          }
+        }
+        const int shift = KV == SJD_BF16 ? 0 : static_cast<int>(__float_as_uint(unit) >> 23) - 127 - kRoom;
+        const float base = (ref == -INFINITY ? 0.0f : ref) + static_cast<float>(shift);
+        Pair total[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+        uint32_t out[kChunks][16];
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+          if (kChunks > 1) {
+            tmem_load32(s_at + copy * kKeys + 32 * i, s);
+            tmem_wait_load(s);
+          }
+          weights_of<KV>(s, fv + 32 * i, c_row, base, out[i], total);
+        }
+        // (the row's weights of the other copies' keys are 0)
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) tmem_store16(s_at + 16 * (copy * kChunks + i), out[i]);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) out[0][j] = 0;
+#pragma unroll
+        for (int i = kChunks; i < 4; ++i) tmem_store16(s_at + 16 * ((copy * kChunks + i) % 4), out[0]);
+        const float2 ends = halves(add2(total[0], total[1]));
+        sum += (ends.x + ends.y) * (KV == SJD_BF16 ? 1.0f : __uint_as_float(static_cast<uint32_t>(127 + shift) << 23));
+        tmem_wait_store();
+        tc_fence_before();
+      }
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(smem_addr(&m->p_full[slot][0]));
+        if (two) mbar_arrive(smem_addr(&m->p_full[slot][1]));
+      }
+    }
+    // The end of the piece: the 2 SP accumulators of a row are added up by way
+    // of the queries' shared memory, a quarter of the columns at a time.
+    wait(m, &m->o_full, w.piece & 1);
+    tc_fence_after();
+    const int tiles = w.k1 - w.k0;
+    copy_barrier();  // (the factors are done with)
+    m->row[slot][0][at] = units > 0 && active ? ref : -INFINITY;
+    m->row[slot][1][at] = units > 0 && active ? sum : 0.0f;
+    named_barrier(1, 256);
+    float most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 2 * SP; ++i) most = fmaxf(most, m->row[i & 1][0][i / 2 * kRows + row]);
+    const float own = units > 0 && active && ref != -INFINITY ? exp2_fast(ref - most) * (KV == SJD_BF16 ? 1.0f : unit * (1.0f / (1 << kRoom))) : 0.0f;
+    const bool wholly = w.k0 == 0 && w.k1 == it.tiles;
+    const bool bad = *const_cast<volatile int*>(&m->bad_values[w.piece & 3]) == w.piece + 1;
+    const long long part = 2ll * blockIdx.x + (w.k0 == 0 ? 1 : 0);
+    constexpr int kColumns = DP / 4, kFours = kColumns / 4;
+    float4* sums = reinterpret_cast<float4*>(queries);
+#pragma unroll 1
+    for (int round = 0; round < 4; ++round) {
+      const int column = round * kColumns;
+      float4* mine = sums + (slot * kTile + at) * kFours;
+      if (active) {
+#pragma unroll
+        for (int i = 0; i < kColumns / 16; ++i) {
+          uint32_t o[16];
+          if (units > 0) {
+            tmem_load16(o_at + column + 16 * i, o);
+            tmem_wait_load(o);
+          }
+#pragma unroll
+          for (int j = 0; j < 16; j += 4) {
+            // (a copy without weights has nothing, whatever its accumulator holds)
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (units > 0 && ref != -INFINITY)
+              v = make_float4(__uint_as_float(o[j]) * own, __uint_as_float(o[j + 1]) * own, __uint_as_float(o[j + 2]) * own, __uint_as_float(o[j + 3]) * own);
+            mine[(4 * i + j / 4) ^ (lane & (kFours - 1))] = v;
+          }
+        }
+      }
+      named_barrier(1, 256);
+      for (int i = threadIdx.x; i < kRows * kFours; i += 256) {
+        const int r = i / kFours, four = i % kFours, col = column + 4 * four;
+        if (r >= it.rows) break;
+        float top = -INFINITY, all = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 2 * SP; ++k) top = fmaxf(top, m->row[k & 1][0][k / 2 * kRows + r]);
+        float o[4] = {};
+#pragma unroll
+        for (int k = 0; k < 2 * SP; ++k) {
+          const int from = k / 2 * kRows + r;
+          const float its = m->row[k & 1][0][from];
+          all += its == -INFINITY ? 0.0f : m->row[k & 1][1][from] * exp2_fast(its - top);
+          const float4 v = sums[((k & 1) * kTile + from) * kFours + (four ^ (from & (kFours - 1)))];
+          o[0] += v.x, o[1] += v.y, o[2] += v.z, o[3] += v.w;
+        }
+        const int its_t = by_group(p.c, r), g = r - its_t * G;
+        if (bad) add_bad_values<KV, 1>(p, it, w.k0, w.k1, its_t, col, o);
+        const long long head = (static_cast<long long>(it.b) * p.c.n + its_t) * p.c.Hq + static_cast<long long>(it.kvh) * G + g;
+        const bool some = all > 0.0f || all != all;
+        if (wholly) {
+          const float inverse = some ? 1.0f / all : 0.0f;
+          if (col < p.c.D)
+            *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.o) + head * p.c.D + col) =
+                make_uint2(pack_bf16(o[0] * inverse, o[1] * inverse), pack_bf16(o[2] * inverse, o[3] * inverse));
+          if (p.lse && col == 0) p.lse[head] = some ? (top + log2f(all)) * 0.69314718055994531f : -INFINITY;
+        } else {
+          *reinterpret_cast<float4*>(parts + (part * kTile + r) * DP + col) = make_float4(o[0], o[1], o[2], o[3]);
+          if (col == 0) part_rows[part * kTile + r] = make_float2(top, all);
+        }
+      }
+      named_barrier(1, 256);
+    }
+    tc_fence_before();
+    if (threadIdx.x == 0) {
+      mbar_arrive(smem_addr(&m->q_empty));  // (the queries' memory is free again)
+      if (w.k0 == 0 && w.k1 < it.tiles) {
+        const long long beyond = m->start.tile + tile_no + it.tiles - 1;
+        shared[blockIdx.x] = {static_cast<int>(beyond / m->start.tiles - blockIdx.x + 1), it.kvh, it.b, it.mt};
+      }
+    }
+    tile_no += tiles;
+    named_barrier(2 + slot, 128);
+    if (tile_no == m->start.tiles) return;
+    if (at == 0) w.next(p);
+    named_barrier(2 + slot, 128);
+  }
+}
+
+template <int KV, int DP, int NM, int SP>
 __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendParams p, float* parts, float2* part_rows, Shared* shared) {
   extern __shared__ __align__(1024) unsigned char raw[];
   using P = Plan<KV, DP, NM>;
@@ -956,7 +1205,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
       mbar_init(smem_addr(&m->k_full[i]), 4), mbar_init(smem_addr(&m->k_empty[i]), 1);
       mbar_init(smem_addr(&m->v_full[i]), 4), mbar_init(smem_addr(&m->v_empty[i]), 1);
     }
-    mbar_init(smem_addr(&m->q_full), 4), mbar_init(smem_addr(&m->q_empty), 1), mbar_init(smem_addr(&m->o_full), 1);
+    mbar_init(smem_addr(&m->q_full), 4), mbar_init(smem_addr(&m->q_empty), SP > 1 ? 2 : 1), mbar_init(smem_addr(&m->o_full), 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_addr(&m->s_full[i]), 1), mbar_init(smem_addr(&m->p_full[i][0]), 4), mbar_init(smem_addr(&m->p_full[i][1]), 4);
     }
@@ -970,12 +1219,13 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
   tc_fence_after();
   const uint32_t tmem = m->tmem;
   if (warp < 8) {
-    softmax_rows<KV, DP, NM>(p, m, tmem, parts, part_rows, shared);
+    if constexpr (SP > 1) softmax_copies<KV, DP, SP>(p, m, raw, tmem, parts, part_rows, shared);
+    else softmax_rows<KV, DP, NM>(p, m, tmem, parts, part_rows, shared);
   } else if (warp < 12) {
-    load_operand<KV, DP, NM, false>(p, m, smem);
+    load_operand<KV, DP, NM, SP, false>(p, m, smem);
   } else if (warp < 16) {
-    load_operand<KV, DP, NM, true>(p, m, smem);
-  } else {
+    load_operand<KV, DP, NM, SP, true>(p, m, smem);
+  } else if (warp == kMmaWarp) {
     issue_products<KV, DP, NM>(p, m, smem, tmem);
   }
   tc_fence_before();
@@ -1045,34 +1295,37 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const AttendParam
   }
 }
 
-template <int KV, int DP, int NM>
+template <int KV, int DP, int NM, int SP>
 cudaError_t launch(const AttendParams& p, int sms, unsigned char* scratch, cudaStream_t s) {
   const int blocks = sms < kMaxAttendBlocks ? sms : kMaxAttendBlocks;
   const size_t rows = static_cast<size_t>(kTile) * NM * 2 * blocks;
   Shared* shared = reinterpret_cast<Shared*>(scratch);
   float2* part_rows = reinterpret_cast<float2*>(scratch + kMaxAttendBlocks * sizeof(Shared));
   float* parts = reinterpret_cast<float*>(part_rows + rows);
-  const cudaError_t e = launch_early(attend_kernel<KV, DP, NM>, blocks, kAttendThreads, shared_bytes<KV, DP, NM>(), s, p, parts, part_rows, shared);
+  const cudaError_t e = launch_early(attend_kernel<KV, DP, NM, SP>, blocks, kAttendThreads, shared_bytes<KV, DP, NM>(), s, p, parts, part_rows, shared);
   if (e != cudaSuccess) return e;
   return launch_early(join_kernel<DP>, dim3(blocks, 8), 32 * kJoinWarps, 0, s, p, parts, part_rows, shared, kTile * NM);
 }
 
-template <int KV>
+template <int KV, int DP>
 cudaError_t launch_of(const AttendParams& p, int sms, unsigned char* scratch, cudaStream_t s) {
-  const bool two = static_cast<long long>(p.c.n) * (p.c.Hq / p.c.Hkv) > kTile;
-  if (p.c.D <= 64) return two ? launch<KV, 64, 2>(p, sms, scratch, s) : launch<KV, 64, 1>(p, sms, scratch, s);
-  return two ? launch<KV, 128, 2>(p, sms, scratch, s) : launch<KV, 128, 1>(p, sms, scratch, s);
+  const long long rows = static_cast<long long>(p.c.n) * p.c.group;
+  if (rows <= kTile / 4) return launch<KV, DP, 1, 4>(p, sms, scratch, s);
+  if (rows <= kTile / 2) return launch<KV, DP, 1, 2>(p, sms, scratch, s);
+  if (rows <= kTile) return launch<KV, DP, 1, 1>(p, sms, scratch, s);
+  return launch<KV, DP, 2, 1>(p, sms, scratch, s);
 }
 
-}  // namespace
-
-namespace {
-
+template <int KV, int DP, int NM, int SP>
+cudaError_t raise_limit() {
+  return cudaFuncSetAttribute(attend_kernel<KV, DP, NM, SP>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_bytes<KV, DP, NM>());
+}
 template <int KV, int DP>
 cudaError_t raise_limits() {
-  const cudaError_t e = cudaFuncSetAttribute(attend_kernel<KV, DP, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_bytes<KV, DP, 1>());
-  if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(attend_kernel<KV, DP, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_bytes<KV, DP, 2>());
+  cudaError_t e = raise_limit<KV, DP, 1, 4>();
+  if (e == cudaSuccess) e = raise_limit<KV, DP, 1, 2>();
+  if (e == cudaSuccess) e = raise_limit<KV, DP, 1, 1>();
+  return e == cudaSuccess ? raise_limit<KV, DP, 2, 1>() : e;
 }
 
 }  // namespace
@@ -1090,9 +1343,10 @@ size_t attend_scratch_bytes(int head_dim, long long rows) {
 }
 
 cudaError_t launch_attend(const AttendParams& p, int kv_dtype, int sms, unsigned char* scratch, cudaStream_t s) {
-  if (kv_dtype == SJD_BF16) return launch_of<SJD_BF16>(p, sms, scratch, s);
-  if (kv_dtype == SJD_E4M3) return launch_of<SJD_E4M3>(p, sms, scratch, s);
-  return launch_of<SJD_S8>(p, sms, scratch, s);
+  const bool small = p.c.D <= 64;
+  if (kv_dtype == SJD_BF16) return small ? launch_of<SJD_BF16, 64>(p, sms, scratch, s) : launch_of<SJD_BF16, 128>(p, sms, scratch, s);
+  if (kv_dtype == SJD_E4M3) return small ? launch_of<SJD_E4M3, 64>(p, sms, scratch, s) : launch_of<SJD_E4M3, 128>(p, sms, scratch, s);
+  return small ? launch_of<SJD_S8, 64>(p, sms, scratch, s) : launch_of<SJD_S8, 128>(p, sms, scratch, s);
 }
 
 }  // namespace sjd_kv_ops
