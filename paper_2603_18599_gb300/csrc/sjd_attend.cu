@@ -375,7 +375,7 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
   uint32_t round = 1;         // parity of the empty barriers' phase before it
   int page = key_page(p.c, w.it, w.k0 * kTile + tid);
   if constexpr (KV == SJD_BF16) {
-    constexpr int kLag = kStages - 1;
+    constexpr int kLag = kStages > 2 ? kStages - 1 : 0;  // (with two, waiting for the next one's place would hold this one up)
     int owed = 0, owed_stage = 0;  // tiles whose arrival has not been told yet, and the first one's stage
     unsigned owed_mixed = 0;       // of them, bit i: the i-th is to be looked over (take_out)
     int owed_piece = 0;
@@ -522,66 +522,101 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
 
 // --- products -------------------------------------------------------------------
 
-// One warp issues the products of both slots, the slots in turn.
+// The same for a whole warp, which stays together.
+template <int NM>
+__device__ __forceinline__ void wait_together(Misc<NM>* m, unsigned long long* bar, uint32_t parity) {
+  const uint32_t at = smem_addr(bar);
+  if (__all_sync(0xffffffffu, mbar_try(at, parity))) return;
+  const long long begun = clock64();
+  while (!__all_sync(0xffffffffu, mbar_try(at, parity))) {
+    const bool late = clock64() - begun > kWaitClocks;
+    if (__any_sync(0xffffffffu, late || *const_cast<volatile int*>(&m->abort))) {
+      *const_cast<volatile int*>(&m->abort) = 1;
+      return;
+    }
+  }
+}
+// A value that is the same in all lanes, in a register that the warp shares.
+__device__ __forceinline__ int shared_value(int x) { return __reduce_max_sync(0xffffffffu, x); }
+
+// One warp issues the products of both slots, the slots in turn. What it
+// counts and addresses with is kept in the warp's shared registers: else a
+// product costs 110 cycles to issue, and this warp is what all others wait for.
 template <int KV, int DP, int NM>
-__device__ __forceinline__ void issue_products(const AttendParams& p, Misc<NM>* m, uint32_t smem, uint32_t tmem) {
+__device__ __forceinline__ void issue_products(const AttendParams& p, Misc<NM>* m, uint32_t smem, uint32_t tmem_) {
   using P = Plan<KV, DP, NM>;
   constexpr uint32_t kScores = product_kind(kTile, kTile, false, KV != SJD_BF16), kValues = product_kind(kTile, DP, true, KV != SJD_BF16);
   const bool lead = elect_lane();
+  const uint32_t tmem = shared_value(tmem_);
   Walk<NM> w;
   if (!w.begin(p, m->start)) return;
-  int tile0 = 0;              // the block's number of the piece's first tile
+  uint32_t ks = 0, kp = 0, vs = 0, vp = 0;  // the rings' stages and their parities
   uint32_t pp = 0;            // bit 2 * slot + h: parity of p_full[slot][h]
-  do {
-    const int tiles = w.k1 - w.k0, turns = NM * tiles;  // of a slot and a tile, the slots in turn
-    const bool half = w.it.keys - (w.k1 - 1) * kTile <= kHalf;  // of the piece's last tile
+  uint32_t piece = 0;
+  bool more = true;
+  while (more) {
+    const int tiles = shared_value(w.k1 - w.k0), turns = NM * tiles;   // of a slot and a tile, the slots in turn
+    const int last_halves = shared_value(w.it.keys - (w.k1 - 1) * kTile <= kHalf ? 1 : 2);  // of the piece's last tile
+    more = shared_value(w.next(p));
     // S of a slot = Q K^T
     auto scores = [&](int turn) {
-      const int slot = turn & 1, tile = tile0 + turn / NM, stage = tile % P::kK;
-      if (NM == 1 || slot == 0) wait(m, &m->k_full[stage], tile / P::kK & 1);
+      const uint32_t slot = turn & 1;
+      if (NM == 1 || slot == 0) wait_together(m, &m->k_full[ks], kp);
       tc_fence_after();
-      const uint32_t q = smem + (NM == 2 ? slot * tile_bytes(DP) : 0), k = smem + P::kAtK + stage * tile_bytes(DP);
+      const uint64_t q = operand_k(smem + (NM == 2 ? slot * tile_bytes(DP) : 0)), k = operand_k(smem + P::kAtK + ks * tile_bytes(DP));
+      const uint32_t s = tmem + slot * kTile;
       if (lead) {
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
-          const uint32_t at = (i / 4) * (kTile * 128) + (i % 4) * 32;
-          mma_ss(tmem + slot * kTile, operand_k(q + at), operand_k(k + at), kScores, i > 0);
+          constexpr uint32_t kAtom = kTile * 128 / 16;
+          const uint64_t at = (i / 4) * kAtom + (i % 4) * 2;
+          mma_ss(s, q + at, k + at, kScores, i > 0);
         }
         mma_commit(smem_addr(&m->s_full[slot]));
-        if (NM == 1 || slot == 1) mma_commit(smem_addr(&m->k_empty[stage]));
+        if (NM == 1 || slot == 1) mma_commit(smem_addr(&m->k_empty[ks]));
         if (turn + 1 == turns) mma_commit(smem_addr(&m->q_empty));
       }
       __syncwarp();
+      if (NM == 1 || slot == 1) {
+        if (++ks == P::kK) ks = 0, kp ^= 1;
+      }
     };
-    wait(m, &m->q_full, w.piece & 1);
+    wait_together(m, &m->q_full, piece & 1);
     scores(0);
     if (turns > 1) scores(1);
     for (int turn = 0; turn < turns; ++turn) {
-      const int slot = turn & 1, tile = tile0 + turn / NM, stage = tile % P::kV;
-      const int halves = half && turn / NM + 1 == tiles ? 1 : 2;
-      if (NM == 1 || slot == 0) wait(m, &m->v_full[stage], tile / P::kV & 1);
-      for (int h = 0; h < halves; ++h) {
-        wait(m, &m->p_full[slot][h], pp >> (2 * slot + h) & 1);
+      const uint32_t slot = turn & 1;
+      const int halves = turn / NM + 1 == tiles ? last_halves : 2;
+      if (NM == 1 || slot == 0) wait_together(m, &m->v_full[vs], vp);
+      const uint64_t v = operand_n(smem + P::kAtV + vs * tile_bytes(DP), kTile * 128);
+      const uint32_t o = tmem + kOColumn + slot * DP, from = tmem + slot * kTile;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (h >= halves) continue;
+        wait_together(m, &m->p_full[slot][h], pp >> (2 * slot + h) & 1);
         pp ^= 1u << (2 * slot + h);
         tc_fence_after();
         // O of a slot += P V; P lies over S, two weights to a column
-        const uint32_t v = smem + P::kAtV + stage * tile_bytes(DP) + h * (kHalf * 128), from = tmem + slot * kTile + h * (kHalf / 2);
         if (lead) {
 #pragma unroll
           for (int i = 0; i < kHalf / 16; ++i)
-            mma_ts(tmem + kOColumn + slot * DP, from + i * 8, operand_n(v + i * 2048, kTile * 128), kValues, turn >= 2 || h > 0 || i > 0);
-          if (h + 1 == halves && (NM == 1 || slot == 1)) mma_commit(smem_addr(&m->v_empty[stage]));
+            mma_ts(o, from + h * (kHalf / 2) + i * 8, v + (h * (kHalf * 128) + i * 2048) / 16, kValues, turn >= 2 || h > 0 || i > 0);
         }
         __syncwarp();
+      }
+      if (lead && (NM == 1 || slot == 1)) mma_commit(smem_addr(&m->v_empty[vs]));
+      __syncwarp();
+      if (NM == 1 || slot == 1) {
+        if (++vs == P::kV) vs = 0, vp ^= 1;
       }
       if (turn + 2 < turns) scores(turn + 2);
     }
     if (lead) mma_commit(smem_addr(&m->o_full));
     __syncwarp();
-    tile0 += tiles;
-  } while (w.next(p));
+    ++piece;
+  }
   // (nothing is in flight when the block ends)
-  wait(m, &m->o_full, w.piece & 1);
+  wait_together(m, &m->o_full, (piece - 1) & 1);
 }
 
 // --- softmax --------------------------------------------------------------------
