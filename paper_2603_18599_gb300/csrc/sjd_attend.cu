@@ -69,13 +69,14 @@ struct Plan {
 struct Start {
   int kvh, b, mt, k;     // the block's first item: key head, sequence, row tile, key tile
   int start, count;      // the sequence's span
-  long long tile, tiles;  // the block's part of all key tiles
+  long long tile, tiles, per;  // the block's part of all key tiles; a block's fair share
 };
 
 // What a block leaves for the joining kernel: the item of which it has the
 // first part, if other blocks have the rest.
 struct Shared {
   int parts, kvh, b, mt;
+  int done;  // of an item that its blocks join themselves: parts that are there (0 between calls)
 };
 
 // An item's position and its keys.
@@ -156,6 +157,7 @@ struct Misc {
       s_full[2], p_full[2][2];  // by slot (and half)
   uint32_t tmem;
   int abort;
+  int last;                // whether the block joins the item's parts
   int bad_values[4];       // number of the piece (modulo 4) in which a value that some rows do not see is not finite
   Start start;
   Walk<NM> walk[2];        // the softmax groups' ways
@@ -199,7 +201,7 @@ __device__ void locate(const AttendParams& p, Start* s) {
   for (int o = 16; o > 0; o /= 2) per_head += __shfl_xor_sync(0xffffffffu, per_head, o);
   const long long all = per_head * p.c.Hkv, per = (all + gridDim.x - 1) / gridDim.x, from = blockIdx.x * per;
   const long long mine = max(0ll, min(per, all - from));
-  if (lane == 0) s->tile = from, s->tiles = mine;
+  if (lane == 0) s->tile = from, s->tiles = mine, s->per = per;
   if (mine == 0) return;
   const int kvh = static_cast<int>(from / per_head);
   long long rest = from - kvh * per_head;
@@ -216,7 +218,7 @@ __device__ void locate(const AttendParams& p, Start* s) {
         rest -= upto - x;
         int mt = 0, t;
         while (rest >= (t = (keys_of<NM>(p, span.x, span.y, mt) + kTile - 1) / kTile)) rest -= t, ++mt;
-        *s = {kvh, b0 + lane, mt, static_cast<int>(rest), span.x, span.y, from, mine};
+        *s = {kvh, b0 + lane, mt, static_cast<int>(rest), span.x, span.y, from, mine, per};
       }
       return;
     }
@@ -794,7 +796,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int a = max(key0 + 32 * i, it.start), e = min(key0 + 32 * i + 32, it.keys);
-#pragma unroll 1
+#pragma unroll 8
               for (int key = a; key < e; ++key)
                 if (!mask[key]) seen[i] &= ~(1u << (key - key0 - 32 * i));
             }
@@ -966,7 +968,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     if (threadIdx.x == 0 && w.k0 == 0 && w.k1 < it.tiles) {
       // the rest of the item lies in the blocks after this one
       const long long beyond = m->start.tile + tile_no + it.tiles - 1;
-      shared[blockIdx.x] = {static_cast<int>(beyond / m->start.tiles - blockIdx.x + 1), it.kvh, it.b, it.mt};
+      shared[blockIdx.x] = {static_cast<int>(beyond / m->start.per - blockIdx.x + 1), it.kvh, it.b, it.mt, 0};
     }
     tile_no += tiles;
     if (NM == 1) {  // both groups have read both accumulators and the rows' sums
@@ -981,11 +983,25 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
   }
 }
 
+// The rows beyond each sequence's span: the block's sequences, a warp (of
+// `step`) to a row.
+__device__ __forceinline__ void clear_rows(const AttendParams& p, int row0, int step, int lane) {
+  for (int b = blockIdx.x; b < p.c.B; b += gridDim.x) {
+    const int2 span = span_of(p.c, b);
+    const long long begin = (static_cast<long long>(b) * p.c.n + span.y) * p.c.Hq, end = (b + 1ll) * p.c.n * p.c.Hq;
+    for (long long row = begin + row0; row < end; row += step) {
+      for (int i = lane; i < p.c.D / 8; i += 32)
+        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.o) + row * p.c.D + 8 * i) = make_uint4(0, 0, 0, 0);
+      if (p.lse && lane == 0) p.lse[row] = -INFINITY;
+    }
+  }
+}
+
 // The softmax of at most 128 / SP rows, SP = 2 or 4 copies of them in the tile
 // (NM = 1). A warp has the 128 / SP keys of its copy.
 template <int KV, int DP, int SP>
 __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m, unsigned char* queries, uint32_t tmem, float* parts, float2* part_rows,
-                                               Shared* shared) {
+                                               Shared* shared, bool join_here) {
   constexpr int kRows = kTile / SP, kKeys = kTile / SP, kChunks = kKeys / 32, kWarps = 4 / SP;  // of a copy
   const int slot = threadIdx.x / 128, at = threadIdx.x & 127, lane = threadIdx.x & 31, copy = at / kRows, row = at % kRows;
   const uint32_t lanes = static_cast<uint32_t>(at & ~31) << 16;
@@ -1072,7 +1088,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
             if (p.mask_kind == SJD_MASK_GIVEN && valid) {
               const uint8_t* mask = p.mask + p.mask_b * it.b + p.mask_r * t - it.start;
               const int a = max(key0 + 32 * i, it.start), e = min(key0 + 32 * i + 32, it.keys);
-#pragma unroll 1
+#pragma unroll 8
               for (int key = a; key < e; ++key)
                 if (!mask[key]) seen &= ~(1u << (key - key0 - 32 * i));
             }
@@ -1209,13 +1225,62 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
       named_barrier(1, 256);
     }
     tc_fence_before();
-    if (threadIdx.x == 0) {
-      mbar_arrive(smem_addr(&m->q_empty));  // (the queries' memory is free again)
-      if (w.k0 == 0 && w.k1 < it.tiles) {
-        const long long beyond = m->start.tile + tile_no + it.tiles - 1;
-        shared[blockIdx.x] = {static_cast<int>(beyond / m->start.tiles - blockIdx.x + 1), it.kvh, it.b, it.mt};
+    if (!wholly) {
+      const long long begin = m->start.tile + tile_no - w.k0, end = begin + it.tiles - 1, per = m->start.per;
+      const int first = static_cast<int>(begin / per), count = static_cast<int>(end / per) - first + 1;
+      if (!join_here) {
+        if (threadIdx.x == 0 && w.k0 == 0) shared[blockIdx.x] = {count, it.kvh, it.b, it.mt, 0};
+      } else {
+        // the block whose part is the last to be there joins them all, in their order
+        __threadfence();
+        named_barrier(1, 256);
+        if (threadIdx.x == 0) {
+          m->last = atomicAdd(&shared[first].done, 1) == count - 1;
+          if (m->last) shared[first].done = 0;
+          __threadfence();
+        }
+        named_barrier(1, 256);
+        if (m->last) {
+          // every part's factor, and each row's sum in the place after them
+          float* factor = reinterpret_cast<float*>(queries);
+          auto part_at = [&](int k, int r) { return (2ll * (first + k) + (k == 0 ? 1 : 0)) * kTile + r; };
+          const int rows = it.rows;
+          for (int r = threadIdx.x / 32; r < rows; r += 8) {
+            const float2 rs = lane < count ? __ldcg(&part_rows[part_at(lane, r)]) : make_float2(-INFINITY, 0.0f);
+            float top = rs.x;
+            for (int k = 16; k > 0; k /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+            const float f = rs.x == -INFINITY ? 0.0f : exp2_fast(rs.x - top);
+            float all = rs.y * f;
+            for (int k = 16; k > 0; k /= 2) all += __shfl_xor_sync(0xffffffffu, all, k);
+            const bool some = all > 0.0f || all != all;
+            factor[32 * r + lane] = f * (some ? 1.0f / all : 0.0f);
+            if (p.lse && lane == 0) {
+              const int its_t = by_group(p.c, r);
+              const long long head = (static_cast<long long>(it.b) * p.c.n + its_t) * p.c.Hq + static_cast<long long>(it.kvh) * G + r - its_t * G;
+              p.lse[head] = some ? (top + log2f(all)) * 0.69314718055994531f : -INFINITY;
+            }
+          }
+          named_barrier(1, 256);
+          constexpr int kAcross = DP / 4;
+          for (int i = threadIdx.x; i < rows * kAcross; i += 256) {
+            const int r = i / kAcross, col = i % kAcross * 4;
+            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+            for (int k = 0; k < count; ++k) {
+              const float f = factor[32 * r + k];
+              const float4 v = __ldcg(reinterpret_cast<const float4*>(parts + part_at(k, r) * DP + col));
+              o.x = fmaf(v.x, f, o.x), o.y = fmaf(v.y, f, o.y), o.z = fmaf(v.z, f, o.z), o.w = fmaf(v.w, f, o.w);
+            }
+            const int its_t = by_group(p.c, r);
+            const long long head = (static_cast<long long>(it.b) * p.c.n + its_t) * p.c.Hq + static_cast<long long>(it.kvh) * G + r - its_t * G;
+            if (col < p.c.D)
+              *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.o) + head * p.c.D + col) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
+          }
+          named_barrier(1, 256);  // (the queries' memory is used no more)
+        }
       }
     }
+    if (threadIdx.x == 0) mbar_arrive(smem_addr(&m->q_empty));  // the queries' memory is free again
     tile_no += tiles;
     named_barrier(2 + slot, 128);
     if (tile_no == m->start.tiles) return;
@@ -1225,15 +1290,13 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
 }
 
 template <int KV, int DP, int NM, int SP>
-__global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendParams p, float* parts, float2* part_rows, Shared* shared) {
+__global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendParams p, float* parts, float2* part_rows, Shared* shared, bool join_here) {
   extern __shared__ __align__(1024) unsigned char raw[];
   using P = Plan<KV, DP, NM>;
   Misc<NM>* m = reinterpret_cast<Misc<NM>*>(raw + P::kAtMisc);
   const uint32_t smem = smem_addr(raw);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0);  // (the same for all lanes, to the compiler too)
   let_next_start();
-  wait_for_previous();
-  if (warp == 0) locate<NM>(p, &m->start);
   if (warp == kMmaWarp) tmem_alloc(smem_addr(&m->tmem), kTmemColumns);
   if (threadIdx.x == 256) {
     for (int i = 0; i < 5; ++i) {
@@ -1246,15 +1309,17 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
     }
     m->abort = 0;
     for (int i = 0; i < 4; ++i) m->bad_values[i] = m->poison[0][i] = m->poison[1][i] = 0;
-    shared[blockIdx.x].parts = 0;
     fence_barrier_init();
   }
+  wait_for_previous();
+  if (warp == 0) locate<NM>(p, &m->start);
+  if (threadIdx.x == 256) shared[blockIdx.x].parts = 0;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = m->tmem;
   if (warp < 8) {
-    if constexpr (SP > 1) softmax_copies<KV, DP, SP>(p, m, raw, tmem, parts, part_rows, shared);
+    if constexpr (SP > 1) softmax_copies<KV, DP, SP>(p, m, raw, tmem, parts, part_rows, shared, join_here);
     else softmax_rows<KV, DP, NM>(p, m, tmem, parts, part_rows, shared);
   } else if (warp < 12) {
     load_operand<KV, DP, NM, SP, false>(p, m, smem);
@@ -1262,6 +1327,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
     load_operand<KV, DP, NM, SP, true>(p, m, smem);
   } else if (warp == kMmaWarp) {
     issue_products<KV, DP, NM>(p, m, smem, tmem);
+  } else if (SP > 1 && join_here) {
+    clear_rows(p, warp - 16, kMmaWarp - 16, threadIdx.x & 31);
   }
   tc_fence_before();
   __syncthreads();
@@ -1319,15 +1386,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const AttendParam
       if (p.lse && lane == 0) p.lse[head] = sum > 0.0f || sum != sum ? (top + log2f(sum)) * 0.69314718055994531f : -INFINITY;
     }
   }
-  for (int b = blockIdx.x; b < p.c.B; b += gridDim.x) {
-    const int2 span = span_of(p.c, b);
-    const long long begin = (static_cast<long long>(b) * p.c.n + span.y) * p.c.Hq, end = (b + 1ll) * p.c.n * p.c.Hq;
-    for (long long row = begin + row0; row < end; row += step) {
-      for (int i = lane; i < p.c.D / 8; i += 32)
-        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.o) + row * p.c.D + 8 * i) = make_uint4(0, 0, 0, 0);
-      if (p.lse && lane == 0) p.lse[row] = -INFINITY;
-    }
-  }
+  clear_rows(p, row0, step, lane);
 }
 
 template <int KV, int DP, int NM, int SP>
@@ -1337,8 +1396,16 @@ cudaError_t launch(const AttendParams& p, int sms, unsigned char* scratch, cudaS
   Shared* shared = reinterpret_cast<Shared*>(scratch);
   float2* part_rows = reinterpret_cast<float2*>(scratch + kMaxAttendBlocks * sizeof(Shared));
   float* parts = reinterpret_cast<float*>(part_rows + rows);
-  const cudaError_t e = launch_early(attend_kernel<KV, DP, NM, SP>, blocks, kAttendThreads, shared_bytes<KV, DP, NM>(), s, p, parts, part_rows, shared);
-  if (e != cudaSuccess) return e;
+  // At most 32 rows, of which at most 22 blocks have a part (an item is at most
+  // one of kv_heads equal shares of the tiles): the last of them to be done joins
+  // them, which saves a launch (one token of two sequences of 300:
+  // 13.0 us a call against 14.6; 64 rows of nine parts take longer that way, 28.7
+  // against 18.5).
+  const bool join_here = SP == 4 && p.c.Hkv >= 8;
+  static_assert(kMaxAttendBlocks / 8 + 2 <= 32, "a lane to a part");
+  const cudaError_t e =
+      launch_early(attend_kernel<KV, DP, NM, SP>, blocks, kAttendThreads, shared_bytes<KV, DP, NM>(), s, p, parts, part_rows, shared, join_here);
+  if (e != cudaSuccess || join_here) return e;
   return launch_early(join_kernel<DP>, dim3(blocks, 8), 32 * kJoinWarps, 0, s, p, parts, part_rows, shared, kTile * NM);
 }
 
@@ -1371,6 +1438,8 @@ cudaError_t prepare_attend(int kv_dtype, int head_dim) {
   if (kv_dtype == SJD_E4M3) return small ? raise_limits<SJD_E4M3, 64>() : raise_limits<SJD_E4M3, 128>();
   return small ? raise_limits<SJD_S8, 64>() : raise_limits<SJD_S8, 128>();
 }
+
+size_t attend_counter_bytes() { return kMaxAttendBlocks * sizeof(Shared); }
 
 size_t attend_scratch_bytes(int head_dim, long long rows) {
   const size_t per = (rows > kTile ? 2 : 1) * static_cast<size_t>(kTile), dp = head_dim <= 64 ? 64 : 128;

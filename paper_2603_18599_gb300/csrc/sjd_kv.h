@@ -115,5 +115,6 @@ cudaError_t launch_attend(const AttendParams& p, int kv_dtype, int sms, unsigned
 // Sets the kernels' limits on the current device, once for a handle.
 cudaError_t prepare_attend(int kv_dtype, int head_dim);
 size_t attend_scratch_bytes(int head_dim, long long rows);
+size_t attend_counter_bytes();  // the scratch's beginning, which is to be 0 before the first call
 
 }  // namespace sjd_kv_ops

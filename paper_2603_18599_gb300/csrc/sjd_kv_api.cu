@@ -122,7 +122,7 @@ int sjd_kv_init(const sjd_kv_config* cfg, void* workspace, size_t ws_bytes, void
   if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
     return SJD_ERR_CUDA;
   if (prepare_attend(cfg->kv_dtype, cfg->head_dim) != cudaSuccess) return SJD_ERR_CUDA;
-  if (cudaMemsetAsync(workspace, 0, kAlign, s) != cudaSuccess) return SJD_ERR_CUDA;
+  if (cudaMemsetAsync(workspace, 0, kAlign + attend_counter_bytes(), s) != cudaSuccess) return SJD_ERR_CUDA;
   sjd_kv* kv = new (std::nothrow) sjd_kv{*cfg, static_cast<unsigned char*>(workspace), s, sms, ""};
   if (!kv) return SJD_ERR_CAPACITY;
   *out = kv;
@@ -197,7 +197,8 @@ int sjd_kv_sync(sjd_kv* kv) {
   cudaError_t e = cudaMemcpyAsync(&bits, kv->ws, sizeof bits, cudaMemcpyDeviceToHost, kv->stream);
   if (e == cudaSuccess) e = cudaStreamSynchronize(kv->stream);
   if (e == cudaSuccess && bits) {
-    e = cudaMemsetAsync(kv->ws, 0, sizeof bits, kv->stream);
+    // (a kernel that gave up may have left its counters)
+    e = cudaMemsetAsync(kv->ws, 0, bits & status_bit(SJD_ERR_TIMEOUT) ? kAlign + attend_counter_bytes() : sizeof bits, kv->stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize(kv->stream);
   }
   if (e != cudaSuccess) return launched(kv, e, "sync");

@@ -130,16 +130,20 @@ class Rope:
         """x [B, n, H, D] (bf16 or f32) turned by positions [B, n, axes]
         int32; with `inverse` by the transpose, which takes the gradient of
         the result to that of x. `out` may be x."""
-        if x.dim() != 4 or x.dtype not in _DTYPES or x.device != self.device:
-            raise ValueError("x must be a [B, n, H, D] bf16 or f32 tensor on %s" % (self.device,))
-        B, n, H, D = x.shape
-        at = _array(positions, "positions", (B, n, self.axes), self.device)
+        dev, dtype = self.device, x.dtype
+        if x.dim() != 4 or dtype not in _DTYPES or x.device != dev:
+            raise ValueError("x must be a [B, n, H, D] bf16 or f32 tensor on %s" % (dev,))
+        shape = B, n, H, D = x.shape
+        at = _array(positions, "positions", (B, n, self.axes), dev)
+        xw = _view_of(x, "x", shape, dtype, dev)
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            out = torch.empty(shape, dtype=dtype, device=dev)
+            ow = _VIEW.pack(out.data_ptr(), n * H * D, H * D, D)
+        else:
+            ow = _view_of(out, "out", shape, dtype, dev)
         if x.numel() == 0:
             return out
-        args = (self._c, _view_of(x, "x", x.shape, x.dtype, x.device), _view_of(out, "out", x.shape, x.dtype, x.device), at,
-                B, n, H, D, _DTYPES[x.dtype], 1 if inverse else 0, _raw_stream(self.device.index))
+        args = (self._c, xw, ow, at, B, n, H, D, _DTYPES[dtype], 1 if inverse else 0, _raw_stream(dev.index))
         if _current_device() == self.device.index:
             rc = load().sjd_rotate(*args)
         else:
@@ -267,9 +271,12 @@ class KV:
             rope_c, pos, turns, axis = rope._c, _array(positions, "positions", (B, n, rope.axes), self.device), rope._turns, rope._axis
         if q is not None:
             shape = (B, n, c.heads, c.head_dim)
+            qw = _view_of(q, "q", shape, dt, self.device)
             if q_out is None:
                 q_out = torch.empty(shape, dtype=dt, device=self.device)
-            qw, ow = _view_of(q, "q", shape, dt, self.device), _view_of(q_out, "q_out", shape, dt, self.device)
+                ow = _VIEW.pack(q_out.data_ptr(), n * c.heads * c.head_dim, c.heads * c.head_dim, c.head_dim)
+            else:
+                ow = _view_of(q_out, "q_out", shape, dt, self.device)
         self._run(self.L.sjd_kv_write, (self.ctx, at, span, _DTYPES[dt], kw, vw, rope_c, pos, qw, ow),
                   (*layer._t, k, v, table, start, count, positions, q, q_out, turns, axis))
         return q_out

@@ -374,6 +374,13 @@ CASES = [  # B, heads, kv_heads, D, page, starts, n, counts, mask
     (2, 2, 2, 128, 64, [20000, 4096], 1, None, "causal"),
     (17, 4, 2, 64, 16, [31 * i for i in range(17)], 2, None, "causal"),
     (40, 2, 1, 64, 16, [5 * i for i in range(40)], 3, [i % 4 for i in range(40)], "causal"),
+    (9, 2, 1, 64, 16, [30000] + [3] * 8, 1, None, "causal"),       # one sequence has nearly all blocks
+    (9, 8, 8, 64, 16, [30000] + [3] * 8, 4, [4] * 8 + [0], "causal"),
+    (3, 32, 8, 128, 32, [2500, 70, 0], 8, [8, 0, 3], "causal"),    # 32 rows
+    (3, 32, 8, 128, 32, [2500, 70, 0], 9, [9, 0, 9], None),        # 36
+    (2, 64, 4, 96, 16, [1300, 1], 4, None, "own"),                 # 64
+    (2, 64, 4, 96, 16, [1300, 1], 5, None, "own"),                 # 80
+    (1, 16, 2, 72, 16, [5000], 4, None, "empty"),                  # vectors of 72 codes
 ]
 
 
