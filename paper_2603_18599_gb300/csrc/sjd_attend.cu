@@ -59,9 +59,9 @@ template <int KV, int DP, int NM>
 struct Plan {
   static constexpr bool kCodes = KV != SJD_BF16;
   static constexpr uint32_t kQ = NM * tile_bytes(DP);
-  static constexpr int kK = kCodes ? (DP == 128 ? 2 : 3) : (DP == 128 ? 3 : 5);                       // key tiles
-  static constexpr int kV = kCodes ? (DP == 128 ? 2 : 3) : (DP == 128 ? (NM == 1 ? 3 : 2) : 5);       // value tiles
-  static constexpr int kRaw = !kCodes ? 0 : DP == 64 ? 4 : NM == 1 ? 2 : 1;  // of keys, and of values
+  static constexpr int kK = kCodes ? (DP == 64 ? 3 : NM == 1 ? 1 : 2) : (DP == 128 ? 3 : 5);          // key tiles
+  static constexpr int kV = kCodes ? (DP == 64 ? 3 : 1) : (DP == 128 ? (NM == 1 ? 3 : 2) : 5);        // value tiles
+  static constexpr int kRaw = !kCodes ? 0 : DP == 64 || NM == 1 ? 4 : 2;  // of keys, and of values
   static constexpr uint32_t kAtK = kQ, kAtV = kAtK + kK * tile_bytes(DP), kAtRawK = kAtV + kV * tile_bytes(DP),
                             kAtRawV = kAtRawK + kRaw * kTile * DP, kAtMisc = kAtRawV + kRaw * kTile * DP;
 };
@@ -377,45 +377,14 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
   uint32_t round = 1;         // parity of the empty barriers' phase before it
   int page = key_page(p.c, w.it, w.k0 * kTile + tid);
   if constexpr (KV == SJD_BF16) {
-    constexpr int kLag = kStages > 2 ? kStages - 1 : 0;  // (with two, waiting for the next one's place would hold this one up)
-    int owed = 0, owed_stage = 0;  // tiles whose arrival has not been told yet, and the first one's stage
-    unsigned owed_mixed = 0;       // of them, bit i: the i-th is to be looked over (take_out)
-    int owed_piece = 0;
-    auto tell = [&]() {
-      if constexpr (IS_V) {
-        if (owed_mixed & 1) {
-          bool bad = false;
-#pragma unroll 1
-          for (int i = 0; i < kRounds; ++i) {
-            const uint32_t at = ring + owed_stage * tile_bytes(DP) + piece_at(warp * 32 + i * kStep + first, piece);
-            uint4 v = shared_load16(at);
-            const bool a = take_out(v.x), b = take_out(v.y), c = take_out(v.z), d = take_out(v.w);
-            if (a || b || c || d) shared_store16(at, v), bad = true;
-          }
-          if (bad) m->bad_values[owed_piece & 3] = owed_piece + 1;
-        }
-        owed_mixed >>= 1;
-      }
-      fence_async_shared();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_addr(&full[owed_stage]));
-      if (++owed_stage == kStages) owed_stage = 0;
-      --owed;
-    };
-    auto drain = [&]() {
-      copy_wait<0>();
-      while (owed > 0) tell();
-    };
     bool more = true;
     while (more) {
       if constexpr (IS_V) {
-        drain();
         queries(w.piece);
         load_queries<DP, NM, SP>(p, w.it, smem, tid);
         queries_there();
-        owed_piece = w.piece;
       }
-      const int common = IS_V ? common_keys<NM>(p, w.it) : 0, k1 = w.k1;
+      const int common = IS_V ? common_keys<NM>(p, w.it) : 0, k1 = w.k1, number = w.piece;
       for (int k = w.k0; k < k1; ++k) {
         const uint32_t mine = vector_in(p.c, page, k * kTile + tid, w.it.kvh);
         if (k + 1 < k1) {
@@ -433,19 +402,25 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
         for (int i = 0; i < kRounds; ++i)
           copy16(to + piece_at(warp * 32 + i * kStep + first, piece), own + static_cast<size_t>(at[i] != kNoVector ? at[i] : 0) * vector_bytes,
                  at[i] != kNoVector ? in : 0);
-        copy_commit();
-        if constexpr (IS_V) {
-          if ((k + 1) * kTile > common) owed_mixed |= 1u << owed;
+        if (IS_V && (k + 1) * kTile > common) {  // some row does not see every key (take_out)
+          copy_commit();
+          copy_wait<0>();
+          bool bad = false;
+#pragma unroll 1
+          for (int i = 0; i < kRounds; ++i) {
+            const uint32_t at = to + piece_at(warp * 32 + i * kStep + first, piece);
+            uint4 v = shared_load16(at);
+            const bool a = take_out(v.x), b = take_out(v.y), c = take_out(v.z), d = take_out(v.w);
+            if (a || b || c || d) shared_store16(at, v), bad = true;
+          }
+          if (bad) m->bad_values[number & 3] = number + 1;
+          mbar_arrive(smem_addr(&full[stage]));
+        } else {
+          copy_arrive(smem_addr(&full[stage]));
         }
-        ++owed;
         if (++stage == kStages) stage = 0, round ^= 1;
-        if (owed > kLag) {
-          copy_wait<kLag>();
-          tell();
-        }
       }
     }
-    drain();
   } else {
     // The codes come into a ring of their own, up to kRaw tiles ahead, 16 to a
     // copy where a vector's length is a multiple of that (past the L1 cache)
@@ -563,7 +538,10 @@ __device__ __forceinline__ void issue_products(const AttendParams& p, Misc<NM>* 
     // S of a slot = Q K^T
     auto scores = [&](int turn) {
       const uint32_t slot = turn & 1;
-      if (NM == 1 || slot == 0) wait_together(m, &m->k_full[ks], kp);
+      if (NM == 1 || slot == 0) {
+        wait_together(m, &m->k_full[ks], kp);
+        if (KV == SJD_BF16) fence_async_shared();  // (of the copies, which the barrier has made this warp see)
+      }
       tc_fence_after();
       const uint64_t q = operand_k(smem + (NM == 2 ? slot * tile_bytes(DP) : 0)), k = operand_k(smem + P::kAtK + ks * tile_bytes(DP));
       const uint32_t s = tmem + slot * kTile;
@@ -589,7 +567,10 @@ __device__ __forceinline__ void issue_products(const AttendParams& p, Misc<NM>* 
     for (int turn = 0; turn < turns; ++turn) {
       const uint32_t slot = turn & 1;
       const int halves = turn / NM + 1 == tiles ? last_halves : 2;
-      if (NM == 1 || slot == 0) wait_together(m, &m->v_full[vs], vp);
+      if (NM == 1 || slot == 0) {
+        wait_together(m, &m->v_full[vs], vp);
+        if (KV == SJD_BF16) fence_async_shared();
+      }
       const uint64_t v = operand_n(smem + P::kAtV + vs * tile_bytes(DP), kTile * 128);
       const uint32_t o = tmem + kOColumn + slot * DP, from = tmem + slot * kTile;
 #pragma unroll
@@ -1300,8 +1281,10 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
   if (warp == kMmaWarp) tmem_alloc(smem_addr(&m->tmem), kTmemColumns);
   if (threadIdx.x == 256) {
     for (int i = 0; i < 5; ++i) {
-      mbar_init(smem_addr(&m->k_full[i]), 4), mbar_init(smem_addr(&m->k_empty[i]), 1);
-      mbar_init(smem_addr(&m->v_full[i]), 4), mbar_init(smem_addr(&m->v_empty[i]), 1);
+      // (16-bit tiles are there when every thread's copies are, 8-bit ones when the warps have turned them into fp16)
+      const int loaders = KV == SJD_BF16 ? 128 : 4;
+      mbar_init(smem_addr(&m->k_full[i]), loaders), mbar_init(smem_addr(&m->k_empty[i]), 1);
+      mbar_init(smem_addr(&m->v_full[i]), loaders), mbar_init(smem_addr(&m->v_empty[i]), 1);
     }
     mbar_init(smem_addr(&m->q_full), 4), mbar_init(smem_addr(&m->q_empty), SP > 1 ? 2 : 1), mbar_init(smem_addr(&m->o_full), 1);
     for (int i = 0; i < 2; ++i) {
