@@ -53,9 +53,9 @@ extern "C" {
 #define SJD_ERR_INVALID_DRAFT 6  /* a draft token has zero draft probability     */
 #define SJD_ERR_CALLBACK 7       /* the forward callback returned non-zero       */
 #define SJD_ERR_STATE 8          /* call out of order (see sjd_draft)            */
-#define SJD_ERR_TIMEOUT 9        /* reserved for a bounded wait inside a kernel;
-                                    no current kernel waits, so it is not
-                                    returned                                    */
+#define SJD_ERR_TIMEOUT 9        /* a wait inside a kernel ran out (sjd_kv_attend,
+                                    whose warps wait for one another; no
+                                    other kernel waits)                         */
 #define SJD_ERR_BOUNDS 10        /* the bounds-checked build (libsjd_checked.so)
                                     found an index outside its array; the
                                     access was clamped, results are not valid  */
@@ -421,13 +421,15 @@ typedef struct {
   int32_t batch;                 /* sequences: an image's conditional and
                                     unconditional branches are two            */
   int32_t heads;                 /* query heads, a multiple of kv_heads        */
-  int32_t kv_heads;              /* key and value heads; query head h reads
-                                    head h / (heads / kv_heads); heads /
-                                    kv_heads at most 128                       */
+  int32_t kv_heads;              /* key and value heads, at most 65536; query
+                                    head h reads head h / (heads / kv_heads);
+                                    heads / kv_heads at most 128               */
   int32_t head_dim;              /* a multiple of 8, 8..128                    */
   int32_t page_size;             /* tokens of a page, any number from 1 on     */
-  int32_t n_pages;               /* pages of the cache                         */
-  int32_t max_pages;             /* entries of one sequence's page table       */
+  int32_t n_pages;               /* pages of the cache; with kv_heads and
+                                    page_size fewer than 2^32 - 1 vectors      */
+  int32_t max_pages;             /* entries of one sequence's page table;
+                                    max_pages * page_size at most 2^30         */
   int32_t max_new;               /* most new tokens of a sequence in a call    */
   int32_t kv_dtype;              /* SJD_BF16, SJD_E4M3 or SJD_S8               */
 } sjd_kv_config;
@@ -478,14 +480,16 @@ int sjd_rope_turns(const double* freq_host, int32_t n, uint64_t* turns_host);
 
 /* y = R(positions) x, or with inverse != 0 its transpose, which is both the
  * inverse and the gradient: dL/dx = R^T dL/dy. x and y: [batch][n][heads]
- * [dim] of dtype SJD_F32 or SJD_BF16 (fp32 inside), dim a multiple of 8 up
- * to 256; y may be x, element for element, or apart from it. positions_dev:
+ * [dim] of dtype SJD_F32 or SJD_BF16 (fp32 inside), heads up to 2^20, dim a
+ * multiple of 8 up to 256; y may be x, element for element, or apart from it. positions_dev:
  * int32 [batch][n][axes], any value. Errors: SJD_ERR_ARG, SJD_ERR_CUDA. */
 int sjd_rotate(const sjd_rope* rope, const sjd_view* x, const sjd_view* y, const int32_t* positions_dev,
                int32_t batch, int32_t n, int32_t heads, int32_t dim, int32_t dtype, int32_t inverse,
                void* cuda_stream);
 
-/* Bytes of device workspace a handle needs (0: invalid configuration). */
+/* Bytes of device workspace a handle needs (0: invalid configuration): the
+ * device status and what the blocks of sjd_kv_attend leave for one another, up
+ * to 42 MB. */
 size_t sjd_kv_workspace_size(const sjd_kv_config* cfg);
 
 /* Check cfg and bind a handle to the caller's workspace (256-byte aligned,
@@ -527,12 +531,15 @@ int sjd_kv_read(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span, 
  *   lse = ln sum_j exp(scale * q . k_j).
  * q [batch][n][heads][head_dim] in bf16, 16-byte aligned rows; o_dev
  * [batch][n][heads][head_dim] in bf16, contiguous; lse_dev fp32 [batch][n]
- * [heads], or NULL. Products are summed in fp32; the weights p are rounded
- * to bf16 before their product with the values (an 8-bit value's scale goes
- * into its weight first), their sum is not. A row that sees no key, and rows
- * from count[b] on, give o = 0 and lse = -inf; a key that a row does not see
- * has no effect on it, whatever it holds. The result does not depend on
- * the GPU's timing: the same inputs give the same bits.
+ * [heads], or NULL. Scores and sums are fp32. The weights are rounded to 16
+ * bits before their product with the values: with a 16-bit cache to bf16, with
+ * an 8-bit one, after a factor of the values' scale over the largest scale so
+ * far, to fp16 (a weight below 2^-30 of the row's largest is then lost). The
+ * queries are exact, but for an 8-bit cache those elements below 2^-15 of
+ * their row's largest, which keep an error of 2^-25 of that. A row that sees no
+ * key, and rows from count[b] on, give o = 0 and lse = -inf; a key that a row
+ * does not see has no effect on it, whatever it holds. The result does not
+ * depend on the GPU's timing: the same inputs give the same bits.
  * mask_dev (SJD_MASK_GIVEN): bytes, element (b, t, i) at mask_batch_stride *
  * b + mask_row_stride * t + i. Errors as sjd_kv_write, and SJD_ERR_TIMEOUT
  * via sjd_kv_sync should a wait inside the kernel have run out (the results

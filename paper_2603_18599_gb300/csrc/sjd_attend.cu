@@ -49,6 +49,7 @@ constexpr uint32_t kOColumn = 2 * kTile;
 constexpr long long kWaitClocks = 4000000000ll;  // about two seconds
 constexpr float kLeast = 1e-30f;
 constexpr int kRoom = 6;
+constexpr float kFar = 0x1p20f;         // from here on a score's product with c is rounded too coarsely (2^-4)
 constexpr float kRise = 8.0f;           // a row's reference maximum moves when it is behind by more than 2^8
 
 __host__ __device__ constexpr uint32_t tile_bytes(int dp) { return static_cast<uint32_t>(kTile) * dp * 2; }
@@ -71,6 +72,17 @@ struct Start {
   int start, count;      // the sequence's span
   long long tile, tiles, per;  // the block's part of all key tiles; a block's fair share
 };
+
+// Weights are powers of two: 2^(c (q . k)), c = |scale| log2 e. (Not 0, so that
+// a score of -inf gives a weight of 0 at any scale.)
+__device__ __forceinline__ float power_factor(const AttendParams& p) { return fmaxf(fabsf(p.scale) * 1.4426950408889634f, kLeast); }
+// What a sum of weights against the reference score `from` is worth against `to`.
+__device__ __forceinline__ float worth(float from, float to, float c) {
+  return from == -INFINITY ? 0.0f : from == to ? 1.0f : exp2_fast((from - to) * c);
+}
+__device__ __forceinline__ float log_of_sum(const AttendParams& p, float ref, float sum) {
+  return sum > 0.0f || sum != sum ? fmaf(log2f(sum), 0.69314718055994531f, ref * fabsf(p.scale)) : -INFINITY;
+}
 
 // What a block leaves for the joining kernel: the item of which it has the
 // first part, if other blocks have the rest.
@@ -665,6 +677,23 @@ __device__ __forceinline__ float largest_of(const uint32_t (&s)[32], float t) {
   }
   return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
 }
+// Scores so large that rounding their product with c would change weights by
+// powers of two are taken less the reference first, in tensor memory.
+template <int KEYS>
+__device__ __noinline__ void less_reference(uint32_t s_at, float ref, float& base) {
+  const float from = ref == -INFINITY ? 0.0f : ref;
+  base = 0.0f;
+#pragma unroll 1
+  for (int i = 0; i < KEYS / 32; ++i) {
+    uint32_t s[32];
+    tmem_load32(s_at + 32 * i, s);
+    tmem_wait_load(s);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) - from);
+    tmem_store32(s_at + 32 * i, s);
+  }
+  tmem_wait_store();
+}
 // The weights of 32 scores, 2^(c s - base), packed to 16 bits, in an 8-bit
 // cache times the values' factors; and their sum.
 template <int KV>
@@ -697,8 +726,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
   const uint32_t lanes = static_cast<uint32_t>(warp_row) << 16;
   const uint32_t s_at = tmem + lanes + slot * kTile, o_at = tmem + lanes + kOColumn;
   const int G = p.c.group;
-  // log2 e: weights are powers of two. (The factors are never 0: times a score of -inf they are -inf.)
-  const float c = fmaxf(fabsf(p.scale) * 1.4426950408889634f, kLeast);
+  const float c = power_factor(p);
   // (the group's way is kept in shared memory: its registers are for the scores)
   Walk<NM>& w = m->walk[slot];
   const Item& it = w.it;
@@ -722,7 +750,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     // In an 8-bit cache the weights are fp16: 2^kRoom p (v / unit), the values' factors v in units
     // of a power of two, the largest so far. With p up to 2^8 nothing overflows, and what is
     // below 2^-30 of the largest is lost.
-    float c_row = c, unit = 0.0f;
+    float c_row = c, row_unit = 1.0f, unit = 0.0f;
     // an 8-bit cache's factors of key `row` of the tiles: the next tile's are on their way while
     // one is worked on, and the page of the one after that
     float next_k = 0.0f, next_v = 0.0f;
@@ -791,7 +819,10 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
         const float* fv = m->row[slot][1];
         float top = -INFINITY, grown = 1.0f;
         if (KV != SJD_BF16) {
-          if (u == 0) c_row = fmaxf(c * __uint_as_float(static_cast<uint32_t>(127 + m->exponents[w.piece & 1][(NM == 2 ? slot * kTile : 0) + row]) << 23), 1e-37f);
+          if (u == 0) {
+            row_unit = __uint_as_float(static_cast<uint32_t>(127 + m->exponents[w.piece & 1][(NM == 2 ? slot * kTile : 0) + row]) << 23);
+            c_row = fmaxf(c * row_unit, 1e-37f);
+          }
           const uint32_t most = max(max(m->most[slot][0], m->most[slot][1]), max(m->most[slot][2], m->most[slot][3]));
           // (the power of two from there on, at least 2^-100 and at most 2^120)
           const float now = __uint_as_float(max(27u << 23, min(247u << 23, (most + 0x7fffffu) & 0x7f800000u)));
@@ -813,13 +844,12 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
         }
         if (!two) tmem_wait_load(s[0]);
         if (KV != SJD_BF16) tmem_wait_store();
-        top *= c_row;
         // The reference that the weights are taken against moves only where a
         // weight could pass 2^8: their relative precision is the same below
         // that, and O is left alone.
-        const bool move = top > ref + kRise || (ref == -INFINITY && top != -INFINITY);
+        const bool move = (top - ref) * c_row > kRise || (ref == -INFINITY && top != -INFINITY);
         if (__any_sync(0xffffffffu, move || grown != 1.0f)) {
-          float f = !move ? 1.0f : ref == -INFINITY ? 0.0f : exp2_fast(ref - top);
+          float f = !move ? 1.0f : worth(ref, top, c_row);
           if (move) ref = top, sum *= f;
           f *= grown;
           __syncwarp();
@@ -836,7 +866,9 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
         }
         // (the unit's exponent, less the room, goes into the powers of two)
         const int shift = KV == SJD_BF16 ? 0 : static_cast<int>(__float_as_uint(unit) >> 23) - 127 - kRoom;
-        const float base = (ref == -INFINITY ? 0.0f : ref) + static_cast<float>(shift);
+        float base = ref == -INFINITY ? 0.0f : ref * c_row;
+        if (__any_sync(0xffffffffu, fabsf(base) > kFar)) less_reference<kTile>(s_at, ref, base);
+        base += static_cast<float>(shift);
         Pair total[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
         tmem_load32(s_at, s[0]);
 #pragma unroll
@@ -872,21 +904,22 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     const bool take[2] = {NM == 1 || slot == 0, NM == 1 ? tiles > 1 : slot == 1};
     if constexpr (NM == 1) {
       named_barrier(2 + slot, 128);  // (the factors are done with)
-      m->row[slot][0][row] = ref;
+      m->row[slot][0][row] = ref * row_unit;
       m->row[slot][1][row] = sum;
       if (KV != SJD_BF16 && row == 0) m->most[slot][0] = __float_as_uint(unit);
       named_barrier(1, 256);
       const float r1 = tiles > 1 ? m->row[1][0][row] : -INFINITY, r0s = m->row[0][0][row];
       const float s1 = tiles > 1 ? m->row[1][1][row] : 0.0f, s0 = m->row[0][1][row];
       ref = fmaxf(r0s, r1);
-      f[0] = r0s == -INFINITY ? 0.0f : exp2_fast(r0s - ref);
-      f[1] = r1 == -INFINITY ? 0.0f : exp2_fast(r1 - ref);
+      f[0] = worth(r0s, ref, c);
+      f[1] = worth(r1, ref, c);
       sum = s0 * f[0] + s1 * f[1];
       if (KV != SJD_BF16) {
         f[0] *= __uint_as_float(m->most[0][0]) * (1.0f / (1 << kRoom));
         if (tiles > 1) f[1] *= __uint_as_float(m->most[1][0]) * (1.0f / (1 << kRoom));
       }
     } else if (KV != SJD_BF16) {
+      ref *= row_unit;
       f[0] = f[1] = unit * (1.0f / (1 << kRoom));
     }
     const bool wholly = w.k0 == 0 && w.k1 == it.tiles;
@@ -940,7 +973,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
       }
       if (valid && (NM == 2 || slot == 0)) {
         if (wholly) {
-          if (p.lse) p.lse[head] = sum > 0.0f || sum != sum ? (ref + log2f(sum)) * 0.69314718055994531f : -INFINITY;
+          if (p.lse) p.lse[head] = log_of_sum(p, ref, sum);
         } else {
           part_rows[part * (kTile * NM) + (NM == 2 ? slot * kTile : 0) + row] = make_float2(ref, sum);
         }
@@ -988,7 +1021,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
   const uint32_t lanes = static_cast<uint32_t>(at & ~31) << 16;
   const uint32_t s_at = tmem + lanes + slot * kTile, o_at = tmem + lanes + kOColumn + slot * DP;
   const int G = p.c.group;
-  const float c = fmaxf(fabsf(p.scale) * 1.4426950408889634f, kLeast);
+  const float c = power_factor(p);
   auto copy_barrier = [&]() {  // the copy's warps
     if constexpr (kWarps == 1) __syncwarp();
     else named_barrier(4 + slot * SP + copy, 32 * kWarps);
@@ -1007,7 +1040,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
     const int limit = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_CAUSAL ? it.start + t + 1 : it.keys;
     const int whole = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_GIVEN ? it.start : limit;
     const int common = common_keys<1>(p, it);
-    float ref = -INFINITY, sum = 0.0f, c_row = c, unit = 0.0f;
+    float ref = -INFINITY, sum = 0.0f, c_row = c, row_unit = 1.0f, unit = 0.0f;
     // the factors of key `at` of a tile, as in softmax_rows
     float next_k = 0.0f, next_v = 0.0f;
     int page = kNoPage;
@@ -1049,7 +1082,10 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
         const bool mixed = !__all_sync(0xffffffffu, key0 + kKeys <= whole) || bad;
         float top = -INFINITY, grown = 1.0f;
         if (KV != SJD_BF16) {
-          if (u == 0) c_row = fmaxf(c * __uint_as_float(static_cast<uint32_t>(127 + m->exponents[w.piece & 1][at]) << 23), 1e-37f);
+          if (u == 0) {
+            row_unit = __uint_as_float(static_cast<uint32_t>(127 + m->exponents[w.piece & 1][at]) << 23);
+            c_row = fmaxf(c * row_unit, 1e-37f);
+          }
           const uint32_t* words = m->most[slot] + copy * kChunks;
           const uint32_t most = SP == 4 ? words[0] : max(words[0], words[1]);
           const float now = __uint_as_float(max(27u << 23, min(247u << 23, (most + 0x7fffffu) & 0x7f800000u)));
@@ -1083,10 +1119,9 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
           top = largest_of(s, top);
         }
         if (kChunks > 1) tmem_wait_store();
-        top *= c_row;
-        const bool move = top > ref + kRise || (ref == -INFINITY && top != -INFINITY);
+        const bool move = (top - ref) * c_row > kRise || (ref == -INFINITY && top != -INFINITY);
         if (__any_sync(0xffffffffu, move || grown != 1.0f)) {
-          float f = !move ? 1.0f : ref == -INFINITY ? 0.0f : exp2_fast(ref - top);
+          float f = !move ? 1.0f : worth(ref, top, c_row);
           if (move) ref = top, sum *= f;
           f *= grown;
           __syncwarp();
@@ -1103,7 +1138,18 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
           }
         }
         const int shift = KV == SJD_BF16 ? 0 : static_cast<int>(__float_as_uint(unit) >> 23) - 127 - kRoom;
-        const float base = (ref == -INFINITY ? 0.0f : ref) + static_cast<float>(shift);
+        float base = ref == -INFINITY ? 0.0f : ref * c_row;
+        if (__any_sync(0xffffffffu, fabsf(base) > kFar)) {
+          if constexpr (kChunks == 1) {
+            const float from = ref == -INFINITY ? 0.0f : ref;
+            base = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) - from);
+          } else {
+            less_reference<kKeys>(s_at + copy * kKeys, ref, base);
+          }
+        }
+        base += static_cast<float>(shift);
         Pair total[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
         uint32_t out[kChunks][16];
 #pragma unroll
@@ -1138,13 +1184,14 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
     tc_fence_after();
     const int tiles = w.k1 - w.k0;
     copy_barrier();  // (the factors are done with)
+    ref *= row_unit;
     m->row[slot][0][at] = units > 0 && active ? ref : -INFINITY;
     m->row[slot][1][at] = units > 0 && active ? sum : 0.0f;
     named_barrier(1, 256);
     float most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 2 * SP; ++i) most = fmaxf(most, m->row[i & 1][0][i / 2 * kRows + row]);
-    const float own = units > 0 && active && ref != -INFINITY ? exp2_fast(ref - most) * (KV == SJD_BF16 ? 1.0f : unit * (1.0f / (1 << kRoom))) : 0.0f;
+    const float own = units > 0 && active ? worth(ref, most, c) * (KV == SJD_BF16 ? 1.0f : unit * (1.0f / (1 << kRoom))) : 0.0f;
     const bool wholly = w.k0 == 0 && w.k1 == it.tiles;
     const bool bad = *const_cast<volatile int*>(&m->bad_values[w.piece & 3]) == w.piece + 1;
     const long long part = 2ll * blockIdx.x + (w.k0 == 0 ? 1 : 0);
@@ -1184,7 +1231,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
         for (int k = 0; k < 2 * SP; ++k) {
           const int from = k / 2 * kRows + r;
           const float its = m->row[k & 1][0][from];
-          all += its == -INFINITY ? 0.0f : m->row[k & 1][1][from] * exp2_fast(its - top);
+          all += m->row[k & 1][1][from] * worth(its, top, c);
           const float4 v = sums[((k & 1) * kTile + from) * kFours + (four ^ (from & (kFours - 1)))];
           o[0] += v.x, o[1] += v.y, o[2] += v.z, o[3] += v.w;
         }
@@ -1197,7 +1244,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
           if (col < p.c.D)
             *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.o) + head * p.c.D + col) =
                 make_uint2(pack_bf16(o[0] * inverse, o[1] * inverse), pack_bf16(o[2] * inverse, o[3] * inverse));
-          if (p.lse && col == 0) p.lse[head] = some ? (top + log2f(all)) * 0.69314718055994531f : -INFINITY;
+          if (p.lse && col == 0) p.lse[head] = log_of_sum(p, top, all);
         } else {
           *reinterpret_cast<float4*>(parts + (part * kTile + r) * DP + col) = make_float4(o[0], o[1], o[2], o[3]);
           if (col == 0) part_rows[part * kTile + r] = make_float2(top, all);
@@ -1230,7 +1277,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
             const float2 rs = lane < count ? __ldcg(&part_rows[part_at(lane, r)]) : make_float2(-INFINITY, 0.0f);
             float top = rs.x;
             for (int k = 16; k > 0; k /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-            const float f = rs.x == -INFINITY ? 0.0f : exp2_fast(rs.x - top);
+            const float f = worth(rs.x, top, c);
             float all = rs.y * f;
             for (int k = 16; k > 0; k /= 2) all += __shfl_xor_sync(0xffffffffu, all, k);
             const bool some = all > 0.0f || all != all;
@@ -1238,7 +1285,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
             if (p.lse && lane == 0) {
               const int its_t = by_group(p.c, r);
               const long long head = (static_cast<long long>(it.b) * p.c.n + its_t) * p.c.Hq + static_cast<long long>(it.kvh) * G + r - its_t * G;
-              p.lse[head] = some ? (top + log2f(all)) * 0.69314718055994531f : -INFINITY;
+              p.lse[head] = log_of_sum(p, top, all);
             }
           }
           named_barrier(1, 256);
@@ -1277,7 +1324,6 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
   Misc<NM>* m = reinterpret_cast<Misc<NM>*>(raw + P::kAtMisc);
   const uint32_t smem = smem_addr(raw);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0);  // (the same for all lanes, to the compiler too)
-  let_next_start();
   if (warp == kMmaWarp) tmem_alloc(smem_addr(&m->tmem), kTmemColumns);
   if (threadIdx.x == 256) {
     for (int i = 0; i < 5; ++i) {
@@ -1295,6 +1341,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
     fence_barrier_init();
   }
   wait_for_previous();
+  let_next_start();
   if (warp == 0) locate<NM>(p, &m->start);
   if (threadIdx.x == 256) shared[blockIdx.x].parts = 0;
   tc_fence_before();
@@ -1330,8 +1377,9 @@ template <int DP>
 __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const AttendParams p, const float* parts, const float2* part_rows,
                                                                const Shared* shared, int rows_per_item) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, G = p.c.group;
-  let_next_start();
   wait_for_previous();
+  let_next_start();
+  const float c = power_factor(p);
   const Shared s = shared[blockIdx.x];
   const int row0 = blockIdx.y * kJoinWarps + warp, step = gridDim.y * kJoinWarps;
   if (s.parts > 1) {
@@ -1347,7 +1395,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const AttendParam
 #pragma unroll 4
       for (int i = 0; i < s.parts; ++i) {
         const float2 rs = part_rows[part_at(i)];
-        const float f = rs.x == -INFINITY ? 0.0f : exp2_fast(rs.x - top);
+        const float f = worth(rs.x, top, c);
         sum += rs.y * f;
         const float* x = parts + part_at(i) * DP + lane * (DP / 32);
         if constexpr (DP == 128) {
@@ -1366,7 +1414,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const AttendParam
 #pragma unroll
         for (int j = 0; j < DP / 32; j += 2) *reinterpret_cast<uint32_t*>(to + j) = pack_bf16(o[j] * inverse, o[j + 1] * inverse);
       }
-      if (p.lse && lane == 0) p.lse[head] = sum > 0.0f || sum != sum ? (top + log2f(sum)) * 0.69314718055994531f : -INFINITY;
+      if (p.lse && lane == 0) p.lse[head] = log_of_sum(p, top, sum);
     }
   }
   clear_rows(p, row0, step, lane);

@@ -57,8 +57,8 @@ __device__ __forceinline__ void angles(const Rope& r, const Tokens& at, float2* 
 template <typename T>
 __global__ void __launch_bounds__(kBlock) rotate_kernel(const RotateParams p, const Share share) {
   __shared__ float2 cs[kTokens * kMaxRotateDim / 2];
-  let_next_start();
   wait_for_previous();
+  let_next_start();
   const Tokens at = tokens_of_block(share, p.B);
   const bool wx = wide4(p.x, sizeof(T)), wy = wide4(p.y, sizeof(T));
   const int items = at.count * p.H * share.chunks;
@@ -118,8 +118,8 @@ __global__ void __launch_bounds__(kBlock) write_kernel(const WriteParams p, cons
   __shared__ uint32_t slots[kTokens];   // the tokens' places for head 0
   __shared__ int there[kTokens];        // whether the token is in its sequence's span
   const Cache& c = p.c;
-  let_next_start();
   wait_for_previous();
+  let_next_start();
   const Tokens at = tokens_of_block(share, c.B);
   const int L = share.lanes, lane = threadIdx.x & (L - 1), groups = kBlock / L;
   const bool turned = p.rope.turns != nullptr;
@@ -244,8 +244,8 @@ template <typename T, int KV>
 __global__ void __launch_bounds__(kBlock) read_kernel(const ReadParams p, const Share share) {
   __shared__ uint32_t slots[kTokens];
   const Cache& c = p.c;
-  let_next_start();
   wait_for_previous();
+  let_next_start();
   const Tokens at = tokens_of_block(share, c.B);
   if (threadIdx.x < at.count) {
     const int of_call = at.first + threadIdx.x, b = over(of_call, share.by_n), t = of_call - b * c.n;

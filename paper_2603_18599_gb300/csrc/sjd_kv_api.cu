@@ -25,7 +25,7 @@ bool valid(const sjd_kv_config* c) {
   return c && c->batch >= 1 && c->kv_heads >= 1 && c->heads >= c->kv_heads && c->heads % c->kv_heads == 0 &&
          c->heads / c->kv_heads <= 128 && c->head_dim >= 8 && c->head_dim <= kMaxDim && c->head_dim % 8 == 0 &&
          c->page_size >= 1 && c->n_pages >= 1 && c->max_pages >= 1 && c->max_new >= 1 &&
-         static_cast<long long>(c->max_pages) * c->page_size <= 0x7fffffffLL &&
+         static_cast<long long>(c->max_pages) * c->page_size <= (1LL << 30) && c->kv_heads <= 65536 &&
          // (vectors are counted in 32 bits)
          static_cast<double>(c->n_pages) * c->kv_heads * c->page_size < 4294967295.0 &&
          static_cast<long long>(c->batch) * c->max_new <= 0x7fffffffLL / 256 &&
@@ -99,7 +99,7 @@ int sjd_rope_turns(const double* freq, int32_t n, uint64_t* turns) {
 int sjd_rotate(const sjd_rope* rope, const sjd_view* x, const sjd_view* y, const int32_t* positions, int32_t batch, int32_t n,
                int32_t heads, int32_t dim, int32_t dtype, int32_t inverse, void* stream) {
   if (!rope || !x || !y || !x->data_dev || !y->data_dev || !positions) return SJD_ERR_ARG;
-  if (batch < 1 || n < 1 || heads < 1 || static_cast<long long>(batch) * n > 0x7fffffffLL) return SJD_ERR_ARG;
+  if (batch < 1 || n < 1 || heads < 1 || heads > (1 << 20) || static_cast<long long>(batch) * n > 0x7fffffffLL) return SJD_ERR_ARG;
   if (dim < 8 || dim > kMaxRotateDim || dim % 8 || (dtype != SJD_F32 && dtype != SJD_BF16)) return SJD_ERR_ARG;
   if ((inverse != 0 && inverse != 1) || bad_rope(rope, dim)) return SJD_ERR_ARG;
   if (!aligned(x->data_dev, size_of(dtype)) || !aligned(y->data_dev, size_of(dtype))) return SJD_ERR_ARG;

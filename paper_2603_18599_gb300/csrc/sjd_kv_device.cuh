@@ -12,7 +12,9 @@
 namespace sjd_kv_ops {
 
 // The kernels are launched while the one before them on the stream drains:
-// this waits until it is done. Nothing is read or written before.
+// this waits until it is done. Nothing is read or written before, and the next
+// kernel is let in only then, so that what is done before a call on the stream
+// is done when anything after the call starts.
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

@@ -260,9 +260,9 @@ class KV:
         axes] the keys are turned first, and q [B, n, heads, D], if given, is
         turned into the result."""
         c = self.cfg
+        if k.dim() != 4 or k.dtype not in _DTYPES:
+            raise ValueError("k must be a [B, n, kv_heads, D] bf16 or f32 tensor")
         B, n, dt = c.batch, k.shape[1], k.dtype
-        if dt not in _DTYPES:
-            raise ValueError("k must be bf16 or f32")
         shape = (B, n, c.kv_heads, c.head_dim)
         kw, vw = _view_of(k, "k", shape, dt, self.device), _view_of(v, "v", shape, dt, self.device)
         at, span = self._layer_of(layer), self._span(table, start, count, n)
@@ -302,6 +302,8 @@ class KV:
         token sees of the chunk. Returns o [B, n, heads, D], or (o, lse
         [B, n, heads] f32)."""
         c = self.cfg
+        if q.dim() != 4:
+            raise ValueError("q must be a [B, n, heads, D] bf16 tensor")
         B, n = c.batch, q.shape[1]
         qw = _view_of(q, "q", (B, n, c.heads, c.head_dim), torch.bfloat16, self.device)
         at, span = self._layer_of(layer), self._span(table, start, count, n)

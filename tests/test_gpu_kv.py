@@ -417,6 +417,28 @@ def test_attend_scores_of_any_size():
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads,n", [(2, 3), (2, 40), (8, 30), (4, 200)])
+@pytest.mark.parametrize("size", [1e2, 1e6, 1e12])
+def test_attend_scores_beyond_every_exponent(dtype, heads, n, size):
+    """Queries that are one key each, many times over: the row's weight is on
+    that key alone, by a margin of hundreds to 10^13 powers of e, and its
+    result the key's value."""
+    D, context = 128, 400
+    h, layer, table, start, g = make(1, heads, 2, D, dtype, 16, [context], n)
+    filled(h, layer, table, [context], n, g)
+    zero = torch.zeros_like(start)
+    whole = kv.KV(1, heads, 2, D, h.cfg.n_pages, 16, h.cfg.max_pages, context + n, dtype)
+    k, v = whole.read(kv.Layer(layer.k, layer.v, layer.k_scale, layer.v_scale), table, zero, context + n, dtype=torch.float32)
+    at = torch.randint(0, context, (n, heads), device=DEV, generator=g)
+    head = torch.arange(heads, device=DEV) * 2 // heads
+    q = (k[0, at, head] * size).bfloat16()[None].contiguous()
+    o, lse = h.attend(layer, q, table, start, lse=True)
+    assert ((o[0].float() - v[0, at, head]).abs() <= 2.0 ** -7 * v[0, at, head].abs() + 1e-6).all()
+    want = (q[0].double() * k[0, at, head].double()).sum(-1) * D ** -0.5
+    assert ((lse[0].double() - want).abs() <= 1e-5 * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("kind", ["causal", "given"])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 def test_unseen_keys_have_no_effect_whatever_they_hold(dtype, kind, bad):
@@ -530,6 +552,37 @@ def test_calls_on_another_stream_are_ordered():
             got = h.attend(layer, mine, table, start)
             assert torch.equal(got, want)
     torch.cuda.synchronize()
+
+
+def test_calls_back_to_back_wait_for_each_other():
+    """Kernels that start while the one before drains: a chain of calls, each
+    on the last one's result, against the same chain with waits between."""
+    starts, n, D = [300, 40], 8, 64
+    h, layer, table, start, g = make(2, 8, 2, D, torch.int8, 16, starts, n)
+    filled(h, layer, table, starts, n, g)
+    rope = kv.Rope.sections((16, 16))
+    positions = torch.randint(0, 500, (2, n, 2), device=DEV, generator=g).int()
+    x0 = normal(g, 2, n, 8, D).bfloat16()
+
+    def chain(wait):
+        x = x0.clone()
+        for _ in range(60):
+            q = rope.rotate(x, positions)
+            wait()
+            turned = h.write(layer, x[:, :, :2], x[:, :, 2:4], table, start, rope=rope, positions=positions, q=q)
+            wait()
+            k, v = h.read(layer, table, start, n)
+            wait()
+            o = h.attend(layer, turned, table, start)
+            wait()
+            x = rope.rotate(o, positions, inverse=True)
+            wait()
+            x = torch.cat([k, v, x[:, :, 4:]], 2) * 1.5    # a kernel of another library between
+        return x
+
+    want = chain(torch.cuda.synchronize)
+    for _ in range(3):
+        assert torch.equal(chain(lambda: None), want)
 
 
 def test_captured_calls_follow_the_device_positions():

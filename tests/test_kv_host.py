@@ -38,7 +38,8 @@ def test_workspace_size_validates_configs(lib):
     assert size(None) == 0
     for over in (dict(batch=0), dict(heads=0), dict(kv_heads=0), dict(kv_heads=5), dict(heads=8 * 129), dict(head_dim=0),
                  dict(head_dim=129), dict(head_dim=136), dict(page_size=0), dict(n_pages=0), dict(max_pages=0), dict(max_new=0),
-                 dict(kv_dtype=0), dict(kv_dtype=4), dict(page_size=1 << 20, max_pages=1 << 12), dict(batch=1 << 20, max_new=1 << 12)):
+                 dict(kv_dtype=0), dict(kv_dtype=4), dict(page_size=1 << 20, max_pages=(1 << 10) + 1), dict(batch=1 << 20, max_new=1 << 12),
+                 dict(n_pages=1 << 20, page_size=512), dict(kv_heads=65537, heads=65537)):
         assert size(ctypes.byref(config(**over))) == 0, over
 
 
