@@ -30,6 +30,17 @@
 // each copy takes the softmax over its own half or quarter of a tile's keys,
 // with a maximum and a sum of its own and weights of 0 for the other keys, and
 // the copies' accumulators are joined at the end like the slots'.
+//
+// What bounds it (one GB300): over a 16-bit cache few rows are bound by HBM (16
+// tokens of 64 heads over up to 32768 tokens, 8 key heads: 249 us, 98 % of the
+// copy rate); the same over e4m3 by what the loaders do for a tile (199 us, 63 %;
+// 197 without products and exponentials). A prompt of 4000 behind 4100 takes 376 us,
+// 1060 TFLOP/s or 55 % of a dense product's rate: a slot's softmax (1811
+// cycles of two slots' 128 x 128 scores), its products (1024 a slot) and the
+// hand-overs between them follow one another, and tensor memory has room for two
+// slots. 32 windows of 64 over 8100 in e4m3 take 342 us (31 %): the keys'
+// and values' factors make that softmax 2799 cycles. One token over 300: 13 to 15
+// us a call, which is the host's part.
 
 #include <cfloat>
 
@@ -47,8 +58,8 @@ constexpr int kMmaWarp = 19;            // (on another scheduler than the first 
 constexpr uint32_t kTmemColumns = 512;  // S of the two slots (P over them), then O of the two
 constexpr uint32_t kOColumn = 2 * kTile;
 constexpr long long kWaitClocks = 4000000000ll;  // about two seconds
-constexpr float kLeast = 1e-30f;
-constexpr int kRoom = 6;
+constexpr float kLeast = 1e-30f;        // least factor of the scores
+constexpr int kRoom = 6;                // weights of an 8-bit cache are times 2^6: at most 2^(8 + 6 + 1), in fp16
 constexpr float kFar = 0x1p20f;         // from here on a score's product with c is rounded too coarsely (2^-4)
 constexpr float kRise = 8.0f;           // a row's reference maximum moves when it is behind by more than 2^8
 
@@ -56,6 +67,13 @@ __host__ __device__ constexpr uint32_t tile_bytes(int dp) { return static_cast<u
 
 // Shared memory: queries, rings of key and value tiles (1024-byte aligned),
 // for an 8-bit cache rings of the codes as they come, then the small things.
+//
+// Key and value tiles, and codes under way, as fit 227 KB. At a head of 128 and
+// 8 bits deeper rings of codes beat more tiles with few rows (16 tokens over 32768:
+// 185 us with one tile of each and four of codes, 205 with two tiles and two);
+// with 256 rows two key tiles let the next scores start (32 windows
+// of 64 over 8100: 343 us; 356 with two value tiles instead, 346 to 349 with one of
+// each and three of codes).
 template <int KV, int DP, int NM>
 struct Plan {
   static constexpr bool kCodes = KV != SJD_BF16;
@@ -166,7 +184,8 @@ struct Walk {
 template <int NM>
 struct Misc {
   unsigned long long k_full[5], k_empty[5], v_full[5], v_empty[5], q_full, q_empty, o_full,
-      s_full[2], p_full[2][2];  // by slot (and half)
+      s_full[2], p_full[2][2],  // by slot (and half)
+      drained;                  // after a wait that ran out: no product is in flight
   uint32_t tmem;
   int abort;
   int last;                // whether the block joins the item's parts
@@ -612,6 +631,12 @@ __device__ __forceinline__ void issue_products(const AttendParams& p, Misc<NM>* 
   }
   // (nothing is in flight when the block ends)
   wait_together(m, &m->o_full, (piece - 1) & 1);
+  if (*const_cast<volatile int*>(&m->abort)) {
+    if (lead) mma_commit(smem_addr(&m->drained));
+    __syncwarp();
+    const long long begun = clock64();
+    while (!mbar_try(smem_addr(&m->drained), 0) && clock64() - begun <= kWaitClocks) {}
+  }
 }
 
 // --- softmax --------------------------------------------------------------------
@@ -1333,6 +1358,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
       mbar_init(smem_addr(&m->v_full[i]), loaders), mbar_init(smem_addr(&m->v_empty[i]), 1);
     }
     mbar_init(smem_addr(&m->q_full), 4), mbar_init(smem_addr(&m->q_empty), SP > 1 ? 2 : 1), mbar_init(smem_addr(&m->o_full), 1);
+    mbar_init(smem_addr(&m->drained), 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_addr(&m->s_full[i]), 1), mbar_init(smem_addr(&m->p_full[i][0]), 4), mbar_init(smem_addr(&m->p_full[i][1]), 4);
     }
@@ -1360,6 +1386,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1) attend_kernel(const AttendP
   } else if (SP > 1 && join_here) {
     clear_rows(p, warp - 16, kMmaWarp - 16, threadIdx.x & 31);
   }
+  copy_wait_all();  // (also where a wait ran out)
   tc_fence_before();
   __syncthreads();
   if (warp == kMmaWarp) {
@@ -1440,6 +1467,10 @@ cudaError_t launch(const AttendParams& p, int sms, unsigned char* scratch, cudaS
   return launch_early(join_kernel<DP>, dim3(blocks, 8), 32 * kJoinWarps, 0, s, p, parts, part_rows, shared, kTile * NM);
 }
 
+// 256 rows to an item share each tile that is loaded between two products;
+// fewer leave the tile's other rows idle, or to copies. 32 sequences over 8100, 8 key heads
+// of 128, by the rows of an item (bf16 / e4m3): 32 137 / 118 us, 64
+// 142 / 172, 128 149 / 202, 256 213 / 346; 132 rows, in an item of 256, 183 / 292.
 template <int KV, int DP>
 cudaError_t launch_of(const AttendParams& p, int sms, unsigned char* scratch, cudaStream_t s) {
   const long long rows = static_cast<long long>(p.c.n) * p.c.group;
