@@ -54,6 +54,9 @@ __device__ __forceinline__ void angles(const Rope& r, const Tokens& at, float2* 
     cs[i] = turn_of(r, r.positions + static_cast<long long>(at.first + i / r.pairs) * r.axes, i % r.pairs);
 }
 
+// Three sequences of 4097 tokens, 20 heads of 80, f32: 28 us, 5.6 TB/s
+// (83 % of the copy rate; half of the issue slots), 47 us with one token to a
+// block. 32 tokens: 11 us a call, the host's.
 template <typename T>
 __global__ void __launch_bounds__(kBlock) rotate_kernel(const RotateParams p, const Share share) {
   __shared__ float2 cs[kTokens * kMaxRotateDim / 2];
@@ -111,8 +114,15 @@ __device__ __forceinline__ void quotients(float (&x)[4], float scale, float inve
   }
 }
 
-// CP chunks of a vector to a thread: chunk i * L + lane.
-template <typename T, int KV, int CP>
+// CP chunks of a vector to a thread: chunk i * L + lane. Four sequences of
+// 8100 tokens, 16 heads of 96, f32 to s8, not rotated: 86 us, 5.8 TB/s (86 %
+// of the copy rate); 410 with one token to a block, one chunk to a thread and
+// plain divisions. 32 windows of 64, keys and queries rotated, bf16 to e4m3: 18 us.
+//
+// With queries (Q) a warp whose vectors are all queries leaves out the codes: 18
+// us instead of 20.5 in the windows above. The vote for it costs the images 11 us
+// (86 against 97), so that calls without queries have a kernel without it.
+template <typename T, int KV, int CP, bool Q>
 __global__ void __launch_bounds__(kBlock) write_kernel(const WriteParams p, const Share share) {
   __shared__ float2 cs[kTokens * kMaxDim / 2];
   __shared__ uint32_t slots[kTokens];   // the tokens' places for head 0
@@ -123,7 +133,7 @@ __global__ void __launch_bounds__(kBlock) write_kernel(const WriteParams p, cons
   const Tokens at = tokens_of_block(share, c.B);
   const int L = share.lanes, lane = threadIdx.x & (L - 1), groups = kBlock / L;
   const bool turned = p.rope.turns != nullptr;
-  const int n_q = p.q.p ? c.Hq : 0, n_vec = n_q + 2 * c.Hkv, items = at.count * n_vec;
+  const int n_q = Q ? c.Hq : 0, n_vec = n_q + 2 * c.Hkv, items = at.count * n_vec;
   const bool wq = wide4(p.q, sizeof(T)), wk = wide4(p.k, sizeof(T)), wv = wide4(p.v, sizeof(T)), wo = wide4(p.q_out, sizeof(T));
   struct Place {
     int token, vec, b, t;
@@ -187,7 +197,7 @@ __global__ void __launch_bounds__(kBlock) write_kernel(const WriteParams p, cons
         }
       }
     }
-    if (n_q > 0 && __all_sync(0xffffffffu, is_q || item >= items)) continue;
+    if (Q && __all_sync(0xffffffffu, is_q || item >= items)) continue;
     using Code = typename Codes<KV>::type;
     const uint32_t slot = slots[q.token];
     const bool store = item < items && !is_q && slot != kNoVector;
@@ -240,6 +250,9 @@ __global__ void __launch_bounds__(kBlock) write_kernel(const WriteParams p, cons
   }
 }
 
+// Up to 8100 tokens of 16 sequences, 8 heads of 128, e4m3 to bf16: 120 us,
+// 5.2 TB/s (77 % of the copy rate, three quarters of the issue slots: conversion);
+// 4 x 8100 tokens of 16 heads of 96, s8 to bf16: 53 us, 5.7 TB/s.
 template <typename T, int KV>
 __global__ void __launch_bounds__(kBlock) read_kernel(const ReadParams p, const Share share) {
   __shared__ uint32_t slots[kTokens];
@@ -306,34 +319,36 @@ __global__ void __launch_bounds__(kBlock) read_kernel(const ReadParams p, const 
   }
 }
 
-// Tokens of a block: as many as leave every SM a few blocks.
+// Tokens of a block: as many as leave every SM four blocks, at most kTokens (32 windows of
+// 64 rotated and written: 18.1 us; 19.6 where eight or sixteen are left).
 Share share_of(int B, int n, int dim, int vectors) {
-  const long long tokens = static_cast<long long>(B) * n, fair = tokens / (152 * 8);
+  const long long tokens = static_cast<long long>(B) * n, fair = tokens / (152 * 4);
   const int per = static_cast<int>(fair < 1 ? 1 : fair < kTokens ? fair : kTokens);
   return {per, n, dim / 8, 0, divisor(n), divisor(dim / 8), divisor(vectors)};
 }
 unsigned blocks_of(const Share& s, int B) { return static_cast<unsigned>((static_cast<long long>(B) * s.n + s.per - 1) / s.per); }
 
-template <typename T, int CP>
-cudaError_t write_by(const WriteParams& p, Share share, int kv_dtype, cudaStream_t s) {
+template <typename T, int CP, bool Q>
+cudaError_t write_by(const WriteParams& p, const Share& share, int kv_dtype, cudaStream_t s) {
   const unsigned blocks = blocks_of(share, p.c.B);
-  if (kv_dtype == SJD_BF16) return launch_early(write_kernel<T, SJD_BF16, CP>, blocks, kBlock, 0, s, p, share);
-  if (kv_dtype == SJD_E4M3) return launch_early(write_kernel<T, SJD_E4M3, CP>, blocks, kBlock, 0, s, p, share);
-  return launch_early(write_kernel<T, SJD_S8, CP>, blocks, kBlock, 0, s, p, share);
+  if (kv_dtype == SJD_BF16) return launch_early(write_kernel<T, SJD_BF16, CP, Q>, blocks, kBlock, 0, s, p, share);
+  if (kv_dtype == SJD_E4M3) return launch_early(write_kernel<T, SJD_E4M3, CP, Q>, blocks, kBlock, 0, s, p, share);
+  return launch_early(write_kernel<T, SJD_S8, CP, Q>, blocks, kBlock, 0, s, p, share);
 }
 
 // Two chunks to a thread, or three where that leaves fewer threads of the
-// group without one (9 to 12 chunks: heads of 72 to 96).
+// group without one (9 to 12 chunks: heads of 72 to 96. The images above: 86
+// us with three, 118 with two).
 template <typename T>
 cudaError_t write_of(const WriteParams& p, int kv_dtype, cudaStream_t s) {
   Share share = share_of(p.c.B, p.c.n, p.c.D, (p.q.p ? p.c.Hq : 0) + 2 * p.c.Hkv);
   const int two = lanes_of((share.chunks + 1) / 2), three = lanes_of((share.chunks + 2) / 3);
   if (3 * three < 2 * two) {
     share.lanes = three;
-    return write_by<T, 3>(p, share, kv_dtype, s);
+    return p.q.p ? write_by<T, 3, true>(p, share, kv_dtype, s) : write_by<T, 3, false>(p, share, kv_dtype, s);
   }
   share.lanes = two;
-  return write_by<T, 2>(p, share, kv_dtype, s);
+  return p.q.p ? write_by<T, 2, true>(p, share, kv_dtype, s) : write_by<T, 2, false>(p, share, kv_dtype, s);
 }
 
 template <typename T>
