@@ -533,8 +533,9 @@ int sjd_kv_read(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span, 
  * [batch][n][heads][head_dim] in bf16, contiguous; lse_dev fp32 [batch][n]
  * [heads], or NULL. Scores and sums are fp32. The weights are rounded to 16
  * bits before their product with the values: with a 16-bit cache to bf16, with
- * an 8-bit one, after a factor of the values' scale over the largest scale so
- * far, to fp16 (a weight below 2^-30 of the row's largest is then lost). The
+ * an 8-bit one times their values' scales to fp16, in units of a power of two
+ * near the largest such product p_j s_j of the keys that the row sees. A
+ * product below 2^-25 of that is lost, whatever the scales of other keys. The
  * queries are exact, but for an 8-bit cache those elements below 2^-15 of
  * their row's largest, which keep an error of 2^-25 of that. A row that sees no
  * key, and rows from count[b] on, give o = 0 and lse = -inf; a key that a row

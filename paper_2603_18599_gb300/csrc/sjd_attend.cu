@@ -39,7 +39,8 @@
 // cycles of two slots' 128 x 128 scores), its products (1024 a slot) and the
 // hand-overs between them follow one another, and tensor memory has room for two
 // slots. 32 windows of 64 over 8100 in e4m3 take 342 us (31 %): the keys'
-// and values' factors make that softmax 2799 cycles. One token over 300: 13 to 15
+// and values' factors make that softmax 2799 cycles (more where the values'
+// factors lie far apart: Unit). One token over 300: 13 to 15
 // us a call, which is the host's part.
 
 #include <cfloat>
@@ -59,7 +60,9 @@ constexpr uint32_t kTmemColumns = 512;  // S of the two slots (P over them), the
 constexpr uint32_t kOColumn = 2 * kTile;
 constexpr long long kWaitClocks = 4000000000ll;  // about two seconds
 constexpr float kLeast = 1e-30f;        // least factor of the scores
-constexpr int kRoom = 6;                // weights of an 8-bit cache are times 2^6: at most 2^(8 + 6 + 1), in fp16
+constexpr int kRoom = 6;                // weights of an 8-bit cache are times 2^6: at most 2^(8 + 6), in fp16
+constexpr float kNear = 64.0f;          // values' factors that share a unit lie within 2^6 of each other, and of 1
+constexpr float kUnits = 0x1p40f;       // within 2^40: see Unit
 constexpr float kFar = 0x1p20f;         // from here on a score's product with c is rounded too coarsely (2^-4)
 constexpr float kRise = 8.0f;           // a row's reference maximum moves when it is behind by more than 2^8
 
@@ -194,7 +197,7 @@ struct Misc {
   Walk<NM> walk[2];        // the softmax groups' ways
   uint32_t poison[2][4];   // per slot: keys of the tile whose factor is no number
   signed char exponents[2][NM * kTile];  // of the queries' rows (8-bit cache), by the piece's number modulo 2
-  uint32_t most[2][4];     // per slot and warp: the largest of the tile's value factors
+  ushort2 range[2][4];     // per slot and warp: the smallest and the largest of the tile's value factors, the upper halves of their bits
   alignas(16) float row[2][2][kTile];  // per slot: factors of the tile's keys and values; at the end the rows' maxima and sums
 };
 
@@ -745,6 +748,139 @@ __device__ __forceinline__ void weights_of(const uint32_t (&s)[32], const float*
   }
 }
 
+// An 8-bit cache's weights go into the product in fp16, p v / unit 2^kRoom with
+// the values' factors v, and O is kept in units. As long as all keys of the tiles
+// so far, whether seen or not, have factors that lie near each other, they share a
+// unit, a power of two above them all: the key with a row's largest score has a
+// weight of 1 at least, and so the row's largest product is 1 / kNear of the unit
+// or more. Else (`wide`: a key's factor could be large, small or 0 where the
+// row's weight is not) each row has a unit of its own, near the largest product
+// p v among the keys that it sees. Either way the row's largest is 2^0 to 2^14
+// as fp16, and a product below 2^-25 of it is lost: less than the codes of the
+// largest resolve (2^-10 of its factor for e4m3, 2^-1 for s8; times codes of
+// up to 448 it is 2^-16).
+struct Unit {
+  bool wide = false;
+  float of = 0.0f;        // the unit; 0: no key yet. wide: its logarithm
+  float low = FLT_MAX;    // the smallest factor so far. wide: the logarithm of the row's largest p v so far, or less
+  __device__ __forceinline__ void widen(bool some) {  // some: the row has seen keys
+    low = some && of > 0.0f ? log2f(low) : -INFINITY;
+    of = some && of > 0.0f ? log2f(of) : 0.0f;
+    wide = true;
+  }
+  // What O is to be times. (Apart from what its reference is worth: the product of the two may underflow.)
+  __device__ __forceinline__ float back() const { return wide ? exp2_fast(of - kRoom) : of * (1.0f / (1 << kRoom)); }
+};
+
+// What is kept of a value's factor for the weights.
+__device__ __forceinline__ float value_factor(float v, bool wide) { return wide ? log2f(v) : v; }
+// The smallest and the largest of the factors of a warp's keys, where there is a key and
+// its factor a number: the upper halves of their bits, the largest's rounded up.
+__device__ __forceinline__ ushort2 range_of_factors(float v, bool there) {
+  const bool counts = there && v < INFINITY;
+  const uint32_t bits = v > 0.0f ? __float_as_uint(v) : 0u;
+  const uint32_t least = __reduce_min_sync(0xffffffffu, counts ? bits : 0x7f7fffffu), most = __reduce_max_sync(0xffffffffu, counts ? bits : 0u);
+  return make_ushort2(static_cast<unsigned short>(least >> 16), static_cast<unsigned short>((most + 0xffffu) >> 16));
+}
+__device__ __forceinline__ ushort2 joint(ushort2 a, ushort2 b) { return make_ushort2(min(a.x, b.x), max(a.y, b.y)); }
+// Another tile's factors: makes the unit wide, or returns the old unit over the
+// new one. some: the row has seen keys.
+__device__ __forceinline__ float take_factors(Unit& unit, ushort2 range, bool some) {
+  // (the power of two from the largest on)
+  const float now = fmaxf(unit.of, __uint_as_float(((static_cast<uint32_t>(range.y) << 16) + 0x7fffffu) & 0x7f800000u));
+  const float low = fminf(unit.low, __uint_as_float(static_cast<uint32_t>(range.x) << 16));
+  float grown = 1.0f;
+  if (now <= kUnits && now >= 1.0f / kUnits && low * kNear >= now) {
+    if (now != unit.of && unit.of > 0.0f) grown = unit.of / now;
+    unit.of = now, unit.low = low;
+  } else {
+    unit.widen(some);
+  }
+  return grown;
+}
+
+// The steps of a row with a unit of its own (of, most: Unit), whose factors come
+// as logarithms.
+// The reference moves to the tile's largest score, if that is far above it; returns by how much it was behind, as a power.
+__device__ __forceinline__ float wide_move(float top, float c, float& ref, float& sum, float& most) {
+  float behind = 0.0f;
+  if ((top - ref) * c > kRise || (ref == -INFINITY && top != -INFINITY)) {
+    if (ref != -INFINITY) behind = (ref - top) * c, sum *= exp2_fast(behind), most += behind;
+    ref = top;
+  }
+  return behind;
+}
+// 32 scores become powers of two; their largest product p v.
+__device__ __forceinline__ float wide_largest(uint32_t (&s)[32], const float* logs, float from, float c, float most) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    const float t = (__uint_as_float(s[j]) - from) * c, u = t + logs[j];
+    s[j] = __float_as_uint(t);
+    most = fmaxf(most, u < INFINITY ? u : most);   // (an infinite factor has no part in it)
+  }
+  return most;
+}
+__device__ __forceinline__ float wide_unit(float of, float most) {
+  const bool turn = most > of + 8.0f || (most < of - 4.0f && most != -INFINITY);
+  return turn ? fminf(133.0f, fmaxf(-120.0f, ceilf(most))) : of;
+}
+// The weights of 32 such powers, packed to 16 bits, and their sum.
+__device__ __forceinline__ float wide_weights_of(const uint32_t (&t)[32], const float* logs, float of, uint32_t (&out)[16]) {
+  const float up = kRoom - of;
+  float sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 32; j += 2) {
+    const float a = __uint_as_float(t[j]), b = __uint_as_float(t[j + 1]);
+    sum += exp2_fast(a) + exp2_fast(b);
+    const __half2 h = __floats2half2_rn(exp2_fast(a + (logs[j] + up)), exp2_fast(b + (logs[j + 1] + up)));
+    out[j / 2] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  return sum;
+}
+
+// The weights of a tile's keys (32 `chunks` of them) that way, from the scores
+// at s_at to the 16-bit weights at w_at. Returns ref, sum, of and most. Three
+// exponentials' worth of work a score: 32 windows of 64 over 8100 in e4m3 take
+// 486 us where every tile comes this way, 359 where none does; 16 tokens over
+// 32768 (the same steps in registers) 234 and 205.
+template <int DP>
+__device__ __noinline__ float4 wide_weights(uint32_t s_at, uint32_t w_at, uint32_t o_at, int chunks, const float* logs, float c, float top,
+                                            bool some_o, float ref, float sum, float of, float most) {
+  const float behind = wide_move(top, c, ref, sum, most);
+  const float from = ref == -INFINITY ? 0.0f : ref;
+  uint32_t s[32];
+#pragma unroll 1
+  for (int i = 0; i < chunks; ++i) {
+    tmem_load32(s_at + 32 * i, s);
+    tmem_wait_load(s);
+    most = wide_largest(s, logs + 32 * i, from, c, most);
+    tmem_store32(s_at + 32 * i, s);
+  }
+  tmem_wait_store();
+  const float now = wide_unit(of, most);
+  if (some_o && __any_sync(0xffffffffu, behind != 0.0f || now != of)) {
+    const float f = exp2_fast(behind + (of - now));
+#pragma unroll 1
+    for (int i = 0; i < DP / 32; ++i) {
+      tmem_load32(o_at + 32 * i, s);
+      tmem_wait_load(s);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) * f);
+      tmem_store32(o_at + 32 * i, s);
+    }
+  }
+#pragma unroll 1
+  for (int i = 0; i < chunks; ++i) {
+    uint32_t out[16];
+    tmem_load32(s_at + 32 * i, s);
+    tmem_wait_load(s);
+    sum += wide_weights_of(s, logs + 32 * i, now, out);
+    tmem_store16(w_at + 16 * i, out);
+  }
+  tmem_wait_store();
+  return make_float4(ref, sum, now, most);
+}
+
 template <int KV, int DP, int NM>
 __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m, uint32_t tmem, float* parts, float2* part_rows, Shared* shared) {
   const int slot = threadIdx.x / 128, row = threadIdx.x & 127, warp_row = row & ~31;
@@ -771,11 +907,8 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     const int limit = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_CAUSAL ? it.start + t + 1 : it.keys;
     const int whole = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_GIVEN ? it.start : limit;
     const int common = common_keys<NM>(p, it);
-    float ref = -INFINITY, sum = 0.0f;
-    // In an 8-bit cache the weights are fp16: 2^kRoom p (v / unit), the values' factors v in units
-    // of a power of two, the largest so far. With p up to 2^8 nothing overflows, and what is
-    // below 2^-30 of the largest is lost.
-    float c_row = c, row_unit = 1.0f, unit = 0.0f;
+    float ref = -INFINITY, sum = 0.0f, c_row = c, row_unit = 1.0f;
+    Unit unit;
     // an 8-bit cache's factors of key `row` of the tiles: the next tile's are on their way while
     // one is worked on, and the page of the one after that
     float next_k = 0.0f, next_v = 0.0f;
@@ -795,6 +928,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     for (int u = 0; u < units; ++u) {
       const int key0 = (k_first + u * stride) * kTile;
       const bool two = it.keys - key0 > kHalf;  // halves of the tile
+      float grown = 1.0f;   // the unit: old over new
       if constexpr (KV != SJD_BF16) {
         // a factor that is no number would reach rows that do not see its key: it is set aside
         // in tiles where there can be such rows (the values' are given to the others at the end)
@@ -802,15 +936,21 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
         const bool bad_k = apart && next_k != next_k, bad_v = apart && next_v != next_v;
         named_barrier(2 + slot, 128);  // all have used the factors of the tile before
         m->row[slot][0][row] = bad_k ? kLeast : fmaxf(next_k, next_k == next_k ? kLeast : next_k);
-        m->row[slot][1][row] = bad_v ? 0.0f : next_v;
+        m->row[slot][1][row] = value_factor(bad_v ? 0.0f : next_v, unit.wide);
         const unsigned poison = __ballot_sync(0xffffffffu, bad_k);
-        if ((threadIdx.x & 31) == 0) m->poison[slot][row / 32] = poison;
         if (bad_v) m->bad_values[w.piece & 3] = w.piece + 1;
-        const uint32_t bits = next_v < INFINITY ? __float_as_uint(next_v) : 0u;
-        const uint32_t most = __reduce_max_sync(0xffffffffu, bits);
-        if ((threadIdx.x & 31) == 0) m->most[slot][row / 32] = most;
+        const ushort2 range = range_of_factors(next_v, key0 + row < it.keys);
+        if ((threadIdx.x & 31) == 0) m->poison[slot][row / 32] = poison, m->range[slot][row / 32] = range;
         named_barrier(2 + slot, 128);
         if (u + 1 < units) factors(u + 1);
+        if (!unit.wide) {
+          const ushort2* of = m->range[slot];
+          grown = take_factors(unit, joint(joint(of[0], of[1]), joint(of[2], of[3])), ref != -INFINITY);
+          if (unit.wide) {  // (the same for the slot)
+            m->row[slot][1][row] = log2f(m->row[slot][1][row]);
+            named_barrier(2 + slot, 128);
+          }
+        }
       }
       wait(m, &m->s_full[slot], sp);
       sp ^= 1;
@@ -842,16 +982,10 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
         // cache): first the largest, then the weights.
         const float* fk = m->row[slot][0];
         const float* fv = m->row[slot][1];
-        float top = -INFINITY, grown = 1.0f;
-        if (KV != SJD_BF16) {
-          if (u == 0) {
-            row_unit = __uint_as_float(static_cast<uint32_t>(127 + m->exponents[w.piece & 1][(NM == 2 ? slot * kTile : 0) + row]) << 23);
-            c_row = fmaxf(c * row_unit, 1e-37f);
-          }
-          const uint32_t most = max(max(m->most[slot][0], m->most[slot][1]), max(m->most[slot][2], m->most[slot][3]));
-          // (the power of two from there on, at least 2^-100 and at most 2^120)
-          const float now = __uint_as_float(max(27u << 23, min(247u << 23, (most + 0x7fffffu) & 0x7f800000u)));
-          if (now > unit) grown = unit > 0.0f ? unit / now : 1.0f, unit = now;
+        float top = -INFINITY;
+        if (KV != SJD_BF16 && u == 0) {
+          row_unit = __uint_as_float(static_cast<uint32_t>(127 + m->exponents[w.piece & 1][(NM == 2 ? slot * kTile : 0) + row]) << 23);
+          c_row = fmaxf(c * row_unit, 1e-37f);
         }
         uint32_t s[2][32];
         tmem_load32(s_at, s[0]);
@@ -869,52 +1003,64 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
         }
         if (!two) tmem_wait_load(s[0]);
         if (KV != SJD_BF16) tmem_wait_store();
-        // The reference that the weights are taken against moves only where a
-        // weight could pass 2^8: their relative precision is the same below
-        // that, and O is left alone.
-        const bool move = (top - ref) * c_row > kRise || (ref == -INFINITY && top != -INFINITY);
-        if (__any_sync(0xffffffffu, move || grown != 1.0f)) {
-          float f = !move ? 1.0f : worth(ref, top, c_row);
-          if (move) ref = top, sum *= f;
-          f *= grown;
+        if (KV != SJD_BF16 && unit.wide) {
           __syncwarp();
-          if (u > 0) {
+          const float4 r = wide_weights<DP>(s_at, s_at, o_at + slot * DP, two ? 4 : 2, fv, c_row, top, u > 0, ref, sum, unit.of, unit.low);
+          ref = r.x, sum = r.y, unit.of = r.z, unit.low = r.w;
+          tc_fence_before();
+          __syncwarp();
+          if ((threadIdx.x & 31) == 0) {
+            mbar_arrive(smem_addr(&m->p_full[slot][0]));
+            if (two) mbar_arrive(smem_addr(&m->p_full[slot][1]));
+          }
+        } else {
+          // The reference that the weights are taken against moves only where a
+          // weight could pass 2^8: their relative precision is the same below
+          // that, and O is left alone.
+          const bool move = (top - ref) * c_row > kRise || (ref == -INFINITY && top != -INFINITY);
+          if (__any_sync(0xffffffffu, move || grown != 1.0f)) {
+            float f = !move ? 1.0f : worth(ref, top, c_row);
+            if (move) ref = top, sum *= f;
+            f *= grown;
+            __syncwarp();
+            if (u > 0) {
 #pragma unroll 1
-            for (int i = 0; i < DP / 32; ++i) {
-              tmem_load32(o_at + slot * DP + 32 * i, s[0]);
-              tmem_wait_load(s[0]);
+              for (int i = 0; i < DP / 32; ++i) {
+                tmem_load32(o_at + slot * DP + 32 * i, s[0]);
+                tmem_wait_load(s[0]);
 #pragma unroll
-              for (int j = 0; j < 32; ++j) s[0][j] = __float_as_uint(__uint_as_float(s[0][j]) * f);
-              tmem_store32(o_at + slot * DP + 32 * i, s[0]);
+                for (int j = 0; j < 32; ++j) s[0][j] = __float_as_uint(__uint_as_float(s[0][j]) * f);
+                tmem_store32(o_at + slot * DP + 32 * i, s[0]);
+              }
             }
           }
-        }
-        // (the unit's exponent, less the room, goes into the powers of two)
-        const int shift = KV == SJD_BF16 ? 0 : static_cast<int>(__float_as_uint(unit) >> 23) - 127 - kRoom;
-        float base = ref == -INFINITY ? 0.0f : ref * c_row;
-        if (__any_sync(0xffffffffu, fabsf(base) > kFar)) less_reference<kTile>(s_at, ref, base);
-        base += static_cast<float>(shift);
-        Pair total[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
-        tmem_load32(s_at, s[0]);
+          // (the unit's exponent, less the room, goes into the powers of two)
+          const int shift = KV == SJD_BF16 ? 0 : static_cast<int>(__float_as_uint(unit.of) >> 23) - 127 - kRoom;
+          float base = ref == -INFINITY ? 0.0f : ref * c_row;
+          if (__any_sync(0xffffffffu, fabsf(base) > kFar)) less_reference<kTile>(s_at, ref, base);
+          base += static_cast<float>(shift);
+          Pair total[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+          tmem_load32(s_at, s[0]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (i < 2 || two) {
-            uint32_t out[16];
-            tmem_wait_load(s[i & 1]);
-            if (i < 3) tmem_load32(s_at + 32 * (i + 1), s[(i + 1) & 1]);
-            weights_of<KV>(s[i & 1], fv + 32 * i, c_row, base, out, total);
-            tmem_store16(s_at + 16 * i, out);
+          for (int i = 0; i < 4; ++i) {
+            if (i < 2 || two) {
+              uint32_t out[16];
+              tmem_wait_load(s[i & 1]);
+              if (i < 3) tmem_load32(s_at + 32 * (i + 1), s[(i + 1) & 1]);
+              weights_of<KV>(s[i & 1], fv + 32 * i, c_row, base, out, total);
+              tmem_store16(s_at + 16 * i, out);
+            }
+            if (i & 1) {
+              tmem_wait_store();
+              tc_fence_before();
+              __syncwarp();
+              if ((threadIdx.x & 31) == 0 && (i == 1 || two)) mbar_arrive(smem_addr(&m->p_full[slot][i / 2]));
+            }
           }
-          if (i & 1) {
-            tmem_wait_store();
-            tc_fence_before();
-            __syncwarp();
-            if ((threadIdx.x & 31) == 0 && (i == 1 || two)) mbar_arrive(smem_addr(&m->p_full[slot][i / 2]));
-          }
+          if (!two) tmem_wait_load(s[0]);
+          const float2 ends = halves(add2(total[0], total[1]));
+          sum += (ends.x + ends.y) * (KV == SJD_BF16 ? 1.0f : __uint_as_float(static_cast<uint32_t>(127 + shift) << 23));
         }
-        if (!two) tmem_wait_load(s[0]);
-        const float2 ends = halves(add2(total[0], total[1]));
-        sum += (ends.x + ends.y) * (KV == SJD_BF16 ? 1.0f : __uint_as_float(static_cast<uint32_t>(127 + shift) << 23));
       } else if ((threadIdx.x & 31) == 0) {
         mbar_arrive(smem_addr(&m->p_full[slot][0]));
         if (two) mbar_arrive(smem_addr(&m->p_full[slot][1]));
@@ -924,14 +1070,13 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     // the end of the piece: O of both slots is complete
     wait(m, &m->o_full, w.piece & 1);
     tc_fence_after();
-    float f[2] = {1.0f, 1.0f};
+    float f[2] = {1.0f, 1.0f}, back[2] = {1.0f, 1.0f};
     const int tiles = w.k1 - w.k0;
     const bool take[2] = {NM == 1 || slot == 0, NM == 1 ? tiles > 1 : slot == 1};
     if constexpr (NM == 1) {
       named_barrier(2 + slot, 128);  // (the factors are done with)
       m->row[slot][0][row] = ref * row_unit;
       m->row[slot][1][row] = sum;
-      if (KV != SJD_BF16 && row == 0) m->most[slot][0] = __float_as_uint(unit);
       named_barrier(1, 256);
       const float r1 = tiles > 1 ? m->row[1][0][row] : -INFINITY, r0s = m->row[0][0][row];
       const float s1 = tiles > 1 ? m->row[1][1][row] : 0.0f, s0 = m->row[0][1][row];
@@ -939,13 +1084,16 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
       f[0] = worth(r0s, ref, c);
       f[1] = worth(r1, ref, c);
       sum = s0 * f[0] + s1 * f[1];
-      if (KV != SJD_BF16) {
-        f[0] *= __uint_as_float(m->most[0][0]) * (1.0f / (1 << kRoom));
-        if (tiles > 1) f[1] *= __uint_as_float(m->most[1][0]) * (1.0f / (1 << kRoom));
+      if constexpr (KV != SJD_BF16) {  // each slot knows its unit
+        named_barrier(1, 256);
+        m->row[slot][0][row] = unit.back();
+        named_barrier(1, 256);
+        back[0] = m->row[0][0][row];
+        back[1] = tiles > 1 ? m->row[1][0][row] : 0.0f;
       }
     } else if (KV != SJD_BF16) {
       ref *= row_unit;
-      f[0] = f[1] = unit * (1.0f / (1 << kRoom));
+      back[0] = back[1] = unit.back();
     }
     const bool wholly = w.k0 == 0 && w.k1 == it.tiles;
     const bool bad = *const_cast<volatile int*>(&m->bad_values[w.piece & 3]) == w.piece + 1;
@@ -972,7 +1120,10 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
           tmem_load32(o_at + e * DP + column, x);
           tmem_wait_load(x);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) o[j] = NM == 1 || KV != SJD_BF16 ? fmaf(__uint_as_float(x[j]), f[e], o[j]) : __uint_as_float(x[j]);
+          for (int j = 0; j < 32; ++j) {
+            const float v = __uint_as_float(x[j]);
+            o[j] = KV != SJD_BF16 ? fmaf(NM == 1 ? v * f[e] : v, back[e], o[j]) : NM == 1 ? fmaf(v, f[e], o[j]) : v;
+          }
         }
         if (bad && valid) {
           float with[32];
@@ -1065,7 +1216,8 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
     const int limit = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_CAUSAL ? it.start + t + 1 : it.keys;
     const int whole = !valid ? 0x7fffffff : p.mask_kind == SJD_MASK_GIVEN ? it.start : limit;
     const int common = common_keys<1>(p, it);
-    float ref = -INFINITY, sum = 0.0f, c_row = c, row_unit = 1.0f, unit = 0.0f;
+    float ref = -INFINITY, sum = 0.0f, c_row = c, row_unit = 1.0f;
+    Unit unit;
     // the factors of key `at` of a tile, as in softmax_rows
     float next_k = 0.0f, next_v = 0.0f;
     int page = kNoPage;
@@ -1084,18 +1236,27 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
     for (int u = 0; u < units; ++u) {
       const int tile_key = (k_first + 2 * u) * kTile, key0 = tile_key + copy * kKeys;
       const bool two = it.keys - tile_key > kHalf;
+      float grown = 1.0f;
       if constexpr (KV != SJD_BF16) {
         const bool apart = tile_key + kTile > common;
         const bool bad_k = apart && next_k != next_k, bad_v = apart && next_v != next_v;
         copy_barrier();  // all have used the factors of the tile before
         m->row[slot][0][at] = bad_k ? kLeast : fmaxf(next_k, next_k == next_k ? kLeast : next_k);
-        m->row[slot][1][at] = bad_v ? 0.0f : next_v;
+        m->row[slot][1][at] = value_factor(bad_v ? 0.0f : next_v, unit.wide);
         const unsigned poison = __ballot_sync(0xffffffffu, bad_k);
         if (bad_v) m->bad_values[w.piece & 3] = w.piece + 1;
-        const uint32_t most = __reduce_max_sync(0xffffffffu, next_v < INFINITY ? __float_as_uint(next_v) : 0u);
-        if (lane == 0) m->poison[slot][at / 32] = poison, m->most[slot][at / 32] = most;
+        const ushort2 range = range_of_factors(next_v, tile_key + at < it.keys);
+        if (lane == 0) m->poison[slot][at / 32] = poison, m->range[slot][at / 32] = range;
         copy_barrier();
         if (u + 1 < units) factors(u + 1);
+        if (!unit.wide) {
+          const ushort2* of = m->range[slot] + copy * kChunks;
+          grown = take_factors(unit, SP == 4 ? of[0] : joint(of[0], of[1]), ref != -INFINITY);
+          if (unit.wide) {  // (the same for the copy)
+            m->row[slot][1][at] = log2f(m->row[slot][1][at]);
+            copy_barrier();
+          }
+        }
       }
       wait(m, &m->s_full[slot], sp);
       sp ^= 1;
@@ -1105,16 +1266,10 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
         uint32_t bad = 0;
         if (KV != SJD_BF16) bad = SP == 4 ? poison[0] : poison[0] | poison[1];
         const bool mixed = !__all_sync(0xffffffffu, key0 + kKeys <= whole) || bad;
-        float top = -INFINITY, grown = 1.0f;
-        if (KV != SJD_BF16) {
-          if (u == 0) {
-            row_unit = __uint_as_float(static_cast<uint32_t>(127 + m->exponents[w.piece & 1][at]) << 23);
-            c_row = fmaxf(c * row_unit, 1e-37f);
-          }
-          const uint32_t* words = m->most[slot] + copy * kChunks;
-          const uint32_t most = SP == 4 ? words[0] : max(words[0], words[1]);
-          const float now = __uint_as_float(max(27u << 23, min(247u << 23, (most + 0x7fffffu) & 0x7f800000u)));
-          if (now > unit) grown = unit > 0.0f ? unit / now : 1.0f, unit = now;
+        float top = -INFINITY;
+        if (KV != SJD_BF16 && u == 0) {
+          row_unit = __uint_as_float(static_cast<uint32_t>(127 + m->exponents[w.piece & 1][at]) << 23);
+          c_row = fmaxf(c * row_unit, 1e-37f);
         }
         const float* fk = m->row[slot][0] + copy * kKeys;
         const float* fv = m->row[slot][1] + copy * kKeys;
@@ -1144,13 +1299,29 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
           top = largest_of(s, top);
         }
         if (kChunks > 1) tmem_wait_store();
-        const bool move = (top - ref) * c_row > kRise || (ref == -INFINITY && top != -INFINITY);
-        if (__any_sync(0xffffffffu, move || grown != 1.0f)) {
-          float f = !move ? 1.0f : worth(ref, top, c_row);
-          if (move) ref = top, sum *= f;
-          f *= grown;
+        if (KV != SJD_BF16 && kChunks > 1 && unit.wide) {
           __syncwarp();
-          if (u > 0) {
+          const float4 r = wide_weights<DP>(s_at + copy * kKeys, s_at + 16 * copy * kChunks, o_at, kChunks, fv, c_row, top, u > 0, ref, sum, unit.of, unit.low);
+          ref = r.x, sum = r.y, unit.of = r.z, unit.low = r.w;
+        } else {
+          const bool wide = KV != SJD_BF16 && kChunks == 1 && unit.wide;  // (a call's registers would cost every tile 30 %)
+          float f = 1.0f;
+          bool turn;
+          if (wide) {
+            const float behind = wide_move(top, c_row, ref, sum, unit.low);
+            unit.low = wide_largest(s, fv, ref == -INFINITY ? 0.0f : ref, c_row, unit.low);
+            const float now = wide_unit(unit.of, unit.low);
+            f = exp2_fast(behind + (unit.of - now));
+            turn = behind != 0.0f || now != unit.of;
+            unit.of = now;
+          } else {
+            const bool move = (top - ref) * c_row > kRise || (ref == -INFINITY && top != -INFINITY);
+            turn = move || grown != 1.0f;
+            if (move) f = worth(ref, top, c_row), ref = top, sum *= f;
+            f *= grown;
+          }
+          __syncwarp();
+          if (u > 0 && __any_sync(0xffffffffu, turn)) {
 #pragma unroll 1
             for (int i = 0; i < DP / 16; ++i) {
               uint32_t o[16];
@@ -1161,39 +1332,44 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
               tmem_store16(o_at + 16 * i, o);
             }
           }
-        }
-        const int shift = KV == SJD_BF16 ? 0 : static_cast<int>(__float_as_uint(unit) >> 23) - 127 - kRoom;
-        float base = ref == -INFINITY ? 0.0f : ref * c_row;
-        if (__any_sync(0xffffffffu, fabsf(base) > kFar)) {
-          if constexpr (kChunks == 1) {
-            const float from = ref == -INFINITY ? 0.0f : ref;
-            base = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) - from);
+          uint32_t out[kChunks][16];
+          if (wide) {
+            sum += wide_weights_of(s, fv, unit.of, out[0]);
           } else {
-            less_reference<kKeys>(s_at + copy * kKeys, ref, base);
-          }
-        }
-        base += static_cast<float>(shift);
-        Pair total[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
-        uint32_t out[kChunks][16];
+            const int shift = KV == SJD_BF16 ? 0 : static_cast<int>(__float_as_uint(unit.of) >> 23) - 127 - kRoom;
+            float base = ref == -INFINITY ? 0.0f : ref * c_row;
+            if (__any_sync(0xffffffffu, fabsf(base) > kFar)) {
+              if constexpr (kChunks == 1) {
+                const float from = ref == -INFINITY ? 0.0f : ref;
+                base = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kChunks; ++i) {
-          if (kChunks > 1) {
-            tmem_load32(s_at + copy * kKeys + 32 * i, s);
-            tmem_wait_load(s);
+                for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) - from);
+              } else {
+                less_reference<kKeys>(s_at + copy * kKeys, ref, base);
+              }
+            }
+            base += static_cast<float>(shift);
+            Pair total[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i) {
+              if (kChunks > 1) {
+                tmem_load32(s_at + copy * kKeys + 32 * i, s);
+                tmem_wait_load(s);
+              }
+              weights_of<KV>(s, fv + 32 * i, c_row, base, out[i], total);
+            }
+            const float2 ends = halves(add2(total[0], total[1]));
+            sum += (ends.x + ends.y) * (KV == SJD_BF16 ? 1.0f : __uint_as_float(static_cast<uint32_t>(127 + shift) << 23));
           }
-          weights_of<KV>(s, fv + 32 * i, c_row, base, out[i], total);
+#pragma unroll
+          for (int i = 0; i < kChunks; ++i) tmem_store16(s_at + 16 * (copy * kChunks + i), out[i]);
         }
         // (the row's weights of the other copies' keys are 0)
+        uint32_t none[16];
 #pragma unroll
-        for (int i = 0; i < kChunks; ++i) tmem_store16(s_at + 16 * (copy * kChunks + i), out[i]);
+        for (int j = 0; j < 16; ++j) none[j] = 0;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) out[0][j] = 0;
-#pragma unroll
-        for (int i = kChunks; i < 4; ++i) tmem_store16(s_at + 16 * ((copy * kChunks + i) % 4), out[0]);
-        const float2 ends = halves(add2(total[0], total[1]));
-        sum += (ends.x + ends.y) * (KV == SJD_BF16 ? 1.0f : __uint_as_float(static_cast<uint32_t>(127 + shift) << 23));
+        for (int i = kChunks; i < 4; ++i) tmem_store16(s_at + 16 * ((copy * kChunks + i) % 4), none);
         tmem_wait_store();
         tc_fence_before();
       }
@@ -1216,7 +1392,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
     float most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 2 * SP; ++i) most = fmaxf(most, m->row[i & 1][0][i / 2 * kRows + row]);
-    const float own = units > 0 && active ? worth(ref, most, c) * (KV == SJD_BF16 ? 1.0f : unit * (1.0f / (1 << kRoom))) : 0.0f;
+    const float own = units > 0 && active ? worth(ref, most, c) : 0.0f, back = KV == SJD_BF16 ? 1.0f : unit.back();
     const bool wholly = w.k0 == 0 && w.k1 == it.tiles;
     const bool bad = *const_cast<volatile int*>(&m->bad_values[w.piece & 3]) == w.piece + 1;
     const long long part = 2ll * blockIdx.x + (w.k0 == 0 ? 1 : 0);
@@ -1239,7 +1415,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
             // (a copy without weights has nothing, whatever its accumulator holds)
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (units > 0 && ref != -INFINITY)
-              v = make_float4(__uint_as_float(o[j]) * own, __uint_as_float(o[j + 1]) * own, __uint_as_float(o[j + 2]) * own, __uint_as_float(o[j + 3]) * own);
+              v = make_float4(__uint_as_float(o[j]) * own * back, __uint_as_float(o[j + 1]) * own * back, __uint_as_float(o[j + 2]) * own * back, __uint_as_float(o[j + 3]) * own * back);
             mine[(4 * i + j / 4) ^ (lane & (kFours - 1))] = v;
           }
         }
