@@ -378,6 +378,24 @@ __device__ __forceinline__ bool take_out(uint32_t& w) {
   return out != 0;
 }
 
+// The same for four codes of e4m3 (0x7f and 0xff stand for NaN).
+__device__ __forceinline__ bool take_out_codes(uint32_t& w) {
+  const uint32_t out = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+  w &= ~((out >> 7) * 0xffu);
+  return out != 0;
+}
+// (a call: it is for the tiles at the end of an item alone)
+__device__ __noinline__ bool take_out_of_codes(uint32_t at, int rounds, int step) {
+  bool any = false;
+#pragma unroll 1
+  for (int i = 0; i < rounds; ++i, at += step) {
+    uint2 v = shared_load8(at);
+    const bool x = take_out_codes(v.x), y = take_out_codes(v.y);
+    if (x || y) shared_store8(at, v), any = true;
+  }
+  return any;
+}
+
 // The four warps of one operand, keys (IS_V false) or values, go through the
 // block's tiles. A thread has the piece tid % (DP / 8) of every 128 / (DP /
 // 8)-th row; a lane finds the vector of row (warp * 32 + lane) and the others
@@ -506,12 +524,18 @@ __device__ __forceinline__ void load_operand(const AttendParams& p, Misc<NM>* m,
         load_half_queries<DP, NM, SP>(p, w.it, smem, tid, m->exponents[w.piece & 1]);
         queries_there();
       }
+      const int common = IS_V && KV == SJD_E4M3 ? common_keys<NM>(p, w.it) : 0x7fffffff;
       for (int k = w.k0; k < w.k1; ++k) {
         wait(m, &empty[stage], round);
         copy_wait<P::kRaw - 1>();
         __syncwarp();
+        if (IS_V && KV == SJD_E4M3 && (k + 1) * kTile > common) {  // some row does not see every key (take_out)
+          if (take_out_of_codes(from + slot * (kTile * DP), kRounds, kStep * DP)) m->bad_values[w.piece & 3] = w.piece + 1;
+        }
         const uint32_t to = ring + stage * tile_bytes(DP);
-#pragma unroll
+        // (unrolled, the batches crowd the instruction cache: 363 us instead of 353 for 32
+        // windows of 64 over 8100, 215 instead of 208 for 16 tokens over 32768)
+#pragma unroll 1
         for (int i0 = 0; i0 < kRounds; i0 += 8) {
           uint2 codes[8];
 #pragma unroll
@@ -644,8 +668,14 @@ __device__ __forceinline__ void issue_products(const AttendParams& p, Misc<NM>* 
 
 // --- softmax --------------------------------------------------------------------
 
-// Values that were taken out of the tiles (take_out) or whose factor was set
-// aside, for the rows that see them.
+template <int KV>
+__device__ __forceinline__ float value_of(typename Codes<KV>::type code) {
+  if constexpr (KV == SJD_E4M3) return __half2float(__half(__nv_cvt_fp8_to_halfraw(code, __NV_E4M3)));
+  else return static_cast<float>(code);
+}
+
+// Values that were taken out of the tiles (take_out, take_out_codes) or whose
+// factor was set aside, for the rows that see them.
 template <int KV, int NM, int N>
 __device__ __noinline__ void add_bad_values(const AttendParams& p, const Item& it, int k0, int k1, int t, int column, float (&o)[N]) {
   // (the tiles that were looked over: those with a key that some row does not see)
@@ -663,8 +693,10 @@ __device__ __noinline__ void add_bad_values(const AttendParams& p, const Item& i
       }
     } else {
       const float f = p.c.vs[at];
-      if (f != f) {
-        for (int i = 0; i < N; ++i) o[i] += f;
+      const typename Codes<KV>::type* v = static_cast<const typename Codes<KV>::type*>(p.c.v) + static_cast<size_t>(at) * p.c.D;
+      for (int i = 0; i < N && column + i < p.c.D; ++i) {
+        const float x = value_of<KV>(v[column + i]);
+        if (!(f < INFINITY) || x != x) o[i] += x * f;
       }
     }
   }
@@ -930,10 +962,11 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
       const bool two = it.keys - key0 > kHalf;  // halves of the tile
       float grown = 1.0f;   // the unit: old over new
       if constexpr (KV != SJD_BF16) {
-        // a factor that is no number would reach rows that do not see its key: it is set aside
-        // in tiles where there can be such rows (the values' are given to the others at the end)
+        // a factor that is no number would reach rows that do not see its key (and so would an
+        // infinite one of a value, times a weight of 0): it is set aside in tiles where there
+        // can be such rows (the values' are given to the others at the end)
         const bool apart = key0 + kTile > common;
-        const bool bad_k = apart && next_k != next_k, bad_v = apart && next_v != next_v;
+        const bool bad_k = apart && next_k != next_k, bad_v = apart && !(next_v < INFINITY);
         named_barrier(2 + slot, 128);  // all have used the factors of the tile before
         m->row[slot][0][row] = bad_k ? kLeast : fmaxf(next_k, next_k == next_k ? kLeast : next_k);
         m->row[slot][1][row] = value_factor(bad_v ? 0.0f : next_v, unit.wide);
@@ -1239,7 +1272,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
       float grown = 1.0f;
       if constexpr (KV != SJD_BF16) {
         const bool apart = tile_key + kTile > common;
-        const bool bad_k = apart && next_k != next_k, bad_v = apart && next_v != next_v;
+        const bool bad_k = apart && next_k != next_k, bad_v = apart && !(next_v < INFINITY);
         copy_barrier();  // all have used the factors of the tile before
         m->row[slot][0][at] = bad_k ? kLeast : fmaxf(next_k, next_k == next_k ? kLeast : next_k);
         m->row[slot][1][at] = value_factor(bad_v ? 0.0f : next_v, unit.wide);
