@@ -676,10 +676,8 @@ __device__ __forceinline__ float value_of(typename Codes<KV>::type code) {
 
 // Values that were taken out of the tiles (take_out, take_out_codes) or whose
 // factor was set aside, for the rows that see them.
-template <int KV, int NM, int N>
-__device__ __noinline__ void add_bad_values(const AttendParams& p, const Item& it, int k0, int k1, int t, int column, float (&o)[N]) {
-  // (the tiles that were looked over: those with a key that some row does not see)
-  const int end = min(it.keys, k1 * kTile), begin = max(k0, common_keys<NM>(p, it) / kTile) * kTile;
+template <int KV, int N>
+__device__ __noinline__ void add_bad_values(const AttendParams& p, const Item& it, int begin, int end, int t, int column, float (&o)[N]) {
   for (int key = begin; key < end; ++key) {
     const bool seen = key < it.start || p.mask_kind == SJD_MASK_ALL ||
                       (p.mask_kind == SJD_MASK_CAUSAL ? key <= it.start + t : p.mask[p.mask_b * it.b + p.mask_r * t + (key - it.start)] != 0);
@@ -700,6 +698,12 @@ __device__ __noinline__ void add_bad_values(const AttendParams& p, const Item& i
       }
     }
   }
+}
+
+// The keys of a piece's tiles that were looked over: those with a key that some row does not see.
+template <int NM>
+__device__ __forceinline__ int first_looked_over(const AttendParams& p, const Item& it, int k0) {
+  return max(k0, common_keys<NM>(p, it) / kTile) * kTile;
 }
 
 // Scores of keys that the row does not see become -inf; of those that it
@@ -1162,7 +1166,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
           float with[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) with[j] = o[j];
-          add_bad_values<KV, NM>(p, it, w.k0, w.k1, t, column, with);
+          add_bad_values<KV>(p, it, first_looked_over<NM>(p, it, w.k0), min(it.keys, w.k1 * kTile), t, column, with);
 #pragma unroll
           for (int j = 0; j < 32; ++j) o[j] = with[j];
         }
@@ -1470,7 +1474,24 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
           o[0] += v.x, o[1] += v.y, o[2] += v.z, o[3] += v.w;
         }
         const int its_t = by_group(p.c, r), g = r - its_t * G;
-        if (bad) add_bad_values<KV, 1>(p, it, w.k0, w.k1, its_t, col, o);
+        const int keys_end = min(it.keys, w.k1 * kTile);
+        if (KV == SJD_BF16 && all == all) {
+          // An infinity that all rows see is in the tile, and the copies that have other keys
+          // made 0 * inf of it: where that left a NaN, the values that are not finite tell.
+#pragma unroll 1
+          for (int i = 0; i < 4; ++i) {
+            const float v = i == 0 ? o[0] : i == 1 ? o[1] : i == 2 ? o[2] : o[3];
+            if (v == v) continue;
+            float x[1] = {0.0f};
+            add_bad_values<KV>(p, it, w.k0 * kTile, keys_end, its_t, col + i, x);
+            if (x[0] == 0.0f) continue;
+            if (i == 0) o[0] = x[0];
+            else if (i == 1) o[1] = x[0];
+            else if (i == 2) o[2] = x[0];
+            else o[3] = x[0];
+          }
+        }
+        if (bad) add_bad_values<KV>(p, it, first_looked_over<1>(p, it, w.k0), keys_end, its_t, col, o);
         const long long head = (static_cast<long long>(it.b) * p.c.n + its_t) * p.c.Hq + static_cast<long long>(it.kvh) * G + g;
         const bool some = all > 0.0f || all != all;
         if (wholly) {

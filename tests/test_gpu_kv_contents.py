@@ -95,3 +95,26 @@ def test_an_infinite_scale_that_is_seen(dtype, rows, where):
     assert torch.equal(hit.nan_to_num(nan=7.0), row.expand_as(hit).nan_to_num(nan=7.0))
     o[:, sees, G:] = want[:, sees, G:]
     assert (o.double() - want.double()).norm() <= 0.003 * want.double().norm()
+
+
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("at", [[40], [300], [40, 200]])
+def test_infinite_values_that_every_row_sees(rows, at):
+    """A 16-bit cache: an infinity stays one, two of both signs give NaN."""
+    heads, kv_heads, n = rows
+    s = 333
+    h, layer, table, start, g = base.make(1, heads, kv_heads, D, torch.bfloat16, 16, [s], n)
+    base.filled(h, layer, table, [s], n, g)
+    q = base.normal(g, 1, n, heads, D).bfloat16()
+    want = h.attend(layer, q, table, start)
+    for i, key in enumerate(at):
+        page, slot = place(table, 16, key)
+        layer.v[page, 1, slot, 5] = -math.inf
+        layer.v[page, 1, slot, 9] = math.inf if i == 0 else -math.inf
+    o = h.attend(layer, q, table, start)
+    G = heads // kv_heads
+    assert (o[:, :, G:, 5] == -math.inf).all()
+    assert (o[:, :, G:, 9] == math.inf).all() if len(at) == 1 else o[:, :, G:, 9].isnan().all()
+    for column in (5, 9):
+        o[:, :, G:, column] = want[:, :, G:, column]
+    assert torch.equal(o, want)
