@@ -52,7 +52,6 @@ namespace sjd_kv_ops {
 
 namespace {
 
-constexpr int kTile = 128;              // rows of a product, and keys of a tile
 constexpr int kHalf = kTile / 2;        // keys whose weights are handed over at a time
 constexpr int kAttendThreads = 20 * 32;
 constexpr int kMmaWarp = 19;            // (on another scheduler than the first rows' softmax)
@@ -120,21 +119,6 @@ struct Item {
   int keys;             // keys that some row of the item sees: 0 .. keys - 1
   int tiles;            // of 128 keys
 };
-
-template <int NM>
-__device__ __forceinline__ int keys_of(const AttendParams& p, int start, int count, int mt) {
-  if (p.mask_kind != SJD_MASK_CAUSAL) return start + count;
-  return start + by_group(p.c, min((mt + 1) * (kTile * NM), count * p.c.group) - 1) + 1;
-}
-
-// Key tiles of one key head of a sequence, all its items.
-template <int NM>
-__device__ int tiles_of(const AttendParams& p, int2 span) {
-  const int items = (span.y * p.c.group + kTile * NM - 1) / (kTile * NM);
-  int sum = 0;
-  for (int mt = 0; mt < items; ++mt) sum += (keys_of<NM>(p, span.x, span.y, mt) + kTile - 1) / kTile;
-  return sum;
-}
 
 template <int NM>
 __device__ __forceinline__ void fill(const AttendParams& p, Item& it) {
@@ -930,7 +914,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
   if (m->start.tiles <= 0) return;
   if (row == 0) w.begin(p, m->start);
   named_barrier(2 + slot, 128);
-  int tile_no = 0;  // the block's number of the piece's first tile
+  long long tile_no = 0;  // the block's number of the piece's first tile
   uint32_t sp = 0;
   for (;;) {
     const int r0 = it.mt * (kTile * NM) + (NM == 2 ? slot * kTile : 0);
@@ -1204,7 +1188,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     } else {
       named_barrier(2 + slot, 128);
     }
-    if (tile_no == m->start.tiles) return;
+    if (tile_no >= m->start.tiles) return;
     if (row == 0) w.next(p);
     named_barrier(2 + slot, 128);
   }
@@ -1244,7 +1228,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
   if (m->start.tiles <= 0) return;
   if (at == 0) w.begin(p, m->start);
   named_barrier(2 + slot, 128);
-  int tile_no = 0;
+  long long tile_no = 0;
   uint32_t sp = 0;
   for (;;) {
     const bool valid = row < it.rows, active = (at & ~31) % kRows < it.rows;
@@ -1566,7 +1550,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
     if (threadIdx.x == 0) mbar_arrive(smem_addr(&m->q_empty));  // the queries' memory is free again
     tile_no += tiles;
     named_barrier(2 + slot, 128);
-    if (tile_no == m->start.tiles) return;
+    if (tile_no >= m->start.tiles) return;
     if (at == 0) w.next(p);
     named_barrier(2 + slot, 128);
   }

@@ -33,11 +33,11 @@ __device__ __forceinline__ int2 span_of(const Cache& c, int b) {
 constexpr uint32_t kNoVector = 0xffffffffu;
 constexpr int kNoPage = -0x7fffffff - 1;  // a token that is not there
 
-__device__ __forceinline__ int divide(int x, uint32_t mul, int shift) {
+__host__ __device__ __forceinline__ int divide(int x, uint32_t mul, int shift) {
   return static_cast<int>(static_cast<unsigned long long>(static_cast<uint32_t>(x)) * mul >> (31 + shift));
 }
 __device__ __forceinline__ int entry_of(const Cache& c, int pos) { return divide(pos, c.ps_mul, c.ps_shift); }
-__device__ __forceinline__ int by_group(const Cache& c, int x) { return divide(x, c.group_mul, c.group_shift); }
+__host__ __device__ __forceinline__ int by_group(const Cache& c, int x) { return divide(x, c.group_mul, c.group_shift); }
 
 // The table's entry of token pos of sequence b, as it stands there.
 __device__ __forceinline__ int page_of(const Cache& c, int b, int pos) {
@@ -50,6 +50,24 @@ __device__ __forceinline__ uint32_t vector_in(const Cache& c, int page, int pos,
     return kNoVector;
   }
   return (static_cast<uint32_t>(page) * c.Hkv + h) * c.ps + (pos - entry_of(c, pos) * c.ps);
+}
+
+constexpr int kTile = 128;              // rows of an attention's product, and keys of a tile
+
+// The keys that some row of item mt (128 NM rows) of a span sees: 0 .. keys - 1.
+template <int NM>
+__host__ __device__ __forceinline__ int keys_of(const AttendParams& p, int start, int count, int mt) {
+  if (p.mask_kind != SJD_MASK_CAUSAL) return start + count;
+  return start + by_group(p.c, min((mt + 1) * (kTile * NM), count * p.c.group) - 1) + 1;
+}
+
+// Key tiles of one key head of a sequence, all its items.
+template <int NM>
+__host__ __device__ long long tiles_of(const AttendParams& p, int2 span) {
+  const int items = (span.y * p.c.group + kTile * NM - 1) / (kTile * NM);
+  long long sum = 0;  // (a long prompt of many heads has more than 2^31)
+  for (int mt = 0; mt < items; ++mt) sum += (keys_of<NM>(p, span.x, span.y, mt) + kTile - 1) / kTile;
+  return sum;
 }
 
 // Four neighbouring elements as fp32, in one access where the address allows
