@@ -258,7 +258,8 @@ class KV:
         start[b] .. start[b] + count[b] - 1 (count None: n) of the sequences
         whose pages are table [B, max_pages]. With rope and positions [B, n,
         axes] the keys are turned first, and q [B, n, heads, D], if given, is
-        turned into the result."""
+        turned into the result (q_out, or a new tensor), whose rows from
+        count[b] on are not written."""
         c = self.cfg
         if k.dim() != 4 or k.dtype not in _DTYPES:
             raise ValueError("k must be a [B, n, kv_heads, D] bf16 or f32 tensor")
@@ -267,7 +268,13 @@ class KV:
         kw, vw = _view_of(k, "k", shape, dt, self.device), _view_of(v, "v", shape, dt, self.device)
         at, span = self._layer_of(layer), self._span(table, start, count, n)
         rope_c = pos = qw = ow = turns = axis = None
+        if q is None and q_out is not None:
+            raise ValueError("q_out goes with q")
         if rope is not None:
+            if rope.device != self.device:
+                raise ValueError("rope is on %s, the cache on %s" % (rope.device, self.device))
+            if positions is None:
+                raise ValueError("rope goes with positions")
             rope_c, pos, turns, axis = rope._c, _array(positions, "positions", (B, n, rope.axes), self.device), rope._turns, rope._axis
         if q is not None:
             shape = (B, n, c.heads, c.head_dim)
