@@ -13,6 +13,10 @@ and attention of a chunk of new tokens over it. Argument marshalling only.
 Calls run on the handle's stream. Where that is not the caller's current
 stream, a call first waits for the current one, and the current one for the
 call, so that tensors may be made and used on either.
+
+No call records a gradient. A tensor that wants one is refused, unless
+gradients are off (torch.no_grad); a rotation's gradient is the rotation with
+inverse=True.
 """
 
 import ctypes
@@ -84,6 +88,8 @@ def _device(device):
 def _view_of(x, name, shape, dtype, device):
     if x.shape != shape or x.dtype != dtype or x.device != device or x.stride(3) != 1:
         raise ValueError("%s must be a %s tensor of shape %s on %s, its last dimension dense" % (name, dtype, tuple(shape), device))
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError("%s wants a gradient, and no call here records one: detach it, or call under torch.no_grad()" % name)
     s = x.stride()
     return _VIEW.pack(x.data_ptr(), s[0], s[1], s[2])
 

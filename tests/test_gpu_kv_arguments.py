@@ -33,3 +33,26 @@ def test_a_rope_of_another_device_or_without_positions_is_refused():
     with pytest.raises(ValueError):
         h.write(layer, x, x, table, start, rope=rope, positions=positions)
     assert torch.equal(layer.k, before)
+
+
+# --- gradients ----------------------------------------------------------------
+
+def test_tensors_that_want_a_gradient_are_refused():
+    """No call records one: it says so, unless gradients are off."""
+    h, layer, table, start, g = base.make(1, 4, 2, 64, torch.bfloat16, 16, [20], 4)
+    base.filled(h, layer, table, [20], 4, g)
+    rope = kv.Rope.sections((16, 16))
+    positions = torch.zeros(1, 4, 2, dtype=torch.int32, device=DEV)
+    x, q = base.normal(g, 1, 4, 2, 64).bfloat16(), base.normal(g, 1, 4, 4, 64).bfloat16()
+    leaf = lambda t: t.clone().requires_grad_()
+    calls = (lambda: rope.rotate(leaf(q), positions), lambda: rope.rotate(q, positions, out=leaf(q)),
+             lambda: h.write(layer, leaf(x), x, table, start), lambda: h.write(layer, x, leaf(x), table, start),
+             lambda: h.write(layer, x, x, table, start, rope=rope, positions=positions, q=leaf(q)),
+             lambda: h.attend(layer, leaf(q), table, start))
+    for call in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    with torch.no_grad():
+        assert torch.equal(h.attend(layer, leaf(q), table, start), h.attend(layer, q, table, start))
+        assert torch.equal(rope.rotate(leaf(q), positions), rope.rotate(q, positions))
+        h.write(layer, leaf(x), leaf(x), table, start)
