@@ -119,6 +119,7 @@ class Rope:
         self._turns = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64, device=self.device)
         self._axis = torch.tensor(axis, dtype=torch.int32, device=self.device)
         self._c = _ROPE.pack(self._turns.data_ptr(), self._axis.data_ptr(), self.pairs, self.axes, self.interleaved)
+        self._made_on = _raw_stream(self.device.index)
 
     @classmethod
     def sections(cls, pairs, theta=10000.0, shared=False, interleaved=False, device="cuda"):
@@ -131,6 +132,13 @@ class Rope:
         else:
             freq = [theta ** (-i / m) for m in pairs for i in range(m)]
         return cls(freq, axis, interleaved, device)
+
+    def _used_on(self, raw, stream):
+        """The tables' memory is not handed out again before a call on another
+        stream than the one they were made on has read them."""
+        if raw != self._made_on:
+            self._turns.record_stream(stream())
+            self._axis.record_stream(stream())
 
     def rotate(self, x, positions, inverse=False, out=None):
         """x [B, n, H, D] (bf16 or f32) turned by positions [B, n, axes]
@@ -149,7 +157,8 @@ class Rope:
             ow = _view_of(out, "out", shape, dtype, dev)
         if x.numel() == 0:
             return out
-        args = (self._c, xw, ow, at, B, n, H, D, _DTYPES[dtype], 1 if inverse else 0, _raw_stream(dev.index))
+        raw = _raw_stream(dev.index)
+        args = (self._c, xw, ow, at, B, n, H, D, _DTYPES[dtype], 1 if inverse else 0, raw)
         if _current_device() == self.device.index:
             rc = load().sjd_rotate(*args)
         else:
@@ -157,6 +166,7 @@ class Rope:
                 rc = load().sjd_rotate(*args)
         if rc != SJD_OK:
             raise SJDError(rc, "sjd_rotate failed (dim a multiple of 8 up to 256, 2 * pairs at most dim)")
+        self._used_on(raw, lambda: torch.cuda.current_stream(dev))
         return out
 
 
@@ -273,7 +283,7 @@ class KV:
         shape = (B, n, c.kv_heads, c.head_dim)
         kw, vw = _view_of(k, "k", shape, dt, self.device), _view_of(v, "v", shape, dt, self.device)
         at, span = self._layer_of(layer), self._span(table, start, count, n)
-        rope_c = pos = qw = ow = turns = axis = None
+        rope_c = pos = qw = ow = None
         if q is None and q_out is not None:
             raise ValueError("q_out goes with q")
         if rope is not None:
@@ -281,7 +291,7 @@ class KV:
                 raise ValueError("rope is on %s, the cache on %s" % (rope.device, self.device))
             if positions is None:
                 raise ValueError("rope goes with positions")
-            rope_c, pos, turns, axis = rope._c, _array(positions, "positions", (B, n, rope.axes), self.device), rope._turns, rope._axis
+            rope_c, pos = rope._c, _array(positions, "positions", (B, n, rope.axes), self.device)
         if q is not None:
             shape = (B, n, c.heads, c.head_dim)
             qw = _view_of(q, "q", shape, dt, self.device)
@@ -291,7 +301,9 @@ class KV:
             else:
                 ow = _view_of(q_out, "q_out", shape, dt, self.device)
         self._run(self.L.sjd_kv_write, (self.ctx, at, span, _DTYPES[dt], kw, vw, rope_c, pos, qw, ow),
-                  (*layer._t, k, v, table, start, count, positions, q, q_out, turns, axis))
+                  (*layer._t, k, v, table, start, count, positions, q, q_out))
+        if rope is not None:
+            rope._used_on(self._raw, lambda: self.stream)
         return q_out
 
     def read(self, layer, table, start, n, count=None, dtype=torch.bfloat16):

@@ -35,6 +35,35 @@ def test_a_rope_of_another_device_or_without_positions_is_refused():
     assert torch.equal(layer.k, before)
 
 
+def test_a_rope_may_go_while_its_last_call_runs():
+    """Tables made on one stream, used on another and given back: their memory
+    is not handed out before the call has read them."""
+    side = torch.cuda.Stream()
+    g = base.gen(1)
+    x = base.normal(g, 1, 64, 4, 64)
+    positions = torch.arange(64, dtype=torch.int32, device=DEV).view(1, 64, 1)
+    want = kv.Rope([0.1 * i for i in range(32)], [0] * 32).rotate(x, positions)
+    h = kv.KV(1, 4, 4, 64, 8, 16, 8, 64, torch.bfloat16, stream=side)
+    layer = h.new_layer()
+    table = torch.arange(8, dtype=torch.int32, device=DEV)[None]
+    start = torch.zeros(1, dtype=torch.int32, device=DEV)
+    big = torch.randn(4000, 4000, device=DEV)
+    torch.cuda.synchronize()
+    for call in ("rotate", "write"):
+        rope = kv.Rope([0.1 * i for i in range(32)], [0] * 32)
+        sizes = [(t.shape, t.dtype) for t in (rope._turns, rope._axis)]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                big = (big @ big).clamp(-1, 1)
+            y = rope.rotate(x, positions) if call == "rotate" else h.write(layer, x, x, table, start, rope=rope, positions=positions, q=x)
+        del rope
+        mine = [torch.zeros(shape, dtype=dtype, device=DEV) for shape, dtype in sizes for _ in range(4)]
+        torch.cuda.synchronize()
+        assert torch.equal(y, want), call
+        del mine
+
+
 # --- gradients ----------------------------------------------------------------
 
 def test_tensors_that_want_a_gradient_are_refused():
