@@ -501,7 +501,7 @@ int sjd_kv_init(const sjd_kv_config* cfg, void* workspace_dev, size_t ws_bytes, 
  * [kv_heads][head_dim] of dtype SJD_F32 or SJD_BF16. With an 8-bit cache
  * each vector x is held as codes c and a scale s = max|x| / M (M = 448 for
  * SJD_E4M3, 127 for SJD_S8), c = x / s rounded to nearest even, both in fp32
- * arithmetic; a vector with a NaN or an infinity gets scale NaN and codes 0
+ * arithmetic, and -M..M where s is subnormal and too coarse; a vector with a NaN or an infinity gets scale NaN and codes 0
  * (all of it reads as NaN), a vector of zeros scale 0. With SJD_BF16 values
  * are rounded to nearest even.
  * rope (NULL: none) turns the keys first, in fp32, and, where q is given,

@@ -114,6 +114,10 @@ __device__ __forceinline__ void quotients(float (&x)[4], float scale, float inve
   }
 }
 
+// A subnormal scale has few bits, and a quotient by it may pass the largest code (100 / 127
+// of the least number is that number: quotients up to 190).
+__device__ __forceinline__ float held(float x, float most) { return fminf(fmaxf(x, -most), most); }
+
 // CP chunks of a vector to a thread: chunk i * L + lane. Four sequences of
 // 8100 tokens, 16 heads of 96, f32 to s8, not rotated: 86 us, 5.8 TB/s (86 %
 // of the copy rate); 410 with one token to a block, one chunk to a thread and
@@ -226,8 +230,8 @@ __global__ void __launch_bounds__(kBlock) write_kernel(const WriteParams p, cons
         for (int i = 0; i < CP; ++i) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            u[i][j] = some ? __fdiv_rn(u[i][j], scale) : 0.0f;
-            w[i][j] = some ? __fdiv_rn(w[i][j], scale) : 0.0f;
+            u[i][j] = some ? held(__fdiv_rn(u[i][j], scale), Codes<KV>::kMost) : 0.0f;
+            w[i][j] = some ? held(__fdiv_rn(w[i][j], scale), Codes<KV>::kMost) : 0.0f;
           }
         }
       }

@@ -85,3 +85,28 @@ def test_tensors_that_want_a_gradient_are_refused():
         assert torch.equal(h.attend(layer, leaf(q), table, start), h.attend(layer, q, table, start))
         assert torch.equal(rope.rotate(leaf(q), positions), rope.rotate(q, positions))
         h.write(layer, leaf(x), leaf(x), table, start)
+
+
+# --- quantising vectors of subnormal numbers ----------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.float8_e4m3fn, torch.int8])
+def test_codes_of_subnormal_vectors_keep_their_signs(dtype):
+    """Scales below 2^-126 are rounded to few bits, and a quotient may pass
+    the largest code: it is held to it."""
+    D, tops = 16, list(range(100, 700, 7)) + [3000, 100000]
+    n = len(tops)
+    h, layer, table, start, g = base.make(1, 2, 2, D, dtype, 16, [0], n)
+    x = np.zeros((1, n, 2, D), dtype=np.float32)
+    for t, top in enumerate(tops):
+        for head in range(2):
+            x[0, t, head] = np.ldexp(np.float32(1.0), -149) * np.rint(np.linspace(-top, top, D)).astype(np.float32)
+    x[:, :, 1] *= -1.0
+    xs = torch.from_numpy(x).to(DEV)
+    h.write(layer, xs, xs, table, start)
+    got, _ = h.read(layer, table, start, n, dtype=torch.float32)
+    most = np.float32(base.MOST[dtype])
+    scale = np.abs(x).max(-1, keepdims=True) / most
+    y = np.clip(np.divide(x, scale, out=np.zeros_like(x), where=scale > 0), -most, most)
+    codes = np.rint(y) if dtype == torch.int8 else torch.from_numpy(y).to(dtype).float().numpy()
+    assert (np.abs(codes) == most).any()
+    np.testing.assert_array_equal(got.cpu().numpy(), (codes * scale).astype(np.float32))
