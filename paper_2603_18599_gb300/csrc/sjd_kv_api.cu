@@ -173,7 +173,9 @@ int sjd_kv_attend(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span
   if (!kv) return SJD_ERR_ARG;
   AttendParams p{};
   if (const char* why = cache_of(kv, layer, span, kv->cfg.max_new, &p.c)) return fail(kv, SJD_ERR_ARG, why);
-  if (!q || !q->data_dev || !aligned(q->data_dev, 16) || q->batch_stride % 8 || q->token_stride % 8 || q->head_stride % 8)
+  // (the stride of a dimension of one element means nothing)
+  if (!q || !q->data_dev || !aligned(q->data_dev, 16) || (kv->cfg.batch > 1 && q->batch_stride % 8) ||
+      (span->n > 1 && q->token_stride % 8) || (kv->cfg.heads > 1 && q->head_stride % 8))
     return fail(kv, SJD_ERR_ARG, "queries must have 16-byte aligned rows");
   if (mask_kind != SJD_MASK_CAUSAL && mask_kind != SJD_MASK_ALL && mask_kind != SJD_MASK_GIVEN)
     return fail(kv, SJD_ERR_ARG, "unknown mask kind");

@@ -110,3 +110,18 @@ def test_codes_of_subnormal_vectors_keep_their_signs(dtype):
     codes = np.rint(y) if dtype == torch.int8 else torch.from_numpy(y).to(dtype).float().numpy()
     assert (np.abs(codes) == most).any()
     np.testing.assert_array_equal(got.cpu().numpy(), (codes * scale).astype(np.float32))
+
+
+# --- strides ------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", base.TYPES)
+def test_strides_of_dimensions_of_one_element_mean_nothing(dtype):
+    for B, n, heads in ((1, 1, 4), (1, 3, 1), (2, 1, 1), (1, 1, 1)):
+        starts = [37, 60][:B]
+        h, layer, table, start, g = base.make(B, heads, 1, 64, dtype, 16, starts, n)
+        base.filled(h, layer, table, starts, n, g)
+        q = base.normal(g, B, n, heads, 64).bfloat16()
+        want = h.attend(layer, q, table, start)
+        strides = [s if m > 1 else s + 3 for m, s in zip(q.shape, q.stride())]
+        odd = torch.as_strided(q, q.shape, strides)
+        assert torch.equal(h.attend(layer, odd, table, start), want)
