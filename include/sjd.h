@@ -529,6 +529,7 @@ int sjd_kv_read(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span, 
  * already, over tokens 0 .. start[b] + count[b] - 1:
  *   o = sum_j p_j v_j,  p = softmax_j(scale * q . k_j) over the keys seen,
  *   lse = ln sum_j exp(scale * q . k_j).
+ * scale: at most 2^127 in magnitude, 0 and negative ones among them.
  * q [batch][n][heads][head_dim] in bf16, 16-byte aligned rows; o_dev
  * [batch][n][heads][head_dim] in bf16, contiguous; lse_dev fp32 [batch][n]
  * [heads], or NULL. Scores and sums are fp32. The weights are rounded to 16

@@ -1006,7 +1006,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
         float top = -INFINITY;
         if (KV != SJD_BF16 && u == 0) {
           row_unit = __uint_as_float(static_cast<uint32_t>(127 + m->exponents[w.piece & 1][(NM == 2 ? slot * kTile : 0) + row]) << 23);
-          c_row = fmaxf(c * row_unit, 1e-37f);
+          c_row = fminf(fmaxf(c * row_unit, 1e-37f), FLT_MAX);
         }
         uint32_t s[2][32];
         tmem_load32(s_at, s[0]);
@@ -1290,7 +1290,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
         float top = -INFINITY;
         if (KV != SJD_BF16 && u == 0) {
           row_unit = __uint_as_float(static_cast<uint32_t>(127 + m->exponents[w.piece & 1][at]) << 23);
-          c_row = fmaxf(c * row_unit, 1e-37f);
+          c_row = fminf(fmaxf(c * row_unit, 1e-37f), FLT_MAX);
         }
         const float* fk = m->row[slot][0] + copy * kKeys;
         const float* fv = m->row[slot][1] + copy * kKeys;

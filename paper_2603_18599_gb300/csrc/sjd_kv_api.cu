@@ -180,7 +180,8 @@ int sjd_kv_attend(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span
   if (mask_kind != SJD_MASK_CAUSAL && mask_kind != SJD_MASK_ALL && mask_kind != SJD_MASK_GIVEN)
     return fail(kv, SJD_ERR_ARG, "unknown mask kind");
   if ((mask_kind == SJD_MASK_GIVEN) != (mask != nullptr)) return fail(kv, SJD_ERR_ARG, "mask_dev goes with SJD_MASK_GIVEN");
-  if (!std::isfinite(scale)) return fail(kv, SJD_ERR_ARG, "scale must be finite");
+  // (the kernel's factor, |scale| log2 e, is to be a number)
+  if (!(std::fabs(scale) <= 0x1p127f)) return fail(kv, SJD_ERR_ARG, "scale must be finite and at most 2^127");
   if (!o || !aligned(o, 16) || !aligned(lse, 4)) return fail(kv, SJD_ERR_ARG, "output is NULL or not aligned");
   p.q = view_of(q);
   p.mask_kind = mask_kind;

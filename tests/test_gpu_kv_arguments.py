@@ -125,3 +125,50 @@ def test_strides_of_dimensions_of_one_element_mean_nothing(dtype):
         strides = [s if m > 1 else s + 3 for m, s in zip(q.shape, q.stride())]
         odd = torch.as_strided(q, q.shape, strides)
         assert torch.equal(h.attend(layer, odd, table, start), want)
+
+
+# --- scales of the scores -----------------------------------------------------
+
+@pytest.mark.parametrize("dtype", base.TYPES)
+@pytest.mark.parametrize("heads,n", [(2, 3), (2, 40), (8, 30), (4, 200)])
+def test_scales_next_to_the_largest_number(dtype, heads, n):
+    """1.5e38 with queries as small: as 1 with queries of their usual size. A
+    scale whose product with log2(e) is no fp32 number is refused."""
+    starts = [300]
+    h, layer, table, start, g = base.make(1, heads, 2, 64, dtype, 16, starts, n)
+    base.filled(h, layer, table, starts, n, g)
+    q = base.normal(g, 1, n, heads, 64).bfloat16()
+    up = 2.0 ** 126
+    want, want_lse = h.attend(layer, q, table, start, scale=0.125, lse=True)
+    small = (q.double() * 2.0 ** -100).bfloat16()
+    o, lse = h.attend(layer, small, table, start, scale=0.125 * 2.0 ** 100, lse=True)
+    assert torch.equal(o, want) and (lse - want_lse).abs().max() <= 1e-4
+    o = h.attend(layer, (q.double() * 2.0 ** -40).bfloat16(), table, start, scale=up)
+    assert o.isfinite().all()
+    for scale in (3e38, -3e38):
+        with pytest.raises(sjd.SJDError) as e:
+            h.attend(layer, q, table, start, scale=scale)
+        assert e.value.code == sjd.SJD_ERR_ARG
+
+
+@pytest.mark.parametrize("dtype", base.TYPES)
+@pytest.mark.parametrize("heads,n", [(2, 3), (2, 40), (8, 30), (4, 200)])
+def test_scaled_scores_past_the_largest_number(dtype, heads, n):
+    """Scores that are numbers and whose product with the scale is none: the
+    weight is on the largest, here a key that the query points to."""
+    D, context = 64, 300
+    h, layer, table, start, g = base.make(1, heads, 2, D, dtype, 16, [context], n)
+    base.filled(h, layer, table, [context], n, g)
+    whole = kv.KV(1, heads, 2, D, h.cfg.n_pages, 16, h.cfg.max_pages, context + n, dtype)
+    k, v = whole.read(kv.Layer(*layer._t), table, torch.zeros_like(start), context + n, dtype=torch.float32)
+    score = torch.einsum("thd,shd->hts", k[0], k[0])
+    at = torch.randint(0, context, (n, heads), device=DEV, generator=g)
+    head = torch.arange(heads, device=DEV) * 2 // heads
+    q = (k[0, at, head] * 1e25).bfloat16()[None].contiguous()
+    o = h.attend(layer, q, table, start, scale=1e15)
+    best = score[head[None, :].expand(n, -1), at].topk(2, -1)         # [n, heads, 2]: a key that wins by far
+    some = (best.indices[..., 0] == at) & (best.values[..., 1] < 0.9 * best.values[..., 0])
+    assert some.float().mean() > 0.8
+    assert o.isfinite().all()
+    off = (o[0].float() - v[0, at, head]).abs() - 2.0 ** -7 * v[0, at, head].abs() - 1e-6
+    assert (off[some] <= 0).all()
