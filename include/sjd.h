@@ -415,7 +415,9 @@ void sjd_destroy(sjd_ctx* ctx);
  * sequence b, count[b] <= n (count_dev NULL: n of them in all sequences). A
  * span that does not fit its sequence's table (max_pages * page_size tokens)
  * is taken as empty, a page outside [0, n_pages) as zeros (reads) or not at
- * all (writes), and SJD_ERR_PAGE is latched for sjd_kv_sync. */
+ * all (writes), and SJD_ERR_PAGE is latched for sjd_kv_sync. The bounds-checked
+ * build also tests what the kernels make of these, and the rotary axes, and latches
+ * SJD_ERR_BOUNDS (sjd_rotate has no handle to latch it in: it only clamps). */
 
 typedef struct {
   int32_t batch;                 /* sequences: an image's conditional and
@@ -467,7 +469,8 @@ typedef struct {
  * elements 2i and 2i + 1 (interleaved) or i and pairs + i. */
 typedef struct {
   const uint64_t* turns_dev;     /* [pairs]                                    */
-  const int32_t* axis_dev;       /* [pairs], each in [0, axes)                 */
+  const int32_t* axis_dev;       /* [pairs], each in [0, axes): not looked at
+                                    but in the bounds-checked build           */
   int32_t pairs;                 /* a multiple of 4, at most head_dim / 2      */
   int32_t axes;                  /* 1..8                                       */
   int32_t interleaved;

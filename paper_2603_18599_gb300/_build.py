@@ -19,9 +19,7 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "_build")
 LIB = os.path.join(OUT, "libsjd.so")
 LIB_CHECKED = os.path.join(OUT, "libsjd_checked.so")
-SOURCES = ["sjd_kernels.cu", "sjd_fast.cu", "sjd_api.cu", "sjd_noalloc.cu"]
-# units without checks to build in: both libraries take the same objects
-SHARED = ["sjd_kv.cu", "sjd_attend.cu", "sjd_kv_api.cu"]
+SOURCES = ["sjd_kernels.cu", "sjd_fast.cu", "sjd_api.cu", "sjd_noalloc.cu", "sjd_kv.cu", "sjd_attend.cu", "sjd_kv_api.cu"]
 # the fast row kernels: sjd_fast_part.cu once per (dtype, mode) pair
 FAST_PARTS = [(dt, mode) for dt in ("SJD_BF16", "SJD_F32") for mode in ("kModeVerify", "kModeStep", "kModeTree", "kModeFromLogits")]
 ARCH = "-gencode=arch=compute_103a,code=sm_103a"
@@ -60,15 +58,14 @@ def build(verbose=False, extra_flags=()):
                "sjd_fast_%s_%s" % (dt[4:].lower(), mode[5:].lower())) for dt, mode in FAST_PARTS]
     jobs = [(src, "", defs, name) for src, defs, name in units]
     jobs += [(src, "checked", defs + ["-DSJD_CHECKS"], name) for src, defs, name in units]
-    jobs += [(src, "", [], os.path.splitext(src)[0]) for src in SHARED]
     # the longest units first
-    order = sorted(range(len(jobs)), key=lambda i: jobs[i][0] != "sjd_fast_part.cu")
+    order = sorted(range(len(jobs)), key=lambda i: jobs[i][0] not in ("sjd_attend.cu", "sjd_fast_part.cu"))
     with ThreadPoolExecutor(min(len(jobs), max(4, os.cpu_count() or 4))) as ex:
         done = dict(zip(order, ex.map(one, [jobs[i] for i in order])))
     objs = [done[i] for i in range(len(jobs))]
-    for lib, part in ((LIB, objs[:len(units)]), (LIB_CHECKED, objs[len(units):2 * len(units)])):
+    for lib, part in ((LIB, objs[:len(units)]), (LIB_CHECKED, objs[len(units):])):
         tmp = lib + ".tmp"
-        cmd = [cc, ARCH, "-shared", "-o", tmp, *part, *objs[2 * len(units):]]
+        cmd = [cc, ARCH, "-shared", "-o", tmp, *part]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError("link failed:\n%s\n%s" % (" ".join(cmd), r.stderr))

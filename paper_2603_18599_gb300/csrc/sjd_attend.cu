@@ -111,6 +111,15 @@ struct Shared {
   int done;  // of an item that its blocks join themselves: parts that are there (0 between calls)
 };
 
+// A row of the call's result (token, head); and a row of a block's part of an item.
+__device__ __forceinline__ long long row_index(const AttendParams& p, long long row) {
+  return SJD_KV_IDX(p.c.status, row, static_cast<long long>(p.c.B) * p.c.n * p.c.Hq);
+}
+template <int NM>
+__device__ __forceinline__ long long part_index(const AttendParams& p, long long part, int row) {
+  return SJD_KV_IDX(p.c.status, part * (kTile * NM) + row, 2ll * gridDim.x * (kTile * NM));
+}
+
 // An item's position and its keys.
 struct Item {
   int kvh, b, mt;       // key head, sequence, tile of 128 NM rows
@@ -1155,7 +1164,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
           for (int j = 0; j < 32; ++j) o[j] = with[j];
         }
         if (valid && wholly) {
-          __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.o) + head * p.c.D + column;
+          __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.o) + row_index(p, head) * p.c.D + column;
 #pragma unroll
           for (int j = 0; j < 32; j += 8)
             if (column + j < p.c.D)
@@ -1163,16 +1172,16 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
                   make_uint4(pack_bf16(o[j] * inverse, o[j + 1] * inverse), pack_bf16(o[j + 2] * inverse, o[j + 3] * inverse),
                              pack_bf16(o[j + 4] * inverse, o[j + 5] * inverse), pack_bf16(o[j + 6] * inverse, o[j + 7] * inverse));
         } else if (valid) {
-          float* to = parts + (part * (kTile * NM) + (NM == 2 ? slot * kTile : 0) + row) * DP + column;
+          float* to = parts + part_index<NM>(p, part, (NM == 2 ? slot * kTile : 0) + row) * DP + column;
 #pragma unroll
           for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
         }
       }
       if (valid && (NM == 2 || slot == 0)) {
         if (wholly) {
-          if (p.lse) p.lse[head] = log_of_sum(p, ref, sum);
+          if (p.lse) p.lse[row_index(p, head)] = log_of_sum(p, ref, sum);
         } else {
-          part_rows[part * (kTile * NM) + (NM == 2 ? slot * kTile : 0) + row] = make_float2(ref, sum);
+          part_rows[part_index<NM>(p, part, (NM == 2 ? slot * kTile : 0) + row)] = make_float2(ref, sum);
         }
       }
     }
@@ -1202,8 +1211,8 @@ __device__ __forceinline__ void clear_rows(const AttendParams& p, int row0, int 
     const long long begin = (static_cast<long long>(b) * p.c.n + span.y) * p.c.Hq, end = (b + 1ll) * p.c.n * p.c.Hq;
     for (long long row = begin + row0; row < end; row += step) {
       for (int i = lane; i < p.c.D / 8; i += 32)
-        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.o) + row * p.c.D + 8 * i) = make_uint4(0, 0, 0, 0);
-      if (p.lse && lane == 0) p.lse[row] = -INFINITY;
+        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.o) + row_index(p, row) * p.c.D + 8 * i) = make_uint4(0, 0, 0, 0);
+      if (p.lse && lane == 0) p.lse[row_index(p, row)] = -INFINITY;
     }
   }
 }
@@ -1481,12 +1490,12 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
         if (wholly) {
           const float inverse = some ? 1.0f / all : 0.0f;
           if (col < p.c.D)
-            *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.o) + head * p.c.D + col) =
+            *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.o) + row_index(p, head) * p.c.D + col) =
                 make_uint2(pack_bf16(o[0] * inverse, o[1] * inverse), pack_bf16(o[2] * inverse, o[3] * inverse));
-          if (p.lse && col == 0) p.lse[head] = log_of_sum(p, top, all);
+          if (p.lse && col == 0) p.lse[row_index(p, head)] = log_of_sum(p, top, all);
         } else {
-          *reinterpret_cast<float4*>(parts + (part * kTile + r) * DP + col) = make_float4(o[0], o[1], o[2], o[3]);
-          if (col == 0) part_rows[part * kTile + r] = make_float2(top, all);
+          *reinterpret_cast<float4*>(parts + part_index<1>(p, part, r) * DP + col) = make_float4(o[0], o[1], o[2], o[3]);
+          if (col == 0) part_rows[part_index<1>(p, part, r)] = make_float2(top, all);
         }
       }
       named_barrier(1, 256);
@@ -1494,7 +1503,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
     tc_fence_before();
     if (!wholly) {
       const long long begin = m->start.tile + tile_no - w.k0, end = begin + it.tiles - 1, per = m->start.per;
-      const int first = static_cast<int>(begin / per), count = static_cast<int>(end / per) - first + 1;
+      const int first = static_cast<int>(SJD_KV_IDX(p.c.status, begin / per, gridDim.x)), count = static_cast<int>(end / per) - first + 1;
       if (!join_here) {
         if (threadIdx.x == 0 && w.k0 == 0) shared[blockIdx.x] = {count, it.kvh, it.b, it.mt, 0};
       } else {
@@ -1510,7 +1519,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
         if (m->last) {
           // every part's factor, and each row's sum in the place after them
           float* factor = reinterpret_cast<float*>(queries);
-          auto part_at = [&](int k, int r) { return (2ll * (first + k) + (k == 0 ? 1 : 0)) * kTile + r; };
+          auto part_at = [&](int k, int r) { return part_index<1>(p, 2ll * (first + k) + (k == 0 ? 1 : 0), r); };
           const int rows = it.rows;
           for (int r = threadIdx.x / 32; r < rows; r += 8) {
             const float2 rs = lane < count ? __ldcg(&part_rows[part_at(lane, r)]) : make_float2(-INFINITY, 0.0f);
@@ -1524,7 +1533,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
             if (p.lse && lane == 0) {
               const int its_t = by_group(p.c, r);
               const long long head = (static_cast<long long>(it.b) * p.c.n + its_t) * p.c.Hq + static_cast<long long>(it.kvh) * G + r - its_t * G;
-              p.lse[head] = log_of_sum(p, top, all);
+              p.lse[row_index(p, head)] = log_of_sum(p, top, all);
             }
           }
           named_barrier(1, 256);
@@ -1541,7 +1550,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
             const int its_t = by_group(p.c, r);
             const long long head = (static_cast<long long>(it.b) * p.c.n + its_t) * p.c.Hq + static_cast<long long>(it.kvh) * G + r - its_t * G;
             if (col < p.c.D)
-              *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.o) + head * p.c.D + col) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
+              *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.o) + row_index(p, head) * p.c.D + col) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
           }
           named_barrier(1, 256);  // (the queries' memory is used no more)
         }
@@ -1628,7 +1637,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const AttendParam
     for (int row = row0; row < rows_per_item; row += step) {
       const int r = s.mt * rows_per_item + row;
       if (r >= span.y * G) break;
-      auto part_at = [&](int i) { return (2ll * (blockIdx.x + i) + (i == 0 ? 1 : 0)) * rows_per_item + row; };
+      auto part_at = [&](int i) {
+        return static_cast<long long>(SJD_KV_IDX(p.c.status, (2ll * (blockIdx.x + i) + (i == 0 ? 1 : 0)) * rows_per_item + row, 2ll * gridDim.x * rows_per_item));
+      };
       float top = -INFINITY;
       for (int i = lane; i < s.parts; i += 32) top = fmaxf(top, part_rows[part_at(i)].x);
       for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -1650,12 +1661,12 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const AttendParam
       const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
       const int t = by_group(p.c, r), g = r - t * G;
       const long long head = (static_cast<long long>(s.b) * p.c.n + t) * p.c.Hq + static_cast<long long>(s.kvh) * G + g;
-      __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.o) + head * p.c.D + lane * (DP / 32);
+      __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.o) + row_index(p, head) * p.c.D + lane * (DP / 32);
       if (lane * (DP / 32) < p.c.D) {
 #pragma unroll
         for (int j = 0; j < DP / 32; j += 2) *reinterpret_cast<uint32_t*>(to + j) = pack_bf16(o[j] * inverse, o[j + 1] * inverse);
       }
-      if (p.lse && lane == 0) p.lse[head] = log_of_sum(p, top, sum);
+      if (p.lse && lane == 0) p.lse[row_index(p, head)] = log_of_sum(p, top, sum);
     }
   }
   clear_rows(p, row0, step, lane);

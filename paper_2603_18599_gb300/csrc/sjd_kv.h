@@ -1,5 +1,5 @@
 // Shared by the window forward's operators: what a call gives the kernels
-// (sjd_rope.cu, sjd_kv.cu, sjd_attend.cu) and their launch entry points.
+// (sjd_kv.cu, sjd_attend.cu) and their launch entry points.
 #pragma once
 
 #include <cstddef>
@@ -46,6 +46,7 @@ struct Rope {
   const int32_t* axis;
   const int32_t* positions;
   int pairs, axes, interleaved, inverse;
+  uint32_t* status;  // NULL: a call without a handle
 };
 
 struct RotateParams {

@@ -53,8 +53,8 @@ const char* bad_rope(const sjd_rope* r, int dim) {
   return nullptr;
 }
 
-Rope rope_of(const sjd_rope* r, const int32_t* positions, int inverse) {
-  return {r->turns_dev, r->axis_dev, positions, r->pairs, r->axes, r->interleaved, inverse};
+Rope rope_of(const sjd_rope* r, const int32_t* positions, int inverse, uint32_t* status) {
+  return {r->turns_dev, r->axis_dev, positions, r->pairs, r->axes, r->interleaved, inverse, status};
 }
 
 View view_of(const sjd_view* v) { return {v->data_dev, v->batch_stride, v->token_stride, v->head_stride}; }
@@ -103,7 +103,7 @@ int sjd_rotate(const sjd_rope* rope, const sjd_view* x, const sjd_view* y, const
   if (dim < 8 || dim > kMaxRotateDim || dim % 8 || (dtype != SJD_F32 && dtype != SJD_BF16)) return SJD_ERR_ARG;
   if ((inverse != 0 && inverse != 1) || bad_rope(rope, dim)) return SJD_ERR_ARG;
   if (!aligned(x->data_dev, size_of(dtype)) || !aligned(y->data_dev, size_of(dtype))) return SJD_ERR_ARG;
-  const RotateParams p{rope_of(rope, positions, inverse), view_of(x), view_of(y), batch, n, heads, dim};
+  const RotateParams p{rope_of(rope, positions, inverse, nullptr), view_of(x), view_of(y), batch, n, heads, dim};
   return launch_rotate(p, dtype, static_cast<cudaStream_t>(stream)) == cudaSuccess ? SJD_OK : SJD_ERR_CUDA;
 }
 
@@ -143,7 +143,7 @@ int sjd_kv_write(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span,
   if (rope) {
     if (const char* why = bad_rope(rope, kv->cfg.head_dim)) return fail(kv, SJD_ERR_ARG, why);
     if (!positions) return fail(kv, SJD_ERR_ARG, "positions are NULL");
-    p.rope = rope_of(rope, positions, 0);
+    p.rope = rope_of(rope, positions, 0, reinterpret_cast<uint32_t*>(kv->ws));
   }
   if ((q != nullptr) != (q_out != nullptr) || (q && !rope)) return fail(kv, SJD_ERR_ARG, "queries come with rope and q_out");
   if (q) {
@@ -206,6 +206,7 @@ int sjd_kv_sync(sjd_kv* kv) {
   }
   if (e != cudaSuccess) return launched(kv, e, "sync");
   if (bits & status_bit(SJD_ERR_TIMEOUT)) return fail(kv, SJD_ERR_TIMEOUT, "a wait inside the attention kernel ran out");
+  if (bits & status_bit(SJD_ERR_BOUNDS)) return fail(kv, SJD_ERR_BOUNDS, "an index outside its array (bounds-checked build); the access was clamped");
   if (bits & status_bit(SJD_ERR_PAGE)) return fail(kv, SJD_ERR_PAGE, "a span outside its page table, or a page outside the cache");
   return SJD_OK;
 }

@@ -18,6 +18,22 @@ namespace sjd_kv_ops {
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// Bounds-checked build (compiled with SJD_CHECKS): an index of a page table, of
+// the cache's vectors, of the rotary axes, of the rows of a call and of the parts that blocks
+// leave for one another is tested against its array's length; one outside latches
+// SJD_ERR_BOUNDS in the status word (where there is one) and is clamped. Without
+// SJD_CHECKS the macro is the index itself.
+#ifdef SJD_CHECKS
+__device__ __forceinline__ long long checked_index(uint32_t* status, long long i, long long n) {
+  if (i >= 0 && i < n) return i;
+  if (status) atomicOr(status, status_bit(SJD_ERR_BOUNDS));
+  return i < 0 ? 0 : n - 1;
+}
+#define SJD_KV_IDX(status, i, n) checked_index((status), (i), (n))
+#else
+#define SJD_KV_IDX(status, i, n) (i)
+#endif
+
 // Sequence b's span of the call, {0, 0} where it does not fit its table.
 __device__ __forceinline__ int2 span_of(const Cache& c, int b) {
   const int start = c.start[b], count = c.count ? c.count[b] : c.n;
@@ -41,7 +57,7 @@ __host__ __device__ __forceinline__ int by_group(const Cache& c, int x) { return
 
 // The table's entry of token pos of sequence b, as it stands there.
 __device__ __forceinline__ int page_of(const Cache& c, int b, int pos) {
-  return c.table[static_cast<long long>(b) * c.max_pages + entry_of(c, pos)];
+  return c.table[static_cast<long long>(b) * c.max_pages + SJD_KV_IDX(c.status, entry_of(c, pos), c.max_pages)];
 }
 // Token pos's vector of head h, or none where the page is no page of the cache.
 __device__ __forceinline__ uint32_t vector_in(const Cache& c, int page, int pos, int h) {
@@ -49,7 +65,8 @@ __device__ __forceinline__ uint32_t vector_in(const Cache& c, int page, int pos,
     if (page != kNoPage) atomicOr(c.status, status_bit(SJD_ERR_PAGE));
     return kNoVector;
   }
-  return (static_cast<uint32_t>(page) * c.Hkv + h) * c.ps + (pos - entry_of(c, pos) * c.ps);
+  return static_cast<uint32_t>(SJD_KV_IDX(c.status, (static_cast<uint32_t>(page) * c.Hkv + h) * c.ps + (pos - entry_of(c, pos) * c.ps),
+                                          static_cast<long long>(c.n_pages) * c.Hkv * c.ps));
 }
 
 constexpr int kTile = 128;              // rows of an attention's product, and keys of a tile
@@ -121,7 +138,7 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, bool wide, const float 
 // too large. Its top 32 bits, as a signed fraction f of half turns in [-1,
 // 1), go to sincospi: the rounding to fp32 keeps 24 bits of f.
 __device__ __forceinline__ float2 turn_of(const Rope& r, const int32_t* positions, int i) {
-  const unsigned long long t = static_cast<unsigned long long>(static_cast<long long>(positions[r.axis[i]])) * r.turns[i];
+  const unsigned long long t = static_cast<unsigned long long>(static_cast<long long>(positions[SJD_KV_IDX(r.status, r.axis[i], r.axes)])) * r.turns[i];
   const float f = static_cast<float>(static_cast<int32_t>(t >> 32)) * 4.656612873077393e-10f;  // 2^-31
   float sn, cs;
   sincospif(f, &sn, &cs);
