@@ -323,10 +323,10 @@ __global__ void __launch_bounds__(kBlock) read_kernel(const ReadParams p, const 
   }
 }
 
-// Tokens of a block: as many as leave every SM four blocks, at most kTokens (32 windows of
+// Tokens of a block: as many as leave each of `sms` SMs four blocks, at most kTokens (32 windows of
 // 64 rotated and written: 18.1 us; 19.6 where eight or sixteen are left).
-Share share_of(int B, int n, int dim, int vectors) {
-  const long long tokens = static_cast<long long>(B) * n, fair = tokens / (152 * 4);
+Share share_of(int B, int n, int dim, int vectors, int sms) {
+  const long long tokens = static_cast<long long>(B) * n, fair = tokens / (4 * sms);
   const int per = static_cast<int>(fair < 1 ? 1 : fair < kTokens ? fair : kTokens);
   return {per, n, dim / 8, 0, divisor(n), divisor(dim / 8), divisor(vectors)};
 }
@@ -344,8 +344,8 @@ cudaError_t write_by(const WriteParams& p, const Share& share, int kv_dtype, cud
 // group without one (9 to 12 chunks: heads of 72 to 96. The images above: 86
 // us with three, 118 with two).
 template <typename T>
-cudaError_t write_of(const WriteParams& p, int kv_dtype, cudaStream_t s) {
-  Share share = share_of(p.c.B, p.c.n, p.c.D, (p.q.p ? p.c.Hq : 0) + 2 * p.c.Hkv);
+cudaError_t write_of(const WriteParams& p, int kv_dtype, int sms, cudaStream_t s) {
+  Share share = share_of(p.c.B, p.c.n, p.c.D, (p.q.p ? p.c.Hq : 0) + 2 * p.c.Hkv, sms);
   const int two = lanes_of((share.chunks + 1) / 2), three = lanes_of((share.chunks + 2) / 3);
   if (3 * three < 2 * two) {
     share.lanes = three;
@@ -356,8 +356,8 @@ cudaError_t write_of(const WriteParams& p, int kv_dtype, cudaStream_t s) {
 }
 
 template <typename T>
-cudaError_t read_of(const ReadParams& p, int kv_dtype, cudaStream_t s) {
-  const Share share = share_of(p.c.B, p.c.n, p.c.D, 2 * p.c.Hkv);
+cudaError_t read_of(const ReadParams& p, int kv_dtype, int sms, cudaStream_t s) {
+  const Share share = share_of(p.c.B, p.c.n, p.c.D, 2 * p.c.Hkv, sms);
   const unsigned blocks = blocks_of(share, p.c.B);
   if (kv_dtype == SJD_BF16) return launch_early(read_kernel<T, SJD_BF16>, blocks, kBlock, 0, s, p, share);
   if (kv_dtype == SJD_E4M3) return launch_early(read_kernel<T, SJD_E4M3>, blocks, kBlock, 0, s, p, share);
@@ -366,19 +366,19 @@ cudaError_t read_of(const ReadParams& p, int kv_dtype, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_rotate(const RotateParams& p, int dtype, cudaStream_t s) {
-  const Share share = share_of(p.B, p.n, p.D, p.H);
+cudaError_t launch_rotate(const RotateParams& p, int dtype, int sms, cudaStream_t s) {
+  const Share share = share_of(p.B, p.n, p.D, p.H, sms);
   const unsigned blocks = blocks_of(share, p.B);
   if (dtype == SJD_BF16) return launch_early(rotate_kernel<__nv_bfloat16>, blocks, kBlock, 0, s, p, share);
   return launch_early(rotate_kernel<float>, blocks, kBlock, 0, s, p, share);
 }
 
-cudaError_t launch_write(const WriteParams& p, int dtype, int kv_dtype, cudaStream_t s) {
-  return dtype == SJD_BF16 ? write_of<__nv_bfloat16>(p, kv_dtype, s) : write_of<float>(p, kv_dtype, s);
+cudaError_t launch_write(const WriteParams& p, int dtype, int kv_dtype, int sms, cudaStream_t s) {
+  return dtype == SJD_BF16 ? write_of<__nv_bfloat16>(p, kv_dtype, sms, s) : write_of<float>(p, kv_dtype, sms, s);
 }
 
-cudaError_t launch_read(const ReadParams& p, int dtype, int kv_dtype, cudaStream_t s) {
-  return dtype == SJD_BF16 ? read_of<__nv_bfloat16>(p, kv_dtype, s) : read_of<float>(p, kv_dtype, s);
+cudaError_t launch_read(const ReadParams& p, int dtype, int kv_dtype, int sms, cudaStream_t s) {
+  return dtype == SJD_BF16 ? read_of<__nv_bfloat16>(p, kv_dtype, sms, s) : read_of<float>(p, kv_dtype, sms, s);
 }
 
 }  // namespace sjd_kv_ops

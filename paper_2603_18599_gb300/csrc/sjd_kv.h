@@ -108,9 +108,9 @@ cudaError_t launch_early(void (*kernel)(Args...), dim3 grid, int threads, size_t
 }
 
 // kv_dtype of the cache: SJD_BF16, SJD_E4M3, SJD_S8; dtype of the caller's tensors: SJD_F32, SJD_BF16.
-cudaError_t launch_rotate(const RotateParams& p, int dtype, cudaStream_t s);
-cudaError_t launch_write(const WriteParams& p, int dtype, int kv_dtype, cudaStream_t s);
-cudaError_t launch_read(const ReadParams& p, int dtype, int kv_dtype, cudaStream_t s);
+cudaError_t launch_rotate(const RotateParams& p, int dtype, int sms, cudaStream_t s);
+cudaError_t launch_write(const WriteParams& p, int dtype, int kv_dtype, int sms, cudaStream_t s);
+cudaError_t launch_read(const ReadParams& p, int dtype, int kv_dtype, int sms, cudaStream_t s);
 // scratch: attend_scratch_bytes(head_dim, max_new * heads / kv_heads), 256-byte aligned.
 cudaError_t launch_attend(const AttendParams& p, int kv_dtype, int sms, unsigned char* scratch, cudaStream_t s);
 // Sets the kernels' limits on the current device, once for a handle.

@@ -43,6 +43,11 @@ int launched(sjd_kv* kv, cudaError_t e, const char* what) {
   return SJD_ERR_CUDA;
 }
 
+bool count_sms(int* sms) {  // of the current device
+  int device = 0;
+  return cudaGetDevice(&device) == cudaSuccess && cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, device) == cudaSuccess;
+}
+
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 const char* bad_rope(const sjd_rope* r, int dim) {
@@ -104,7 +109,9 @@ int sjd_rotate(const sjd_rope* rope, const sjd_view* x, const sjd_view* y, const
   if ((inverse != 0 && inverse != 1) || bad_rope(rope, dim)) return SJD_ERR_ARG;
   if (!aligned(x->data_dev, size_of(dtype)) || !aligned(y->data_dev, size_of(dtype))) return SJD_ERR_ARG;
   const RotateParams p{rope_of(rope, positions, inverse, nullptr), view_of(x), view_of(y), batch, n, heads, dim};
-  return launch_rotate(p, dtype, static_cast<cudaStream_t>(stream)) == cudaSuccess ? SJD_OK : SJD_ERR_CUDA;
+  int sms = 0;
+  if (!count_sms(&sms)) return SJD_ERR_CUDA;
+  return launch_rotate(p, dtype, sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? SJD_OK : SJD_ERR_CUDA;
 }
 
 size_t sjd_kv_workspace_size(const sjd_kv_config* cfg) {
@@ -118,9 +125,8 @@ int sjd_kv_init(const sjd_kv_config* cfg, void* workspace, size_t ws_bytes, void
   if (!valid(cfg) || !workspace || !aligned(workspace, kAlign)) return SJD_ERR_ARG;
   if (ws_bytes < sjd_kv_workspace_size(cfg)) return SJD_ERR_CAPACITY;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  int device = 0, sms = 0;
-  if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
-    return SJD_ERR_CUDA;
+  int sms = 0;
+  if (!count_sms(&sms)) return SJD_ERR_CUDA;
   if (prepare_attend(cfg->kv_dtype, cfg->head_dim) != cudaSuccess) return SJD_ERR_CUDA;
   if (cudaMemsetAsync(workspace, 0, kAlign + attend_counter_bytes(), s) != cudaSuccess) return SJD_ERR_CUDA;
   sjd_kv* kv = new (std::nothrow) sjd_kv{*cfg, static_cast<unsigned char*>(workspace), s, sms, ""};
@@ -152,7 +158,7 @@ int sjd_kv_write(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span,
     p.q = view_of(q);
     p.q_out = view_of(q_out);
   }
-  return launched(kv, launch_write(p, dtype, kv->cfg.kv_dtype, kv->stream), "write");
+  return launched(kv, launch_write(p, dtype, kv->cfg.kv_dtype, kv->sms, kv->stream), "write");
 }
 
 int sjd_kv_read(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span, int32_t dtype, void* k_out, void* v_out) {
@@ -165,7 +171,7 @@ int sjd_kv_read(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span, 
   if (static_cast<long long>(p.c.B) * p.c.n > 0x7fffffffLL) return fail(kv, SJD_ERR_ARG, "span: too many tokens");
   p.k_out = k_out;
   p.v_out = v_out;
-  return launched(kv, launch_read(p, dtype, kv->cfg.kv_dtype, kv->stream), "read");
+  return launched(kv, launch_read(p, dtype, kv->cfg.kv_dtype, kv->sms, kv->stream), "read");
 }
 
 int sjd_kv_attend(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span, const sjd_view* q, int32_t mask_kind,
