@@ -923,7 +923,6 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
   if (m->start.tiles <= 0) return;
   if (row == 0) w.begin(p, m->start);
   named_barrier(2 + slot, 128);
-  long long tile_no = 0;  // the block's number of the piece's first tile
   uint32_t sp = 0;
   for (;;) {
     const int r0 = it.mt * (kTile * NM) + (NM == 2 ? slot * kTile : 0);
@@ -1136,7 +1135,7 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     const int g = r0 + row - t * G;
     const long long head = token * p.c.Hq + static_cast<long long>(it.kvh) * G + g;
     if (active) {
-#pragma unroll
+#pragma unroll 1
       for (int i = 0; i < kColumns / 32; ++i) {
         const int column = column0 + 32 * i;
         __syncwarp();
@@ -1187,17 +1186,17 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
     }
     if (threadIdx.x == 0 && w.k0 == 0 && w.k1 < it.tiles) {
       // the rest of the item lies in the blocks after this one
-      const long long beyond = m->start.tile + tile_no + it.tiles - 1;
+      const long long beyond = m->start.tile + m->start.tiles - w.left + it.tiles - 1;
       shared[blockIdx.x] = {static_cast<int>(beyond / m->start.per - blockIdx.x + 1), it.kvh, it.b, it.mt, 0};
     }
-    tile_no += tiles;
+    const bool last = w.left <= tiles;
     if (NM == 1) {  // both groups have read both accumulators and the rows' sums
       tc_fence_before();
       named_barrier(1, 256);
     } else {
       named_barrier(2 + slot, 128);
     }
-    if (tile_no >= m->start.tiles) return;
+    if (last) return;
     if (row == 0) w.next(p);
     named_barrier(2 + slot, 128);
   }
@@ -1237,7 +1236,6 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
   if (m->start.tiles <= 0) return;
   if (at == 0) w.begin(p, m->start);
   named_barrier(2 + slot, 128);
-  long long tile_no = 0;
   uint32_t sp = 0;
   for (;;) {
     const bool valid = row < it.rows, active = (at & ~31) % kRows < it.rows;
@@ -1502,7 +1500,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
     }
     tc_fence_before();
     if (!wholly) {
-      const long long begin = m->start.tile + tile_no - w.k0, end = begin + it.tiles - 1, per = m->start.per;
+      const long long begin = m->start.tile + m->start.tiles - w.left - w.k0, end = begin + it.tiles - 1, per = m->start.per;
       const int first = static_cast<int>(SJD_KV_IDX(p.c.status, begin / per, gridDim.x)), count = static_cast<int>(end / per) - first + 1;
       if (!join_here) {
         if (threadIdx.x == 0 && w.k0 == 0) shared[blockIdx.x] = {count, it.kvh, it.b, it.mt, 0};
@@ -1557,9 +1555,9 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
       }
     }
     if (threadIdx.x == 0) mbar_arrive(smem_addr(&m->q_empty));  // the queries' memory is free again
-    tile_no += tiles;
+    const bool last = w.left <= tiles;
     named_barrier(2 + slot, 128);
-    if (tile_no >= m->start.tiles) return;
+    if (last) return;
     if (at == 0) w.next(p);
     named_barrier(2 + slot, 128);
   }
