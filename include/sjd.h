@@ -539,7 +539,8 @@ int sjd_kv_read(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span, 
  * bits before their product with the values: with a 16-bit cache to bf16, with
  * an 8-bit one times their values' scales to fp16, in units of a power of two
  * near the largest such product p_j s_j of the keys that the row sees. A
- * product below 2^-25 of that is lost, whatever the scales of other keys. The
+ * product below 2^-29 of that is lost, whatever the scales of other keys; a
+ * weight below 2^-126 of the row's largest may be taken as 0. The
  * queries are exact, but for an 8-bit cache those elements below 2^-15 of
  * their row's largest, which keep an error of 2^-25 of that. A row that sees no
  * key, and rows from count[b] on, give o = 0 and lse = -inf; a key that a row

@@ -59,11 +59,12 @@ constexpr uint32_t kTmemColumns = 512;  // S of the two slots (P over them), the
 constexpr uint32_t kOColumn = 2 * kTile;
 constexpr long long kWaitClocks = 4000000000ll;  // about two seconds
 constexpr float kLeast = 1e-30f;        // least factor of the scores
-constexpr int kRoom = 6;                // weights of an 8-bit cache are times 2^6: at most 2^(8 + 6), in fp16
+constexpr int kRoom = 10;               // weights of an 8-bit cache are times 2^10: at most 2^(4 + 10), in fp16
 constexpr float kNear = 64.0f;          // values' factors that share a unit lie within 2^6 of each other, and of 1
 constexpr float kUnits = 0x1p40f;       // within 2^40: see Unit
 constexpr float kFar = 0x1p20f;         // from here on a score's product with c is rounded too coarsely (2^-4)
-constexpr float kRise = 8.0f;           // a row's reference maximum moves when it is behind by more than 2^8
+template <int KV>
+constexpr float kRise = KV == SJD_BF16 ? 8.0f : 4.0f;  // a row's reference maximum moves when it is behind by more than 2^kRise
 
 __host__ __device__ constexpr uint32_t tile_bytes(int dp) { return static_cast<uint32_t>(kTile) * dp * 2; }
 
@@ -784,10 +785,10 @@ __device__ __forceinline__ void weights_of(const uint32_t (&s)[32], const float*
 // weight of 1 at least, and so the row's largest product is 1 / kNear of the unit
 // or more. Else (`wide`: a key's factor could be large, small or 0 where the
 // row's weight is not) each row has a unit of its own, near the largest product
-// p v among the keys that it sees. Either way the row's largest is 2^0 to 2^14
-// as fp16, and a product below 2^-25 of it is lost: less than the codes of the
+// p v among the keys that it sees. Either way the row's largest is 2^4 to 2^14
+// as fp16, and a product below 2^-29 of it is lost: less than the codes of the
 // largest resolve (2^-10 of its factor for e4m3, 2^-1 for s8; times codes of
-// up to 448 it is 2^-16).
+// up to 448 it is 2^-20).
 struct Unit {
   bool wide = false;
   float of = 0.0f;        // the unit; 0: no key yet. wide: its logarithm
@@ -833,7 +834,7 @@ __device__ __forceinline__ float take_factors(Unit& unit, ushort2 range, bool so
 // The reference moves to the tile's largest score, if that is far above it; returns by how much it was behind, as a power.
 __device__ __forceinline__ float wide_move(float top, float c, float& ref, float& sum, float& most) {
   float behind = 0.0f;
-  if ((top - ref) * c > kRise || (ref == -INFINITY && top != -INFINITY)) {
+  if ((top - ref) * c > kRise<SJD_E4M3> || (ref == -INFINITY && top != -INFINITY)) {
     if (ref != -INFINITY) behind = (ref - top) * c, sum *= exp2_fast(behind), most += behind;
     ref = top;
   }
@@ -850,8 +851,8 @@ __device__ __forceinline__ float wide_largest(uint32_t (&s)[32], const float* lo
   return most;
 }
 __device__ __forceinline__ float wide_unit(float of, float most) {
-  const bool turn = most > of + 8.0f || (most < of - 4.0f && most != -INFINITY);
-  return turn ? fminf(133.0f, fmaxf(-120.0f, ceilf(most))) : of;
+  const bool turn = most > of + 4.0f || (most < of - 4.0f && most != -INFINITY);
+  return turn ? fminf(133.0f, fmaxf(-116.0f, ceilf(most))) : of;
 }
 // The weights of 32 such powers, packed to 16 bits, and their sum.
 __device__ __forceinline__ float wide_weights_of(const uint32_t (&t)[32], const float* logs, float of, uint32_t (&out)[16]) {
@@ -1044,9 +1045,9 @@ __device__ __forceinline__ void softmax_rows(const AttendParams& p, Misc<NM>* m,
           }
         } else {
           // The reference that the weights are taken against moves only where a
-          // weight could pass 2^8: their relative precision is the same below
+          // weight could pass 2^kRise: their relative precision is the same below
           // that, and O is left alone.
-          const bool move = (top - ref) * c_row > kRise || (ref == -INFINITY && top != -INFINITY);
+          const bool move = (top - ref) * c_row > kRise<KV> || (ref == -INFINITY && top != -INFINITY);
           if (__any_sync(0xffffffffu, move || grown != 1.0f)) {
             float f = !move ? 1.0f : worth(ref, top, c_row);
             if (move) ref = top, sum *= f;
@@ -1343,7 +1344,7 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
             turn = behind != 0.0f || now != unit.of;
             unit.of = now;
           } else {
-            const bool move = (top - ref) * c_row > kRise || (ref == -INFINITY && top != -INFINITY);
+            const bool move = (top - ref) * c_row > kRise<KV> || (ref == -INFINITY && top != -INFINITY);
             turn = move || grown != 1.0f;
             if (move) f = worth(ref, top, c_row), ref = top, sum *= f;
             f *= grown;
