@@ -877,6 +877,7 @@ template <int DP>
 __device__ __noinline__ float4 wide_weights(uint32_t s_at, uint32_t w_at, uint32_t o_at, int chunks, const float* logs, float c, float top,
                                             bool some_o, float ref, float sum, float of, float most) {
   const float behind = wide_move(top, c, ref, sum, most);
+  __syncwarp();
   const float from = ref == -INFINITY ? 0.0f : ref;
   uint32_t s[32];
 #pragma unroll 1
@@ -1328,68 +1329,84 @@ __device__ __forceinline__ void softmax_copies(const AttendParams& p, Misc<1>* m
           top = largest_of(s, top);
         }
         if (kChunks > 1) tmem_wait_store();
-        if (KV != SJD_BF16 && kChunks > 1 && unit.wide) {
+        // (wide_weights' steps in place: with a call the other tiles lose registers too, 16 tokens
+        // over 32768 252 us instead of 209; 32 chunks of 64 rows over 8100 211 instead of 203)
+        const bool wide = KV != SJD_BF16 && unit.wide;
+        float f = 1.0f;
+        bool turn;
+        if (wide) {
+          const float behind = wide_move(top, c_row, ref, sum, unit.low);
           __syncwarp();
-          const float4 r = wide_weights<DP>(s_at + copy * kKeys, s_at + 16 * copy * kChunks, o_at, kChunks, fv, c_row, top, u > 0, ref, sum, unit.of, unit.low);
-          ref = r.x, sum = r.y, unit.of = r.z, unit.low = r.w;
-        } else {
-          const bool wide = KV != SJD_BF16 && kChunks == 1 && unit.wide;  // (a call's registers would cost every tile 30 %)
-          float f = 1.0f;
-          bool turn;
-          if (wide) {
-            const float behind = wide_move(top, c_row, ref, sum, unit.low);
-            unit.low = wide_largest(s, fv, ref == -INFINITY ? 0.0f : ref, c_row, unit.low);
-            const float now = wide_unit(unit.of, unit.low);
-            f = exp2_fast(behind + (unit.of - now));
-            turn = behind != 0.0f || now != unit.of;
-            unit.of = now;
-          } else {
-            const bool move = (top - ref) * c_row > kRise<KV> || (ref == -INFINITY && top != -INFINITY);
-            turn = move || grown != 1.0f;
-            if (move) f = worth(ref, top, c_row), ref = top, sum *= f;
-            f *= grown;
-          }
-          __syncwarp();
-          if (u > 0 && __any_sync(0xffffffffu, turn)) {
+          const float from = ref == -INFINITY ? 0.0f : ref;
 #pragma unroll 1
-            for (int i = 0; i < DP / 16; ++i) {
-              uint32_t o[16];
-              tmem_load16(o_at + 16 * i, o);
-              tmem_wait_load(o);
-#pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tmem_store16(o_at + 16 * i, o);
+          for (int i = 0; i < kChunks; ++i) {
+            if (kChunks > 1) {
+              tmem_load32(s_at + copy * kKeys + 32 * i, s);
+              tmem_wait_load(s);
             }
+            unit.low = wide_largest(s, fv + 32 * i, from, c_row, unit.low);
+            if (kChunks > 1) tmem_store32(s_at + copy * kKeys + 32 * i, s);
           }
+          if (kChunks > 1) tmem_wait_store();
+          const float now = wide_unit(unit.of, unit.low);
+          f = exp2_fast(behind + (unit.of - now));
+          turn = behind != 0.0f || now != unit.of;
+          unit.of = now;
+        } else {
+          const bool move = (top - ref) * c_row > kRise<KV> || (ref == -INFINITY && top != -INFINITY);
+          turn = move || grown != 1.0f;
+          if (move) f = worth(ref, top, c_row), ref = top, sum *= f;
+          f *= grown;
+        }
+        __syncwarp();
+        if (u > 0 && __any_sync(0xffffffffu, turn)) {
+#pragma unroll 1
+          for (int i = 0; i < DP / 16; ++i) {
+            uint32_t o[16];
+            tmem_load16(o_at + 16 * i, o);
+            tmem_wait_load(o);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+            tmem_store16(o_at + 16 * i, o);
+          }
+        }
+        if (wide) {
+#pragma unroll 1
+          for (int i = 0; i < kChunks; ++i) {
+            if (kChunks > 1) {
+              tmem_load32(s_at + copy * kKeys + 32 * i, s);
+              tmem_wait_load(s);
+            }
+            uint32_t out[16];
+            sum += wide_weights_of(s, fv + 32 * i, unit.of, out);
+            tmem_store16(s_at + 16 * (copy * kChunks + i), out);
+          }
+        } else {
           uint32_t out[kChunks][16];
-          if (wide) {
-            sum += wide_weights_of(s, fv, unit.of, out[0]);
-          } else {
-            const int shift = KV == SJD_BF16 ? 0 : static_cast<int>(__float_as_uint(unit.of) >> 23) - 127 - kRoom;
-            float base = ref == -INFINITY ? 0.0f : ref * c_row;
-            if (__any_sync(0xffffffffu, fabsf(base) > kFar)) {
-              if constexpr (kChunks == 1) {
-                const float from = ref == -INFINITY ? 0.0f : ref;
-                base = 0.0f;
+          const int shift = KV == SJD_BF16 ? 0 : static_cast<int>(__float_as_uint(unit.of) >> 23) - 127 - kRoom;
+          float base = ref == -INFINITY ? 0.0f : ref * c_row;
+          if (__any_sync(0xffffffffu, fabsf(base) > kFar)) {
+            if constexpr (kChunks == 1) {
+              const float from = ref == -INFINITY ? 0.0f : ref;
+              base = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) - from);
-              } else {
-                less_reference<kKeys>(s_at + copy * kKeys, ref, base);
-              }
+              for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) - from);
+            } else {
+              less_reference<kKeys>(s_at + copy * kKeys, ref, base);
             }
-            base += static_cast<float>(shift);
-            Pair total[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
-#pragma unroll
-            for (int i = 0; i < kChunks; ++i) {
-              if (kChunks > 1) {
-                tmem_load32(s_at + copy * kKeys + 32 * i, s);
-                tmem_wait_load(s);
-              }
-              weights_of<KV>(s, fv + 32 * i, c_row, base, out[i], total);
-            }
-            const float2 ends = halves(add2(total[0], total[1]));
-            sum += (ends.x + ends.y) * (KV == SJD_BF16 ? 1.0f : __uint_as_float(static_cast<uint32_t>(127 + shift) << 23));
           }
+          base += static_cast<float>(shift);
+          Pair total[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+#pragma unroll
+          for (int i = 0; i < kChunks; ++i) {
+            if (kChunks > 1) {
+              tmem_load32(s_at + copy * kKeys + 32 * i, s);
+              tmem_wait_load(s);
+            }
+            weights_of<KV>(s, fv + 32 * i, c_row, base, out[i], total);
+          }
+          const float2 ends = halves(add2(total[0], total[1]));
+          sum += (ends.x + ends.y) * (KV == SJD_BF16 ? 1.0f : __uint_as_float(static_cast<uint32_t>(127 + shift) << 23));
 #pragma unroll
           for (int i = 0; i < kChunks; ++i) tmem_store16(s_at + 16 * (copy * kChunks + i), out[i]);
         }
