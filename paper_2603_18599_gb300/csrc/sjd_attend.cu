@@ -816,9 +816,10 @@ __device__ __forceinline__ ushort2 joint(ushort2 a, ushort2 b) { return make_ush
 // Another tile's factors: makes the unit wide, or returns the old unit over the
 // new one. some: the row has seen keys.
 __device__ __forceinline__ float take_factors(Unit& unit, ushort2 range, bool some) {
+  const float least = __uint_as_float(static_cast<uint32_t>(range.x) << 16), most = __uint_as_float(static_cast<uint32_t>(range.y) << 16);
+  if (least >= unit.low && most <= unit.of) return 1.0f;
   // (the power of two from the largest on)
-  const float now = fmaxf(unit.of, __uint_as_float(((static_cast<uint32_t>(range.y) << 16) + 0x7fffffu) & 0x7f800000u));
-  const float low = fminf(unit.low, __uint_as_float(static_cast<uint32_t>(range.x) << 16));
+  const float now = fmaxf(unit.of, __uint_as_float((__float_as_uint(most) + 0x7fffffu) & 0x7f800000u)), low = fminf(unit.low, least);
   float grown = 1.0f;
   if (now <= kUnits && now >= 1.0f / kUnits && low * kNear >= now) {
     if (now != unit.of && unit.of > 0.0f) grown = unit.of / now;
