@@ -401,7 +401,8 @@ void sjd_destroy(sjd_ctx* ctx);
  * They have a handle of their own, sjd_kv, bound to a CUDA stream like
  * sjd_ctx; calls are asynchronous on that stream and share the handle's
  * workspace. The cache itself, one sjd_kv_layer per layer of the model, is
- * passed to each call.
+ * passed to each call. A call that is captured into a graph has to be on the
+ * capture's stream: make a handle with that stream for it.
  *
  * Layouts. Cache: k_dev and v_dev [n_pages][kv_heads][page_size][head_dim]
  * in kv_dtype, 16-byte aligned; with an 8-bit kv_dtype also k_scale_dev and v_scale_dev,
@@ -463,8 +464,9 @@ typedef struct {
 /* Rotary positions with several axes (a running position, an image's row
  * and column, ...): pair i of a vector is turned by the angle
  * positions[axis_dev[i]] * f_i. The frequencies are given as fractions of a
- * turn, turns_dev[i] = f_i / (2 pi) * 2^64 mod 2^64 (sjd_rope_turns), so
- * that the angle is reduced exactly, in integers, at any position. The first
+ * turn, turns_dev[i] = f_i / (2 pi) * 2^64 mod 2^64 (sjd_rope_turns, to 53
+ * bits of f_i / (2 pi)), so that their product with any position is reduced
+ * exactly, in integers. The first
  * 2 * pairs elements of a vector are turned and the others kept; pair i is
  * elements 2i and 2i + 1 (interleaved) or i and pairs + i. */
 typedef struct {
@@ -544,7 +546,9 @@ int sjd_kv_read(sjd_kv* kv, const sjd_kv_layer* layer, const sjd_kv_span* span, 
  * queries are exact, but for an 8-bit cache those elements below 2^-15 of
  * their row's largest, which keep an error of 2^-25 of that. A row that sees no
  * key, and rows from count[b] on, give o = 0 and lse = -inf; a key that a row
- * does not see has no effect on it, whatever it holds. The result does not
+ * does not see has no effect on it, whatever it holds (over an 8-bit cache the
+ * size of its values may decide which way the row's weights are rounded, within
+ * the bounds above). The result does not
  * depend on the GPU's timing: the same inputs give the same bits.
  * mask_dev (SJD_MASK_GIVEN): bytes, element (b, t, i) at mask_batch_stride *
  * b + mask_row_stride * t + i. Errors as sjd_kv_write, and SJD_ERR_TIMEOUT

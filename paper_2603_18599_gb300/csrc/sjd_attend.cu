@@ -32,16 +32,18 @@
 // the copies' accumulators are joined at the end like the slots'.
 //
 // What bounds it (one GB300): over a 16-bit cache few rows are bound by HBM (16
-// tokens of 64 heads over up to 32768 tokens, 8 key heads: 249 us, 98 % of the
-// copy rate); the same over e4m3 by what the loaders do for a tile (199 us, 63 %;
-// 197 without products and exponentials). A prompt of 4000 behind 4100 takes 376 us,
-// 1060 TFLOP/s or 55 % of a dense product's rate: a slot's softmax (1811
-// cycles of two slots' 128 x 128 scores), its products (1024 a slot) and the
-// hand-overs between them follow one another, and tensor memory has room for two
-// slots. 32 windows of 64 over 8100 in e4m3 take 342 us (31 %): the keys'
-// and values' factors make that softmax 2799 cycles (more where the values'
-// factors lie far apart: Unit). One token over 300: 13 to 15
-// us a call, which is the host's part.
+// tokens of 64 heads over up to 32768 tokens, 8 key heads: 253 us, 97 % of the
+// copy rate); the same over e4m3 by what the loaders do for a tile (212 us, 60 %;
+// of 214 in a loop of this call alone 199 stay without products and
+// exponentials). A prompt of 4000 behind 4100 takes 380 us, 1050 TFLOP/s or 54 %
+// of a dense product's rate: a tile of 256 rows takes 4400 cycles where its products
+// take 2048 and both slots' softmax, measured alone, 1811. A slot's softmax, its
+// products and the hand-overs between them follow one another, and the two slots
+// that tensor memory has room for overlap little. 32 windows of 64 over 8100 in e4m3
+// take 354 us (30 %): the keys' and values' factors make that softmax 2799 cycles
+// (measured alone, without the upkeep of the values' unit; more where the values'
+// factors lie far apart: Unit). One token over 300: 13 to 20 us a call, which is
+// the host's part.
 
 #include <cfloat>
 
@@ -73,9 +75,9 @@ __host__ __device__ constexpr uint32_t tile_bytes(int dp) { return static_cast<u
 //
 // Key and value tiles, and codes under way, as fit 227 KB. At a head of 128 and
 // 8 bits deeper rings of codes beat more tiles with few rows (16 tokens over 32768:
-// 185 us with one tile of each and four of codes, 205 with two tiles and two);
+// 212 us with one tile of each and four of codes, 231 with two tiles and two);
 // with 256 rows two key tiles let the next scores start (32 windows
-// of 64 over 8100: 343 us; 356 with two value tiles instead, 346 to 349 with one of
+// of 64 over 8100: 357 us; 361 with two value tiles instead, 357 with one of
 // each and three of codes).
 template <int KV, int DP, int NM>
 struct Plan {
@@ -870,10 +872,10 @@ __device__ __forceinline__ float wide_weights_of(const uint32_t (&t)[32], const 
 }
 
 // The weights of a tile's keys (32 `chunks` of them) that way, from the scores
-// at s_at to the 16-bit weights at w_at. Returns ref, sum, of and most. Three
-// exponentials' worth of work a score: 32 windows of 64 over 8100 in e4m3 take
-// 486 us where every tile comes this way, 359 where none does; 16 tokens over
-// 32768 (the same steps in registers) 234 and 205.
+// at s_at to the 16-bit weights at w_at. Returns ref, sum, of and most. Two
+// exponentials a score and a pass more over the scores: 32 windows of 64 over 8100 in
+// e4m3 take 488 us where every tile comes this way, 354 where none does; 16 tokens
+// over 32768 (the same steps in place) 241 and 212.
 template <int DP>
 __device__ __noinline__ float4 wide_weights(uint32_t s_at, uint32_t w_at, uint32_t o_at, int chunks, const float* logs, float c, float top,
                                             bool some_o, float ref, float sum, float of, float most) {
@@ -1711,8 +1713,8 @@ cudaError_t launch(const AttendParams& p, int sms, unsigned char* scratch, cudaS
 
 // 256 rows to an item share each tile that is loaded between two products;
 // fewer leave the tile's other rows idle, or to copies. 32 sequences over 8100, 8 key heads
-// of 128, by the rows of an item (bf16 / e4m3): 32 137 / 118 us, 64
-// 142 / 172, 128 149 / 202, 256 213 / 346; 132 rows, in an item of 256, 183 / 292.
+// of 128, by the rows of an item (bf16 / e4m3): 32 138 / 141 us, 64
+// 144 / 200, 128 146 / 204, 256 214 / 355; 132 rows, in an item of 256, 189 / 292.
 template <int KV, int DP>
 cudaError_t launch_of(const AttendParams& p, int sms, unsigned char* scratch, cudaStream_t s) {
   const long long rows = static_cast<long long>(p.c.n) * p.c.group;

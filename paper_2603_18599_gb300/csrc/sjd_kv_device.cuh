@@ -134,8 +134,9 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, bool wide, const float 
 
 // Cosine and sine of pair i at a position. The product of a position and a
 // fraction of a turn in units of 2^-64, modulo 2^64, is the angle's fraction
-// of a turn: exact to 2^-64 turns for each position, so that no position is
-// too large. Its top 32 bits, as a signed fraction f of half turns in [-1,
+// of a turn: the product is reduced exactly at any position. (The table holds a
+// frequency to 53 bits, so that the angle is off by up to 2^-52 of position times
+// frequency: 5e-7 turns at position 2^31 and a turn a position.) Its top 32 bits, as a signed fraction f of half turns in [-1,
 // 1), go to sincospi: the rounding to fp32 keeps 24 bits of f.
 __device__ __forceinline__ float2 turn_of(const Rope& r, const int32_t* positions, int i) {
   const unsigned long long t = static_cast<unsigned long long>(static_cast<long long>(positions[SJD_KV_IDX(r.status, r.axis[i], r.axes)])) * r.turns[i];

@@ -12,7 +12,9 @@ and attention of a chunk of new tokens over it. Argument marshalling only.
 
 Calls run on the handle's stream. Where that is not the caller's current
 stream, a call first waits for the current one, and the current one for the
-call, so that tensors may be made and used on either.
+call, so that tensors may be made and used on either. A capture cannot wait
+for a stream outside it: calls that are captured into a graph need a handle made with
+the capture's stream (KV(..., stream=side), torch.cuda.graph(..., stream=side)).
 
 No call records a gradient. A tensor that wants one is refused, unless
 gradients are off (torch.no_grad); a rotation's gradient is the rotation with
