@@ -121,7 +121,7 @@ class Rope:
         self._turns = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64, device=self.device)
         self._axis = torch.tensor(axis, dtype=torch.int32, device=self.device)
         self._c = _ROPE.pack(self._turns.data_ptr(), self._axis.data_ptr(), self.pairs, self.axes, self.interleaved)
-        self._made_on = _raw_stream(self.device.index)
+        self._streams = {_raw_stream(self.device.index)}   # that the allocator knows the tables to be used on
 
     @classmethod
     def sections(cls, pairs, theta=10000.0, shared=False, interleaved=False, device="cuda"):
@@ -138,7 +138,8 @@ class Rope:
     def _used_on(self, raw, stream):
         """The tables' memory is not handed out again before a call on another
         stream than the one they were made on has read them."""
-        if raw != self._made_on:
+        if raw not in self._streams:
+            self._streams.add(raw)
             self._turns.record_stream(stream())
             self._axis.record_stream(stream())
 
