@@ -853,6 +853,8 @@ __device__ __forceinline__ float wide_largest(uint32_t (&s)[32], const float* lo
   }
   return most;
 }
+// The unit moves where the largest product has left 2^-4 to 2^4 of it. (-116 to 133: O's factor,
+// 2^(of - kRoom), is a normal number, and no weight overflows at scales up to the largest number.)
 __device__ __forceinline__ float wide_unit(float of, float most) {
   const bool turn = most > of + 4.0f || (most < of - 4.0f && most != -INFINITY);
   return turn ? fminf(133.0f, fmaxf(-116.0f, ceilf(most))) : of;
