@@ -5,8 +5,8 @@ values are small or zero; and values near the ends of fp32's range.
 
 Tolerances, from the arithmetic that include/sjd.h declares for an 8-bit cache:
 - a weight times its value's scale is rounded to fp16, 2^-11 of it, or loses
-  at most 2^-25 of the row's largest such product where it is far below that:
-  2^-11 size + 2^-25 max(p s) sum |code|, both times 1.05 for what the fp32
+  at most 2^-29 of the row's largest such product where it is far below that:
+  2^-11 size + 2^-29 max(p s) sum |code|, both times 1.05 for what the fp32
   steps before add;
 - a result is rounded to bf16 once: half a unit, at most 2^-8 of the value;
   over many results 2^-9 / sqrt(3) of 1.4, the middle of an octave, at most in
@@ -60,7 +60,7 @@ def check(h, layer, q, table, starts, mask, got, lse, scale=None):
             p = torch.softmax(score, -1).nan_to_num(0.0)          # (a row that sees nothing)
             ps = p * vs[:, g]
             o, size = ps @ vc[:, g], ps @ vc[:, g].abs()
-            lost = 2.0 ** -25 * ps.amax(-1, keepdim=True) * (seen.double() @ vc[:, g].abs())
+            lost = 2.0 ** -29 * ps.amax(-1, keepdim=True) * (seen.double() @ vc[:, g].abs())
             wrong = 2.0 ** -17 * spread + 2e-6
             tol = 1.05 * (2.0 ** -11 * size + lost) + 2.0 ** -8 * o.abs() + 2 * wrong[:, None] * size
             mine = got[b, :, head].double()
