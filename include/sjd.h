@@ -568,6 +568,95 @@ const char* sjd_kv_last_error(const sjd_kv* kv);
 /* Free the host handle (workspace and cache stay the caller's). */
 void sjd_kv_destroy(sjd_kv* kv);
 
+/* ---------------------------------------------------------------------------
+ * The forward's operators on rows of features, around the attention: the
+ * embedding of tokens and its gradient, norms with a residual and their
+ * gradient, and matrix products of 8-bit integers with a scale for each token
+ * and each channel, with what quantises their rows (a norm can, on the way).
+ *
+ * They have no handle: a call is asynchronous on the stream that it is given,
+ * on the current device, and takes a workspace where it needs one (256-byte
+ * aligned; what is in it does not matter; in use until the call is done, and
+ * not shared with a call that may run at the same time). rows are tokens, of
+ * any sequences, up to 2^31 - 1. Features of a row are neighbours, the rows row_stride elements
+ * apart; accesses are widest where data, strides and the number of features
+ * are multiples of 16 bytes. Vectors of one value a feature, channel or row
+ * (gains, biases, scales) are contiguous fp32. dtype is SJD_F32 or
+ * SJD_BF16 throughout, sums are fp32, and a result is rounded once, to nearest
+ * even. Outputs do not overlap inputs. The same inputs give the same bits.
+ * Errors: SJD_ERR_ARG, SJD_ERR_CUDA, SJD_ERR_CAPACITY (workspace too small). */
+
+typedef struct {
+  void* data_dev;
+  int64_t row_stride;            /* in elements                                */
+} sjd_rows;
+
+/* Rows as 8-bit codes: x[t][i] is about scale[t] * codes[t][i], scale[t] =
+ * max_i |x[t][i]| / 127, codes = x / scale rounded to nearest even, both in
+ * fp32 arithmetic, and -127..127 where scale is subnormal and too coarse; a row
+ * with a NaN or an infinity gets scale NaN and codes 0, a row of zeros scale 0.
+ * codes_dev [rows][dim] and scale_dev [rows] are contiguous. dim is at most 16384. */
+int sjd_quantise(const sjd_rows* x, int32_t rows, int32_t dim, int32_t dtype, int8_t* codes_dev, float* scale_dev,
+                 void* cuda_stream);
+
+/* h = x + residual, rounded to dtype (without residual, both NULL: h = x);
+ *   y[t][i] = (h[t][i] - m_t) r_t gain[i] + bias[i],
+ *   r_t = 1 / sqrt(mean_i (h[t][i] - m_t)^2 + eps),
+ * m_t the mean of h[t] with centre != 0 (layer norm), else 0. gain_dev NULL: 1,
+ * bias_dev NULL: 0. Either y is written, or (y NULL) codes_dev [rows][dim] and
+ * scale_dev [rows], what sjd_quantise makes of y before it is rounded. eps >=
+ * 0; a row of zeros with eps 0 is not a number, and rows whose squares pass the
+ * fp32 range are 0. dim is at most 16384. */
+int sjd_norm(const sjd_rows* x, const sjd_rows* residual, const float* gain_dev, const float* bias_dev, float eps,
+             int32_t centre, int32_t rows, int32_t dim, int32_t dtype, const sjd_rows* h, const sjd_rows* y,
+             int8_t* codes_dev, float* scale_dev, void* cuda_stream);
+
+/* The gradient of sjd_norm at h = x. With u = (x - m) r and g = dy gain:
+ *   dx[t] = r_t (g[t] - mean(g[t]) - u[t] mean(g[t] u[t])) + dh[t]
+ * (without mean(g) where centre is 0), dh (or NULL) the gradient that reaches h
+ * otherwise; dx is that of x and of residual alike. dgain_dev[i] = sum_t dy[t][i]
+ * u[t][i], dbias_dev[i] = sum_t dy[t][i] (NULL: not wanted), fp32, written, not
+ * added to. dim is at most 16384. */
+size_t sjd_norm_gradient_workspace_size(int32_t rows, int32_t dim);
+int sjd_norm_gradient(const sjd_rows* dy, const sjd_rows* x, const float* gain_dev, float eps, int32_t centre,
+                      const sjd_rows* dh, int32_t rows, int32_t dim, int32_t dtype, const sjd_rows* dx,
+                      float* dgain_dev, float* dbias_dev, void* workspace_dev, size_t ws_bytes, void* cuda_stream);
+
+/* y[t] = scale table[tokens[t]], zeros where the token is outside [0, vocab).
+ * The table's type is its own. dim is at most 65536. */
+int sjd_embed(const sjd_rows* table, int32_t vocab, int32_t table_dtype, const int32_t* tokens_dev, int32_t rows,
+              int32_t dim, float scale, int32_t dtype, const sjd_rows* y, void* cuda_stream);
+
+/* The gradient of sjd_embed by its table: grad_dev[v] = scale sum of dy[t] over
+ * the t with tokens[t] = v, in a fixed order; fp32 [vocab][dim], contiguous, written
+ * as a whole. */
+size_t sjd_embed_gradient_workspace_size(int32_t rows, int32_t vocab);
+int sjd_embed_gradient(const sjd_rows* dy, const int32_t* tokens_dev, int32_t rows, int32_t dim, int32_t vocab,
+                       float scale, int32_t dtype, float* grad_dev, void* workspace_dev, size_t ws_bytes,
+                       void* cuda_stream);
+
+/* A weight of `out` channels of `in` features in codes (any int8) and a scale
+ * for each channel, laid out for sjd_product. packed_dev: sjd_weight_size bytes
+ * (0: invalid sizes; out up to 2^24, in up to 65536), 256-byte aligned, a byte a code
+ * with out and in filled up to multiples of 256 and 128, not to be changed while products use it. */
+size_t sjd_weight_size(int32_t out, int32_t in);
+int sjd_weight_pack(const int8_t* w_dev, int64_t row_stride, const float* scale_dev, int32_t out, int32_t in,
+                    void* packed_dev, size_t bytes, void* cuda_stream);
+
+/* y[t][n] = (sum_i codes[t][i] w[n][i]) scale[t] w_scale[n] + bias[n] +
+ * residual[t][n], in this order, each step rounded to fp32; bias_dev and residual
+ * may be NULL. The sum is exact (an integer, rounded once to fp32), so that a
+ * row's result does not depend on the call's other rows. Should a wait inside the kernel run out, SJD_ERR_TIMEOUT
+ * is latched in the packed weight (the results are then not valid). */
+size_t sjd_product_workspace_size(int32_t rows, int32_t out, int32_t in);
+int sjd_product(const void* packed_dev, int32_t out, int32_t in, const sjd_rows* codes, const float* scale_dev,
+                int32_t rows, const float* bias_dev, const sjd_rows* residual, int32_t dtype, const sjd_rows* y,
+                void* workspace_dev, size_t ws_bytes, void* cuda_stream);
+
+/* Synchronise the stream, then return and clear the weight's device-side
+ * error (SJD_OK if none). */
+int sjd_weight_sync(void* packed_dev, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,7 +19,8 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "_build")
 LIB = os.path.join(OUT, "libsjd.so")
 LIB_CHECKED = os.path.join(OUT, "libsjd_checked.so")
-SOURCES = ["sjd_kernels.cu", "sjd_fast.cu", "sjd_api.cu", "sjd_noalloc.cu", "sjd_kv.cu", "sjd_attend.cu", "sjd_kv_api.cu"]
+SOURCES = ["sjd_kernels.cu", "sjd_fast.cu", "sjd_api.cu", "sjd_noalloc.cu", "sjd_kv.cu", "sjd_attend.cu", "sjd_kv_api.cu",
+           "sjd_dense.cu", "sjd_product.cu", "sjd_dense_api.cu"]
 # the fast row kernels: sjd_fast_part.cu once per (dtype, mode) pair
 FAST_PARTS = [(dt, mode) for dt in ("SJD_BF16", "SJD_F32") for mode in ("kModeVerify", "kModeStep", "kModeTree", "kModeFromLogits")]
 ARCH = "-gencode=arch=compute_103a,code=sm_103a"
