@@ -1,15 +1,34 @@
 // Matrix products of 8-bit integers with scales per token and per channel:
 // y[t][n] = sx[t] sw[n] sum_k x[t][k] w[n][k] + bias[n] + residual[t][n], the
 // sum exact.
+//
+// sm_103a's tensor cores have no rate to speak of for 8-bit integers; fp16 holds
+// them exactly, and so do its fp32 accumulators as long as every partial sum
+// stays within 2^24. By Cauchy and Schwarz a sum over any part of the features is
+// at most |x[t]| |w[n]|, the roots of the sums of squares, which the packing and
+// the spreading of the codes leave behind: where their product is at most 2^24 (weights
+// and activations of a bell shape, up to about 14000 features) a tile is summed
+// up in one go, else in parts of 1024 features, 2^14 * 2^10 at most, that are
+// added up as integers.
+//
+// The weight stays in 8 bits on its way: two blocks (a cluster) take 256 channels
+// x up to 256 tokens together. Each copies its 128 channels' codes, tile by tile,
+// into shared memory; eight warps turn them into fp16 in tensor memory, from
+// where the product takes them as its A; the tokens' codes, spread to fp16 by a
+// small kernel before, are its B, half of them in each block. So the weight is read
+// once in bytes, which bounds calls of few tokens, and the conversion of a tile costs
+// each thread 32 exchanges of bytes and 32 sums beside a product of 1024 cycles
+// (256 tokens), which bounds those of many.
+
+#include <cuda_fp16.h>
 
 #include "sjd_dense.h"
 #include "sjd_kv_device.cuh"
+#include "sjd_tcgen05.cuh"
 
 namespace sjd_dense_ops {
 
-using sjd_kv_ops::launch_early;
-using sjd_kv_ops::let_next_start;
-using sjd_kv_ops::wait_for_previous;
+using namespace sjd_kv_ops;
 
 namespace {
 
@@ -37,55 +56,495 @@ __global__ void __launch_bounds__(128) pack_kernel(const int8_t* w, long long st
   }
 }
 
-// 64 channels x 64 tokens to a block, 4 x 4 to a thread.
-template <typename T>
-__global__ void __launch_bounds__(256) product_kernel(const ProductParams p) {
-  __shared__ uint32_t ws[64][17], xs[64][17];
-  wait_for_previous();
-  let_next_start();
-  const int n0 = blockIdx.x * 64, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  const long long t0 = static_cast<long long>(blockIdx.y) * 64;
-  int sum[4][4] = {};
-  for (int k0 = 0; k0 < p.w.in; k0 += 64) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < 64 * 16; i += 256) {
-      const int r = i / 16, word = i % 16, k = k0 + 4 * word;
-      const unsigned char* tile = p.w.codes + (static_cast<long long>((n0 + r) / kTileOut) * p.w.tiles_in + k / kTileIn) * kTileBytes;
-      const int c = (n0 + r) % kTileOut;
-      ws[r][word] = *reinterpret_cast<const uint32_t*>(tile + c * kTileIn + ((k % kTileIn / 16) ^ (c % 8)) * 16 + k % 16) ^ 0x80808080u;
-      uint32_t x = 0;
-      if (t0 + r < p.rows) {
-        const int8_t* row = p.codes + (t0 + r) * p.codes_stride;
-        for (int j = 0; j < 4; ++j) {
-          if (k + j < p.w.in) x |= static_cast<uint32_t>(row[k + j] & 0xff) << 8 * j;
-        }
-      }
-      xs[r][word] = x;
+constexpr int kPart = 1024 / kTileIn;           // feature tiles of a part that cannot pass 2^24
+constexpr int kStages = 4;                      // feature tiles on their way through tensor memory
+constexpr int kStageColumns = kTileIn / 2;      // a tile's features in tensor memory, two to a column
+constexpr int kAtStages = 256, kTmemColumns = 512;
+constexpr int kMostTokens = 256;                // of a tile
+constexpr int kMostCodes = 12;                  // tiles of codes in shared memory
+constexpr uint32_t kAtMisc = 224 * 1024;        // (the ring of codes, then that of the tokens)
+constexpr int kSlots = 3;                       // what a block leaves of up to two tiles that others have a part in, and the sum of a tile's parts
+constexpr int kMaxPairs = 80;
+constexpr int kThreads = 512;
+constexpr long long kWaitClocks = 1ll << 31;    // (about a second)
+
+// How a call is shared out. The first `whole` tiles go round the pairs of blocks; the
+// feature tiles of the others, `units`, are cut into equal runs, so that no
+// pair waits for a last round, and a tile's parts are added up as integers.
+struct Plan {
+  int pairs, channel_tiles, token_tiles, per_tile;  // pairs of blocks; tiles of 256 channels; of tokens; feature tiles
+  int tokens, codes_ring, accumulators;             // tokens of a tile, stages
+  int whole, shares;                                // shares: pairs that the rest is cut up for
+  long long units;
+  const unsigned char* x;                           // the tokens' codes in fp16
+  const uint32_t* squares;                          // of each token's codes
+  int32_t* slots;
+  int32_t* counters;
+};
+
+__host__ __device__ __forceinline__ long long share_begin(const Plan& g, int share) { return g.units * share / g.shares; }
+
+// One piece of work: feature tiles k0 .. k1 - 1 of a tile.
+struct Piece {
+  int tile, channel, token, k0, k1;   // (channel, token: numbers of tiles)
+};
+struct Walk {
+  int tile;
+  long long at, end;
+  __device__ __forceinline__ Walk(const Plan& g, int pair) : tile(pair), at(0), end(0) {
+    if (pair < g.shares) at = share_begin(g, pair), end = share_begin(g, pair + 1);
+  }
+  __device__ __forceinline__ bool next(const Plan& g, Piece& p) {
+    if (tile < g.whole) {
+      p.tile = tile, p.k0 = 0, p.k1 = g.per_tile;
+      tile += g.pairs;
+    } else if (at < end) {
+      const int t = static_cast<int>(at / g.per_tile);
+      p.tile = g.whole + t;
+      p.k0 = static_cast<int>(at - static_cast<long long>(t) * g.per_tile);
+      p.k1 = static_cast<int>(min(static_cast<long long>(g.per_tile), p.k0 + (end - at)));
+      at += p.k1 - p.k0;
+    } else {
+      return false;
     }
-    __syncthreads();
-    for (int word = 0; word < 16; ++word) {
+    // eight tiles of tokens side by side: the pairs at work share what they read in L2
+    const int band = p.tile / (8 * g.channel_tiles), in = p.tile - band * 8 * g.channel_tiles, across = min(8, g.token_tiles - 8 * band);
+    p.channel = in / across;
+    p.token = 8 * band + in - p.channel * across;
+    return true;
+  }
+};
+
+struct Misc {
+  unsigned long long codes_full[kMostCodes], codes_empty[kMostCodes];  // a tile of codes is there; has been turned into fp16
+  unsigned long long x_full[kStages];                                  // the tokens' tile is there
+  unsigned long long full[kStages], empty[kStages];                    // (block 0's) both operands of both blocks are there; have been used
+  unsigned long long sum_full[2], sum_empty[2];                        // an accumulator is done; (block 0's) has been read
+  unsigned long long drained;
+  uint32_t tmem;
+  int abort;
+  int last;
+};
+
+__device__ __forceinline__ void wait(Misc* m, unsigned long long* bar, uint32_t parity) {
+  const uint32_t at = smem_addr(bar);
+  if (mbar_try_cluster(at, parity)) return;
+  const long long begun = clock64();
+  while (!mbar_try_cluster(at, parity)) {
+    // once a wait has run out, none waits any more: the block goes on to its
+    // end over results that do not count
+    if (*const_cast<volatile int*>(&m->abort)) return;
+    if (clock64() - begun > kWaitClocks) {
+      *const_cast<volatile int*>(&m->abort) = 1;
+      return;
+    }
+  }
+}
+__device__ __forceinline__ bool aborted(Misc* m) { return *const_cast<volatile int*>(&m->abort) != 0; }
+
+// The next stage of a ring, and the parity of its barriers' phase.
+struct Ring {
+  int i = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void step(int n) {
+    if (++i == n) i = 0, phase ^= 1;
+  }
+};
+
+// Whether a piece's sums can pass 2^24 (all lanes of a warp).
+__device__ __forceinline__ bool in_parts(const ProductParams& p, const Plan& g, const Piece& q) {
+  if (q.k1 - q.k0 <= kPart) return false;
+  const int lane = threadIdx.x & 31;
+  uint32_t w = 0, x = 0;
+#pragma unroll
+  for (int i = 0; i < 2 * kTileOut; i += 32) w = max(w, __ldg(p.w.squares + q.channel * (2 * kTileOut) + i + lane));
+  const long long t0 = static_cast<long long>(q.token) * g.tokens;
+#pragma unroll
+  for (int i = 0; i < kMostTokens; i += 32) {
+    const long long t = t0 + i + lane;
+    if (i + lane < g.tokens && t < p.rows) x = max(x, g.squares[t]);
+  }
+  w = __reduce_max_sync(0xffffffffu, w), x = __reduce_max_sync(0xffffffffu, x);
+  return static_cast<unsigned long long>(w) * x > 1ull << 48;
+}
+
+// Copies of this block's tiles into a ring of `n` stages of `bytes` (one lane).
+// What is in flight lands before the block ends.
+template <typename Source>
+__device__ __forceinline__ void copy_tiles(Misc* m, const Plan& g, int pair, uint32_t ring_at, int n, uint32_t bytes, unsigned long long* full,
+                                           unsigned long long* empty, Source source) {
+  Ring r;
+  int sent = 0;
+  Walk walk(g, pair);
+  Piece q;
+  while (walk.next(g, q)) {
+    const unsigned char* from = source(q);
+    for (int k = q.k0; k < q.k1; ++k) {
+      wait(m, &empty[r.i], r.phase ^ 1);
+      if (aborted(m)) goto done;
+      mbar_expect(smem_addr(&full[r.i]), bytes);
+      copy_bulk(ring_at + r.i * bytes, from + static_cast<long long>(k) * bytes, bytes, smem_addr(&full[r.i]));
+      r.step(n);
+      sent = min(sent + 1, n);
+    }
+  }
+done:
+  for (; sent > 0; --sent) {
+    if (--r.i < 0) r.i = n - 1, r.phase ^= 1;
+    const long long begun = clock64();
+    while (!mbar_try(smem_addr(&full[r.i]), r.phase) && clock64() - begun <= kWaitClocks) {}
+  }
+}
+
+// Codes (c + 128) of four neighbouring features as fp16: the byte behind 0x64 is
+// 1024 + 128 + c.
+__device__ __forceinline__ void halves_of(uint32_t codes, uint32_t& lo, uint32_t& hi) {
+  const __half2 less = __half2half2(__ushort_as_half(0x6480));   // 1152
+  const uint32_t a = __byte_perm(codes, 0x64646464u, 0x4140), b = __byte_perm(codes, 0x64646464u, 0x4342);
+  const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), less), y = __hsub2(*reinterpret_cast<const __half2*>(&b), less);
+  lo = *reinterpret_cast<const uint32_t*>(&x), hi = *reinterpret_cast<const uint32_t*>(&y);
+}
+
+// Warps 0 to 3 take the first 64 features of a tile, 4 to 7 the others; a lane a channel.
+__device__ __forceinline__ void convert(Misc* m, const Plan& g, int pair, int warp, uint32_t codes_at, uint32_t tmem) {
+  const int lane = threadIdx.x & 31, half = warp / 4, channel = (warp & 3) * 32 + lane;
+  const uint32_t full0 = cluster_addr(smem_addr(&m->full[0]), 0);
+  Ring c, s;
+  Walk walk(g, pair);
+  Piece q;
+  while (walk.next(g, q)) {
+    for (int k = q.k0; k < q.k1; ++k) {
+      wait(m, &m->codes_full[c.i], c.phase);
+      const uint32_t row = codes_at + c.i * kTileBytes + channel * kTileIn;
+      uint32_t v[32];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
+        const uint4 u = shared_load16(row + (((half * 4 + i) ^ (channel & 7)) << 4));
+        halves_of(u.x, v[8 * i], v[8 * i + 1]), halves_of(u.y, v[8 * i + 2], v[8 * i + 3]);
+        halves_of(u.z, v[8 * i + 4], v[8 * i + 5]), halves_of(u.w, v[8 * i + 6], v[8 * i + 7]);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_addr(&m->codes_empty[c.i]));
+      wait(m, &m->empty[s.i], s.phase ^ 1);
+      tc_fence_after();
+      tmem_store32(tmem + kAtStages + s.i * kStageColumns + half * 32 + (static_cast<uint32_t>((warp & 3) * 32) << 16), v);
+      tmem_wait_store();
+      // (one warp's arrival tells of this block's tokens too)
+      if (warp == 0) wait(m, &m->x_full[s.i], s.phase);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(full0 + s.i * 8);
+      c.step(g.codes_ring);
+      s.step(kStages);
+    }
+  }
+}
+
+// The products of both blocks (one warp of block 0).
+__device__ __forceinline__ void issue(const ProductParams& p, Misc* m, const Plan& g, int pair, uint32_t x_at, uint32_t tmem) {
+  const bool lead = elect_lane();
+  const uint32_t kind = product_kind(2 * kTileOut, g.tokens, false, true), half_tile = g.tokens / 2 * 128, x_bytes = 2 * half_tile;
+  Ring s, d;
+  Walk walk(g, pair);
+  Piece q;
+  while (walk.next(g, q)) {
+    const bool parts = in_parts(p, g, q);
+    for (int k = q.k0; k < q.k1; ++k) {
+      const bool first = k == q.k0 || (parts && (k - q.k0) % kPart == 0);
+      const bool end = k + 1 == q.k1 || (parts && (k + 1 - q.k0) % kPart == 0);
+      if (first) wait(m, &m->sum_empty[d.i], d.phase ^ 1);
+      wait(m, &m->full[s.i], s.phase);
+      tc_fence_after();
+      const uint32_t a = tmem + kAtStages + s.i * kStageColumns, sum = tmem + d.i * (kAtStages / 2);
+      const uint64_t b0 = operand_k(x_at + s.i * x_bytes), b1 = operand_k(x_at + s.i * x_bytes + half_tile);
+      if (lead) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[i][j] = __dp4a(static_cast<int>(ws[tx + 16 * i][word]), static_cast<int>(xs[ty + 16 * j][word]), sum[i][j]);
+        for (int i = 0; i < kTileIn / 16; ++i) mma_ts_pair(sum, a + i * 8, (i < 4 ? b0 : b1) + (i & 3) * 2, kind, !first || i > 0);
+        mma_commit_pair(smem_addr(&m->empty[s.i]));
+        if (end) mma_commit_pair(smem_addr(&m->sum_full[d.i]));
+      }
+      __syncwarp();
+      s.step(kStages);
+      if (end) d.step(g.accumulators);
+    }
+  }
+  if (lead) mma_commit_pair(smem_addr(&m->drained));
+  __syncwarp();
+}
+
+// Results of a lane's channel and 32 tokens from t0 on. (Each step is rounded by
+// itself: the result is the same whichever way the sum was taken.)
+template <typename T>
+__device__ __forceinline__ void finish(const ProductParams& p, int n, long long t0, int count, float scale, float bias, float (&v)[32]) {
+  const bool mine = n < p.w.out;
+  if (p.residual.p) {
+    const T* r = static_cast<const T*>(p.residual.p) + t0 * p.residual.stride + n;
+    float x[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) x[j] = mine && j < count ? static_cast<float>(r[j * p.residual.stride]) : 0.0f;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const float sx = j < count ? __ldg(p.scale + t0 + j) : 0.0f;
+      v[j] = __fmul_rn(__fmul_rn(v[j], sx), scale);
+      if (p.bias) v[j] = __fadd_rn(v[j], bias);
+      v[j] = __fadd_rn(v[j], x[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const float sx = j < count ? __ldg(p.scale + t0 + j) : 0.0f;
+      v[j] = __fmul_rn(__fmul_rn(v[j], sx), scale);
+      if (p.bias) v[j] = __fadd_rn(v[j], bias);
+    }
+  }
+  if (!mine) return;
+  T* y = static_cast<T*>(p.y.p) + t0 * p.y.stride + n;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    if (j < count) y[j * p.y.stride] = static_cast<T>(v[j]);
+  }
+}
+
+// Four warps read the accumulators, a lane a channel.
+template <typename T>
+__device__ __forceinline__ void results(const ProductParams& p, Misc* m, const Plan& g, int pair, int rank, int warp, uint32_t tmem) {
+  const int lane = threadIdx.x & 31, row = warp * 32 + lane;
+  const uint32_t empty0 = cluster_addr(smem_addr(&m->sum_empty[0]), 0);
+  const long long slot_size = static_cast<long long>(g.tokens) * kTileOut;
+  auto slot_of = [&](int of_pair, int slot) { return g.slots + ((2ll * of_pair + rank) * kSlots + slot) * slot_size + row; };
+  Ring d;
+  Walk walk(g, pair);
+  Piece q;
+  while (walk.next(g, q)) {
+    const bool parts = in_parts(p, g, q), whole = q.k1 - q.k0 == g.per_tile;
+    const int n = (q.channel * 2 + rank) * kTileOut + row;
+    const long long t0 = static_cast<long long>(q.token) * g.tokens;
+    const int tokens = static_cast<int>(min(static_cast<long long>(g.tokens), p.rows - t0));
+    const float scale = __ldg(p.w.scale + n), bias = p.bias && n < p.w.out ? __ldg(p.bias + n) : 0.0f;
+    const int mine = static_cast<int>(share_begin(g, pair) / g.per_tile) == q.tile - g.whole ? 0 : 1;
+    int32_t* sum = slot_of(pair, 2);
+    int32_t* left = slot_of(pair, mine);
+    const int turns = parts ? (q.k1 - q.k0 + kPart - 1) / kPart : 1;
+    for (int turn = 0; turn < turns; ++turn) {
+      wait(m, &m->sum_full[d.i], d.phase);
+      tc_fence_after();
+      for (int c = 0; c < g.tokens; c += 32) {
+        uint32_t u[32];
+        tmem_load32(tmem + d.i * (kAtStages / 2) + c + (static_cast<uint32_t>(warp * 32) << 16), u);
+        tmem_wait_load(u);
+        const int columns = min(32, g.tokens - c);
+        if (turns == 1 && whole) {
+          float v[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(u[j]);
+          finish<T>(p, n, t0 + c, tokens - c, scale, bias, v);
+          continue;
+        }
+        int v[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = __float2int_rn(__uint_as_float(u[j]));
+        if (turn > 0) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] += j < columns ? sum[static_cast<long long>(c + j) * kTileOut] : 0;
+        }
+        if (turn + 1 < turns || !whole) {
+          int32_t* to = turn + 1 < turns ? sum : left;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            if (j < columns) to[static_cast<long long>(c + j) * kTileOut] = v[j];
+          }
+        } else {
+          float f[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) f[j] = __int2float_rn(v[j]);
+          finish<T>(p, n, t0 + c, tokens - c, scale, bias, f);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(empty0 + d.i * 8);
+      d.step(g.accumulators);
+    }
+    if (whole) continue;
+    // the last of the tile's pairs to be done adds its parts up
+    const int of = q.tile - g.whole;
+    const long long begin = static_cast<long long>(of) * g.per_tile, end = begin + g.per_tile;
+    int first = static_cast<int>(begin * g.shares / g.units);
+    while (share_begin(g, first + 1) <= begin) ++first;
+    while (share_begin(g, first) > begin) --first;
+    int after = first + 1;
+    while (after < g.shares && share_begin(g, after) < end) ++after;
+    named_barrier(1, 128);
+    if (warp == 0 && lane == 0) {
+      __threadfence();
+      m->last = atomicAdd(&g.counters[2 * of + rank], 1) == after - first - 1;
+      __threadfence();
+    }
+    named_barrier(1, 128);
+    if (!*const_cast<volatile int*>(&m->last)) continue;
+    for (int c = 0; c < tokens; c += 32) {
+      int v[32] = {};
+      const int columns = min(32, g.tokens - c);
+      for (int other = first; other < after; ++other) {
+        const int slot = static_cast<int>(share_begin(g, other) / g.per_tile) == of ? 0 : 1;
+        const int32_t* from = slot_of(other, slot);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] += j < columns ? __ldcg(from + static_cast<long long>(c + j) * kTileOut) : 0;
+      }
+      float f[32];
+#pragma unroll
+      for (int j = 0; j < 32; ++j) f[j] = __int2float_rn(v[j]);
+      finish<T>(p, n, t0 + c, tokens - c, scale, bias, f);
+    }
+  }
+}
+
+template <typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product_kernel(const ProductParams p, const Plan g) {
+  extern __shared__ __align__(1024) unsigned char raw[];
+  Misc* m = reinterpret_cast<Misc*>(raw + kAtMisc);
+  const uint32_t smem = smem_addr(raw), x_at = smem + g.codes_ring * kTileBytes;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), rank = static_cast<int>(cluster_rank()), pair = blockIdx.x / 2;
+  if (warp == 3) tmem_alloc_pair(smem_addr(&m->tmem), kTmemColumns);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kMostCodes; ++i) mbar_init(smem_addr(&m->codes_full[i]), 1), mbar_init(smem_addr(&m->codes_empty[i]), 8);
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(smem_addr(&m->x_full[i]), 1), mbar_init(smem_addr(&m->full[i]), 16), mbar_init(smem_addr(&m->empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) mbar_init(smem_addr(&m->sum_full[i]), 1), mbar_init(smem_addr(&m->sum_empty[i]), 8);
+    mbar_init(smem_addr(&m->drained), 1);
+    m->abort = 0;
+    fence_barrier_init();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem = m->tmem;
+  // The weight's codes are read at once: the kernel before this one, which spreads
+  // the tokens' codes, has let it in after all before that was done. All else waits for it.
+  if (warp != 0) wait_for_previous();
+  if (warp == 0) {
+    if (elect_lane()) {
+      copy_tiles(m, g, pair, smem, g.codes_ring, kTileBytes, m->codes_full, m->codes_empty, [&](const Piece& q) {
+        return p.w.codes + static_cast<long long>(q.channel * 2 + rank) * p.w.tiles_in * kTileBytes;
+      });
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    const uint32_t bytes = static_cast<uint32_t>(g.tokens) * 128;
+    if (elect_lane()) {
+      copy_tiles(m, g, pair, x_at, kStages, bytes, m->x_full, m->empty,
+                 [&](const Piece& q) { return g.x + static_cast<long long>(q.token * 2 + rank) * g.per_tile * bytes; });
+    }
+    __syncwarp();
+  } else if (warp == 2) {
+    if (rank == 0) issue(p, m, g, pair, x_at, tmem);
+  } else if (warp == 3) {
+    let_next_start();
+  } else if (warp < 12) {
+    convert(m, g, pair, warp - 4, smem, tmem);
+  } else {
+    results<T>(p, m, g, pair, rank, warp - 12, tmem);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 2) {
+    // (no product is in flight, and no arrival at the other block's barriers, when the blocks end)
+    const long long begun = clock64();
+    while (!mbar_try(smem_addr(&m->drained), 0) && clock64() - begun <= kWaitClocks) {}
+    __syncwarp();
+  }
+  cluster_sync();
+  if (warp == 3) {
+    tc_fence_after();
+    tmem_free_pair(tmem, kTmemColumns);
+  }
+  if (threadIdx.x == 0 && m->abort) atomicOr(&p.w.header->status, status_bit(SJD_ERR_TIMEOUT));
+}
+
+// The tokens' codes in fp16, in the order in which the product's tiles lie in
+// shared memory (the 128-byte swizzle), the sum of each token's squares, and the
+// counters of shared tiles. A block takes a token.
+__global__ void __launch_bounds__(256) spread_kernel(const ProductParams p, const Plan g, unsigned char* x, uint32_t* squares) {
+  __shared__ uint32_t words[8];
+  wait_for_previous();
+  let_next_start();
+  const int t = blockIdx.x, lane = threadIdx.x & 31, half = g.tokens / 2;
+  if (blockIdx.x == 0) {
+    for (int i = threadIdx.x; i < 4 * kMaxPairs; i += 256) g.counters[i] = 0;
+  }
+  const int8_t* from = p.codes + t * p.codes_stride;
+  const int tile = t / g.tokens, r = t - tile * g.tokens, of_half = r / half, row = r - of_half * half;
+  unsigned char* to = x + static_cast<long long>(tile * 2 + of_half) * g.per_tile * half * 256 + row * 128;
+  const bool wide = reinterpret_cast<uintptr_t>(from) % 16 == 0;
+  uint32_t sum = 0;
+  for (int k = threadIdx.x * 16; k < g.per_tile * kTileIn; k += 256 * 16) {
+    uint32_t c[4] = {0, 0, 0, 0};
+    if (wide && k + 16 <= p.w.in) {
+      const uint4 u = *reinterpret_cast<const uint4*>(from + k);
+      c[0] = u.x, c[1] = u.y, c[2] = u.z, c[3] = u.w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        if (k + j < p.w.in) c[j / 4] |= static_cast<uint32_t>(from[k + j] & 0xff) << 8 * (j % 4);
       }
     }
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const long long t = t0 + ty + 16 * j;
-    if (t >= p.rows) continue;
+    uint32_t h[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int n = n0 + tx + 16 * i;
-      if (n >= p.w.out) continue;
-      // (each step rounded by itself: the result is the same whichever way the sum was taken)
-      float y = __fmul_rn(__fmul_rn(static_cast<float>(sum[i][j]), p.scale[t]), p.w.scale[n]);
-      if (p.bias) y = __fadd_rn(y, p.bias[n]);
-      if (p.residual.p) y = __fadd_rn(y, static_cast<float>(static_cast<const T*>(p.residual.p)[t * p.residual.stride + n]));
-      static_cast<T*>(p.y.p)[t * p.y.stride + n] = static_cast<T>(y);
+      sum = __dp4a(static_cast<int>(c[i]), static_cast<int>(c[i]), static_cast<int>(sum));
+      halves_of(c[i] ^ 0x80808080u, h[2 * i], h[2 * i + 1]);
     }
+    unsigned char* at = to + (static_cast<long long>(k / kTileIn) * 2 + (k % kTileIn) / 64) * half * 128;
+    const int piece = (k % 64) / 8;
+    *reinterpret_cast<uint4*>(at + ((piece ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+    *reinterpret_cast<uint4*>(at + (((piece + 1) ^ (row & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
   }
+  sum = __reduce_add_sync(0xffffffffu, sum);
+  if (lane == 0) words[threadIdx.x / 32] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 8; ++i) sum += words[i];
+    squares[t] = sum;
+  }
+}
+
+struct Scratch {
+  size_t squares, x, slots, bytes;   // (the counters are at the beginning)
+};
+
+Plan plan_of(int rows, const Packed& w, int sms, Scratch* at) {
+  Plan g{};
+  g.pairs = min(sms / 2, kMaxPairs);
+  g.channel_tiles = w.tiles_out / 2;
+  g.per_tile = w.tiles_in;
+  g.token_tiles = static_cast<int>((static_cast<long long>(rows) + kMostTokens - 1) / kMostTokens);
+  g.tokens = ((rows + g.token_tiles - 1) / g.token_tiles + 15) / 16 * 16;
+  g.accumulators = g.tokens <= kAtStages / 2 ? 2 : 1;
+  g.codes_ring = min(kMostCodes, static_cast<int>((kAtMisc - kStages * g.tokens * 128) / kTileBytes));
+  const long long tiles = static_cast<long long>(g.channel_tiles) * g.token_tiles;
+  // whole tiles as long as they go round, but for the last round; one round and what is left over are cut up
+  const long long rounds = tiles % g.pairs == 0 ? tiles / g.pairs : max(0ll, tiles / g.pairs - 1);
+  g.whole = static_cast<int>(rounds * g.pairs);
+  g.units = (tiles - g.whole) * g.per_tile;
+  g.shares = static_cast<int>(min(static_cast<long long>(g.pairs), max(1ll, g.units / 2)));
+  at->squares = 4096;
+  static_assert(4 * kMaxPairs * sizeof(int32_t) <= 4096, "counters");
+  at->x = at->squares + (static_cast<size_t>(rows) * sizeof(uint32_t) + 255) / 256 * 256;
+  at->slots = at->x + static_cast<size_t>(g.token_tiles) * g.tokens * g.per_tile * kTileIn * sizeof(__half);
+  at->bytes = at->slots + 2 * static_cast<size_t>(g.pairs) * kSlots * g.tokens * kTileOut * sizeof(int32_t);
+  return g;
+}
+
+template <typename T>
+cudaError_t product_of(const ProductParams& p, const Plan& g, unsigned char* x, uint32_t* squares, cudaStream_t s) {
+  constexpr int kShared = kAtMisc + sizeof(Misc);
+  static_assert(kShared <= 227 * 1024, "shared memory");
+  cudaError_t e = cudaFuncSetAttribute(product_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
+  if (e == cudaSuccess) e = launch_early(spread_kernel, p.rows, 256, 0, s, p, g, x, squares);
+  if (e != cudaSuccess) return e;
+  return launch_early(product_kernel<T>, 2 * g.pairs, kThreads, kShared, s, p, g);
 }
 
 }  // namespace
@@ -94,12 +553,23 @@ cudaError_t launch_pack(const int8_t* w, long long stride, const float* scale, c
   return launch_early(pack_kernel, static_cast<unsigned>(to.tiles_out) * kTileOut, 128, 0, s, w, stride, scale, to);
 }
 
-size_t product_scratch_bytes(int rows, int out, int in, int sms) { return 256; }
+size_t product_scratch_bytes(int rows, int out, int in, int sms) {
+  Packed w;
+  packed_layout(out, in, nullptr, &w);
+  Scratch at;
+  plan_of(rows, w, sms, &at);
+  return at.bytes;
+}
 
 cudaError_t launch_product(const ProductParams& p, int dtype, int sms, unsigned char* scratch, cudaStream_t s) {
-  const dim3 grid((p.w.out + 63) / 64, (p.rows + 63) / 64);
-  if (dtype == SJD_BF16) return launch_early(product_kernel<__nv_bfloat16>, grid, 256, 0, s, p);
-  return launch_early(product_kernel<float>, grid, 256, 0, s, p);
+  Scratch at;
+  Plan g = plan_of(p.rows, p.w, sms, &at);
+  g.counters = reinterpret_cast<int32_t*>(scratch);
+  g.squares = reinterpret_cast<uint32_t*>(scratch + at.squares);
+  g.x = scratch + at.x;
+  g.slots = reinterpret_cast<int32_t*>(scratch + at.slots);
+  if (dtype == SJD_BF16) return product_of<__nv_bfloat16>(p, g, scratch + at.x, reinterpret_cast<uint32_t*>(scratch + at.squares), s);
+  return product_of<float>(p, g, scratch + at.x, reinterpret_cast<uint32_t*>(scratch + at.squares), s);
 }
 
 }  // namespace sjd_dense_ops
