@@ -638,7 +638,7 @@ int sjd_embed_gradient(const sjd_rows* dy, const int32_t* tokens_dev, int32_t ro
 /* A weight of `out` channels of `in` features in codes (any int8) and a scale
  * for each channel, laid out for sjd_product. packed_dev: sjd_weight_size bytes
  * (0: invalid sizes; out up to 2^24, in up to 65536), 256-byte aligned, a byte a code
- * with out and in filled up to multiples of 256 and 128, not to be changed while products use it. */
+ * with out and in filled up to multiples of 256 and 64, not to be changed while products use it. */
 size_t sjd_weight_size(int32_t out, int32_t in);
 int sjd_weight_pack(const int8_t* w_dev, int64_t row_stride, const float* scale_dev, int32_t out, int32_t in,
                     void* packed_dev, size_t bytes, void* cuda_stream);

@@ -62,9 +62,10 @@ struct EmbedGradientParams {
 // A packed weight: a header, the channels' scales and the codes in tiles of
 // kTileOut channels x kTileIn features, one after another along the features.
 // In a tile a channel's kTileIn codes are neighbours, in pieces of 16 that
-// stand in the order piece ^ (channel % 8); a code c is held as c + 128.
+// stand in the order piece ^ (channel / 2 % 4), so that eight channels' pieces
+// of one number lie in different banks; a code c is held as c + 128.
 // Channels and features that fill up the last tiles are codes of 0.
-constexpr int kTileOut = 128, kTileIn = 128;
+constexpr int kTileOut = 128, kTileIn = 64;
 constexpr int kTileBytes = kTileOut * kTileIn;
 struct PackedHeader {
   uint32_t status;

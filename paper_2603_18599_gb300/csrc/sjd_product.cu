@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(128) pack_kernel(const int8_t* w, long long st
   for (int k = threadIdx.x; k < to.tiles_in * kTileIn; k += 128) {
     const int c = channel < to.out && k < to.in ? w[channel * stride + k] : 0;
     squares += c * c;
-    const int piece = (k % kTileIn) / 16 ^ (r % 8);
+    const int piece = (k % kTileIn) / 16 ^ (r / 2 % 4);
     tile[static_cast<long long>(k / kTileIn) * kTileBytes + piece * 16 + k % 16] = static_cast<unsigned char>(c + 128);
   }
   squares = __reduce_add_sync(0xffffffffu, squares);
@@ -57,23 +57,23 @@ __global__ void __launch_bounds__(128) pack_kernel(const int8_t* w, long long st
 }
 
 constexpr int kPart = 1024 / kTileIn;           // feature tiles of a part that cannot pass 2^24
-constexpr int kStages = 4;                      // feature tiles on their way through tensor memory
+constexpr int kMostTokens = 256, kTwoSums = 192; // of a tile; of one that has two accumulators
 constexpr int kStageColumns = kTileIn / 2;      // a tile's features in tensor memory, two to a column
-constexpr int kAtStages = 256, kTmemColumns = 512;
-constexpr int kMostTokens = 256;                // of a tile
-constexpr int kMostCodes = 12;                  // tiles of codes in shared memory
+constexpr int kTmemColumns = 512;
+constexpr int kMostCodes = 24, kStages = 8;     // most tiles on their way: codes, tokens and codes in fp16
 constexpr uint32_t kAtMisc = 224 * 1024;        // (the ring of codes, then that of the tokens)
 constexpr int kSlots = 3;                       // what a block leaves of up to two tiles that others have a part in, and the sum of a tile's parts
 constexpr int kMaxPairs = 80;
 constexpr int kThreads = 512;
-constexpr long long kWaitClocks = 1ll << 31;    // (about a second)
+constexpr long long kWaitClocks = 4000000000ll; // about two seconds
 
 // How a call is shared out. The first `whole` tiles go round the pairs of blocks; the
 // feature tiles of the others, `units`, are cut into equal runs, so that no
 // pair waits for a last round, and a tile's parts are added up as integers.
 struct Plan {
   int pairs, channel_tiles, token_tiles, per_tile;  // pairs of blocks; tiles of 256 channels; of tokens; feature tiles
-  int tokens, codes_ring, accumulators;             // tokens of a tile, stages
+  int tokens, codes_ring, x_ring, stages;           // tokens of a tile; tiles in shared memory, of codes in tensor memory
+  int accumulators, sum_columns;                    // columns from one accumulator to the next
   int whole, shares;                                // shares: pairs that the rest is cut up for
   long long units;
   const unsigned char* x;                           // the tokens' codes in fp16
@@ -115,22 +115,30 @@ struct Walk {
   }
 };
 
+// What a piece's products and results need to know of its tokens.
+struct Ready {
+  alignas(16) float scale[kMostTokens];  // (0 behind the last)
+  int parts;                             // its sums can pass 2^24
+};
+
 struct Misc {
   unsigned long long codes_full[kMostCodes], codes_empty[kMostCodes];  // a tile of codes is there; has been turned into fp16
-  unsigned long long x_full[kStages];                                  // the tokens' tile is there
-  unsigned long long full[kStages], empty[kStages];                    // (block 0's) both operands of both blocks are there; have been used
+  unsigned long long x_full[kStages], x_empty[kStages];                // the tokens' tile is there; has been used
+  unsigned long long full[kStages], empty[kStages];                    // (block 0's) both operands of both blocks are there; A has been used
   unsigned long long sum_full[2], sum_empty[2];                        // an accumulator is done; (block 0's) has been read
+  unsigned long long ready_full[2], ready_empty[2];
   unsigned long long drained;
   uint32_t tmem;
   int abort;
   int last;
+  Ready ready[2];
 };
 
 __device__ __forceinline__ void wait(Misc* m, unsigned long long* bar, uint32_t parity) {
   const uint32_t at = smem_addr(bar);
-  if (mbar_try_cluster(at, parity)) return;
+  if (mbar_try(at, parity)) return;
   const long long begun = clock64();
-  while (!mbar_try_cluster(at, parity)) {
+  while (!mbar_try(at, parity)) {
     // once a wait has run out, none waits any more: the block goes on to its
     // end over results that do not count
     if (*const_cast<volatile int*>(&m->abort)) return;
@@ -150,23 +158,6 @@ struct Ring {
     if (++i == n) i = 0, phase ^= 1;
   }
 };
-
-// Whether a piece's sums can pass 2^24 (all lanes of a warp).
-__device__ __forceinline__ bool in_parts(const ProductParams& p, const Plan& g, const Piece& q) {
-  if (q.k1 - q.k0 <= kPart) return false;
-  const int lane = threadIdx.x & 31;
-  uint32_t w = 0, x = 0;
-#pragma unroll
-  for (int i = 0; i < 2 * kTileOut; i += 32) w = max(w, __ldg(p.w.squares + q.channel * (2 * kTileOut) + i + lane));
-  const long long t0 = static_cast<long long>(q.token) * g.tokens;
-#pragma unroll
-  for (int i = 0; i < kMostTokens; i += 32) {
-    const long long t = t0 + i + lane;
-    if (i + lane < g.tokens && t < p.rows) x = max(x, g.squares[t]);
-  }
-  w = __reduce_max_sync(0xffffffffu, w), x = __reduce_max_sync(0xffffffffu, x);
-  return static_cast<unsigned long long>(w) * x > 1ull << 48;
-}
 
 // Copies of this block's tiles into a ring of `n` stages of `bytes` (one lane).
 // What is in flight lands before the block ends.
@@ -196,6 +187,40 @@ done:
   }
 }
 
+// The tokens' scales and whether a piece's sums can pass 2^24 (a warp, a piece
+// or two ahead: two round trips to memory that nothing else waits for).
+__device__ __forceinline__ void prepare(const ProductParams& p, Misc* m, const Plan& g, int pair) {
+  const int lane = threadIdx.x & 31;
+  Ring r;
+  Walk walk(g, pair);
+  Piece q;
+  while (walk.next(g, q)) {
+    const long long t0 = static_cast<long long>(q.token) * g.tokens;
+    uint32_t w[2 * kTileOut / 32], x[kMostTokens / 32];
+    float scale[kMostTokens / 32];
+#pragma unroll
+    for (int i = 0; i < 2 * kTileOut / 32; ++i) w[i] = __ldg(p.w.squares + q.channel * (2 * kTileOut) + 32 * i + lane);
+#pragma unroll
+    for (int i = 0; i < kMostTokens / 32; ++i) {
+      const bool is = 32 * i + lane < g.tokens && t0 + 32 * i + lane < p.rows;
+      x[i] = is ? g.squares[t0 + 32 * i + lane] : 0;
+      scale[i] = is ? __ldg(p.scale + t0 + 32 * i + lane) : 0.0f;
+    }
+#pragma unroll
+    for (int i = 1; i < 2 * kTileOut / 32; ++i) w[0] = max(w[0], w[i]);
+#pragma unroll
+    for (int i = 1; i < kMostTokens / 32; ++i) x[0] = max(x[0], x[i]);
+    const uint32_t most_w = __reduce_max_sync(0xffffffffu, w[0]), most_x = __reduce_max_sync(0xffffffffu, x[0]);
+    wait(m, &m->ready_empty[r.i], r.phase ^ 1);
+#pragma unroll
+    for (int i = 0; i < kMostTokens / 32; ++i) m->ready[r.i].scale[32 * i + lane] = scale[i];
+    if (lane == 0) m->ready[r.i].parts = q.k1 - q.k0 > kPart && static_cast<unsigned long long>(most_w) * most_x > 1ull << 48;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_addr(&m->ready_full[r.i]));
+    r.step(2);
+  }
+}
+
 // Codes (c + 128) of four neighbouring features as fp16: the byte behind 0x64 is
 // 1024 + 128 + c.
 __device__ __forceinline__ void halves_of(uint32_t codes, uint32_t& lo, uint32_t& hi) {
@@ -205,66 +230,78 @@ __device__ __forceinline__ void halves_of(uint32_t codes, uint32_t& lo, uint32_t
   lo = *reinterpret_cast<const uint32_t*>(&x), hi = *reinterpret_cast<const uint32_t*>(&y);
 }
 
-// Warps 0 to 3 take the first 64 features of a tile, 4 to 7 the others; a lane a channel.
+// Warps 0 to 3 take every other tile, warps 4 to 7 those between; a lane a channel.
 __device__ __forceinline__ void convert(Misc* m, const Plan& g, int pair, int warp, uint32_t codes_at, uint32_t tmem) {
-  const int lane = threadIdx.x & 31, half = warp / 4, channel = (warp & 3) * 32 + lane;
-  const uint32_t full0 = cluster_addr(smem_addr(&m->full[0]), 0);
-  Ring c, s;
+  const int lane = threadIdx.x & 31, turn = warp / 4, channel = (warp & 3) * 32 + lane;
+  const uint32_t full0 = cluster_addr(smem_addr(&m->full[0]), 0), stages_at = tmem + g.accumulators * g.sum_columns + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+  Ring c, s, x;
+  int mine = 0;
   Walk walk(g, pair);
   Piece q;
   while (walk.next(g, q)) {
     for (int k = q.k0; k < q.k1; ++k) {
-      wait(m, &m->codes_full[c.i], c.phase);
-      const uint32_t row = codes_at + c.i * kTileBytes + channel * kTileIn;
-      uint32_t v[32];
+      if (mine == turn) {
+        wait(m, &m->codes_full[c.i], c.phase);
+        const uint32_t row = codes_at + c.i * kTileBytes + channel * kTileIn;
+        uint32_t v[32];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint4 u = shared_load16(row + (((half * 4 + i) ^ (channel & 7)) << 4));
-        halves_of(u.x, v[8 * i], v[8 * i + 1]), halves_of(u.y, v[8 * i + 2], v[8 * i + 3]);
-        halves_of(u.z, v[8 * i + 4], v[8 * i + 5]), halves_of(u.w, v[8 * i + 6], v[8 * i + 7]);
+        for (int i = 0; i < 4; ++i) {
+          const uint4 u = shared_load16(row + ((i ^ (channel / 2 & 3)) << 4));
+          halves_of(u.x, v[8 * i], v[8 * i + 1]), halves_of(u.y, v[8 * i + 2], v[8 * i + 3]);
+          halves_of(u.z, v[8 * i + 4], v[8 * i + 5]), halves_of(u.w, v[8 * i + 6], v[8 * i + 7]);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_addr(&m->codes_empty[c.i]));
+        wait(m, &m->empty[s.i], s.phase ^ 1);
+        tc_fence_after();
+        tmem_store32(stages_at + s.i * kStageColumns, v);
+        tmem_wait_store();
+        // (one warp's arrival tells of this block's tokens too)
+        if ((warp & 3) == 0) wait(m, &m->x_full[x.i], x.phase);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(full0 + s.i * 8);
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_addr(&m->codes_empty[c.i]));
-      wait(m, &m->empty[s.i], s.phase ^ 1);
-      tc_fence_after();
-      tmem_store32(tmem + kAtStages + s.i * kStageColumns + half * 32 + (static_cast<uint32_t>((warp & 3) * 32) << 16), v);
-      tmem_wait_store();
-      // (one warp's arrival tells of this block's tokens too)
-      if (warp == 0) wait(m, &m->x_full[s.i], s.phase);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(full0 + s.i * 8);
+      mine ^= 1;
       c.step(g.codes_ring);
-      s.step(kStages);
+      s.step(g.stages);
+      x.step(g.x_ring);
     }
   }
 }
 
 // The products of both blocks (one warp of block 0).
-__device__ __forceinline__ void issue(const ProductParams& p, Misc* m, const Plan& g, int pair, uint32_t x_at, uint32_t tmem) {
+__device__ __forceinline__ void issue(Misc* m, const Plan& g, int pair, uint32_t x_at, uint32_t tmem) {
   const bool lead = elect_lane();
-  const uint32_t kind = product_kind(2 * kTileOut, g.tokens, false, true), half_tile = g.tokens / 2 * 128, x_bytes = 2 * half_tile;
-  Ring s, d;
+  const uint32_t kind = product_kind(2 * kTileOut, g.tokens, false, true), x_bytes = g.tokens * kTileIn;
+  const uint32_t stages_at = tmem + g.accumulators * g.sum_columns;
+  Ring s, x, d, r;
   Walk walk(g, pair);
   Piece q;
   while (walk.next(g, q)) {
-    const bool parts = in_parts(p, g, q);
+    wait(m, &m->ready_full[r.i], r.phase);
+    const bool parts = *const_cast<volatile int*>(&m->ready[r.i].parts) != 0;
+    __syncwarp();
+    if (lead) mbar_arrive(smem_addr(&m->ready_empty[r.i]));
+    r.step(2);
     for (int k = q.k0; k < q.k1; ++k) {
       const bool first = k == q.k0 || (parts && (k - q.k0) % kPart == 0);
       const bool end = k + 1 == q.k1 || (parts && (k + 1 - q.k0) % kPart == 0);
       if (first) wait(m, &m->sum_empty[d.i], d.phase ^ 1);
       wait(m, &m->full[s.i], s.phase);
       tc_fence_after();
-      const uint32_t a = tmem + kAtStages + s.i * kStageColumns, sum = tmem + d.i * (kAtStages / 2);
-      const uint64_t b0 = operand_k(x_at + s.i * x_bytes), b1 = operand_k(x_at + s.i * x_bytes + half_tile);
+      const uint32_t a = stages_at + s.i * kStageColumns, sum = tmem + d.i * g.sum_columns;
+      const uint64_t b = operand_k(x_at + x.i * x_bytes);
       if (lead) {
 #pragma unroll
-        for (int i = 0; i < kTileIn / 16; ++i) mma_ts_pair(sum, a + i * 8, (i < 4 ? b0 : b1) + (i & 3) * 2, kind, !first || i > 0);
+        for (int i = 0; i < kTileIn / 16; ++i) mma_ts_pair(sum, a + i * 8, b + i * 2, kind, !first || i > 0);
         mma_commit_pair(smem_addr(&m->empty[s.i]));
+        mma_commit_pair(smem_addr(&m->x_empty[x.i]));
         if (end) mma_commit_pair(smem_addr(&m->sum_full[d.i]));
       }
       __syncwarp();
-      s.step(kStages);
+      s.step(g.stages);
+      x.step(g.x_ring);
       if (end) d.step(g.accumulators);
     }
   }
@@ -272,36 +309,89 @@ __device__ __forceinline__ void issue(const ProductParams& p, Misc* m, const Pla
   __syncwarp();
 }
 
-// Results of a lane's channel and 32 tokens from t0 on. (Each step is rounded by
-// itself: the result is the same whichever way the sum was taken.)
+// A result from an exact sum. (Each step is rounded by itself: it is the same
+// whichever way the sum was taken.)
+__device__ __forceinline__ float result(const ProductParams& p, float sum, float token_scale, float channel_scale, float bias) {
+  const float y = __fmul_rn(__fmul_rn(sum, token_scale), channel_scale);
+  return p.bias ? __fadd_rn(y, bias) : y;
+}
+
+// Results of a lane's channel and 32 tokens from t0 on, of which `count` are there.
 template <typename T>
-__device__ __forceinline__ void finish(const ProductParams& p, int n, long long t0, int count, float scale, float bias, float (&v)[32]) {
-  const bool mine = n < p.w.out;
+__device__ __forceinline__ void finish(const ProductParams& p, int n, long long t0, int count, const float* token_scale, float scale, float bias,
+                                       float (&v)[32]) {
+  if (count <= 0 || n >= p.w.out) return;
+  float x[32];
   if (p.residual.p) {
+    // (rows behind the last one: the last one's)
     const T* r = static_cast<const T*>(p.residual.p) + t0 * p.residual.stride + n;
-    float x[32];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) x[j] = mine && j < count ? static_cast<float>(r[j * p.residual.stride]) : 0.0f;
+    for (int j = 0; j < 32; ++j) x[j] = static_cast<float>(r[min(j, count - 1) * p.residual.stride]);
+  }
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      const float sx = j < count ? __ldg(p.scale + t0 + j) : 0.0f;
-      v[j] = __fmul_rn(__fmul_rn(v[j], sx), scale);
-      if (p.bias) v[j] = __fadd_rn(v[j], bias);
-      v[j] = __fadd_rn(v[j], x[j]);
-    }
+  for (int j = 0; j < 32; j += 4) {
+    const float4 sx = *reinterpret_cast<const float4*>(token_scale + j);
+    v[j] = result(p, v[j], sx.x, scale, bias), v[j + 1] = result(p, v[j + 1], sx.y, scale, bias);
+    v[j + 2] = result(p, v[j + 2], sx.z, scale, bias), v[j + 3] = result(p, v[j + 3], sx.w, scale, bias);
+  }
+  if (p.residual.p) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = __fadd_rn(v[j], x[j]);
+  }
+  T* y = static_cast<T*>(p.y.p) + t0 * p.y.stride + n;
+  if (count >= 32) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) y[j * p.y.stride] = static_cast<T>(v[j]);
   } else {
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
-      const float sx = j < count ? __ldg(p.scale + t0 + j) : 0.0f;
-      v[j] = __fmul_rn(__fmul_rn(v[j], sx), scale);
-      if (p.bias) v[j] = __fadd_rn(v[j], bias);
+      if (j < count) y[j * p.y.stride] = static_cast<T>(v[j]);
     }
   }
-  if (!mine) return;
-  T* y = static_cast<T*>(p.y.p) + t0 * p.y.stride + n;
+}
+
+// Adds up the parts of shared tile `of` that the pairs from `first` to before
+// `after` left, and gives the results. A lane takes four neighbouring channels,
+// a warp every fourth token.
+template <typename T>
+__device__ __forceinline__ void join(const ProductParams& p, const Plan& g, const float* token_scale, int of, int first, int after, int rank, int n0,
+                                     long long t0, int tokens, int warp, long long slot_size) {
+  constexpr int kDeep = 8;
+  const int lane = threadIdx.x & 31, n = n0 + 4 * lane;
+  if (n >= p.w.out) return;
+  const float4 scale = __ldg(reinterpret_cast<const float4*>(p.w.scale + n));
+  float bias[4] = {};
+  if (p.bias) {
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    if (j < count) y[j * p.y.stride] = static_cast<T>(v[j]);
+    for (int i = 0; i < 4; ++i) bias[i] = n + i < p.w.out ? __ldg(p.bias + n + i) : 0.0f;
+  }
+  for (int c0 = warp; c0 < tokens; c0 += 4 * kDeep) {
+    int4 sum[kDeep];
+#pragma unroll
+    for (int j = 0; j < kDeep; ++j) sum[j] = make_int4(0, 0, 0, 0);
+    for (int other = first; other < after; ++other) {
+      const int slot = static_cast<int>(share_begin(g, other) / g.per_tile) == of ? 0 : 1;
+      const int32_t* from = g.slots + ((2ll * other + rank) * kSlots + slot) * slot_size + 4 * lane;
+      int4 v[kDeep];
+#pragma unroll
+      for (int j = 0; j < kDeep; ++j) v[j] = __ldcg(reinterpret_cast<const int4*>(from + min(c0 + 4 * j, tokens - 1) * kTileOut));
+#pragma unroll
+      for (int j = 0; j < kDeep; ++j) sum[j].x += v[j].x, sum[j].y += v[j].y, sum[j].z += v[j].z, sum[j].w += v[j].w;
+    }
+#pragma unroll
+    for (int j = 0; j < kDeep; ++j) {
+      const int c = c0 + 4 * j;
+      if (c >= tokens) continue;
+      const float sx = token_scale[c];
+      float v[4] = {result(p, __int2float_rn(sum[j].x), sx, scale.x, bias[0]), result(p, __int2float_rn(sum[j].y), sx, scale.y, bias[1]),
+                    result(p, __int2float_rn(sum[j].z), sx, scale.z, bias[2]), result(p, __int2float_rn(sum[j].w), sx, scale.w, bias[3])};
+      T* y = static_cast<T*>(p.y.p) + (t0 + c) * p.y.stride + n;
+      const T* r = static_cast<const T*>(p.residual.p) + (t0 + c) * p.residual.stride + n;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (n + i < p.w.out) y[i] = static_cast<T>(p.residual.p ? __fadd_rn(v[i], static_cast<float>(r[i])) : v[i]);
+      }
+    }
   }
 }
 
@@ -310,34 +400,40 @@ template <typename T>
 __device__ __forceinline__ void results(const ProductParams& p, Misc* m, const Plan& g, int pair, int rank, int warp, uint32_t tmem) {
   const int lane = threadIdx.x & 31, row = warp * 32 + lane;
   const uint32_t empty0 = cluster_addr(smem_addr(&m->sum_empty[0]), 0);
-  const long long slot_size = static_cast<long long>(g.tokens) * kTileOut;
-  auto slot_of = [&](int of_pair, int slot) { return g.slots + ((2ll * of_pair + rank) * kSlots + slot) * slot_size + row; };
-  Ring d;
+  const long long slot_size = static_cast<long long>((g.tokens + 31) / 32 * 32) * kTileOut;
+  Ring d, r;
   Walk walk(g, pair);
   Piece q;
   while (walk.next(g, q)) {
-    const bool parts = in_parts(p, g, q), whole = q.k1 - q.k0 == g.per_tile;
-    const int n = (q.channel * 2 + rank) * kTileOut + row;
+    const bool whole = q.k1 - q.k0 == g.per_tile;
+    const int n0 = (q.channel * 2 + rank) * kTileOut, n = n0 + row;
     const long long t0 = static_cast<long long>(q.token) * g.tokens;
     const int tokens = static_cast<int>(min(static_cast<long long>(g.tokens), p.rows - t0));
     const float scale = __ldg(p.w.scale + n), bias = p.bias && n < p.w.out ? __ldg(p.bias + n) : 0.0f;
-    const int mine = static_cast<int>(share_begin(g, pair) / g.per_tile) == q.tile - g.whole ? 0 : 1;
-    int32_t* sum = slot_of(pair, 2);
-    int32_t* left = slot_of(pair, mine);
-    const int turns = parts ? (q.k1 - q.k0 + kPart - 1) / kPart : 1;
+    int32_t* mine = g.slots + (2ll * pair + rank) * kSlots * slot_size + row;
+    int32_t* sum = mine + 2 * slot_size;
+    int32_t* left = static_cast<int>(share_begin(g, pair) / g.per_tile) == q.tile - g.whole ? mine : mine + slot_size;
+    wait(m, &m->ready_full[r.i], r.phase);
+    const Ready& ready = m->ready[r.i];
+    const int turns = ready.parts ? (q.k1 - q.k0 + kPart - 1) / kPart : 1;
     for (int turn = 0; turn < turns; ++turn) {
       wait(m, &m->sum_full[d.i], d.phase);
       tc_fence_after();
       for (int c = 0; c < g.tokens; c += 32) {
         uint32_t u[32];
-        tmem_load32(tmem + d.i * (kAtStages / 2) + c + (static_cast<uint32_t>(warp * 32) << 16), u);
+        __syncwarp();
+        tmem_load32(tmem + d.i * g.sum_columns + c + (static_cast<uint32_t>(warp * 32) << 16), u);
         tmem_wait_load(u);
-        const int columns = min(32, g.tokens - c);
+        if (c + 32 >= g.tokens) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(empty0 + d.i * 8);
+        }
+        float f[32];
         if (turns == 1 && whole) {
-          float v[32];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(u[j]);
-          finish<T>(p, n, t0 + c, tokens - c, scale, bias, v);
+          for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(u[j]);
+          finish<T>(p, n, t0 + c, tokens - c, ready.scale + c, scale, bias, f);
           continue;
         }
         int v[32];
@@ -345,57 +441,41 @@ __device__ __forceinline__ void results(const ProductParams& p, Misc* m, const P
         for (int j = 0; j < 32; ++j) v[j] = __float2int_rn(__uint_as_float(u[j]));
         if (turn > 0) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] += j < columns ? sum[static_cast<long long>(c + j) * kTileOut] : 0;
+          for (int j = 0; j < 32; ++j) v[j] += sum[(c + j) * kTileOut];
         }
         if (turn + 1 < turns || !whole) {
           int32_t* to = turn + 1 < turns ? sum : left;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            if (j < columns) to[static_cast<long long>(c + j) * kTileOut] = v[j];
-          }
+          for (int j = 0; j < 32; ++j) to[(c + j) * kTileOut] = v[j];
         } else {
-          float f[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) f[j] = __int2float_rn(v[j]);
-          finish<T>(p, n, t0 + c, tokens - c, scale, bias, f);
+          finish<T>(p, n, t0 + c, tokens - c, ready.scale + c, scale, bias, f);
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(empty0 + d.i * 8);
       d.step(g.accumulators);
     }
-    if (whole) continue;
-    // the last of the tile's pairs to be done adds its parts up
-    const int of = q.tile - g.whole;
-    const long long begin = static_cast<long long>(of) * g.per_tile, end = begin + g.per_tile;
-    int first = static_cast<int>(begin * g.shares / g.units);
-    while (share_begin(g, first + 1) <= begin) ++first;
-    while (share_begin(g, first) > begin) --first;
-    int after = first + 1;
-    while (after < g.shares && share_begin(g, after) < end) ++after;
-    named_barrier(1, 128);
-    if (warp == 0 && lane == 0) {
-      __threadfence();
-      m->last = atomicAdd(&g.counters[2 * of + rank], 1) == after - first - 1;
-      __threadfence();
-    }
-    named_barrier(1, 128);
-    if (!*const_cast<volatile int*>(&m->last)) continue;
-    for (int c = 0; c < tokens; c += 32) {
-      int v[32] = {};
-      const int columns = min(32, g.tokens - c);
-      for (int other = first; other < after; ++other) {
-        const int slot = static_cast<int>(share_begin(g, other) / g.per_tile) == of ? 0 : 1;
-        const int32_t* from = slot_of(other, slot);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] += j < columns ? __ldcg(from + static_cast<long long>(c + j) * kTileOut) : 0;
+    if (!whole) {
+      // the last of the tile's pairs to be done adds its parts up
+      const int of = q.tile - g.whole;
+      const long long begin = static_cast<long long>(of) * g.per_tile, end = begin + g.per_tile;
+      int first = static_cast<int>(begin * g.shares / g.units);
+      while (share_begin(g, first + 1) <= begin) ++first;
+      while (share_begin(g, first) > begin) --first;
+      int after = first + 1;
+      while (after < g.shares && share_begin(g, after) < end) ++after;
+      named_barrier(1, 128);
+      if (warp == 0 && lane == 0) {
+        __threadfence();
+        m->last = atomicAdd(&g.counters[2 * of + rank], 1) == after - first - 1;
+        __threadfence();
       }
-      float f[32];
-#pragma unroll
-      for (int j = 0; j < 32; ++j) f[j] = __int2float_rn(v[j]);
-      finish<T>(p, n, t0 + c, tokens - c, scale, bias, f);
+      named_barrier(1, 128);
+      if (*const_cast<volatile int*>(&m->last)) join<T>(p, g, ready.scale, of, first, after, rank, n0, t0, tokens, warp, slot_size);
     }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_addr(&m->ready_empty[r.i]));
+    r.step(2);
   }
 }
 
@@ -407,11 +487,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), rank = static_cast<int>(cluster_rank()), pair = blockIdx.x / 2;
   if (warp == 3) tmem_alloc_pair(smem_addr(&m->tmem), kTmemColumns);
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kMostCodes; ++i) mbar_init(smem_addr(&m->codes_full[i]), 1), mbar_init(smem_addr(&m->codes_empty[i]), 8);
+    for (int i = 0; i < kMostCodes; ++i) mbar_init(smem_addr(&m->codes_full[i]), 1), mbar_init(smem_addr(&m->codes_empty[i]), 4);
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(smem_addr(&m->x_full[i]), 1), mbar_init(smem_addr(&m->full[i]), 16), mbar_init(smem_addr(&m->empty[i]), 1);
+      mbar_init(smem_addr(&m->x_full[i]), 1), mbar_init(smem_addr(&m->x_empty[i]), 1);
+      mbar_init(smem_addr(&m->full[i]), 8), mbar_init(smem_addr(&m->empty[i]), 1);
     }
-    for (int i = 0; i < 2; ++i) mbar_init(smem_addr(&m->sum_full[i]), 1), mbar_init(smem_addr(&m->sum_empty[i]), 8);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_addr(&m->sum_full[i]), 1), mbar_init(smem_addr(&m->sum_empty[i]), 8);
+      mbar_init(smem_addr(&m->ready_full[i]), 1), mbar_init(smem_addr(&m->ready_empty[i]), rank == 0 ? 5 : 4);
+    }
     mbar_init(smem_addr(&m->drained), 1);
     m->abort = 0;
     fence_barrier_init();
@@ -432,16 +516,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     }
     __syncwarp();
   } else if (warp == 1) {
-    const uint32_t bytes = static_cast<uint32_t>(g.tokens) * 128;
+    const uint32_t bytes = static_cast<uint32_t>(g.tokens) * kTileIn;
     if (elect_lane()) {
-      copy_tiles(m, g, pair, x_at, kStages, bytes, m->x_full, m->empty,
+      copy_tiles(m, g, pair, x_at, g.x_ring, bytes, m->x_full, m->x_empty,
                  [&](const Piece& q) { return g.x + static_cast<long long>(q.token * 2 + rank) * g.per_tile * bytes; });
     }
     __syncwarp();
   } else if (warp == 2) {
-    if (rank == 0) issue(p, m, g, pair, x_at, tmem);
+    if (rank == 0) issue(m, g, pair, x_at, tmem);
   } else if (warp == 3) {
     let_next_start();
+    prepare(p, m, g, pair);
   } else if (warp < 12) {
     convert(m, g, pair, warp - 4, smem, tmem);
   } else {
@@ -464,8 +549,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 }
 
 // The tokens' codes in fp16, in the order in which the product's tiles lie in
-// shared memory (the 128-byte swizzle), the sum of each token's squares, and the
-// counters of shared tiles. A block takes a token.
+// shared memory (rows of 128 bytes, the 128-byte swizzle), the sum of each token's
+// squares, and the counters of shared tiles. A block takes a token.
 __global__ void __launch_bounds__(256) spread_kernel(const ProductParams p, const Plan g, unsigned char* x, uint32_t* squares) {
   __shared__ uint32_t words[8];
   wait_for_previous();
@@ -476,7 +561,7 @@ __global__ void __launch_bounds__(256) spread_kernel(const ProductParams p, cons
   }
   const int8_t* from = p.codes + t * p.codes_stride;
   const int tile = t / g.tokens, r = t - tile * g.tokens, of_half = r / half, row = r - of_half * half;
-  unsigned char* to = x + static_cast<long long>(tile * 2 + of_half) * g.per_tile * half * 256 + row * 128;
+  unsigned char* to = x + static_cast<long long>(tile * 2 + of_half) * g.per_tile * half * 128 + row * 128;
   const bool wide = reinterpret_cast<uintptr_t>(from) % 16 == 0;
   uint32_t sum = 0;
   for (int k = threadIdx.x * 16; k < g.per_tile * kTileIn; k += 256 * 16) {
@@ -496,8 +581,8 @@ __global__ void __launch_bounds__(256) spread_kernel(const ProductParams p, cons
       sum = __dp4a(static_cast<int>(c[i]), static_cast<int>(c[i]), static_cast<int>(sum));
       halves_of(c[i] ^ 0x80808080u, h[2 * i], h[2 * i + 1]);
     }
-    unsigned char* at = to + (static_cast<long long>(k / kTileIn) * 2 + (k % kTileIn) / 64) * half * 128;
-    const int piece = (k % 64) / 8;
+    unsigned char* at = to + static_cast<long long>(k / kTileIn) * half * 128;
+    const int piece = (k % kTileIn) / 8;
     *reinterpret_cast<uint4*>(at + ((piece ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
     *reinterpret_cast<uint4*>(at + (((piece + 1) ^ (row & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
   }
@@ -519,21 +604,25 @@ Plan plan_of(int rows, const Packed& w, int sms, Scratch* at) {
   g.pairs = min(sms / 2, kMaxPairs);
   g.channel_tiles = w.tiles_out / 2;
   g.per_tile = w.tiles_in;
-  g.token_tiles = static_cast<int>((static_cast<long long>(rows) + kMostTokens - 1) / kMostTokens);
+  const int most = rows <= kMostTokens ? kMostTokens : kTwoSums;
+  g.token_tiles = static_cast<int>((static_cast<long long>(rows) + most - 1) / most);
   g.tokens = ((rows + g.token_tiles - 1) / g.token_tiles + 15) / 16 * 16;
-  g.accumulators = g.tokens <= kAtStages / 2 ? 2 : 1;
-  g.codes_ring = min(kMostCodes, static_cast<int>((kAtMisc - kStages * g.tokens * 128) / kTileBytes));
+  g.accumulators = g.tokens <= kTwoSums ? 2 : 1;
+  g.sum_columns = (g.tokens + 31) / 32 * 32;
+  g.stages = min(kStages, (kTmemColumns - g.accumulators * g.sum_columns) / kStageColumns);
+  g.x_ring = kStages;
+  g.codes_ring = min(kMostCodes, static_cast<int>((kAtMisc - g.x_ring * g.tokens * kTileIn) / kTileBytes));
   const long long tiles = static_cast<long long>(g.channel_tiles) * g.token_tiles;
   // whole tiles as long as they go round, but for the last round; one round and what is left over are cut up
   const long long rounds = tiles % g.pairs == 0 ? tiles / g.pairs : max(0ll, tiles / g.pairs - 1);
   g.whole = static_cast<int>(rounds * g.pairs);
   g.units = (tiles - g.whole) * g.per_tile;
-  g.shares = static_cast<int>(min(static_cast<long long>(g.pairs), max(1ll, g.units / 2)));
+  g.shares = static_cast<int>(min(static_cast<long long>(g.pairs), max(1ll, g.units / 4)));
   at->squares = 4096;
   static_assert(4 * kMaxPairs * sizeof(int32_t) <= 4096, "counters");
   at->x = at->squares + (static_cast<size_t>(rows) * sizeof(uint32_t) + 255) / 256 * 256;
   at->slots = at->x + static_cast<size_t>(g.token_tiles) * g.tokens * g.per_tile * kTileIn * sizeof(__half);
-  at->bytes = at->slots + 2 * static_cast<size_t>(g.pairs) * kSlots * g.tokens * kTileOut * sizeof(int32_t);
+  at->bytes = at->slots + 2 * static_cast<size_t>(g.pairs) * kSlots * g.sum_columns * kTileOut * sizeof(int32_t);
   return g;
 }
 

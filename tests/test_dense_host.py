@@ -25,7 +25,7 @@ def test_sizes(lib):
     assert dense._ROWS.size == 16
     size = lib.sjd_weight_size
     # a byte a code, channels and features filled up, and 256 bytes and 8 a channel beside them
-    assert size(1, 1) == 256 + 256 * 8 + 256 * 128
+    assert size(1, 1) == 256 + 256 * 8 + 256 * 64
     assert size(4096, 4096) == 256 + 4096 * 8 + 4096 * 4096
     assert size(1 << 24, 65536) == 256 + (1 << 27) + (1 << 40)
     for out, dim in ((0, 1), (1, 0), (-1, 5), ((1 << 24) + 1, 1), (1, 65537)):
