@@ -74,23 +74,26 @@ struct Plan {
   int pairs, channel_tiles, token_tiles, per_tile;  // pairs of blocks; tiles of 256 channels; of tokens; feature tiles
   int tokens, codes_ring, x_ring, stages;           // tokens of a tile; tiles in shared memory, of codes in tensor memory
   int accumulators, sum_columns;                    // columns from one accumulator to the next
-  int whole, shares;                                // shares: pairs that the rest is cut up for
-  long long units;
+  int whole, shares, units;                         // shares: pairs that the rest is cut up for
+  int share, longer;                                // units of a share; shares that have one more
   const unsigned char* x;                           // the tokens' codes in fp16
   const uint32_t* squares;                          // of each token's codes
   int32_t* slots;
   int32_t* counters;
 };
 
-__host__ __device__ __forceinline__ long long share_begin(const Plan& g, int share) { return g.units * share / g.shares; }
+__device__ __forceinline__ int share_begin(const Plan& g, int share) { return share * g.share + min(share, g.longer); }
+__device__ __forceinline__ int share_of(const Plan& g, int unit) {
+  const int of_longer = g.longer * (g.share + 1);
+  return unit < of_longer ? unit / (g.share + 1) : g.longer + (unit - of_longer) / g.share;
+}
 
 // One piece of work: feature tiles k0 .. k1 - 1 of a tile.
 struct Piece {
   int tile, channel, token, k0, k1;   // (channel, token: numbers of tiles)
 };
 struct Walk {
-  int tile;
-  long long at, end;
+  int tile, at, end;
   __device__ __forceinline__ Walk(const Plan& g, int pair) : tile(pair), at(0), end(0) {
     if (pair < g.shares) at = share_begin(g, pair), end = share_begin(g, pair + 1);
   }
@@ -99,10 +102,10 @@ struct Walk {
       p.tile = tile, p.k0 = 0, p.k1 = g.per_tile;
       tile += g.pairs;
     } else if (at < end) {
-      const int t = static_cast<int>(at / g.per_tile);
+      const int t = at / g.per_tile;
       p.tile = g.whole + t;
-      p.k0 = static_cast<int>(at - static_cast<long long>(t) * g.per_tile);
-      p.k1 = static_cast<int>(min(static_cast<long long>(g.per_tile), p.k0 + (end - at)));
+      p.k0 = at - t * g.per_tile;
+      p.k1 = min(g.per_tile, p.k0 + end - at);
       at += p.k1 - p.k0;
     } else {
       return false;
@@ -230,43 +233,58 @@ __device__ __forceinline__ void halves_of(uint32_t codes, uint32_t& lo, uint32_t
   lo = *reinterpret_cast<const uint32_t*>(&x), hi = *reinterpret_cast<const uint32_t*>(&y);
 }
 
-// Warps 0 to 3 take every other tile, warps 4 to 7 those between; a lane a channel.
+// Warps 0 to 3 take every other tile, warps 4 to 7 those between; a lane a
+// channel. The next tile's codes are loaded while this one's fp16 is on its way
+// into tensor memory.
 __device__ __forceinline__ void convert(Misc* m, const Plan& g, int pair, int warp, uint32_t codes_at, uint32_t tmem) {
-  const int lane = threadIdx.x & 31, turn = warp / 4, channel = (warp & 3) * 32 + lane;
+  const int lane = threadIdx.x & 31, channel = (warp & 3) * 32 + lane, turn = warp / 4;
   const uint32_t full0 = cluster_addr(smem_addr(&m->full[0]), 0), stages_at = tmem + g.accumulators * g.sum_columns + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+  const uint32_t row = codes_at + channel * kTileIn, swap = (channel / 2 & 3) << 4;
+  int left = 0;   // tiles of all pieces
+  {
+    Walk walk(g, pair);
+    Piece q;
+    while (walk.next(g, q)) left += q.k1 - q.k0;
+  }
+  left -= turn;
+  if (left <= 0) return;
   Ring c, s, x;
-  int mine = 0;
-  Walk walk(g, pair);
-  Piece q;
-  while (walk.next(g, q)) {
-    for (int k = q.k0; k < q.k1; ++k) {
-      if (mine == turn) {
-        wait(m, &m->codes_full[c.i], c.phase);
-        const uint32_t row = codes_at + c.i * kTileBytes + channel * kTileIn;
-        uint32_t v[32];
+  if (turn) c.step(g.codes_ring), s.step(g.stages), x.step(g.x_ring);
+  uint4 u[4];
+  auto load = [&]() {
+    wait(m, &m->codes_full[c.i], c.phase);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint4 u = shared_load16(row + ((i ^ (channel / 2 & 3)) << 4));
-          halves_of(u.x, v[8 * i], v[8 * i + 1]), halves_of(u.y, v[8 * i + 2], v[8 * i + 3]);
-          halves_of(u.z, v[8 * i + 4], v[8 * i + 5]), halves_of(u.w, v[8 * i + 6], v[8 * i + 7]);
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_addr(&m->codes_empty[c.i]));
-        wait(m, &m->empty[s.i], s.phase ^ 1);
-        tc_fence_after();
-        tmem_store32(stages_at + s.i * kStageColumns, v);
-        tmem_wait_store();
-        // (one warp's arrival tells of this block's tokens too)
-        if ((warp & 3) == 0) wait(m, &m->x_full[x.i], x.phase);
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(full0 + s.i * 8);
-      }
-      mine ^= 1;
-      c.step(g.codes_ring);
-      s.step(g.stages);
-      x.step(g.x_ring);
+    for (int i = 0; i < 4; ++i) u[i] = shared_load16(row + c.i * kTileBytes + ((i << 4) ^ swap));
+  };
+  load();
+  for (;;) {
+    uint32_t v[32];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      halves_of(u[i].x, v[8 * i], v[8 * i + 1]), halves_of(u[i].y, v[8 * i + 2], v[8 * i + 3]);
+      halves_of(u[i].z, v[8 * i + 4], v[8 * i + 5]), halves_of(u[i].w, v[8 * i + 6], v[8 * i + 7]);
     }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_addr(&m->codes_empty[c.i]));
+    wait(m, &m->empty[s.i], s.phase ^ 1);
+    tc_fence_after();
+    __syncwarp();
+    tmem_store32(stages_at + s.i * kStageColumns, v);
+    left -= 2;
+    if (left > 0) {
+      c.step(g.codes_ring), c.step(g.codes_ring);
+      load();
+    }
+    __syncwarp();
+    tmem_wait_store();
+    // (one warp's arrival tells of this block's tokens too)
+    if ((warp & 3) == 0) wait(m, &m->x_full[x.i], x.phase);
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive_cluster(full0 + s.i * 8);
+    if (left <= 0) return;
+    s.step(g.stages), s.step(g.stages);
+    x.step(g.x_ring), x.step(g.x_ring);
   }
 }
 
@@ -310,57 +328,52 @@ __device__ __forceinline__ void issue(Misc* m, const Plan& g, int pair, uint32_t
 }
 
 // A result from an exact sum. (Each step is rounded by itself: it is the same
-// whichever way the sum was taken.)
-__device__ __forceinline__ float result(const ProductParams& p, float sum, float token_scale, float channel_scale, float bias) {
-  const float y = __fmul_rn(__fmul_rn(sum, token_scale), channel_scale);
-  return p.bias ? __fadd_rn(y, bias) : y;
+// whichever way the sum was taken. Without a bias, -0 is added, which changes nothing.)
+__device__ __forceinline__ float result(float sum, float token_scale, float channel_scale, float bias) {
+  return __fadd_rn(__fmul_rn(__fmul_rn(sum, token_scale), channel_scale), bias);
 }
 
-// Results of a lane's channel and 32 tokens from t0 on, of which `count` are there.
+constexpr int kColumns = 16;   // of an accumulator that are read at once
+
+// Results of a lane's channel and kColumns tokens from t0 on, of which `count` are there.
 template <typename T>
 __device__ __forceinline__ void finish(const ProductParams& p, int n, long long t0, int count, const float* token_scale, float scale, float bias,
-                                       float (&v)[32]) {
+                                       float (&v)[kColumns]) {
   if (count <= 0 || n >= p.w.out) return;
-  float x[32];
+#pragma unroll
+  for (int j = 0; j < kColumns; j += 4) {
+    const float4 sx = *reinterpret_cast<const float4*>(token_scale + j);
+    v[j] = result(v[j], sx.x, scale, bias), v[j + 1] = result(v[j + 1], sx.y, scale, bias);
+    v[j + 2] = result(v[j + 2], sx.z, scale, bias), v[j + 3] = result(v[j + 3], sx.w, scale, bias);
+  }
   if (p.residual.p) {
     // (rows behind the last one: the last one's)
     const T* r = static_cast<const T*>(p.residual.p) + t0 * p.residual.stride + n;
+    T x[kColumns];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) x[j] = static_cast<float>(r[min(j, count - 1) * p.residual.stride]);
-  }
+    for (int j = 0; j < kColumns; ++j) x[j] = r[min(j, count - 1) * p.residual.stride];
 #pragma unroll
-  for (int j = 0; j < 32; j += 4) {
-    const float4 sx = *reinterpret_cast<const float4*>(token_scale + j);
-    v[j] = result(p, v[j], sx.x, scale, bias), v[j + 1] = result(p, v[j + 1], sx.y, scale, bias);
-    v[j + 2] = result(p, v[j + 2], sx.z, scale, bias), v[j + 3] = result(p, v[j + 3], sx.w, scale, bias);
-  }
-  if (p.residual.p) {
-#pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = __fadd_rn(v[j], x[j]);
+    for (int j = 0; j < kColumns; ++j) v[j] = __fadd_rn(v[j], static_cast<float>(x[j]));
   }
   T* y = static_cast<T*>(p.y.p) + t0 * p.y.stride + n;
-  if (count >= 32) {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) y[j * p.y.stride] = static_cast<T>(v[j]);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      if (j < count) y[j * p.y.stride] = static_cast<T>(v[j]);
-    }
+  for (int j = 0; j < kColumns; ++j) {
+    if (j < count) *y = static_cast<T>(v[j]);
+    y += p.y.stride;
   }
 }
 
-// Adds up the parts of shared tile `of` that the pairs from `first` to before
-// `after` left, and gives the results. A lane takes four neighbouring channels,
-// a warp every fourth token.
+// Adds up the parts of a shared tile, whose first unit is `begin`, that the pairs from
+// `first` to before `after` left, and gives the results. A lane takes four
+// neighbouring channels, a warp every fourth token.
 template <typename T>
-__device__ __forceinline__ void join(const ProductParams& p, const Plan& g, const float* token_scale, int of, int first, int after, int rank, int n0,
+__device__ __forceinline__ void join(const ProductParams& p, const Plan& g, const float* token_scale, int begin, int first, int after, int rank, int n0,
                                      long long t0, int tokens, int warp, long long slot_size) {
-  constexpr int kDeep = 8;
+  constexpr int kDeep = 4;
   const int lane = threadIdx.x & 31, n = n0 + 4 * lane;
   if (n >= p.w.out) return;
   const float4 scale = __ldg(reinterpret_cast<const float4*>(p.w.scale + n));
-  float bias[4] = {};
+  float bias[4] = {-0.0f, -0.0f, -0.0f, -0.0f};
   if (p.bias) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) bias[i] = n + i < p.w.out ? __ldg(p.bias + n + i) : 0.0f;
@@ -369,8 +382,9 @@ __device__ __forceinline__ void join(const ProductParams& p, const Plan& g, cons
     int4 sum[kDeep];
 #pragma unroll
     for (int j = 0; j < kDeep; ++j) sum[j] = make_int4(0, 0, 0, 0);
+#pragma unroll 4
     for (int other = first; other < after; ++other) {
-      const int slot = static_cast<int>(share_begin(g, other) / g.per_tile) == of ? 0 : 1;
+      const int slot = share_begin(g, other) >= begin ? 0 : 1;
       const int32_t* from = g.slots + ((2ll * other + rank) * kSlots + slot) * slot_size + 4 * lane;
       int4 v[kDeep];
 #pragma unroll
@@ -383,95 +397,100 @@ __device__ __forceinline__ void join(const ProductParams& p, const Plan& g, cons
       const int c = c0 + 4 * j;
       if (c >= tokens) continue;
       const float sx = token_scale[c];
-      float v[4] = {result(p, __int2float_rn(sum[j].x), sx, scale.x, bias[0]), result(p, __int2float_rn(sum[j].y), sx, scale.y, bias[1]),
-                    result(p, __int2float_rn(sum[j].z), sx, scale.z, bias[2]), result(p, __int2float_rn(sum[j].w), sx, scale.w, bias[3])};
+      float v[4] = {result(__int2float_rn(sum[j].x), sx, scale.x, bias[0]), result(__int2float_rn(sum[j].y), sx, scale.y, bias[1]),
+                    result(__int2float_rn(sum[j].z), sx, scale.z, bias[2]), result(__int2float_rn(sum[j].w), sx, scale.w, bias[3])};
       T* y = static_cast<T*>(p.y.p) + (t0 + c) * p.y.stride + n;
-      const T* r = static_cast<const T*>(p.residual.p) + (t0 + c) * p.residual.stride + n;
+      if (p.residual.p) {
+        const T* r = static_cast<const T*>(p.residual.p) + (t0 + c) * p.residual.stride + n;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (n + i < p.w.out) v[i] = __fadd_rn(v[i], static_cast<float>(r[i]));
+        }
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (n + i < p.w.out) y[i] = static_cast<T>(p.residual.p ? __fadd_rn(v[i], static_cast<float>(r[i])) : v[i]);
+        if (n + i < p.w.out) y[i] = static_cast<T>(v[i]);
       }
     }
   }
+}
+
+__device__ __forceinline__ int count_one(int32_t* at) {
+  int old;
+  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(old) : "l"(at) : "memory");
+  return old;
 }
 
 // Four warps read the accumulators, a lane a channel.
 template <typename T>
 __device__ __forceinline__ void results(const ProductParams& p, Misc* m, const Plan& g, int pair, int rank, int warp, uint32_t tmem) {
   const int lane = threadIdx.x & 31, row = warp * 32 + lane;
-  const uint32_t empty0 = cluster_addr(smem_addr(&m->sum_empty[0]), 0);
-  const long long slot_size = static_cast<long long>((g.tokens + 31) / 32 * 32) * kTileOut;
+  const uint32_t empty0 = cluster_addr(smem_addr(&m->sum_empty[0]), 0), sums_at = tmem + (static_cast<uint32_t>(warp * 32) << 16);
+  const long long slot_size = static_cast<long long>(g.sum_columns) * kTileOut;
+  int32_t* const slots = g.slots + (2ll * pair + rank) * kSlots * slot_size + row;
   Ring d, r;
   Walk walk(g, pair);
   Piece q;
   while (walk.next(g, q)) {
     const bool whole = q.k1 - q.k0 == g.per_tile;
-    const int n0 = (q.channel * 2 + rank) * kTileOut, n = n0 + row;
+    const int n0 = (q.channel * 2 + rank) * kTileOut, n = n0 + row, begin = (q.tile - g.whole) * g.per_tile;
     const long long t0 = static_cast<long long>(q.token) * g.tokens;
     const int tokens = static_cast<int>(min(static_cast<long long>(g.tokens), p.rows - t0));
-    const float scale = __ldg(p.w.scale + n), bias = p.bias && n < p.w.out ? __ldg(p.bias + n) : 0.0f;
-    int32_t* mine = g.slots + (2ll * pair + rank) * kSlots * slot_size + row;
-    int32_t* sum = mine + 2 * slot_size;
-    int32_t* left = static_cast<int>(share_begin(g, pair) / g.per_tile) == q.tile - g.whole ? mine : mine + slot_size;
+    const float scale = __ldg(p.w.scale + n), bias = p.bias && n < p.w.out ? __ldg(p.bias + n) : -0.0f;
     wait(m, &m->ready_full[r.i], r.phase);
     const Ready& ready = m->ready[r.i];
     const int turns = ready.parts ? (q.k1 - q.k0 + kPart - 1) / kPart : 1;
     for (int turn = 0; turn < turns; ++turn) {
+      const bool last = turn + 1 == turns;
+      // (the sum of the parts so far, and in the end what is left for the pair that joins the tile)
+      int32_t* const sum = slots + 2 * slot_size;
+      int32_t* const to = last ? slots + (share_begin(g, pair) >= begin ? 0 : slot_size) : sum;
       wait(m, &m->sum_full[d.i], d.phase);
       tc_fence_after();
-      for (int c = 0; c < g.tokens; c += 32) {
-        uint32_t u[32];
-        __syncwarp();
-        tmem_load32(tmem + d.i * g.sum_columns + c + (static_cast<uint32_t>(warp * 32) << 16), u);
+      __syncwarp();
+      uint32_t u[kColumns];
+      tmem_load16(sums_at + d.i * g.sum_columns, u);
+#pragma unroll 1
+      for (int c = 0; c < g.tokens; c += kColumns) {
         tmem_wait_load(u);
-        if (c + 32 >= g.tokens) {
+        float f[kColumns];
+#pragma unroll
+        for (int j = 0; j < kColumns; ++j) f[j] = __uint_as_float(u[j]);
+        __syncwarp();
+        if (c + kColumns < g.tokens) {
+          tmem_load16(sums_at + d.i * g.sum_columns + c + kColumns, u);
+        } else {
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(empty0 + d.i * 8);
         }
-        float f[32];
-        if (turns == 1 && whole) {
+        if (turns > 1 || !whole) {
+          int v[kColumns];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(u[j]);
-          finish<T>(p, n, t0 + c, tokens - c, ready.scale + c, scale, bias, f);
-          continue;
+          for (int j = 0; j < kColumns; ++j) v[j] = __float2int_rn(f[j]);
+          if (turn > 0) {
+#pragma unroll
+            for (int j = 0; j < kColumns; ++j) v[j] += sum[(c + j) * kTileOut];
+          }
+          if (!last || !whole) {
+#pragma unroll
+            for (int j = 0; j < kColumns; ++j) to[(c + j) * kTileOut] = v[j];
+            continue;
+          }
+#pragma unroll
+          for (int j = 0; j < kColumns; ++j) f[j] = __int2float_rn(v[j]);
         }
-        int v[32];
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = __float2int_rn(__uint_as_float(u[j]));
-        if (turn > 0) {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] += sum[(c + j) * kTileOut];
-        }
-        if (turn + 1 < turns || !whole) {
-          int32_t* to = turn + 1 < turns ? sum : left;
-#pragma unroll
-          for (int j = 0; j < 32; ++j) to[(c + j) * kTileOut] = v[j];
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) f[j] = __int2float_rn(v[j]);
-          finish<T>(p, n, t0 + c, tokens - c, ready.scale + c, scale, bias, f);
-        }
+        finish<T>(p, n, t0 + c, tokens - c, ready.scale + c, scale, bias, f);
       }
       d.step(g.accumulators);
     }
     if (!whole) {
       // the last of the tile's pairs to be done adds its parts up
-      const int of = q.tile - g.whole;
-      const long long begin = static_cast<long long>(of) * g.per_tile, end = begin + g.per_tile;
-      int first = static_cast<int>(begin * g.shares / g.units);
-      while (share_begin(g, first + 1) <= begin) ++first;
-      while (share_begin(g, first) > begin) --first;
-      int after = first + 1;
-      while (after < g.shares && share_begin(g, after) < end) ++after;
+      const int first = share_of(g, begin), after = share_of(g, begin + g.per_tile - 1) + 1;
       named_barrier(1, 128);
-      if (warp == 0 && lane == 0) {
-        __threadfence();
-        m->last = atomicAdd(&g.counters[2 * of + rank], 1) == after - first - 1;
-        __threadfence();
-      }
+      if (warp == 0 && lane == 0) m->last = count_one(&g.counters[2 * (q.tile - g.whole) + rank]) == after - first - 1;
       named_barrier(1, 128);
-      if (*const_cast<volatile int*>(&m->last)) join<T>(p, g, ready.scale, of, first, after, rank, n0, t0, tokens, warp, slot_size);
+      if (*const_cast<volatile int*>(&m->last)) join<T>(p, g, ready.scale, begin, first, after, rank, n0, t0, tokens, warp, slot_size);
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_addr(&m->ready_empty[r.i]));
@@ -616,8 +635,10 @@ Plan plan_of(int rows, const Packed& w, int sms, Scratch* at) {
   // whole tiles as long as they go round, but for the last round; one round and what is left over are cut up
   const long long rounds = tiles % g.pairs == 0 ? tiles / g.pairs : max(0ll, tiles / g.pairs - 1);
   g.whole = static_cast<int>(rounds * g.pairs);
-  g.units = (tiles - g.whole) * g.per_tile;
-  g.shares = static_cast<int>(min(static_cast<long long>(g.pairs), max(1ll, g.units / 4)));
+  g.units = static_cast<int>(tiles - g.whole) * g.per_tile;
+  g.shares = min(g.pairs, max(1, g.units / 4));
+  g.share = g.units / g.shares;
+  g.longer = g.units % g.shares;
   at->squares = 4096;
   static_assert(4 * kMaxPairs * sizeof(int32_t) <= 4096, "counters");
   at->x = at->squares + (static_cast<size_t>(rows) * sizeof(uint32_t) + 255) / 256 * 256;
