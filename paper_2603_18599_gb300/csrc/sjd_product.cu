@@ -64,8 +64,10 @@ constexpr int kMostCodes = 24, kStages = 8;     // most tiles on their way: code
 constexpr uint32_t kAtMisc = 224 * 1024;        // (the ring of codes, then that of the tokens)
 constexpr int kSlots = 3;                       // what a block leaves of up to two tiles that others have a part in, and the sum of a tile's parts
 constexpr int kMaxPairs = 80;
-constexpr int kThreads = 512;
+constexpr int kConvert = 4, kResults = 12;       // the first warps that convert codes, that give results: eight each
+constexpr int kThreads = 640;
 constexpr long long kWaitClocks = 4000000000ll; // about two seconds
+constexpr uint32_t kAsleep = 100000;            // (0.1 ms: warps that wait leave the others the issue slots)
 
 // How a call is shared out. The first `whole` tiles go round the pairs of blocks; the
 // feature tiles of the others, `units`, are cut into equal runs, so that no
@@ -133,7 +135,7 @@ struct Misc {
   unsigned long long drained;
   uint32_t tmem;
   int abort;
-  int last;
+  int others[2], last;   // whether the others' parts are there (by the shared piece's number modulo 2), all are
   Ready ready[2];
 };
 
@@ -141,7 +143,7 @@ __device__ __forceinline__ void wait(Misc* m, unsigned long long* bar, uint32_t 
   const uint32_t at = smem_addr(bar);
   if (mbar_try(at, parity)) return;
   const long long begun = clock64();
-  while (!mbar_try(at, parity)) {
+  while (!mbar_try_for(at, parity, kAsleep)) {
     // once a wait has run out, none waits any more: the block goes on to its
     // end over results that do not count
     if (*const_cast<volatile int*>(&m->abort)) return;
@@ -365,7 +367,7 @@ __device__ __forceinline__ void finish(const ProductParams& p, int n, long long 
 
 // Adds up the parts of a shared tile, whose first unit is `begin`, that the pairs from
 // `first` to before `after` left, and gives the results. A lane takes four
-// neighbouring channels, a warp every fourth token.
+// neighbouring channels, a warp every eighth token.
 template <typename T>
 __device__ __forceinline__ void join(const ProductParams& p, const Plan& g, const float* token_scale, int begin, int first, int after, int rank, int n0,
                                      long long t0, int tokens, int warp, long long slot_size) {
@@ -378,23 +380,23 @@ __device__ __forceinline__ void join(const ProductParams& p, const Plan& g, cons
 #pragma unroll
     for (int i = 0; i < 4; ++i) bias[i] = n + i < p.w.out ? __ldg(p.bias + n + i) : 0.0f;
   }
-  for (int c0 = warp; c0 < tokens; c0 += 4 * kDeep) {
+  for (int c0 = warp; c0 < tokens; c0 += 8 * kDeep) {
     int4 sum[kDeep];
 #pragma unroll
     for (int j = 0; j < kDeep; ++j) sum[j] = make_int4(0, 0, 0, 0);
-#pragma unroll 4
+#pragma unroll 2
     for (int other = first; other < after; ++other) {
       const int slot = share_begin(g, other) >= begin ? 0 : 1;
       const int32_t* from = g.slots + ((2ll * other + rank) * kSlots + slot) * slot_size + 4 * lane;
       int4 v[kDeep];
 #pragma unroll
-      for (int j = 0; j < kDeep; ++j) v[j] = __ldcg(reinterpret_cast<const int4*>(from + min(c0 + 4 * j, tokens - 1) * kTileOut));
+      for (int j = 0; j < kDeep; ++j) v[j] = __ldcg(reinterpret_cast<const int4*>(from + min(c0 + 8 * j, tokens - 1) * kTileOut));
 #pragma unroll
       for (int j = 0; j < kDeep; ++j) sum[j].x += v[j].x, sum[j].y += v[j].y, sum[j].z += v[j].z, sum[j].w += v[j].w;
     }
 #pragma unroll
     for (int j = 0; j < kDeep; ++j) {
-      const int c = c0 + 4 * j;
+      const int c = c0 + 8 * j;
       if (c >= tokens) continue;
       const float sx = token_scale[c];
       float v[4] = {result(__int2float_rn(sum[j].x), sx, scale.x, bias[0]), result(__int2float_rn(sum[j].y), sx, scale.y, bias[1]),
@@ -420,14 +422,27 @@ __device__ __forceinline__ int count_one(int32_t* at) {
   asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(old) : "l"(at) : "memory");
   return old;
 }
+__device__ __forceinline__ int counted(const int32_t* at) {
+  int now;
+  asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(now) : "l"(at) : "memory");
+  return now;
+}
 
-// Four warps read the accumulators, a lane a channel.
+// Eight warps read the accumulators, a lane a channel, warps 0 to 3 every other
+// 16 columns, warps 4 to 7 those between.
+//
+// Of a shared tile's pairs of blocks the last to be done gives the results. Most
+// often the others' parts are there when it comes to its own (a run of
+// units begins in one tile early and ends in the next one late): then it adds them to its
+// accumulator's columns on the way. Else it leaves its part too, and whichever
+// pair turns out to be the last adds them all up.
 template <typename T>
 __device__ __forceinline__ void results(const ProductParams& p, Misc* m, const Plan& g, int pair, int rank, int warp, uint32_t tmem) {
-  const int lane = threadIdx.x & 31, row = warp * 32 + lane;
-  const uint32_t empty0 = cluster_addr(smem_addr(&m->sum_empty[0]), 0), sums_at = tmem + (static_cast<uint32_t>(warp * 32) << 16);
+  const int lane = threadIdx.x & 31, row = (warp & 3) * 32 + lane;
+  const uint32_t empty0 = cluster_addr(smem_addr(&m->sum_empty[0]), 0), sums_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
   const long long slot_size = static_cast<long long>(g.sum_columns) * kTileOut;
-  int32_t* const slots = g.slots + (2ll * pair + rank) * kSlots * slot_size + row;
+  auto slot_of = [&](int of, int slot) { return g.slots + ((2ll * of + rank) * kSlots + slot) * slot_size; };
+  int shared = 0;
   Ring d, r;
   Walk walk(g, pair);
   Piece q;
@@ -437,33 +452,38 @@ __device__ __forceinline__ void results(const ProductParams& p, Misc* m, const P
     const long long t0 = static_cast<long long>(q.token) * g.tokens;
     const int tokens = static_cast<int>(min(static_cast<long long>(g.tokens), p.rows - t0));
     const float scale = __ldg(p.w.scale + n), bias = p.bias && n < p.w.out ? __ldg(p.bias + n) : -0.0f;
+    int first = 0, after = 0;   // the pairs with a part in the tile
+    if (!whole) first = share_of(g, begin), after = share_of(g, begin + g.per_tile - 1) + 1;
+    int32_t* const counter = &g.counters[2 * (q.tile - g.whole) + rank];
+    bool leave = false;
     wait(m, &m->ready_full[r.i], r.phase);
     const Ready& ready = m->ready[r.i];
     const int turns = ready.parts ? (q.k1 - q.k0 + kPart - 1) / kPart : 1;
     for (int turn = 0; turn < turns; ++turn) {
       const bool last = turn + 1 == turns;
-      // (the sum of the parts so far, and in the end what is left for the pair that joins the tile)
-      int32_t* const sum = slots + 2 * slot_size;
-      int32_t* const to = last ? slots + (share_begin(g, pair) >= begin ? 0 : slot_size) : sum;
       wait(m, &m->sum_full[d.i], d.phase);
       tc_fence_after();
       __syncwarp();
+      if (!whole && last) {
+        if (warp == 0 && lane == 0) m->others[shared & 1] = counted(counter) == after - first - 1;
+        named_barrier(1, 256);
+        leave = *const_cast<volatile int*>(&m->others[shared & 1]) == 0;
+        ++shared;
+      }
+      // (the sum of the parts so far; what is left for the pair that joins the tile)
+      int32_t* const sum = slot_of(pair, 2) + row;
+      int32_t* const to = last ? slot_of(pair, share_begin(g, pair) >= begin ? 0 : 1) + row : sum;
+      const int c0 = warp / 4 * kColumns;
       uint32_t u[kColumns];
-      tmem_load16(sums_at + d.i * g.sum_columns, u);
+      if (c0 < g.tokens) tmem_load16(sums_at + d.i * g.sum_columns + c0, u);
 #pragma unroll 1
-      for (int c = 0; c < g.tokens; c += kColumns) {
+      for (int c = c0; c < g.tokens; c += 2 * kColumns) {
         tmem_wait_load(u);
         float f[kColumns];
 #pragma unroll
         for (int j = 0; j < kColumns; ++j) f[j] = __uint_as_float(u[j]);
         __syncwarp();
-        if (c + kColumns < g.tokens) {
-          tmem_load16(sums_at + d.i * g.sum_columns + c + kColumns, u);
-        } else {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(empty0 + d.i * 8);
-        }
+        if (c + 2 * kColumns < g.tokens) tmem_load16(sums_at + d.i * g.sum_columns + c + 2 * kColumns, u);
         if (turns > 1 || !whole) {
           int v[kColumns];
 #pragma unroll
@@ -472,24 +492,34 @@ __device__ __forceinline__ void results(const ProductParams& p, Misc* m, const P
 #pragma unroll
             for (int j = 0; j < kColumns; ++j) v[j] += sum[(c + j) * kTileOut];
           }
-          if (!last || !whole) {
+          if (!last || leave) {
 #pragma unroll
             for (int j = 0; j < kColumns; ++j) to[(c + j) * kTileOut] = v[j];
             continue;
+          }
+          for (int other = first; other < after; ++other) {
+            if (other == pair) continue;
+            const int32_t* from = slot_of(other, share_begin(g, other) >= begin ? 0 : 1) + row + c * kTileOut;
+            int w[kColumns];
+#pragma unroll
+            for (int j = 0; j < kColumns; ++j) w[j] = __ldcg(from + j * kTileOut);
+#pragma unroll
+            for (int j = 0; j < kColumns; ++j) v[j] += w[j];
           }
 #pragma unroll
           for (int j = 0; j < kColumns; ++j) f[j] = __int2float_rn(v[j]);
         }
         finish<T>(p, n, t0 + c, tokens - c, ready.scale + c, scale, bias, f);
       }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(empty0 + d.i * 8);
       d.step(g.accumulators);
     }
-    if (!whole) {
-      // the last of the tile's pairs to be done adds its parts up
-      const int first = share_of(g, begin), after = share_of(g, begin + g.per_tile - 1) + 1;
-      named_barrier(1, 128);
-      if (warp == 0 && lane == 0) m->last = count_one(&g.counters[2 * (q.tile - g.whole) + rank]) == after - first - 1;
-      named_barrier(1, 128);
+    if (leave) {
+      named_barrier(1, 256);
+      if (warp == 0 && lane == 0) m->last = count_one(counter) == after - first - 1;
+      named_barrier(1, 256);
       if (*const_cast<volatile int*>(&m->last)) join<T>(p, g, ready.scale, begin, first, after, rank, n0, t0, tokens, warp, slot_size);
     }
     __syncwarp();
@@ -512,8 +542,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
       mbar_init(smem_addr(&m->full[i]), 8), mbar_init(smem_addr(&m->empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_addr(&m->sum_full[i]), 1), mbar_init(smem_addr(&m->sum_empty[i]), 8);
-      mbar_init(smem_addr(&m->ready_full[i]), 1), mbar_init(smem_addr(&m->ready_empty[i]), rank == 0 ? 5 : 4);
+      mbar_init(smem_addr(&m->sum_full[i]), 1), mbar_init(smem_addr(&m->sum_empty[i]), 16);
+      mbar_init(smem_addr(&m->ready_full[i]), 1), mbar_init(smem_addr(&m->ready_empty[i]), rank == 0 ? 9 : 8);
     }
     mbar_init(smem_addr(&m->drained), 1);
     m->abort = 0;
@@ -546,10 +576,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   } else if (warp == 3) {
     let_next_start();
     prepare(p, m, g, pair);
-  } else if (warp < 12) {
-    convert(m, g, pair, warp - 4, smem, tmem);
+  } else if (warp < kResults) {
+    convert(m, g, pair, warp - kConvert, smem, tmem);
   } else {
-    results<T>(p, m, g, pair, rank, warp - 12, tmem);
+    results<T>(p, m, g, pair, rank, warp - kResults, tmem);
   }
   tc_fence_before();
   __syncthreads();
