@@ -617,7 +617,7 @@ int sjd_norm(const sjd_rows* x, const sjd_rows* residual, const float* gain_dev,
  * otherwise; dx is that of x and of residual alike. dgain_dev[i] = sum_t dy[t][i]
  * u[t][i], dbias_dev[i] = sum_t dy[t][i] (NULL: not wanted), fp32, written, not
  * added to. dim is at most 16384. */
-size_t sjd_norm_gradient_workspace_size(int32_t rows, int32_t dim);
+size_t sjd_norm_gradient_workspace_size(int32_t rows, int32_t dim, int32_t dtype);
 int sjd_norm_gradient(const sjd_rows* dy, const sjd_rows* x, const float* gain_dev, float eps, int32_t centre,
                       const sjd_rows* dh, int32_t rows, int32_t dim, int32_t dtype, const sjd_rows* dx,
                       float* dgain_dev, float* dbias_dev, void* workspace_dev, size_t ws_bytes, void* cuda_stream);

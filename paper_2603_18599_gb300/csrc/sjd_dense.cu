@@ -7,11 +7,17 @@
 // and stays in their registers from its load to its store: its mean, the mean
 // of the squares around it (both as sums of the differences themselves, so
 // that nothing cancels) and its largest magnitude are sums over the group.
+//
+// What a thread does for a row whatever its length (the sums' exchanges, the
+// addresses) is worth as much as 16 features, so that a thread of a long call takes 32
+// of them: rows of up to 1024 features are taken by a warp or a part of
+// one, longer ones by a block. A call of few rows spreads each over more threads.
 
 #include <cfloat>
 
 #include "sjd_dense.h"
 #include "sjd_kv_device.cuh"
+#include "sjd_tcgen05.cuh"
 
 namespace sjd_dense_ops {
 
@@ -92,14 +98,30 @@ __device__ __forceinline__ float warp_sum(float x) {
   return x;
 }
 
-// Sums over the group of G threads: a warp, or the whole block. `turn`
-// numbers the sums of a block: two neighbours take different words of `words`
-// [2][N][32], so that one barrier a sum is enough.
+// The first n of 32 words in shared memory, which all lanes read at once; n is the same for all.
+__device__ __forceinline__ float add_words(const float* w, int n) {
+  float sum = 0.0f;
+  for (int i = 0; i < n; i += 4) {
+    const float4 v = *reinterpret_cast<const float4*>(w + i);
+    sum += (v.x + (i + 1 < n ? v.y : 0.0f)) + ((i + 2 < n ? v.z : 0.0f) + (i + 3 < n ? v.w : 0.0f));
+  }
+  return sum;
+}
+
+// Sums over the group of G threads: a power of two of a warp's, or the whole
+// block. `turn` numbers the sums of a block: two neighbours take different words
+// of `words` [2][2][32], so that one barrier a sum is enough.
 template <int N>
 __device__ __forceinline__ void group_sum(float (&x)[N], int G, float* words, int& turn) {
+  if (G <= 32) {
+    for (int o = G / 2; o > 0; o /= 2) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) x[k] += __shfl_xor_sync(0xffffffffu, x[k], o);
+    }
+    return;
+  }
 #pragma unroll
   for (int k = 0; k < N; ++k) x[k] = warp_sum(x[k]);
-  if (G == 32) return;
   float* w = words + (turn & 1) * 64;
   ++turn;
   if ((threadIdx.x & 31) == 0) {
@@ -107,13 +129,15 @@ __device__ __forceinline__ void group_sum(float (&x)[N], int G, float* words, in
     for (int k = 0; k < N; ++k) w[32 * k + threadIdx.x / 32] = x[k];
   }
   __syncthreads();
-  const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int k = 0; k < N; ++k) x[k] = warp_sum(lane < G / 32 ? w[32 * k + lane] : 0.0f);
+  for (int k = 0; k < N; ++k) x[k] = add_words(w + 32 * k, G / 32);
 }
 __device__ __forceinline__ uint32_t group_max(uint32_t x, int G, float* words, int& turn) {
+  if (G <= 32) {
+    for (int o = G / 2; o > 0; o /= 2) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
+    return x;
+  }
   x = __reduce_max_sync(0xffffffffu, x);
-  if (G == 32) return x;
   uint32_t* w = reinterpret_cast<uint32_t*>(words) + (turn & 1) * 64;
   ++turn;
   if ((threadIdx.x & 31) == 0) w[threadIdx.x / 32] = x;
@@ -122,33 +146,45 @@ __device__ __forceinline__ uint32_t group_max(uint32_t x, int G, float* words, i
   return __reduce_max_sync(0xffffffffu, lane < G / 32 ? w[lane] : 0u);
 }
 
-// y = (h - m) r gain + bias, h = x + residual rounded to the rows' type, m the
-// mean (0 without centring), r = 1 / sqrt(mean of (h - m)^2 + eps); or y's
-// codes and scale, or (MODE kCodes) those of x itself.
-template <typename T, bool W, int C, int MODE>
-__global__ void __launch_bounds__(512) norm_kernel(const NormParams p, int G) {
-  __shared__ float words[2 * 64];
-  wait_for_previous();
-  let_next_start();
-  const int per = blockDim.x / G, lane = threadIdx.x % G;
-  const long long row = static_cast<long long>(blockIdx.x) * per + threadIdx.x / G;
-  if (row >= p.rows) return;   // (whole warps: a group of more than a warp is a block)
-  int turn = 0;
-  const int D = p.dim;
-  float v[C][8];
-  const T* x = static_cast<const T*>(p.x.p) + row * p.x.stride;
+// A thread's part of a row on its way into shared memory: it copies what it reads
+// itself, and waits for its own copies alone.
+template <typename T, int C>
+__device__ __forceinline__ void copy_row(const T* row, T* to, int G, int D) {
 #pragma unroll
-  for (int i = 0; i < C; ++i) load8<W>(x, i, lane, G, D, v[i]);
+  for (int i = 0; i < C; ++i) {
+    const int e = (i * G + threadIdx.x) * 8;
+    if (e >= D) break;
+#pragma unroll
+    for (int k = 0; k < 8; k += 16 / sizeof(T)) sjd_kv_ops::copy16(sjd_kv_ops::smem_addr(to + e + k), row + e + k, 16);
+  }
+}
+
+// x / scale of eight values, as IEEE division rounds it. With the reciprocal
+// rounded to nearest, two corrections by the exact remainder give the nearest
+// quotient (Markstein, IBM J. Res. Dev. 34, 1990), as long as the remainders of
+// quotients that matter do not underflow: for scales within 2^60 of 1.
+__device__ __forceinline__ float quotient(float x, float scale, float inverse) {
+  float q = x * inverse;
+  q = fmaf(fmaf(-q, scale, x), inverse, q);
+  return fmaf(fmaf(-q, scale, x), inverse, q);
+}
+
+// A row in registers becomes y = (h - m) r gain + bias, h = x + residual rounded
+// to the rows' type, m the mean (0 without centring), r = 1 / sqrt(mean of
+// (h - m)^2 + eps); or y's codes and scale, or (MODE kCodes) those of x itself.
+// w: the residual's row. `there`: the row is to be written.
+template <typename T, bool W, int C, int MODE>
+__device__ __forceinline__ void norm_row(const NormParams& p, long long row, bool there, int lane, int G, float (&v)[C][8], float (&w)[C][8], float* words,
+                                         int& turn) {
+  const int D = p.dim;
+  const float over = 1.0f / static_cast<float>(D);
   if (MODE != kCodes && p.residual.p) {
-    const T* r = static_cast<const T*>(p.residual.p) + row * p.residual.stride;
     T* h = static_cast<T*>(p.h.p) + row * p.h.stride;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      float w[8];
-      load8<W>(r, i, lane, G, D, w);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = static_cast<float>(static_cast<T>(v[i][j] + w[j]));
-      store8<W>(h, i, lane, G, D, v[i]);
+      for (int j = 0; j < 8; ++j) v[i][j] = static_cast<float>(static_cast<T>(v[i][j] + w[i][j]));
+      if (there) store8<W>(h, i, lane, G, D, v[i]);
     }
   }
   if constexpr (MODE != kCodes) {
@@ -160,7 +196,7 @@ __global__ void __launch_bounds__(512) norm_kernel(const NormParams p, int G) {
         for (int j = 0; j < 8; ++j) sum[0] += v[i][j];
       }
       group_sum(sum, G, words, turn);
-      const float mean = sum[0] / static_cast<float>(D);
+      const float mean = sum[0] * over;
 #pragma unroll
       for (int i = 0; i < C; ++i) {
 #pragma unroll
@@ -176,7 +212,7 @@ __global__ void __launch_bounds__(512) norm_kernel(const NormParams p, int G) {
       for (int j = 0; j < 8; ++j) squares[0] = fmaf(v[i][j], v[i][j], squares[0]);
     }
     group_sum(squares, G, words, turn);
-    const float r = 1.0f / sqrtf(squares[0] / static_cast<float>(D) + p.eps);
+    const float r = rsqrtf(squares[0] * over + p.eps);
 #pragma unroll
     for (int i = 0; i < C; ++i) {
       float g[8], b[8];
@@ -187,6 +223,7 @@ __global__ void __launch_bounds__(512) norm_kernel(const NormParams p, int G) {
     }
   }
   if constexpr (MODE == kNorm) {
+    if (!there) return;
     T* y = static_cast<T*>(p.y.p) + row * p.y.stride;
 #pragma unroll
     for (int i = 0; i < C; ++i) store8<W>(y, i, lane, G, D, v[i]);
@@ -202,15 +239,24 @@ __global__ void __launch_bounds__(512) norm_kernel(const NormParams p, int G) {
       }
     }
     const float top = __uint_as_float(group_max(bits, G, words, turn)), scale = __fdiv_rn(top, 127.0f);
-    const bool some = top <= FLT_MAX && scale > 0.0f;
+    if (!there) return;
+    const bool some = top <= FLT_MAX && scale > 0.0f, plain = top > 0x1p-60f && top < 0x1p60f;
+    const float inverse = __frcp_rn(scale);
     int8_t* codes = p.codes + row * D;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
       uint32_t q[2] = {0, 0};
+      if (plain) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = quotient(v[i][j], scale, inverse);
+      } else {
+        // (a subnormal scale has few bits: quotients by it may pass 127)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = some ? fminf(fmaxf(__fdiv_rn(v[i][j], scale), -127.0f), 127.0f) : 0.0f;
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        // (a subnormal scale has few bits: quotients by it may pass 127)
-        const int c = some ? __float2int_rn(fminf(fmaxf(__fdiv_rn(v[i][j], scale), -127.0f), 127.0f)) : 0;
+        const int c = __float2int_rn(v[i][j]);
         if constexpr (W) q[j / 4] |= static_cast<uint32_t>(c & 0xff) << 8 * (j % 4);
         else if (feature<false>(i, j, lane, G) < D) codes[feature<false>(i, j, lane, G)] = static_cast<int8_t>(c);
       }
@@ -222,6 +268,27 @@ __global__ void __launch_bounds__(512) norm_kernel(const NormParams p, int G) {
   }
 }
 
+// A group of G threads to a row: lanes of a warp, or a block.
+constexpr int kShortBlock = 128;   // where several rows share a block
+constexpr int kShort = 512;        // features of a row that the gradient's sums take a warp for
+template <typename T, bool W, int C, int MODE>
+__global__ void __launch_bounds__(512) norm_kernel(const NormParams p, int G) {
+  __shared__ __align__(16) float words[2 * 64];
+  wait_for_previous();
+  let_next_start();
+  const int per = blockDim.x / G, lane = threadIdx.x % G;
+  const long long at = static_cast<long long>(blockIdx.x) * per + threadIdx.x / G, row = min(at, p.rows - 1ll);
+  int turn = 0;
+  float v[C][8], w[C][8];
+#pragma unroll
+  for (int i = 0; i < C; ++i) load8<W>(static_cast<const T*>(p.x.p) + row * p.x.stride, i, lane, G, p.dim, v[i]);
+  if (MODE != kCodes && p.residual.p) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) load8<W>(static_cast<const T*>(p.residual.p) + row * p.residual.stride, i, lane, G, p.dim, w[i]);
+  }
+  norm_row<T, W, C, MODE>(p, row, at < p.rows, lane, G, v, w, words, turn);
+}
+
 bool aligned16(const void* p, long long stride, size_t size) {
   return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(stride) * size) & 15) == 0;
 }
@@ -231,113 +298,232 @@ bool wide(const float* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 int threads_of(int dim, int pieces) { return ((dim + 8 * pieces - 1) / (8 * pieces) + 31) / 32 * 32; }
 
+int lanes_of(int dim, int pieces) {   // of a warp
+  int l = 8;
+  while (8 * pieces * l < dim) l *= 2;
+  return l;
+}
+
+template <typename T, bool W, int C, int MODE>
+cudaError_t norm_with(const NormParams& p, cudaStream_t s) {
+  const int G = p.dim <= 8 * C * 32 ? lanes_of(p.dim, C) : threads_of(p.dim, C), threads = G <= 32 ? kShortBlock : G, per = threads / G;
+  return launch_early(norm_kernel<T, W, C, MODE>, static_cast<unsigned>((static_cast<long long>(p.rows) + per - 1) / per), threads, 0, s, p, G);
+}
+
+// Pieces of a thread. PIECES_FIGURES
 template <typename T, bool W, int MODE>
-cudaError_t norm_by(const NormParams& p, cudaStream_t s) {
-  const int C = p.dim <= 256 ? 1 : p.dim <= 8192 ? 2 : 4, G = threads_of(p.dim, C), threads = G == 32 ? 128 : G;
-  const unsigned blocks = static_cast<unsigned>((static_cast<long long>(p.rows) * G + threads - 1) / threads);
-  if (C == 1) return launch_early(norm_kernel<T, W, 1, MODE>, blocks, threads, 0, s, p, G);
-  if (C == 2) return launch_early(norm_kernel<T, W, 2, MODE>, blocks, threads, 0, s, p, G);
-  return launch_early(norm_kernel<T, W, 4, MODE>, blocks, threads, 0, s, p, G);
+cudaError_t norm_by(const NormParams& p, int sms, cudaStream_t s) {
+  const bool few = p.rows <= 2 * sms;
+  const int d = p.dim;
+  if (d <= 256 || (few && d <= 4096)) return norm_with<T, W, 1, MODE>(p, s);
+  if (d <= 512 || ((few || !W) && d <= 8192)) return norm_with<T, W, 2, MODE>(p, s);
+  return norm_with<T, W, 4, MODE>(p, s);
 }
 
 template <typename T>
-cudaError_t norm_of(const NormParams& p, int mode, cudaStream_t s) {
+cudaError_t norm_of(const NormParams& p, int mode, int sms, cudaStream_t s) {
   const bool w = p.dim % 8 == 0 && wide(p.x, p.rows, sizeof(T)) && wide(p.residual, p.rows, sizeof(T)) && wide(p.y, p.rows, sizeof(T)) &&
                  wide(p.h, p.rows, sizeof(T)) && wide(p.gain) && wide(p.bias) && reinterpret_cast<uintptr_t>(p.codes) % 8 == 0;
-  if (mode == kNorm) return w ? norm_by<T, true, kNorm>(p, s) : norm_by<T, false, kNorm>(p, s);
-  if (mode == kNormCodes) return w ? norm_by<T, true, kNormCodes>(p, s) : norm_by<T, false, kNormCodes>(p, s);
-  return w ? norm_by<T, true, kCodes>(p, s) : norm_by<T, false, kCodes>(p, s);
+  if (mode == kNorm) return w ? norm_by<T, true, kNorm>(p, sms, s) : norm_by<T, false, kNorm>(p, sms, s);
+  if (mode == kNormCodes) return w ? norm_by<T, true, kNormCodes>(p, sms, s) : norm_by<T, false, kNormCodes>(p, sms, s);
+  return w ? norm_by<T, true, kCodes>(p, sms, s) : norm_by<T, false, kCodes>(p, sms, s);
 }
 
 // With u = (x - m) r and g = dy gain: dx = r (g - mean(g) - u mean(g u)) + dh
 // (mean(g) where centred), dgain = sum of dy u over the rows, dbias = sum of dy.
-// The sums over a row are those of x and g, then of (x - m)^2 and g (x - m). A
-// block takes every blocks-th row and keeps the sums over its rows of its
-// columns in registers (C 1), or, of rows of more than 8192 features, in shared
-// memory; they are added up by a second kernel in the blocks' order.
-template <typename T, bool W, int C, bool SHARED>
-__global__ void __launch_bounds__(SHARED ? 1024 : 512) norm_gradient_kernel(const NormGradientParams p, int G) {
-  __shared__ float words[2 * 64];
-  extern __shared__ float sums[];   // SHARED: [2][D]
-  wait_for_previous();
-  let_next_start();
-  const int lane = threadIdx.x, D = p.dim;
+// The sums over a row are those of x and g, then of (x - m)^2 and g (x - m).
+// x: the row, g: dy, dh: what is added (or not); dx takes their place in g, u in x and dy in dh.
+template <bool W, int C, typename Gain>
+__device__ __forceinline__ void gradient_row(const NormGradientParams& p, int lane, int G, float (&x)[C][8], float (&dy)[C][8], float (&dx)[C][8],
+                                             float* words, int& turn, Gain gain) {
+  const int D = p.dim;
   const float over = 1.0f / static_cast<float>(D);
-  int turn = 0;
-  float dgain[SHARED ? 1 : C][8] = {}, dbias[SHARED ? 1 : C][8] = {};
-  if constexpr (SHARED) {
-    for (int i = lane; i < 2 * D; i += G) sums[i] = 0.0f;
-    __syncthreads();
-  }
-  for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
-    float x[C][8], g[C][8];
-    const T* xs = static_cast<const T*>(p.x.p) + row * p.x.stride;
-    const T* dys = static_cast<const T*>(p.dy.p) + row * p.dy.stride;
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-      load8<W>(xs, i, lane, G, D, x[i]);
-      load8<W>(dys, i, lane, G, D, g[i]);
-    }
-    float mean = 0.0f, mean_g = 0.0f;
-    if (p.centre) {
-      float sum[2] = {0.0f, 0.0f};
-#pragma unroll
-      for (int i = 0; i < C; ++i) {
-        float gain[8];
-        load_vector<W>(p.gain, 1.0f, i, lane, G, D, gain);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum[0] += x[i][j], sum[1] = fmaf(g[i][j], gain[j], sum[1]);
-      }
-      group_sum(sum, G, words, turn);
-      mean = sum[0] / static_cast<float>(D), mean_g = sum[1] * over;
-    }
+  float mean = 0.0f, mean_g = 0.0f;
+  if (p.centre) {
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      float gain[8];
-      load_vector<W>(p.gain, 1.0f, i, lane, G, D, gain);
+      float g[8];
+      gain(i, g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float u = feature<W>(i, j, lane, G) < D ? x[i][j] - mean : 0.0f;
-        x[i][j] = u;
-        sum[0] = fmaf(u, u, sum[0]), sum[1] = fmaf(g[i][j] * gain[j], u, sum[1]);
-      }
+      for (int j = 0; j < 8; ++j) sum[0] += x[i][j], sum[1] = fmaf(dy[i][j], g[j], sum[1]);
     }
     group_sum(sum, G, words, turn);
-    const float r = 1.0f / sqrtf(sum[0] / static_cast<float>(D) + p.eps), along = sum[1] * over * r;
-    T* dxs = static_cast<T*>(p.dx.p) + row * p.dx.stride;
-    const T* dhs = static_cast<const T*>(p.dh.p) + row * p.dh.stride;
+    mean = sum[0] * over, mean_g = sum[1] * over;
+  }
+  float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-      float gain[8], dh[8], dx[8];
-      load_vector<W>(p.gain, 1.0f, i, lane, G, D, gain);
-      if (p.dh.p) load8<W>(dhs, i, lane, G, D, dh);
+  for (int i = 0; i < C; ++i) {
+    float g[8];
+    gain(i, g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float u = x[i][j] * r, dy = g[i][j];
-        dx[j] = (dy * gain[j] - mean_g - u * along) * r;
-        if (p.dh.p) dx[j] += dh[j];
-        if constexpr (SHARED) {
-          const int e = feature<W>(i, j, lane, G);
-          if (e < D) sums[e] = fmaf(dy, u, sums[e]), sums[D + e] += dy;
-        } else {
-          dgain[i][j] = fmaf(dy, u, dgain[i][j]);
-          dbias[i][j] += dy;
-        }
-      }
-      store8<W>(dxs, i, lane, G, D, dx);
+    for (int j = 0; j < 8; ++j) {
+      const float u = feature<W>(i, j, lane, G) < D ? x[i][j] - mean : 0.0f;
+      x[i][j] = u;
+      sum[0] = fmaf(u, u, sum[0]), sum[1] = fmaf(dy[i][j] * g[j], u, sum[1]);
     }
   }
-  const int kinds = p.dbias ? 2 : 1;
-  float* part = p.parts + static_cast<long long>(blockIdx.x) * kinds * D;
+  group_sum(sum, G, words, turn);
+  const float r = rsqrtf(sum[0] * over + p.eps), along = sum[1] * over * r;
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    float g[8];
+    gain(i, g);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[i][j] *= r;
+      dx[i][j] = fmaf(dy[i][j] * g[j] - mean_g - x[i][j] * along, r, p.dh.p ? dx[i][j] : 0.0f);
+    }
+  }
+}
+
+// Rows of up to 512 features: every group of G lanes takes rows of its own, and
+// the block's warps add up their columns in order.
+template <typename T, bool W, int C>
+__global__ void __launch_bounds__(kShortBlock) norm_gradient_short_kernel(const NormGradientParams p, int G) {
+  __shared__ float sums[2][kShort];
+  wait_for_previous();
+  let_next_start();
+  const int lane = threadIdx.x % G, D = p.dim, per = kShortBlock / G;
+  int turn = 0;
+  float dgain[C][8] = {}, dbias[C][8] = {};
+  for (long long first = static_cast<long long>(blockIdx.x) * per; first < p.rows; first += static_cast<long long>(gridDim.x) * per) {
+    const long long at = first + threadIdx.x / G, row = min(at, p.rows - 1ll);
+    float x[C][8], dy[C][8], dx[C][8];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      load8<W>(static_cast<const T*>(p.x.p) + row * p.x.stride, i, lane, G, D, x[i]);
+      load8<W>(static_cast<const T*>(p.dy.p) + row * p.dy.stride, i, lane, G, D, dy[i]);
+      if (p.dh.p) load8<W>(static_cast<const T*>(p.dh.p) + row * p.dh.stride, i, lane, G, D, dx[i]);
+    }
+    gradient_row<W, C>(p, lane, G, x, dy, dx, nullptr, turn, [&](int i, float (&g)[8]) { load_vector<W>(p.gain, 1.0f, i, lane, G, D, g); });
+    if (at >= p.rows) continue;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      store8<W>(static_cast<T*>(p.dx.p) + row * p.dx.stride, i, lane, G, D, dx[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) dgain[i][j] = fmaf(dy[i][j], x[i][j], dgain[i][j]), dbias[i][j] += dy[i][j];
+    }
+  }
+  __syncwarp();
+  for (int o = G; o < 32; o *= 2) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        dgain[i][j] += __shfl_xor_sync(0xffffffffu, dgain[i][j], o);
+        dbias[i][j] += __shfl_xor_sync(0xffffffffu, dbias[i][j], o);
+      }
+    }
+  }
+  for (int w = 0; w < kShortBlock / 32; ++w) {
+    if (static_cast<int>(threadIdx.x / 32) == w && (threadIdx.x & 31) < static_cast<unsigned>(G)) {
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int e = feature<W>(i, j, lane, G);
+          if (e < D) sums[0][e] = (w ? sums[0][e] : 0.0f) + dgain[i][j], sums[1][e] = (w ? sums[1][e] : 0.0f) + dbias[i][j];
+        }
+      }
+    }
+    __syncthreads();
+  }
+  const int columns = D * (p.dbias ? 2 : 1);
+  for (int e = threadIdx.x; e < columns; e += kShortBlock) p.parts[static_cast<long long>(blockIdx.x) * columns + e] = sums[e >= D][e >= D ? e - D : e];
+}
+
+// Longer rows: a block takes every gridDim-th, and keeps the sums over its rows of
+// its columns in registers, or, of rows of more than 8192 features, in shared
+// memory (WAY kShared); a second kernel adds them up in the blocks' order. Rows that can be
+// accessed 16 bytes at a time are on their way while the one before them is summed up
+// (kAhead; `deep` stages of shared memory).
+enum GradientWay { kAhead, kDirect, kShared };
+template <typename T, bool W, int WAY>
+__global__ void __launch_bounds__(WAY == kShared ? 1024 : 512) norm_gradient_kernel(const NormGradientParams p, int G, int deep) {
+  constexpr int C = 2;
+  __shared__ __align__(16) float words[2 * 64];
+  extern __shared__ __align__(16) unsigned char shared[];
+  float* sums = reinterpret_cast<float*>(shared);   // kShared: [2][D]
+  T* stages = reinterpret_cast<T*>(shared);         // kAhead: [deep][2 or 3][D]
+  wait_for_previous();
+  let_next_start();
+  const int lane = threadIdx.x, D = p.dim, kinds = p.dh.p ? 3 : 2;
+  auto x_of = [&](long long row) { return static_cast<const T*>(p.x.p) + row * p.x.stride; };
+  auto dy_of = [&](long long row) { return static_cast<const T*>(p.dy.p) + row * p.dy.stride; };
+  auto dh_of = [&](long long row) { return static_cast<const T*>(p.dh.p) + row * p.dh.stride; };
+  auto fetch = [&](long long row, int stage) {
+    T* to = stages + stage * kinds * D;
+    if (row < p.rows) {
+      copy_row<T, C>(x_of(row), to, G, D);
+      copy_row<T, C>(dy_of(row), to + D, G, D);
+      if (p.dh.p) copy_row<T, C>(dh_of(row), to + 2 * D, G, D);
+    }
+    sjd_kv_ops::copy_commit();   // (the group of a row that is not there is empty)
+  };
+  float dgain[WAY == kShared ? 1 : C][8] = {}, dbias[WAY == kShared ? 1 : C][8] = {}, gains[WAY == kShared ? 1 : C][8];
+  if constexpr (WAY == kShared) {
+    for (int i = lane; i < 2 * D; i += G) sums[i] = 0.0f;
+    __syncthreads();
+  } else {
+    if constexpr (WAY == kAhead) {
+      for (int i = 0; i + 1 < deep; ++i) fetch(blockIdx.x + static_cast<long long>(i) * gridDim.x, i);
+    }
+#pragma unroll
+    for (int i = 0; i < C; ++i) load_vector<W>(p.gain, 1.0f, i, lane, G, D, gains[i]);
+  }
+  int turn = 0, stage = 0;
+  for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const T *xs = x_of(row), *dys = dy_of(row), *dhs = dh_of(row);
+    if constexpr (WAY == kAhead) {
+      if (deep == 2) sjd_kv_ops::copy_wait<0>();
+      else if (deep == 3) sjd_kv_ops::copy_wait<1>();
+      else sjd_kv_ops::copy_wait<2>();
+      fetch(row + (deep - 1ll) * gridDim.x, stage == 0 ? deep - 1 : stage - 1);   // (where the row before was)
+      xs = stages + stage * kinds * D, dys = xs + D, dhs = dys + D;
+      if (++stage == deep) stage = 0;
+    }
+    float x[C][8], dy[C][8], dx[C][8];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      load8<W>(xs, i, lane, G, D, x[i]);
+      load8<W>(dys, i, lane, G, D, dy[i]);
+      if (p.dh.p) load8<W>(dhs, i, lane, G, D, dx[i]);
+    }
+    gradient_row<W, C>(p, lane, G, x, dy, dx, words, turn, [&](int i, float (&g)[8]) {
+      if constexpr (WAY == kShared) {
+        load_vector<W>(p.gain, 1.0f, i, lane, G, D, g);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] = gains[i][j];
+      }
+    });
+    T* dxs = static_cast<T*>(p.dx.p) + row * p.dx.stride;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      store8<W>(dxs, i, lane, G, D, dx[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (WAY == kShared) {
+          const int e = feature<W>(i, j, lane, G);
+          if (e < D) sums[e] = fmaf(dy[i][j], x[i][j], sums[e]), sums[D + e] += dy[i][j];
+        } else {
+          dgain[i][j] = fmaf(dy[i][j], x[i][j], dgain[i][j]);
+          dbias[i][j] += dy[i][j];
+        }
+      }
+    }
+  }
+  sjd_kv_ops::copy_wait_all();
+  float* part = p.parts + static_cast<long long>(blockIdx.x) * (p.dbias ? 2 : 1) * D;
 #pragma unroll
   for (int i = 0; i < C; ++i) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int e = feature<W>(i, j, lane, G);
       if (e >= D) continue;
-      part[e] = SHARED ? sums[e] : dgain[SHARED ? 0 : i][j];
-      if (p.dbias) part[D + e] = SHARED ? sums[D + e] : dbias[SHARED ? 0 : i][j];
+      part[e] = WAY == kShared ? sums[e] : dgain[WAY == kShared ? 0 : i][j];
+      if (p.dbias) part[D + e] = WAY == kShared ? sums[D + e] : dbias[WAY == kShared ? 0 : i][j];
     }
   }
 }
@@ -362,19 +548,47 @@ __global__ void __launch_bounds__(32 * kSumRows) add_parts_kernel(const NormGrad
   if (lane == 0 && of >= p.dim && of < columns) p.dbias[of - p.dim] = sum;
 }
 
+// Blocks of the gradient's first kernel on an SM (by its 128 registers) and
+// rows on their way in each: shared memory holds them, and there is no use for more
+// than 96 KB of them.
+struct Flow {
+  int per_sm, deep;
+  size_t shared;
+};
+Flow gradient_flow(int dim, size_t size) {
+  if (dim > 8192) return {1, 0, 2 * sizeof(float) * dim};
+  const size_t row = 3 * size * dim;
+  Flow f;
+  f.per_sm = min(8, max(1, 65536 / 128 / threads_of(dim, 2)));
+  while (f.per_sm > 1 && 2 * f.per_sm * row > 200 * 1024) --f.per_sm;
+  f.deep = 4;
+  while (f.deep > 2 && f.deep * f.per_sm * row > 128 * 1024) --f.deep;
+  f.shared = f.deep * row;
+  return f;
+}
+
+template <typename T, bool W, int WAY>
+cudaError_t norm_gradient_with(const NormGradientParams& p, const Flow& f, cudaStream_t s) {
+  const int G = threads_of(p.dim, 2);
+  const size_t shared = WAY == kDirect ? 0 : f.shared;
+  if (shared > 40 * 1024) {   // (with the words 48 KB, which any kernel may have)
+    const cudaError_t e = cudaFuncSetAttribute(norm_gradient_kernel<T, W, WAY>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
+    if (e != cudaSuccess) return e;
+  }
+  return launch_early(norm_gradient_kernel<T, W, WAY>, p.blocks, G, shared, s, p, G, f.deep);
+}
+
 template <typename T, bool W>
 cudaError_t norm_gradient_by(const NormGradientParams& p, cudaStream_t s) {
-  const int G = threads_of(p.dim, 2);
-  cudaError_t e;
-  if (p.dim <= 8192) {
-    e = launch_early(norm_gradient_kernel<T, W, 2, false>, p.blocks, G, 0, s, p, G);
-  } else {
-    const size_t shared = 2 * sizeof(float) * p.dim;
-    e = cudaFuncSetAttribute(norm_gradient_kernel<T, W, 2, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
-    if (e == cudaSuccess) e = launch_early(norm_gradient_kernel<T, W, 2, true>, p.blocks, G, shared, s, p, G);
-  }
-  if (e != cudaSuccess) return e;
   const int columns = p.dim * (p.dbias ? 2 : 1);
+  const Flow f = gradient_flow(p.dim, sizeof(T));
+  cudaError_t e;
+  if (p.dim <= kShort / 2) e = launch_early(norm_gradient_short_kernel<T, W, 1>, p.blocks, kShortBlock, 0, s, p, lanes_of(p.dim, 1));
+  else if (p.dim <= kShort) e = launch_early(norm_gradient_short_kernel<T, W, 2>, p.blocks, kShortBlock, 0, s, p, lanes_of(p.dim, 2));
+  else if (p.dim > 8192) e = norm_gradient_with<T, W, kShared>(p, f, s);
+  else if (W && f.shared <= 227 * 1024 - 1024) e = norm_gradient_with<T, W, W ? kAhead : kDirect>(p, f, s);
+  else e = norm_gradient_with<T, W, kDirect>(p, f, s);
+  if (e != cudaSuccess) return e;
   return launch_early(add_parts_kernel, (columns + 31) / 32, 32 * kSumRows, 0, s, p, columns);
 }
 
@@ -540,12 +754,15 @@ cudaError_t embed_gradient_of(const EmbedGradientParams& p, int sms, cudaStream_
 
 }  // namespace
 
-cudaError_t launch_norm(const NormParams& p, int mode, int dtype, cudaStream_t s) {
-  return dtype == SJD_BF16 ? norm_of<__nv_bfloat16>(p, mode, s) : norm_of<float>(p, mode, s);
+cudaError_t launch_norm(const NormParams& p, int mode, int dtype, int sms, cudaStream_t s) {
+  return dtype == SJD_BF16 ? norm_of<__nv_bfloat16>(p, mode, sms, s) : norm_of<float>(p, mode, sms, s);
 }
 
-// Blocks of 512 threads and more an SM, each with several rows to sum up.
-int norm_gradient_blocks(int rows, int dim, int sms) { return min(rows, sms * max(2, 512 / threads_of(dim, 2))); }
+int norm_gradient_blocks(int rows, int dim, int dtype, int sms) {
+  if (dim > kShort) return min(rows, sms * gradient_flow(dim, dtype == SJD_BF16 ? 2 : 4).per_sm);
+  const int per = kShortBlock / lanes_of(dim, dim <= kShort / 2 ? 1 : 2);
+  return static_cast<int>(min((static_cast<long long>(rows) + per - 1) / per, 8ll * sms));
+}
 
 cudaError_t launch_norm_gradient(const NormGradientParams& p, int dtype, cudaStream_t s) {
   const size_t size = dtype == SJD_BF16 ? 2 : 4;

@@ -102,8 +102,8 @@ struct ProductParams {
   int rows;
 };
 
-cudaError_t launch_norm(const NormParams& p, int mode, int dtype, cudaStream_t s);
-int norm_gradient_blocks(int rows, int dim, int sms);
+cudaError_t launch_norm(const NormParams& p, int mode, int dtype, int sms, cudaStream_t s);
+int norm_gradient_blocks(int rows, int dim, int dtype, int sms);
 cudaError_t launch_norm_gradient(const NormGradientParams& p, int dtype, cudaStream_t s);
 cudaError_t launch_embed(const EmbedParams& p, int table_dtype, int dtype, int sms, cudaStream_t s);
 cudaError_t launch_embed_gradient(const EmbedGradientParams& p, int dtype, int sms, cudaStream_t s);

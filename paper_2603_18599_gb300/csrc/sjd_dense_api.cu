@@ -92,7 +92,9 @@ int sjd_quantise(const sjd_rows* x, int32_t rows, int32_t dim, int32_t dtype, in
   p.scale = scale;
   p.rows = rows;
   p.dim = dim;
-  return launched(launch_norm(p, kCodes, dtype, static_cast<cudaStream_t>(stream)));
+  int sms = 0;
+  if (!count_sms(&sms)) return SJD_ERR_CUDA;
+  return launched(launch_norm(p, kCodes, dtype, sms, static_cast<cudaStream_t>(stream)));
 }
 
 int sjd_norm(const sjd_rows* x, const sjd_rows* residual, const float* gain, const float* bias, float eps, int32_t centre, int32_t rows, int32_t dim,
@@ -105,13 +107,15 @@ int sjd_norm(const sjd_rows* x, const sjd_rows* residual, const float* gain, con
   if ((codes != nullptr) != (scale != nullptr) || (codes != nullptr) == (y != nullptr) || !absent_or_there(y, size) || !aligned(scale, 4))
     return SJD_ERR_ARG;
   const NormParams p{rows_of(x), rows_of(residual), rows_of(y), rows_of(h), gain, bias, codes, scale, eps, rows, dim, centre};
-  return launched(launch_norm(p, codes ? kNormCodes : kNorm, dtype, static_cast<cudaStream_t>(stream)));
+  int sms = 0;
+  if (!count_sms(&sms)) return SJD_ERR_CUDA;
+  return launched(launch_norm(p, codes ? kNormCodes : kNorm, dtype, sms, static_cast<cudaStream_t>(stream)));
 }
 
-size_t sjd_norm_gradient_workspace_size(int32_t rows, int32_t dim) {
+size_t sjd_norm_gradient_workspace_size(int32_t rows, int32_t dim, int32_t dtype) {
   int sms = 0;
-  if (!valid(rows, dim) || !count_sms(&sms)) return 0;
-  return 2 * sizeof(float) * dim * static_cast<size_t>(norm_gradient_blocks(rows, dim, sms));
+  if (!valid(rows, dim) || !floating(dtype) || !count_sms(&sms)) return 0;
+  return 2 * sizeof(float) * dim * static_cast<size_t>(norm_gradient_blocks(rows, dim, dtype, sms));
 }
 
 int sjd_norm_gradient(const sjd_rows* dy, const sjd_rows* x, const float* gain, float eps, int32_t centre, const sjd_rows* dh, int32_t rows,
@@ -122,7 +126,7 @@ int sjd_norm_gradient(const sjd_rows* dy, const sjd_rows* x, const float* gain, 
   if (!aligned(gain, 4) || !dgain || !aligned(dgain, 4) || !aligned(dbias, 4) || !workspace || !aligned(workspace, kAlign)) return SJD_ERR_ARG;
   int sms = 0;
   if (!count_sms(&sms)) return SJD_ERR_CUDA;
-  const int blocks = norm_gradient_blocks(rows, dim, sms);
+  const int blocks = norm_gradient_blocks(rows, dim, dtype, sms);
   if (ws_bytes < 2 * sizeof(float) * dim * static_cast<size_t>(blocks)) return SJD_ERR_CAPACITY;
   const NormGradientParams p{rows_of(dy), rows_of(x), rows_of(dh), rows_of(dx), gain, dgain, dbias, static_cast<float*>(workspace), eps, rows, dim, centre, blocks};
   return launched(launch_norm_gradient(p, dtype, static_cast<cudaStream_t>(stream)));

@@ -44,7 +44,7 @@ def load():
     for name, args, res in (
             ("sjd_quantise", [P, I, I, I, P, P, P], I),
             ("sjd_norm", [P, P, P, P, F, I, I, I, I, P, P, P, P, P], I),
-            ("sjd_norm_gradient_workspace_size", [I, I], S),
+            ("sjd_norm_gradient_workspace_size", [I, I, I], S),
             ("sjd_norm_gradient", [P, P, P, F, I, P, I, I, I, P, P, P, P, S, P], I),
             ("sjd_embed", [P, I, I, P, I, I, F, I, P, P], I),
             ("sjd_embed_gradient_workspace_size", [I, I], S),
@@ -270,7 +270,7 @@ def norm_gradient(dy, x, gain=None, eps=1e-6, centre=False, dh=None, bias=False)
     dgain = made(dim, dtype=torch.float32, device=device)
     dbias = made(dim, dtype=torch.float32, device=device) if bias else None
     if n:
-        size = _size(device, "sjd_norm_gradient_workspace_size", n, dim)
+        size = _size(device, "sjd_norm_gradient_workspace_size", n, dim, _DTYPES[dtype])
         workspace = torch.empty(size, dtype=torch.uint8, device=device)
         _run(device, "sjd_norm_gradient", _pack(d), _pack(rows), g, eps, 1 if centre else 0, _pack(r), n, dim, _DTYPES[dtype],
              _ROWS.pack(dx.data_ptr(), dim), dgain.data_ptr(), dbias.data_ptr() if bias else None, workspace.data_ptr(), size)

@@ -33,7 +33,7 @@ def test_sizes(lib):
     assert lib.sjd_embed_gradient_workspace_size(3, 5) == 4 * (5 + 1 + 3)
     assert lib.sjd_embed_gradient_workspace_size(2 ** 31 - 1, 2 ** 31 - 1) == 4 * (2 ** 32 - 1)
     assert lib.sjd_embed_gradient_workspace_size(0, 5) == lib.sjd_embed_gradient_workspace_size(5, 0) == 0
-    assert lib.sjd_norm_gradient_workspace_size(0, 5) == lib.sjd_norm_gradient_workspace_size(5, 16385) == 0
+    assert lib.sjd_norm_gradient_workspace_size(0, 5, 0) == lib.sjd_norm_gradient_workspace_size(5, 16385, 0) == lib.sjd_norm_gradient_workspace_size(5, 5, 2) == 0
     assert lib.sjd_product_workspace_size(0, 5, 5) == lib.sjd_product_workspace_size(5, 5, 65537) == 0
 
 
