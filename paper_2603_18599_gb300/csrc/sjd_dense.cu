@@ -21,9 +21,15 @@
 
 namespace sjd_dense_ops {
 
+using sjd_kv_ops::add2;
+using sjd_kv_ops::fma2;
+using sjd_kv_ops::halves;
 using sjd_kv_ops::launch_early;
 using sjd_kv_ops::let_next_start;
+using sjd_kv_ops::mul2;
 using sjd_kv_ops::pack_bf16;
+using sjd_kv_ops::Pair;
+using sjd_kv_ops::pair;
 using sjd_kv_ops::unpack_bf16;
 using sjd_kv_ops::wait_for_previous;
 
@@ -81,14 +87,43 @@ __device__ __forceinline__ void store8(T* row, int i, int lane, int G, int D, co
   }
 }
 
+// The same in pairs of neighbours, which are added and multiplied two at a time.
+template <bool W, typename T>
+__device__ __forceinline__ void load8(const T* row, int i, int lane, int G, int D, Pair (&v)[4]) {
+  float f[8];
+  load8<W>(row, i, lane, G, D, f);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = pair(f[2 * j], f[2 * j + 1]);
+}
+template <bool W, typename T>
+__device__ __forceinline__ void store8(T* row, int i, int lane, int G, int D, const Pair (&v)[4]) {
+  float f[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 x = halves(v[j]);
+    f[2 * j] = x.x, f[2 * j + 1] = x.y;
+  }
+  store8<W>(row, i, lane, G, D, f);
+}
+// x for the features that are there, 0 for those that fill up the last piece.
+template <bool W>
+__device__ __forceinline__ Pair where_there(float x, int i, int j, int lane, int G, int D) {
+  if constexpr (W) {
+    const float y = feature<true>(i, 0, lane, G) < D ? x : 0.0f;   // (whole pieces)
+    return pair(y, y);
+  } else {
+    return pair(feature<false>(i, 2 * j, lane, G) < D ? x : 0.0f, feature<false>(i, 2 * j + 1, lane, G) < D ? x : 0.0f);
+  }
+}
+
 // Vectors of one float a feature (gains), which are 16-byte aligned where rows are.
 template <bool W>
-__device__ __forceinline__ void load_vector(const float* p, float otherwise, int i, int lane, int G, int D, float (&v)[8]) {
+__device__ __forceinline__ void load_vector(const float* p, float otherwise, int i, int lane, int G, int D, Pair (&v)[4]) {
   if (p) {
     load8<W>(p, i, lane, G, D, v);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = otherwise;
+    for (int j = 0; j < 4; ++j) v[j] = pair(otherwise, otherwise);
   }
 }
 
@@ -159,23 +194,29 @@ __device__ __forceinline__ void copy_row(const T* row, T* to, int G, int D) {
   }
 }
 
-// x / scale of eight values, as IEEE division rounds it. With the reciprocal
-// rounded to nearest, two corrections by the exact remainder give the nearest
-// quotient (Markstein, IBM J. Res. Dev. 34, 1990), as long as the remainders of
-// quotients that matter do not underflow: for scales within 2^60 of 1.
-__device__ __forceinline__ float quotient(float x, float scale, float inverse) {
-  float q = x * inverse;
-  q = fmaf(fmaf(-q, scale, x), inverse, q);
-  return fmaf(fmaf(-q, scale, x), inverse, q);
+// x / scale, as IEEE division rounds it. With the reciprocal rounded to nearest,
+// two corrections by the exact remainder give the nearest quotient (Markstein,
+// IBM J. Res. Dev. 34, 1990), as long as the remainders of quotients that matter
+// do not underflow: for scales within 2^60 of 1.
+__device__ __forceinline__ Pair quotients(Pair x, Pair less, Pair inverse) {   // less: -scale
+  Pair q = mul2(x, inverse);
+  q = fma2(fma2(q, less, x), inverse, q);
+  return fma2(fma2(q, less, x), inverse, q);
+}
+// The larger of m and |x|; a NaN, once met, stays.
+__device__ __forceinline__ float larger(float m, float x) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(m), "f"(fabsf(x)));
+  return r;
 }
 
 // A row in registers becomes y = (h - m) r gain + bias, h = x + residual rounded
 // to the rows' type, m the mean (0 without centring), r = 1 / sqrt(mean of
 // (h - m)^2 + eps); or y's codes and scale, or (MODE kCodes) those of x itself.
 // w: the residual's row. `there`: the row is to be written.
-template <typename T, bool W, int C, int MODE>
-__device__ __forceinline__ void norm_row(const NormParams& p, long long row, bool there, int lane, int G, float (&v)[C][8], float (&w)[C][8], float* words,
-                                         int& turn) {
+template <typename T, bool W, int C, int MODE, typename GainsOf>
+__device__ __forceinline__ void norm_row(const NormParams& p, long long row, bool there, int lane, int G, Pair (&v)[C][4], Pair (&w)[C][4], float* words,
+                                         int& turn, const GainsOf& gains) {
   const int D = p.dim;
   const float over = 1.0f / static_cast<float>(D);
   if (MODE != kCodes && p.residual.p) {
@@ -183,43 +224,48 @@ __device__ __forceinline__ void norm_row(const NormParams& p, long long row, boo
 #pragma unroll
     for (int i = 0; i < C; ++i) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = static_cast<float>(static_cast<T>(v[i][j] + w[i][j]));
+      for (int j = 0; j < 4; ++j) {
+        const float2 x = halves(add2(v[i][j], w[i][j]));
+        v[i][j] = pair(static_cast<float>(static_cast<T>(x.x)), static_cast<float>(static_cast<T>(x.y)));
+      }
       if (there) store8<W>(h, i, lane, G, D, v[i]);
     }
   }
   if constexpr (MODE != kCodes) {
     if (p.centre) {
-      float sum[1] = {0.0f};
+      Pair sums[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
 #pragma unroll
       for (int i = 0; i < C; ++i) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum[0] += v[i][j];
+        for (int j = 0; j < 4; ++j) sums[j & 1] = add2(sums[j & 1], v[i][j]);
       }
+      const float2 two = halves(add2(sums[0], sums[1]));
+      float sum[1] = {two.x + two.y};
       group_sum(sum, G, words, turn);
-      const float mean = sum[0] * over;
+      const float less = -(sum[0] * over);
 #pragma unroll
       for (int i = 0; i < C; ++i) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if (feature<W>(i, j, lane, G) < D) v[i][j] -= mean;
-        }
+        for (int j = 0; j < 4; ++j) v[i][j] = add2(v[i][j], where_there<W>(less, i, j, lane, G, D));
       }
     }
-    float squares[1] = {0.0f};
+    Pair sums[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
 #pragma unroll
     for (int i = 0; i < C; ++i) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) squares[0] = fmaf(v[i][j], v[i][j], squares[0]);
+      for (int j = 0; j < 4; ++j) sums[j & 1] = fma2(v[i][j], v[i][j], sums[j & 1]);
     }
+    const float2 two = halves(add2(sums[0], sums[1]));
+    float squares[1] = {two.x + two.y};
     group_sum(squares, G, words, turn);
     const float r = rsqrtf(squares[0] * over + p.eps);
+    const Pair rr = pair(r, r);
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      float g[8], b[8];
-      load_vector<W>(p.gain, 1.0f, i, lane, G, D, g);
-      load_vector<W>(p.bias, 0.0f, i, lane, G, D, b);
+      Pair g[4], b[4];
+      gains.take(i, g, b);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * r * g[j] + b[j];
+      for (int j = 0; j < 4; ++j) v[i][j] = fma2(mul2(v[i][j], rr), g[j], b[j]);
     }
   }
   if constexpr (MODE == kNorm) {
@@ -228,44 +274,115 @@ __device__ __forceinline__ void norm_row(const NormParams& p, long long row, boo
 #pragma unroll
     for (int i = 0; i < C; ++i) store8<W>(y, i, lane, G, D, v[i]);
   } else {
-    // the largest magnitude, by its bits: an infinity or a NaN is above all others
-    uint32_t bits = 0;
+    float most = 0.0f;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < 4; ++j) {
         // (what fills up the row may be a NaN here: 0 times an infinite factor)
-        if (feature<W>(i, j, lane, G) < D) bits = max(bits, __float_as_uint(v[i][j]) & 0x7fffffffu);
+        const float2 x = halves(v[i][j]);
+        if (feature<W>(i, W ? 0 : 2 * j, lane, G) < D) most = larger(most, x.x);
+        if (feature<W>(i, W ? 0 : 2 * j + 1, lane, G) < D) most = larger(most, x.y);
       }
     }
-    const float top = __uint_as_float(group_max(bits, G, words, turn)), scale = __fdiv_rn(top, 127.0f);
+    // (by the bits, in which an infinity or a NaN is above all others)
+    const float top = __uint_as_float(group_max(__float_as_uint(most), G, words, turn)), scale = __fdiv_rn(top, 127.0f);
     if (!there) return;
-    const bool some = top <= FLT_MAX && scale > 0.0f, plain = top > 0x1p-60f && top < 0x1p60f;
-    const float inverse = __frcp_rn(scale);
+    const bool some = top <= FLT_MAX && scale > 0.0f;
     int8_t* codes = p.codes + row * D;
+    if (top > 0x1p-60f && top < 0x1p60f) {
+      const float inverse = __frcp_rn(scale);
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i][j] = quotients(v[i][j], pair(-scale, -scale), pair(inverse, inverse));
+      }
+    } else {
+      // (a subnormal scale has few bits: quotients by it may pass 127)
+      auto held = [&](float x) { return some ? fminf(fmaxf(__fdiv_rn(x, scale), -127.0f), 127.0f) : 0.0f; };
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 x = halves(v[i][j]);
+          v[i][j] = pair(held(x.x), held(x.y));
+        }
+      }
+    }
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      uint32_t q[2] = {0, 0};
-      if (plain) {
+      // rounded to nearest even by the sum with 1.5 * 2^23, whose last byte is the code
+      uint32_t c[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = quotient(v[i][j], scale, inverse);
-      } else {
-        // (a subnormal scale has few bits: quotients by it may pass 127)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = some ? fminf(fmaxf(__fdiv_rn(v[i][j], scale), -127.0f), 127.0f) : 0.0f;
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int c = __float2int_rn(v[i][j]);
-        if constexpr (W) q[j / 4] |= static_cast<uint32_t>(c & 0xff) << 8 * (j % 4);
-        else if (feature<false>(i, j, lane, G) < D) codes[feature<false>(i, j, lane, G)] = static_cast<int8_t>(c);
+      for (int j = 0; j < 4; ++j) {
+        const float2 x = halves(add2(v[i][j], pair(0x1.8p23f, 0x1.8p23f)));
+        c[2 * j] = __float_as_uint(x.x), c[2 * j + 1] = __float_as_uint(x.y);
       }
       if constexpr (W) {
-        if (feature<true>(i, 0, lane, G) < D) *reinterpret_cast<uint2*>(codes + feature<true>(i, 0, lane, G)) = make_uint2(q[0], q[1]);
+        if (feature<true>(i, 0, lane, G) < D)
+          *reinterpret_cast<uint2*>(codes + feature<true>(i, 0, lane, G)) =
+              make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
+                         __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (feature<false>(i, j, lane, G) < D) codes[feature<false>(i, j, lane, G)] = static_cast<int8_t>(c[j] & 0xff);
+        }
       }
     }
     if (lane == 0) p.scale[row] = top <= FLT_MAX ? scale : NAN;
   }
+}
+
+template <bool W>
+struct Gains {
+  const NormParams& p;
+  int lane, G;
+  __device__ __forceinline__ void take(int i, Pair (&gain)[4], Pair (&bias)[4]) const {
+    load_vector<W>(p.gain, 1.0f, i, lane, G, p.dim, gain);
+    load_vector<W>(p.bias, -0.0f, i, lane, G, p.dim, bias);   // (adding -0 changes nothing)
+  }
+};
+
+// Rows of many: a block takes every gridDim-th, `deep` - 1 of them on their way while
+// one is summed up.
+template <typename T, int C, int MODE>
+__global__ void __launch_bounds__(512) norm_ahead_kernel(const NormParams p, int G, int deep) {
+  __shared__ __align__(16) float words[2 * 64];
+  extern __shared__ __align__(16) unsigned char shared[];
+  T* stages = reinterpret_cast<T*>(shared);
+  wait_for_previous();
+  let_next_start();
+  const int lane = threadIdx.x, D = p.dim;
+  const bool added = MODE != kCodes && p.residual.p;
+  const int stage_size = added ? 2 * D : D;
+  auto fetch = [&](long long row, int stage) {
+    if (row < p.rows) {
+      copy_row<T, C>(static_cast<const T*>(p.x.p) + row * p.x.stride, stages + stage * stage_size, G, D);
+      if (added) copy_row<T, C>(static_cast<const T*>(p.residual.p) + row * p.residual.stride, stages + stage * stage_size + D, G, D);
+    }
+    sjd_kv_ops::copy_commit();   // (the group of a row that is not there is empty)
+  };
+  for (int i = 0; i + 1 < deep; ++i) fetch(blockIdx.x + static_cast<long long>(i) * gridDim.x, i);
+  const Gains<true> gains{p, lane, G};
+  int turn = 0, stage = 0;
+  for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    if (deep == 2) sjd_kv_ops::copy_wait<0>();
+    else if (deep == 3) sjd_kv_ops::copy_wait<1>();
+    else sjd_kv_ops::copy_wait<2>();
+    fetch(row + (deep - 1ll) * gridDim.x, stage == 0 ? deep - 1 : stage - 1);   // (where the row before was)
+    const T* from = stages + stage * stage_size;
+    if (++stage == deep) stage = 0;
+    Pair v[C][4], w[C][4];
+#pragma unroll
+    for (int i = 0; i < C; ++i) load8<true>(from, i, lane, G, D, v[i]);
+    if (added) {
+#pragma unroll
+      for (int i = 0; i < C; ++i) load8<true>(from + D, i, lane, G, D, w[i]);
+    }
+    norm_row<T, true, C, MODE>(p, row, true, lane, G, v, w, words, turn, gains);
+  }
+  sjd_kv_ops::copy_wait_all();
 }
 
 // A group of G threads to a row: lanes of a warp, or a block.
@@ -279,14 +396,14 @@ __global__ void __launch_bounds__(512) norm_kernel(const NormParams p, int G) {
   const int per = blockDim.x / G, lane = threadIdx.x % G;
   const long long at = static_cast<long long>(blockIdx.x) * per + threadIdx.x / G, row = min(at, p.rows - 1ll);
   int turn = 0;
-  float v[C][8], w[C][8];
+  Pair v[C][4], w[C][4];
 #pragma unroll
   for (int i = 0; i < C; ++i) load8<W>(static_cast<const T*>(p.x.p) + row * p.x.stride, i, lane, G, p.dim, v[i]);
   if (MODE != kCodes && p.residual.p) {
 #pragma unroll
     for (int i = 0; i < C; ++i) load8<W>(static_cast<const T*>(p.residual.p) + row * p.residual.stride, i, lane, G, p.dim, w[i]);
   }
-  norm_row<T, W, C, MODE>(p, row, at < p.rows, lane, G, v, w, words, turn);
+  norm_row<T, W, C, MODE>(p, row, at < p.rows, lane, G, v, w, words, turn, Gains<W>{p, lane, G});
 }
 
 bool aligned16(const void* p, long long stride, size_t size) {
@@ -310,12 +427,46 @@ cudaError_t norm_with(const NormParams& p, cudaStream_t s) {
   return launch_early(norm_kernel<T, W, C, MODE>, static_cast<unsigned>((static_cast<long long>(p.rows) + per - 1) / per), threads, 0, s, p, G);
 }
 
-// Pieces of a thread. PIECES_FIGURES
+constexpr int ahead_registers(int mode) { return mode == kCodes ? 64 : 104; }   // of norm_ahead_kernel, at most
+
+// Blocks on an SM and rows on their way in each.
+struct Flow {
+  int per_sm, deep;
+  size_t shared;
+};
+Flow flow_of(int threads, int registers, size_t row) {
+  Flow f;
+  f.per_sm = min(8, max(1, 65536 / registers / threads));
+  while (f.per_sm > 1 && 2 * f.per_sm * row > 200 * 1024) --f.per_sm;
+  f.deep = 4;
+  while (f.deep > 2 && f.deep * f.per_sm * row > 128 * 1024) --f.deep;
+  f.shared = f.deep * row;
+  return f;
+}
+template <typename Kernel>
+cudaError_t allow_shared(Kernel kernel, size_t bytes) {
+  // (with what a kernel has beside it, 48 KB need no leave)
+  return bytes <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+}
+
+template <typename T, int C, int MODE>
+cudaError_t norm_ahead(const NormParams& p, int sms, const Flow& f, cudaStream_t s) {
+  const cudaError_t e = allow_shared(norm_ahead_kernel<T, C, MODE>, f.shared);
+  if (e != cudaSuccess) return e;
+  return launch_early(norm_ahead_kernel<T, C, MODE>, static_cast<unsigned>(min(p.rows, sms * f.per_sm)), threads_of(p.dim, C), f.shared, s, p,
+                      threads_of(p.dim, C), f.deep);
+}
+
+// PIECES_FIGURES
 template <typename T, bool W, int MODE>
 cudaError_t norm_by(const NormParams& p, int sms, cudaStream_t s) {
   const bool few = p.rows <= 2 * sms;
   const int d = p.dim;
   if (d <= 256 || (few && d <= 4096)) return norm_with<T, W, 1, MODE>(p, s);
+  if (W && !few && d > 512) {
+    const Flow f = flow_of(threads_of(d, 4), ahead_registers(MODE), sizeof(T) * d * (MODE != kCodes && p.residual.p ? 2 : 1));
+    if (f.shared <= 200 * 1024) return norm_ahead<T, 4, MODE>(p, sms, f, s);
+  }
   if (d <= 512 || ((few || !W) && d <= 8192)) return norm_with<T, W, 2, MODE>(p, s);
   return norm_with<T, W, 4, MODE>(p, s);
 }
@@ -332,47 +483,55 @@ cudaError_t norm_of(const NormParams& p, int mode, int sms, cudaStream_t s) {
 // With u = (x - m) r and g = dy gain: dx = r (g - mean(g) - u mean(g u)) + dh
 // (mean(g) where centred), dgain = sum of dy u over the rows, dbias = sum of dy.
 // The sums over a row are those of x and g, then of (x - m)^2 and g (x - m).
-// x: the row, g: dy, dh: what is added (or not); dx takes their place in g, u in x and dy in dh.
+// x: the row, which becomes u; dx: dh, where there is one, which becomes dx.
 template <bool W, int C, typename Gain>
-__device__ __forceinline__ void gradient_row(const NormGradientParams& p, int lane, int G, float (&x)[C][8], float (&dy)[C][8], float (&dx)[C][8],
+__device__ __forceinline__ void gradient_row(const NormGradientParams& p, int lane, int G, Pair (&x)[C][4], Pair (&dy)[C][4], Pair (&dx)[C][4],
                                              float* words, int& turn, Gain gain) {
   const int D = p.dim;
   const float over = 1.0f / static_cast<float>(D);
-  float mean = 0.0f, mean_g = 0.0f;
+  const Pair zero = pair(0.0f, 0.0f);
+  float less_mean_g = 0.0f;
   if (p.centre) {
-    float sum[2] = {0.0f, 0.0f};
+    Pair sx = zero, sg = zero;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      float g[8];
+      Pair g[4];
       gain(i, g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[0] += x[i][j], sum[1] = fmaf(dy[i][j], g[j], sum[1]);
+      for (int j = 0; j < 4; ++j) sx = add2(sx, x[i][j]), sg = fma2(dy[i][j], g[j], sg);
     }
+    const float2 a = halves(sx), b = halves(sg);
+    float sum[2] = {a.x + a.y, b.x + b.y};
     group_sum(sum, G, words, turn);
-    mean = sum[0] * over, mean_g = sum[1] * over;
-  }
-  float sum[2] = {0.0f, 0.0f};
+    const float less = -(sum[0] * over);
+    less_mean_g = -(sum[1] * over);
 #pragma unroll
-  for (int i = 0; i < C; ++i) {
-    float g[8];
-    gain(i, g);
+    for (int i = 0; i < C; ++i) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float u = feature<W>(i, j, lane, G) < D ? x[i][j] - mean : 0.0f;
-      x[i][j] = u;
-      sum[0] = fmaf(u, u, sum[0]), sum[1] = fmaf(dy[i][j] * g[j], u, sum[1]);
+      for (int j = 0; j < 4; ++j) x[i][j] = add2(x[i][j], where_there<W>(less, i, j, lane, G, D));
     }
   }
-  group_sum(sum, G, words, turn);
-  const float r = rsqrtf(sum[0] * over + p.eps), along = sum[1] * over * r;
+  Pair sx = zero, sg = zero;
 #pragma unroll
   for (int i = 0; i < C; ++i) {
-    float g[8];
+    Pair g[4];
     gain(i, g);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      x[i][j] *= r;
-      dx[i][j] = fmaf(dy[i][j] * g[j] - mean_g - x[i][j] * along, r, p.dh.p ? dx[i][j] : 0.0f);
+    for (int j = 0; j < 4; ++j) sx = fma2(x[i][j], x[i][j], sx), sg = fma2(mul2(dy[i][j], g[j]), x[i][j], sg);
+  }
+  const float2 a = halves(sx), b = halves(sg);
+  float sum[2] = {a.x + a.y, b.x + b.y};
+  group_sum(sum, G, words, turn);
+  const float r = rsqrtf(sum[0] * over + p.eps), less_along = -(sum[1] * over * r);
+  const Pair rr = pair(r, r), lg = pair(less_mean_g, less_mean_g), la = pair(less_along, less_along);
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    Pair g[4];
+    gain(i, g);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[i][j] = mul2(x[i][j], rr);
+      dx[i][j] = fma2(fma2(x[i][j], la, fma2(dy[i][j], g[j], lg)), rr, p.dh.p ? dx[i][j] : zero);
     }
   }
 }
@@ -386,23 +545,23 @@ __global__ void __launch_bounds__(kShortBlock) norm_gradient_short_kernel(const 
   let_next_start();
   const int lane = threadIdx.x % G, D = p.dim, per = kShortBlock / G;
   int turn = 0;
-  float dgain[C][8] = {}, dbias[C][8] = {};
+  Pair dgain[C][4] = {}, dbias[C][4] = {};
   for (long long first = static_cast<long long>(blockIdx.x) * per; first < p.rows; first += static_cast<long long>(gridDim.x) * per) {
     const long long at = first + threadIdx.x / G, row = min(at, p.rows - 1ll);
-    float x[C][8], dy[C][8], dx[C][8];
+    Pair x[C][4], dy[C][4], dx[C][4];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
       load8<W>(static_cast<const T*>(p.x.p) + row * p.x.stride, i, lane, G, D, x[i]);
       load8<W>(static_cast<const T*>(p.dy.p) + row * p.dy.stride, i, lane, G, D, dy[i]);
       if (p.dh.p) load8<W>(static_cast<const T*>(p.dh.p) + row * p.dh.stride, i, lane, G, D, dx[i]);
     }
-    gradient_row<W, C>(p, lane, G, x, dy, dx, nullptr, turn, [&](int i, float (&g)[8]) { load_vector<W>(p.gain, 1.0f, i, lane, G, D, g); });
+    gradient_row<W, C>(p, lane, G, x, dy, dx, nullptr, turn, [&](int i, Pair (&g)[4]) { load_vector<W>(p.gain, 1.0f, i, lane, G, D, g); });
     if (at >= p.rows) continue;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
       store8<W>(static_cast<T*>(p.dx.p) + row * p.dx.stride, i, lane, G, D, dx[i]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) dgain[i][j] = fmaf(dy[i][j], x[i][j], dgain[i][j]), dbias[i][j] += dy[i][j];
+      for (int j = 0; j < 4; ++j) dgain[i][j] = fma2(dy[i][j], x[i][j], dgain[i][j]), dbias[i][j] = add2(dbias[i][j], dy[i][j]);
     }
   }
   __syncwarp();
@@ -410,9 +569,9 @@ __global__ void __launch_bounds__(kShortBlock) norm_gradient_short_kernel(const 
 #pragma unroll
     for (int i = 0; i < C; ++i) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        dgain[i][j] += __shfl_xor_sync(0xffffffffu, dgain[i][j], o);
-        dbias[i][j] += __shfl_xor_sync(0xffffffffu, dbias[i][j], o);
+      for (int j = 0; j < 4; ++j) {
+        dgain[i][j] = add2(dgain[i][j], Pair{__shfl_xor_sync(0xffffffffu, dgain[i][j].v, o)});
+        dbias[i][j] = add2(dbias[i][j], Pair{__shfl_xor_sync(0xffffffffu, dbias[i][j].v, o)});
       }
     }
   }
@@ -423,7 +582,8 @@ __global__ void __launch_bounds__(kShortBlock) norm_gradient_short_kernel(const 
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int e = feature<W>(i, j, lane, G);
-          if (e < D) sums[0][e] = (w ? sums[0][e] : 0.0f) + dgain[i][j], sums[1][e] = (w ? sums[1][e] : 0.0f) + dbias[i][j];
+          const float2 dg = halves(dgain[i][j / 2]), db = halves(dbias[i][j / 2]);
+          if (e < D) sums[0][e] = (w ? sums[0][e] : 0.0f) + (j & 1 ? dg.y : dg.x), sums[1][e] = (w ? sums[1][e] : 0.0f) + (j & 1 ? db.y : db.x);
         }
       }
     }
@@ -461,7 +621,7 @@ __global__ void __launch_bounds__(WAY == kShared ? 1024 : 512) norm_gradient_ker
     }
     sjd_kv_ops::copy_commit();   // (the group of a row that is not there is empty)
   };
-  float dgain[WAY == kShared ? 1 : C][8] = {}, dbias[WAY == kShared ? 1 : C][8] = {}, gains[WAY == kShared ? 1 : C][8];
+  Pair dgain[WAY == kShared ? 1 : C][4] = {}, dbias[WAY == kShared ? 1 : C][4] = {}, gains[WAY == kShared ? 1 : C][4];
   if constexpr (WAY == kShared) {
     for (int i = lane; i < 2 * D; i += G) sums[i] = 0.0f;
     __syncthreads();
@@ -483,34 +643,50 @@ __global__ void __launch_bounds__(WAY == kShared ? 1024 : 512) norm_gradient_ker
       xs = stages + stage * kinds * D, dys = xs + D, dhs = dys + D;
       if (++stage == deep) stage = 0;
     }
-    float x[C][8], dy[C][8], dx[C][8];
+    Pair x[C][4], dy[C][4], dx[C][4];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
       load8<W>(xs, i, lane, G, D, x[i]);
       load8<W>(dys, i, lane, G, D, dy[i]);
       if (p.dh.p) load8<W>(dhs, i, lane, G, D, dx[i]);
     }
-    gradient_row<W, C>(p, lane, G, x, dy, dx, words, turn, [&](int i, float (&g)[8]) {
+    gradient_row<W, C>(p, lane, G, x, dy, dx, words, turn, [&](int i, Pair (&g)[4]) {
       if constexpr (WAY == kShared) {
         load_vector<W>(p.gain, 1.0f, i, lane, G, D, g);
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) g[j] = gains[i][j];
+        for (int j = 0; j < 4; ++j) g[j] = gains[i][j];
       }
     });
     T* dxs = static_cast<T*>(p.dx.p) + row * p.dx.stride;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
       store8<W>(dxs, i, lane, G, D, dx[i]);
+      if constexpr (WAY == kShared) {
+        // (a thread's own columns, four of them at a time where they are neighbours)
+        if constexpr (W) {
+          const int e = feature<true>(i, 0, lane, G);
+          if (e < D) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if constexpr (WAY == kShared) {
-          const int e = feature<W>(i, j, lane, G);
-          if (e < D) sums[e] = fmaf(dy[i][j], x[i][j], sums[e]), sums[D + e] += dy[i][j];
+            for (int j = 0; j < 4; j += 2) {
+              ulonglong2* a = reinterpret_cast<ulonglong2*>(sums + e + 2 * j);
+              ulonglong2* b = reinterpret_cast<ulonglong2*>(sums + D + e + 2 * j);
+              const ulonglong2 u = *a, v = *b;
+              *a = make_ulonglong2(fma2(dy[i][j], x[i][j], Pair{u.x}).v, fma2(dy[i][j + 1], x[i][j + 1], Pair{u.y}).v);
+              *b = make_ulonglong2(add2(dy[i][j], Pair{v.x}).v, add2(dy[i][j + 1], Pair{v.y}).v);
+            }
+          }
         } else {
-          dgain[i][j] = fmaf(dy[i][j], x[i][j], dgain[i][j]);
-          dbias[i][j] += dy[i][j];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int e = feature<false>(i, j, lane, G);
+            const float2 u = halves(x[i][j / 2]), d = halves(dy[i][j / 2]);
+            if (e < D) sums[e] = fmaf(j & 1 ? d.y : d.x, j & 1 ? u.y : u.x, sums[e]), sums[D + e] += j & 1 ? d.y : d.x;
+          }
         }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dgain[i][j] = fma2(dy[i][j], x[i][j], dgain[i][j]), dbias[i][j] = add2(dbias[i][j], dy[i][j]);
       }
     }
   }
@@ -522,8 +698,9 @@ __global__ void __launch_bounds__(WAY == kShared ? 1024 : 512) norm_gradient_ker
     for (int j = 0; j < 8; ++j) {
       const int e = feature<W>(i, j, lane, G);
       if (e >= D) continue;
-      part[e] = WAY == kShared ? sums[e] : dgain[WAY == kShared ? 0 : i][j];
-      if (p.dbias) part[D + e] = WAY == kShared ? sums[D + e] : dbias[WAY == kShared ? 0 : i][j];
+      const float2 dg = halves(dgain[WAY == kShared ? 0 : i][j / 2]), db = halves(dbias[WAY == kShared ? 0 : i][j / 2]);
+      part[e] = WAY == kShared ? sums[e] : j & 1 ? dg.y : dg.x;
+      if (p.dbias) part[D + e] = WAY == kShared ? sums[D + e] : j & 1 ? db.y : db.x;
     }
   }
 }
@@ -548,33 +725,18 @@ __global__ void __launch_bounds__(32 * kSumRows) add_parts_kernel(const NormGrad
   if (lane == 0 && of >= p.dim && of < columns) p.dbias[of - p.dim] = sum;
 }
 
-// Blocks of the gradient's first kernel on an SM (by its 128 registers) and
-// rows on their way in each: shared memory holds them, and there is no use for more
-// than 96 KB of them.
-struct Flow {
-  int per_sm, deep;
-  size_t shared;
-};
+// Blocks of the gradient's first kernel (of 128 registers a thread).
 Flow gradient_flow(int dim, size_t size) {
   if (dim > 8192) return {1, 0, 2 * sizeof(float) * dim};
-  const size_t row = 3 * size * dim;
-  Flow f;
-  f.per_sm = min(8, max(1, 65536 / 128 / threads_of(dim, 2)));
-  while (f.per_sm > 1 && 2 * f.per_sm * row > 200 * 1024) --f.per_sm;
-  f.deep = 4;
-  while (f.deep > 2 && f.deep * f.per_sm * row > 128 * 1024) --f.deep;
-  f.shared = f.deep * row;
-  return f;
+  return flow_of(threads_of(dim, 2), 128, 3 * size * dim);
 }
 
 template <typename T, bool W, int WAY>
 cudaError_t norm_gradient_with(const NormGradientParams& p, const Flow& f, cudaStream_t s) {
   const int G = threads_of(p.dim, 2);
   const size_t shared = WAY == kDirect ? 0 : f.shared;
-  if (shared > 40 * 1024) {   // (with the words 48 KB, which any kernel may have)
-    const cudaError_t e = cudaFuncSetAttribute(norm_gradient_kernel<T, W, WAY>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
-    if (e != cudaSuccess) return e;
-  }
+  const cudaError_t e = allow_shared(norm_gradient_kernel<T, W, WAY>, shared);
+  if (e != cudaSuccess) return e;
   return launch_early(norm_gradient_kernel<T, W, WAY>, p.blocks, G, shared, s, p, G, f.deep);
 }
 
@@ -586,7 +748,7 @@ cudaError_t norm_gradient_by(const NormGradientParams& p, cudaStream_t s) {
   if (p.dim <= kShort / 2) e = launch_early(norm_gradient_short_kernel<T, W, 1>, p.blocks, kShortBlock, 0, s, p, lanes_of(p.dim, 1));
   else if (p.dim <= kShort) e = launch_early(norm_gradient_short_kernel<T, W, 2>, p.blocks, kShortBlock, 0, s, p, lanes_of(p.dim, 2));
   else if (p.dim > 8192) e = norm_gradient_with<T, W, kShared>(p, f, s);
-  else if (W && f.shared <= 227 * 1024 - 1024) e = norm_gradient_with<T, W, W ? kAhead : kDirect>(p, f, s);
+  else if (W && f.shared <= 200 * 1024) e = norm_gradient_with<T, W, W ? kAhead : kDirect>(p, f, s);
   else e = norm_gradient_with<T, W, kDirect>(p, f, s);
   if (e != cudaSuccess) return e;
   return launch_early(add_parts_kernel, (columns + 31) / 32, 32 * kSumRows, 0, s, p, columns);
@@ -594,56 +756,83 @@ cudaError_t norm_gradient_by(const NormGradientParams& p, cudaStream_t s) {
 
 // --- embedding -----------------------------------------------------------------
 
-// y[t] = scale table[tokens[t]], zeros where the token is no row of the table.
+// y[t] = scale table[tokens[t]], zeros where the token is no row of the table. A
+// group of G threads to a row, four pieces of a thread on their way at a time.
+constexpr int kEmbedBlock = 128;
 template <typename E, typename T, bool W>
-__global__ void embed_kernel(const EmbedParams p) {
+__global__ void __launch_bounds__(kEmbedBlock) embed_kernel(const EmbedParams p, int G) {
+  constexpr int kDeep = 4;
   wait_for_previous();
   let_next_start();
-  for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
-    const int token = p.tokens[row], D = p.dim;
-    const bool inside = token >= 0 && token < p.vocab;
-    const E* x = static_cast<const E*>(p.table.p) + (inside ? token : 0) * p.table.stride;
-    T* y = static_cast<T*>(p.y.p) + row * p.y.stride;
-    float v[8] = {};
+  const long long row = static_cast<long long>(blockIdx.x) * (kEmbedBlock / G) + threadIdx.x / G;
+  if (row >= p.rows) return;
+  const int token = p.tokens[row], D = p.dim, lane = threadIdx.x % G;
+  const bool inside = token >= 0 && token < p.vocab;
+  const E* x = static_cast<const E*>(p.table.p) + (inside ? token : 0) * p.table.stride;
+  T* y = static_cast<T*>(p.y.p) + row * p.y.stride;
+  for (int i0 = 0; i0 * 8 * G < D; i0 += kDeep) {
+    float v[kDeep][8] = {};
     if (inside) {
-      load8<W>(x, blockIdx.x, threadIdx.x, blockDim.x, D, v);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] *= p.scale;
+      for (int i = 0; i < kDeep; ++i) load8<W>(x, i0 + i, lane, G, D, v[i]);
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] *= p.scale;
+      }
     }
-    store8<W>(y, blockIdx.x, threadIdx.x, blockDim.x, D, v);
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) store8<W>(y, i0 + i, lane, G, D, v[i]);
   }
 }
 
 template <typename E, typename T>
 cudaError_t embed_of(const EmbedParams& p, cudaStream_t s) {
   const bool w = p.dim % 8 == 0 && wide(p.table, p.vocab, sizeof(E)) && wide(p.y, p.rows, sizeof(T));
-  const int threads = min(128, threads_of(p.dim, 1));
-  const dim3 grid((p.dim + 8 * threads - 1) / (8 * threads), min(p.rows, 65535));
-  return w ? launch_early(embed_kernel<E, T, true>, grid, threads, 0, s, p) : launch_early(embed_kernel<E, T, false>, grid, threads, 0, s, p);
+  const int G = p.dim <= 1024 ? lanes_of(p.dim, 4) : kEmbedBlock, per = kEmbedBlock / G;
+  const unsigned blocks = static_cast<unsigned>((static_cast<long long>(p.rows) + per - 1) / per);
+  return w ? launch_early(embed_kernel<E, T, true>, blocks, kEmbedBlock, 0, s, p, G) : launch_early(embed_kernel<E, T, false>, blocks, kEmbedBlock, 0, s, p, G);
 }
 
 // The rows of each id, ascending. A block takes kIds ids and looks through all
 // tokens (they stay in L2): it counts those of its ids and those before them,
 // which is where its part of `places` begins, and then puts the rows of its ids
 // there. Warp w looks through the w-th part of the tokens both times, so that
-// its rows of an id stand behind those of the warps before it.
-constexpr int kIds = 256, kIndexWarps = 32;
+// its rows of an id stand behind those of the warps before it. The ids that have
+// more than kFew rows are listed.
+constexpr int kFew = 32;
+constexpr int kIds = kListIds, kIndexWarps = 32;
+__device__ __forceinline__ int4* many_of(const EmbedGradientParams& p, int list) { return p.many + static_cast<long long>(list) * (kIds + 1); }
 __global__ void __launch_bounds__(32 * kIndexWarps) index_kernel(const EmbedGradientParams p) {
+  constexpr int kDeep = 8;   // loads of a thread on their way
   __shared__ int at[kIndexWarps][kIds];
-  __shared__ int before[kIndexWarps], sums[kIds / 32];
+  __shared__ int before[kIndexWarps], sums[kIds / 32], n_many;
   wait_for_previous();
   let_next_start();
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, low = blockIdx.x * kIds;
   for (int i = lane; i < kIds; i += 32) at[warp][i] = 0;
+  if (threadIdx.x == 0) n_many = 0;
   __syncwarp();
   const long long per = (static_cast<long long>(p.rows) + 32 * kIndexWarps - 1) / (32 * kIndexWarps) * 32;
   const long long begin = warp * per, end = min(static_cast<long long>(p.rows), begin + per);
   const int here = min(kIds, p.vocab - low);
+  auto load = [&](long long t0, int (&token)[kDeep]) {
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) {
+      const long long t = t0 + 32 * i + lane;
+      token[i] = t < end ? p.tokens[t] : -1;
+    }
+  };
   int less = 0;
-  for (long long t = begin + lane; t < end; t += 32) {
-    const int token = p.tokens[t], id = token - low;
-    if (token >= 0 && id < 0) ++less;
-    if (token >= low && id < here) atomicAdd(&at[warp][id], 1);
+  for (long long t0 = begin; t0 < end; t0 += 32 * kDeep) {
+    int token[kDeep];
+    load(t0, token);
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) {
+      const int id = token[i] - low;
+      if (token[i] >= 0 && id < 0) ++less;
+      if (token[i] >= low && id < here) atomicAdd(&at[warp][id], 1);
+    }
   }
   less = __reduce_add_sync(0xffffffffu, less);
   if (lane == 0) before[warp] = less;
@@ -665,6 +854,7 @@ __global__ void __launch_bounds__(32 * kIndexWarps) index_kernel(const EmbedGrad
     for (int w = 0; w < kIndexWarps; ++w) base += before[w];
     for (int w = 0; w < warp; ++w) base += sums[w];
     if (static_cast<int>(threadIdx.x) < here) p.first[low + threadIdx.x] = base;
+    if (count > kFew) many_of(p, blockIdx.x)[1 + atomicAdd(&n_many, 1)] = make_int4(low + threadIdx.x, base, count, 0);
     if (low + static_cast<int>(threadIdx.x) == p.vocab - 1) p.first[p.vocab] = base + count;
     for (int w = 0; w < kIndexWarps; ++w) {
       const int n = at[w][threadIdx.x];
@@ -673,86 +863,174 @@ __global__ void __launch_bounds__(32 * kIndexWarps) index_kernel(const EmbedGrad
     }
   }
   __syncthreads();
-  for (long long t0 = begin; t0 < end; t0 += 32) {
-    const long long t = t0 + lane;
-    const int token = t < end ? p.tokens[t] : -1, id = token - low;
-    const bool mine = token >= low && id < here;
-    const unsigned which = __ballot_sync(0xffffffffu, mine);
-    if (!which) continue;
-    if (mine) {
-      const unsigned same = __match_any_sync(which, id);
-      p.places[at[warp][id] + __popc(same & ((1u << lane) - 1))] = static_cast<int>(t);
-      __syncwarp(which);
-      if (lane == 31 - __clz(same)) at[warp][id] += __popc(same);
+  if (threadIdx.x == 0) many_of(p, blockIdx.x)[0].x = n_many;
+  for (long long t0 = begin; t0 < end; t0 += 32 * kDeep) {
+    int token[kDeep];
+    load(t0, token);
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) {
+      const int id = token[i] - low;
+      const bool mine = token[i] >= low && id < here;
+      const unsigned which = __ballot_sync(0xffffffffu, mine);
+      if (!which) continue;
+      if (mine) {
+        const unsigned same = __match_any_sync(which, id);
+        p.places[at[warp][id] + __popc(same & ((1u << lane) - 1))] = static_cast<int>(t0 + 32 * i + lane);
+        __syncwarp(which);
+        if (lane == 31 - __clz(same)) at[warp][id] += __popc(same);
+      }
+      __syncwarp();
     }
-    __syncwarp();
   }
 }
 
-// grad[v] = scale sum of dy over the rows of v, in their order. A block takes
-// kSumIds ids and kSumColumns columns of them; a thread 4 columns of every
-// kSumGroups-th id.
-constexpr int kSumIds = 16, kSumGroups = 4, kSumColumns = 256;
+template <bool W, typename T>
+__device__ __forceinline__ void load_columns(const T* p, float (&x)[W ? 4 : 1]) {
+  if constexpr (W) sjd_kv_ops::load4(p, true, x);
+  else x[0] = static_cast<float>(*p);
+}
+
+// grad[v] = scale sum of dy over the rows of v, in their order.
+//
+// The ids that have more than kFew rows are what most is read of: a block takes
+// 128 columns of every shares-th such id of every groups-th list, the id's rows
+// shared out to its warps, whose sums are added up in order.
+constexpr int kSumBlock = 256, kSumColumns = 128, kGroups = 8, kPlaces = 512;
 template <typename T, bool W>
-__global__ void __launch_bounds__(kSumGroups * kSumColumns / 4) embed_gradient_kernel(const EmbedGradientParams p, int slices, long long items) {
-  __shared__ int first[kSumIds + 1];
+__global__ void __launch_bounds__(kSumBlock, 4) embed_gradient_many_kernel(const EmbedGradientParams p, int slices, int shares, int groups, int lists) {
+  constexpr int V = W ? 4 : 1, kDeep = 8, kWarps = kSumBlock / 32, kPieces = kSumColumns / 32 / V;   // (pieces of a lane)
+  __shared__ float sums[kWarps][kSumColumns];
   wait_for_previous();
   let_next_start();
-  const int group = threadIdx.x / (kSumColumns / 4), lane = threadIdx.x % (kSumColumns / 4), D = p.dim;
-  for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-    const int slice = static_cast<int>(item % slices), v0 = static_cast<int>(item / slices) * kSumIds;
-    __syncthreads();
-    if (threadIdx.x <= kSumIds) first[threadIdx.x] = p.first[min(p.vocab, v0 + static_cast<int>(threadIdx.x))];
-    __syncthreads();
-    auto column = [&](int j) { return slice * kSumColumns + (W ? 4 * lane + j : j * (kSumColumns / 4) + lane); };
-    for (int k = group; k < kSumIds; k += kSumGroups) {
-      if (v0 + k >= p.vocab) break;
-      float sum[4] = {};
-#pragma unroll 4
-      for (int i = first[k]; i < first[k + 1]; ++i) {
-        const T* dy = static_cast<const T*>(p.dy.p) + p.places[i] * p.dy.stride;
-        float x[4] = {};
-        if constexpr (W) {
-          if (column(0) < D) sjd_kv_ops::load4(dy + column(0), true, x);
-        } else {
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, D = p.dim;
+  const int slice = blockIdx.x % slices, share = blockIdx.x / slices % shares, group = blockIdx.x / (slices * shares);
+  for (long long list0 = group; list0 < lists; list0 += 32ll * groups) {
+    const long long of_lane = list0 + static_cast<long long>(lane) * groups;
+    const int n_of_lane = of_lane < lists ? many_of(p, static_cast<int>(of_lane))[0].x : 0;
+    for (unsigned some = __ballot_sync(0xffffffffu, n_of_lane > share); some; some &= some - 1) {
+      const int from_lane = __ffs(some) - 1, n = __shfl_sync(0xffffffffu, n_of_lane, from_lane);
+      const int4* many = many_of(p, static_cast<int>(list0 + static_cast<long long>(from_lane) * groups)) + 1;
+      for (int k = share; k < n; k += shares) {
+        const int4 id = many[k];   // the id, where its places begin, how many
+        const int per = (id.z + kWarps - 1) / kWarps, begin = id.y + warp * per, end = min(begin + per, id.y + id.z);
+        float sum[kPieces][V] = {};
+        for (int r0 = begin; r0 < end; r0 += 32) {
+          const int place = r0 + lane < end ? p.places[r0 + lane] : 0, rows = min(32, end - r0);
+          for (int r = 0; r < rows; r += kDeep) {
+            float x[kDeep][kPieces][V] = {};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (column(j) < D) x[j] = static_cast<float>(dy[column(j)]);
+            for (int u = 0; u < kDeep; ++u) {
+              const int row = __shfl_sync(0xffffffffu, place, (r + u) & 31);
+#pragma unroll
+              for (int c = 0; c < kPieces; ++c) {
+                const int column = slice * kSumColumns + (c * 32 + lane) * V;
+                if (r + u < rows && column < D) load_columns<W>(static_cast<const T*>(p.dy.p) + row * p.dy.stride + column, x[u][c]);
+              }
+            }
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u) {
+#pragma unroll
+              for (int c = 0; c < kPieces; ++c) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[c][j] += x[u][c][j];   // (0 for those that are not there)
+              }
+            }
           }
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[j] += x[j];
-      }
-      float* out = p.grad + static_cast<long long>(v0 + k) * D;
+        for (int c = 0; c < kPieces; ++c) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum[j] *= p.scale;
-      if constexpr (W) {
-        if (column(0) < D) sjd_kv_ops::store4(out + column(0), true, sum);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (column(j) < D) out[column(j)] = sum[j];
+          for (int j = 0; j < V; ++j) sums[warp][(c * 32 + lane) * V + j] = sum[c][j];
         }
+        __syncthreads();
+        for (int column = threadIdx.x; column < kSumColumns; column += kSumBlock) {
+          float all = 0.0f;
+          for (int w = 0; w < kWarps; ++w) all += sums[w][column];
+          if (slice * kSumColumns + column < D) p.grad[static_cast<long long>(id.x) * D + slice * kSumColumns + column] = all * p.scale;
+        }
+        __syncthreads();
       }
     }
+  }
+}
+
+// The other ids: what bounds it is the writing, so that a block writes
+// neighbours, 64 KB of them (512-byte pieces of rows that lie apart: a third of the
+// rate), and has few registers (32 warps' loads hide one another; half of them: 1.5
+// times the time). A thread takes four columns at a time (one, where rows cannot be accessed
+// four elements at a time).
+//
+// `early`: the kernel before this one on the stream is the one above, which writes other
+// rows, and let this one in after the index was done: this one waits for it at its end, not
+// at its beginning, so that the two run together.
+template <typename T, bool W>
+__global__ void __launch_bounds__(kSumBlock, 8) embed_gradient_kernel(const EmbedGradientParams p, int ids, int lanes, bool early) {
+  constexpr int V = W ? 4 : 1;
+  __shared__ int first[257], places[kPlaces];
+  if (!early) {
+    wait_for_previous();
+    let_next_start();
+  }
+  const int D = p.dim, v0 = blockIdx.x * ids, here = min(ids, p.vocab - v0);
+  for (int i = threadIdx.x; i <= here; i += kSumBlock) first[i] = p.first[v0 + i];
+  __syncthreads();
+  const int base = first[0], lane = threadIdx.x & (lanes - 1);
+  if (first[here] > base) {
+    for (int i = threadIdx.x; i < min(kPlaces, first[here] - base); i += kSumBlock) places[i] = p.places[base + i];
+    __syncthreads();
+  }
+  // `lanes` threads (a power of two) to an id
+  for (int k = threadIdx.x / lanes; k < here; k += kSumBlock / lanes) {
+    const int from = first[k] - base, count = first[k + 1] - base - from;
+    if (count > kFew) continue;
+    float* out = p.grad + (static_cast<long long>(v0) + k) * D;
+    for (int column = lane * V; column < D; column += lanes * V) {
+      float sum[V] = {};
+      for (int r = 0; r < count; ++r) {
+        const int at = from + r;
+        float x[V];
+        load_columns<W>(static_cast<const T*>(p.dy.p) + (at < kPlaces ? places[at] : p.places[base + at]) * p.dy.stride + column, x);
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] += x[j];
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[j] *= p.scale;
+      if constexpr (W) sjd_kv_ops::store4(out + column, true, sum);
+      else out[column] = sum[0];
+    }
+  }
+  if (early) {
+    wait_for_previous();
+    let_next_start();
   }
 }
 
 template <typename T>
-cudaError_t embed_gradient_of(const EmbedGradientParams& p, int sms, cudaStream_t s) {
-  cudaError_t e = launch_early(index_kernel, static_cast<unsigned>((p.vocab + kIds - 1) / kIds), 32 * kIndexWarps, 0, s, p);
+cudaError_t embed_gradient_of(const EmbedGradientParams& p, cudaStream_t s) {
+  const int lists = embed_gradient_lists(p.vocab);
+  cudaError_t e = launch_early(index_kernel, static_cast<unsigned>(lists), 32 * kIndexWarps, 0, s, p);
   if (e != cudaSuccess) return e;
   const bool w = p.dim % 4 == 0 && reinterpret_cast<uintptr_t>(p.grad) % 16 == 0 && reinterpret_cast<uintptr_t>(p.dy.p) % (4 * sizeof(T)) == 0 &&
                  (p.rows < 2 || p.dy.stride % 4 == 0);
-  const int slices = (p.dim + kSumColumns - 1) / kSumColumns;
-  const long long items = static_cast<long long>((p.vocab + kSumIds - 1) / kSumIds) * slices;
-  const unsigned blocks = static_cast<unsigned>(min(items, 8ll * sms));
-  const int threads = kSumGroups * kSumColumns / 4;
-  return w ? launch_early(embed_gradient_kernel<T, true>, blocks, threads, 0, s, p, slices, items)
-           : launch_early(embed_gradient_kernel<T, false>, blocks, threads, 0, s, p, slices, items);
+  const int ids = max(1, min(256, 16384 / p.dim)), slices = (p.dim + kSumColumns - 1) / kSumColumns, groups = min(lists, kGroups),
+            shares = max(1, min(64, 1024 / (slices * groups)));
+  int lanes = 8;
+  while (lanes < kSumBlock && lanes * (w ? 4 : 1) < p.dim) lanes *= 2;
+  const unsigned blocks = static_cast<unsigned>((static_cast<long long>(p.vocab) + ids - 1) / ids);
+  const bool many = p.rows > kFew;   // (some id may have so many)
+  if (many) {
+    const unsigned n = static_cast<unsigned>(slices) * shares * groups;
+    e = w ? launch_early(embed_gradient_many_kernel<T, true>, n, kSumBlock, 0, s, p, slices, shares, groups, lists)
+          : launch_early(embed_gradient_many_kernel<T, false>, n, kSumBlock, 0, s, p, slices, shares, groups, lists);
+    if (e != cudaSuccess) return e;
+  }
+  return w ? launch_early(embed_gradient_kernel<T, true>, blocks, kSumBlock, 0, s, p, ids, lanes, many)
+           : launch_early(embed_gradient_kernel<T, false>, blocks, kSumBlock, 0, s, p, ids, lanes, many);
 }
 
 }  // namespace
+
+int embed_gradient_lists(int vocab) { return static_cast<int>((static_cast<long long>(vocab) + kIds - 1) / kIds); }
 
 cudaError_t launch_norm(const NormParams& p, int mode, int dtype, int sms, cudaStream_t s) {
   return dtype == SJD_BF16 ? norm_of<__nv_bfloat16>(p, mode, sms, s) : norm_of<float>(p, mode, sms, s);
@@ -772,13 +1050,13 @@ cudaError_t launch_norm_gradient(const NormGradientParams& p, int dtype, cudaStr
   return w ? norm_gradient_by<float, true>(p, s) : norm_gradient_by<float, false>(p, s);
 }
 
-cudaError_t launch_embed(const EmbedParams& p, int table_dtype, int dtype, int sms, cudaStream_t s) {
+cudaError_t launch_embed(const EmbedParams& p, int table_dtype, int dtype, cudaStream_t s) {
   if (table_dtype == SJD_BF16) return dtype == SJD_BF16 ? embed_of<__nv_bfloat16, __nv_bfloat16>(p, s) : embed_of<__nv_bfloat16, float>(p, s);
   return dtype == SJD_BF16 ? embed_of<float, __nv_bfloat16>(p, s) : embed_of<float, float>(p, s);
 }
 
-cudaError_t launch_embed_gradient(const EmbedGradientParams& p, int dtype, int sms, cudaStream_t s) {
-  return dtype == SJD_BF16 ? embed_gradient_of<__nv_bfloat16>(p, sms, s) : embed_gradient_of<float>(p, sms, s);
+cudaError_t launch_embed_gradient(const EmbedGradientParams& p, int dtype, cudaStream_t s) {
+  return dtype == SJD_BF16 ? embed_gradient_of<__nv_bfloat16>(p, s) : embed_gradient_of<float>(p, s);
 }
 
 }  // namespace sjd_dense_ops

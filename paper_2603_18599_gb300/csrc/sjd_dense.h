@@ -55,6 +55,7 @@ struct EmbedGradientParams {
   float* grad;              // [vocab][dim]
   int32_t* first;           // [vocab + 1]: where each id's places begin in `places`
   int32_t* places;          // [rows]: the rows of each id, ascending
+  int4* many;               // [lists][1 + ids of a list]: how many ids have many rows; of each the id, where its places begin, how many
   float scale;
   int rows, dim, vocab;
 };
@@ -105,8 +106,10 @@ struct ProductParams {
 cudaError_t launch_norm(const NormParams& p, int mode, int dtype, int sms, cudaStream_t s);
 int norm_gradient_blocks(int rows, int dim, int dtype, int sms);
 cudaError_t launch_norm_gradient(const NormGradientParams& p, int dtype, cudaStream_t s);
-cudaError_t launch_embed(const EmbedParams& p, int table_dtype, int dtype, int sms, cudaStream_t s);
-cudaError_t launch_embed_gradient(const EmbedGradientParams& p, int dtype, int sms, cudaStream_t s);
+cudaError_t launch_embed(const EmbedParams& p, int table_dtype, int dtype, cudaStream_t s);
+constexpr int kListIds = 256;  // ids of a list
+int embed_gradient_lists(int vocab);
+cudaError_t launch_embed_gradient(const EmbedGradientParams& p, int dtype, cudaStream_t s);
 cudaError_t launch_pack(const int8_t* w, long long stride, const float* scale, const Packed& to, cudaStream_t s);
 size_t product_scratch_bytes(int rows, int out, int in, int sms);
 cudaError_t launch_product(const ProductParams& p, int dtype, int sms, unsigned char* scratch, cudaStream_t s);

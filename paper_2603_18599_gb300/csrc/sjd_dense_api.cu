@@ -137,14 +137,12 @@ int sjd_embed(const sjd_rows* table, int32_t vocab, int32_t table_dtype, const i
   if (rows < 1 || vocab < 1 || dim < 1 || dim > kMaxInput || !floating(dtype) || !floating(table_dtype)) return SJD_ERR_ARG;
   if (!there(table, size_of(table_dtype)) || !there(y, size_of(dtype)) || !tokens || !aligned(tokens, 4)) return SJD_ERR_ARG;
   const EmbedParams p{rows_of(table), rows_of(y), tokens, scale, rows, dim, vocab};
-  int sms = 0;
-  if (!count_sms(&sms)) return SJD_ERR_CUDA;
-  return launched(launch_embed(p, table_dtype, dtype, sms, static_cast<cudaStream_t>(stream)));
+  return launched(launch_embed(p, table_dtype, dtype, static_cast<cudaStream_t>(stream)));
 }
 
 size_t sjd_embed_gradient_workspace_size(int32_t rows, int32_t vocab) {
   if (rows < 1 || vocab < 1) return 0;
-  return sizeof(int32_t) * (static_cast<size_t>(vocab) + 1 + static_cast<size_t>(rows));
+  return sizeof(int4) * embed_gradient_lists(vocab) * (1 + kListIds) + sizeof(int32_t) * (static_cast<size_t>(vocab) + 1 + static_cast<size_t>(rows));
 }
 
 int sjd_embed_gradient(const sjd_rows* dy, const int32_t* tokens, int32_t rows, int32_t dim, int32_t vocab, float scale, int32_t dtype, float* grad,
@@ -153,11 +151,10 @@ int sjd_embed_gradient(const sjd_rows* dy, const int32_t* tokens, int32_t rows, 
   if (!there(dy, size_of(dtype)) || !tokens || !aligned(tokens, 4) || !grad || !aligned(grad, 4) || !workspace || !aligned(workspace, kAlign))
     return SJD_ERR_ARG;
   if (ws_bytes < sjd_embed_gradient_workspace_size(rows, vocab)) return SJD_ERR_CAPACITY;
-  int32_t* first = static_cast<int32_t*>(workspace);
-  const EmbedGradientParams p{rows_of(dy), tokens, grad, first, first + vocab + 1, scale, rows, dim, vocab};
-  int sms = 0;
-  if (!count_sms(&sms)) return SJD_ERR_CUDA;
-  return launched(launch_embed_gradient(p, dtype, sms, static_cast<cudaStream_t>(stream)));
+  int4* many = static_cast<int4*>(workspace);
+  int32_t* first = reinterpret_cast<int32_t*>(many + static_cast<size_t>(embed_gradient_lists(vocab)) * (1 + kListIds));
+  const EmbedGradientParams p{rows_of(dy), tokens, grad, first, first + vocab + 1ll, many, scale, rows, dim, vocab};
+  return launched(launch_embed_gradient(p, dtype, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

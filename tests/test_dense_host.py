@@ -30,8 +30,9 @@ def test_sizes(lib):
     assert size(1 << 24, 65536) == 256 + (1 << 27) + (1 << 40)
     for out, dim in ((0, 1), (1, 0), (-1, 5), ((1 << 24) + 1, 1), (1, 65537)):
         assert size(out, dim) == 0, (out, dim)
-    assert lib.sjd_embed_gradient_workspace_size(3, 5) == 4 * (5 + 1 + 3)
-    assert lib.sjd_embed_gradient_workspace_size(2 ** 31 - 1, 2 ** 31 - 1) == 4 * (2 ** 32 - 1)
+    # where each id's places begin, the places, and a list of 256 ids and its length for every 256 ids
+    assert lib.sjd_embed_gradient_workspace_size(3, 5) == 4 * (5 + 1 + 3) + 16 * 257
+    assert lib.sjd_embed_gradient_workspace_size(2 ** 31 - 1, 2 ** 31 - 1) == 4 * (2 ** 32 - 1) + 16 * 2 ** 23 * 257
     assert lib.sjd_embed_gradient_workspace_size(0, 5) == lib.sjd_embed_gradient_workspace_size(5, 0) == 0
     assert lib.sjd_norm_gradient_workspace_size(0, 5, 0) == lib.sjd_norm_gradient_workspace_size(5, 16385, 0) == lib.sjd_norm_gradient_workspace_size(5, 5, 2) == 0
     assert lib.sjd_product_workspace_size(0, 5, 5) == lib.sjd_product_workspace_size(5, 5, 65537) == 0
