@@ -43,20 +43,24 @@ __device__ __forceinline__ int feature(int i, int j, int lane, int G) {
   return W ? (i * G + lane) * 8 + j : (i * 8 + j) * G + lane;
 }
 
-template <bool W, typename T>
+// (Wide loads behind the row's end take its last piece instead, and `FILL` puts zeros in its
+// place: a select costs less than a branch around the load.)
+template <bool W, bool FILL = true, typename T>
 __device__ __forceinline__ void load8(const T* row, int i, int lane, int G, int D, float (&v)[8]) {
   if constexpr (W) {
-    const int e = (i * G + lane) * 8;
-    if (e >= D) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-    } else if constexpr (sizeof(T) == 2) {
-      const uint4 u = *reinterpret_cast<const uint4*>(row + e);
+    const int e = (i * G + lane) * 8, at = min(e, D - 8);
+    if constexpr (sizeof(T) == 2) {
+      uint4 u = *reinterpret_cast<const uint4*>(row + at);
+      if (FILL) u.x = e < D ? u.x : 0, u.y = e < D ? u.y : 0, u.z = e < D ? u.z : 0, u.w = e < D ? u.w : 0;
       const float2 a = unpack_bf16(u.x), b = unpack_bf16(u.y), c = unpack_bf16(u.z), d = unpack_bf16(u.w);
       v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
     } else {
-      const float4 a = *reinterpret_cast<const float4*>(row + e), b = *reinterpret_cast<const float4*>(row + e + 4);
+      const float4 a = *reinterpret_cast<const float4*>(row + at), b = *reinterpret_cast<const float4*>(row + at + 4);
       v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+      if (FILL) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = e < D ? v[j] : 0.0f;
+      }
     }
   } else {
 #pragma unroll
@@ -88,10 +92,10 @@ __device__ __forceinline__ void store8(T* row, int i, int lane, int G, int D, co
 }
 
 // The same in pairs of neighbours, which are added and multiplied two at a time.
-template <bool W, typename T>
+template <bool W, bool FILL = true, typename T>
 __device__ __forceinline__ void load8(const T* row, int i, int lane, int G, int D, Pair (&v)[4]) {
   float f[8];
-  load8<W>(row, i, lane, G, D, f);
+  load8<W, FILL>(row, i, lane, G, D, f);
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] = pair(f[2 * j], f[2 * j + 1]);
 }
@@ -120,7 +124,7 @@ __device__ __forceinline__ Pair where_there(float x, int i, int j, int lane, int
 template <bool W>
 __device__ __forceinline__ void load_vector(const float* p, float otherwise, int i, int lane, int G, int D, Pair (&v)[4]) {
   if (p) {
-    load8<W>(p, i, lane, G, D, v);
+    load8<W, false>(p, i, lane, G, D, v);
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = pair(otherwise, otherwise);
@@ -167,18 +171,27 @@ __device__ __forceinline__ void group_sum(float (&x)[N], int G, float* words, in
 #pragma unroll
   for (int k = 0; k < N; ++k) x[k] = add_words(w + 32 * k, G / 32);
 }
-__device__ __forceinline__ uint32_t group_max(uint32_t x, int G, float* words, int& turn) {
+template <int N>
+__device__ __forceinline__ void group_max(uint32_t (&x)[N], int G, float* words, int& turn) {
   if (G <= 32) {
-    for (int o = G / 2; o > 0; o /= 2) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
-    return x;
+    for (int o = G / 2; o > 0; o /= 2) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) x[k] = max(x[k], __shfl_xor_sync(0xffffffffu, x[k], o));
+    }
+    return;
   }
-  x = __reduce_max_sync(0xffffffffu, x);
+#pragma unroll
+  for (int k = 0; k < N; ++k) x[k] = __reduce_max_sync(0xffffffffu, x[k]);
   uint32_t* w = reinterpret_cast<uint32_t*>(words) + (turn & 1) * 64;
   ++turn;
-  if ((threadIdx.x & 31) == 0) w[threadIdx.x / 32] = x;
+  if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) w[32 * k + threadIdx.x / 32] = x[k];
+  }
   __syncthreads();
   const int lane = threadIdx.x & 31;
-  return __reduce_max_sync(0xffffffffu, lane < G / 32 ? w[lane] : 0u);
+#pragma unroll
+  for (int k = 0; k < N; ++k) x[k] = __reduce_max_sync(0xffffffffu, lane < G / 32 ? w[32 * k + lane] : 0u);
 }
 
 // A thread's part of a row on its way into shared memory: it copies what it reads
@@ -188,9 +201,10 @@ __device__ __forceinline__ void copy_row(const T* row, T* to, int G, int D) {
 #pragma unroll
   for (int i = 0; i < C; ++i) {
     const int e = (i * G + threadIdx.x) * 8;
-    if (e >= D) break;
+    if (e < D) {
 #pragma unroll
-    for (int k = 0; k < 8; k += 16 / sizeof(T)) sjd_kv_ops::copy16(sjd_kv_ops::smem_addr(to + e + k), row + e + k, 16);
+      for (int k = 0; k < 8; k += 16 / sizeof(T)) sjd_kv_ops::copy16(sjd_kv_ops::smem_addr(to + e + k), row + e + k, 16);
+    }
   }
 }
 
@@ -210,130 +224,167 @@ __device__ __forceinline__ float larger(float m, float x) {
   return r;
 }
 
-// A row in registers becomes y = (h - m) r gain + bias, h = x + residual rounded
+// R rows in registers become y = (h - m) r gain + bias, h = x + residual rounded
 // to the rows' type, m the mean (0 without centring), r = 1 / sqrt(mean of
 // (h - m)^2 + eps); or y's codes and scale, or (MODE kCodes) those of x itself.
-// w: the residual's row. `there`: the row is to be written.
-template <typename T, bool W, int C, int MODE, typename GainsOf>
-__device__ __forceinline__ void norm_row(const NormParams& p, long long row, bool there, int lane, int G, Pair (&v)[C][4], Pair (&w)[C][4], float* words,
-                                         int& turn, const GainsOf& gains) {
+// w: the residuals' rows. `there`: the row is to be written.
+template <typename T, bool W, int C, int MODE, int R, typename GainsOf>
+__device__ __forceinline__ void norm_rows(const NormParams& p, const long long (&row)[R], const bool (&there)[R], int lane, int G, Pair (&v)[R][C][4],
+                                          Pair (&w)[R][C][4], float* words, int& turn, const GainsOf& gains) {
   const int D = p.dim;
   const float over = 1.0f / static_cast<float>(D);
   if (MODE != kCodes && p.residual.p) {
-    T* h = static_cast<T*>(p.h.p) + row * p.h.stride;
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
+    for (int q = 0; q < R; ++q) {
+      T* h = static_cast<T*>(p.h.p) + row[q] * p.h.stride;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 x = halves(add2(v[i][j], w[i][j]));
-        v[i][j] = pair(static_cast<float>(static_cast<T>(x.x)), static_cast<float>(static_cast<T>(x.y)));
+      for (int i = 0; i < C; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 x = halves(add2(v[q][i][j], w[q][i][j]));
+          v[q][i][j] = pair(static_cast<float>(static_cast<T>(x.x)), static_cast<float>(static_cast<T>(x.y)));
+        }
+        if (there[q]) store8<W>(h, i, lane, G, D, v[q][i]);
       }
-      if (there) store8<W>(h, i, lane, G, D, v[i]);
     }
   }
   if constexpr (MODE != kCodes) {
+    float sum[R];
     if (p.centre) {
+#pragma unroll
+      for (int q = 0; q < R; ++q) {
+        Pair sums[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sums[j & 1] = add2(sums[j & 1], v[q][i][j]);
+        }
+        const float2 two = halves(add2(sums[0], sums[1]));
+        sum[q] = two.x + two.y;
+      }
+      group_sum(sum, G, words, turn);
+#pragma unroll
+      for (int q = 0; q < R; ++q) {
+        const float less = -(sum[q] * over);
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[q][i][j] = add2(v[q][i][j], where_there<W>(less, i, j, lane, G, D));
+        }
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
       Pair sums[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
 #pragma unroll
       for (int i = 0; i < C; ++i) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sums[j & 1] = add2(sums[j & 1], v[i][j]);
+        for (int j = 0; j < 4; ++j) sums[j & 1] = fma2(v[q][i][j], v[q][i][j], sums[j & 1]);
       }
       const float2 two = halves(add2(sums[0], sums[1]));
-      float sum[1] = {two.x + two.y};
-      group_sum(sum, G, words, turn);
-      const float less = -(sum[0] * over);
-#pragma unroll
-      for (int i = 0; i < C; ++i) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[i][j] = add2(v[i][j], where_there<W>(less, i, j, lane, G, D));
-      }
+      sum[q] = two.x + two.y;
     }
-    Pair sums[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+    group_sum(sum, G, words, turn);
+    Pair r[R];
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sums[j & 1] = fma2(v[i][j], v[i][j], sums[j & 1]);
+    for (int q = 0; q < R; ++q) {
+      const float x = rsqrtf(sum[q] * over + p.eps);
+      r[q] = pair(x, x);
     }
-    const float2 two = halves(add2(sums[0], sums[1]));
-    float squares[1] = {two.x + two.y};
-    group_sum(squares, G, words, turn);
-    const float r = rsqrtf(squares[0] * over + p.eps);
-    const Pair rr = pair(r, r);
 #pragma unroll
     for (int i = 0; i < C; ++i) {
       Pair g[4], b[4];
       gains.take(i, g, b);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[i][j] = fma2(mul2(v[i][j], rr), g[j], b[j]);
+      for (int q = 0; q < R; ++q) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[q][i][j] = fma2(mul2(v[q][i][j], r[q]), g[j], b[j]);
+      }
     }
   }
   if constexpr (MODE == kNorm) {
-    if (!there) return;
-    T* y = static_cast<T*>(p.y.p) + row * p.y.stride;
 #pragma unroll
-    for (int i = 0; i < C; ++i) store8<W>(y, i, lane, G, D, v[i]);
-  } else {
-    float most = 0.0f;
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        // (what fills up the row may be a NaN here: 0 times an infinite factor)
-        const float2 x = halves(v[i][j]);
-        if (feature<W>(i, W ? 0 : 2 * j, lane, G) < D) most = larger(most, x.x);
-        if (feature<W>(i, W ? 0 : 2 * j + 1, lane, G) < D) most = larger(most, x.y);
-      }
-    }
-    // (by the bits, in which an infinity or a NaN is above all others)
-    const float top = __uint_as_float(group_max(__float_as_uint(most), G, words, turn)), scale = __fdiv_rn(top, 127.0f);
-    if (!there) return;
-    const bool some = top <= FLT_MAX && scale > 0.0f;
-    int8_t* codes = p.codes + row * D;
-    if (top > 0x1p-60f && top < 0x1p60f) {
-      const float inverse = __frcp_rn(scale);
+    for (int q = 0; q < R; ++q) {
+      T* y = static_cast<T*>(p.y.p) + row[q] * p.y.stride;
 #pragma unroll
       for (int i = 0; i < C; ++i) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[i][j] = quotients(v[i][j], pair(-scale, -scale), pair(inverse, inverse));
+        if (there[q]) store8<W>(y, i, lane, G, D, v[q][i]);
       }
-    } else {
-      // (a subnormal scale has few bits: quotients by it may pass 127)
-      auto held = [&](float x) { return some ? fminf(fmaxf(__fdiv_rn(x, scale), -127.0f), 127.0f) : 0.0f; };
+    }
+  } else {
+    uint32_t tops[R];
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      float most = 0.0f;
 #pragma unroll
       for (int i = 0; i < C; ++i) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float2 x = halves(v[i][j]);
-          v[i][j] = pair(held(x.x), held(x.y));
+          // (what fills up the row may be a NaN here: 0 times an infinite factor)
+          const float2 x = halves(v[q][i][j]);
+          if (feature<W>(i, W ? 0 : 2 * j, lane, G) < D) most = larger(most, x.x);
+          if (feature<W>(i, W ? 0 : 2 * j + 1, lane, G) < D) most = larger(most, x.y);
         }
       }
+      tops[q] = __float_as_uint(most);
     }
+    group_max(tops, G, words, turn);   // (by the bits, in which an infinity or a NaN is above all others)
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-      // rounded to nearest even by the sum with 1.5 * 2^23, whose last byte is the code
-      uint32_t c[8];
+    for (int q = 0; q < R; ++q) {
+      const float top = __uint_as_float(tops[q]), scale = __fdiv_rn(top, 127.0f);
+      if (!there[q]) continue;
+      const bool some = top <= FLT_MAX && scale > 0.0f;
+      int8_t* codes = p.codes + row[q] * D;
+      if (top > 0x1p-60f && top < 0x1p60f) {
+        const float inverse = __frcp_rn(scale);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 x = halves(add2(v[i][j], pair(0x1.8p23f, 0x1.8p23f)));
-        c[2 * j] = __float_as_uint(x.x), c[2 * j + 1] = __float_as_uint(x.y);
-      }
-      if constexpr (W) {
-        if (feature<true>(i, 0, lane, G) < D)
-          *reinterpret_cast<uint2*>(codes + feature<true>(i, 0, lane, G)) =
-              make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
-                         __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
+        for (int i = 0; i < C; ++i) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[q][i][j] = quotients(v[q][i][j], pair(-scale, -scale), pair(inverse, inverse));
+        }
       } else {
+        // (a subnormal scale has few bits: quotients by it may pass 127)
+        auto held = [&](float x) { return some ? fminf(fmaxf(__fdiv_rn(x, scale), -127.0f), 127.0f) : 0.0f; };
+#pragma unroll 1
+        for (int i = 0; i < C; ++i) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if (feature<false>(i, j, lane, G) < D) codes[feature<false>(i, j, lane, G)] = static_cast<int8_t>(c[j] & 0xff);
+          for (int k = 0; k < C; ++k) {
+            if (k != i) continue;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float2 x = halves(v[q][k][j]);
+              v[q][k][j] = pair(held(x.x), held(x.y));
+            }
+          }
         }
       }
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        // rounded to nearest even by the sum with 1.5 * 2^23, whose last byte is the code
+        uint32_t c[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 x = halves(add2(v[q][i][j], pair(0x1.8p23f, 0x1.8p23f)));
+          c[2 * j] = __float_as_uint(x.x), c[2 * j + 1] = __float_as_uint(x.y);
+        }
+        if constexpr (W) {
+          if (feature<true>(i, 0, lane, G) < D)
+            *reinterpret_cast<uint2*>(codes + feature<true>(i, 0, lane, G)) =
+                make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
+                           __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            if (feature<false>(i, j, lane, G) < D) codes[feature<false>(i, j, lane, G)] = static_cast<int8_t>(c[j] & 0xff);
+          }
+        }
+      }
+      if (lane == 0) p.scale[row[q]] = top <= FLT_MAX ? scale : NAN;
     }
-    if (lane == 0) p.scale[row] = top <= FLT_MAX ? scale : NAN;
   }
 }
 
+// Gains as they lie in memory, or in registers.
 template <bool W>
 struct Gains {
   const NormParams& p;
@@ -344,10 +395,26 @@ struct Gains {
   }
 };
 
-// Rows of many: a block takes every gridDim-th, `deep` - 1 of them on their way while
-// one is summed up.
-template <typename T, int C, int MODE>
+template <int C>
+struct Kept {
+  Pair g[C][4], b[C][4];
+  __device__ __forceinline__ Kept(const NormParams& p, int lane, int G) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) load_vector<true>(p.gain, 1.0f, i, lane, G, p.dim, g[i]), load_vector<true>(p.bias, -0.0f, i, lane, G, p.dim, b[i]);
+  }
+  __device__ __forceinline__ void take(int i, Pair (&gain)[4], Pair (&bias)[4]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) gain[j] = g[i][j], bias[j] = b[i][j];
+  }
+};
+
+// Calls of many rows: a block takes two rows at a time, every gridDim-th, which share
+// the sums' barriers, and `deep` - 1 pairs of them are on their way into shared memory
+// meanwhile. The gains stay in registers (from the first-level cache they would be four times the
+// bytes of a bf16 row).
+template <typename T, int MODE>
 __global__ void __launch_bounds__(512) norm_ahead_kernel(const NormParams p, int G, int deep) {
+  constexpr int C = 2, R = 2;
   __shared__ __align__(16) float words[2 * 64];
   extern __shared__ __align__(16) unsigned char shared[];
   T* stages = reinterpret_cast<T*>(shared);
@@ -355,32 +422,42 @@ __global__ void __launch_bounds__(512) norm_ahead_kernel(const NormParams p, int
   let_next_start();
   const int lane = threadIdx.x, D = p.dim;
   const bool added = MODE != kCodes && p.residual.p;
-  const int stage_size = added ? 2 * D : D;
-  auto fetch = [&](long long row, int stage) {
-    if (row < p.rows) {
-      copy_row<T, C>(static_cast<const T*>(p.x.p) + row * p.x.stride, stages + stage * stage_size, G, D);
-      if (added) copy_row<T, C>(static_cast<const T*>(p.residual.p) + row * p.residual.stride, stages + stage * stage_size + D, G, D);
+  const int row_size = added ? 2 * D : D;
+  auto fetch = [&](long long first, int stage) {
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      const long long row = first + q * static_cast<long long>(gridDim.x);
+      T* to = stages + (stage * R + q) * row_size;
+      if (row < p.rows) {
+        copy_row<T, C>(static_cast<const T*>(p.x.p) + row * p.x.stride, to, G, D);
+        if (added) copy_row<T, C>(static_cast<const T*>(p.residual.p) + row * p.residual.stride, to + D, G, D);
+      }
     }
-    sjd_kv_ops::copy_commit();   // (the group of a row that is not there is empty)
+    sjd_kv_ops::copy_commit();   // (the group of rows that are not there is empty)
   };
-  for (int i = 0; i + 1 < deep; ++i) fetch(blockIdx.x + static_cast<long long>(i) * gridDim.x, i);
-  const Gains<true> gains{p, lane, G};
+  const long long step = static_cast<long long>(R) * gridDim.x;
+  for (int i = 0; i + 1 < deep; ++i) fetch(blockIdx.x + i * step, i);
+  const Kept<C> gains(p, lane, G);
   int turn = 0, stage = 0;
-  for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
+  for (long long first = blockIdx.x; first < p.rows; first += step) {
     if (deep == 2) sjd_kv_ops::copy_wait<0>();
     else if (deep == 3) sjd_kv_ops::copy_wait<1>();
     else sjd_kv_ops::copy_wait<2>();
-    fetch(row + (deep - 1ll) * gridDim.x, stage == 0 ? deep - 1 : stage - 1);   // (where the row before was)
-    const T* from = stages + stage * stage_size;
+    fetch(first + (deep - 1) * step, stage == 0 ? deep - 1 : stage - 1);   // (where the rows before were)
+    const T* from = stages + stage * R * row_size;
     if (++stage == deep) stage = 0;
-    Pair v[C][4], w[C][4];
+    const long long row[R] = {first, first + gridDim.x};
+    const bool there[R] = {true, row[1] < p.rows};   // (else what is left from another row, to no effect)
+    Pair v[R][C][4], w[R][C][4];
 #pragma unroll
-    for (int i = 0; i < C; ++i) load8<true>(from, i, lane, G, D, v[i]);
-    if (added) {
+    for (int q = 0; q < R; ++q) {
 #pragma unroll
-      for (int i = 0; i < C; ++i) load8<true>(from + D, i, lane, G, D, w[i]);
+      for (int i = 0; i < C; ++i) {
+        load8<true>(from + q * row_size, i, lane, G, D, v[q][i]);
+        if (added) load8<true>(from + q * row_size + D, i, lane, G, D, w[q][i]);
+      }
     }
-    norm_row<T, true, C, MODE>(p, row, true, lane, G, v, w, words, turn, gains);
+    norm_rows<T, true, C, MODE, R>(p, row, there, lane, G, v, w, words, turn, gains);
   }
   sjd_kv_ops::copy_wait_all();
 }
@@ -394,16 +471,17 @@ __global__ void __launch_bounds__(512) norm_kernel(const NormParams p, int G) {
   wait_for_previous();
   let_next_start();
   const int per = blockDim.x / G, lane = threadIdx.x % G;
-  const long long at = static_cast<long long>(blockIdx.x) * per + threadIdx.x / G, row = min(at, p.rows - 1ll);
+  const long long at = static_cast<long long>(blockIdx.x) * per + threadIdx.x / G, row[1] = {min(at, p.rows - 1ll)};
+  const bool there[1] = {at < p.rows};
   int turn = 0;
-  Pair v[C][4], w[C][4];
+  Pair v[1][C][4], w[1][C][4];
 #pragma unroll
-  for (int i = 0; i < C; ++i) load8<W>(static_cast<const T*>(p.x.p) + row * p.x.stride, i, lane, G, p.dim, v[i]);
+  for (int i = 0; i < C; ++i) load8<W>(static_cast<const T*>(p.x.p) + row[0] * p.x.stride, i, lane, G, p.dim, v[0][i]);
   if (MODE != kCodes && p.residual.p) {
 #pragma unroll
-    for (int i = 0; i < C; ++i) load8<W>(static_cast<const T*>(p.residual.p) + row * p.residual.stride, i, lane, G, p.dim, w[i]);
+    for (int i = 0; i < C; ++i) load8<W>(static_cast<const T*>(p.residual.p) + row[0] * p.residual.stride, i, lane, G, p.dim, w[0][i]);
   }
-  norm_row<T, W, C, MODE>(p, row, at < p.rows, lane, G, v, w, words, turn, Gains<W>{p, lane, G});
+  norm_rows<T, W, C, MODE, 1>(p, row, there, lane, G, v, w, words, turn, Gains<W>{p, lane, G});
 }
 
 bool aligned16(const void* p, long long stride, size_t size) {
@@ -427,7 +505,7 @@ cudaError_t norm_with(const NormParams& p, cudaStream_t s) {
   return launch_early(norm_kernel<T, W, C, MODE>, static_cast<unsigned>((static_cast<long long>(p.rows) + per - 1) / per), threads, 0, s, p, G);
 }
 
-constexpr int ahead_registers(int mode) { return mode == kCodes ? 64 : 104; }   // of norm_ahead_kernel, at most
+constexpr int ahead_registers(int mode) { return mode == kCodes ? 64 : 128; }   // of norm_ahead_kernel, at most
 
 // Blocks on an SM and rows on their way in each.
 struct Flow {
@@ -449,12 +527,12 @@ cudaError_t allow_shared(Kernel kernel, size_t bytes) {
   return bytes <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
 }
 
-template <typename T, int C, int MODE>
+template <typename T, int MODE>
 cudaError_t norm_ahead(const NormParams& p, int sms, const Flow& f, cudaStream_t s) {
-  const cudaError_t e = allow_shared(norm_ahead_kernel<T, C, MODE>, f.shared);
+  const cudaError_t e = allow_shared(norm_ahead_kernel<T, MODE>, f.shared);
   if (e != cudaSuccess) return e;
-  return launch_early(norm_ahead_kernel<T, C, MODE>, static_cast<unsigned>(min(p.rows, sms * f.per_sm)), threads_of(p.dim, C), f.shared, s, p,
-                      threads_of(p.dim, C), f.deep);
+  return launch_early(norm_ahead_kernel<T, MODE>, static_cast<unsigned>(min(p.rows, sms * f.per_sm)), threads_of(p.dim, 2), f.shared, s, p,
+                      threads_of(p.dim, 2), f.deep);
 }
 
 // PIECES_FIGURES
@@ -463,9 +541,9 @@ cudaError_t norm_by(const NormParams& p, int sms, cudaStream_t s) {
   const bool few = p.rows <= 2 * sms;
   const int d = p.dim;
   if (d <= 256 || (few && d <= 4096)) return norm_with<T, W, 1, MODE>(p, s);
-  if (W && !few && d > 512) {
-    const Flow f = flow_of(threads_of(d, 4), ahead_registers(MODE), sizeof(T) * d * (MODE != kCodes && p.residual.p ? 2 : 1));
-    if (f.shared <= 200 * 1024) return norm_ahead<T, 4, MODE>(p, sms, f, s);
+  if (W && !few && d > 512 && d <= 8192) {
+    const Flow f = flow_of(threads_of(d, 2), ahead_registers(MODE), 2 * sizeof(T) * d * (MODE != kCodes && p.residual.p ? 2 : 1));
+    if (f.shared <= 200 * 1024) return norm_ahead<T, MODE>(p, sms, f, s);
   }
   if (d <= 512 || ((few || !W) && d <= 8192)) return norm_with<T, W, 2, MODE>(p, s);
   return norm_with<T, W, 4, MODE>(p, s);
