@@ -35,27 +35,40 @@ using sjd_kv_ops::wait_for_previous;
 
 namespace {
 
-// Feature j of piece i of a thread: neighbours where a row can be accessed 16
-// bytes at a time (`W`), else every G-th, so that a warp's accesses of single
-// elements lie side by side.
+// A thread's features of a row: pieces of 8 neighbours, `step` apart, where a row
+// can be accessed 16 bytes at a time (`W`). Else a warp's pieces follow one
+// another and a piece's features lie 32 apart, so that a warp's accesses of single elements are side by
+// side, at distances that are known beforehand.
+struct Place {
+  int first, step;
+};
 template <bool W>
-__device__ __forceinline__ int feature(int i, int j, int lane, int G) {
-  return W ? (i * G + lane) * 8 + j : (i * 8 + j) * G + lane;
+__device__ __forceinline__ Place place_of(int lane, int G, int pieces) {
+  return W ? Place{8 * lane, 8 * G} : Place{lane / 32 * 256 * pieces + lane % 32, 256};
+}
+// Feature j of piece i; whether it is one of the row's.
+template <bool W>
+__device__ __forceinline__ int feature(int i, int j, Place at) {
+  return W ? at.first + i * at.step + j : at.first + i * 256 + j * 32;
+}
+template <bool W>
+__device__ __forceinline__ bool is_there(int i, int j, Place at, int D) {
+  return W ? feature<true>(i, 0, at) < D : i * 256 + j * 32 < D - at.first;   // (pieces are there as a whole, or not)
 }
 
 // (Wide loads behind the row's end take its last piece instead, and `FILL` puts zeros in its
 // place: a select costs less than a branch around the load.)
 template <bool W, bool FILL = true, typename T>
-__device__ __forceinline__ void load8(const T* row, int i, int lane, int G, int D, float (&v)[8]) {
+__device__ __forceinline__ void load8(const T* row, int i, Place at, int D, float (&v)[8]) {
   if constexpr (W) {
-    const int e = (i * G + lane) * 8, at = min(e, D - 8);
+    const int e = feature<true>(i, 0, at), here = min(e, D - 8);
     if constexpr (sizeof(T) == 2) {
-      uint4 u = *reinterpret_cast<const uint4*>(row + at);
+      uint4 u = *reinterpret_cast<const uint4*>(row + here);
       if (FILL) u.x = e < D ? u.x : 0, u.y = e < D ? u.y : 0, u.z = e < D ? u.z : 0, u.w = e < D ? u.w : 0;
       const float2 a = unpack_bf16(u.x), b = unpack_bf16(u.y), c = unpack_bf16(u.z), d = unpack_bf16(u.w);
       v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
     } else {
-      const float4 a = *reinterpret_cast<const float4*>(row + at), b = *reinterpret_cast<const float4*>(row + at + 4);
+      const float4 a = *reinterpret_cast<const float4*>(row + here), b = *reinterpret_cast<const float4*>(row + here + 4);
       v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
       if (FILL) {
 #pragma unroll
@@ -65,16 +78,15 @@ __device__ __forceinline__ void load8(const T* row, int i, int lane, int G, int 
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int e = feature<false>(i, j, lane, G);
-      v[j] = e < D ? static_cast<float>(row[e]) : 0.0f;
+      v[j] = is_there<false>(i, j, at, D) ? static_cast<float>(row[feature<false>(i, j, at)]) : 0.0f;
     }
   }
 }
 
 template <bool W, typename T>
-__device__ __forceinline__ void store8(T* row, int i, int lane, int G, int D, const float (&v)[8]) {
+__device__ __forceinline__ void store8(T* row, int i, Place at, int D, const float (&v)[8]) {
   if constexpr (W) {
-    const int e = (i * G + lane) * 8;
+    const int e = feature<true>(i, 0, at);
     if (e >= D) return;
     if constexpr (sizeof(T) == 2) {
       *reinterpret_cast<uint4*>(row + e) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
@@ -85,46 +97,45 @@ __device__ __forceinline__ void store8(T* row, int i, int lane, int G, int D, co
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int e = feature<false>(i, j, lane, G);
-      if (e < D) row[e] = static_cast<T>(v[j]);
+      if (is_there<false>(i, j, at, D)) row[feature<false>(i, j, at)] = static_cast<T>(v[j]);
     }
   }
 }
 
 // The same in pairs of neighbours, which are added and multiplied two at a time.
 template <bool W, bool FILL = true, typename T>
-__device__ __forceinline__ void load8(const T* row, int i, int lane, int G, int D, Pair (&v)[4]) {
+__device__ __forceinline__ void load8(const T* row, int i, Place at, int D, Pair (&v)[4]) {
   float f[8];
-  load8<W, FILL>(row, i, lane, G, D, f);
+  load8<W, FILL>(row, i, at, D, f);
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] = pair(f[2 * j], f[2 * j + 1]);
 }
 template <bool W, typename T>
-__device__ __forceinline__ void store8(T* row, int i, int lane, int G, int D, const Pair (&v)[4]) {
+__device__ __forceinline__ void store8(T* row, int i, Place at, int D, const Pair (&v)[4]) {
   float f[8];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float2 x = halves(v[j]);
     f[2 * j] = x.x, f[2 * j + 1] = x.y;
   }
-  store8<W>(row, i, lane, G, D, f);
+  store8<W>(row, i, at, D, f);
 }
 // x for the features that are there, 0 for those that fill up the last piece.
 template <bool W>
-__device__ __forceinline__ Pair where_there(float x, int i, int j, int lane, int G, int D) {
+__device__ __forceinline__ Pair where_there(float x, int i, int j, Place at, int D) {
   if constexpr (W) {
-    const float y = feature<true>(i, 0, lane, G) < D ? x : 0.0f;   // (whole pieces)
+    const float y = is_there<true>(i, 0, at, D) ? x : 0.0f;
     return pair(y, y);
   } else {
-    return pair(feature<false>(i, 2 * j, lane, G) < D ? x : 0.0f, feature<false>(i, 2 * j + 1, lane, G) < D ? x : 0.0f);
+    return pair(is_there<false>(i, 2 * j, at, D) ? x : 0.0f, is_there<false>(i, 2 * j + 1, at, D) ? x : 0.0f);
   }
 }
 
 // Vectors of one float a feature (gains), which are 16-byte aligned where rows are.
 template <bool W>
-__device__ __forceinline__ void load_vector(const float* p, float otherwise, int i, int lane, int G, int D, Pair (&v)[4]) {
+__device__ __forceinline__ void load_vector(const float* p, float otherwise, int i, Place at, int D, Pair (&v)[4]) {
   if (p) {
-    load8<W, false>(p, i, lane, G, D, v);
+    load8<W, false>(p, i, at, D, v);
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = pair(otherwise, otherwise);
@@ -229,7 +240,7 @@ __device__ __forceinline__ float larger(float m, float x) {
 // (h - m)^2 + eps); or y's codes and scale, or (MODE kCodes) those of x itself.
 // w: the residuals' rows. `there`: the row is to be written.
 template <typename T, bool W, int C, int MODE, int R, typename GainsOf>
-__device__ __forceinline__ void norm_rows(const NormParams& p, const long long (&row)[R], const bool (&there)[R], int lane, int G, Pair (&v)[R][C][4],
+__device__ __forceinline__ void norm_rows(const NormParams& p, const long long (&row)[R], const bool (&there)[R], int lane, int G, Place at, Pair (&v)[R][C][4],
                                           Pair (&w)[R][C][4], float* words, int& turn, const GainsOf& gains) {
   const int D = p.dim;
   const float over = 1.0f / static_cast<float>(D);
@@ -244,7 +255,7 @@ __device__ __forceinline__ void norm_rows(const NormParams& p, const long long (
           const float2 x = halves(add2(v[q][i][j], w[q][i][j]));
           v[q][i][j] = pair(static_cast<float>(static_cast<T>(x.x)), static_cast<float>(static_cast<T>(x.y)));
         }
-        if (there[q]) store8<W>(h, i, lane, G, D, v[q][i]);
+        if (there[q]) store8<W>(h, i, at, D, v[q][i]);
       }
     }
   }
@@ -269,7 +280,7 @@ __device__ __forceinline__ void norm_rows(const NormParams& p, const long long (
 #pragma unroll
         for (int i = 0; i < C; ++i) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[q][i][j] = add2(v[q][i][j], where_there<W>(less, i, j, lane, G, D));
+          for (int j = 0; j < 4; ++j) v[q][i][j] = add2(v[q][i][j], where_there<W>(less, i, j, at, D));
         }
       }
     }
@@ -308,7 +319,7 @@ __device__ __forceinline__ void norm_rows(const NormParams& p, const long long (
       T* y = static_cast<T*>(p.y.p) + row[q] * p.y.stride;
 #pragma unroll
       for (int i = 0; i < C; ++i) {
-        if (there[q]) store8<W>(y, i, lane, G, D, v[q][i]);
+        if (there[q]) store8<W>(y, i, at, D, v[q][i]);
       }
     }
   } else {
@@ -322,8 +333,8 @@ __device__ __forceinline__ void norm_rows(const NormParams& p, const long long (
         for (int j = 0; j < 4; ++j) {
           // (what fills up the row may be a NaN here: 0 times an infinite factor)
           const float2 x = halves(v[q][i][j]);
-          if (feature<W>(i, W ? 0 : 2 * j, lane, G) < D) most = larger(most, x.x);
-          if (feature<W>(i, W ? 0 : 2 * j + 1, lane, G) < D) most = larger(most, x.y);
+          if (is_there<W>(i, 2 * j, at, D)) most = larger(most, x.x);
+          if (is_there<W>(i, 2 * j + 1, at, D)) most = larger(most, x.y);
         }
       }
       tops[q] = __float_as_uint(most);
@@ -368,14 +379,14 @@ __device__ __forceinline__ void norm_rows(const NormParams& p, const long long (
           c[2 * j] = __float_as_uint(x.x), c[2 * j + 1] = __float_as_uint(x.y);
         }
         if constexpr (W) {
-          if (feature<true>(i, 0, lane, G) < D)
-            *reinterpret_cast<uint2*>(codes + feature<true>(i, 0, lane, G)) =
+          if (is_there<true>(i, 0, at, D))
+            *reinterpret_cast<uint2*>(codes + feature<true>(i, 0, at)) =
                 make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
                            __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            if (feature<false>(i, j, lane, G) < D) codes[feature<false>(i, j, lane, G)] = static_cast<int8_t>(c[j] & 0xff);
+            if (is_there<false>(i, j, at, D)) codes[feature<false>(i, j, at)] = static_cast<int8_t>(c[j] & 0xff);
           }
         }
       }
@@ -388,19 +399,19 @@ __device__ __forceinline__ void norm_rows(const NormParams& p, const long long (
 template <bool W>
 struct Gains {
   const NormParams& p;
-  int lane, G;
+  Place at;
   __device__ __forceinline__ void take(int i, Pair (&gain)[4], Pair (&bias)[4]) const {
-    load_vector<W>(p.gain, 1.0f, i, lane, G, p.dim, gain);
-    load_vector<W>(p.bias, -0.0f, i, lane, G, p.dim, bias);   // (adding -0 changes nothing)
+    load_vector<W>(p.gain, 1.0f, i, at, p.dim, gain);
+    load_vector<W>(p.bias, -0.0f, i, at, p.dim, bias);   // (adding -0 changes nothing)
   }
 };
 
 template <int C>
 struct Kept {
   Pair g[C][4], b[C][4];
-  __device__ __forceinline__ Kept(const NormParams& p, int lane, int G) {
+  __device__ __forceinline__ Kept(const NormParams& p, Place at) {
 #pragma unroll
-    for (int i = 0; i < C; ++i) load_vector<true>(p.gain, 1.0f, i, lane, G, p.dim, g[i]), load_vector<true>(p.bias, -0.0f, i, lane, G, p.dim, b[i]);
+    for (int i = 0; i < C; ++i) load_vector<true>(p.gain, 1.0f, i, at, p.dim, g[i]), load_vector<true>(p.bias, -0.0f, i, at, p.dim, b[i]);
   }
   __device__ __forceinline__ void take(int i, Pair (&gain)[4], Pair (&bias)[4]) const {
 #pragma unroll
@@ -421,6 +432,7 @@ __global__ void __launch_bounds__(512) norm_ahead_kernel(const NormParams p, int
   wait_for_previous();
   let_next_start();
   const int lane = threadIdx.x, D = p.dim;
+  const Place at = place_of<true>(lane, G, C);
   const bool added = MODE != kCodes && p.residual.p;
   const int row_size = added ? 2 * D : D;
   auto fetch = [&](long long first, int stage) {
@@ -437,7 +449,7 @@ __global__ void __launch_bounds__(512) norm_ahead_kernel(const NormParams p, int
   };
   const long long step = static_cast<long long>(R) * gridDim.x;
   for (int i = 0; i + 1 < deep; ++i) fetch(blockIdx.x + i * step, i);
-  const Kept<C> gains(p, lane, G);
+  const Kept<C> gains(p, at);
   int turn = 0, stage = 0;
   for (long long first = blockIdx.x; first < p.rows; first += step) {
     if (deep == 2) sjd_kv_ops::copy_wait<0>();
@@ -453,11 +465,11 @@ __global__ void __launch_bounds__(512) norm_ahead_kernel(const NormParams p, int
     for (int q = 0; q < R; ++q) {
 #pragma unroll
       for (int i = 0; i < C; ++i) {
-        load8<true>(from + q * row_size, i, lane, G, D, v[q][i]);
-        if (added) load8<true>(from + q * row_size + D, i, lane, G, D, w[q][i]);
+        load8<true>(from + q * row_size, i, at, D, v[q][i]);
+        if (added) load8<true>(from + q * row_size + D, i, at, D, w[q][i]);
       }
     }
-    norm_rows<T, true, C, MODE, R>(p, row, there, lane, G, v, w, words, turn, gains);
+    norm_rows<T, true, C, MODE, R>(p, row, there, lane, G, at, v, w, words, turn, gains);
   }
   sjd_kv_ops::copy_wait_all();
 }
@@ -471,17 +483,18 @@ __global__ void __launch_bounds__(512) norm_kernel(const NormParams p, int G) {
   wait_for_previous();
   let_next_start();
   const int per = blockDim.x / G, lane = threadIdx.x % G;
-  const long long at = static_cast<long long>(blockIdx.x) * per + threadIdx.x / G, row[1] = {min(at, p.rows - 1ll)};
-  const bool there[1] = {at < p.rows};
+  const Place at = place_of<W>(lane, G, C);
+  const long long mine = static_cast<long long>(blockIdx.x) * per + threadIdx.x / G, row[1] = {min(mine, p.rows - 1ll)};
+  const bool there[1] = {mine < p.rows};
   int turn = 0;
   Pair v[1][C][4], w[1][C][4];
 #pragma unroll
-  for (int i = 0; i < C; ++i) load8<W>(static_cast<const T*>(p.x.p) + row[0] * p.x.stride, i, lane, G, p.dim, v[0][i]);
+  for (int i = 0; i < C; ++i) load8<W>(static_cast<const T*>(p.x.p) + row[0] * p.x.stride, i, at, p.dim, v[0][i]);
   if (MODE != kCodes && p.residual.p) {
 #pragma unroll
-    for (int i = 0; i < C; ++i) load8<W>(static_cast<const T*>(p.residual.p) + row[0] * p.residual.stride, i, lane, G, p.dim, w[0][i]);
+    for (int i = 0; i < C; ++i) load8<W>(static_cast<const T*>(p.residual.p) + row[0] * p.residual.stride, i, at, p.dim, w[0][i]);
   }
-  norm_rows<T, W, C, MODE, 1>(p, row, there, lane, G, v, w, words, turn, Gains<W>{p, lane, G});
+  norm_rows<T, W, C, MODE, 1>(p, row, there, lane, G, at, v, w, words, turn, Gains<W>{p, at});
 }
 
 bool aligned16(const void* p, long long stride, size_t size) {
@@ -493,15 +506,15 @@ bool wide(const float* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 int threads_of(int dim, int pieces) { return ((dim + 8 * pieces - 1) / (8 * pieces) + 31) / 32 * 32; }
 
-int lanes_of(int dim, int pieces) {   // of a warp
-  int l = 8;
+int lanes_of(int dim, int pieces, bool w) {   // of a warp
+  int l = w ? 8 : 32;
   while (8 * pieces * l < dim) l *= 2;
   return l;
 }
 
 template <typename T, bool W, int C, int MODE>
 cudaError_t norm_with(const NormParams& p, cudaStream_t s) {
-  const int G = p.dim <= 8 * C * 32 ? lanes_of(p.dim, C) : threads_of(p.dim, C), threads = G <= 32 ? kShortBlock : G, per = threads / G;
+  const int G = p.dim <= 8 * C * 32 ? lanes_of(p.dim, C, W) : threads_of(p.dim, C), threads = G <= 32 ? kShortBlock : G, per = threads / G;
   return launch_early(norm_kernel<T, W, C, MODE>, static_cast<unsigned>((static_cast<long long>(p.rows) + per - 1) / per), threads, 0, s, p, G);
 }
 
@@ -563,7 +576,7 @@ cudaError_t norm_of(const NormParams& p, int mode, int sms, cudaStream_t s) {
 // The sums over a row are those of x and g, then of (x - m)^2 and g (x - m).
 // x: the row, which becomes u; dx: dh, where there is one, which becomes dx.
 template <bool W, int C, typename Gain>
-__device__ __forceinline__ void gradient_row(const NormGradientParams& p, int lane, int G, Pair (&x)[C][4], Pair (&dy)[C][4], Pair (&dx)[C][4],
+__device__ __forceinline__ void gradient_row(const NormGradientParams& p, int G, Place at, Pair (&x)[C][4], Pair (&dy)[C][4], Pair (&dx)[C][4],
                                              float* words, int& turn, Gain gain) {
   const int D = p.dim;
   const float over = 1.0f / static_cast<float>(D);
@@ -586,7 +599,7 @@ __device__ __forceinline__ void gradient_row(const NormGradientParams& p, int la
 #pragma unroll
     for (int i = 0; i < C; ++i) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[i][j] = add2(x[i][j], where_there<W>(less, i, j, lane, G, D));
+      for (int j = 0; j < 4; ++j) x[i][j] = add2(x[i][j], where_there<W>(less, i, j, at, D));
     }
   }
   Pair sx = zero, sg = zero;
@@ -622,22 +635,23 @@ __global__ void __launch_bounds__(kShortBlock) norm_gradient_short_kernel(const 
   wait_for_previous();
   let_next_start();
   const int lane = threadIdx.x % G, D = p.dim, per = kShortBlock / G;
+  const Place at = place_of<W>(lane, G, C);
   int turn = 0;
   Pair dgain[C][4] = {}, dbias[C][4] = {};
   for (long long first = static_cast<long long>(blockIdx.x) * per; first < p.rows; first += static_cast<long long>(gridDim.x) * per) {
-    const long long at = first + threadIdx.x / G, row = min(at, p.rows - 1ll);
+    const long long mine = first + threadIdx.x / G, row = min(mine, p.rows - 1ll);
     Pair x[C][4], dy[C][4], dx[C][4];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      load8<W>(static_cast<const T*>(p.x.p) + row * p.x.stride, i, lane, G, D, x[i]);
-      load8<W>(static_cast<const T*>(p.dy.p) + row * p.dy.stride, i, lane, G, D, dy[i]);
-      if (p.dh.p) load8<W>(static_cast<const T*>(p.dh.p) + row * p.dh.stride, i, lane, G, D, dx[i]);
+      load8<W>(static_cast<const T*>(p.x.p) + row * p.x.stride, i, at, D, x[i]);
+      load8<W>(static_cast<const T*>(p.dy.p) + row * p.dy.stride, i, at, D, dy[i]);
+      if (p.dh.p) load8<W>(static_cast<const T*>(p.dh.p) + row * p.dh.stride, i, at, D, dx[i]);
     }
-    gradient_row<W, C>(p, lane, G, x, dy, dx, nullptr, turn, [&](int i, Pair (&g)[4]) { load_vector<W>(p.gain, 1.0f, i, lane, G, D, g); });
-    if (at >= p.rows) continue;
+    gradient_row<W, C>(p, G, at, x, dy, dx, nullptr, turn, [&](int i, Pair (&g)[4]) { load_vector<W>(p.gain, 1.0f, i, at, D, g); });
+    if (mine >= p.rows) continue;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      store8<W>(static_cast<T*>(p.dx.p) + row * p.dx.stride, i, lane, G, D, dx[i]);
+      store8<W>(static_cast<T*>(p.dx.p) + row * p.dx.stride, i, at, D, dx[i]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) dgain[i][j] = fma2(dy[i][j], x[i][j], dgain[i][j]), dbias[i][j] = add2(dbias[i][j], dy[i][j]);
     }
@@ -659,7 +673,7 @@ __global__ void __launch_bounds__(kShortBlock) norm_gradient_short_kernel(const 
       for (int i = 0; i < C; ++i) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int e = feature<W>(i, j, lane, G);
+          const int e = feature<W>(i, j, at);
           const float2 dg = halves(dgain[i][j / 2]), db = halves(dbias[i][j / 2]);
           if (e < D) sums[0][e] = (w ? sums[0][e] : 0.0f) + (j & 1 ? dg.y : dg.x), sums[1][e] = (w ? sums[1][e] : 0.0f) + (j & 1 ? db.y : db.x);
         }
@@ -687,6 +701,7 @@ __global__ void __launch_bounds__(WAY == kShared ? 1024 : 512) norm_gradient_ker
   wait_for_previous();
   let_next_start();
   const int lane = threadIdx.x, D = p.dim, kinds = p.dh.p ? 3 : 2;
+  const Place at = place_of<W>(lane, G, C);
   auto x_of = [&](long long row) { return static_cast<const T*>(p.x.p) + row * p.x.stride; };
   auto dy_of = [&](long long row) { return static_cast<const T*>(p.dy.p) + row * p.dy.stride; };
   auto dh_of = [&](long long row) { return static_cast<const T*>(p.dh.p) + row * p.dh.stride; };
@@ -708,7 +723,7 @@ __global__ void __launch_bounds__(WAY == kShared ? 1024 : 512) norm_gradient_ker
       for (int i = 0; i + 1 < deep; ++i) fetch(blockIdx.x + static_cast<long long>(i) * gridDim.x, i);
     }
 #pragma unroll
-    for (int i = 0; i < C; ++i) load_vector<W>(p.gain, 1.0f, i, lane, G, D, gains[i]);
+    for (int i = 0; i < C; ++i) load_vector<W>(p.gain, 1.0f, i, at, D, gains[i]);
   }
   int turn = 0, stage = 0;
   for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
@@ -724,13 +739,13 @@ __global__ void __launch_bounds__(WAY == kShared ? 1024 : 512) norm_gradient_ker
     Pair x[C][4], dy[C][4], dx[C][4];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      load8<W>(xs, i, lane, G, D, x[i]);
-      load8<W>(dys, i, lane, G, D, dy[i]);
-      if (p.dh.p) load8<W>(dhs, i, lane, G, D, dx[i]);
+      load8<W>(xs, i, at, D, x[i]);
+      load8<W>(dys, i, at, D, dy[i]);
+      if (p.dh.p) load8<W>(dhs, i, at, D, dx[i]);
     }
-    gradient_row<W, C>(p, lane, G, x, dy, dx, words, turn, [&](int i, Pair (&g)[4]) {
+    gradient_row<W, C>(p, G, at, x, dy, dx, words, turn, [&](int i, Pair (&g)[4]) {
       if constexpr (WAY == kShared) {
-        load_vector<W>(p.gain, 1.0f, i, lane, G, D, g);
+        load_vector<W>(p.gain, 1.0f, i, at, D, g);
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) g[j] = gains[i][j];
@@ -739,11 +754,11 @@ __global__ void __launch_bounds__(WAY == kShared ? 1024 : 512) norm_gradient_ker
     T* dxs = static_cast<T*>(p.dx.p) + row * p.dx.stride;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      store8<W>(dxs, i, lane, G, D, dx[i]);
+      store8<W>(dxs, i, at, D, dx[i]);
       if constexpr (WAY == kShared) {
         // (a thread's own columns, four of them at a time where they are neighbours)
         if constexpr (W) {
-          const int e = feature<true>(i, 0, lane, G);
+          const int e = feature<true>(i, 0, at);
           if (e < D) {
 #pragma unroll
             for (int j = 0; j < 4; j += 2) {
@@ -757,7 +772,7 @@ __global__ void __launch_bounds__(WAY == kShared ? 1024 : 512) norm_gradient_ker
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int e = feature<false>(i, j, lane, G);
+            const int e = feature<false>(i, j, at);
             const float2 u = halves(x[i][j / 2]), d = halves(dy[i][j / 2]);
             if (e < D) sums[e] = fmaf(j & 1 ? d.y : d.x, j & 1 ? u.y : u.x, sums[e]), sums[D + e] += j & 1 ? d.y : d.x;
           }
@@ -774,7 +789,7 @@ __global__ void __launch_bounds__(WAY == kShared ? 1024 : 512) norm_gradient_ker
   for (int i = 0; i < C; ++i) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int e = feature<W>(i, j, lane, G);
+      const int e = feature<W>(i, j, at);
       if (e >= D) continue;
       const float2 dg = halves(dgain[WAY == kShared ? 0 : i][j / 2]), db = halves(dbias[WAY == kShared ? 0 : i][j / 2]);
       part[e] = WAY == kShared ? sums[e] : j & 1 ? dg.y : dg.x;
@@ -823,8 +838,8 @@ cudaError_t norm_gradient_by(const NormGradientParams& p, cudaStream_t s) {
   const int columns = p.dim * (p.dbias ? 2 : 1);
   const Flow f = gradient_flow(p.dim, sizeof(T));
   cudaError_t e;
-  if (p.dim <= kShort / 2) e = launch_early(norm_gradient_short_kernel<T, W, 1>, p.blocks, kShortBlock, 0, s, p, lanes_of(p.dim, 1));
-  else if (p.dim <= kShort) e = launch_early(norm_gradient_short_kernel<T, W, 2>, p.blocks, kShortBlock, 0, s, p, lanes_of(p.dim, 2));
+  if (p.dim <= kShort / 2) e = launch_early(norm_gradient_short_kernel<T, W, 1>, p.blocks, kShortBlock, 0, s, p, lanes_of(p.dim, 1, W));
+  else if (p.dim <= kShort) e = launch_early(norm_gradient_short_kernel<T, W, 2>, p.blocks, kShortBlock, 0, s, p, lanes_of(p.dim, 2, W));
   else if (p.dim > 8192) e = norm_gradient_with<T, W, kShared>(p, f, s);
   else if (W && f.shared <= 200 * 1024) e = norm_gradient_with<T, W, W ? kAhead : kDirect>(p, f, s);
   else e = norm_gradient_with<T, W, kDirect>(p, f, s);
@@ -848,11 +863,12 @@ __global__ void __launch_bounds__(kEmbedBlock) embed_kernel(const EmbedParams p,
   const bool inside = token >= 0 && token < p.vocab;
   const E* x = static_cast<const E*>(p.table.p) + (inside ? token : 0) * p.table.stride;
   T* y = static_cast<T*>(p.y.p) + row * p.y.stride;
+  const Place at = place_of<W>(lane, G, (D + 8 * G - 1) / (8 * G));
   for (int i0 = 0; i0 * 8 * G < D; i0 += kDeep) {
     float v[kDeep][8] = {};
     if (inside) {
 #pragma unroll
-      for (int i = 0; i < kDeep; ++i) load8<W>(x, i0 + i, lane, G, D, v[i]);
+      for (int i = 0; i < kDeep; ++i) load8<W>(x, i0 + i, at, D, v[i]);
 #pragma unroll
       for (int i = 0; i < kDeep; ++i) {
 #pragma unroll
@@ -860,14 +876,14 @@ __global__ void __launch_bounds__(kEmbedBlock) embed_kernel(const EmbedParams p,
       }
     }
 #pragma unroll
-    for (int i = 0; i < kDeep; ++i) store8<W>(y, i0 + i, lane, G, D, v[i]);
+    for (int i = 0; i < kDeep; ++i) store8<W>(y, i0 + i, at, D, v[i]);
   }
 }
 
 template <typename E, typename T>
 cudaError_t embed_of(const EmbedParams& p, cudaStream_t s) {
   const bool w = p.dim % 8 == 0 && wide(p.table, p.vocab, sizeof(E)) && wide(p.y, p.rows, sizeof(T));
-  const int G = p.dim <= 1024 ? lanes_of(p.dim, 4) : kEmbedBlock, per = kEmbedBlock / G;
+  const int G = p.dim <= 1024 ? lanes_of(p.dim, 4, w) : kEmbedBlock, per = kEmbedBlock / G;
   const unsigned blocks = static_cast<unsigned>((static_cast<long long>(p.rows) + per - 1) / per);
   return w ? launch_early(embed_kernel<E, T, true>, blocks, kEmbedBlock, 0, s, p, G) : launch_early(embed_kernel<E, T, false>, blocks, kEmbedBlock, 0, s, p, G);
 }
@@ -1116,7 +1132,7 @@ cudaError_t launch_norm(const NormParams& p, int mode, int dtype, int sms, cudaS
 
 int norm_gradient_blocks(int rows, int dim, int dtype, int sms) {
   if (dim > kShort) return min(rows, sms * gradient_flow(dim, dtype == SJD_BF16 ? 2 : 4).per_sm);
-  const int per = kShortBlock / lanes_of(dim, dim <= kShort / 2 ? 1 : 2);
+  const int per = kShortBlock / lanes_of(dim, dim <= kShort / 2 ? 1 : 2, true);
   return static_cast<int>(min((static_cast<long long>(rows) + per - 1) / per, 8ll * sms));
 }
 
