@@ -20,6 +20,8 @@
 // each thread 32 exchanges of bytes and 32 sums beside a product of 1024 cycles
 // (256 tokens), which bounds those of many.
 
+#include <atomic>
+
 #include <cuda_fp16.h>
 
 #include "sjd_dense.h"
@@ -61,7 +63,8 @@ constexpr int kMostTokens = 256, kTwoSums = 192; // of a tile; of one that has t
 constexpr int kStageColumns = kTileIn / 2;      // a tile's features in tensor memory, two to a column
 constexpr int kTmemColumns = 512;
 constexpr int kMostCodes = 24, kStages = 8;     // most tiles on their way: codes, tokens and codes in fp16
-constexpr uint32_t kAtMisc = 224 * 1024;        // (the ring of codes, then that of the tokens)
+constexpr uint32_t kRings = 222 * 1024;         // bytes of shared memory for them; in a call of few tokens less, which lets a block of
+constexpr uint32_t kRingsBeside = 216 * 1024;   // the spreading kernel stay on the SM while this kernel's starts
 constexpr int kSlots = 3;                       // what a block leaves of up to two tiles that others have a part in, and the sum of a tile's parts
 constexpr int kMaxPairs = 80;
 constexpr int kConvert = 4, kResults = 12;       // the first warps that convert codes, that give results: eight each
@@ -138,6 +141,7 @@ struct Misc {
   int others[2], last;   // whether the others' parts are there (by the shared piece's number modulo 2), all are
   Ready ready[2];
 };
+constexpr uint32_t kAtRings = (sizeof(Misc) + 1023) / 1024 * 1024;
 
 __device__ __forceinline__ void wait(Misc* m, unsigned long long* bar, uint32_t parity) {
   const uint32_t at = smem_addr(bar);
@@ -531,8 +535,8 @@ __device__ __forceinline__ void results(const ProductParams& p, Misc* m, const P
 template <typename T>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product_kernel(const ProductParams p, const Plan g) {
   extern __shared__ __align__(1024) unsigned char raw[];
-  Misc* m = reinterpret_cast<Misc*>(raw + kAtMisc);
-  const uint32_t smem = smem_addr(raw), x_at = smem + g.codes_ring * kTileBytes;
+  Misc* m = reinterpret_cast<Misc*>(raw);
+  const uint32_t smem = smem_addr(raw) + kAtRings, x_at = smem + g.codes_ring * kTileBytes;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), rank = static_cast<int>(cluster_rank()), pair = blockIdx.x / 2;
   if (warp == 3) tmem_alloc_pair(smem_addr(&m->tmem), kTmemColumns);
   if (threadIdx.x == 0) {
@@ -600,20 +604,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 // The tokens' codes in fp16, in the order in which the product's tiles lie in
 // shared memory (rows of 128 bytes, the 128-byte swizzle), the sum of each token's
 // squares, and the counters of shared tiles. A block takes a token.
-__global__ void __launch_bounds__(256) spread_kernel(const ProductParams p, const Plan g, unsigned char* x, uint32_t* squares) {
-  __shared__ uint32_t words[8];
+constexpr int kSpreadBlock = 128;   // (with at most 32 registers a thread there is room for it beside a block of the product)
+__global__ void __launch_bounds__(kSpreadBlock, 16) spread_kernel(const ProductParams p, const Plan g, unsigned char* x, uint32_t* squares) {
+  __shared__ uint32_t words[kSpreadBlock / 32];
   wait_for_previous();
   let_next_start();
   const int t = blockIdx.x, lane = threadIdx.x & 31, half = g.tokens / 2;
   if (blockIdx.x == 0) {
-    for (int i = threadIdx.x; i < 4 * kMaxPairs; i += 256) g.counters[i] = 0;
+    for (int i = threadIdx.x; i < 4 * kMaxPairs; i += kSpreadBlock) g.counters[i] = 0;
   }
   const int8_t* from = p.codes + t * p.codes_stride;
   const int tile = t / g.tokens, r = t - tile * g.tokens, of_half = r / half, row = r - of_half * half;
   unsigned char* to = x + static_cast<long long>(tile * 2 + of_half) * g.per_tile * half * 128 + row * 128;
   const bool wide = reinterpret_cast<uintptr_t>(from) % 16 == 0;
   uint32_t sum = 0;
-  for (int k = threadIdx.x * 16; k < g.per_tile * kTileIn; k += 256 * 16) {
+#pragma unroll 2
+  for (int k = threadIdx.x * 16; k < g.per_tile * kTileIn; k += kSpreadBlock * 16) {
     uint32_t c[4] = {0, 0, 0, 0};
     if (wide && k + 16 <= p.w.in) {
       const uint4 u = *reinterpret_cast<const uint4*>(from + k);
@@ -639,9 +645,110 @@ __global__ void __launch_bounds__(256) spread_kernel(const ProductParams p, cons
   if (lane == 0) words[threadIdx.x / 32] = sum;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int i = 1; i < 8; ++i) sum += words[i];
+    for (int i = 1; i < kSpreadBlock / 32; ++i) sum += words[i];
     squares[t] = sum;
   }
+}
+
+// --- a few tokens ---------------------------------------------------------------
+// Up to kFewTokens tokens need nothing but the weight's bytes: integer dot
+// products of four codes take less time than reading them, and the one launch
+// has neither fp16 nor shared tiles to wait for. A block takes 32 channels, a warp
+// every eighth tile of 64 features of them (2 KB side by side), kAhead of them in its
+// registers at a time; a lane reads piece l % 4 of channels l / 4, 8 + l / 4, ... and adds to
+// their sums with all tokens, whose codes lie in shared memory. FEW_FIGURES
+constexpr int kFewTokens = 8, kFewWarps = 8, kFewChannels = 32;
+
+template <typename T, int N>   // N: at least the call's tokens
+__global__ void __launch_bounds__(32 * kFewWarps, 2) few_kernel(const ProductParams p) {
+  constexpr int kAhead = 4, kChunk = kFewWarps * kAhead * kTileIn;
+  __shared__ __align__(16) unsigned char x[N][kChunk];
+  __shared__ int sums[kFewWarps][N][kFewChannels];
+  wait_for_previous();
+  let_next_start();
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, n0 = blockIdx.x * kFewChannels;
+  const unsigned char* from = p.w.codes + static_cast<long long>(n0 / kTileOut) * p.w.tiles_in * kTileBytes + n0 % kTileOut * kTileIn + lane * 16;
+  const int piece = ((lane & 3) ^ (lane / 8 & 3)) * 16;   // that the lane's codes are
+  int sum[4][N] = {};
+  for (int k0 = 0; k0 < p.w.in; k0 += kChunk) {
+    uint4 w[kAhead][4];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int tile = min(k0 / kTileIn + a * kFewWarps + warp, p.w.tiles_in - 1);   // (behind the last: with codes of 0 for the tokens)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[a][i] = __ldg(reinterpret_cast<const uint4*>(from + static_cast<long long>(tile) * kTileBytes + i * 512));
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < N * (kChunk / 16); i += 32 * kFewWarps) {
+      const int t = i / (kChunk / 16), k = i % (kChunk / 16) * 16;
+      const int8_t* row = p.codes + (t < p.rows ? t : 0) * p.codes_stride + k0 + k;
+      uint32_t c[4] = {0, 0, 0, 0};
+      if (t < p.rows) {
+        if (k0 + k + 16 <= p.w.in && reinterpret_cast<uintptr_t>(row) % 16 == 0) {
+          const uint4 u = *reinterpret_cast<const uint4*>(row);
+          c[0] = u.x, c[1] = u.y, c[2] = u.z, c[3] = u.w;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            if (k0 + k + j < p.w.in) c[j / 4] |= static_cast<uint32_t>(row[j] & 0xff) << 8 * (j % 4);
+          }
+        }
+      }
+      *reinterpret_cast<uint4*>(&x[t][k]) = make_uint4(c[0], c[1], c[2], c[3]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[a][i].x ^= 0x80808080u, w[a][i].y ^= 0x80808080u, w[a][i].z ^= 0x80808080u, w[a][i].w ^= 0x80808080u;
+#pragma unroll
+      for (int t = 0; t < N; ++t) {
+        const uint4 v = *reinterpret_cast<const uint4*>(&x[t][(a * kFewWarps + warp) * kTileIn + piece]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          int s = __dp4a(static_cast<int>(w[a][i].x), static_cast<int>(v.x), sum[i][t]);
+          s = __dp4a(static_cast<int>(w[a][i].y), static_cast<int>(v.y), s);
+          s = __dp4a(static_cast<int>(w[a][i].z), static_cast<int>(v.z), s);
+          sum[i][t] = __dp4a(static_cast<int>(w[a][i].w), static_cast<int>(v.w), s);
+        }
+      }
+    }
+  }
+  // the four lanes of a channel, then the warps
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sum[i][t] += __shfl_xor_sync(0xffffffffu, sum[i][t], 1);
+      sum[i][t] += __shfl_xor_sync(0xffffffffu, sum[i][t], 2);
+      if ((lane & 3) == i) sums[warp][t][8 * i + lane / 4] = sum[i][t];
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < N * kFewChannels; i += 32 * kFewWarps) {
+    const int t = i / kFewChannels, c = i % kFewChannels, n = n0 + c;
+    if (t >= p.rows || n >= p.w.out) continue;
+    int all = 0;
+#pragma unroll
+    for (int k = 0; k < kFewWarps; ++k) all += sums[k][t][c];
+    float y = result(__int2float_rn(all), p.scale[t], p.w.scale[n], p.bias ? p.bias[n] : -0.0f);
+    if (p.residual.p) y = __fadd_rn(y, static_cast<float>(static_cast<const T*>(p.residual.p)[t * p.residual.stride + n]));
+    static_cast<T*>(p.y.p)[t * p.y.stride + n] = static_cast<T>(y);
+  }
+}
+
+// Whether a call goes that way: its dot products take as long as the reading from
+// about six tokens on, which large weights feel. FEW_RULE
+bool is_few(int rows, int out, int in) { return rows <= 4 || (rows <= kFewTokens && static_cast<long long>(out) * in <= 1ll << 26); }
+
+template <typename T>
+cudaError_t few_of(const ProductParams& p, cudaStream_t s) {
+  const unsigned blocks = static_cast<unsigned>((p.w.out + kFewChannels - 1) / kFewChannels);
+  constexpr int kBlock = 32 * kFewWarps;
+  if (p.rows == 1) return launch_early(few_kernel<T, 1>, blocks, kBlock, 0, s, p);
+  if (p.rows == 2) return launch_early(few_kernel<T, 2>, blocks, kBlock, 0, s, p);
+  if (p.rows <= 4) return launch_early(few_kernel<T, 4>, blocks, kBlock, 0, s, p);
+  return launch_early(few_kernel<T, 8>, blocks, kBlock, 0, s, p);
 }
 
 struct Scratch {
@@ -660,13 +767,22 @@ Plan plan_of(int rows, const Packed& w, int sms, Scratch* at) {
   g.sum_columns = (g.tokens + 31) / 32 * 32;
   g.stages = min(kStages, (kTmemColumns - g.accumulators * g.sum_columns) / kStageColumns);
   g.x_ring = kStages;
-  g.codes_ring = min(kMostCodes, static_cast<int>((kAtMisc - g.x_ring * g.tokens * kTileIn) / kTileBytes));
+  g.codes_ring = min(kMostCodes, static_cast<int>(((rows <= 2 * g.pairs ? kRingsBeside : kRings) - g.x_ring * g.tokens * kTileIn) / kTileBytes));
   const long long tiles = static_cast<long long>(g.channel_tiles) * g.token_tiles;
-  // whole tiles as long as they go round, but for the last round; one round and what is left over are cut up
-  const long long rounds = tiles % g.pairs == 0 ? tiles / g.pairs : max(0ll, tiles / g.pairs - 1);
-  g.whole = static_cast<int>(rounds * g.pairs);
+  // Whole tiles as long as they go round, but for the last round; one round and
+  // what is left over are cut up, unless another round of whole tiles takes less time than
+  // the joining of parts. (In ns: a feature tile takes as long as its products, 2 cycles
+  // a token, or the reading of its codes; leaving and joining parts 30 a token and 2000. PLAN_FIGURES)
+  const long long left = tiles % g.pairs, stage = max(g.tokens, 175) * 105ll / 100;
+  const bool cut = left && (g.pairs - left) * g.per_tile * stage / g.pairs > 30ll * g.tokens + 2000;
+  const long long rounds = cut ? max(0ll, tiles / g.pairs - 1) : (tiles + g.pairs - 1) / g.pairs;
+  g.whole = static_cast<int>(min(tiles, rounds * g.pairs));
   g.units = static_cast<int>(tiles - g.whole) * g.per_tile;
   g.shares = min(g.pairs, max(1, g.units / 4));
+  // Fewer tiles than pairs: as many shares to each (16 tiles of 32 tokens over 76
+  // pairs, 64 features tiles each: ALIGNED_FIGURES).
+  const int of_tile = g.pairs / static_cast<int>(max(1ll, min(tiles, static_cast<long long>(g.pairs))));
+  if (g.whole == 0 && of_tile > 1 && g.per_tile >= 4 * of_tile) g.shares = static_cast<int>(tiles) * of_tile;
   g.share = g.units / g.shares;
   g.longer = g.units % g.shares;
   at->squares = 4096;
@@ -679,12 +795,20 @@ Plan plan_of(int rows, const Packed& w, int sms, Scratch* at) {
 
 template <typename T>
 cudaError_t product_of(const ProductParams& p, const Plan& g, unsigned char* x, uint32_t* squares, cudaStream_t s) {
-  constexpr int kShared = kAtMisc + sizeof(Misc);
+  constexpr int kShared = kAtRings + kRings;
   static_assert(kShared <= 227 * 1024, "shared memory");
-  cudaError_t e = cudaFuncSetAttribute(product_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
-  if (e == cudaSuccess) e = launch_early(spread_kernel, p.rows, 256, 0, s, p, g, x, squares);
+  const int shared = kAtRings + g.codes_ring * kTileBytes + g.x_ring * g.tokens * kTileIn;
+  // (once a device: the call costs as much as a launch)
+  static std::atomic<uint64_t> allowed{0};
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e == cudaSuccess && (device >= 64 || !(allowed.load(std::memory_order_relaxed) >> device & 1))) {
+    e = cudaFuncSetAttribute(product_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
+    if (e == cudaSuccess && device < 64) allowed.fetch_or(1ull << device, std::memory_order_relaxed);
+  }
+  if (e == cudaSuccess) e = launch_early(spread_kernel, p.rows, kSpreadBlock, 0, s, p, g, x, squares);
   if (e != cudaSuccess) return e;
-  return launch_early(product_kernel<T>, 2 * g.pairs, kThreads, kShared, s, p, g);
+  return launch_early(product_kernel<T>, 2 * g.pairs, kThreads, shared, s, p, g);
 }
 
 }  // namespace
@@ -694,6 +818,7 @@ cudaError_t launch_pack(const int8_t* w, long long stride, const float* scale, c
 }
 
 size_t product_scratch_bytes(int rows, int out, int in, int sms) {
+  if (is_few(rows, out, in)) return 256;   // (not used)
   Packed w;
   packed_layout(out, in, nullptr, &w);
   Scratch at;
@@ -702,6 +827,7 @@ size_t product_scratch_bytes(int rows, int out, int in, int sms) {
 }
 
 cudaError_t launch_product(const ProductParams& p, int dtype, int sms, unsigned char* scratch, cudaStream_t s) {
+  if (is_few(p.rows, p.w.out, p.w.in)) return dtype == SJD_BF16 ? few_of<__nv_bfloat16>(p, s) : few_of<float>(p, s);
   Scratch at;
   Plan g = plan_of(p.rows, p.w, sms, &at);
   g.counters = reinterpret_cast<int32_t*>(scratch);

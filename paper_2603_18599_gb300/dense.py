@@ -20,6 +20,7 @@ gradients.
 """
 
 import ctypes
+import functools
 import struct
 from ctypes import c_float, c_int32, c_int64, c_size_t, c_void_p
 
@@ -67,9 +68,10 @@ def _no_gradient(x, name):
 
 def _rows(x, name, dtypes, device=None):
     """x as [rows, features], its last dimension dense."""
-    if x.dim() < 1 or x.dtype not in dtypes or x.device.type != "cuda" or (device is not None and x.device != device):
+    if x.dtype not in dtypes or not x.is_cuda or (device is not None and x.device != device) or x.dim() < 1:
         raise ValueError("%s must be a tensor of %s on %s" % (name, " or ".join(str(d) for d in dtypes), device or "a GPU"))
-    _no_gradient(x, name)
+    if x.requires_grad:
+        _no_gradient(x, name)
     if x.dim() != 2:
         try:
             x = x.view(-1, x.shape[-1]) if x.numel() else x.reshape(x.shape[:-1].numel(), x.shape[-1])
@@ -90,9 +92,10 @@ def _same(x, name, like):
 def _vector(x, name, n, device):
     if x is None:
         return None
-    if x.shape != (n,) or x.dtype != torch.float32 or x.device != device or not x.is_contiguous():
+    if x.dtype != torch.float32 or x.dim() != 1 or x.shape[0] != n or x.device != device or not x.is_contiguous():
         raise ValueError("%s must be a contiguous float32 tensor of shape (%d,) on %s" % (name, n, device))
-    _no_gradient(x, name)
+    if x.requires_grad:
+        _no_gradient(x, name)
     return x.data_ptr()
 
 
@@ -112,24 +115,24 @@ def _tokens(tokens, device):
 
 
 def _run(device, name, *args):
-    """One call, its last argument the device's current stream."""
-    call = getattr(load(), name)
-    if _current_device() == device.index:
-        rc = call(*args, _raw_stream(device.index))
+    """One call, its last argument the device's current stream, which is returned."""
+    call, index = getattr(_lib or load(), name), device.index
+    raw = _raw_stream(index)
+    if _current_device() == index:
+        rc = call(*args, raw)
     else:
         with torch.cuda.device(device):
-            rc = call(*args, _raw_stream(device.index))
+            rc = call(*args, raw)
     if rc != SJD_OK:
         raise SJDError(rc, "%s failed" % name)
+    return raw
 
 
-def _size(device, name, *args):
-    """A workspace's size, on the device that it is for."""
-    call = getattr(load(), name)
-    if _current_device() == device.index:
-        return call(*args)
-    with torch.cuda.device(device):
-        return call(*args)
+@functools.lru_cache(4096)
+def _size(index, name, *args):
+    """A workspace's size, on the device that it is for (it depends on nothing else)."""
+    with torch.cuda.device(index):
+        return getattr(load(), name)(*args)
 
 
 class Weight:
@@ -159,9 +162,8 @@ class Weight:
     def _used_on(self, raw):
         """The codes' memory is not handed out again before a call on another
         stream than the one they were made on has read them."""
-        if raw not in self._streams:
-            self._streams.add(raw)
-            self._packed.record_stream(torch.cuda.current_stream(self.device))
+        self._streams.add(raw)
+        self._packed.record_stream(torch.cuda.current_stream(self.device))
 
     def sync(self):
         """Returns the device-side status code of the products with this weight
@@ -181,21 +183,24 @@ def product(codes, scale, weight, bias=None, residual=None, dtype=torch.bfloat16
     if x.shape[1] != weight.dim:
         raise ValueError("codes have %d features, the weight %d" % (x.shape[1], weight.dim))
     rows, out = x.shape[0], weight.out
-    if scale.shape != shape[:-1]:
+    if (scale.shape[0] != rows if scale.dim() == 1 == len(shape) - 1 else scale.shape != shape[:-1]):
         raise ValueError("scale must have the shape %s" % (tuple(shape[:-1]),))
-    at = _vector(scale if scale.dim() == 1 else scale.reshape(-1) if scale.is_contiguous() else scale, "scale", rows, device)
+    if scale.dim() != 1 and scale.is_contiguous():
+        scale = scale.view(-1)
+    at = _vector(scale, "scale", rows, device)
     b = _vector(bias, "bias", out, device)
-    y = torch.empty((*shape[:-1], out), dtype=dtype, device=device)
+    y = torch.empty((rows, out) if len(shape) == 2 else (*shape[:-1], out), dtype=dtype, device=device)
     r = None
     if residual is not None:
         r = _same(residual, "residual", y)
     if rows == 0:
         return y
-    size = _size(device, "sjd_product_workspace_size", rows, out, weight.dim)
+    size = _size(device.index, "sjd_product_workspace_size", rows, out, weight.dim)
     workspace = torch.empty(size, dtype=torch.uint8, device=device)
-    _run(device, "sjd_product", weight._at, out, weight.dim, _pack(x), at, rows, b, _pack(r), _DTYPES[dtype],
+    raw = _run(device, "sjd_product", weight._at, out, weight.dim, _pack(x), at, rows, b, _pack(r), _DTYPES[dtype],
          _ROWS.pack(y.data_ptr(), out), workspace.data_ptr(), size)
-    weight._used_on(_raw_stream(device.index))
+    if raw not in weight._streams:
+        weight._used_on(raw)
     return y
 
 
@@ -270,7 +275,7 @@ def norm_gradient(dy, x, gain=None, eps=1e-6, centre=False, dh=None, bias=False)
     dgain = made(dim, dtype=torch.float32, device=device)
     dbias = made(dim, dtype=torch.float32, device=device) if bias else None
     if n:
-        size = _size(device, "sjd_norm_gradient_workspace_size", n, dim, _DTYPES[dtype])
+        size = _size(device.index, "sjd_norm_gradient_workspace_size", n, dim, _DTYPES[dtype])
         workspace = torch.empty(size, dtype=torch.uint8, device=device)
         _run(device, "sjd_norm_gradient", _pack(d), _pack(rows), g, eps, 1 if centre else 0, _pack(r), n, dim, _DTYPES[dtype],
              _ROWS.pack(dx.data_ptr(), dim), dgain.data_ptr(), dbias.data_ptr() if bias else None, workspace.data_ptr(), size)
