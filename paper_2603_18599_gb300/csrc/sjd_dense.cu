@@ -894,7 +894,7 @@ cudaError_t embed_of(const EmbedParams& p, cudaStream_t s) {
 // there. Warp w looks through the w-th part of the tokens both times, so that
 // its rows of an id stand behind those of the warps before it. The ids that have
 // more than kFew rows are listed.
-constexpr int kFew = 32;
+constexpr int kFew = 8;
 constexpr int kIds = kListIds, kIndexWarps = 32;
 __device__ __forceinline__ int4* many_of(const EmbedGradientParams& p, int list) { return p.many + static_cast<long long>(list) * (kIds + 1); }
 __global__ void __launch_bounds__(32 * kIndexWarps) index_kernel(const EmbedGradientParams p) {
@@ -986,10 +986,11 @@ __device__ __forceinline__ void load_columns(const T* p, float (&x)[W ? 4 : 1]) 
 
 // grad[v] = scale sum of dy over the rows of v, in their order.
 //
-// The ids that have more than kFew rows are what most is read of: a block takes
-// 128 columns of every shares-th such id of every groups-th list, the id's rows
-// shared out to its warps, whose sums are added up in order.
-constexpr int kSumBlock = 256, kSumColumns = 128, kGroups = 8, kPlaces = 512;
+// The ids that have more than kFew rows are what most is read of. A block takes 128
+// columns of its share of some lists: a warp an id, but for those of more than
+// kMost rows, which are shared out to the block's warps, and their sums added up
+// in order.
+constexpr int kSumBlock = 256, kSumColumns = 128, kGroups = 8, kMost = 256, kPlaces = 512;
 template <typename T, bool W>
 __global__ void __launch_bounds__(kSumBlock, 4) embed_gradient_many_kernel(const EmbedGradientParams p, int slices, int shares, int groups, int lists) {
   constexpr int V = W ? 4 : 1, kDeep = 8, kWarps = kSumBlock / 32, kPieces = kSumColumns / 32 / V;   // (pieces of a lane)
@@ -998,51 +999,74 @@ __global__ void __launch_bounds__(kSumBlock, 4) embed_gradient_many_kernel(const
   let_next_start();
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, D = p.dim;
   const int slice = blockIdx.x % slices, share = blockIdx.x / slices % shares, group = blockIdx.x / (slices * shares);
-  for (long long list0 = group; list0 < lists; list0 += 32ll * groups) {
-    const long long of_lane = list0 + static_cast<long long>(lane) * groups;
-    const int n_of_lane = of_lane < lists ? many_of(p, static_cast<int>(of_lane))[0].x : 0;
-    for (unsigned some = __ballot_sync(0xffffffffu, n_of_lane > share); some; some &= some - 1) {
-      const int from_lane = __ffs(some) - 1, n = __shfl_sync(0xffffffffu, n_of_lane, from_lane);
-      const int4* many = many_of(p, static_cast<int>(list0 + static_cast<long long>(from_lane) * groups)) + 1;
-      for (int k = share; k < n; k += shares) {
-        const int4 id = many[k];   // the id, where its places begin, how many
-        const int per = (id.z + kWarps - 1) / kWarps, begin = id.y + warp * per, end = min(begin + per, id.y + id.z);
-        float sum[kPieces][V] = {};
-        for (int r0 = begin; r0 < end; r0 += 32) {
-          const int place = r0 + lane < end ? p.places[r0 + lane] : 0, rows = min(32, end - r0);
-          for (int r = 0; r < rows; r += kDeep) {
-            float x[kDeep][kPieces][V] = {};
+  auto column = [&](int c) { return slice * kSumColumns + (c * 32 + lane) * V; };
+  auto add_rows = [&](int begin, int end, float (&sum)[kPieces][V]) {
+    for (int r0 = begin; r0 < end; r0 += 32) {
+      const int place = r0 + lane < end ? p.places[r0 + lane] : 0, rows = min(32, end - r0);
+      for (int r = 0; r < rows; r += kDeep) {
+        float x[kDeep][kPieces][V] = {};
 #pragma unroll
-            for (int u = 0; u < kDeep; ++u) {
-              const int row = __shfl_sync(0xffffffffu, place, (r + u) & 31);
+        for (int u = 0; u < kDeep; ++u) {
+          const int row = __shfl_sync(0xffffffffu, place, (r + u) & 31);
 #pragma unroll
-              for (int c = 0; c < kPieces; ++c) {
-                const int column = slice * kSumColumns + (c * 32 + lane) * V;
-                if (r + u < rows && column < D) load_columns<W>(static_cast<const T*>(p.dy.p) + row * p.dy.stride + column, x[u][c]);
-              }
-            }
-#pragma unroll
-            for (int u = 0; u < kDeep; ++u) {
-#pragma unroll
-              for (int c = 0; c < kPieces; ++c) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) sum[c][j] += x[u][c][j];   // (0 for those that are not there)
-              }
-            }
+          for (int c = 0; c < kPieces; ++c) {
+            if (r + u < rows && column(c) < D) load_columns<W>(static_cast<const T*>(p.dy.p) + row * p.dy.stride + column(c), x[u][c]);
           }
         }
 #pragma unroll
+        for (int u = 0; u < kDeep; ++u) {
+#pragma unroll
+          for (int c = 0; c < kPieces; ++c) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum[c][j] += x[u][c][j];   // (0 for those that are not there)
+          }
+        }
+      }
+    }
+  };
+  for (long long list0 = group; list0 < lists; list0 += 32ll * groups) {
+    const long long of_lane = list0 + static_cast<long long>(lane) * groups;
+    const int n_of_lane = of_lane < lists ? many_of(p, static_cast<int>(of_lane))[0].x : 0;
+    for (unsigned some = __ballot_sync(0xffffffffu, n_of_lane > 0); some; some &= some - 1) {
+      const int from_lane = __ffs(some) - 1, n = __shfl_sync(0xffffffffu, n_of_lane, from_lane);
+      const int4* many = many_of(p, static_cast<int>(list0 + static_cast<long long>(from_lane) * groups)) + 1;
+      for (int k = share * kWarps + warp; k < n; k += shares * kWarps) {
+        const int4 id = many[k];   // the id, where its places begin, how many
+        if (id.z > kMost) continue;
+        float sum[kPieces][V] = {};
+        add_rows(id.y, id.y + id.z, sum);
+        float* out = p.grad + static_cast<long long>(id.x) * D;
+#pragma unroll
         for (int c = 0; c < kPieces; ++c) {
 #pragma unroll
-          for (int j = 0; j < V; ++j) sums[warp][(c * 32 + lane) * V + j] = sum[c][j];
+          for (int j = 0; j < V; ++j) sum[c][j] *= p.scale;
+          if (column(c) >= D) continue;
+          if constexpr (W) sjd_kv_ops::store4(out + column(c), true, sum[c]);
+          else out[column(c)] = sum[c][0];
         }
-        __syncthreads();
-        for (int column = threadIdx.x; column < kSumColumns; column += kSumBlock) {
-          float all = 0.0f;
-          for (int w = 0; w < kWarps; ++w) all += sums[w][column];
-          if (slice * kSumColumns + column < D) p.grad[static_cast<long long>(id.x) * D + slice * kSumColumns + column] = all * p.scale;
+      }
+      for (int k0 = 0; k0 < n; k0 += 32) {
+        const bool most = k0 + lane < n && many[k0 + lane].z > kMost;
+        for (unsigned of = __ballot_sync(0xffffffffu, most); of; of &= of - 1) {
+          const int k = k0 + __ffs(of) - 1;
+          if (k % shares != share) continue;
+          const int4 id = many[k];
+          const int per = (id.z + kWarps - 1) / kWarps, begin = id.y + warp * per;
+          float sum[kPieces][V] = {};
+          add_rows(begin, min(begin + per, id.y + id.z), sum);
+#pragma unroll
+          for (int c = 0; c < kPieces; ++c) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) sums[warp][(c * 32 + lane) * V + j] = sum[c][j];
+          }
+          __syncthreads();
+          for (int i = threadIdx.x; i < kSumColumns; i += kSumBlock) {
+            float all = 0.0f;
+            for (int w = 0; w < kWarps; ++w) all += sums[w][i];
+            if (slice * kSumColumns + i < D) p.grad[static_cast<long long>(id.x) * D + slice * kSumColumns + i] = all * p.scale;
+          }
+          __syncthreads();
         }
-        __syncthreads();
       }
     }
   }

@@ -11,7 +11,11 @@ step before (a rejected draft's are replaced at once), attends with W queries
 to everything before each of them, and gives the logits of W positions. Where
 the window stands is read from device arrays: no step waits for the host.
 
-    python -m paper_2603_18599_gb300.window_model --cache e4m3 --grid 24
+With weights="s8" the embedding, the norms and the matrix products run on the
+library too (dense.py): weights and what goes into a product are held in
+8-bit codes, with a scale for each channel and each token.
+
+    python -m paper_2603_18599_gb300.window_model --cache e4m3 --weights s8 --grid 24
 """
 
 import argparse
@@ -19,7 +23,7 @@ import time
 
 import torch
 
-from . import kv, sjd
+from . import dense, kv, sjd
 
 CACHES = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "s8": torch.int8}
 
@@ -30,7 +34,7 @@ class WindowModel:
     and column in the image's grid."""
 
     def __init__(self, images, window, prompts, grid, vocab=8192, layers=2, heads=8, kv_heads=2, head_dim=64, page_size=32,
-                 cache=torch.bfloat16, seed=0, device="cuda"):
+                 cache=torch.bfloat16, seed=0, device="cuda", weights="bf16"):
         self.images, self.window, self.grid, self.vocab, self.device = images, window, grid, vocab, device
         self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
         dim = heads * head_dim
@@ -46,6 +50,15 @@ class WindowModel:
         self.layers = [{"qkv": weight(dim, (heads + 2 * kv_heads) * head_dim), "o": weight(dim, dim),
                         "up": weight(dim, 2 * dim), "down": weight(2 * dim, dim)} for _ in range(layers)]
         self.head = weight(dim, vocab)
+        if weights not in ("bf16", "s8"):
+            raise ValueError("weights are bf16 or s8")
+        self.packed = None
+        if weights == "s8":
+            def packed(w):
+                return dense.Weight.quantise(w.T.contiguous())
+
+            self.packed = [{name: packed(w) for name, w in layer.items()} for layer in self.layers]
+            self.packed_head = packed(self.head)
         pairs = head_dim // 2
         side = pairs // 8 * 3
         self.rope = kv.Rope.sections((pairs - 2 * side, side, side), device=device)
@@ -78,6 +91,8 @@ class WindowModel:
         B, n = tokens.shape
         h, g, d = self.heads, self.kv_heads, self.head_dim
         positions = self.positions(start[:, None] + torch.arange(n, device=self.device))
+        if self.packed:
+            return self._hidden_in_codes(tokens, positions, start, count)
         x = self.embed[tokens]
         for w, held in zip(self.layers, self.held):
             qkv = (self.norm(x) @ w["qkv"]).view(B, n, h + 2 * g, d)
@@ -87,6 +102,26 @@ class WindowModel:
             x = x + o.view(B, n, h * d) @ w["o"]
             x = x + torch.nn.functional.silu(self.norm(x) @ w["up"]) @ w["down"]
         return x
+
+    def _hidden_in_codes(self, tokens, positions, start, count):
+        """The same with the products in 8-bit codes; a branch's sum with the
+        residual stream is part of its last product, the norm that follows gives codes."""
+        B, n = tokens.shape
+        h, g, d = self.heads, self.kv_heads, self.head_dim
+        x = dense.embed(self.embed, tokens.int().contiguous())
+        for w, held in zip(self.packed, self.held):
+            qkv = dense.product(*dense.norm_codes(x), w["qkv"]).view(B, n, h + 2 * g, d)
+            q = self.cache.write(held, qkv[:, :, h:h + g], qkv[:, :, h + g:], self.table, start, count, rope=self.rope,
+                                 positions=positions, q=qkv[:, :, :h])
+            o = self.cache.attend(held, q, self.table, start, count)
+            x = dense.product(*dense.quantise(o.view(B, n, h * d)), w["o"], residual=x)
+            up = torch.nn.functional.silu(dense.product(*dense.norm_codes(x), w["up"]))
+            x = dense.product(*dense.quantise(up), w["down"], residual=x)
+        return x
+
+    def logits(self, x):
+        """Logits [..., vocab] of the last layer's output."""
+        return dense.product(*dense.norm_codes(x), self.packed_head) if self.packed else self.norm(x) @ self.head
 
     def prefill(self):
         """The prompts, but for their last tokens, into the cache: one chunk,
@@ -105,7 +140,7 @@ class WindowModel:
         last = torch.where(abs_pos == 0, opening, prev.expand(2, -1))
         tokens = torch.cat([last[:, :, None], window[:, :-1].expand(2, -1, -1)], 2).view(2 * self.images, -1)
         x = self.hidden(tokens, self.first + abs_pos.repeat(2))
-        logits = (self.norm(x) @ self.head).view(2, self.images, self.window, self.vocab)
+        logits = self.logits(x).view(2, self.images, self.window, self.vocab)
         cond.copy_(logits[0])
         uncond.copy_(logits[1])
 
@@ -113,6 +148,7 @@ class WindowModel:
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--cache", choices=sorted(CACHES), default="e4m3")
+    ap.add_argument("--weights", choices=("bf16", "s8"), default="bf16")
     ap.add_argument("--images", type=int, default=2)
     ap.add_argument("--window", type=int, default=16)
     ap.add_argument("--grid", type=int, default=24, help="image tokens per row and column")
@@ -120,7 +156,7 @@ def main():
     args = ap.parse_args()
     B, W, V = args.images, args.window, args.vocab
     prompts = [20 + 7 * b for b in range(B)] + [1] * B                       # conditional, unconditional
-    model = WindowModel(B, W, prompts, args.grid, V, cache=CACHES[args.cache])
+    model = WindowModel(B, W, prompts, args.grid, V, cache=CACHES[args.cache], weights=args.weights)
     cfg = sjd.make_config(B, W, V, cfg_scale=3.0, top_k=2000, seed=0)
     ctx = sjd.SJD(cfg)
     cond, uncond = (torch.empty(B, W, V, dtype=torch.bfloat16, device="cuda") for _ in range(2))
@@ -131,8 +167,10 @@ def main():
     seconds = time.perf_counter() - begun
     if model.cache.sync() != sjd.SJD_OK:
         raise SystemExit("cache: " + model.cache.last_error())
-    print("%d images of %d tokens: %d steps, %.2f tokens accepted per step, %.2f ms per step, %s cache" % (
-        B, tokens.shape[1], steps, B * tokens.shape[1] / (B * steps), seconds / steps * 1e3, args.cache))
+    if model.packed and any(w.sync() != sjd.SJD_OK for w in (model.packed_head, *(w for layer in model.packed for w in layer.values()))):
+        raise SystemExit("a product's wait ran out")
+    print("%d images of %d tokens: %d steps, %.2f tokens accepted per step, %.2f ms per step, %s cache, %s weights" % (
+        B, tokens.shape[1], steps, B * tokens.shape[1] / (B * steps), seconds / steps * 1e3, args.cache, args.weights))
 
 
 if __name__ == "__main__":
