@@ -893,8 +893,7 @@ cudaError_t embed_of(const EmbedParams& p, cudaStream_t s) {
 // which is where its part of `places` begins, and then puts the rows of its ids
 // there. Warp w looks through the w-th part of the tokens both times, so that
 // its rows of an id stand behind those of the warps before it. The ids that have
-// more than kFew rows are listed.
-constexpr int kFew = 8;
+// more than p.few rows are listed.
 constexpr int kIds = kListIds, kIndexWarps = 32;
 __device__ __forceinline__ int4* many_of(const EmbedGradientParams& p, int list) { return p.many + static_cast<long long>(list) * (kIds + 1); }
 __global__ void __launch_bounds__(32 * kIndexWarps) index_kernel(const EmbedGradientParams p) {
@@ -948,7 +947,7 @@ __global__ void __launch_bounds__(32 * kIndexWarps) index_kernel(const EmbedGrad
     for (int w = 0; w < kIndexWarps; ++w) base += before[w];
     for (int w = 0; w < warp; ++w) base += sums[w];
     if (static_cast<int>(threadIdx.x) < here) p.first[low + threadIdx.x] = base;
-    if (count > kFew) many_of(p, blockIdx.x)[1 + atomicAdd(&n_many, 1)] = make_int4(low + threadIdx.x, base, count, 0);
+    if (count > p.few) many_of(p, blockIdx.x)[1 + atomicAdd(&n_many, 1)] = make_int4(low + threadIdx.x, base, count, 0);
     if (low + static_cast<int>(threadIdx.x) == p.vocab - 1) p.first[p.vocab] = base + count;
     for (int w = 0; w < kIndexWarps; ++w) {
       const int n = at[w][threadIdx.x];
@@ -986,14 +985,14 @@ __device__ __forceinline__ void load_columns(const T* p, float (&x)[W ? 4 : 1]) 
 
 // grad[v] = scale sum of dy over the rows of v, in their order.
 //
-// The ids that have more than kFew rows are what most is read of. A block takes 128
+// The ids that have more than p.few rows are what most is read of. A block takes 128
 // columns of its share of some lists: a warp an id, but for those of more than
 // kMost rows, which are shared out to the block's warps, and their sums added up
 // in order.
-constexpr int kSumBlock = 256, kSumColumns = 128, kGroups = 8, kMost = 256, kPlaces = 512;
+constexpr int kSumBlock = 256, kSumColumns = 128, kGroups = 8, kMost = 64, kPlaces = 512;
 template <typename T, bool W>
-__global__ void __launch_bounds__(kSumBlock, 4) embed_gradient_many_kernel(const EmbedGradientParams p, int slices, int shares, int groups, int lists) {
-  constexpr int V = W ? 4 : 1, kDeep = 8, kWarps = kSumBlock / 32, kPieces = kSumColumns / 32 / V;   // (pieces of a lane)
+__global__ void __launch_bounds__(kSumBlock, 2) embed_gradient_many_kernel(const EmbedGradientParams p, int slices, int shares, int groups, int lists) {
+  constexpr int V = W ? 4 : 1, kDeep = W ? 16 : 8, kWarps = kSumBlock / 32, kPieces = kSumColumns / 32 / V;   // (pieces of a lane)
   __shared__ float sums[kWarps][kSumColumns];
   wait_for_previous();
   let_next_start();
@@ -1100,7 +1099,7 @@ __global__ void __launch_bounds__(kSumBlock, 8) embed_gradient_kernel(const Embe
   // `lanes` threads (a power of two) to an id
   for (int k = threadIdx.x / lanes; k < here; k += kSumBlock / lanes) {
     const int from = first[k] - base, count = first[k + 1] - base - from;
-    if (count > kFew) continue;
+    if (count > p.few) continue;
     float* out = p.grad + (static_cast<long long>(v0) + k) * D;
     for (int column = lane * V; column < D; column += lanes * V) {
       float sum[V] = {};
@@ -1135,7 +1134,7 @@ cudaError_t embed_gradient_of(const EmbedGradientParams& p, cudaStream_t s) {
   int lanes = 8;
   while (lanes < kSumBlock && lanes * (w ? 4 : 1) < p.dim) lanes *= 2;
   const unsigned blocks = static_cast<unsigned>((static_cast<long long>(p.vocab) + ids - 1) / ids);
-  const bool many = p.rows > kFew;   // (some id may have so many)
+  const bool many = p.rows > p.few;   // (some id may have so many)
   if (many) {
     const unsigned n = static_cast<unsigned>(slices) * shares * groups;
     e = w ? launch_early(embed_gradient_many_kernel<T, true>, n, kSumBlock, 0, s, p, slices, shares, groups, lists)

@@ -58,6 +58,7 @@ struct EmbedGradientParams {
   int4* many;               // [lists][1 + ids of a list]: how many ids have many rows; of each the id, where its places begin, how many
   float scale;
   int rows, dim, vocab;
+  int few;                  // an id with more rows is one of many
 };
 
 // A packed weight: a header, the channels' scales and the codes in tiles of
