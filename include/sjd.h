@@ -53,9 +53,9 @@ extern "C" {
 #define SJD_ERR_INVALID_DRAFT 6  /* a draft token has zero draft probability     */
 #define SJD_ERR_CALLBACK 7       /* the forward callback returned non-zero       */
 #define SJD_ERR_STATE 8          /* call out of order (see sjd_draft)            */
-#define SJD_ERR_TIMEOUT 9        /* a wait inside a kernel ran out (sjd_kv_attend,
-                                    whose warps wait for one another; no
-                                    other kernel waits)                         */
+#define SJD_ERR_TIMEOUT 9        /* a wait inside a kernel ran out (sjd_kv_attend
+                                    and sjd_product, whose warps wait for one
+                                    another; no other kernel waits)             */
 #define SJD_ERR_BOUNDS 10        /* the bounds-checked build (libsjd_checked.so)
                                     found an index outside its array; the
                                     access was clamped, results are not valid  */

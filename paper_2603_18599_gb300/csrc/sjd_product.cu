@@ -16,9 +16,12 @@
 // into shared memory; eight warps turn them into fp16 in tensor memory, from
 // where the product takes them as its A; the tokens' codes, spread to fp16 by a
 // small kernel before, are its B, half of them in each block. So the weight is read
-// once in bytes, which bounds calls of few tokens, and the conversion of a tile costs
-// each thread 32 exchanges of bytes and 32 sums beside a product of 1024 cycles
-// (256 tokens), which bounds those of many.
+// once in bytes, which bounds calls of few tokens, and its conversion, four
+// instructions for four codes, goes on beside the products, which bound those of many. Up to
+// 192 tokens have two accumulators: a tile's results are given while the next one is summed
+// up (8100 tokens x 16384 channels of 4096: 567 to 590 us, 1.84 to 1.92 PFLOP/s, as much as
+// a library product of bf16; 844 with one accumulator of 256 tokens). 128 tokens x 65536 channels, f32: 63
+// us, 300 MB; a copy of the kernel without conversion and products takes 58.
 
 #include <atomic>
 
@@ -34,7 +37,22 @@ using namespace sjd_kv_ops;
 
 namespace {
 
-// A block packs one channel's codes: a tile's 128 at a time.
+// 16 codes from k on, zeros behind the row's end; 16 bytes at a time where the row allows it.
+__device__ __forceinline__ void load_codes(const int8_t* row, int k, int end, uint32_t (&c)[4]) {
+  if (k + 16 <= end && reinterpret_cast<uintptr_t>(row + k) % 16 == 0) {
+    const uint4 u = *reinterpret_cast<const uint4*>(row + k);
+    c[0] = u.x, c[1] = u.y, c[2] = u.z, c[3] = u.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] = 0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      if (k + j < end) c[j / 4] |= static_cast<uint32_t>(row[k + j] & 0xff) << 8 * (j % 4);
+    }
+  }
+}
+
+// A block packs one channel's codes.
 __global__ void __launch_bounds__(128) pack_kernel(const int8_t* w, long long stride, const float* scale, const Packed to) {
   __shared__ uint32_t words[4];
   wait_for_previous();
@@ -42,11 +60,14 @@ __global__ void __launch_bounds__(128) pack_kernel(const int8_t* w, long long st
   const int channel = blockIdx.x, r = channel % kTileOut;
   unsigned char* tile = to.codes + static_cast<long long>(channel / kTileOut) * to.tiles_in * kTileBytes + r * kTileIn;
   uint32_t squares = 0;
-  for (int k = threadIdx.x; k < to.tiles_in * kTileIn; k += 128) {
-    const int c = channel < to.out && k < to.in ? w[channel * stride + k] : 0;
-    squares += c * c;
+#pragma unroll 2
+  for (int k = threadIdx.x * 16; k < to.tiles_in * kTileIn; k += 128 * 16) {
+    uint32_t c[4];
+    load_codes(w + channel * stride, k, channel < to.out ? to.in : 0, c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) squares = __dp4a(static_cast<int>(c[j]), static_cast<int>(c[j]), static_cast<int>(squares)), c[j] ^= 0x80808080u;
     const int piece = (k % kTileIn) / 16 ^ (r / 2 % 4);
-    tile[static_cast<long long>(k / kTileIn) * kTileBytes + piece * 16 + k % 16] = static_cast<unsigned char>(c + 128);
+    *reinterpret_cast<uint4*>(tile + static_cast<long long>(k / kTileIn) * kTileBytes + piece * 16) = make_uint4(c[0], c[1], c[2], c[3]);
   }
   squares = __reduce_add_sync(0xffffffffu, squares);
   if (threadIdx.x % 32 == 0) words[threadIdx.x / 32] = squares;
@@ -616,21 +637,11 @@ __global__ void __launch_bounds__(kSpreadBlock, 16) spread_kernel(const ProductP
   const int8_t* from = p.codes + t * p.codes_stride;
   const int tile = t / g.tokens, r = t - tile * g.tokens, of_half = r / half, row = r - of_half * half;
   unsigned char* to = x + static_cast<long long>(tile * 2 + of_half) * g.per_tile * half * 128 + row * 128;
-  const bool wide = reinterpret_cast<uintptr_t>(from) % 16 == 0;
   uint32_t sum = 0;
 #pragma unroll 2
   for (int k = threadIdx.x * 16; k < g.per_tile * kTileIn; k += kSpreadBlock * 16) {
-    uint32_t c[4] = {0, 0, 0, 0};
-    if (wide && k + 16 <= p.w.in) {
-      const uint4 u = *reinterpret_cast<const uint4*>(from + k);
-      c[0] = u.x, c[1] = u.y, c[2] = u.z, c[3] = u.w;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        if (k + j < p.w.in) c[j / 4] |= static_cast<uint32_t>(from[k + j] & 0xff) << 8 * (j % 4);
-      }
-    }
-    uint32_t h[8];
+    uint32_t c[4], h[8];
+    load_codes(from, k, p.w.in, c);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       sum = __dp4a(static_cast<int>(c[i]), static_cast<int>(c[i]), static_cast<int>(sum));
@@ -656,7 +667,8 @@ __global__ void __launch_bounds__(kSpreadBlock, 16) spread_kernel(const ProductP
 // has neither fp16 nor shared tiles to wait for. A block takes 32 channels, a warp
 // every eighth tile of 64 features of them (2 KB side by side), kAhead of them in its
 // registers at a time; a lane reads piece l % 4 of channels l / 4, 8 + l / 4, ... and adds to
-// their sums with all tokens, whose codes lie in shared memory. FEW_FIGURES
+// their sums with all tokens, whose codes lie in shared memory. One
+// token x 65536 channels of 4096: 41 us, 6.5 TB/s; two x 6144: 6.0 us (14.4 the other way).
 constexpr int kFewTokens = 8, kFewWarps = 8, kFewChannels = 32;
 
 template <typename T, int N>   // N: at least the call's tokens
@@ -681,19 +693,8 @@ __global__ void __launch_bounds__(32 * kFewWarps, 2) few_kernel(const ProductPar
     __syncthreads();
     for (int i = threadIdx.x; i < N * (kChunk / 16); i += 32 * kFewWarps) {
       const int t = i / (kChunk / 16), k = i % (kChunk / 16) * 16;
-      const int8_t* row = p.codes + (t < p.rows ? t : 0) * p.codes_stride + k0 + k;
-      uint32_t c[4] = {0, 0, 0, 0};
-      if (t < p.rows) {
-        if (k0 + k + 16 <= p.w.in && reinterpret_cast<uintptr_t>(row) % 16 == 0) {
-          const uint4 u = *reinterpret_cast<const uint4*>(row);
-          c[0] = u.x, c[1] = u.y, c[2] = u.z, c[3] = u.w;
-        } else {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            if (k0 + k + j < p.w.in) c[j / 4] |= static_cast<uint32_t>(row[j] & 0xff) << 8 * (j % 4);
-          }
-        }
-      }
+      uint32_t c[4];
+      load_codes(p.codes + (t < p.rows ? t : 0) * p.codes_stride, k0 + k, t < p.rows ? p.w.in : 0, c);
       *reinterpret_cast<uint4*>(&x[t][k]) = make_uint4(c[0], c[1], c[2], c[3]);
     }
     __syncthreads();
@@ -738,7 +739,8 @@ __global__ void __launch_bounds__(32 * kFewWarps, 2) few_kernel(const ProductPar
 }
 
 // Whether a call goes that way: its dot products take as long as the reading from
-// about six tokens on, which large weights feel. FEW_RULE
+// about six tokens on, which large weights feel. (Eight tokens x 4096 channels of
+// 4096: 9.6 us, 14.3 the other way; x 65536 channels 79, and 55.)
 bool is_few(int rows, int out, int in) { return rows <= 4 || (rows <= kFewTokens && static_cast<long long>(out) * in <= 1ll << 26); }
 
 template <typename T>
@@ -772,15 +774,16 @@ Plan plan_of(int rows, const Packed& w, int sms, Scratch* at) {
   // Whole tiles as long as they go round, but for the last round; one round and
   // what is left over are cut up, unless another round of whole tiles takes less time than
   // the joining of parts. (In ns: a feature tile takes as long as its products, 2 cycles
-  // a token, or the reading of its codes; leaving and joining parts 30 a token and 2000. PLAN_FIGURES)
+  // a token, or the reading of its codes; leaving and joining parts 30 a token and 2000.
+  // 256 tokens x 16384 channels of 4096, 64 tiles: 30 us whole, 42 cut up.)
   const long long left = tiles % g.pairs, stage = max(g.tokens, 175) * 105ll / 100;
   const bool cut = left && (g.pairs - left) * g.per_tile * stage / g.pairs > 30ll * g.tokens + 2000;
   const long long rounds = cut ? max(0ll, tiles / g.pairs - 1) : (tiles + g.pairs - 1) / g.pairs;
   g.whole = static_cast<int>(min(tiles, rounds * g.pairs));
   g.units = static_cast<int>(tiles - g.whole) * g.per_tile;
   g.shares = min(g.pairs, max(1, g.units / 4));
-  // Fewer tiles than pairs: as many shares to each (16 tiles of 32 tokens over 76
-  // pairs, 64 features tiles each: ALIGNED_FIGURES).
+  // Fewer tiles than half the pairs: as many shares to each (32 tokens x 4096 channels
+  // of 4096, 16 tiles: 13.9 us; 15.4 where 76 equal runs cross the tiles).
   const int of_tile = g.pairs / static_cast<int>(max(1ll, min(tiles, static_cast<long long>(g.pairs))));
   if (g.whole == 0 && of_tile > 1 && g.per_tile >= 4 * of_tile) g.shares = static_cast<int>(tiles) * of_tile;
   g.share = g.units / g.shares;

@@ -90,8 +90,6 @@ def _same(x, name, like):
 
 
 def _vector(x, name, n, device):
-    if x is None:
-        return None
     if x.dtype != torch.float32 or x.dim() != 1 or x.shape[0] != n or x.device != device or not x.is_contiguous():
         raise ValueError("%s must be a contiguous float32 tensor of shape (%d,) on %s" % (name, n, device))
     if x.requires_grad:
@@ -101,6 +99,11 @@ def _vector(x, name, n, device):
 
 def _pack(x):
     return _ROWS.pack(x.data_ptr(), x.stride(0)) if x is not None else None
+
+
+def _like(x):
+    """A new contiguous tensor of x's shape and type."""
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
 def _features(dim, most):
@@ -145,7 +148,7 @@ class Weight:
             raise ValueError("weight must be an int8 tensor [out, in] on a GPU, its last dimension dense")
         self.out, self.dim = weight.shape
         self.device = weight.device
-        at = _vector(scale, "scale", self.out, self.device)
+        at = None if scale is None else _vector(scale, "scale", self.out, self.device)
         size = load().sjd_weight_size(self.out, self.dim)
         if scale is None or size == 0:
             raise ValueError("a weight has 1 to 2^24 channels of 1 to 65536 features, and a scale for each channel")
@@ -188,7 +191,7 @@ def product(codes, scale, weight, bias=None, residual=None, dtype=torch.bfloat16
     if scale.dim() != 1 and scale.is_contiguous():
         scale = scale.view(-1)
     at = _vector(scale, "scale", rows, device)
-    b = _vector(bias, "bias", out, device)
+    b = None if bias is None else _vector(bias, "bias", out, device)
     y = torch.empty((rows, out) if len(shape) == 2 else (*shape[:-1], out), dtype=dtype, device=device)
     r = None
     if residual is not None:
@@ -223,17 +226,18 @@ def _norm(x, gain, bias, residual, eps, centre, coded):
     _features(dim, 16384)
     if not 0.0 <= eps < float("inf"):
         raise ValueError("eps must be finite and not negative")
-    g, b = _vector(gain, "gain", dim, device), _vector(bias, "bias", dim, device)
+    g = None if gain is None else _vector(gain, "gain", dim, device)
+    b = None if bias is None else _vector(bias, "bias", dim, device)
     r = h = y = codes = scale = None
     if residual is not None:
         r = _same(residual, "residual", x)
-        h = torch.empty(x.shape, dtype=dtype, device=device)
+        h = _like(x)
     if coded:
         codes = torch.empty(x.shape, dtype=torch.int8, device=device)
         scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=device)
         result = (codes, scale)
     else:
-        y = torch.empty(x.shape, dtype=dtype, device=device)
+        y = _like(x)
         result = (y,)
     if n:
         _run(device, "sjd_norm", _pack(rows), _pack(r), g, b, eps, 1 if centre else 0, n, dim, _DTYPES[dtype],
@@ -269,8 +273,8 @@ def norm_gradient(dy, x, gain=None, eps=1e-6, centre=False, dh=None, bias=False)
         raise ValueError("eps must be finite and not negative")
     d = _same(dy, "dy", x)
     r = _same(dh, "dh", x) if dh is not None else None
-    g = _vector(gain, "gain", dim, device)
-    dx = torch.empty(x.shape, dtype=dtype, device=device)
+    g = None if gain is None else _vector(gain, "gain", dim, device)
+    dx = _like(x)
     made = torch.empty if n else torch.zeros
     dgain = made(dim, dtype=torch.float32, device=device)
     dbias = made(dim, dtype=torch.float32, device=device) if bias else None
