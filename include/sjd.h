@@ -646,8 +646,10 @@ int sjd_weight_pack(const int8_t* w_dev, int64_t row_stride, const float* scale_
 /* y[t][n] = (sum_i codes[t][i] w[n][i]) scale[t] w_scale[n] + bias[n] +
  * residual[t][n], in this order, each step rounded to fp32; bias_dev and residual
  * may be NULL. The sum is exact (an integer, rounded once to fp32), so that a
- * row's result does not depend on the call's other rows. Should a wait inside the kernel run out, SJD_ERR_TIMEOUT
- * is latched in the packed weight (the results are then not valid). */
+ * row's result does not depend on the call's other rows. A call of a few rows
+ * needs no workspace (a size of 0, which invalid sizes have too): it may be NULL
+ * then. Should a wait inside the kernel run out, SJD_ERR_TIMEOUT is latched in the
+ * packed weight (the results are then not valid). */
 size_t sjd_product_workspace_size(int32_t rows, int32_t out, int32_t in);
 int sjd_product(const void* packed_dev, int32_t out, int32_t in, const sjd_rows* codes, const float* scale_dev,
                 int32_t rows, const float* bias_dev, const sjd_rows* residual, int32_t dtype, const sjd_rows* y,

@@ -67,11 +67,13 @@ int sjd_product(const void* packed, int32_t out, int32_t in, const sjd_rows* cod
                 const sjd_rows* residual, int32_t dtype, const sjd_rows* y, void* workspace, size_t ws_bytes, void* stream) {
   if (!packed || !aligned(packed, kAlign) || !valid_weight(out, in) || rows < 1 || !floating(dtype)) return SJD_ERR_ARG;
   if (!there(codes, 1) || !scale || !aligned(scale, 4) || !aligned(bias, 4) || !absent_or_there(residual, size_of(dtype)) ||
-      !there(y, size_of(dtype)) || !workspace || !aligned(workspace, kAlign))
+      !there(y, size_of(dtype)) || !aligned(workspace, kAlign))
     return SJD_ERR_ARG;
   int sms = 0;
   if (!count_sms(&sms)) return SJD_ERR_CUDA;
-  if (ws_bytes < product_scratch_bytes(rows, out, in, sms)) return SJD_ERR_CAPACITY;
+  const size_t needed = product_scratch_bytes(rows, out, in, sms);
+  if (needed && !workspace) return SJD_ERR_ARG;
+  if (ws_bytes < needed) return SJD_ERR_CAPACITY;
   ProductParams p{};
   packed_layout(out, in, const_cast<void*>(packed), &p.w);
   p.codes = static_cast<const int8_t*>(codes->data_dev);

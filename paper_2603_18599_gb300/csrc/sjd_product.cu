@@ -821,7 +821,7 @@ cudaError_t launch_pack(const int8_t* w, long long stride, const float* scale, c
 }
 
 size_t product_scratch_bytes(int rows, int out, int in, int sms) {
-  if (is_few(rows, out, in)) return 256;   // (not used)
+  if (is_few(rows, out, in)) return 0;
   Packed w;
   packed_layout(out, in, nullptr, &w);
   Scratch at;

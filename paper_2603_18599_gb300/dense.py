@@ -32,6 +32,9 @@ from .sjd import SJD_OK, SJDError
 
 _DTYPES = {torch.float32: sjd.SJD_F32, torch.bfloat16: sjd.SJD_BF16}
 _ROWS = struct.Struct("Qq")         # sjd_rows
+_INF = float("inf")
+
+_empty_like = torch.empty_like
 
 _lib = None
 
@@ -68,6 +71,9 @@ def _no_gradient(x, name):
 
 def _rows(x, name, dtypes, device=None):
     """x as [rows, features], its last dimension dense."""
+    # (most often all is as it should be: calls are short, and what the host does for one counts)
+    if x.dim() == 2 and x.dtype in dtypes and x.is_cuda and (device is None or x.device == device) and not x.requires_grad and x.stride(1) == 1:
+        return x
     if x.dtype not in dtypes or not x.is_cuda or (device is not None and x.device != device) or x.dim() < 1:
         raise ValueError("%s must be a tensor of %s on %s" % (name, " or ".join(str(d) for d in dtypes), device or "a GPU"))
     if x.requires_grad:
@@ -103,7 +109,7 @@ def _pack(x):
 
 def _like(x):
     """A new contiguous tensor of x's shape and type."""
-    return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    return _empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
 def _features(dim, most):
@@ -199,9 +205,9 @@ def product(codes, scale, weight, bias=None, residual=None, dtype=torch.bfloat16
     if rows == 0:
         return y
     size = _size(device.index, "sjd_product_workspace_size", rows, out, weight.dim)
-    workspace = torch.empty(size, dtype=torch.uint8, device=device)
+    workspace = torch.empty(size, dtype=torch.uint8, device=device) if size else None
     raw = _run(device, "sjd_product", weight._at, out, weight.dim, _pack(x), at, rows, b, _pack(r), _DTYPES[dtype],
-         _ROWS.pack(y.data_ptr(), out), workspace.data_ptr(), size)
+         _ROWS.pack(y.data_ptr(), out), workspace.data_ptr() if size else None, size)
     if raw not in weight._streams:
         weight._used_on(raw)
     return y
@@ -223,29 +229,29 @@ def _norm(x, gain, bias, residual, eps, centre, coded):
     rows = _rows(x, "x", _DTYPES)
     n, dim = rows.shape
     device, dtype = x.device, x.dtype
-    _features(dim, 16384)
-    if not 0.0 <= eps < float("inf"):
+    if not 1 <= dim <= 16384:
+        _features(dim, 16384)
+    if not 0.0 <= eps < _INF:
         raise ValueError("eps must be finite and not negative")
     g = None if gain is None else _vector(gain, "gain", dim, device)
     b = None if bias is None else _vector(bias, "bias", dim, device)
-    r = h = y = codes = scale = None
+    r = h = hw = yw = c_at = s_at = None
     if residual is not None:
-        r = _same(residual, "residual", x)
+        r = _pack(_same(residual, "residual", x))
         h = _like(x)
+        hw = _ROWS.pack(h.data_ptr(), dim)
     if coded:
         codes = torch.empty(x.shape, dtype=torch.int8, device=device)
-        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=device)
-        result = (codes, scale)
+        scale = torch.empty((n,) if x.dim() == 2 else x.shape[:-1], dtype=torch.float32, device=device)
+        c_at, s_at = codes.data_ptr(), scale.data_ptr()
     else:
         y = _like(x)
-        result = (y,)
+        yw = _ROWS.pack(y.data_ptr(), dim)
     if n:
-        _run(device, "sjd_norm", _pack(rows), _pack(r), g, b, eps, 1 if centre else 0, n, dim, _DTYPES[dtype],
-             _ROWS.pack(h.data_ptr(), dim) if h is not None else None, _ROWS.pack(y.data_ptr(), dim) if y is not None else None,
-             codes.data_ptr() if coded else None, scale.data_ptr() if coded else None)
-    if h is not None:
-        result += (h,)
-    return result if len(result) > 1 else result[0]
+        _run(device, "sjd_norm", _ROWS.pack(rows.data_ptr(), rows.stride(0)), r, g, b, eps, 1 if centre else 0, n, dim, _DTYPES[dtype], hw, yw, c_at, s_at)
+    if coded:
+        return (codes, scale) if h is None else (codes, scale, h)
+    return y if h is None else (y, h)
 
 
 def norm(x, gain=None, bias=None, residual=None, eps=1e-6, centre=False):

@@ -75,7 +75,7 @@ def test_bad_arguments_are_refused(lib):
     assert lib.sjd_embed_gradient(x, at, 2, 64, 10, 1.0, 0, at, at, lib.sjd_embed_gradient_workspace_size(2, 10) - 1, None) == 3
     refused("sjd_product", [at, 10, 64, x, at, 2, at, x, 1, x, at, 1 << 30, None],
             {0: (None, at + 128), 1: (*sizes, (1 << 24) + 1), 2: (*sizes, 65537), 3: (None, rows(0)), 4: (None, at + 2), 5: sizes, 6: (at + 2,),
-             7: (rows(0), rows(at + 1)), 8: (2,), 9: (None, rows(at + 1)), 10: (None, at + 128)})
+             7: (rows(0), rows(at + 1)), 8: (2,), 9: (None, rows(at + 1)), 10: (at + 128,)})
     assert lib.sjd_weight_sync(None, None) == lib.sjd_weight_sync(at + 8, None) == arg
 
 

@@ -542,3 +542,15 @@ def test_refusals():
             pytest.fail("call %d was taken" % i)
     with torch.no_grad():
         assert torch.equal(dense.norm(wants), dense.norm(wants.detach()))
+    # what the binding sees to itself: a workspace, and one that is large enough
+    L = dense.load()
+    codes, y = codes_of(g, 20, 64), torch.empty(20, 32, dtype=BF16, device=DEV)
+    size, room = L.sjd_product_workspace_size(20, 32, 64), torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    assert size > 0 and L.sjd_product_workspace_size(2, 32, 64) == 0
+    args = [weight._at, 32, 64, dense._pack(codes), v.data_ptr(), 20, None, None, sjd.SJD_BF16, dense._pack(y), None, size, None]
+    assert L.sjd_product(*args) == sjd.SJD_ERR_ARG
+    args[10:12] = room.data_ptr(), size - 1
+    assert L.sjd_product(*args) == sjd.SJD_ERR_CAPACITY
+    size = L.sjd_norm_gradient_workspace_size(4, 64, sjd.SJD_F32)
+    assert L.sjd_norm_gradient(dense._pack(x), dense._pack(x), None, 1e-6, 0, None, 4, 64, sjd.SJD_F32, dense._pack(x.clone()), v.data_ptr(), None,
+                               room.data_ptr(), size - 1, None) == sjd.SJD_ERR_CAPACITY
