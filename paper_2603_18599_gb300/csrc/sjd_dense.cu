@@ -1135,16 +1135,17 @@ __global__ void __launch_bounds__(kSumBlock, 8) embed_gradient_kernel(const Embe
 }
 
 template <typename T>
-cudaError_t embed_gradient_of(const EmbedGradientParams& p, cudaStream_t s) {
+cudaError_t embed_gradient_of(const EmbedGradientParams& p, int sms, cudaStream_t s) {
   const int lists = embed_gradient_lists(p.vocab);
   cudaError_t e = launch_early(index_kernel, static_cast<unsigned>(lists), 32 * kIndexWarps, 0, s, p);
   if (e != cudaSuccess) return e;
   const bool w = p.dim % 4 == 0 && reinterpret_cast<uintptr_t>(p.grad) % 16 == 0 && reinterpret_cast<uintptr_t>(p.dy.p) % (4 * sizeof(T)) == 0 &&
                  (p.rows < 2 || p.dy.stride % 4 == 0);
-  const int ids = max(1, min(256, 16384 / p.dim)), slices = (p.dim + kSumColumns - 1) / kSumColumns, groups = min(lists, kGroups),
-            shares = max(1, min(64, 1024 / (slices * groups)));
   int lanes = 8;
   while (lanes < kSumBlock && lanes * (w ? 4 : 1) < p.dim) lanes *= 2;
+  // (64 KB to a block, or less where that leaves fewer than eight blocks to an SM)
+  const int ids = max(kSumBlock / lanes, min(min(256, 16384 / p.dim), p.vocab / (8 * sms))), slices = (p.dim + kSumColumns - 1) / kSumColumns,
+            groups = min(lists, kGroups), shares = max(1, min(min(64, 1024 / (slices * groups)), p.rows / (p.few * kSumBlock / 32 * groups) + 1));
   const unsigned blocks = static_cast<unsigned>((static_cast<long long>(p.vocab) + ids - 1) / ids);
   const bool many = p.rows > p.few;   // (some id may have so many)
   if (many) {
@@ -1184,8 +1185,8 @@ cudaError_t launch_embed(const EmbedParams& p, int table_dtype, int dtype, cudaS
   return dtype == SJD_BF16 ? embed_of<float, __nv_bfloat16>(p, s) : embed_of<float, float>(p, s);
 }
 
-cudaError_t launch_embed_gradient(const EmbedGradientParams& p, int dtype, cudaStream_t s) {
-  return dtype == SJD_BF16 ? embed_gradient_of<__nv_bfloat16>(p, s) : embed_gradient_of<float>(p, s);
+cudaError_t launch_embed_gradient(const EmbedGradientParams& p, int dtype, int sms, cudaStream_t s) {
+  return dtype == SJD_BF16 ? embed_gradient_of<__nv_bfloat16>(p, sms, s) : embed_gradient_of<float>(p, sms, s);
 }
 
 }  // namespace sjd_dense_ops

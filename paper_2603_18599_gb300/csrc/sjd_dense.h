@@ -110,7 +110,7 @@ cudaError_t launch_norm_gradient(const NormGradientParams& p, int dtype, cudaStr
 cudaError_t launch_embed(const EmbedParams& p, int table_dtype, int dtype, cudaStream_t s);
 constexpr int kListIds = 256;  // ids of a list
 int embed_gradient_lists(int vocab);
-cudaError_t launch_embed_gradient(const EmbedGradientParams& p, int dtype, cudaStream_t s);
+cudaError_t launch_embed_gradient(const EmbedGradientParams& p, int dtype, int sms, cudaStream_t s);
 cudaError_t launch_pack(const int8_t* w, long long stride, const float* scale, const Packed& to, cudaStream_t s);
 size_t product_scratch_bytes(int rows, int out, int in, int sms);
 cudaError_t launch_product(const ProductParams& p, int dtype, int sms, unsigned char* scratch, cudaStream_t s);

@@ -156,7 +156,9 @@ int sjd_embed_gradient(const sjd_rows* dy, const int32_t* tokens, int32_t rows, 
   int4* many = static_cast<int4*>(workspace);
   int32_t* first = reinterpret_cast<int32_t*>(many + static_cast<size_t>(embed_gradient_lists(vocab)) * (1 + kListIds));
   const EmbedGradientParams p{rows_of(dy), tokens, grad, first, first + vocab + 1ll, many, scale, rows, dim, vocab, rows <= 32 ? 32 : 8};
-  return launched(launch_embed_gradient(p, dtype, static_cast<cudaStream_t>(stream)));
+  int sms = 0;
+  if (!count_sms(&sms)) return SJD_ERR_CUDA;
+  return launched(launch_embed_gradient(p, dtype, sms, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

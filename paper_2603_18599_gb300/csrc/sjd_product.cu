@@ -24,6 +24,7 @@
 // us, 300 MB; a copy of the kernel without conversion and products takes 58.
 
 #include <atomic>
+#include <cmath>
 
 #include <cuda_fp16.h>
 
@@ -784,8 +785,13 @@ Plan plan_of(int rows, const Packed& w, int sms, Scratch* at) {
   g.shares = min(g.pairs, max(1, g.units / 4));
   // Fewer tiles than half the pairs: as many shares to each (32 tokens x 4096 channels
   // of 4096, 16 tiles: 13.9 us; 15.4 where 76 equal runs cross the tiles).
-  const int of_tile = g.pairs / static_cast<int>(max(1ll, min(tiles, static_cast<long long>(g.pairs))));
-  if (g.whole == 0 && of_tile > 1 && g.per_tile >= 4 * of_tile) g.shares = static_cast<int>(tiles) * of_tile;
+  // Not more than their joining, 15 ns a token and part, is worth (408 tokens x 32 channels
+  // of 8192: 39 us, 87 where each of
+  // three tiles has 25 parts).
+  if (g.whole == 0 && 2 * tiles <= g.pairs) {
+    const int worth = static_cast<int>(std::lround(std::sqrt(static_cast<double>(g.per_tile) * stage / (15.0 * g.tokens))));
+    g.shares = static_cast<int>(tiles) * max(1, min(min(worth, g.pairs / static_cast<int>(tiles)), g.per_tile / 4));
+  }
   g.share = g.units / g.shares;
   g.longer = g.units % g.shares;
   at->squares = 4096;
