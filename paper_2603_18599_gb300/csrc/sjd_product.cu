@@ -262,8 +262,9 @@ __device__ __forceinline__ void halves_of(uint32_t codes, uint32_t& lo, uint32_t
 }
 
 // Warps 0 to 3 take every other tile, warps 4 to 7 those between; a lane a
-// channel. The next tile's codes are loaded while this one's fp16 is on its way
-// into tensor memory.
+// channel. A tile's fp16 is on its way into tensor memory while the next one's codes are
+// loaded and converted, and is announced after that (or at once, where the next
+// codes are not there yet).
 __device__ __forceinline__ void convert(Misc* m, const Plan& g, int pair, int warp, uint32_t codes_at, uint32_t tmem) {
   const int lane = threadIdx.x & 31, channel = (warp & 3) * 32 + lane, turn = warp / 4;
   const uint32_t full0 = cluster_addr(smem_addr(&m->full[0]), 0), stages_at = tmem + g.accumulators * g.sum_columns + (static_cast<uint32_t>((warp & 3) * 32) << 16);
@@ -280,10 +281,21 @@ __device__ __forceinline__ void convert(Misc* m, const Plan& g, int pair, int wa
   if (turn) c.step(g.codes_ring), s.step(g.stages), x.step(g.x_ring);
   uint4 u[4];
   auto load = [&]() {
-    wait(m, &m->codes_full[c.i], c.phase);
 #pragma unroll
     for (int i = 0; i < 4; ++i) u[i] = shared_load16(row + c.i * kTileBytes + ((i << 4) ^ swap));
   };
+  int stage = -1;   // that is to be announced
+  auto announce = [&]() {
+    tmem_wait_store();
+    // (one warp's arrival tells of this block's tokens too)
+    if ((warp & 3) == 0) wait(m, &m->x_full[x.i], x.phase);
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive_cluster(full0 + stage * 8);
+    stage = -1;
+    x.step(g.x_ring), x.step(g.x_ring);
+  };
+  wait(m, &m->codes_full[c.i], c.phase);
   load();
   for (;;) {
     uint32_t v[32];
@@ -294,26 +306,24 @@ __device__ __forceinline__ void convert(Misc* m, const Plan& g, int pair, int wa
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_addr(&m->codes_empty[c.i]));
+    if (stage >= 0) announce();
     wait(m, &m->empty[s.i], s.phase ^ 1);
     tc_fence_after();
     __syncwarp();
     tmem_store32(stages_at + s.i * kStageColumns, v);
+    stage = s.i;
     left -= 2;
-    if (left > 0) {
-      c.step(g.codes_ring), c.step(g.codes_ring);
-      load();
-    }
-    __syncwarp();
-    tmem_wait_store();
-    // (one warp's arrival tells of this block's tokens too)
-    if ((warp & 3) == 0) wait(m, &m->x_full[x.i], x.phase);
-    tc_fence_before();
-    __syncwarp();
-    if (lane == 0) mbar_arrive_cluster(full0 + s.i * 8);
-    if (left <= 0) return;
+    if (left <= 0) break;
     s.step(g.stages), s.step(g.stages);
-    x.step(g.x_ring), x.step(g.x_ring);
+    c.step(g.codes_ring), c.step(g.codes_ring);
+    if (!__all_sync(0xffffffffu, mbar_test(smem_addr(&m->codes_full[c.i]), c.phase))) {
+      announce();
+      wait(m, &m->codes_full[c.i], c.phase);
+    }
+    load();
+    __syncwarp();
   }
+  announce();
 }
 
 // The products of both blocks (one warp of block 0).
