@@ -19,10 +19,11 @@
 // once in bytes, which bounds calls of few tokens, and its conversion, four
 // instructions for four codes, goes on beside the products, which bound those of many. Up to
 // 192 tokens have two accumulators: a tile's results are given while the next one is summed
-// up (8100 tokens x 16384 channels of 4096: 567 to 590 us, 1.84 to 1.92 PFLOP/s, as much as
-// a library product of bf16; 844 with one accumulator of 256 tokens). 128 tokens x 65536 channels, f32: 63
-// us, 300 MB; a copy of the kernel without conversion and products takes 58.
+// up (8100 tokens x 16384 channels of 4096: 558 to 562 us, 1.94 PFLOP/s, as much as
+// a library product of bf16; 844 with one accumulator of 256 tokens). 128 tokens x 65536 channels, f32: 62
+// us, 300 MB; a copy of the kernel without conversion and products took 58 where this one took 64.
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 
@@ -768,40 +769,67 @@ struct Scratch {
   size_t squares, x, slots, bytes;   // (the counters are at the beginning)
 };
 
+// How a call is shared out is chosen by the time that it is expected to take, in
+// ns. A feature tile takes as long as its products and their share of the rest, 1.22 a token,
+// or its conversion, 225; all tiles no less than the weight takes from memory
+// (6.5 bytes) or, once for each tile of tokens, from L2 (10); a tile's results 12 a token; leaving
+// parts 15 a token, joining them 15 a token and part, and 2000.
+// - Tiles of tokens: the fewest, or smaller ones, whose whole tiles fill the pairs
+//   (1337 tokens x 512 channels of 4096: 24 us, 27 in tiles of 192; 408 x 32 of 8192: 30, 39).
+// - Whole tiles go round the pairs. Or one round and what is left over are cut into equal runs (256 tokens x
+//   16384 channels of 4096, 64 tiles: 30 us whole, 42 cut up). Or, of fewer tiles than half the pairs, each
+//   into as many parts as their joining is worth (32 tokens x 4096 channels of 4096, 16 tiles: 13.5 us; 15.4
+//   in 76 equal runs that cross the tiles; 408 x 32 of 8192: 39 us, 87 in 25 parts each).
+struct Way {
+  double ns;
+  int token_tiles, tokens;
+  bool cut;
+  int parts;   // of a tile, or 0: equal runs
+};
+Way way_of(int rows, const Packed& w, int pairs) {
+  Way best{};
+  const double weight = static_cast<double>(w.tiles_out) * w.tiles_in * kTileBytes;
+  const int most = rows <= kMostTokens ? kMostTokens : kTwoSums;
+  long long n = (static_cast<long long>(rows) + most - 1) / most;
+  for (;;) {
+    const int tokens = static_cast<int>((rows + n - 1) / n + 15) / 16 * 16;
+    n = (static_cast<long long>(rows) + tokens - 1) / tokens;
+    const long long tiles = n * (w.tiles_out / 2), rounds = (tiles + pairs - 1) / pairs;
+    const double stage = std::fmax(1.22 * tokens, 225.0), flow = std::fmax(weight / 6500.0, n * weight / 10000.0), results = 12.0 * tokens;
+    auto offer = [&](double ns, bool cut, int parts) {
+      if (best.token_tiles == 0 || ns < best.ns) best = {ns, static_cast<int>(n), tokens, cut, parts};
+    };
+    offer(std::fmax(rounds * w.tiles_in * stage, flow) + (tokens > kTwoSums ? rounds : 1) * results, false, 0);
+    if (2 * tiles <= pairs) {
+      const int worth = static_cast<int>(std::lround(std::sqrt(w.tiles_in * stage / (15.0 * tokens))));
+      const int parts = std::min({worth, pairs / static_cast<int>(tiles), w.tiles_in / 4});
+      if (parts > 1) offer(std::fmax(w.tiles_in * stage / parts, flow) + 15.0 * (parts + 1) * tokens + 2000.0 + results, true, parts);
+    } else if (tiles % pairs && w.tiles_in >= 8) {
+      offer(std::fmax(tiles * w.tiles_in * stage / pairs, flow) + 30.0 * tokens + 2000.0 + results, true, 0);
+    }
+    if (tokens <= 16 || tiles > 4ll * pairs) return best;
+    n = (static_cast<long long>(rows) + tokens - 17) / (tokens - 16);
+  }
+}
+
 Plan plan_of(int rows, const Packed& w, int sms, Scratch* at) {
   Plan g{};
   g.pairs = min(sms / 2, kMaxPairs);
   g.channel_tiles = w.tiles_out / 2;
   g.per_tile = w.tiles_in;
-  const int most = rows <= kMostTokens ? kMostTokens : kTwoSums;
-  g.token_tiles = static_cast<int>((static_cast<long long>(rows) + most - 1) / most);
-  g.tokens = ((rows + g.token_tiles - 1) / g.token_tiles + 15) / 16 * 16;
+  const Way way = way_of(rows, w, g.pairs);
+  g.token_tiles = way.token_tiles;
+  g.tokens = way.tokens;
   g.accumulators = g.tokens <= kTwoSums ? 2 : 1;
   g.sum_columns = (g.tokens + 31) / 32 * 32;
   g.stages = min(kStages, (kTmemColumns - g.accumulators * g.sum_columns) / kStageColumns);
   g.x_ring = kStages;
   g.codes_ring = min(kMostCodes, static_cast<int>(((rows <= 2 * g.pairs ? kRingsBeside : kRings) - g.x_ring * g.tokens * kTileIn) / kTileBytes));
   const long long tiles = static_cast<long long>(g.channel_tiles) * g.token_tiles;
-  // Whole tiles as long as they go round, but for the last round; one round and
-  // what is left over are cut up, unless another round of whole tiles takes less time than
-  // the joining of parts. (In ns: a feature tile takes as long as its products, 2 cycles
-  // a token, or the reading of its codes; leaving and joining parts 30 a token and 2000.
-  // 256 tokens x 16384 channels of 4096, 64 tiles: 30 us whole, 42 cut up.)
-  const long long left = tiles % g.pairs, stage = max(g.tokens, 175) * 105ll / 100;
-  const bool cut = left && (g.pairs - left) * g.per_tile * stage / g.pairs > 30ll * g.tokens + 2000;
-  const long long rounds = cut ? max(0ll, tiles / g.pairs - 1) : (tiles + g.pairs - 1) / g.pairs;
+  const long long rounds = way.cut ? max(0ll, tiles / g.pairs - 1) : (tiles + g.pairs - 1) / g.pairs;
   g.whole = static_cast<int>(min(tiles, rounds * g.pairs));
   g.units = static_cast<int>(tiles - g.whole) * g.per_tile;
-  g.shares = min(g.pairs, max(1, g.units / 4));
-  // Fewer tiles than half the pairs: as many shares to each (32 tokens x 4096 channels
-  // of 4096, 16 tiles: 13.9 us; 15.4 where 76 equal runs cross the tiles).
-  // Not more than their joining, 15 ns a token and part, is worth (408 tokens x 32 channels
-  // of 8192: 39 us, 87 where each of
-  // three tiles has 25 parts).
-  if (g.whole == 0 && 2 * tiles <= g.pairs) {
-    const int worth = static_cast<int>(std::lround(std::sqrt(static_cast<double>(g.per_tile) * stage / (15.0 * g.tokens))));
-    g.shares = static_cast<int>(tiles) * max(1, min(min(worth, g.pairs / static_cast<int>(tiles)), g.per_tile / 4));
-  }
+  g.shares = way.parts ? static_cast<int>(tiles) * way.parts : min(g.pairs, max(1, g.units / 4));
   g.share = g.units / g.shares;
   g.longer = g.units % g.shares;
   at->squares = 4096;
