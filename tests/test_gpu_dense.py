@@ -351,7 +351,8 @@ def test_norm_gradient_against_differences(centre):
         down = loss(x.double() - e * vx, w.double() - e * vw, b.double() - e * vb)
         along = (dx.double() * vx).sum() + (dgain.double() * vw).sum() + (dbias.double() * vb).sum()
         # (sums of 700 products, each off by 2^-16, and the differences' 1e-8 of a third derivative below 100 a row)
-        assert abs((up - down) / (2 * e) - along) <= 2.0 ** -16 * ((dx.double() * vx).abs().sum() + (dgain.double() * vw).abs().sum() + (dbias.double() * vb).abs().sum()) + 1e-6 * t * 100
+        terms = (dx.double() * vx).abs().sum() + (dgain.double() * vw).abs().sum() + (dbias.double() * vb).abs().sum()
+        assert abs((up - down) / (2 * e) - along) <= 2.0 ** -16 * terms + 1e-6 * t * 100
 
 
 # --- embedding ------------------------------------------------------------------
@@ -417,6 +418,46 @@ def test_offsets_past_32_bits_in_an_embedding():
     del y
     grad = dense.embed_gradient(E[-3:], tokens[-3:], v)
     assert torch.equal(grad[-1], E[-1].float()) and torch.equal(grad[-2], E[-3].float() + E[-2].float())
+
+
+# --- shapes and strides that documents allow and callers seldom use -------------------
+
+@pytest.mark.parametrize("d", [64, 100, 1600, 4096])
+def test_rows_that_repeat_single_rows_and_vectors_off_boundaries(d):
+    """Rows of stride 0 (a broadcast), one row without a dimension for it, and
+    gains, biases and scales that do not start on 16-byte boundaries: the same bits as
+    from contiguous copies (whose sums are taken in the same order where the ways
+    are the same; else within the norm's bound)."""
+    g = gen(d)
+    row, dy = normal(g, 1, d).bfloat16(), normal(g, 1, d).bfloat16()
+    many, dys = row.expand(7, d), dy.expand(7, d)
+    ids = torch.arange(7, device=DEV).int() // 3
+    for a, b in ((dense.norm(many), dense.norm(many.contiguous())), (dense.quantise(many)[0], dense.quantise(many.contiguous())[0]),
+                 *zip(dense.norm_gradient(dys, many, bias=True), dense.norm_gradient(dys.contiguous(), many.contiguous(), bias=True)),
+                 (dense.embed_gradient(dys, ids, 4), dense.embed_gradient(dys.contiguous(), ids, 4))):
+        assert torch.equal(a, b)
+    assert torch.equal(dense.norm(row[0]), dense.norm(row)[0])
+    E, token = normal(g, 5, d), torch.tensor(3, dtype=torch.int32, device=DEV)
+    assert torch.equal(dense.embed(E, token), E[3])
+    assert torch.equal(dense.embed_gradient(E[1], token, 5)[3], E[1])
+    held = normal(g, 3, d + 1)
+    w, b = held[0, 1:], held[1, 1:]
+    x = normal(g, 40, d)
+    for centre in (False, True):
+        want, _, _, size = plain_norm(x, w, b, 1e-6, centre)
+        assert ((dense.norm(x, w, b, centre=centre).double() - want).abs() <= SUM * size + want.abs() * 2.0 ** -24).all()
+        dx, dg, db, size, gsize, bsize = plain_norm_gradient(x, x, w, 1e-6, centre, None)
+        got = dense.norm_gradient(x, x, w, 1e-6, centre, bias=True)
+        assert ((got[0].double() - dx).abs() <= 2.5 * SUM * size * 1.01 + dx.abs() * 2.0 ** -24).all()
+        assert ((got[1].double() - dg).abs() <= (ROWS_OF_A_BLOCK + 128) * 2.0 ** -24 * gsize).all()
+    codes, weight = codes_of(g, 41, d), codes_of(g, 72, d)
+    scale, sw, bias = held[2, :1].abs().expand(41).contiguous(), normal(g, 73)[1:].abs(), normal(g, 73)[1:]
+    for n in (1, 3, 7, 41):
+        got = dense.product(codes[:n], scale[:n], dense.Weight(weight, sw), bias=bias, dtype=F32)
+        assert torch.equal(got, plain_product(codes[:n], scale[:n], weight, sw, bias, None, F32))
+    repeated = codes[:1].expand(30, d)
+    assert torch.equal(dense.product(repeated, scale[:30], dense.Weight(weight, sw), dtype=F32),
+                       plain_product(repeated, scale[:30], weight, sw, None, None, F32))
 
 
 # --- streams, graphs, refusals -----------------------------------------------------
