@@ -88,7 +88,6 @@ constexpr int kTmemColumns = 512;
 constexpr int kMostCodes = 24, kStages = 8;     // most tiles on their way: codes, tokens and codes in fp16
 constexpr uint32_t kRings = 222 * 1024;         // bytes of shared memory for them; in a call of few tokens less, which lets a block of
 constexpr uint32_t kRingsBeside = 216 * 1024;   // the spreading kernel stay on the SM while this kernel's starts
-constexpr int kSlots = 3;                       // what a block leaves of up to two tiles that others have a part in, and the sum of a tile's parts
 constexpr int kMaxPairs = 80;
 constexpr int kConvert = 4, kResults = 12;       // the first warps that convert codes, that give results: eight each
 constexpr int kThreads = 640;
@@ -104,6 +103,8 @@ struct Plan {
   int accumulators, sum_columns;                    // columns from one accumulator to the next
   int whole, shares, units;                         // shares: pairs that the rest is cut up for
   int share, longer;                                // units of a share; shares that have one more
+  int block_slots, sum_slot;                        // what a block may leave: of up to two tiles that others have a part in, where tiles are
+                                                    // cut up; the sum so far of a tile's parts, where there may be such
   const unsigned char* x;                           // the tokens' codes in fp16
   const uint32_t* squares;                          // of each token's codes
   int32_t* slots;
@@ -424,7 +425,7 @@ __device__ __forceinline__ void join(const ProductParams& p, const Plan& g, cons
 #pragma unroll 2
     for (int other = first; other < after; ++other) {
       const int slot = share_begin(g, other) >= begin ? 0 : 1;
-      const int32_t* from = g.slots + ((2ll * other + rank) * kSlots + slot) * slot_size + 4 * lane;
+      const int32_t* from = g.slots + ((2ll * other + rank) * g.block_slots + slot) * slot_size + 4 * lane;
       int4 v[kDeep];
 #pragma unroll
       for (int j = 0; j < kDeep; ++j) v[j] = __ldcg(reinterpret_cast<const int4*>(from + min(c0 + 8 * j, tokens - 1) * kTileOut));
@@ -478,7 +479,7 @@ __device__ __forceinline__ void results(const ProductParams& p, Misc* m, const P
   const int lane = threadIdx.x & 31, row = (warp & 3) * 32 + lane;
   const uint32_t empty0 = cluster_addr(smem_addr(&m->sum_empty[0]), 0), sums_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
   const long long slot_size = static_cast<long long>(g.sum_columns) * kTileOut;
-  auto slot_of = [&](int of, int slot) { return g.slots + ((2ll * of + rank) * kSlots + slot) * slot_size; };
+  auto slot_of = [&](int of, int slot) { return g.slots + ((2ll * of + rank) * g.block_slots + slot) * slot_size; };
   int shared = 0;
   Ring d, r;
   Walk walk(g, pair);
@@ -508,7 +509,7 @@ __device__ __forceinline__ void results(const ProductParams& p, Misc* m, const P
         ++shared;
       }
       // (the sum of the parts so far; what is left for the pair that joins the tile)
-      int32_t* const sum = slot_of(pair, 2) + row;
+      int32_t* const sum = slot_of(pair, g.sum_slot) + row;
       int32_t* const to = last ? slot_of(pair, share_begin(g, pair) >= begin ? 0 : 1) + row : sum;
       const int c0 = warp / 4 * kColumns;
       uint32_t u[kColumns];
@@ -830,13 +831,15 @@ Plan plan_of(int rows, const Packed& w, int sms, Scratch* at) {
   g.whole = static_cast<int>(min(tiles, rounds * g.pairs));
   g.units = static_cast<int>(tiles - g.whole) * g.per_tile;
   g.shares = way.parts ? static_cast<int>(tiles) * way.parts : min(g.pairs, max(1, g.units / 4));
+  g.sum_slot = g.units ? 2 : 0;
+  g.block_slots = g.sum_slot + (g.per_tile > kPart ? 1 : 0);
   g.share = g.units / g.shares;
   g.longer = g.units % g.shares;
   at->squares = 4096;
   static_assert(4 * kMaxPairs * sizeof(int32_t) <= 4096, "counters");
   at->x = at->squares + (static_cast<size_t>(rows) * sizeof(uint32_t) + 255) / 256 * 256;
   at->slots = at->x + static_cast<size_t>(g.token_tiles) * g.tokens * g.per_tile * kTileIn * sizeof(__half);
-  at->bytes = at->slots + 2 * static_cast<size_t>(g.pairs) * kSlots * g.sum_columns * kTileOut * sizeof(int32_t);
+  at->bytes = at->slots + 2 * static_cast<size_t>(g.pairs) * g.block_slots * g.sum_columns * kTileOut * sizeof(int32_t);
   return g;
 }
 
