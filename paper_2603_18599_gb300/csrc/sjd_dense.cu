@@ -993,6 +993,20 @@ __device__ __forceinline__ void load_columns(const T* p, float (&x)[W ? 4 : 1]) 
   if constexpr (W) sjd_kv_ops::load4(p, true, x);
   else x[0] = static_cast<float>(*p);
 }
+// The same past the first-level cache.
+template <bool W, typename T>
+__device__ __forceinline__ void load_columns_l2(const T* p, float (&x)[W ? 4 : 1]) {
+  if constexpr (!W) {
+    x[0] = static_cast<float>(__ldcg(p));
+  } else if constexpr (sizeof(T) == 2) {
+    const uint2 v = __ldcg(reinterpret_cast<const uint2*>(p));
+    const float2 a = unpack_bf16(v.x), b = unpack_bf16(v.y);
+    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+  } else {
+    const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
+    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+  }
+}
 
 // grad[v] = scale sum of dy over the rows of v, in their order.
 //
@@ -1091,7 +1105,13 @@ __global__ void __launch_bounds__(kSumBlock, 2) embed_gradient_many_kernel(const
 //
 // `early`: the kernel before this one on the stream is the one above, which writes other
 // rows, and let this one in after the index was done: this one waits for it at its end, not
-// at its beginning, so that the two run together.
+// at its beginning, so that the two run together. Its own wait has then not yet made
+// what the index and the caller's kernels wrote visible to it, but the wait of the kernel
+// above, which every block of that one has passed before the first block of this one starts, comes
+// after those kernels' ends, when their writes stand in global memory. What this
+// one must not do is find older values of those addresses in the first-level cache, which
+// the other kernels' blocks on the SM share: it loads all of them (index, places and
+// rows) past it, from L2.
 template <typename T, bool W>
 __global__ void __launch_bounds__(kSumBlock, 8) embed_gradient_kernel(const EmbedGradientParams p, int ids, int lanes, bool early) {
   constexpr int V = W ? 4 : 1;
@@ -1101,11 +1121,11 @@ __global__ void __launch_bounds__(kSumBlock, 8) embed_gradient_kernel(const Embe
     let_next_start();
   }
   const int D = p.dim, v0 = blockIdx.x * ids, here = min(ids, p.vocab - v0);
-  for (int i = threadIdx.x; i <= here; i += kSumBlock) first[i] = p.first[v0 + i];
+  for (int i = threadIdx.x; i <= here; i += kSumBlock) first[i] = __ldcg(p.first + v0 + i);
   __syncthreads();
   const int base = first[0], lane = threadIdx.x & (lanes - 1);
   if (first[here] > base) {
-    for (int i = threadIdx.x; i < min(kPlaces, first[here] - base); i += kSumBlock) places[i] = p.places[base + i];
+    for (int i = threadIdx.x; i < min(kPlaces, first[here] - base); i += kSumBlock) places[i] = __ldcg(p.places + base + i);
     __syncthreads();
   }
   // `lanes` threads (a power of two) to an id
@@ -1118,7 +1138,7 @@ __global__ void __launch_bounds__(kSumBlock, 8) embed_gradient_kernel(const Embe
       for (int r = 0; r < count; ++r) {
         const int at = from + r;
         float x[V];
-        load_columns<W>(row_of<T>(p, at < kPlaces ? places[at] : p.places[base + at]) + column, x);
+        load_columns_l2<W>(row_of<T>(p, at < kPlaces ? places[at] : __ldcg(p.places + base + at)) + column, x);
 #pragma unroll
         for (int j = 0; j < V; ++j) sum[j] += x[j];
       }
