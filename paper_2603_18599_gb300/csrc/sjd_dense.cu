@@ -16,6 +16,7 @@
 #include <cfloat>
 
 #include "sjd_dense.h"
+#include "sjd_dense_rows.cuh"
 #include "sjd_kv_device.cuh"
 #include "sjd_tcgen05.cuh"
 
@@ -34,27 +35,6 @@ using sjd_kv_ops::unpack_bf16;
 using sjd_kv_ops::wait_for_previous;
 
 namespace {
-
-// A thread's features of a row: pieces of 8 neighbours, `step` apart, where a row
-// can be accessed 16 bytes at a time (`W`). Else a warp's pieces follow one
-// another and a piece's features lie 32 apart, so that a warp's accesses of single elements are side by
-// side, at distances that are known beforehand.
-struct Place {
-  int first, step;
-};
-template <bool W>
-__device__ __forceinline__ Place place_of(int lane, int G, int pieces) {
-  return W ? Place{8 * lane, 8 * G} : Place{lane / 32 * 256 * pieces + lane % 32, 256};
-}
-// Feature j of piece i; whether it is one of the row's.
-template <bool W>
-__device__ __forceinline__ int feature(int i, int j, Place at) {
-  return W ? at.first + i * at.step + j : at.first + i * 256 + j * 32;
-}
-template <bool W>
-__device__ __forceinline__ bool is_there(int i, int j, Place at, int D) {
-  return W ? feature<true>(i, 0, at) < D : i * 256 + j * 32 < D - at.first;   // (pieces are there as a whole, or not)
-}
 
 // (Wide loads behind the row's end take its last piece instead, and `FILL` puts zeros in its
 // place: a select costs less than a branch around the load.)
@@ -868,12 +848,15 @@ __global__ void __launch_bounds__(kEmbedBlock) embed_kernel(const EmbedParams p,
   const bool inside = token >= 0 && token < p.vocab;
   const E* x = static_cast<const E*>(p.table.p) + (inside ? token : 0) * p.table.stride;
   T* y = static_cast<T*>(p.y.p) + row * p.y.stride;
-  const Place at = place_of<W>(lane, G, (D + 8 * G - 1) / (8 * G));
-  for (int i0 = 0; i0 * 8 * G < D; i0 += kDeep) {
+  const int pieces = pieces_of(D, G);
+  const Place at = place_of<W>(lane, G, pieces);
+  for (int i0 = 0; i0 < pieces; i0 += kDeep) {
     float v[kDeep][8] = {};
     if (inside) {
 #pragma unroll
-      for (int i = 0; i < kDeep; ++i) load8<W>(x, i0 + i, at, D, v[i]);
+      for (int i = 0; i < kDeep; ++i) {
+        if (is_mine<W>(i0 + i, pieces)) load8<W>(x, i0 + i, at, D, v[i]);
+      }
 #pragma unroll
       for (int i = 0; i < kDeep; ++i) {
 #pragma unroll
@@ -881,7 +864,9 @@ __global__ void __launch_bounds__(kEmbedBlock) embed_kernel(const EmbedParams p,
       }
     }
 #pragma unroll
-    for (int i = 0; i < kDeep; ++i) store8<W>(y, i0 + i, at, D, v[i]);
+    for (int i = 0; i < kDeep; ++i) {
+      if (is_mine<W>(i0 + i, pieces)) store8<W>(y, i0 + i, at, D, v[i]);
+    }
   }
 }
 
