@@ -514,15 +514,12 @@ Flow flow_of(int threads, int registers, size_t row) {
   f.shared = f.deep * row;
   return f;
 }
-template <typename Kernel>
-cudaError_t allow_shared(Kernel kernel, size_t bytes) {
-  // (with what a kernel has beside it, 48 KB need no leave)
-  return bytes <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
-}
+constexpr int kMostShared = 200 * 1024;   // dynamic shared memory of any call's block
+static_assert(2 * sizeof(float) * kMaxFeatures <= kMostShared, "the columns' sums of the longest rows");
 
 template <typename T, int MODE>
 cudaError_t norm_ahead(const NormParams& p, int sms, const Flow& f, cudaStream_t s) {
-  const cudaError_t e = allow_shared(norm_ahead_kernel<T, MODE>, f.shared);
+  const cudaError_t e = allow_shared<norm_ahead_kernel<T, MODE>>(kMostShared);
   if (e != cudaSuccess) return e;
   return launch_early(norm_ahead_kernel<T, MODE>, static_cast<unsigned>(min(p.rows, sms * f.per_sm)), threads_of(p.dim, 2), f.shared, s, p,
                       threads_of(p.dim, 2), f.deep);
@@ -538,7 +535,7 @@ cudaError_t norm_by(const NormParams& p, int sms, cudaStream_t s) {
   if (d <= 256 || (few && d <= 4096)) return norm_with<T, W, 1, MODE>(p, s);
   if (W && !few && d > 512 && d <= 8192) {
     const Flow f = flow_of(threads_of(d, 2), ahead_registers(MODE), 2 * sizeof(T) * d * (MODE != kCodes && p.residual.p ? 2 : 1));
-    if (f.shared <= 200 * 1024) return norm_ahead<T, MODE>(p, sms, f, s);
+    if (f.shared <= kMostShared) return norm_ahead<T, MODE>(p, sms, f, s);
   }
   if (d <= 512 || ((few || !W) && d <= 8192)) return norm_with<T, W, 2, MODE>(p, s);
   return norm_with<T, W, 4, MODE>(p, s);
@@ -812,7 +809,7 @@ template <typename T, bool W, int WAY>
 cudaError_t norm_gradient_with(const NormGradientParams& p, const Flow& f, cudaStream_t s) {
   const int G = threads_of(p.dim, 2);
   const size_t shared = WAY == kDirect ? 0 : f.shared;
-  const cudaError_t e = allow_shared(norm_gradient_kernel<T, W, WAY>, shared);
+  const cudaError_t e = WAY == kDirect ? cudaSuccess : allow_shared<norm_gradient_kernel<T, W, WAY>>(kMostShared);
   if (e != cudaSuccess) return e;
   return launch_early(norm_gradient_kernel<T, W, WAY>, p.blocks, G, shared, s, p, G, f.deep);
 }
@@ -825,7 +822,7 @@ cudaError_t norm_gradient_by(const NormGradientParams& p, cudaStream_t s) {
   if (p.dim <= kShort / 2) e = launch_early(norm_gradient_short_kernel<T, W, 1>, p.blocks, kShortBlock, 0, s, p, lanes_of(p.dim, 1, W));
   else if (p.dim <= kShort) e = launch_early(norm_gradient_short_kernel<T, W, 2>, p.blocks, kShortBlock, 0, s, p, lanes_of(p.dim, 2, W));
   else if (p.dim > 8192) e = norm_gradient_with<T, W, kShared>(p, f, s);
-  else if (W && f.shared <= 200 * 1024) e = norm_gradient_with<T, W, W ? kAhead : kDirect>(p, f, s);
+  else if (W && f.shared <= kMostShared) e = norm_gradient_with<T, W, W ? kAhead : kDirect>(p, f, s);
   else e = norm_gradient_with<T, W, kDirect>(p, f, s);
   if (e != cudaSuccess) return e;
   return launch_early(add_parts_kernel, (columns + 31) / 32, 32 * kSumRows, 0, s, p, columns);

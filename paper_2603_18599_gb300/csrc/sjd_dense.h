@@ -2,6 +2,7 @@
 // kernels (sjd_dense.cu, sjd_product.cu) and their launch entry points.
 #pragma once
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 
@@ -103,6 +104,21 @@ struct ProductParams {
   Rows y;
   int rows;
 };
+
+// Lets a kernel's launches on the current device take up to `most` bytes of dynamic shared
+// memory, whatever one of them asks for. The limit is the kernel's on the device, not the call's:
+// were it set to what each call needs, another host thread could lower it between a call's setting and
+// its launch. So it is the same for all calls of a kernel, and set once a device (it costs as much as a launch).
+template <auto Kernel>
+cudaError_t allow_shared(int most) {
+  static std::atomic<uint64_t> allowed{0};
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess || (device < 64 && (allowed.load(std::memory_order_acquire) >> device & 1))) return e;
+  e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+  if (e == cudaSuccess && device < 64) allowed.fetch_or(1ull << device, std::memory_order_release);
+  return e;
+}
 
 cudaError_t launch_norm(const NormParams& p, int mode, int dtype, int sms, cudaStream_t s);
 int norm_gradient_blocks(int rows, int dim, int dtype, int sms);

@@ -24,7 +24,6 @@
 // us, 300 MB; a copy of the kernel without conversion and products took 58 where this one took 64.
 
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 
 #include <cuda_fp16.h>
@@ -848,14 +847,7 @@ cudaError_t product_of(const ProductParams& p, const Plan& g, unsigned char* x, 
   constexpr int kShared = kAtRings + kRings;
   static_assert(kShared <= 227 * 1024, "shared memory");
   const int shared = kAtRings + g.codes_ring * kTileBytes + g.x_ring * g.tokens * kTileIn;
-  // (once a device: the call costs as much as a launch)
-  static std::atomic<uint64_t> allowed{0};
-  int device = 0;
-  cudaError_t e = cudaGetDevice(&device);
-  if (e == cudaSuccess && (device >= 64 || !(allowed.load(std::memory_order_relaxed) >> device & 1))) {
-    e = cudaFuncSetAttribute(product_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
-    if (e == cudaSuccess && device < 64) allowed.fetch_or(1ull << device, std::memory_order_relaxed);
-  }
+  cudaError_t e = allow_shared<product_kernel<T>>(kShared);
   if (e == cudaSuccess) e = launch_early(spread_kernel, p.rows, kSpreadBlock, 0, s, p, g, x, squares);
   if (e != cudaSuccess) return e;
   return launch_early(product_kernel<T>, 2 * g.pairs, kThreads, shared, s, p, g);

@@ -3,10 +3,12 @@ workspaces that are written again right before a call, host threads, sizes
 that an int32 does not hold. Values are small integers where sums are
 compared, so that these are exact and equal whatever their order."""
 
+import threading
+
 import pytest
 import torch
 
-from paper_2603_18599_gb300 import dense
+from paper_2603_18599_gb300 import dense, sjd
 
 pytestmark = pytest.mark.gpu
 
@@ -18,6 +20,10 @@ def gen(seed):
     g = torch.Generator(device=DEV)
     g.manual_seed(seed)
     return g
+
+
+def normal(g, *shape):
+    return torch.randn(*shape, device=DEV, generator=g)
 
 
 def whole(g, most, *shape):
@@ -60,3 +66,54 @@ def test_a_tables_gradient_reads_what_was_written_right_before(t, v, d, dtype):
         out += [x.clone() for x in captured]
     for i, x in enumerate(out):
         assert torch.equal(x, sets[i % 3][2]), i
+
+
+def test_host_threads_at_once():
+    """Host threads whose calls of many rows take kernels of one kind with
+    different amounts of shared memory, each on a stream of its own: every call
+    is taken, and gives what it gives alone."""
+    L, rows, turns = dense.load(), 400, 4000
+    g = gen(11)
+
+    def calls(d):
+        """Calls at the C boundary, and their outputs: a loop over them is as dense as a host thread's can be."""
+        x, y, dx = normal(g, rows, d).bfloat16(), torch.empty(rows, d, dtype=BF16, device=DEV), torch.empty(rows, d, dtype=BF16, device=DEV)
+        codes, scale, dgain = torch.empty(rows, d, dtype=torch.int8, device=DEV), torch.empty(rows, device=DEV), torch.empty(d, device=DEV)
+        size = L.sjd_norm_gradient_workspace_size(rows, d, sjd.SJD_BF16)
+        room = torch.empty(size, dtype=torch.uint8, device=DEV)
+        at = [dense._pack(t) for t in (x, y, dx)]
+        some = [(L.sjd_norm_gradient, at[0], at[0], None, 1e-6, 0, None, rows, d, sjd.SJD_BF16, at[2], dgain.data_ptr(), None, room.data_ptr(), size)]
+        if d <= 8192:
+            some += [(L.sjd_norm, at[0], None, None, None, 1e-6, 0, rows, d, sjd.SJD_BF16, None, at[1], None, None),
+                     (L.sjd_quantise, at[0], rows, d, sjd.SJD_BF16, codes.data_ptr(), scale.data_ptr())]
+        return some, (x, room), (y, dx, codes, scale, dgain) if d <= 8192 else (dx, dgain)
+
+    jobs = [calls(d) for d in (8192, 4096, 16384, 9000)]
+    want = []
+    for some, _, out in jobs:
+        for call, *args in some:
+            assert call(*args, None) == sjd.SJD_OK
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in out])
+        for t in out:
+            t.zero_()
+    begin, refused = threading.Barrier(len(jobs)), [0] * len(jobs)
+    streams = [torch.cuda.Stream() for _ in jobs]
+    torch.cuda.synchronize()
+
+    def work(i):
+        raw = streams[i].cuda_stream
+        begin.wait(60)
+        for _ in range(turns):
+            for call, *args in jobs[i][0]:
+                refused[i] += call(*args, raw) != sjd.SJD_OK
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(jobs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not any(refused), refused
+    for (_, _, out), alone in zip(jobs, want):
+        assert all(torch.equal(a, b) for a, b in zip(out, alone))
