@@ -10,7 +10,7 @@ each channel. Argument marshalling only.
     codes, scale, x = dense.norm_codes(y, gain, residual=x)
 
 Rows are the last dimension; the others are tokens, in any number of
-dimensions that can be seen as one. Calls run on the caller's current stream, on
+dimensions that can be seen as one, up to 2^31 - 1 of them. Calls run on the caller's current stream, on
 the device of their tensors, and take the workspace that they need from torch's
 allocator.
 
@@ -33,6 +33,7 @@ from .sjd import SJD_OK, SJDError
 _DTYPES = {torch.float32: sjd.SJD_F32, torch.bfloat16: sjd.SJD_BF16}
 _ROWS = struct.Struct("Qq")         # sjd_rows
 _INF = float("inf")
+_MOST = 2 ** 31 - 1                 # rows, places and ids of a call
 
 _empty_like = torch.empty_like
 
@@ -117,6 +118,12 @@ def _features(dim, most):
         raise ValueError("rows have 1 to %d features" % most)
 
 
+def _count(n, what):
+    """(The library takes an int32: more would arrive as another number.)"""
+    if n > _MOST:
+        raise ValueError("a call has at most 2^31 - 1 %s" % what)
+
+
 def _tokens(tokens, device):
     if tokens.dtype != torch.int32 or tokens.device != device or not tokens.is_contiguous():
         raise ValueError("tokens must be a contiguous int32 tensor on %s" % (device,))
@@ -155,7 +162,7 @@ class Weight:
         self.out, self.dim = weight.shape
         self.device = weight.device
         at = None if scale is None else _vector(scale, "scale", self.out, self.device)
-        size = load().sjd_weight_size(self.out, self.dim)
+        size = load().sjd_weight_size(self.out, self.dim) if max(self.out, self.dim) <= _MOST else 0
         if scale is None or size == 0:
             raise ValueError("a weight has 1 to 2^24 channels of 1 to 65536 features, and a scale for each channel")
         self._packed = torch.empty(size, dtype=torch.uint8, device=self.device)
@@ -192,6 +199,8 @@ def product(codes, scale, weight, bias=None, residual=None, dtype=torch.bfloat16
     if x.shape[1] != weight.dim:
         raise ValueError("codes have %d features, the weight %d" % (x.shape[1], weight.dim))
     rows, out = x.shape[0], weight.out
+    if rows > _MOST:
+        _count(rows, "rows")
     if (scale.shape[0] != rows if scale.dim() == 1 == len(shape) - 1 else scale.shape != shape[:-1]):
         raise ValueError("scale must have the shape %s" % (tuple(shape[:-1]),))
     if scale.dim() != 1 and scale.is_contiguous():
@@ -218,6 +227,7 @@ def quantise(x):
     rows = _rows(x, "x", _DTYPES)
     n, dim = rows.shape
     _features(dim, 16384)
+    _count(n, "rows")
     codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
     scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     if n:
@@ -231,6 +241,8 @@ def _norm(x, gain, bias, residual, eps, centre, coded):
     device, dtype = x.device, x.dtype
     if not 1 <= dim <= 16384:
         _features(dim, 16384)
+    if n > _MOST:
+        _count(n, "rows")
     if not 0.0 <= eps < _INF:
         raise ValueError("eps must be finite and not negative")
     g = None if gain is None else _vector(gain, "gain", dim, device)
@@ -275,6 +287,7 @@ def norm_gradient(dy, x, gain=None, eps=1e-6, centre=False, dh=None, bias=False)
     n, dim = rows.shape
     device, dtype = x.device, x.dtype
     _features(dim, 16384)
+    _count(n, "rows")
     if not 0.0 <= eps < float("inf"):
         raise ValueError("eps must be finite and not negative")
     d = _same(dy, "dy", x)
@@ -306,6 +319,8 @@ def embed(table, tokens, scale=1.0, dtype=None):
     _features(dim, 65536)
     if vocab < 1:
         raise ValueError("the table has no rows")
+    _count(vocab, "ids")
+    _count(tokens.numel(), "tokens")
     at = _tokens(tokens, table.device)
     y = torch.empty((*tokens.shape, dim), dtype=dtype, device=table.device)
     if tokens.numel():
@@ -322,6 +337,8 @@ def embed_gradient(dy, tokens, vocab, scale=1.0):
     _features(dim, 65536)
     if vocab < 1:
         raise ValueError("the table has no rows")
+    _count(vocab, "ids")
+    _count(n, "rows")
     if tokens.shape != dy.shape[:-1]:
         raise ValueError("tokens must have the shape %s" % (tuple(dy.shape[:-1]),))
     at = _tokens(tokens, dy.device)

@@ -117,3 +117,43 @@ def test_host_threads_at_once():
     assert not any(refused), refused
     for (_, _, out), alone in zip(jobs, want):
         assert all(torch.equal(a, b) for a, b in zip(out, alone))
+
+
+def test_sizes_that_an_int32_does_not_hold_are_refused():
+    """2^32 + 5 of anything would arrive as 5."""
+    n = 2 ** 32 + 5
+    row, code, vector = torch.ones(1, 1, device=DEV), torch.ones(1, 1, dtype=torch.int8, device=DEV), torch.ones(1, device=DEV)
+    weight, few = dense.Weight(code, vector), torch.zeros(3, dtype=torch.int32, device=DEV)
+    many, ids = row.expand(n, 1), torch.empty(n, dtype=torch.int32, device=DEV)
+    scale = ids.view(F32)
+    calls = {
+        "quantise": lambda: dense.quantise(many), "norm": lambda: dense.norm(many), "norm_codes": lambda: dense.norm_codes(many),
+        "norm_gradient": lambda: dense.norm_gradient(many, many), "product": lambda: dense.product(code.expand(n, 1), scale, weight),
+        "channels": lambda: dense.Weight(code.expand(n, 1), scale), "features": lambda: dense.Weight(torch.empty(1, n, dtype=torch.int8, device=DEV), vector),
+        "table": lambda: dense.embed(many, few), "tokens": lambda: dense.embed(row, ids), "rows": lambda: dense.embed_gradient(many, ids, 3),
+        "vocabulary": lambda: dense.embed_gradient(row.expand(3, 1), few, n),
+    }
+    taken = []
+    for name, call in calls.items():
+        try:
+            call()
+            taken.append(name)
+        except ValueError:
+            pass
+    assert not taken
+
+
+def test_the_largest_numbers_of_rows_and_ids():
+    n = 2 ** 31 - 1
+    x = torch.full((1, 1), -3.0, device=DEV)
+    codes, scale = dense.quantise(x.expand(n, 1))
+    assert codes.shape == (n, 1) and bool((codes.view(-1)[::4097] == -127).all()) and bool((scale[::4097] == scale[0]).all())
+    assert codes[-1] == -127 and scale[-1] == scale[0]
+    del codes, scale
+    # ids at both ends, some of them in many rows
+    ids = torch.tensor([0, n - 1, n - 2, 1] * 10 + [n - 1] * 60 + [-1, n], dtype=torch.int32, device=DEV)
+    rows = torch.arange(ids.numel(), device=DEV, dtype=F32)[:, None].contiguous()
+    grad = dense.embed_gradient(rows, ids, n)
+    for v in (0, 1, n - 2, n - 1):
+        assert grad[v] == rows[ids == v].sum(), v
+    assert torch.count_nonzero(grad) == 4
