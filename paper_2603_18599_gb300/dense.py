@@ -15,8 +15,8 @@ the device of their tensors, and take the workspace that they need from torch's
 allocator.
 
 No call records a gradient. A tensor that wants one is refused, unless
-gradients are off (torch.no_grad); norm_gradient and embed_gradient are the
-gradients.
+gradients are off (torch.no_grad), and so is one with a tangent of forward mode;
+norm_gradient and embed_gradient are the gradients.
 """
 
 import ctypes
@@ -25,6 +25,7 @@ import struct
 from ctypes import c_float, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
+from torch.autograd import forward_ad
 
 from . import sjd
 from .kv import _current_device, _raw_stream
@@ -68,16 +69,23 @@ def load():
 def _no_gradient(x, name):
     if x.requires_grad and torch.is_grad_enabled():
         raise ValueError("%s wants a gradient, and no call here records one: detach it, or call under torch.no_grad()" % name)
+    if forward_ad.unpack_dual(x).tangent is not None:
+        raise ValueError("%s has a forward-mode tangent, and no call here takes it on: detach it" % name)
+
+
+def _plain(x):
+    """Whether x has nothing to do with gradients. (Outside of forward mode, which is asked for first: tensors have no tangents there.)"""
+    return forward_ad._current_level < 0 and not x.requires_grad
 
 
 def _rows(x, name, dtypes, device=None):
     """x as [rows, features], its last dimension dense."""
     # (most often all is as it should be: calls are short, and what the host does for one counts)
-    if x.dim() == 2 and x.dtype in dtypes and x.is_cuda and (device is None or x.device == device) and not x.requires_grad and x.stride(1) == 1:
+    if x.dim() == 2 and x.dtype in dtypes and x.is_cuda and (device is None or x.device == device) and x.stride(1) == 1 and _plain(x):
         return x
     if x.dtype not in dtypes or not x.is_cuda or (device is not None and x.device != device) or x.dim() < 1:
         raise ValueError("%s must be a tensor of %s on %s" % (name, " or ".join(str(d) for d in dtypes), device or "a GPU"))
-    if x.requires_grad:
+    if not _plain(x):
         _no_gradient(x, name)
     if x.dim() != 2:
         try:
@@ -99,7 +107,7 @@ def _same(x, name, like):
 def _vector(x, name, n, device):
     if x.dtype != torch.float32 or x.dim() != 1 or x.shape[0] != n or x.device != device or not x.is_contiguous():
         raise ValueError("%s must be a contiguous float32 tensor of shape (%d,) on %s" % (name, n, device))
-    if x.requires_grad:
+    if not _plain(x):
         _no_gradient(x, name)
     return x.data_ptr()
 

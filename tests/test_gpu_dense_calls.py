@@ -7,6 +7,7 @@ import threading
 
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 from paper_2603_18599_gb300 import dense, sjd
 
@@ -157,3 +158,20 @@ def test_the_largest_numbers_of_rows_and_ids():
     for v in (0, 1, n - 2, n - 1):
         assert grad[v] == rows[ids == v].sum(), v
     assert torch.count_nonzero(grad) == 4
+
+
+def test_tangents_of_forward_mode_are_refused():
+    x, w = torch.ones(4, 64, device=DEV), torch.ones(64, device=DEV)
+    ids, codes = torch.zeros(4, dtype=torch.int32, device=DEV), torch.ones(4, 64, dtype=torch.int8, device=DEV)
+    weight = dense.Weight(codes, w[:4].contiguous())
+    with forward_ad.dual_level():
+        d, dw, ds = (forward_ad.make_dual(t, torch.ones_like(t)) for t in (x, w, w[:4].contiguous()))
+        for call in (lambda: dense.quantise(d), lambda: dense.norm(d), lambda: dense.norm(x, dw), lambda: dense.norm(x, w, dw), lambda: dense.norm(x, residual=d),
+                     lambda: dense.norm_codes(d[None]), lambda: dense.norm_gradient(d, x), lambda: dense.norm_gradient(x, d), lambda: dense.norm_gradient(x, x, dh=d),
+                     lambda: dense.embed(d, ids), lambda: dense.embed_gradient(d, ids, 3), lambda: dense.product(codes, ds, weight),
+                     lambda: dense.product(codes, w[:4], weight, bias=ds), lambda: dense.product(codes, w[:4], weight, residual=d[:, :4], dtype=F32),
+                     lambda: dense.Weight(codes, ds), lambda: dense.Weight.quantise(d)):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+        assert torch.equal(dense.norm(d.detach(), w), dense.norm(x, w))
+    assert torch.equal(dense.norm(x, w), dense.norm(x))
