@@ -584,7 +584,11 @@ void sjd_kv_destroy(sjd_kv* kv);
  * (gains, biases, scales) are contiguous fp32. dtype is SJD_F32 or
  * SJD_BF16 throughout, sums are fp32, and a result is rounded once, to nearest
  * even. Outputs do not overlap inputs. The same inputs give the same bits.
- * Errors: SJD_ERR_ARG, SJD_ERR_CUDA, SJD_ERR_CAPACITY (workspace too small). */
+ * Errors: SJD_ERR_ARG, SJD_ERR_CUDA, SJD_ERR_CAPACITY (workspace too small); what
+ * sjd_product finds on the device is latched in the packed weight: SJD_ERR_TIMEOUT and, in the
+ * bounds-checked build, SJD_ERR_BOUNDS. (The other calls have no handle to latch
+ * that in: sjd_embed_gradient only clamps; the rest compute their indexes, but for
+ * sjd_embed's tokens, which every build tests.) */
 
 typedef struct {
   void* data_dev;
@@ -649,14 +653,14 @@ int sjd_weight_pack(const int8_t* w_dev, int64_t row_stride, const float* scale_
  * row's result does not depend on the call's other rows. A call of a few rows
  * needs no workspace (a size of 0, which invalid sizes have too): it may be NULL
  * then. Should a wait inside the kernel run out, SJD_ERR_TIMEOUT is latched in the
- * packed weight (the results are then not valid). */
+ * packed weight (the results are then not valid; nothing else tells). */
 size_t sjd_product_workspace_size(int32_t rows, int32_t out, int32_t in);
 int sjd_product(const void* packed_dev, int32_t out, int32_t in, const sjd_rows* codes, const float* scale_dev,
                 int32_t rows, const float* bias_dev, const sjd_rows* residual, int32_t dtype, const sjd_rows* y,
                 void* workspace_dev, size_t ws_bytes, void* cuda_stream);
 
 /* Synchronise the stream, then return and clear the weight's device-side
- * error (SJD_OK if none). */
+ * error (SJD_ERR_TIMEOUT, SJD_ERR_BOUNDS; SJD_OK if none). */
 int sjd_weight_sync(void* packed_dev, void* cuda_stream);
 
 #ifdef __cplusplus

@@ -22,6 +22,9 @@
 
 namespace sjd_dense_ops {
 
+#ifdef SJD_CHECKS
+using sjd_kv_ops::checked_index;
+#endif
 using sjd_kv_ops::add2;
 using sjd_kv_ops::fma2;
 using sjd_kv_ops::halves;
@@ -955,7 +958,7 @@ __global__ void __launch_bounds__(32 * kIndexWarps) index_kernel(const EmbedGrad
       if (!which) continue;
       if (mine) {
         const unsigned same = __match_any_sync(which, id);
-        p.places[at[warp][id] + __popc(same & ((1u << lane) - 1))] = static_cast<int>(t0 + 32 * i + lane);
+        p.places[SJD_KV_IDX(nullptr, at[warp][id] + __popc(same & ((1u << lane) - 1)), p.rows)] = static_cast<int>(t0 + 32 * i + lane);
         __syncwarp(which);
         if (lane == 31 - __clz(same)) at[warp][id] += __popc(same);
       }
@@ -964,10 +967,9 @@ __global__ void __launch_bounds__(32 * kIndexWarps) index_kernel(const EmbedGrad
   }
 }
 
-// (The bounds-checked build tests the rows of the index, and takes the nearest one.)
+// (The bounds-checked build tests the index's places, rows and ids, and takes the nearest one.)
 template <typename T>
 __device__ __forceinline__ const T* row_of(const EmbedGradientParams& p, int row) {
-  using namespace sjd_kv_ops;
   return static_cast<const T*>(p.dy.p) + SJD_KV_IDX(nullptr, row, p.rows) * p.dy.stride;
 }
 template <bool W, typename T>
@@ -1008,7 +1010,7 @@ __global__ void __launch_bounds__(kSumBlock, 2) embed_gradient_many_kernel(const
   auto column = [&](int c) { return slice * kSumColumns + (c * 32 + lane) * V; };
   auto add_rows = [&](int begin, int end, float (&sum)[kPieces][V]) {
     for (int r0 = begin; r0 < end; r0 += 32) {
-      const int place = r0 + lane < end ? p.places[r0 + lane] : 0, rows = min(32, end - r0);
+      const int place = r0 + lane < end ? p.places[SJD_KV_IDX(nullptr, r0 + lane, p.rows)] : 0, rows = min(32, end - r0);
       for (int r = 0; r < rows; r += kDeep) {
         float x[kDeep][kPieces][V] = {};
 #pragma unroll
@@ -1041,7 +1043,7 @@ __global__ void __launch_bounds__(kSumBlock, 2) embed_gradient_many_kernel(const
         if (id.z > kMost) continue;
         float sum[kPieces][V] = {};
         add_rows(id.y, id.y + id.z, sum);
-        float* out = p.grad + static_cast<long long>(id.x) * D;
+        float* out = p.grad + static_cast<long long>(SJD_KV_IDX(nullptr, id.x, p.vocab)) * D;
 #pragma unroll
         for (int c = 0; c < kPieces; ++c) {
 #pragma unroll
@@ -1069,7 +1071,7 @@ __global__ void __launch_bounds__(kSumBlock, 2) embed_gradient_many_kernel(const
           for (int i = threadIdx.x; i < kSumColumns; i += kSumBlock) {
             float all = 0.0f;
             for (int w = 0; w < kWarps; ++w) all += sums[w][i];
-            if (slice * kSumColumns + i < D) p.grad[static_cast<long long>(id.x) * D + slice * kSumColumns + i] = all * p.scale;
+            if (slice * kSumColumns + i < D) p.grad[static_cast<long long>(SJD_KV_IDX(nullptr, id.x, p.vocab)) * D + slice * kSumColumns + i] = all * p.scale;
           }
           __syncthreads();
         }
@@ -1107,20 +1109,20 @@ __global__ void __launch_bounds__(kSumBlock, 8) embed_gradient_kernel(const Embe
   __syncthreads();
   const int base = first[0], lane = threadIdx.x & (lanes - 1);
   if (first[here] > base) {
-    for (int i = threadIdx.x; i < min(kPlaces, first[here] - base); i += kSumBlock) places[i] = __ldcg(p.places + base + i);
+    for (int i = threadIdx.x; i < min(kPlaces, first[here] - base); i += kSumBlock) places[i] = __ldcg(p.places + SJD_KV_IDX(nullptr, base + i, p.rows));
     __syncthreads();
   }
   // `lanes` threads (a power of two) to an id
   for (int k = threadIdx.x / lanes; k < here; k += kSumBlock / lanes) {
     const int from = first[k] - base, count = first[k + 1] - base - from;
     if (count > p.few) continue;
-    float* out = p.grad + (static_cast<long long>(v0) + k) * D;
+    float* out = p.grad + SJD_KV_IDX(nullptr, static_cast<long long>(v0) + k, p.vocab) * D;
     for (int column = lane * V; column < D; column += lanes * V) {
       float sum[V] = {};
       for (int r = 0; r < count; ++r) {
         const int at = from + r;
         float x[V];
-        load_columns_l2<W>(row_of<T>(p, at < kPlaces ? places[at] : __ldcg(p.places + base + at)) + column, x);
+        load_columns_l2<W>(row_of<T>(p, at < kPlaces ? places[at] : __ldcg(p.places + SJD_KV_IDX(nullptr, base + at, p.rows))) + column, x);
 #pragma unroll
         for (int j = 0; j < V; ++j) sum[j] += x[j];
       }

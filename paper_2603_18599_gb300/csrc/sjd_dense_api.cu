@@ -54,7 +54,8 @@ int sjd_weight_sync(void* packed, void* stream) {
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   }
   if (e != cudaSuccess) return SJD_ERR_CUDA;
-  return bits ? SJD_ERR_TIMEOUT : SJD_OK;
+  if (bits & sjd_kv_ops::status_bit(SJD_ERR_TIMEOUT)) return SJD_ERR_TIMEOUT;
+  return bits ? SJD_ERR_BOUNDS : SJD_OK;
 }
 
 size_t sjd_product_workspace_size(int32_t rows, int32_t out, int32_t in) {

@@ -19,8 +19,8 @@ __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontr
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // Bounds-checked build (compiled with SJD_CHECKS): an index of a page table, of
-// the cache's vectors, of the rotary axes, of the rows of a call and of the parts that blocks
-// leave for one another is tested against its array's length; one outside latches
+// the cache's vectors, of the rotary axes, of the rows of a call, of a product's tiles and of the parts and
+// counters that blocks leave for one another is tested against its array's length; one outside latches
 // SJD_ERR_BOUNDS in the status word (where there is one) and is clamped. Without
 // SJD_CHECKS the macro is the index itself.
 #ifdef SJD_CHECKS

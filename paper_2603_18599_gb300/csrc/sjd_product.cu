@@ -116,6 +116,16 @@ __device__ __forceinline__ int share_of(const Plan& g, int unit) {
   return unit < of_longer ? unit / (g.share + 1) : g.longer + (unit - of_longer) / g.share;
 }
 
+// What the bounds-checked build latches an index outside its array in (SJD_KV_IDX).
+[[maybe_unused]] __device__ __forceinline__ uint32_t* status_of(const ProductParams& p) { return &p.w.header->status; }
+// Part `slot` of what block `rank` of pair `of` may leave, and the counter of a shared tile.
+__device__ __forceinline__ int32_t* slot_at(const ProductParams& p, const Plan& g, int of, int rank, int slot, long long slot_size) {
+  return g.slots + SJD_KV_IDX(status_of(p), (2ll * of + rank) * g.block_slots + slot, 2ll * g.pairs * g.block_slots) * slot_size;
+}
+__device__ __forceinline__ int32_t* counter_at(const ProductParams& p, const Plan& g, int tile, int rank) {
+  return g.counters + SJD_KV_IDX(status_of(p), 2 * (tile - g.whole) + rank, 4 * kMaxPairs);
+}
+
 // One piece of work: feature tiles k0 .. k1 - 1 of a tile.
 struct Piece {
   int tile, channel, token, k0, k1;   // (channel, token: numbers of tiles)
@@ -424,7 +434,7 @@ __device__ __forceinline__ void join(const ProductParams& p, const Plan& g, cons
 #pragma unroll 2
     for (int other = first; other < after; ++other) {
       const int slot = share_begin(g, other) >= begin ? 0 : 1;
-      const int32_t* from = g.slots + ((2ll * other + rank) * g.block_slots + slot) * slot_size + 4 * lane;
+      const int32_t* from = slot_at(p, g, other, rank, slot, slot_size) + 4 * lane;
       int4 v[kDeep];
 #pragma unroll
       for (int j = 0; j < kDeep; ++j) v[j] = __ldcg(reinterpret_cast<const int4*>(from + min(c0 + 8 * j, tokens - 1) * kTileOut));
@@ -478,7 +488,7 @@ __device__ __forceinline__ void results(const ProductParams& p, Misc* m, const P
   const int lane = threadIdx.x & 31, row = (warp & 3) * 32 + lane;
   const uint32_t empty0 = cluster_addr(smem_addr(&m->sum_empty[0]), 0), sums_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
   const long long slot_size = static_cast<long long>(g.sum_columns) * kTileOut;
-  auto slot_of = [&](int of, int slot) { return g.slots + ((2ll * of + rank) * g.block_slots + slot) * slot_size; };
+  auto slot_of = [&](int of, int slot) { return slot_at(p, g, of, rank, slot, slot_size); };
   int shared = 0;
   Ring d, r;
   Walk walk(g, pair);
@@ -491,7 +501,6 @@ __device__ __forceinline__ void results(const ProductParams& p, Misc* m, const P
     const float scale = __ldg(p.w.scale + n), bias = p.bias && n < p.w.out ? __ldg(p.bias + n) : -0.0f;
     int first = 0, after = 0;   // the pairs with a part in the tile
     if (!whole) first = share_of(g, begin), after = share_of(g, begin + g.per_tile - 1) + 1;
-    int32_t* const counter = &g.counters[2 * (q.tile - g.whole) + rank];
     bool leave = false;
     wait(m, &m->ready_full[r.i], r.phase);
     const Ready& ready = m->ready[r.i];
@@ -502,14 +511,14 @@ __device__ __forceinline__ void results(const ProductParams& p, Misc* m, const P
       tc_fence_after();
       __syncwarp();
       if (!whole && last) {
-        if (warp == 0 && lane == 0) m->others[shared & 1] = counted(counter) == after - first - 1;
+        if (warp == 0 && lane == 0) m->others[shared & 1] = counted(counter_at(p, g, q.tile, rank)) == after - first - 1;
         named_barrier(1, 256);
         leave = *const_cast<volatile int*>(&m->others[shared & 1]) == 0;
         ++shared;
       }
       // (the sum of the parts so far; what is left for the pair that joins the tile)
-      int32_t* const sum = slot_of(pair, g.sum_slot) + row;
-      int32_t* const to = last ? slot_of(pair, share_begin(g, pair) >= begin ? 0 : 1) + row : sum;
+      int32_t* const sum = turns > 1 ? slot_of(pair, g.sum_slot) + row : nullptr;
+      int32_t* const to = !last ? sum : leave ? slot_of(pair, share_begin(g, pair) >= begin ? 0 : 1) + row : nullptr;
       const int c0 = warp / 4 * kColumns;
       uint32_t u[kColumns];
       if (c0 < g.tokens) tmem_load16(sums_at + d.i * g.sum_columns + c0, u);
@@ -555,7 +564,7 @@ __device__ __forceinline__ void results(const ProductParams& p, Misc* m, const P
     }
     if (leave) {
       named_barrier(1, 256);
-      if (warp == 0 && lane == 0) m->last = count_one(counter) == after - first - 1;
+      if (warp == 0 && lane == 0) m->last = count_one(counter_at(p, g, q.tile, rank)) == after - first - 1;
       named_barrier(1, 256);
       if (*const_cast<volatile int*>(&m->last)) join<T>(p, g, ready.scale, begin, first, after, rank, n0, t0, tokens, warp, slot_size);
     }
@@ -597,7 +606,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   if (warp == 0) {
     if (elect_lane()) {
       copy_tiles(m, g, pair, smem, g.codes_ring, kTileBytes, m->codes_full, m->codes_empty, [&](const Piece& q) {
-        return p.w.codes + static_cast<long long>(q.channel * 2 + rank) * p.w.tiles_in * kTileBytes;
+        return p.w.codes + static_cast<long long>(SJD_KV_IDX(status_of(p), q.channel * 2 + rank, p.w.tiles_out)) * p.w.tiles_in * kTileBytes;
       });
     }
     __syncwarp();
@@ -605,7 +614,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     const uint32_t bytes = static_cast<uint32_t>(g.tokens) * kTileIn;
     if (elect_lane()) {
       copy_tiles(m, g, pair, x_at, g.x_ring, bytes, m->x_full, m->x_empty,
-                 [&](const Piece& q) { return g.x + static_cast<long long>(q.token * 2 + rank) * g.per_tile * bytes; });
+                 [&](const Piece& q) { return g.x + static_cast<long long>(SJD_KV_IDX(status_of(p), q.token * 2 + rank, 2ll * g.token_tiles)) * g.per_tile * bytes; });
     }
     __syncwarp();
   } else if (warp == 2) {
@@ -647,7 +656,7 @@ __global__ void __launch_bounds__(kSpreadBlock, 16) spread_kernel(const ProductP
     for (int i = threadIdx.x; i < 4 * kMaxPairs; i += kSpreadBlock) g.counters[i] = 0;
   }
   const int8_t* from = p.codes + t * p.codes_stride;
-  const int tile = t / g.tokens, r = t - tile * g.tokens, of_half = r / half, row = r - of_half * half;
+  const int tile = static_cast<int>(SJD_KV_IDX(status_of(p), t / g.tokens, g.token_tiles)), r = t - tile * g.tokens, of_half = r / half, row = r - of_half * half;
   unsigned char* to = x + static_cast<long long>(tile * 2 + of_half) * g.per_tile * half * 128 + row * 128;
   uint32_t sum = 0;
 #pragma unroll 2

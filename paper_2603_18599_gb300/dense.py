@@ -191,7 +191,8 @@ class Weight:
 
     def sync(self):
         """Returns the device-side status code of the products with this weight
-        on the current stream (0 = OK) and clears it."""
+        on the current stream (0 = OK; SJD_ERR_TIMEOUT or, from the
+        bounds-checked build, SJD_ERR_BOUNDS: results are not valid) and clears it."""
         with torch.cuda.device(self.device):
             return int(load().sjd_weight_sync(self._at, _raw_stream(self.device.index)))
 

@@ -168,7 +168,7 @@ def main():
     if model.cache.sync() != sjd.SJD_OK:
         raise SystemExit("cache: " + model.cache.last_error())
     if model.packed and any(w.sync() != sjd.SJD_OK for w in (model.packed_head, *(w for layer in model.packed for w in layer.values()))):
-        raise SystemExit("a product's wait ran out")
+        raise SystemExit("a product's results are not valid")
     print("%d images of %d tokens: %d steps, %.2f tokens accepted per step, %.2f ms per step, %s cache, %s weights" % (
         B, tokens.shape[1], steps, B * tokens.shape[1] / (B * steps), seconds / steps * 1e3, args.cache, args.weights))
 
