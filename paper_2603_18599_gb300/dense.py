@@ -25,7 +25,7 @@ import struct
 from ctypes import c_float, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
-from torch.autograd import forward_ad
+from torch.autograd import forward_ad as _forward
 
 from . import sjd
 from .kv import _current_device, _raw_stream
@@ -69,23 +69,18 @@ def load():
 def _no_gradient(x, name):
     if x.requires_grad and torch.is_grad_enabled():
         raise ValueError("%s wants a gradient, and no call here records one: detach it, or call under torch.no_grad()" % name)
-    if forward_ad.unpack_dual(x).tangent is not None:
+    if _forward.unpack_dual(x).tangent is not None:
         raise ValueError("%s has a forward-mode tangent, and no call here takes it on: detach it" % name)
-
-
-def _plain(x):
-    """Whether x has nothing to do with gradients. (Outside of forward mode, which is asked for first: tensors have no tangents there.)"""
-    return forward_ad._current_level < 0 and not x.requires_grad
 
 
 def _rows(x, name, dtypes, device=None):
     """x as [rows, features], its last dimension dense."""
     # (most often all is as it should be: calls are short, and what the host does for one counts)
-    if x.dim() == 2 and x.dtype in dtypes and x.is_cuda and (device is None or x.device == device) and x.stride(1) == 1 and _plain(x):
+    if x.dim() == 2 and x.dtype in dtypes and x.is_cuda and (device is None or x.device == device) and x.stride(1) == 1 and not x.requires_grad and _forward._current_level < 0:
         return x
     if x.dtype not in dtypes or not x.is_cuda or (device is not None and x.device != device) or x.dim() < 1:
         raise ValueError("%s must be a tensor of %s on %s" % (name, " or ".join(str(d) for d in dtypes), device or "a GPU"))
-    if not _plain(x):
+    if x.requires_grad or _forward._current_level >= 0:   # (no tensor has a tangent outside of forward mode)
         _no_gradient(x, name)
     if x.dim() != 2:
         try:
@@ -107,7 +102,7 @@ def _same(x, name, like):
 def _vector(x, name, n, device):
     if x.dtype != torch.float32 or x.dim() != 1 or x.shape[0] != n or x.device != device or not x.is_contiguous():
         raise ValueError("%s must be a contiguous float32 tensor of shape (%d,) on %s" % (name, n, device))
-    if not _plain(x):
+    if x.requires_grad or _forward._current_level >= 0:   # (no tensor has a tangent outside of forward mode)
         _no_gradient(x, name)
     return x.data_ptr()
 
@@ -235,12 +230,15 @@ def quantise(x):
     """sjd_quantise: (codes int8 of x's shape, scale float32 of its rows)."""
     rows = _rows(x, "x", _DTYPES)
     n, dim = rows.shape
-    _features(dim, 16384)
-    _count(n, "rows")
-    codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
-    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    device = x.device
+    if not 1 <= dim <= 16384:
+        _features(dim, 16384)
+    if n > _MOST:
+        _count(n, "rows")
+    codes = torch.empty(x.shape, dtype=torch.int8, device=device)
+    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=device)
     if n:
-        _run(x.device, "sjd_quantise", _pack(rows), n, dim, _DTYPES[x.dtype], codes.data_ptr(), scale.data_ptr())
+        _run(device, "sjd_quantise", _ROWS.pack(rows.data_ptr(), rows.stride(0)), n, dim, _DTYPES[x.dtype], codes.data_ptr(), scale.data_ptr())
     return codes, scale
 
 
@@ -295,8 +293,10 @@ def norm_gradient(dy, x, gain=None, eps=1e-6, centre=False, dh=None, bias=False)
     rows = _rows(x, "x", _DTYPES)
     n, dim = rows.shape
     device, dtype = x.device, x.dtype
-    _features(dim, 16384)
-    _count(n, "rows")
+    if not 1 <= dim <= 16384:
+        _features(dim, 16384)
+    if n > _MOST:
+        _count(n, "rows")
     if not 0.0 <= eps < float("inf"):
         raise ValueError("eps must be finite and not negative")
     d = _same(dy, "dy", x)
@@ -325,16 +325,17 @@ def embed(table, tokens, scale=1.0, dtype=None):
         raise ValueError("dtype must be bf16 or f32")
     t = _rows(table, "table", _DTYPES)
     vocab, dim = t.shape
-    _features(dim, 65536)
+    if not 1 <= dim <= 65536:
+        _features(dim, 65536)
     if vocab < 1:
         raise ValueError("the table has no rows")
-    _count(vocab, "ids")
-    _count(tokens.numel(), "tokens")
-    at = _tokens(tokens, table.device)
-    y = torch.empty((*tokens.shape, dim), dtype=dtype, device=table.device)
-    if tokens.numel():
-        _run(table.device, "sjd_embed", _pack(t), vocab, _DTYPES[table.dtype], at, tokens.numel(), dim, scale, _DTYPES[dtype],
-             _ROWS.pack(y.data_ptr(), dim))
+    n, device = tokens.numel(), table.device
+    if vocab > _MOST or n > _MOST:
+        _count(max(vocab, n), "tokens and ids")
+    at = _tokens(tokens, device)
+    y = torch.empty((*tokens.shape, dim), dtype=dtype, device=device)
+    if n:
+        _run(device, "sjd_embed", _pack(t), vocab, _DTYPES[table.dtype], at, n, dim, scale, _DTYPES[dtype], _ROWS.pack(y.data_ptr(), dim))
     return y
 
 
@@ -343,11 +344,12 @@ def embed_gradient(dy, tokens, vocab, scale=1.0):
     from dy [..., dim] and the tokens [...]."""
     rows = _rows(dy, "dy", _DTYPES)
     n, dim = rows.shape
-    _features(dim, 65536)
+    if not 1 <= dim <= 65536:
+        _features(dim, 65536)
     if vocab < 1:
         raise ValueError("the table has no rows")
-    _count(vocab, "ids")
-    _count(n, "rows")
+    if vocab > _MOST or n > _MOST:
+        _count(max(vocab, n), "rows and ids")
     if tokens.shape != dy.shape[:-1]:
         raise ValueError("tokens must have the shape %s" % (tuple(dy.shape[:-1]),))
     at = _tokens(tokens, dy.device)
