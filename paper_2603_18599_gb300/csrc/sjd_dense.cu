@@ -40,11 +40,12 @@ using sjd_kv_ops::wait_for_previous;
 namespace {
 
 // (Wide loads behind the row's end take its last piece instead, and `FILL` puts zeros in its
-// place: a select costs less than a branch around the load.)
-template <bool W, bool FILL = true, typename T>
+// place: a select costs less than a branch around the load. `OWN`: the thread's first piece,
+// which every thread has in rows of more than 512 features where it has two.)
+template <bool W, bool FILL = true, bool OWN = false, typename T>
 __device__ __forceinline__ void load8(const T* row, int i, Place at, int D, float (&v)[8]) {
   if constexpr (W) {
-    const int e = feature<true>(i, 0, at), here = min(e, D - 8);
+    const int e = feature<true>(i, 0, at), here = OWN ? (e < D ? e : at.first) : min(e, D - 8);
     if constexpr (sizeof(T) == 2) {
       uint4 u = *reinterpret_cast<const uint4*>(row + here);
       if (FILL) u.x = e < D ? u.x : 0, u.y = e < D ? u.y : 0, u.z = e < D ? u.z : 0, u.w = e < D ? u.w : 0;
@@ -86,12 +87,18 @@ __device__ __forceinline__ void store8(T* row, int i, Place at, int D, const flo
 }
 
 // The same in pairs of neighbours, which are added and multiplied two at a time.
-template <bool W, bool FILL = true, typename T>
+template <bool W, bool FILL = true, bool OWN = false, typename T>
 __device__ __forceinline__ void load8(const T* row, int i, Place at, int D, Pair (&v)[4]) {
   float f[8];
-  load8<W, FILL>(row, i, at, D, f);
+  load8<W, FILL, OWN>(row, i, at, D, f);
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] = pair(f[2 * j], f[2 * j + 1]);
+}
+// Of a row that copy_row brought: the thread's own pieces alone are looked at, as the others'
+// may be on their way.
+template <typename T>
+__device__ __forceinline__ void load_own8(const T* row, int i, Place at, int D, Pair (&v)[4]) {
+  load8<true, true, true>(row, i, at, D, v);
 }
 template <bool W, typename T>
 __device__ __forceinline__ void store8(T* row, int i, Place at, int D, const Pair (&v)[4]) {
@@ -448,8 +455,8 @@ __global__ void __launch_bounds__(512) norm_ahead_kernel(const NormParams p, int
     for (int q = 0; q < R; ++q) {
 #pragma unroll
       for (int i = 0; i < C; ++i) {
-        load8<true>(from + q * row_size, i, at, D, v[q][i]);
-        if (added) load8<true>(from + q * row_size + D, i, at, D, w[q][i]);
+        load_own8(from + q * row_size, i, at, D, v[q][i]);
+        if (added) load_own8(from + q * row_size + D, i, at, D, w[q][i]);
       }
     }
     norm_rows<T, true, C, MODE, R>(p, row, there, lane, G, at, v, w, words, turn, gains);
@@ -723,9 +730,15 @@ __global__ void __launch_bounds__(WAY == kShared ? 1024 : 512) norm_gradient_ker
     Pair x[C][4], dy[C][4], dx[C][4];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      load8<W>(xs, i, at, D, x[i]);
-      load8<W>(dys, i, at, D, dy[i]);
-      if (p.dh.p) load8<W>(dhs, i, at, D, dx[i]);
+      if constexpr (WAY == kAhead) {
+        load_own8(xs, i, at, D, x[i]);
+        load_own8(dys, i, at, D, dy[i]);
+        if (p.dh.p) load_own8(dhs, i, at, D, dx[i]);
+      } else {
+        load8<W>(xs, i, at, D, x[i]);
+        load8<W>(dys, i, at, D, dy[i]);
+        if (p.dh.p) load8<W>(dhs, i, at, D, dx[i]);
+      }
     }
     gradient_row<W, C>(p, G, at, x, dy, dx, words, turn, [&](int i, Pair (&g)[4]) {
       if constexpr (WAY == kShared) {

@@ -35,3 +35,11 @@ def test_every_feature_is_taken_once(tmp_path):
     assert len(got) == len(cases)
     wrong = [(c, n) for c, n in zip(cases, got) if n != (1, 1, 0)]
     assert not wrong, wrong
+
+
+def test_every_thread_has_the_first_of_two_pieces():
+    """Behind a row's end a thread of the kernels for many rows (513 to 8192
+    features, two pieces) looks at its first piece again: every thread has one."""
+    for d in range(520, 8193, 8):
+        threads = -(-(-(-d // 16)) // 32) * 32
+        assert 8 * (threads - 1) < d, d
