@@ -609,8 +609,8 @@ int sjd_quantise(const sjd_rows* x, int32_t rows, int32_t dim, int32_t dtype, in
  * m_t the mean of h[t] with centre != 0 (layer norm), else 0. gain_dev NULL: 1,
  * bias_dev NULL: 0. Either y is written, or (y NULL) codes_dev [rows][dim] and
  * scale_dev [rows], what sjd_quantise makes of y before it is rounded. eps >=
- * 0; a row of zeros with eps 0 is not a number, and rows whose squares pass the
- * fp32 range are 0. dim is at most 16384. */
+ * 0; with eps 0 a row of zeros is not a number and one whose squares vanish in fp32
+ * is not finite; rows whose squares pass the fp32 range are 0. dim is at most 16384. */
 int sjd_norm(const sjd_rows* x, const sjd_rows* residual, const float* gain_dev, const float* bias_dev, float eps,
              int32_t centre, int32_t rows, int32_t dim, int32_t dtype, const sjd_rows* h, const sjd_rows* y,
              int8_t* codes_dev, float* scale_dev, void* cuda_stream);

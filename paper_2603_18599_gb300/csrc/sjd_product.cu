@@ -19,9 +19,10 @@
 // once in bytes, which bounds calls of few tokens, and its conversion, four
 // instructions for four codes, goes on beside the products, which bound those of many. Up to
 // 192 tokens have two accumulators: a tile's results are given while the next one is summed
-// up (8100 tokens x 16384 channels of 4096: 558 to 562 us, 1.94 PFLOP/s, as much as
-// a library product of bf16; 844 with one accumulator of 256 tokens). 128 tokens x 65536 channels, f32: 62
-// us, 300 MB; a copy of the kernel without conversion and products took 58 where this one took 64.
+// up (8100 tokens x 16384 channels of 4096: 551 to 560 us in short runs, 1.97 PFLOP/s, and 614 to 619 in a long
+// loop under the power cap, 1.77: a library product of bf16 reaches 1.90 and 1.71; 844 with one
+// accumulator of 256 tokens). 128 tokens x 65536 channels, f32: 62 us, 300 MB; a copy of the kernel without
+// conversion and products took 58 where this one took 64.
 
 #include <algorithm>
 #include <cmath>
@@ -601,7 +602,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   tc_fence_after();
   const uint32_t tmem = m->tmem;
   // The weight's codes are read at once: the kernel before this one, which spreads
-  // the tokens' codes, has let it in after all before that was done. All else waits for it.
+  // the tokens' codes, has let it in after all before that was done and stood in global
+  // memory, from where (through L2) bulk copies read, past the first-level cache. All else waits for it.
   if (warp != 0) wait_for_previous();
   if (warp == 0) {
     if (elect_lane()) {
@@ -689,7 +691,8 @@ __global__ void __launch_bounds__(kSpreadBlock, 16) spread_kernel(const ProductP
 // every eighth tile of 64 features of them (2 KB side by side), kAhead of them in its
 // registers at a time; a lane reads piece l % 4 of channels l / 4, 8 + l / 4, ... and adds to
 // their sums with all tokens, whose codes lie in shared memory. One
-// token x 65536 channels of 4096: 41 us, 6.5 TB/s; two x 6144: 6.0 us (14.4 the other way).
+// token x 65536 channels of 4096: 41 us, 6.5 TB/s; two x 6144: 6.0 us (14.4 the other way) where the
+// weight's 25 MB are in L2, 7.6 where they come from HBM, as in a step that reads each weight once.
 constexpr int kFewTokens = 8, kFewWarps = 8, kFewChannels = 32;
 
 template <typename T, int N>   // N: at least the call's tokens
@@ -761,7 +764,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, 2) few_kernel(const ProductPar
 
 // Whether a call goes that way: its dot products take as long as the reading from
 // about six tokens on, which large weights feel. (Eight tokens x 4096 channels of
-// 4096: 9.6 us, 14.3 the other way; x 65536 channels 79, and 55.)
+// 4096: 9.6 us, 14.3 the other way, and 12.6 with the weight from HBM; x 65536 channels 79, and 55.)
 bool is_few(int rows, int out, int in) { return rows <= 4 || (rows <= kFewTokens && static_cast<long long>(out) * in <= 1ll << 26); }
 
 template <typename T>
