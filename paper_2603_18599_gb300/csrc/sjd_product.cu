@@ -19,8 +19,8 @@
 // once in bytes, which bounds calls of few tokens, and its conversion, four
 // instructions for four codes, goes on beside the products, which bound those of many. Up to
 // 192 tokens have two accumulators: a tile's results are given while the next one is summed
-// up (8100 tokens x 16384 channels of 4096: 551 to 560 us in short runs, 1.97 PFLOP/s, and 614 to 619 in a long
-// loop under the power cap, 1.77: a library product of bf16 reaches 1.90 and 1.71; 844 with one
+// up (8100 tokens x 16384 channels of 4096: 551 to 560 us in short runs, 1.97 PFLOP/s, and 614 to 629 in a long
+// loop under the power cap, 1.75: a library product of bf16 reaches 1.90 and 1.71; 844 with one
 // accumulator of 256 tokens). 128 tokens x 65536 channels, f32: 62 us, 300 MB; a copy of the kernel without
 // conversion and products took 58 where this one took 64.
 
